@@ -28,36 +28,37 @@ TYPES = {"fp16": torch.float16, "bf16": torch.bfloat16}
 def listed():
     return [
         # the plan of one step of eight requests that each generate a token: the smallest call of a serving loop
-        dict(name="tables step 8", op="tables", req=8, page=16, past=(256, 1024), new=(1, 1), pad=0, mix=1),
+        dict(name="tables step 8", op="tables", req=8, page=16, past_lo=256, past_hi=1024, new_lo=1, new_hi=1, pad=0, mix=1),
         # admission of a large mixed batch: prompts' chunks beside single tokens, a padded row buffer
-        dict(name="tables mixed 1024", op="tables", req=1024, page=16, past=(1, 16384), new=(1, 1024), pad=777, mix=2),
+        dict(name="tables mixed 1024", op="tables", req=1024, page=16, past_lo=1, past_hi=16384, new_lo=1,
+             new_hi=1024, pad=777, mix=2),
         # one generated token per request of workload 3, written into its page (rows of a joint q/k/v projection)
-        dict(name="write step 16", op="write", dtype="fp16", req=16, hkv=8, page=64, past=(4096, 8192), new=(1, 1),
-             heads_first=False, mix=3),
+        dict(name="write step 16", op="write", dtype="fp16", req=16, hkv=8, page=64, past_lo=4096, past_hi=8192,
+             new_lo=1, new_hi=1, heads_first=False, mix=3),
         # the prompts of workload 2, written at once, ragged by a little; pages with the heads outside the tokens
-        dict(name="write prompts 8x4096", op="write", dtype="bf16", req=8, hkv=8, page=64, past=(1, 64), new=(3840, 4096),
-             heads_first=True, mix=4),
+        dict(name="write prompts 8x4096", op="write", dtype="bf16", req=8, hkv=8, page=64, past_lo=1, past_hi=64,
+             new_lo=3840, new_hi=4096, heads_first=True, mix=4),
         # workload 2's finished prompts, from pages to the dense tensors that prefill compression takes
-        dict(name="read prompts 8x4096", op="read", dtype="bf16", req=8, hkv=8, page=16, past=(4096, 4096), new=(0, 0),
-             heads_first=False, mix=5),
+        dict(name="read prompts 8x4096", op="read", dtype="bf16", req=8, hkv=8, page=16, past_lo=4096, past_hi=4096,
+             new_lo=0, new_hi=0, heads_first=False, mix=5),
         # few short requests, one token each: latency
-        dict(name="decode 4x512", op="attend", dtype="bf16", req=4, hq=32, hkv=8, page=16, past=(200, 512), new=(1, 1),
-             window=0, sinks=0, heads_first=False, mix=6),
+        dict(name="decode 4x512", op="attend", dtype="bf16", req=4, hq=32, hkv=8, page=16, past_lo=200, past_hi=512,
+             new_lo=1, new_hi=1, window=0, sinks=0, heads_first=False, mix=6),
         # workload 4's heads (one query head per key head): the most bytes per step
-        dict(name="decode mha 32x4096", op="attend", dtype="fp16", req=32, hq=32, hkv=32, page=64, past=(2048, 4096), new=(1, 1),
-             window=0, sinks=0, heads_first=False, mix=7),
+        dict(name="decode mha 32x4096", op="attend", dtype="fp16", req=32, hq=32, hkv=32, page=64, past_lo=2048,
+             past_hi=4096, new_lo=1, new_hi=1, window=0, sinks=0, heads_first=False, mix=7),
         # a chunk of a long prompt over workload 5's context
-        dict(name="chunk 2048 at 32768", op="attend", dtype="bf16", req=1, hq=32, hkv=8, page=64, past=(30720, 30720),
-             new=(2048, 2048), window=0, sinks=0, heads_first=True, mix=8),
+        dict(name="chunk 2048 at 30000", op="attend", dtype="bf16", req=1, hq=32, hkv=8, page=64, past_lo=30000, past_hi=30000,
+             new_lo=2048, new_hi=2048, window=0, sinks=0, heads_first=True, mix=8),
         # a step that mixes chunks of every length with single tokens, ragged contexts
-        dict(name="chunks mixed 16", op="attend", dtype="fp16", req=16, hq=32, hkv=8, page=16, past=(1, 8192), new=(1, 1024),
-             window=0, sinks=0, heads_first=False, mix=9),
+        dict(name="chunks mixed 16", op="attend", dtype="fp16", req=16, hq=32, hkv=8, page=16, past_lo=1, past_hi=8192,
+             new_lo=1, new_hi=1024, window=0, sinks=0, heads_first=False, mix=9),
         # workload 3 with its model family's window of 4096 and four first tokens kept: single tokens
-        dict(name="window decode 16x8192", op="attend", dtype="fp16", req=16, hq=32, hkv=8, page=64, past=(4100, 8192),
-             new=(1, 1), window=4096, sinks=4, heads_first=False, mix=10),
+        dict(name="window decode 16x8192", op="attend", dtype="fp16", req=16, hq=32, hkv=8, page=64, past_lo=4100, past_hi=8192,
+             new_lo=1, new_hi=1, window=4096, sinks=4, heads_first=False, mix=10),
         # the same window over chunks of long prompts
-        dict(name="window chunks 4x1024", op="attend", dtype="bf16", req=4, hq=32, hkv=8, page=128, past=(0, 28000),
-             new=(700, 1024), window=4096, sinks=4, heads_first=False, mix=11),
+        dict(name="window chunks 4x1024", op="attend", dtype="bf16", req=4, hq=32, hkv=8, page=128, past_lo=0, past_hi=28000,
+             new_lo=700, new_hi=1024, window=4096, sinks=4, heads_first=False, mix=11),
         # a whole prompt of workload 3 in dense tensors, under the same window
         dict(name="window prompt 8192", op="prompt", dtype="fp16", req=1, hq=32, hkv=8, l=8192, window=4096, sinks=4),
     ]
@@ -75,8 +76,8 @@ def draw(rng):
         if op == "tables":
             lo, hi = sorted((_log(rng, 1, 16384), _log(rng, 1, 16384)))
             nlo, nhi = sorted((_log(rng, 1, 1024), _log(rng, 1, 1024)))
-            case = dict(op=op, req=_log(rng, 1, 1024), page=rng.choice([16, 32, 64, 128, 256]), past=(lo, hi), new=(nlo, nhi),
-                        pad=rng.choice([0, 0, 1, 100, 777]), mix=mix)
+            case = dict(op=op, req=_log(rng, 1, 1024), page=rng.choice([16, 32, 64, 128, 256]), past_lo=lo, past_hi=hi,
+                        new_lo=nlo, new_hi=nhi, pad=rng.choice([0, 0, 1, 100, 777]), mix=mix)
             if case["req"] * nhi > 600000:
                 continue
             return case
@@ -87,8 +88,10 @@ def draw(rng):
             req = _log(rng, 1, 64)
             lo, hi = sorted((_log(rng, 1, 8192), _log(rng, 1, 8192)))
             hkv = rng.choice([1, 2, 4, 8, 32])
-            case = dict(op=op, dtype=dtype, req=req, hkv=hkv, page=page, past=(0, 100) if op == "write" else (hi, hi),
-                        new=(lo, hi) if op == "write" else (0, 0), heads_first=heads_first, mix=mix)
+            case = dict(op=op, dtype=dtype, req=req, hkv=hkv, page=page, past_lo=0, past_hi=100, new_lo=lo, new_hi=hi,
+                        heads_first=heads_first, mix=mix)
+            if op == "read":     # dense tensors of one length
+                case.update(past_lo=hi, past_hi=hi, new_lo=0, new_hi=0)
             if req * hi * hkv > 8 * 4096 * 8:
                 continue
             return case
@@ -103,11 +106,12 @@ def draw(rng):
             lo, hi = sorted((_log(rng, 1, 32768), _log(rng, 1, 32768)))
             nlo, nhi = (1, 1) if single else sorted((_log(rng, 1, 2048), _log(rng, 1, 2048)))
             case = dict(op=op, dtype=dtype, req=_log(rng, 1, 64 if single else 16), hq=hkv * group, hkv=hkv, page=page,
-                        past=(lo, hi), new=(nlo, nhi), window=window, sinks=sinks, heads_first=heads_first, mix=mix)
+                        past_lo=lo, past_hi=hi, new_lo=nlo, new_hi=nhi, window=window, sinks=sinks,
+                        heads_first=heads_first, mix=mix)
         # no dearer than the largest listed cases, and no larger a table of logits in the plain form
         w = work(case)
-        n, s = (case["l"], case["l"]) if op == "prompt" else (case["new"][1], case["past"][1] + case["new"][1])
-        if w["flops"] <= 1.0e12 and w["bytes"] <= 1.9e9 and case["req"] * case["hq"] * n * s <= 2.2e9 \
+        n, s = (case["l"], case["l"]) if op == "prompt" else (case["new_hi"], case["past_hi"] + case["new_hi"])
+        if w["flops"] <= 1.0e12 and w["bytes"] <= 1.49e9 and case["req"] * case["hq"] * n * s <= 2.2e9 \
                 and case["req"] * case["hkv"] * s <= 5e6:
             return case
 
@@ -116,8 +120,8 @@ def _lengths(case):
     """Tokens already cached and new tokens of each request: the case's own, whatever the seed."""
     r = random.Random(case["mix"])
     draw_one = lambda lo, hi: lo if lo == hi else _log(r, lo, hi) if hi > 16 * max(1, lo) else r.randint(lo, hi)  # noqa: E731
-    past = [draw_one(*case["past"]) for _ in range(case["req"])]
-    new = [draw_one(*case["new"]) for _ in range(case["req"])]
+    past = [draw_one(case["past_lo"], case["past_hi"]) for _ in range(case["req"])]
+    new = [draw_one(case["new_lo"], case["new_hi"]) for _ in range(case["req"])]
     return past, new
 
 
