@@ -237,7 +237,8 @@ def _handles(st):
     elif case["op"] == "prompt":
         st["cache"] = zc.ZipCache(st["q"].dtype, case["req"], case["hq"], case["hkv"], case["l"], 1, 0.4, device=DEV)
     else:
-        st["pool"] = zc.PagedKV(st["k"], st["v"], case.get("hq", case["hkv"]))
+        st["pool"] = zc.PagedKV(st["k"], st["v"], case.get("hq", case["hkv"]), max_req=case["req"],
+                                max_rows=st["q"].shape[0] if "q" in st else 0)
     if "q" in st:
         st["out"], st["lse"] = torch.empty_like(st["q"]), torch.empty(st["q"].shape[:-1], dtype=torch.float32, device=DEV)
 
