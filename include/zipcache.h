@@ -262,6 +262,108 @@ int zc_export_segment(zc_cache* c, int segment, int tensor, int subset, int32_t*
 int zc_decode_attention_noalloc(zc_cache* c, const void* q, void* out, int is_probe_step,
                                 zc_stream_t stream);
 
+/* ---- full-precision pages ------------------------------------------------------------------
+ * Keys and values of requests whose prompts are not complete yet (or that are never compressed)
+ * live at the input type in pages of `page_size` consecutive tokens of one request, all KV heads.
+ * A request's pages are listed, in token order, in its row of a block table: table [device] n_req x
+ * table_width int32, row-major; token t of request r is row t % page_size of page
+ * table[r][t / page_size].  A slot is page * page_size + row.  The steps of a serving loop:
+ * zc_page_tables (pages and slots for the step's new tokens), zc_page_write (their K / V rows into
+ * the slots), zc_paged_attention (from the new tokens to everything cached), and, when a prompt is
+ * complete, zc_page_read (its rows as the dense tensors zc_prefill_compress takes).
+ * All lengths and tables are read on the device, so that a step can be captured in a CUDA graph
+ * and replayed with other lengths of the same n_req / n_rows.  The calling thread's current device
+ * must be the one that holds the buffers. */
+typedef struct {
+  int32_t struct_size;    /* sizeof(zc_page_config) */
+  int32_t dtype;          /* ZC_F16 | ZC_BF16 */
+  int32_t n_q_heads;      /* h_q, multiple of n_kv_heads, at most 16 per KV head */
+  int32_t n_kv_heads;     /* h_kv */
+  int32_t head_dim;       /* must be 128 */
+  int32_t page_size;      /* tokens per page: 16, 32, 64, 128 or 256 */
+  int32_t n_pages;        /* n_pages * page_size <= 2^31 - 1 */
+  int32_t reserved;       /* 0 */
+  int64_t strides[3];     /* of (page, token, KV head) in ELEMENTS, for both tensors: multiples of 8,
+                             at least 128 where the extent exceeds 1; d contiguous.  Any order of
+                             the three is accepted. */
+} zc_page_config;
+
+typedef struct zc_pages zc_pages; /* small host-side handle */
+
+/* Device scratch [host] that zc_paged_attention needs for calls of up to n_req requests and n_rows rows:
+ * the call's list of work items and the partial results of long rows that several items share.  Its
+ * contents need no initialisation and nothing in it survives a call; it must not be used by calls that
+ * may run at the same time (other streams, graphs replayed side by side). */
+int zc_pages_workspace(const zc_page_config* cfg, int n_req, int n_rows, size_t* workspace_bytes);
+/* Handle over caller-owned pages K, V [device, 16-byte aligned].  No device work is enqueued. */
+int zc_pages_init(void* k_pages, void* v_pages, const zc_page_config* cfg, zc_pages** out);
+void zc_pages_free(zc_pages* p);
+
+/* Block tables and slot maps of one step.  past, fresh [device] n_req int32: tokens request r has
+ * cached, and tokens it adds now (negative values count as 0; sums must stay below 2^31).
+ * free_pages [device] n_free int32: page ids; free_state [device] 3 int32: {next, end, -}: entries
+ * next .. end - 1 of free_pages are free (end is taken as at most n_free).  Requests take pages in
+ * their order: request r the next ceil((past + fresh) / page_size) - ceil(past / page_size) entries,
+ * which are stored into its row of table behind those it holds.  Where the free list runs out, or
+ * the table's row is full, a page is missing: its table entry (if the row has room) becomes -1.
+ * Outputs [device], int32:
+ *   table        in place, new entries only
+ *   kv_len       n_req: past + fresh
+ *   row_start    n_req + 1: prefix sums of fresh: the new tokens of request r are rows row_start[r]
+ *                .. row_start[r + 1] - 1 of the step's row-wise tensors
+ *   slots, pos   n_rows: slot and position of every row; slot -1 for a token whose page is missing;
+ *                both -1 for rows behind the last request's (padding)
+ *   free_out     3: {next + pages taken, end, pages missing}; not the buffer of free_state (ZC_EINVAL)
+ * A step with pages missing must not be carried on with as it is: free pages and build it again. */
+int zc_page_tables(int page_size, int n_req, const int32_t* past, const int32_t* fresh,
+                   const int32_t* free_pages, int n_free, const int32_t* free_state, int32_t* table,
+                   int table_width, int32_t* kv_len, int32_t* row_start, int n_rows, int32_t* slots,
+                   int32_t* pos, int32_t* free_out, zc_stream_t stream);
+
+/* New rows into pages: k_rows, v_rows [device] n_rows x h_kv x d of cfg.dtype, row_strides [host] =
+ * strides of (row, head) in elements (multiples of 8), d contiguous; row i goes to slots[i] [device].
+ * Rows whose slot is negative (or beyond the pages) are skipped.  Two rows with the same slot:
+ * either may win.  n_rows = 0 is a no-op. */
+int zc_page_write(zc_pages* p, const void* k_rows, const void* v_rows, const int64_t row_strides[2],
+                  const int32_t* slots, int n_rows, zc_stream_t stream);
+
+/* Pages to dense tensors: the first l tokens of every request to K, V [device] n_req x h_kv x l x d,
+ * kv_strides [host] = strides of (request, head, token) in elements, as zc_prefill_compress takes
+ * them.  Tokens on pages outside [0, n_pages) come as zeros. */
+int zc_page_read(zc_pages* p, const int32_t* table, int table_width, int n_req, int l, void* K, void* V,
+                 const int64_t kv_strides[3], zc_stream_t stream);
+
+/* Attention from each request's newest tokens to its cached ones (Eq. 2 and Eq. 4 over pages): the
+ * rows row_start[r] .. row_start[r + 1] - 1 of q are the last n_r of the request's kv_len[r] tokens,
+ * whose K / V rows are in the pages already; row i of them, at position p = kv_len[r] - n_r + i, sees
+ * the keys j <= p and, with window > 0, of those only j > p - window and the first `sinks` tokens
+ * (j < sinks).  window = 0: no window.
+ *   q [device] n_rows x h_q x d, q_strides [host] = strides of (row, head) in elements (multiples of
+ *   8); table [device] n_req x table_width; row_start [device] n_req + 1 ascending; kv_len [device]
+ *   n_req; out [device] n_rows x h_q x d, contiguous, cfg.dtype; row_lse [device or NULL] n_rows x h_q
+ *   floats, base-2 log-sum-exp of the scaled logits (as zc_prefill_attention's).
+ *   max_rows [host]: a bound on n_r that the caller vouches for; it chooses the kernel, and rows of
+ *   a request beyond it may be left as they were.
+ * A row that sees no key (kv_len[r] < n_r) gives 0 and a log-sum-exp of -inf.  Rows of out outside
+ * row_start[0] .. row_start[n_req] - 1 are left as they were.  Slots that no row of a request sees are
+ * not read into its results, whatever they hold: pages that lie wholly outside the window and the sinks
+ * may have been given away (any table entry).  kv_len beyond the table's width is taken as the width's
+ * tokens.  Keys on pages outside [0, n_pages) give undefined values, no fault. */
+int zc_paged_attention(zc_pages* p, const void* q, const int64_t q_strides[2], const int32_t* table,
+                       int table_width, const int32_t* row_start, const int32_t* kv_len, int n_req,
+                       int n_rows, int max_rows, int window, int sinks, void* out, float* row_lse,
+                       void* workspace, size_t workspace_bytes, zc_stream_t stream);
+
+/* zc_prefill_attention with a sliding window: row i sees the keys j <= i with j > i - window, and the
+ * first `sinks` tokens (j < sinks); window >= 1, sinks >= 0.  Arguments, outputs and errors as there.
+ * row_lse belongs to the windowed rows: zc_prefill_compress_lse wants zc_prefill_attention's. */
+int zc_prefill_attention_window(zc_cache* c, const void* Q, const void* K, const void* V, int l,
+                                const int64_t q_strides[3], const int64_t kv_strides[3], int window,
+                                int sinks, void* O, float* row_lse, zc_stream_t stream);
+
+/* Kernel launches enqueued through this handle since it was created. */
+int64_t zc_pages_launch_count(const zc_pages* p);
+
 /* Algorithmic bytes one zc_decode_attention call must read in the cache's current
  * state (packed codes + per-token parameters + tail + channel factors + q and out). */
 int64_t zc_decode_bytes(const zc_cache* c);
@@ -271,7 +373,7 @@ int64_t zc_launch_count(const zc_cache* c);
 /* Synchronises the device and reads the library's device-side error word into *code
  * [host]: 0 = none, 1 = a bounded wait on an asynchronous copy inside the decode kernel
  * ran out, 2 = a bounded wait for an earlier decode call of the stream ran out, 3 = a bounded wait
- * on the tensor cores inside a probe-score or prefill-attention kernel ran out (outputs are then invalid).  Device code never traps or spins forever. */
+ * on the tensor cores inside a probe-score or prefill-attention kernel ran out, 4 = a bounded wait inside a paged-attention or windowed prefill-attention kernel ran out (outputs are then invalid).  Device code never traps or spins forever. */
 int zc_device_status(int* code);
 
 /* Host-only model of the ordering the library applies to zc_decode_attention calls issued on

@@ -44,6 +44,20 @@ class ZcConfig(C.Structure):
                    int(k_scheme), int(scope))
 
 
+class ZcPageConfig(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_int32), ("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+        ("head_dim", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("reserved", C.c_int32),
+        ("strides", C.c_int64 * 3),
+    ]
+
+    @classmethod
+    def make(cls, dtype, n_q_heads, n_kv_heads, page_size, n_pages, strides, head_dim=128) -> "ZcPageConfig":
+        code = {torch.float16: ZC_F16, torch.bfloat16: ZC_BF16}.get(dtype, dtype)
+        return cls(C.sizeof(cls), code, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, 0,
+                   (C.c_int64 * 3)(*strides))
+
+
 _lib = None
 
 _SIGS = {
@@ -74,6 +88,23 @@ _SIGS = {
     "zc_tail_tokens": (C.c_int, [C.c_void_p]),
     "zc_export_segment": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
                                     C.c_void_p, C.c_void_p, C.c_void_p]),
+    "zc_pages_workspace": (C.c_int, [C.POINTER(ZcPageConfig), C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "zc_pages_init": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(ZcPageConfig), C.POINTER(C.c_void_p)]),
+    "zc_pages_free": (None, [C.c_void_p]),
+    "zc_pages_launch_count": (C.c_int64, [C.c_void_p]),
+    "zc_page_tables": (C.c_int, [C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p,
+                                 C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p,
+                                 C.c_void_p, C.c_void_p]),
+    "zc_page_write": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p, C.c_int,
+                                C.c_void_p]),
+    "zc_page_read": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
+                               C.POINTER(C.c_int64), C.c_void_p]),
+    "zc_paged_attention": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p, C.c_int,
+                                     C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "zc_prefill_attention_window": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
+                                              C.POINTER(C.c_int64), C.POINTER(C.c_int64), C.c_int, C.c_int,
+                                              C.c_void_p, C.c_void_p, C.c_void_p]),
     "zc_decode_bytes": (C.c_int64, [C.c_void_p]),
     "zc_launch_count": (C.c_int64, [C.c_void_p]),
     "zc_device_status": (C.c_int, [C.POINTER(C.c_int)]),
@@ -200,6 +231,15 @@ def zc_prefill_compress_lse(handle, Q, K, V, l: int, probe_pos: Sequence[int], r
            "zc_prefill_compress_lse")
 
 
+def zc_prefill_attention_window(handle, Q, K, V, l: int, window: int, sinks: int, O, row_lse, stream=None) -> None:
+    qs = (C.c_int64 * 3)(*Q.stride()[:3])
+    ks = (C.c_int64 * 3)(*K.stride()[:3])
+    if K.stride() != V.stride():
+        raise ZipCacheError("K and V must share strides")
+    _check(lib().zc_prefill_attention_window(handle, _ptr(Q), _ptr(K), _ptr(V), l, qs, ks, window, sinks, _ptr(O),
+                                             _ptr(row_lse), _stream(stream)), "zc_prefill_attention_window")
+
+
 def zc_append(handle, k_new, v_new, stream=None) -> None:
     _check(lib().zc_append(handle, _ptr(k_new), _ptr(v_new), _stream(stream)), "zc_append")
 
@@ -254,6 +294,60 @@ def zc_device_status() -> int:
     return code.value
 
 
+# ---- full-precision pages ----
+def zc_pages_workspace(cfg: ZcPageConfig, n_req: int, n_rows: int) -> int:
+    nbytes = C.c_size_t(0)
+    _check(lib().zc_pages_workspace(C.byref(cfg), n_req, n_rows, C.byref(nbytes)), "zc_pages_workspace")
+    return nbytes.value
+
+
+def zc_pages_init(k_pages, v_pages, cfg: ZcPageConfig) -> int:
+    h = C.c_void_p(0)
+    _check(lib().zc_pages_init(_ptr(k_pages), _ptr(v_pages), C.byref(cfg), C.byref(h)), "zc_pages_init")
+    return h.value
+
+
+def zc_pages_free(handle: int) -> None:
+    lib().zc_pages_free(handle)
+
+
+def zc_pages_launch_count(handle) -> int:
+    return lib().zc_pages_launch_count(handle)
+
+
+def zc_page_tables(page_size: int, past, fresh, free_pages, free_state, table, kv_len, row_start, slots, pos,
+                   free_out, stream=None) -> None:
+    _check(lib().zc_page_tables(page_size, past.numel(), _ptr(past), _ptr(fresh), _ptr(free_pages), free_pages.numel(),
+                                _ptr(free_state), _ptr(table), table.shape[1], _ptr(kv_len), _ptr(row_start),
+                                slots.numel(), _ptr(slots), _ptr(pos), _ptr(free_out), _stream(stream)),
+           "zc_page_tables")
+
+
+def zc_page_write(handle, k_rows, v_rows, slots, stream=None) -> None:
+    if k_rows.stride() != v_rows.stride():
+        raise ZipCacheError("k_rows and v_rows must share strides")
+    rs = (C.c_int64 * 2)(*k_rows.stride()[:2])
+    _check(lib().zc_page_write(handle, _ptr(k_rows), _ptr(v_rows), rs, _ptr(slots), k_rows.shape[0],
+                               _stream(stream)), "zc_page_write")
+
+
+def zc_page_read(handle, table, l: int, K, V, stream=None) -> None:
+    if K.stride() != V.stride():
+        raise ZipCacheError("K and V must share strides")
+    ks = (C.c_int64 * 3)(*K.stride()[:3])
+    _check(lib().zc_page_read(handle, _ptr(table), table.shape[1], table.shape[0], l, _ptr(K), _ptr(V), ks,
+                              _stream(stream)), "zc_page_read")
+
+
+def zc_paged_attention(handle, q, table, row_start, kv_len, max_rows: int, window: int, sinks: int, out, row_lse,
+                       workspace, stream=None) -> None:
+    qs = (C.c_int64 * 2)(*q.stride()[:2])
+    _check(lib().zc_paged_attention(handle, _ptr(q), qs, _ptr(table), table.shape[1], _ptr(row_start), _ptr(kv_len),
+                                    kv_len.numel(), q.shape[0], max_rows, window, sinks, _ptr(out), _ptr(row_lse),
+                                    _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+           "zc_paged_attention")
+
+
 ORDER_FIELDS = ("epoch_start", "e", "need_start", "need_end", "slot", "tag", "record", "drain")
 
 
@@ -269,6 +363,155 @@ def zc_order_model_call(stream_id, cache_id, q, k_new, v_new, out, io_bytes, kv_
     _check(lib().zc_order_model_call(stream_id, cache_id, addr, io_bytes, kv_bytes, int(collect),
                                      ws_addr, ws_bytes, need, capture_id, res), "zc_order_model_call")
     return dict(zip(ORDER_FIELDS, list(res)))
+
+
+def _want(t, name: str, shape, dtype, contiguous: bool = True) -> None:
+    """Refuses a tensor whose type, shape or layout the library would misread."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or (contiguous and not t.is_contiguous()):
+        raise ZipCacheError(f"{name}: expected {dtype} {tuple(shape)}{', contiguous' if contiguous else ''}, got "
+                            f"{t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+
+
+class _OnDevice:
+    """The library works on the calling thread's current device: makes `device` current for the
+    call when another one is, and picks its current stream unless one is given."""
+
+    def __init__(self, device):
+        self.device = device
+
+    def __enter__(self):
+        self.other = torch.cuda.current_device()
+        if self.other != self.device.index:
+            torch.cuda.set_device(self.device)
+
+    def __exit__(self, *exc):
+        if self.other != self.device.index:
+            torch.cuda.set_device(self.other)
+
+
+def _cuda_device(device) -> torch.device:
+    if not torch.cuda.is_available():
+        raise ZipCacheError("a CUDA device is required (no CPU fallback)")
+    device = torch.device(device)
+    return torch.device("cuda", torch.cuda.current_device() if device.index is None else device.index)
+
+
+class StepTables:
+    """The buffers of one serving step's lengths and slots (zc_page_tables): kv_len [n_req],
+    row_start [n_req + 1], slots and pos [n_rows], free_state [3], all int32.  Reused from step to
+    step; two steps whose free_state feeds the next one's take two of these in turn."""
+
+    def __init__(self, n_req: int, n_rows: int, device="cuda:0"):
+        self.device = _cuda_device(device)
+        self.n_req, self.n_rows = n_req, n_rows
+        new = lambda n: torch.zeros(n, dtype=torch.int32, device=self.device)  # noqa: E731
+        self.kv_len, self.row_start, self.slots, self.pos = new(n_req), new(n_req + 1), new(n_rows), new(n_rows)
+        self.free_state = new(3)
+        self._on = _OnDevice(self.device)
+
+    def build(self, page_size: int, past, fresh, free_pages, free_state, table, stream=None) -> "StepTables":
+        """past, fresh [n_req], free_pages [any], free_state [3] (next, end, -) and table [n_req, width]
+        (extended in place), all int32 on this object's device."""
+        i32 = torch.int32
+        _want(past, "past", (self.n_req,), i32)
+        _want(fresh, "fresh", (self.n_req,), i32)
+        _want(free_pages, "free_pages", (free_pages.numel(),), i32)
+        _want(free_state, "free_state", (3,), i32)
+        _want(table, "table", (self.n_req, table.shape[-1]), i32)
+        with self._on:
+            zc_page_tables(page_size, past, fresh, free_pages, free_state, table, self.kv_len, self.row_start,
+                           self.slots, self.pos, self.free_state, stream)
+        return self
+
+
+class PagedKV:
+    """Keys and values at full precision in pages: a handle over the caller's tensors, both
+    [n_pages, page_size, n_kv_heads, 128] with any strides of the first three dimensions (for pages
+    stored [n_pages, n_kv_heads, page_size, 128] pass .transpose(1, 2)).  Holds the workspace of
+    attention calls of up to max_req requests and max_rows rows."""
+
+    def __init__(self, k_pages, v_pages, n_q_heads: int, max_req: int = 256, max_rows: int = 8192,
+                 workspace: Optional[torch.Tensor] = None):
+        self.device = _cuda_device(k_pages.device)
+        if k_pages.dim() != 4 or k_pages.stride(3) != 1 or k_pages.stride() != v_pages.stride():
+            raise ZipCacheError("pages must be [n_pages, page_size, n_kv_heads, 128], the last dimension contiguous, "
+                                "K and V with the same strides")
+        _want(v_pages, "v_pages", k_pages.shape, k_pages.dtype, contiguous=False)
+        if k_pages.dtype not in (torch.float16, torch.bfloat16):
+            raise ZipCacheError("pages must be float16 or bfloat16")
+        n_pages, page_size, n_kv, d = k_pages.shape
+        self.cfg = ZcPageConfig.make(k_pages.dtype, n_q_heads, n_kv, page_size, n_pages, k_pages.stride()[:3], d)
+        self.k_pages, self.v_pages = k_pages, v_pages
+        self.dtype, self.page_size, self.n_q_heads, self.n_kv_heads = k_pages.dtype, page_size, n_q_heads, n_kv
+        self.workspace_bytes = zc_pages_workspace(self.cfg, max_req, max_rows)
+        self._on = _OnDevice(self.device)
+        if workspace is None:
+            workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
+        if workspace.numel() * workspace.element_size() < self.workspace_bytes:
+            raise ZipCacheError("shared workspace too small")
+        self.workspace = workspace
+        with self._on:
+            self.handle = zc_pages_init(k_pages, v_pages, self.cfg)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            zc_pages_free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def write(self, k_rows, v_rows, slots, stream=None):
+        """Rows [n, n_kv_heads, 128] into slots [n] (int32; negative: skipped)."""
+        shape = (slots.numel(), self.n_kv_heads, 128)
+        _want(slots, "slots", shape[:1], torch.int32)
+        _want(k_rows, "k_rows", shape, self.dtype, contiguous=False)
+        _want(v_rows, "v_rows", shape, self.dtype, contiguous=False)
+        if k_rows.stride(2) != 1:
+            raise ZipCacheError("the channels of a row must be contiguous")
+        with self._on:
+            zc_page_write(self.handle, k_rows, v_rows, slots, stream)
+
+    def read(self, table, l: int, K=None, V=None, stream=None):
+        """The first l tokens of every request in table [n_req, width]: K, V [n_req, n_kv_heads, l, 128]."""
+        shape = (table.shape[0], self.n_kv_heads, l, 128)
+        _want(table, "table", (table.shape[0], table.shape[-1]), torch.int32)
+        K = torch.empty(shape, dtype=self.dtype, device=self.device) if K is None else K
+        V = torch.empty(shape, dtype=self.dtype, device=self.device) if V is None else V
+        _want(K, "K", shape, self.dtype, contiguous=False)
+        _want(V, "V", shape, self.dtype, contiguous=False)
+        if K.stride(3) != 1:
+            raise ZipCacheError("the channels of a row must be contiguous")
+        with self._on:
+            zc_page_read(self.handle, table, l, K, V, stream)
+        return K, V
+
+    def attention(self, q, table, row_start, kv_len, max_rows: int, window: int = 0, sinks: int = 0, out=None,
+                  row_lse=None, stream=None):
+        """From q [n_rows, n_q_heads, 128], the newest tokens of the requests (rows row_start[r] ..
+        row_start[r + 1] - 1 are the last of kv_len[r] tokens), to the cached keys and values: out like q
+        (contiguous) and the rows' base-2 log-sum-exp [n_rows, n_q_heads].  max_rows bounds a request's
+        rows; window > 0 keeps the last `window` tokens and the first `sinks` ones visible."""
+        n_req, i32 = kv_len.numel(), torch.int32
+        _want(q, "q", (q.shape[0], self.n_q_heads, 128), self.dtype, contiguous=False)
+        _want(kv_len, "kv_len", (n_req,), i32)
+        _want(row_start, "row_start", (n_req + 1,), i32)
+        _want(table, "table", (n_req, table.shape[-1]), i32)
+        if q.stride(2) != 1:
+            raise ZipCacheError("the channels of a row must be contiguous")
+        if out is None:
+            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        if row_lse is None:
+            row_lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device)
+        _want(out, "out", q.shape, self.dtype)
+        _want(row_lse, "row_lse", q.shape[:2], torch.float32)
+        with self._on:
+            zc_paged_attention(self.handle, q, table, row_start, kv_len, max_rows, window, sinks, out, row_lse,
+                               self.workspace, stream)
+        return out, row_lse
 
 
 class ZipCache:
@@ -349,6 +592,19 @@ class ZipCache:
         lse = torch.empty((self.batch, self.n_q_heads, l), dtype=torch.float32, device=self.device)
         zc_prefill_attention(self.handle, Q, K, V, l, O, lse, stream)
         return O, lse
+
+    def prefill_attention_window(self, Q, K, V, window: int, sinks: int = 0, out=None, row_lse=None, stream=None):
+        """prefill_attention under a sliding window: a row sees the last `window` tokens up to itself and
+        the first `sinks` ones.  out and row_lse may be given (contiguous)."""
+        l = K.shape[2]
+        if out is None:
+            out = torch.empty((self.batch, self.n_q_heads, l, 128), dtype=self.dtype, device=self.device)
+        if row_lse is None:
+            row_lse = torch.empty((self.batch, self.n_q_heads, l), dtype=torch.float32, device=self.device)
+        _want(out, "out", (self.batch, self.n_q_heads, l, 128), self.dtype)
+        _want(row_lse, "row_lse", (self.batch, self.n_q_heads, l), torch.float32)
+        zc_prefill_attention_window(self.handle, Q, K, V, l, window, sinks, out, row_lse, stream)
+        return out, row_lse
 
     def prefill_compress_lse(self, Q, K, V, probe_pos, row_lse, stream=None):
         zc_prefill_compress_lse(self.handle, Q, K, V, K.shape[2], probe_pos, row_lse, self.workspace, stream)

@@ -8,6 +8,7 @@
 #include <algorithm>
 #include "zc_internal.h"
 #include "zc_layout.cuh"
+#include "zc_pages.h"
 
 namespace {
 
@@ -154,6 +155,8 @@ int cuda_fail(cudaError_t e) {
   } while (0)
 
 }  // namespace
+
+int zc_cuda_status(int e) { return e == (int)cudaSuccess ? ZC_OK : cuda_fail((cudaError_t)e); }
 
 // Performs a deferred append as its own launch (a call other than decode attention came first).
 static int flush_pending(zc_cache* c) {
@@ -602,6 +605,10 @@ int zc_device_status(int* code) {
   ZC_CUDA(zc_probe_error_code(&probe));
   ZC_CUDA(zc_attention_error_code(&att));
   if (*code == 0 && (probe || att)) *code = 3;
+  int paged = 0, chunk = 0;
+  ZC_CUDA(zc_paged_decode_error_code(&paged));
+  ZC_CUDA(zc_paged_chunk_error_code(&chunk));
+  if (*code == 0 && (paged || chunk)) *code = 4;
   int dbg_c = 0, dbg_d = 0;   // bounds-checked build only: 100 + the first failed check
   ZC_CUDA(zc_debug_code_compress(&dbg_c));
   ZC_CUDA(zc_debug_code_decode(&dbg_d));

@@ -149,6 +149,8 @@ enum {
   ZC_DBG_TOPK_INDEX = 7,    // split: an index list entry beyond its list
 };
 
+// ZC_OK, or ZC_ECUDA with the error's text kept for zc_strerror.
+int zc_cuda_status(int cuda_error);
 ZcSeg zc_segment(const zc_cache* c, int seg);
 ZcDecodePlan zc_make_plan(const zc_cache* c);
 

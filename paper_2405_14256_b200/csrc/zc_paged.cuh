@@ -1,0 +1,104 @@
+// Device helpers that the paged attention kernels share: tensor-map copies of page rows, output rows,
+// the joining of partial results, and launches that may start beside the kernel they follow.
+#pragma once
+#include "zc_pages.h"
+#include "zc_tc.cuh"
+
+bool zc_page_maps(zc_pages* p);   // encodes the handle's tensor maps (once); false: not supported
+
+namespace {
+
+template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// One box of a page: rows `row` ... of it, half `half` of the channels on.
+__device__ __forceinline__ void page_copy(const CUtensorMap* map, uint32_t dst, uint64_t* bar, int row, int half,
+                                          int head, int page) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], "
+      "[%7];\n" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(half), "r"(head), "r"(page), "r"(zc_smem_u32(bar))
+      : "memory");
+}
+
+// Output row `at` (128 channels, a warp holds four each) from sum = sum of the weights 2^(s - m) and
+// acc = sum of the weighted values; a row without keys (sum 0) gives 0 and a log-sum-exp of -inf.
+template <typename T>
+__device__ __forceinline__ void store_row(void* out, float* lse, long long at, int lane, float m, float sum, float4 acc) {
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const uint2 w = make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
+  *reinterpret_cast<uint2*>(reinterpret_cast<T*>(out) + at * ZC_D + 4 * lane) = w;
+  if (lse && lane == 0) lse[at] = sum > 0.f ? m + log2f(sum) : -INFINITY;
+}
+
+// One row from its n pieces (each: maximum, sum, -, -, 128 accumulated channels), in their order.
+template <typename T, typename At>
+__device__ __forceinline__ void join_row(void* out, float* lse, long long at, int lane, int n, At piece) {
+  float m = -1e30f;
+  for (int i = lane; i < n; i += 32) m = fmaxf(m, piece(i)[0]);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    const float* p = piece(i);
+    const float f = zc_exp2(p[0] - m);
+    const float4 x = *reinterpret_cast<const float4*>(p + 4 + 4 * lane);
+    sum = fmaf(p[1], f, sum);
+    acc.x = fmaf(x.x, f, acc.x);
+    acc.y = fmaf(x.y, f, acc.y);
+    acc.z = fmaf(x.z, f, acc.z);
+    acc.w = fmaf(x.w, f, acc.w);
+  }
+  store_row<T>(out, lse, at, lane, m, sum, acc);
+}
+
+// Tensor map in the 128-byte swizzle; strides in bytes.  False when the driver's entry point is missing
+// or refuses the tensor.
+inline bool zc_encode_map(CUtensorMap* map, int dtype, int rank, const void* at, const cuuint64_t* dims,
+                          const cuuint64_t* strides, const cuuint32_t* box) {
+  typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                               const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                               CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static EncodeFn encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      return (EncodeFn)f;
+    cudaGetLastError();
+    return (EncodeFn) nullptr;
+  }();
+  if (!encode) return false;
+  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  return encode(map, dtype == ZC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                (cuuint32_t)rank, const_cast<void*>(at), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Launch that may begin while the kernel before it still runs (it orders itself by griddepcontrol.wait).
+template <typename... KArgs, typename... Args>
+cudaError_t zc_launch_early(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+
+}  // namespace

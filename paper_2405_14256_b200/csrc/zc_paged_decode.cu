@@ -1,0 +1,502 @@
+// Attention of a few rows per request (a generated token, or a handful: rows x query heads of a KV
+// head <= 16) over its cached keys in pages (Eq. 4; bound: HBM, every visible key and value once).
+//
+// The visible keys of every (request, KV head) are cut into steps of 128 (eight blocks of 16); all
+// steps of the call, laid end to end, are dealt out to the CTAs in equal, consecutive shares, so that
+// ragged lengths do not matter.  A CTA is eight warps; warp w takes block w of each step through a ring
+// of its own (bulk tensor copies of 16 keys and 16 values, 8 KB a stage), so that no warp waits for
+// another inside a share.  Per block, with the query rows as the N dimension of the tensor-core tiles:
+//   S^T (16 keys x 8 rows) = K Q^T        A = keys from shared memory, B = rows kept in registers
+//   O^T (128 x 8 rows)    += V^T P^T      A = values read transposed, B = P^T = 2^(S - m), rounded to
+//                                         the input type (half a step relative, as a stored weight
+//                                         would be) and transposed in registers
+// Running maximum and sum per row in fp32; O is rescaled only when a row's maximum grows by more than
+// 8 (base 2).  At the end of a unit's steps the eight warps' results meet in shared memory.  A unit
+// that one CTA holds whole is written out; one that a share's border cuts goes to the workspace, and
+// k_paged_join puts its pieces together in the order of the CTAs (the result does not depend on timing).
+#include <cstring>
+#include "zc_pages.h"
+#include "zc_layout.cuh"
+#include "zc_tc.cuh"
+#include "zc_paged.cuh"
+
+namespace {
+
+constexpr int kDecWarps = 8, kDecThreads = 32 * kDecWarps;
+constexpr int kBlkLog2 = 4, kBlk = 1 << kBlkLog2;      // keys of a block
+constexpr int kHalf = kBlk * ZC_D * 2;                 // 4 KB: keys (or values) of a stage, [2][16][128 B]
+constexpr int kStages = 3;
+constexpr int kRing = kDecWarps * kStages * 2 * kHalf; // 192 KB
+constexpr int kJoinStride = ZC_PART_STRIDE;            // m, sum, -, -, acc[128]
+constexpr int kJoinBytes = kDecWarps * 8 * kJoinStride * 4;
+constexpr int kScanBytes = kDecWarps * 8 + 16;
+constexpr int kDecSmem = kRing + kJoinBytes + kDecWarps * kStages * 8 + kScanBytes + 1024;   // 1 KB: alignment
+constexpr float kNoMax = -1e30f;                       // running maximum before any key
+constexpr float kTau = 8.f;
+
+// What k_paged_join needs to know about the unit that a CTA's share begins inside.
+struct JoinDesc {
+  int on, first_cta, last_cta, kv, row0, rows;
+  int first_slot, pad;
+};
+
+struct Req {
+  int row0, n, p0;   // first row, rows, position of the first
+  ZcSeen s;
+};
+__device__ __forceinline__ int load_req(const ZcPagedArgs& a, int r, Req* q) {
+  const int e0 = min(max(a.row_start[r], 0), a.n_rows);
+  const int e1 = min(max(a.row_start[r + 1], e0), a.n_rows);
+  const long long cap = (long long)a.table_width << a.page_log2;
+  const int kv = (int)min((long long)max(a.kv_len[r], 0), cap);
+  q->row0 = e0;
+  q->n = min(e1 - e0, a.max_rows);
+  q->p0 = kv - (e1 - e0);
+  q->s = zc_seen(q->p0, q->p0 + q->n - 1, a.window, a.sinks, kBlkLog2);
+  return q->n > 0 ? max(1, (q->s.nb + kDecWarps - 1) / kDecWarps) : 0;
+}
+
+// One unit's steps a .. b - 1 inside a CTA's share.
+struct Seg {
+  int r, kv, a, b, steps;
+  long long left;   // steps of the share after this segment
+  Req q;
+};
+__device__ __forceinline__ bool seg_next(const ZcPagedArgs& a, Seg& g) {
+  if (g.left <= 0) return false;
+  if (++g.kv == a.h_kv) {
+    g.kv = 0;
+    do {
+      if (++g.r >= a.n_req) return false;
+      g.steps = load_req(a, g.r, &g.q);
+    } while (g.steps == 0);
+  }
+  g.a = 0;
+  g.b = (int)min((long long)g.steps, g.left);
+  g.left -= g.b;
+  return true;
+}
+
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+
+// NT: groups of 8 rows
+template <typename T, int NT>
+__global__ void __launch_bounds__(kDecThreads, 1)
+    k_paged_decode(const ZcPagedArgs a, float* __restrict__ parts, JoinDesc* __restrict__ descs,
+                   const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
+  extern __shared__ __align__(1024) char smem_raw[];
+  const uint32_t raw_u = zc_smem_u32(smem_raw);
+  const uint32_t base_u = (raw_u + 1023u) & ~1023u;
+  char* base = smem_raw + (base_u - raw_u);
+  float* s_join = reinterpret_cast<float*>(base + kRing);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(base + kRing + kJoinBytes);
+  long long* s_sum = reinterpret_cast<long long*>(bars + kDecWarps * kStages);
+  volatile long long& s_off = *reinterpret_cast<volatile long long*>(s_sum + kDecWarps);
+  volatile int& s_req = *reinterpret_cast<volatile int*>(s_sum + kDecWarps + 1);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // the joining kernel may be brought in beside this one; it waits for this grid's end
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  if (tid < kDecWarps * kStages) bar_init(&bars[tid], 1);
+  asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+
+  // ---- this CTA's share ----
+  long long sum = 0;
+  int mine = 0;
+  for (int r = tid; r < a.n_req; r += kDecThreads) {
+    Req q;
+    mine = load_req(a, r, &q);
+    sum += mine;
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) s_sum[warp] = sum;
+  if (tid == 0) s_req = -1;
+  __syncthreads();
+  long long total = 0;
+#pragma unroll
+  for (int w = 0; w < kDecWarps; ++w) total += s_sum[w];
+  total *= a.h_kv;
+  const long long g = min((long long)gridDim.x, total);   // CTAs with work
+  const long long c = blockIdx.x;
+  if (c >= g) {
+    if (tid == 0) descs[c].on = 0;
+    return;
+  }
+  const long long begin = c * total / g, end = (c + 1) * total / g;
+  long long before = 0;
+  for (int c0 = 0; c0 < a.n_req; c0 += kDecThreads) {
+    if (a.n_req > kDecThreads) {
+      Req q;
+      mine = c0 + tid < a.n_req ? load_req(a, c0 + tid, &q) : 0;
+    } else if (tid >= a.n_req) mine = 0;
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += u;
+    }
+    __syncthreads();
+    if (lane == 31) s_sum[warp] = incl;
+    __syncthreads();
+    long long off = before + incl - mine;
+#pragma unroll
+    for (int w = 0; w < kDecWarps; ++w) {
+      if (w < warp) off += s_sum[w];
+      before += s_sum[w];
+    }
+    if (mine > 0 && begin >= off * a.h_kv && begin < (off + mine) * a.h_kv) {
+      s_req = c0 + tid;
+      s_off = begin - off * a.h_kv;
+    }
+    __syncthreads();
+    if (s_req >= 0) break;
+  }
+  Seg seg;
+  seg.r = s_req;
+  seg.steps = load_req(a, seg.r, &seg.q);
+  const long long in_req = s_off;
+  seg.kv = (int)(in_req / seg.steps);
+  seg.a = (int)(in_req % seg.steps);
+  seg.b = (int)min((long long)seg.steps, seg.a + (end - begin));
+  seg.left = (end - begin) - (seg.b - seg.a);
+  if (tid == 0) {
+    JoinDesc d;
+    const long long u0 = begin - seg.a;
+    d.first_cta = (int)(((u0 + 1) * g - 1) / total);
+    d.last_cta = (int)(((u0 + seg.steps) * g - 1) / total);
+    d.on = seg.a > 0 && c == d.first_cta + 1;
+    // the first CTA's piece is its last segment: slot 1, unless its share begins with the unit
+    d.first_slot = (long long)d.first_cta * total / g < u0 ? 1 : 0;
+    d.kv = seg.kv;
+    d.row0 = seg.q.row0;
+    d.rows = seg.q.n * a.G;
+    d.pad = 0;
+    descs[c] = d;
+  }
+
+  // ---- copies: lane 0 of every warp, running ahead of the warp's own blocks ----
+  Seg ps = seg;
+  int pstep = seg.a, pkey = -1, ppage = 0, pkv = 0;
+  auto fetch = [&]() {   // the next block of this warp; its page id is asked for now and used at the next issue
+    for (;;) {
+      for (; pstep < ps.b; ++pstep) {
+        const int vb = pstep * kDecWarps + warp;
+        if (vb < ps.q.s.nb) {
+          pkey = (vb < ps.q.s.nsb ? vb : ps.q.s.wb0 + vb - ps.q.s.nsb) << kBlkLog2;
+          pkv = ps.kv;
+          ppage = a.table[(long long)ps.r * a.table_width + (pkey >> a.page_log2)];
+          ++pstep;
+          return;
+        }
+      }
+      if (!seg_next(a, ps)) {
+        pkey = -1;
+        return;
+      }
+      pstep = 0;
+    }
+  };
+  const uint32_t ring = base_u + warp * kStages * 2 * kHalf;
+  uint64_t* full = bars + warp * kStages;
+  auto issue = [&](int stage) {
+    if (pkey < 0) return;
+    if (lane == 0) {
+      const int page = ppage >= 0 && ppage < a.n_pages ? ppage : a.n_pages;   // beyond the pool: arrives as zeros
+      const int row = pkey & ((1 << a.page_log2) - 1);
+      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(zc_smem_u32(&full[stage])),
+                   "r"(2 * kHalf)
+                   : "memory");
+      const uint32_t dst = ring + stage * 2 * kHalf;
+      page_copy(&kmap, dst, &full[stage], row, 0, pkv, page);
+      page_copy(&vmap, dst + kHalf, &full[stage], row, 0, pkv, page);
+    }
+    fetch();
+  };
+  fetch();
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) issue(i);
+
+  const float scale = kLog2e * rsqrtf((float)ZC_D);
+  const int quad = lane & 3, oct = lane >> 2;
+  int stage = 0;
+  uint32_t phase = 0;
+  bool first_seg = true;
+  for (;;) {
+    const int rows = seg.q.n * a.G;
+    // this unit's query rows as B fragments: row = oct + 8 nt, two consecutive channels a register
+    uint32_t qf[NT][8][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int row = oct + 8 * nt, tok = row / a.G;
+      const T* qp = reinterpret_cast<const T*>(a.q) + (long long)(seg.q.row0 + tok) * a.qs_row +
+                    (long long)(seg.kv * a.G + (row - tok * a.G)) * a.qs_head + 2 * quad;
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) {
+        qf[nt][ks][0] = row < rows ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks) : 0u;
+        qf[nt][ks][1] = row < rows ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks + 8) : 0u;
+      }
+    }
+    // positions of this thread's rows (rows 2 quad, 2 quad + 1 of each group of 8)
+    int pos[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int row = 8 * nt + 2 * quad + e;
+        pos[nt][e] = row < rows ? seg.q.p0 + row / a.G : -1;
+      }
+    const int p_last = seg.q.p0 + seg.q.n - 1;
+    float o[NT][8][4], m[NT][2], s[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
+      m[nt][0] = m[nt][1] = kNoMax;
+      s[nt][0] = s[nt][1] = 0.f;
+    }
+    for (int step = seg.a; step < seg.b; ++step) {
+      const int vb = step * kDecWarps + warp;
+      if (vb >= seg.q.s.nb) break;
+      const int key0 = (vb < seg.q.s.nsb ? vb : seg.q.s.wb0 + vb - seg.q.s.nsb) << kBlkLog2;
+      const uint32_t kt = ring + stage * 2 * kHalf, vt = kt + kHalf;
+      bar_wait(&full[stage], phase);
+      // ---- S^T = K Q^T ----
+      float sc[NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[nt][e] = 0.f;
+      const int lrow = lane & 15;                         // matrices 0, 2: keys 0-7; 1, 3: keys 8-15
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) {
+        const int chunk = 2 * ks + (lane >> 4);
+        uint32_t kf[4];
+        ldmatrix_x4(kf, kt + (chunk >> 3) * (kBlk * 128) + lrow * 128 + (((chunk & 7) ^ (lrow & 7)) << 4));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) zc_mma16816<T>(sc[nt], kf, qf[nt][ks][0], qf[nt][ks][1]);
+      }
+      // ---- masks: only blocks at a border ----
+      if (key0 + kBlk - 1 > seg.q.p0 || (key0 <= p_last - a.window && key0 + kBlk > a.sinks)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int key = key0 + oct + 8 * (e >> 1), p = pos[nt][e & 1];
+            const bool seen = key <= p && (key > p - a.window || key < a.sinks);
+            if (!seen) sc[nt][e] = -INFINITY;
+          }
+        // values that no row sees may hold anything (2^-inf = 0 times NaN is NaN): zeros in their place
+        const int vr = lane >> 1, vkey = key0 + vr;
+        const bool dead = vkey >= seg.q.s.hi || (vkey < seg.q.s.lo && vkey >= seg.q.s.sink_n);
+        if (dead) {
+          char* at = base + (vt - base_u) + (lane & 1) * (kBlk * 128) + vr * 128;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(at + 16 * i) = make_uint4(0, 0, 0, 0);
+        }
+        async_proxy_fence();   // the stage's next copy is ordered behind these stores
+        __syncwarp();
+      }
+      // ---- running maximum and sum ----
+      uint32_t pf[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float mx[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          mx[e] = fmaxf(sc[nt][e], sc[nt][e + 2]) * scale;
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], x));
+        }
+        const bool grow0 = mx[0] > m[nt][0] + kTau, grow1 = mx[1] > m[nt][1] + kTau;
+        if (__any_sync(0xffffffffu, grow0 || grow1)) {
+          const float al0 = grow0 ? zc_exp2(m[nt][0] - mx[0]) : 1.f, al1 = grow1 ? zc_exp2(m[nt][1] - mx[1]) : 1.f;
+          if (grow0) m[nt][0] = mx[0];
+          if (grow1) m[nt][1] = mx[1];
+          s[nt][0] *= al0;
+          s[nt][1] *= al1;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            o[nt][i][0] *= al0;
+            o[nt][i][1] *= al1;
+            o[nt][i][2] *= al0;
+            o[nt][i][3] *= al1;
+          }
+        }
+        const float p0 = zc_exp2(fmaf(sc[nt][0], scale, -m[nt][0])), p1 = zc_exp2(fmaf(sc[nt][1], scale, -m[nt][1]));
+        const float p2 = zc_exp2(fmaf(sc[nt][2], scale, -m[nt][0])), p3 = zc_exp2(fmaf(sc[nt][3], scale, -m[nt][1]));
+        s[nt][0] += p0 + p2;
+        s[nt][1] += p1 + p3;
+        pf[nt][0] = movmatrix_trans(pack2<T>(p0, p1));    // keys 0-7 of the block
+        pf[nt][1] = movmatrix_trans(pack2<T>(p2, p3));    // keys 8-15
+      }
+      // ---- O^T += V^T P^T ----
+      const int vrow = (lane & 7) + ((lane >> 4) << 3);   // matrices 0, 1: keys 0-7; 2, 3: keys 8-15
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt) {
+        const int chunk = 2 * mt + ((lane >> 3) & 1);
+        uint32_t vf[4];
+        ldmatrix_x4_trans(vf, vt + (chunk >> 3) * (kBlk * 128) + vrow * 128 + (((chunk & 7) ^ (vrow & 7)) << 4));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) zc_mma16816<T>(o[nt][mt], vf, pf[nt][0], pf[nt][1]);
+      }
+      __syncwarp();
+      issue(stage);
+      if (++stage == kStages) {
+        stage = 0;
+        phase ^= 1u;
+      }
+    }
+    // ---- the eight warps' results of this unit ----
+    const bool whole = seg.a == 0 && seg.b == seg.steps;
+    float* slot = parts + (2 * c + (first_seg ? 0 : 1)) * (long long)ZC_PAGED_ROWS * kJoinStride;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (8 * nt >= rows) break;
+      __syncthreads();   // the join area is free
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float t = s[nt][e];
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) t += __shfl_xor_sync(0xffffffffu, t, x);
+        float* jr = s_join + (warp * 8 + 2 * quad + e) * kJoinStride;
+        if (oct == 0) {
+          jr[0] = m[nt][e];
+          jr[1] = t;
+        }
+#pragma unroll
+        for (int mt = 0; mt < 8; ++mt) {
+          jr[4 + 16 * mt + oct] = o[nt][mt][e];
+          jr[4 + 16 * mt + oct + 8] = o[nt][mt][e + 2];
+        }
+      }
+      __syncthreads();
+      const int row = 8 * nt + warp;
+      if (row < rows) {
+        float mt = kNoMax;
+#pragma unroll
+        for (int w = 0; w < kDecWarps; ++w) mt = fmaxf(mt, s_join[(w * 8 + warp) * kJoinStride]);
+        float total_s = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kDecWarps; ++w) {
+          const float* jr = s_join + (w * 8 + warp) * kJoinStride;
+          const float f = zc_exp2(jr[0] - mt);
+          const float4 x = *reinterpret_cast<const float4*>(jr + 4 + 4 * lane);
+          total_s = fmaf(jr[1], f, total_s);
+          acc.x = fmaf(x.x, f, acc.x);
+          acc.y = fmaf(x.y, f, acc.y);
+          acc.z = fmaf(x.z, f, acc.z);
+          acc.w = fmaf(x.w, f, acc.w);
+        }
+        if (whole) {
+          const int tok = row / a.G;
+          const long long at = (long long)(seg.q.row0 + tok) * a.h_q + seg.kv * a.G + (row - tok * a.G);
+          store_row<T>(a.out, a.lse, at, lane, mt, total_s, acc);
+        } else {
+          float* pr = slot + row * kJoinStride;
+          if (lane == 0) {
+            pr[0] = mt;
+            pr[1] = total_s;
+          }
+          *reinterpret_cast<float4*>(pr + 4 + 4 * lane) = acc;
+        }
+      }
+    }
+    first_seg = false;
+    if (!seg_next(a, seg)) break;
+  }
+}
+
+// Block c - 1: the unit that the border before CTA c cuts first.  A warp takes a row.
+template <typename T>
+__global__ void __launch_bounds__(256) k_paged_join(const ZcPagedArgs a, const float* __restrict__ parts,
+                                                    const JoinDesc* __restrict__ descs) {
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  const JoinDesc d = descs[blockIdx.x + 1];
+  if (!d.on) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int row = warp; row < d.rows; row += 8) {
+    const int tok = row / a.G;
+    const long long at = (long long)(d.row0 + tok) * a.h_q + d.kv * a.G + (row - tok * a.G);
+    join_row<T>(a.out, a.lse, at, lane, d.last_cta - d.first_cta + 1, [&](int i) {
+      const long long slot = 2LL * (d.first_cta + i) + (i == 0 ? d.first_slot : 0);
+      return parts + (slot * ZC_PAGED_ROWS + row) * kJoinStride;
+    });
+  }
+}
+
+template <typename T, int NT>
+int launch(zc_pages* p, const ZcPagedArgs& a, float* parts, JoinDesc* descs, cudaStream_t st) {
+  static bool once[64] = {};   // per device: the attribute belongs to the device's copy of the kernel
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64 || !once[dev]) {
+    e = cudaFuncSetAttribute(k_paged_decode<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDecSmem);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) once[dev] = true;
+  }
+  k_paged_decode<T, NT><<<p->n_sm, kDecThreads, kDecSmem, st>>>(a, parts, descs, p->k16, p->v16);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  p->launches += 1;
+  if (p->n_sm > 1) {
+    e = zc_launch_early(k_paged_join<T>, dim3(p->n_sm - 1), dim3(256), 0, st, a, (const float*)parts, (const JoinDesc*)descs);
+    if (e != cudaSuccess) return e;
+    p->launches += 1;
+  }
+  return cudaSuccess;
+}
+
+}  // namespace
+
+size_t zc_paged_decode_workspace(const zc_pages*) {
+  return (size_t)ZC_PAGED_MAX_CTAS * (2 * ZC_PAGED_ROWS * kJoinStride * 4 + sizeof(JoinDesc));
+}
+
+int zc_launch_paged_decode(zc_pages* p, const ZcPagedArgs& a, char* ws, cudaStream_t st) {
+  if (!zc_page_maps(p)) return (int)cudaErrorNotSupported;
+  JoinDesc* descs = (JoinDesc*)ws;
+  float* parts = (float*)(ws + (size_t)ZC_PAGED_MAX_CTAS * sizeof(JoinDesc));
+  const bool one = a.max_rows * a.G <= 8;
+  if (p->cfg.dtype == ZC_F16)
+    return one ? launch<__half, 1>(p, a, parts, descs, st) : launch<__half, 2>(p, a, parts, descs, st);
+  return one ? launch<__nv_bfloat16, 1>(p, a, parts, descs, st) : launch<__nv_bfloat16, 2>(p, a, parts, descs, st);
+}
+
+// Tensor maps of the pages: (64 channels, token of the page, half of the channels, KV head, page).
+bool zc_page_maps(zc_pages* p) {
+  if (p->maps_ready) return true;
+  const int64_t* s = p->cfg.strides;
+  const cuuint64_t dims[5] = {64, (cuuint64_t)p->cfg.page_size, 2, (cuuint64_t)p->cfg.n_kv_heads,
+                              (cuuint64_t)p->cfg.n_pages};
+  const cuuint64_t strides[4] = {(cuuint64_t)s[1] * 2, 128, (cuuint64_t)s[2] * 2, (cuuint64_t)s[0] * 2};
+  const cuuint32_t small[5] = {64, kBlk, 2, 1, 1};
+  const cuuint32_t large[5] = {64, (cuuint32_t)(p->cfg.page_size < kM ? p->cfg.page_size : kM), 1, 1, 1};
+  struct { CUtensorMap* map; void* at; const cuuint32_t* box; } todo[4] = {
+      {&p->k16, p->k, small}, {&p->v16, p->v, small}, {&p->k128, p->k, large}, {&p->v128, p->v, large}};
+  for (auto& t : todo)
+    if (!zc_encode_map(t.map, p->cfg.dtype, 5, t.at, dims, strides, t.box)) return false;
+  p->maps_ready = true;
+  return true;
+}
+
+int zc_paged_decode_error_code(int* out) { return (int)cudaMemcpyFromSymbol(out, g_zc_tc_error, sizeof(int)); }
