@@ -3,21 +3,27 @@
 //
 // The query heads of a KV head are packed beside each other: row = token * G + head, 128 / G tokens to
 // a tile of 128 rows, so that short chunks fill the tile, a key tile is read once for the whole group and
-// little work falls on tiles that the causal mask or the window cuts.  A work item is two such tiles
-// (groups 0 and 1) of one request and KV head, and the key tiles (128 keys) that any of its rows sees:
-// those of the first `sinks` tokens, then those of the window.  Items go through the kernel of
-// persistent CTAs one after the other:
-//   warp 0   the matrix products, tcgen05.mma with accumulators in tensor memory:
-//            S_g = Q_g K^T (both K-major in shared memory), O_g += P_g V (P_g in tensor memory over
-//            the first 64 columns of S_g, V with its channels contiguous)
-//   warp 1   the copies: Q by one box per tile half, K and V page by page (a lane per page)
+// little work falls on tiles that the causal mask or the window cuts.  A work item is one request's and
+// KV head's rows of two such tiles (groups 0 and 1 take one each), or of one (the groups then take the
+// even and the odd key tiles, and their results meet at the end), and the key tiles (64 keys) that any
+// of its rows sees: those of the first `sinks` tokens, then those of the window.  The CTAs are
+// persistent, one per SM; each works through items until there are none:
+//   warp 2      fetches the items ahead of the others (for pages from a common counter, the longest first)
+//   warp 1      the copies: Q by one box per tile half, K and V page by page (a lane per page)
+//   warps 0, 3  the matrix products of group 0 and 1, tcgen05.mma with accumulators in tensor memory:
+//               S_g = Q_g K^T (both K-major in shared memory), 128 x 64, and O_g += P_g V (P_g in tensor
+//               memory over the first half of its S, V with its channels contiguous), 128 x 128
 //   warps 4-7, 8-11  groups 0 and 1, one row per thread: running maximum (O rescaled when it grows by
-//            more than 8, base 2) and sum in fp32, P rounded to the input type, output and log-sum-exp
-// While one group turns S into P the tensor cores work for the other; the next item's Q and first key
-// tiles arrive while this one's output is written.
+//               more than 8, base 2) and sum in fp32, P rounded to the input type, output and log-sum-exp
+// Each group has two places for S, and S of a key tile is computed two tiles ahead: a group turns one S
+// after the other into P without waiting for a product, and the tensor cores' work hides behind that of
+// the groups (and the other way round).  With 128 keys to a tile and one place for S, the chain product -
+// weights - product left either side idle half of the time (5000 cycles per 256 rows x 128 keys).  The
+// next item's Q and first key tiles arrive while this one's output is written.
 // For pages the list of items is made on the device (k_chunk_plan: lengths stay there).  Where a call has
 // few items for the GPU, those with many key tiles are cut into pieces along the keys, and k_chunk_join
 // puts the pieces together in their order.
+#include <algorithm>
 #include <cstring>
 #include "zc_paged.cuh"
 #include "zc_layout.cuh"
@@ -25,19 +31,26 @@
 namespace {
 
 constexpr int kThreads = 384;
-constexpr int kKS = 3, kVS = 2;                       // key and value buffers
-constexpr uint32_t kCols = 512;                       // S_0 | S_1 | O_0 | O_1
-constexpr int kTiles = (2 + kKS + kVS) * kTile;       // 224 KB
-constexpr int kSmem = kTiles + 1024 + 256;
+constexpr int kN = 64;                                // keys of a tile
+constexpr int kTileLog2 = 6;
+constexpr int kKvTile = kN * ZC_D * 2;                // 16 KB: [2][64][128 B]
+constexpr int kKvBlock = kN * 128;
+constexpr int kKS = 5, kVS = 5;                       // key and value buffers
+constexpr uint32_t kCols = 512;                       // S_0 twice | S_1 twice | O_0 | O_1
+constexpr int kTiles = 2 * kTile + (kKS + kVS) * kKvTile;   // 224 KB
+constexpr int kRingN = 2;                             // items fetched ahead
+constexpr int kRingInts = 24;
+constexpr int kSmem = kTiles + 1024 + 384 + 1024 + kRingN * kRingInts * 4;   // alignment, barriers, (m, sum) of group 1
+constexpr int kPoly = 2;                              // of 8 pairs of weights, those without the exp2 unit
 constexpr float kTau = 8.f;
 constexpr float kNoMax = -1e30f;
-constexpr int kTileLog2 = 7;
 constexpr int kPartStride = ZC_PART_STRIDE;           // m, sum, -, -, acc[128]
 constexpr int kItemRows = 2 * kM;
 // Pieces: at most kPieces key-tile ranges of full length over all heads, and no more remainders.
 constexpr int kPieces = 2 * ZC_PAGED_MAX_CTAS;
 constexpr int kMaxSlots = 2 * kPieces;
 constexpr int kPlanThreads = 1024;
+constexpr int kReqShared = 2048;                      // requests whose lengths the planner keeps in shared memory
 
 // One piece of work: tokens tok0 ... of request r (one item), key tiles t0 .. t1 - 1 of those it sees.
 struct ChunkWork {
@@ -46,7 +59,7 @@ struct ChunkWork {
   int pad[3];
 };
 struct ChunkJoin { int r, tok0, slot, n; };
-struct ChunkHead { int n_work, n_join, slots_per_head, pad; };
+struct ChunkHead { int n_work, n_join, slots_per_head, next; };   // next: the first item that no CTA has taken
 
 struct ChunkWs {
   ChunkHead* head;
@@ -82,119 +95,171 @@ __device__ __forceinline__ int item_tiles(const ZcPagedArgs& a, const Chunk& c, 
   return zc_seen(c.p0 + tok0, c.p0 + last, a.window, a.sinks, kTileLog2).nb;
 }
 
-__device__ __forceinline__ int block_scan(int v, int* s_warp, int* total) {   // exclusive, kPlanThreads threads
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int incl = v;
+// Exclusive sums over the block of two counts at once, and their totals.
+__device__ __forceinline__ int2 block_scan2(int2 v, int2* s_warp, int2* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warp = blockDim.x >> 5;
+  int2 incl = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += u;
+    const int x = __shfl_up_sync(0xffffffffu, incl.x, o), y = __shfl_up_sync(0xffffffffu, incl.y, o);
+    if (lane >= o) {
+      incl.x += x;
+      incl.y += y;
+    }
   }
   __syncthreads();
   if (lane == 31) s_warp[warp] = incl;
   __syncthreads();
-  if (warp == 0) {
-    int w = s_warp[lane];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, w, o);
-      if (lane >= o) w += u;
+  int2 before = make_int2(incl.x - v.x, incl.y - v.y);
+  total->x = total->y = 0;
+  for (int w = 0; w < n_warp; ++w) {
+    const int2 u = s_warp[w];
+    if (w < warp) {
+      before.x += u.x;
+      before.y += u.y;
     }
-    s_warp[lane] = w;
+    total->x += u.x;
+    total->y += u.y;
   }
-  __syncthreads();
-  *total = s_warp[31];
-  return incl - v + (warp ? s_warp[warp - 1] : 0);
+  return before;
 }
 
-// The list of work of one KV head (every head has the same), and the items that are in pieces.
-// One CTA; lengths are read here and nowhere on the host.
+// Piece lengths in 64 classes, four to a power of two, the longest class first.
+__device__ __forceinline__ int length_class(int n) {
+  if (n < 4) return 63 - n;
+  const int e = 31 - __clz(n);
+  return max(0, 63 - (4 * e - 4 + ((n >> (e - 2)) & 3)));
+}
+
+// The list of work of one KV head (every head has the same), the longest pieces first, and the items
+// that are in pieces.  One CTA; lengths are read here and nowhere on the host.
 __global__ void __launch_bounds__(kPlanThreads, 1) k_chunk_plan(const ChunkArgs k, int n_cta) {
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-  __shared__ int s_warp[32];
-  __shared__ long long s_tiles;
+  __shared__ int2 s_warp[32];
+  __shared__ unsigned long long s_tiles;
+  __shared__ int s_class[64];
+  __shared__ int s_start[kReqShared + 1], s_n[kReqShared], s_p0[kReqShared];
   const ZcPagedArgs& a = k.a;
-  const int tid = threadIdx.x, tpi = 2 * k.tpt;
+  const int tid = threadIdx.x, n_thread = blockDim.x, tpi = 2 * k.tpt;
+  const bool shared = a.n_req <= kReqShared;   // else the items' starts go through the workspace
+  int* start = shared ? s_start : k.ws.item_start;
   if (tid == 0) s_tiles = 0;
+  for (int i = tid; i < 64; i += n_thread) s_class[i] = 0;
   int items = 0;
-  for (int c0 = 0; c0 < a.n_req; c0 += kPlanThreads) {
+  for (int c0 = 0; c0 < a.n_req; c0 += n_thread) {
+    const int r = c0 + tid;
     int n = 0;
-    if (c0 + tid < a.n_req) n = (load_chunk(a, c0 + tid).n + tpi - 1) / tpi;
-    int t;
-    const int at = block_scan(n, s_warp, &t);
-    if (c0 + tid < a.n_req) k.ws.item_start[c0 + tid] = items + at;
-    items += t;
+    if (r < a.n_req) {
+      const Chunk c = load_chunk(a, r);
+      n = (c.n + tpi - 1) / tpi;
+      if (shared) {
+        s_n[r] = c.n;
+        s_p0[r] = c.p0;
+      }
+    }
+    int2 t;
+    const int2 at = block_scan2(make_int2(n, 0), s_warp, &t);
+    if (r < a.n_req) start[r] = items + at.x;
+    items += t.x;
   }
-  if (tid == 0) k.ws.item_start[a.n_req] = items;
+  if (tid == 0) start[a.n_req] = items;
   __syncthreads();
-  auto find = [&](int i, int* tok0) {   // request and first token of item i
+  auto item = [&](int i, int* tok0, int* nt) {   // request, first token and key tiles of item i
     int lo = 0, hi = a.n_req;
     while (hi - lo > 1) {
       const int m = (lo + hi) >> 1;
-      if (k.ws.item_start[m] <= i) lo = m; else hi = m;
+      if (start[m] <= i) lo = m; else hi = m;
     }
-    *tok0 = (i - k.ws.item_start[lo]) * tpi;
+    *tok0 = (i - start[lo]) * tpi;
+    Chunk c;
+    if (shared) {
+      c.n = s_n[lo];
+      c.p0 = s_p0[lo];
+    } else {
+      c = load_chunk(a, lo);
+    }
+    *nt = item_tiles(a, c, *tok0, tpi);
     return lo;
   };
-  long long tiles = 0;
-  for (int i = tid; i < items; i += kPlanThreads) {
-    int tok0;
-    const int r = find(i, &tok0);
-    tiles += item_tiles(a, load_chunk(a, r), tok0, tpi);
+  unsigned long long tiles = 0;
+  for (int i = tid; i < items; i += n_thread) {
+    int tok0, nt;
+    item(i, &tok0, &nt);
+    tiles += nt;
   }
-  atomicAdd(reinterpret_cast<unsigned long long*>(&s_tiles), (unsigned long long)tiles);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, o);
+  if ((tid & 31) == 0) atomicAdd(&s_tiles, tiles);
   __syncthreads();
-  // Pieces: where the items of all heads come to fewer than four per CTA, none is longer than half a
-  // CTA's even share (so that the busiest CTA ends within about half a share of the others), and no
-  // shorter than 4 tiles, below which writing and joining the pieces costs more than it evens out.
-  const long long all = s_tiles * a.h_kv;
-  long long most = 1LL << 40;
-  if ((long long)items * a.h_kv < 4LL * n_cta) {
-    most = (all + 2 * n_cta - 1) / (2 * n_cta);
-    if (most < 4) most = 4;
+  // No piece is longer than half a CTA's even share, so that handing out the longest first leaves the
+  // CTAs about even, and none is shorter than 8 tiles, below which writing and joining the pieces costs
+  // more than it evens out.
+  const long long all = (long long)s_tiles * a.h_kv;
+  long long most = (all + 2 * n_cta - 1) / (2 * n_cta);
+  if (most < 8) most = 8;
+  auto pieces_of = [&](int nt) { return nt <= most ? 1 : (int)((nt + most - 1) / most); };
+  for (int i = tid; i < items; i += n_thread) {
+    int tok0, nt;
+    item(i, &tok0, &nt);
+    const int pieces = pieces_of(nt);
+    atomicAdd(&s_class[length_class((nt + pieces - 1) / pieces)], pieces);
   }
-  int n_work = 0, n_slot = 0, n_join = 0;
-  for (int c0 = 0; c0 < items; c0 += kPlanThreads) {
+  __syncthreads();
+  if (tid < 32) {   // starts of the classes
+    const int x = s_class[2 * tid], y = s_class[2 * tid + 1];
+    int incl = x + y;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (tid >= o) incl += u;
+    }
+    s_class[2 * tid] = incl - x - y;
+    s_class[2 * tid + 1] = incl - y;
+  }
+  __syncthreads();
+  int n_slot = 0, n_join = 0, n_work = 0;
+  for (int c0 = 0; c0 < items; c0 += n_thread) {
     const int i = c0 + tid;
     int r = 0, tok0 = 0, nt = 0, pieces = 0;
     if (i < items) {
-      r = find(i, &tok0);
-      nt = item_tiles(a, load_chunk(a, r), tok0, tpi);
-      pieces = nt <= most ? 1 : (int)((nt + most - 1) / most);
+      r = item(i, &tok0, &nt);
+      pieces = pieces_of(nt);
     }
-    int t_work, t_slot, t_join;
-    const int w = n_work + block_scan(pieces, s_warp, &t_work);
-    const int s = n_slot + block_scan(pieces > 1 ? pieces : 0, s_warp, &t_slot);
-    const int j = n_join + block_scan(pieces > 1 ? 1 : 0, s_warp, &t_join);
-    for (int q = 0; q < pieces; ++q) {
-      ChunkWork x;
-      x.r = r;
-      x.tok0 = tok0;
-      // equal pieces rather than full ones and a remainder
-      x.t0 = (int)((long long)q * nt / pieces);
-      x.t1 = (int)((long long)(q + 1) * nt / pieces);
-      x.slot = pieces > 1 ? s + q : -1;
-      x.pad[0] = x.pad[1] = x.pad[2] = 0;
-      k.ws.work[w + q] = x;
+    // partial results have places by the order of the items: the results do not depend on the schedule
+    int2 t;
+    const bool cut = pieces > 1;
+    const int2 at = block_scan2(make_int2(cut ? pieces : 0, cut ? 1 : 0), s_warp, &t);
+    if (pieces) {
+      const int w = atomicAdd(&s_class[length_class((nt + pieces - 1) / pieces)], pieces);
+      for (int q = 0; q < pieces; ++q) {
+        ChunkWork x;
+        x.r = r;
+        x.tok0 = tok0;
+        x.t0 = (int)((long long)q * nt / pieces);
+        x.t1 = (int)((long long)(q + 1) * nt / pieces);
+        x.slot = cut ? n_slot + at.x + q : -1;
+        x.pad[0] = x.pad[1] = x.pad[2] = 0;
+        k.ws.work[w + q] = x;
+      }
+      if (cut) {
+        ChunkJoin x;
+        x.r = r;
+        x.tok0 = tok0;
+        x.slot = n_slot + at.x;
+        x.n = pieces;
+        k.ws.joins[n_join + at.y] = x;
+      }
     }
-    if (pieces > 1) {
-      ChunkJoin x;
-      x.r = r;
-      x.tok0 = tok0;
-      x.slot = s;
-      x.n = pieces;
-      k.ws.joins[j] = x;
-    }
-    n_work += t_work;
-    n_slot += t_slot;
-    n_join += t_join;
+    n_slot += t.x;
+    n_join += t.y;
   }
+  n_work = items - n_join + n_slot;
   if (tid == 0) {
     ChunkHead h;
     h.n_work = n_work;
     h.n_join = n_join;
     h.slots_per_head = n_slot;
-    h.pad = 0;
+    h.next = n_cta;   // the first n_cta items belong to the CTAs of their number
     *k.ws.head = h;
   }
 }
@@ -202,20 +267,33 @@ __global__ void __launch_bounds__(kPlanThreads, 1) k_chunk_plan(const ChunkArgs 
 // Shared-memory descriptor of a B operand whose N dimension is contiguous: rows are keys of 128 bytes
 // (64 channels), groups of 8 rows 1024 bytes apart, the other 64 channels one k-block further.
 __device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
-  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(kKBlock >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(kKvBlock >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
          ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
-__device__ __forceinline__ void mma_pv(uint32_t tmem_o, uint32_t tmem_p, uint32_t v_addr, uint32_t idesc, bool accumulate) {
+// The tensor cores take a few products ahead of the one they work on and no more, so what the issuing
+// thread does between two of them is time lost: descriptors of whole tiles are made beforehand and a step
+// adds a constant to each (the address field counts 16 bytes and cannot overflow into its neighbour).
+__device__ __forceinline__ void mma_s(uint32_t tmem_s, uint64_t da, uint64_t db, uint32_t idesc) {
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) {
-    const uint64_t db = desc_mn(v_addr + ks * 16 * 128);
-    const uint32_t acc = (accumulate || ks > 0) ? 1u : 0u;
+    const uint64_t qo = (uint64_t)(((ks >> 2) * kKBlock + (ks & 3) * 32) >> 4);
+    const uint64_t ko = (uint64_t)(((ks >> 2) * kKvBlock + (ks & 3) * 32) >> 4);
     asm volatile(
         "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n}\n" ::"r"(tmem_o),
-        "r"(tmem_p + 8u * ks), "l"(db), "r"(idesc), "r"(acc), "r"(0u)
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(tmem_s),
+        "l"(da + qo), "l"(db + ko), "r"(idesc), "r"(ks > 0 ? 1u : 0u)
         : "memory");
   }
+}
+// O (+)= P V: four steps of 16 keys (A = P from tensor memory, 8 columns a step).
+__device__ __forceinline__ void mma_pv(uint32_t tmem_o, uint32_t tmem_p, uint64_t db, uint32_t idesc, bool accumulate) {
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks)
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(tmem_o),
+        "r"(tmem_p + 8u * ks), "l"(db + (uint64_t)((ks * 16 * 128) >> 4)), "r"(idesc), "r"((accumulate || ks > 0) ? 1u : 0u)
+        : "memory");
 }
 __device__ __forceinline__ void tmem_st32(const uint32_t* r, uint32_t taddr) {
   asm volatile(
@@ -240,38 +318,44 @@ __device__ __forceinline__ void tmem_st8(const float* v, uint32_t taddr) {
                "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
-// Q rows of one tile half: (64 channels, G heads, tokens, batch row) boxes.
-__device__ __forceinline__ void q_copy(const CUtensorMap* map, uint32_t dst, uint64_t* bar, int kb, int head, int tok, int b) {
+// One box of 64 channels of a dense tensor: half kb of the channels, from (head, token) of batch row b on;
+// the maps of Q have the heads inside the tokens, those of K and V (swapped) the tokens inside the heads.
+__device__ __forceinline__ void q_copy(const CUtensorMap* map, uint32_t dst, uint64_t* bar, int kb, int head, int tok,
+                                       int b, bool swapped = false) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
       "[%6];\n" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(kb * 64), "r"(head), "r"(tok), "r"(b), "r"(zc_smem_u32(bar))
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(kb * 64), "r"(swapped ? tok : head), "r"(swapped ? head : tok), "r"(b),
+      "r"(zc_smem_u32(bar))
       : "memory");
 }
 __device__ __forceinline__ void expect_bytes(uint64_t* bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(zc_smem_u32(bar)), "r"(bytes) : "memory");
 }
 
-// An item as every role of a CTA derives it from the list.
+// An item as the fetching warp hands it to the other roles.
 struct Item {
-  int r, kv, tok0, ntok;      // request (dense form: batch row), KV head, tokens
+  int r, kv, tok0, ntok;      // request (dense form: batch row), KV head, tokens; r < 0: no more items
   int row0;                   // row of the request's token 0
-  int p_first;
-  int t0, t1, slot;
+  int p_first, t0, t1, slot;
+  int narrow;                 // one tile of rows: the groups take the even and the odd key tiles
   ZcSeen s;
-  int ga[2], ge[2];           // key tiles that group 0 / 1 takes part in (empty: ga >= ge)
+  int ga[2], ge[2];           // key tiles from .. to that group 0 / 1 takes part in (narrow: both all)
   __device__ __forceinline__ int key0(int t) const { return (t < s.nsb ? t : s.wb0 + t - s.nsb) << kTileLog2; }
 };
+static_assert(sizeof(Item) <= kRingInts * 4, "an item fits its place in the ring");
 
 template <bool PAGED>
-__device__ __forceinline__ Item load_item(const ChunkArgs& k, long long idx, int n_work) {
+__device__ __forceinline__ Item load_item(const ChunkArgs& k, long long idx) {
   const ZcPagedArgs& a = k.a;
   Item it;
   const int tpi = 2 * k.tpt;
   int n;
   if (PAGED) {
-    it.kv = (int)(idx / n_work);
-    const ChunkWork w = k.ws.work[idx - (long long)it.kv * n_work];
+    // all heads of a piece beside each other: the list's order, the longest first, holds for all of them
+    const long long at = idx / a.h_kv;
+    it.kv = (int)(idx - at * a.h_kv);
+    const ChunkWork w = k.ws.work[at];
     const Chunk c = load_chunk(a, w.r);
     it.r = w.r;
     it.tok0 = w.tok0;
@@ -282,16 +366,17 @@ __device__ __forceinline__ Item load_item(const ChunkArgs& k, long long idx, int
     it.p_first = c.p0 + w.tok0;
     n = c.n;
   } else {
-    const int unit = (int)(idx / k.items);
+    const int units = a.n_req * a.h_kv, q = (int)(idx / units), unit = (int)(idx - (long long)q * units);
     it.r = unit / a.h_kv;
     it.kv = unit - it.r * a.h_kv;
-    it.tok0 = (k.items - 1 - (int)(idx - (long long)unit * k.items)) * tpi;   // the last, longest rows first
+    it.tok0 = (k.items - 1 - q) * tpi;   // the last, longest rows first
     it.slot = -1;
     it.row0 = 0;
     it.p_first = it.tok0;
     n = k.l;
   }
   it.ntok = min(tpi, n - it.tok0);
+  it.narrow = it.ntok <= k.tpt;
   it.s = zc_seen(it.p_first, it.p_first + it.ntok - 1, a.window, a.sinks, kTileLog2);
   if (!PAGED) {
     it.t0 = 0;
@@ -301,13 +386,94 @@ __device__ __forceinline__ Item load_item(const ChunkArgs& k, long long idx, int
   for (int g = 0; g < 2; ++g) {
     const int first = it.p_first + g * k.tpt, last = it.p_first + min(it.ntok, (g + 1) * k.tpt) - 1;
     const int lo = max(0, first - a.window + 1), hi = max(0, last + 1);
-    const int end = it.s.nsb + max(0, ((hi + kM - 1) >> kTileLog2) - it.s.wb0);
-    const int begin = it.s.nsb > 0 ? 0 : max(0, (lo >> kTileLog2) - it.s.wb0);
-    it.ga[g] = max(it.t0, begin);
-    it.ge[g] = last >= first ? min(it.t1, end) : it.t0;
+    const int end = it.s.nsb + max(0, ((hi + kN - 1) >> kTileLog2) - it.s.wb0);
+    // sinks: from the first tile on, also where the other group's window still reaches back to them
+    const int begin = a.sinks > 0 ? 0 : max(0, (lo >> kTileLog2) - it.s.wb0);
+    it.ga[g] = it.narrow ? it.t0 : max(it.t0, begin);
+    it.ge[g] = it.narrow ? it.t1 : min(it.t1, end);
   }
   return it;
 }
+
+// bar_wait that says whether the phase completed (false: the bound ran out here or elsewhere).
+__device__ __forceinline__ bool bar_wait_ok(uint64_t* bar, uint32_t parity) {
+  bar_wait(bar, parity);
+  return bar_try(bar, parity);
+}
+
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
+      " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 d, a, b;\n"
+      " mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// 2^x of two values without the exp2 unit: x = n + f with n the nearest whole number (the low bits of
+// x + 1.5 * 2^23), 2^f by the polynomial of degree 5 whose largest relative error on |f| <= 1/2 is least
+// (7.5e-8, found by the Remez exchange), n added to the exponent.  x is held at -126 or more.
+__device__ __forceinline__ float2 exp2_poly(float2 x) {
+  x.x = fmaxf(x.x, -126.f);
+  x.y = fmaxf(x.y, -126.f);
+  const float2 big = make_float2(12582912.f, 12582912.f), neg = make_float2(-12582912.f, -12582912.f);
+  const float2 t = add2(x, big), n = add2(t, neg);
+  const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
+  float2 p = fma2(f, make_float2(1.32764721678e-3f, 1.32764721678e-3f), make_float2(9.67554133102e-3f, 9.67554133102e-3f));
+  p = fma2(p, f, make_float2(5.55071327288e-2f, 5.55071327288e-2f));
+  p = fma2(p, f, make_float2(0.24022119724f, 0.24022119724f));
+  p = fma2(p, f, make_float2(0.693146967065f, 0.693146967065f));
+  p = fma2(p, f, make_float2(1.00000007165f, 1.00000007165f));
+  return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
+                     __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+
+// The weights of 64 keys, 2^(v * scale - m), packed to the input type, and their sums (of the unrounded
+// values) by two accumulators.  POLY of every 8 pairs take exp2_poly: the exp2 unit, at a quarter of a
+// warp per cycle and quarter of the SM, would otherwise be what the groups wait for.
+template <typename T, int POLY>
+__device__ __forceinline__ void weights(const float* v, float2 scale, float2 neg_m, float2 (&add)[2], uint32_t* w) {
+#pragma unroll
+  for (int c = 0; c < 32; ++c) {
+    const float2 x = fma2(make_float2(v[2 * c], v[2 * c + 1]), scale, neg_m);
+    const float2 p = (c * POLY) % 8 + POLY > 7 && POLY ? exp2_poly(x) : make_float2(zc_exp2(x.x), zc_exp2(x.y));
+    add[c & 1] = add2(add[c & 1], p);
+    w[c] = pack2<T>(p.x, p.y);
+  }
+}
+
+// The loads that wrote v[0 .. 31] have completed (the operands keep their uses behind the wait).
+__device__ __forceinline__ void tmem_wait32(float* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;\n"
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                 "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+                 "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+                 "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+               :
+               : "memory");
+}
+// One thread of the (converged) warp, the same each time.  What it issues is computed by the whole warp
+// from values that are the same in all lanes: the operands of tcgen05.mma then live in uniform registers
+// instead of being moved there one by one (75 against 48 cycles from one 128 x 64 x 16 product to the next).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+  return p != 0;
+}
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ void groups_sync() { asm volatile("bar.sync 1, 256;\n" ::: "memory"); }   // both groups
 
 template <typename T, bool PAGED>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -318,35 +484,49 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t raw_u = zc_smem_u32(smem_raw);
   const uint32_t base_u = (raw_u + 1023u) & ~1023u;
   char* base = smem_raw + (base_u - raw_u);
-  const uint32_t q_addr = base_u, k_addr = base_u + 2 * kTile, v_addr = k_addr + kKS * kTile;
+  const uint32_t q_addr = base_u, k_addr = base_u + 2 * kTile, v_addr = k_addr + kKS * kKvTile;
   uint64_t* bars = reinterpret_cast<uint64_t*>(base + kTiles);
   uint64_t* q_full = bars;                  // an item's Q tiles landed
-  uint64_t* q_free = bars + 1;              // an item's last S completed
+  uint64_t* q_free = bars + 1;              // both groups' last S of an item completed
   uint64_t* k_full = bars + 2;              // [kKS] key tile landed
-  uint64_t* k_free = k_full + kKS;          // [kKS] both groups' S of that tile completed
+  uint64_t* k_free = k_full + kKS;          // [kKS] both groups are through with that tile
   uint64_t* v_full = k_free + kKS;          // [kVS] value tile landed
-  uint64_t* v_free = v_full + kVS;          // [kVS] both groups' P V of that tile completed
-  uint64_t* s_done = v_free + kVS;          // [2] S_g of a tile completed
-  uint64_t* p_full = s_done + 2;            // [2] the group's four warps have written P_g
-  uint64_t* o_done = p_full + 2;            // [2] the group's last P V of an item completed
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_done + 2);
+  uint64_t* v_free = v_full + kVS;          // [kVS] both groups are through with that tile
+  uint64_t* s_done = v_free + kVS;          // [2][2] S_g of a tile completed, by its place
+  uint64_t* p_full = s_done + 4;            // [2][2] the group's four warps have written P_g
+  uint64_t* o_last = p_full + 4;            // [2] the group's last P V but one of an item completed
+  uint64_t* o_done = o_last + 2;            // [2] the group's last P V of an item completed
+  uint64_t* i_full = o_done + 2;            // [kRingN] an item is in the ring
+  uint64_t* i_free = i_full + kRingN;       // [kRingN] all roles have read it
+  uint64_t* m_free = i_free + kRingN;       // the groups' meeting over a narrow item is over
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(m_free + 1);
+  float2* s_ms = reinterpret_cast<float2*>(base + kTiles + 384);                    // [128] narrow items: group 1's (m, sum)
+  int* ring = reinterpret_cast<int*>(base + kTiles + 384 + 1024);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   if (tid == 0) {
     bar_init(q_full, 1);
-    bar_init(q_free, 1);
+    bar_init(q_free, 2);
+    bar_init(m_free, 1);
     for (int i = 0; i < kKS; ++i) {
       bar_init(&k_full[i], 1);
-      bar_init(&k_free[i], 1);
+      bar_init(&k_free[i], 2);
     }
     for (int i = 0; i < kVS; ++i) {
       bar_init(&v_full[i], 1);
-      bar_init(&v_free[i], 1);
+      bar_init(&v_free[i], 2);
     }
     for (int g = 0; g < 2; ++g) {
-      bar_init(&s_done[g], 1);
-      bar_init(&p_full[g], 4);
+      for (int i = 0; i < 2; ++i) {
+        bar_init(&s_done[2 * g + i], 1);
+        bar_init(&p_full[2 * g + i], 4);
+      }
+      bar_init(&o_last[g], 1);
       bar_init(&o_done[g], 1);
+    }
+    for (int i = 0; i < kRingN; ++i) {
+      bar_init(&i_full[i], 1);
+      bar_init(&i_free[i], 11);   // copies, two warps for the products, eight worker warps
     }
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
@@ -363,20 +543,82 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);
   asm volatile("griddepcontrol.wait;\n" ::: "memory");   // the list of work (and all that came before it)
 
-  const int n_work = PAGED ? k.ws.head->n_work : k.items;
-  const long long n_idx = PAGED ? (long long)n_work * a.h_kv : (long long)k.items * a.n_req * a.h_kv;
+  uint32_t n_item = 0;   // items taken from the ring
+  // Next item of the ring; a whole warp calls.  False: there are no more (or a wait ran out).
+  auto next_item = [&](Item& it) {
+    const uint32_t at = n_item % kRingN;
+    if (!bar_wait_ok(&i_full[at], (n_item / kRingN) & 1u)) return false;
+    const int* src = ring + at * kRingInts;
+    int* dst = reinterpret_cast<int*>(&it);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(Item) / 4); ++i) dst[i] = src[i];
+    __syncwarp();
+    if (lane == 0) bar_arrive(&i_free[at]);
+    ++n_item;
+    return it.r >= 0;
+  };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
-    if (warp == 1) {
+    if (warp == 2) {
+      // ---- items ----
+      if (lane == 0) {
+        const long long n_idx = PAGED ? (long long)k.ws.head->n_work * a.h_kv : (long long)k.items * a.n_req * a.h_kv;
+        long long idx = blockIdx.x;
+        for (uint32_t n = 0;; ++n) {
+          Item it;
+          const bool more = idx < n_idx;
+          if (more) it = load_item<PAGED>(k, idx);
+          if (!more) it.r = -1;
+          const uint32_t at = n % kRingN;
+          if (n >= kRingN && !bar_wait_ok(&i_free[at], (n / kRingN - 1) & 1u)) break;
+          int* dst = ring + at * kRingInts;
+          const int* src = reinterpret_cast<const int*>(&it);
+#pragma unroll
+          for (int i = 0; i < (int)(sizeof(Item) / 4); ++i) dst[i] = src[i];
+          bar_arrive(&i_full[at]);
+          if (!more) break;
+          idx = PAGED ? (long long)atomicAdd(&k.ws.head->next, 1) : idx + gridDim.x;
+        }
+      }
+    } else if (warp == 1) {
       // ---- copies ----
-      uint32_t tile = 0, item = 0;   // key tiles and items (with tiles) so far
-      for (long long idx = blockIdx.x; idx < n_idx; idx += gridDim.x) {
-        const Item it = load_item<PAGED>(k, idx, n_work);
+      uint32_t k_n = 0, v_n = 0, item = 0, meetings = 0;   // tiles, items with tiles, narrow ones among them so far
+      // The n-th tile of keys (or values) into its place; the whole warp calls.
+      auto kv_tile = [&](const Item& it, int t, const CUtensorMap* map, uint32_t at, uint64_t* full, uint64_t* free,
+                         uint32_t places, uint32_t n) {
+        const uint32_t s = n % places;
+        const int key0 = it.key0(t);
+        if (PAGED) {
+          // lane i brings the i-th page of the tile, if any row of the item sees a key of it
+          const int rows = min(kN, 1 << a.page_log2), pk0 = key0 + lane * rows;
+          const bool on = lane < kN / rows && (pk0 < it.s.sink_n || (pk0 < it.s.hi && pk0 + rows > it.s.lo));
+          const int page = on ? a.table[(long long)it.r * a.table_width + (pk0 >> a.page_log2)] : 0;
+          const int pg = page >= 0 && page < a.n_pages ? page : a.n_pages;   // beyond the pool: arrives as zeros
+          const int row = pk0 & ((1 << a.page_log2) - 1);
+          const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, on)) * (uint32_t)rows * (ZC_D * 2);
+          if (lane == 0) {
+            if (n >= places) bar_wait(&free[s], (n / places - 1) & 1u);
+            expect_bytes(&full[s], bytes);
+          }
+          __syncwarp();
+          if (on)
+            for (int kb = 0; kb < 2; ++kb)
+              page_copy(map, at + s * kKvTile + kb * kKvBlock + lane * rows * 128, &full[s], row, kb, it.kv, pg);
+        } else if (lane == 0) {
+          if (n >= places) bar_wait(&free[s], (n / places - 1) & 1u);
+          expect_bytes(&full[s], kKvTile);
+          for (int kb = 0; kb < 2; ++kb) q_copy(map, at + s * kKvTile + kb * kKvBlock, &full[s], kb, it.kv, key0, it.r, true);
+        }
+      };
+      bool met = true;                             // the last item's meeting is waited for (or it had none)
+      Item it;
+      while (next_item(it)) {
         if (it.t0 >= it.t1) continue;
         if (lane == 0) {
           if (item > 0) bar_wait(q_free, (item - 1) & 1u);
-          const int tiles = it.ntok > k.tpt ? 2 : 1;
+          if (!met) bar_wait(m_free, (meetings - 1) & 1u);
+          const int tiles = it.narrow ? 1 : 2;
           expect_bytes(q_full, (uint32_t)(tiles * k.tpt * a.G * ZC_D * 2));
           for (int g = 0; g < tiles; ++g)
             for (int kb = 0; kb < 2; ++kb)
@@ -384,90 +626,92 @@ __global__ void __launch_bounds__(kThreads, 1)
                      it.row0 + it.tok0 + g * k.tpt, PAGED ? 0 : it.r);
         }
         ++item;
-        for (int t = it.t0; t < it.t1; ++t, ++tile) {
-          const int ks = tile % kKS, vs = tile % kVS, key0 = it.key0(t);
-          if (PAGED) {
-            // lane i brings the i-th page of the tile, if any row of the item sees a key of it
-            const int rows = min(kM, 1 << a.page_log2), n_page = kM / rows;
-            const int pk0 = key0 + lane * rows;
-            const bool on = lane < n_page &&
-                            (pk0 < it.s.sink_n || (pk0 < it.s.hi && pk0 + rows > it.s.lo));
-            const int page = on ? a.table[(long long)it.r * a.table_width + (pk0 >> a.page_log2)] : 0;
-            const int pg = page >= 0 && page < a.n_pages ? page : a.n_pages;   // beyond the pool: arrives as zeros
-            const int row = pk0 & ((1 << a.page_log2) - 1);
-            const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, on)) * (uint32_t)rows * (ZC_D * 2);
-            if (lane == 0) {
-              if (tile >= kKS) bar_wait(&k_free[ks], (tile / kKS - 1) & 1u);
-              expect_bytes(&k_full[ks], bytes);
-            }
-            __syncwarp();
-            if (on)
-              for (int kb = 0; kb < 2; ++kb)
-                page_copy(&kmap, k_addr + ks * kTile + kb * kKBlock + lane * rows * 128, &k_full[ks], row, kb, it.kv, pg);
-            if (lane == 0) {
-              if (tile >= kVS) bar_wait(&v_free[vs], (tile / kVS - 1) & 1u);
-              expect_bytes(&v_full[vs], bytes);
-            }
-            __syncwarp();
-            if (on)
-              for (int kb = 0; kb < 2; ++kb)
-                page_copy(&vmap, v_addr + vs * kTile + kb * kKBlock + lane * rows * 128, &v_full[vs], row, kb, it.kv, pg);
-          } else if (lane == 0) {
-            if (tile >= kKS) bar_wait(&k_free[ks], (tile / kKS - 1) & 1u);
-            tma_key_tile(&kmap, k_addr + ks * kTile, &k_full[ks], key0, it.kv, it.r);
-            if (tile >= kVS) bar_wait(&v_free[vs], (tile / kVS - 1) & 1u);
-            tma_key_tile(&vmap, v_addr + vs * kTile, &v_full[vs], key0, it.kv, it.r);
+        met = !it.narrow;
+        meetings += it.narrow ? 1u : 0u;
+        // keys run two tiles ahead of the values, as their products do
+        for (int t = it.t0 - 2; t < it.t1; ++t) {
+          if (t >= it.t0) {
+            kv_tile(it, t, &vmap, v_addr, v_full, v_free, kVS, v_n);
+            ++v_n;
+          }
+          if (t + 2 < it.t1) {
+            kv_tile(it, t + 2, &kmap, k_addr, k_full, k_free, kKS, k_n);
+            ++k_n;
           }
         }
       }
-    } else if (warp == 0 && lane == 0) {
-      // ---- matrix products ----
-      const uint32_t idesc_s = instr_desc<T>();
+    } else {
+      // ---- matrix products of group g ----
+      // Per tile: O += P V, then the group's S two of its tiles on, into the place that this P leaves.  Each
+      // group has a warp of its own for them: the tensor cores queue only a few products, and what one warp
+      // spends on barriers and commits the other's products fill.
+      const int g = uniform(warp == 0 ? 0 : 1);
+      const uint32_t tm = (uint32_t)uniform((int)tmem), tm_s = tm + g * kM, tm_o = tm + (2 + g) * kM;
+      const uint32_t idesc_s = (instr_desc<T>() & ~(0x3Fu << 17)) | ((uint32_t)(kN >> 3) << 17);
       const uint32_t idesc_pv = instr_desc<T>() | (1u << 16);   // B with its N dimension contiguous
-      uint32_t tile = 0, item = 0, n_s[2] = {0, 0};             // n_s: S tiles of a group whose P V is issued
-      for (long long idx = blockIdx.x; idx < n_idx; idx += gridDim.x) {
-        const Item it = load_item<PAGED>(k, idx, n_work);
-        if (it.t0 >= it.t1) continue;
+      const uint64_t q_desc = smem_desc(q_addr), k_desc = smem_desc(k_addr), v_desc = desc_mn(v_addr);
+      uint32_t item = 0, n_s = 0, n_p = 0;                 // items so far; tiles of the group whose S / P V is issued
+      uint32_t ks = 0, kp = 0, vs = 0, vp = 0;             // place and phase of the next key and value tile
+      Item it;
+      while (next_item(it)) {
+        const int t0 = uniform(it.t0), n = uniform(it.t1) - t0, narrow = uniform(it.narrow);
+        const int ga = uniform(g ? it.ga[1] : it.ga[0]) - t0, ge = uniform(g ? it.ge[1] : it.ge[0]) - t0;
+        if (n <= 0) continue;
+        const int ahead = narrow ? 4 : 2, step = narrow ? 2 : 1;
+        const uint64_t qd = q_desc + (uint64_t)((narrow ? 0 : g) * (kTile >> 4));
+        auto mine = [&](int i) { return narrow ? (i & 1) == g : i >= ga && i < ge; };
+        auto keys = [&](int i) {        // the item's key tile i: its S, and the tile's release
+          bar_wait(&k_full[ks], kp);
+          const uint64_t kd = k_desc + (uint64_t)(ks * (kKvTile >> 4));
+          const uint32_t place = n_s & 1u;
+          const bool on = mine(i);
+          if (elect_one()) {
+            if (on) {
+              mma_s(tm_s + place * kN, qd, kd, idesc_s);
+              mma_commit(&s_done[2 * g + place]);
+            }
+            mma_commit(&k_free[ks]);
+            if (i + 1 == n) mma_commit(q_free);
+          }
+          __syncwarp();
+          n_s += on ? 1u : 0u;
+          if (++ks == kKS) {
+            ks = 0;
+            kp ^= 1u;
+          }
+        };
         bar_wait(q_full, item & 1u);
         ++item;
-        bar_wait(&k_full[tile % kKS], (tile / kKS) & 1u);
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-          if (it.ga[g] == it.t0 && it.ga[g] < it.ge[g]) {
-            mma_tile(tmem + g * kM, q_addr + g * kTile, k_addr + (tile % kKS) * kTile, idesc_s);
-            mma_commit(&s_done[g]);
-          }
-        mma_commit(&k_free[tile % kKS]);
-        if (it.t0 + 1 == it.t1) mma_commit(q_free);
-        for (int t = it.t0; t < it.t1; ++t, ++tile) {
-          const uint32_t vs = tile % kVS, next = tile + 1, ks1 = next % kKS;
-          const uint32_t v_tile = v_addr + vs * kTile, k_next = k_addr + ks1 * kTile;
-          bool v_ready = false, k_ready = false;
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            if (t >= it.ga[g] && t < it.ge[g]) {
-              bar_wait(&p_full[g], n_s[g] & 1u);
-              ++n_s[g];
-              if (!v_ready) bar_wait(&v_full[vs], (tile / kVS) & 1u);
-              v_ready = true;
-              tc_fence_after();
-              mma_pv(tmem + (2 + g) * kM, tmem + g * kM, v_tile, idesc_pv, t > it.ga[g]);
-              if (t + 1 == it.ge[g]) mma_commit(&o_done[g]);
+#pragma unroll 1
+        for (int i = 0; i < min(n, ahead); ++i) keys(i);
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+          bar_wait(&v_full[vs], vp);
+          const uint64_t vd = v_desc + (uint64_t)(vs * (kKvTile >> 4));
+          const bool on = mine(i);
+          if (on) {
+            const uint32_t place = n_p & 1u;
+            const bool first = narrow ? i < 2 : i == ga;
+            const bool last = narrow ? i + step >= n : i + 1 == ge;
+            const bool last_but_one = !last && (narrow ? i + 2 * step >= n : i + 2 == ge);
+            bar_wait(&p_full[2 * g + place], (n_p >> 1) & 1u);
+            tc_fence_after();
+            if (elect_one()) {
+              mma_pv(tm_o, tm_s + place * kN, vd, idesc_pv, !first);
+              mma_commit(&v_free[vs]);
+              if (last_but_one) mma_commit(&o_last[g]);
+              if (last) mma_commit(&o_done[g]);
             }
-            if (t + 1 >= it.ga[g] && t + 1 < it.ge[g]) {
-              if (!k_ready) bar_wait(&k_full[ks1], (next / kKS) & 1u);
-              k_ready = true;
-              tc_fence_after();
-              mma_tile(tmem + g * kM, q_addr + g * kTile, k_next, idesc_s);
-              mma_commit(&s_done[g]);
-            }
+            ++n_p;
+          } else if (elect_one()) {
+            mma_commit(&v_free[vs]);
           }
-          mma_commit(&v_free[vs]);
-          if (t + 1 < it.t1) {
-            if (!k_ready) bar_wait(&k_full[ks1], (next / kKS) & 1u);
-            mma_commit(&k_free[ks1]);
-            if (t + 2 == it.t1) mma_commit(q_free);
+          __syncwarp();
+          if (++vs == kVS) {
+            vs = 0;
+            vp ^= 1u;
           }
+          if (i + ahead < n) keys(i + ahead);
         }
       }
     }
@@ -476,109 +720,156 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int g = (warp >> 2) - 1, quarter = warp & 3, row = quarter * 32 + lane;
     const int tok_in = row / a.G, head_in = row - tok_in * a.G;
     const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
-    const uint32_t tmem_s = tmem + lane_off + (uint32_t)g * kM, tmem_o = tmem + lane_off + (uint32_t)(2 + g) * kM;
+    const uint32_t tmem_g = tmem + lane_off + (uint32_t)g * kM, tmem_o = tmem + lane_off + (uint32_t)(2 + g) * kM;
     const float scale = kLog2e * rsqrtf((float)ZC_D);
-    uint32_t tile0 = 0, n_s = 0, n_o = 0;
-    for (long long idx = blockIdx.x; idx < n_idx; idx += gridDim.x) {
-      const Item it = load_item<PAGED>(k, idx, n_work);
-      const int tok = g * k.tpt + tok_in;                           // token of the item
+    uint32_t tile0 = 0, n_s = 0, n_o = 0, n_last = 0;
+    Item it;
+    while (next_item(it)) {
+      const int rows_at = it.narrow ? 0 : g;                         // which tile of rows
+      const int tok = rows_at * k.tpt + tok_in;                      // token of the item
       const bool valid = tok_in < k.tpt && tok < it.ntok;
       const int pos = valid ? it.p_first + tok : -1;
-      const int first = it.p_first + g * k.tpt, last = it.p_first + min(it.ntok, (g + 1) * k.tpt) - 1;
+      const int first = it.p_first + rows_at * k.tpt;
+      const int last = it.p_first + min(it.ntok, (rows_at + 1) * k.tpt) - 1;
       const int ga = g ? it.ga[1] : it.ga[0], ge = g ? it.ge[1] : it.ge[0];
+      const int step = it.narrow ? 2 : 1, t_first = it.narrow ? it.t0 + g : ga;
       float m_run = kNoMax, s_run = 0.f;
-      for (int t = ga; t < ge; ++t) {
+      for (int t = t_first; t < ge; t += step) {
         const int key0 = it.key0(t);
-        float v[kM];
-        bar_wait(&s_done[g], n_s & 1u);
+        const uint32_t place = n_s & 1u, tmem_s = tmem_g + place * kN;
+        float v[kN];
+        bar_wait(&s_done[2 * g + place], (n_s >> 1) & 1u);
         ++n_s;
         tc_fence_after();
-        tmem_ld128(v, tmem_s);
-        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        if (key0 + kM - 1 > first || (key0 <= last - a.window && key0 + kM > a.sinks)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) tmem_ld32_nowait(v + 32 * h, tmem_s + 32 * h);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) tmem_wait32(v + 32 * h);
+        const bool edge = key0 + kN - 1 > first || (key0 <= last - a.window && key0 + kN > a.sinks);
+        if (edge) {
           // the tile crosses the diagonal, the window's edge or the end of the sinks
           const int e_hi = pos - key0, e_lo = max(pos - a.window, -1) - key0, e_sink = a.sinks - key0;
 #pragma unroll
-          for (int e = 0; e < kM; ++e) {
+          for (int e = 0; e < kN; ++e)
             if (!(e <= e_hi && (e > e_lo || e < e_sink))) v[e] = -INFINITY;
-            mx4[e & 3] = fmaxf(mx4[e & 3], v[e]);
-          }
           // values that no row of the item sees may hold anything (a weight of 0 times NaN is NaN)
-          if (key0 + kM > it.s.hi || (key0 < it.s.lo && key0 + kM > it.s.sink_n)) {
+          if (key0 + kN > it.s.hi || (key0 < it.s.lo && key0 + kN > it.s.sink_n)) {
             const uint32_t tile = tile0 + (uint32_t)(t - it.t0), vs = tile % kVS;
             bar_wait(&v_full[vs], (tile / kVS) & 1u);
-            const int key = key0 + row;
+            const int key = key0 + (row & (kN - 1));               // a thread clears 64 of a key's channels
             if (key >= it.s.hi || (key < it.s.lo && key >= it.s.sink_n)) {
-              char* at = base + (v_addr - base_u) + vs * kTile + row * 128;
+              char* at = base + (v_addr - base_u) + vs * kKvTile + (row / kN) * kKvBlock + (row & (kN - 1)) * 128;
 #pragma unroll
-              for (int c = 0; c < 16; ++c)
-                *reinterpret_cast<uint4*>(at + (c >> 3) * kKBlock + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+              for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(at + c * 16) = make_uint4(0, 0, 0, 0);
             }
             async_proxy_fence();
           }
-        } else {
-#pragma unroll
-          for (int e = 0; e < kM; ++e) mx4[e & 3] = fmaxf(mx4[e & 3], v[e]);
         }
-        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale;
+        float mx4[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+        for (int e = 4; e < kN; e += 8)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mx4[i] = e + 4 < kN ? max3(mx4[i], v[e + i], v[e + 4 + i]) : fmaxf(mx4[i], v[e + i]);
+        const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * scale;
         const bool grow = mx > m_run + kTau;
-        if (__any_sync(0xffffffffu, grow && t > ga)) {
+        if (__any_sync(0xffffffffu, grow)) {
           const float alpha = grow ? zc_exp2(m_run - mx) : 1.f;
+          if (t > t_first) {
+            // O has every product up to the tile before once the next tile's S is there (it was issued behind
+            // them), or, at the last tile, once they say so themselves
+            if (t + step < ge) bar_wait(&s_done[2 * g + (n_s & 1u)], (n_s >> 1) & 1u);
+            else bar_wait(&o_last[g], n_last & 1u);
+            tc_fence_after();
 #pragma unroll 1
-          for (int q8 = 0; q8 < 16; ++q8) {
-            float o[8];
-            tmem_ld8(o, tmem_o + 8 * q8);
+            for (int q8 = 0; q8 < 16; ++q8) {
+              float o[8];
+              tmem_ld8(o, tmem_o + 8 * q8);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] *= alpha;
-            tmem_st8(o, tmem_o + 8 * q8);
+              for (int e = 0; e < 8; ++e) o[e] *= alpha;
+              tmem_st8(o, tmem_o + 8 * q8);
+            }
           }
+          s_run *= alpha;
+          if (grow) m_run = mx;
         }
-        if (grow) {
-          s_run *= zc_exp2(m_run - mx);
-          m_run = mx;
-        }
-        float add[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint32_t w[32];
-#pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            const float p0 = zc_exp2(fmaf(v[64 * half + 2 * c], scale, -m_run));
-            const float p1 = zc_exp2(fmaf(v[64 * half + 2 * c + 1], scale, -m_run));
-            add[c & 1] += p0;
-            add[2 + (c & 1)] += p1;
-            w[c] = pack2<T>(p0, p1);
-          }
-          tmem_st32(w, tmem_s + 32 * half);
-        }
-        s_run += (add[0] + add[1]) + (add[2] + add[3]);
+        const float2 sc2 = make_float2(scale, scale), m2 = make_float2(-m_run, -m_run);
+        float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        uint32_t w[32];
+        if (edge) weights<T, 0>(v, sc2, m2, add, w);   // hidden keys weigh 0 exactly
+        else weights<T, kPoly>(v, sc2, m2, add, w);
+        tmem_st32(w, tmem_s);
         asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) bar_arrive(&p_full[g]);
+        if (lane == 0) bar_arrive(&p_full[2 * g + place]);
+        s_run += (add[0].x + add[0].y) + (add[1].x + add[1].y);
       }
+      if (ge - t_first > step) ++n_last;   // an item of two or more of this group's tiles
       tile0 += (uint32_t)max(0, it.t1 - it.t0);
       // ---- the row's output and log-sum-exp, or its partial result ----
-      const bool any = ga < ge;
+      const bool any = t_first < ge;
       if (any) {
         bar_wait(&o_done[g], n_o & 1u);
         ++n_o;
         tc_fence_after();
       }
+      const bool meet = it.narrow && it.t0 < it.t1;
+      const bool other = meet && it.t0 + 1 < it.t1;                  // group 1 has a share of a narrow item
+      float f_own = 1.f, f_other = 0.f;
+      if (meet) {
+        // group 1's sums and its O, 32 channels at a time through two halves of the second Q tile's place, to
+        // group 0 (which has read a half by the time the other half's values are announced)
+        if (g == 1) s_ms[row] = make_float2(m_run, s_run);
+        groups_sync();
+        if (g == 0 && other) {
+          const float2 o = s_ms[row];
+          const float m = fmaxf(m_run, o.x);
+          f_own = zc_exp2(m_run - m);
+          f_other = zc_exp2(o.x - m);
+          s_run = s_run * f_own + o.y * f_other;
+          m_run = m;
+        }
+      }
+      const bool writer = valid && !(it.narrow && g == 1);
+      const bool some = any && s_run > 0.f;
+      const float inv = some ? 1.f / s_run : 0.f;
       const int h = it.kv * a.G + head_in;
-      if (it.slot < 0) {
-        const bool some = any && s_run > 0.f;
-        const float inv = some ? 1.f / s_run : 0.f;
-        const long long at = (PAGED ? 0 : it.r * k.o_req) + (long long)(it.row0 + it.tok0 + tok) * k.o_row + h * k.o_head;
-        T* orow = reinterpret_cast<T*>(a.out) + at;
+      const long long at = (PAGED ? 0 : it.r * k.o_req) + (long long)(it.row0 + it.tok0 + tok) * k.o_row + h * k.o_head;
+      float* pr = nullptr;
+      if (PAGED && it.slot >= 0)
+        pr = k.ws.parts + (((long long)it.kv * k.ws.head->slots_per_head + it.slot) * kItemRows + rows_at * kM + row) * kPartStride;
 #pragma unroll 1
-        for (int q4 = 0; q4 < 4; ++q4) {
-          float o[32];
-          if (any) {
-            tmem_ld32_nowait(o, tmem_o + 32 * q4);
-            asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
+      for (int q4 = 0; q4 < 4; ++q4) {
+        float o[32];
+        if (any) {
+          tmem_ld32_nowait(o, tmem_o + 32 * q4);
+          tmem_wait32(o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+        }
+        if (other) {
+          float4* xr = reinterpret_cast<float4*>(base + kTile) + row * 16 + 8 * (q4 & 1);   // 64 channels a row
+          if (g == 1) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) xr[c ^ (row & 7)] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+            async_proxy_fence();
           }
-          if (valid) {
+          groups_sync();
+          if (g == 0) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              const float4 x = xr[c ^ (row & 7)];
+              o[4 * c] = o[4 * c] * f_own + x.x * f_other;
+              o[4 * c + 1] = o[4 * c + 1] * f_own + x.y * f_other;
+              o[4 * c + 2] = o[4 * c + 2] * f_own + x.z * f_other;
+              o[4 * c + 3] = o[4 * c + 3] * f_own + x.w * f_other;
+            }
+          }
+        }
+        if (writer) {
+          if (!pr) {
+            T* orow = reinterpret_cast<T*>(a.out) + at + 32 * q4;
 #pragma unroll
             for (int c4 = 0; c4 < 4; ++c4) {
               uint4 w = make_uint4(pack2<T>(o[8 * c4] * inv, o[8 * c4 + 1] * inv),
@@ -586,32 +877,23 @@ __global__ void __launch_bounds__(kThreads, 1)
                                    pack2<T>(o[8 * c4 + 4] * inv, o[8 * c4 + 5] * inv),
                                    pack2<T>(o[8 * c4 + 6] * inv, o[8 * c4 + 7] * inv));
               if (!some) w = make_uint4(0, 0, 0, 0);
-              *reinterpret_cast<uint4*>(orow + 32 * q4 + 8 * c4) = w;
+              *reinterpret_cast<uint4*>(orow + 8 * c4) = w;
             }
-          }
-        }
-        if (valid && a.lse) a.lse[at / ZC_D] = some ? m_run + log2f(s_run) : -INFINITY;
-      } else {
-        float* pr = k.ws.parts + (((long long)it.kv * k.ws.head->slots_per_head + it.slot) * kItemRows + g * kM + row) *
-                                     kPartStride;
-        if (valid) *reinterpret_cast<float4*>(pr) = make_float4(m_run, any ? s_run : 0.f, 0.f, 0.f);
-#pragma unroll 1
-        for (int q4 = 0; q4 < 4; ++q4) {
-          float o[32];
-          if (any) {
-            tmem_ld32_nowait(o, tmem_o + 32 * q4);
-            asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
           } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0.f;
-          }
-          if (valid) {
 #pragma unroll
             for (int c = 0; c < 8; ++c)
               *reinterpret_cast<float4*>(pr + 4 + 32 * q4 + 4 * c) =
                   make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
           }
         }
+      }
+      if (writer) {
+        if (!pr && a.lse) a.lse[at / ZC_D] = some ? m_run + log2f(s_run) : -INFINITY;
+        if (pr) *reinterpret_cast<float4*>(pr) = make_float4(m_run, any ? s_run : 0.f, 0.f, 0.f);
+      }
+      if (meet) {
+        groups_sync();   // the second Q tile's place and the sums are free
+        if (tid == 128) bar_arrive(m_free);
       }
       // this row's O is in registers or memory: the next item's products may overwrite it
       tc_fence_before();
@@ -624,25 +906,29 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kCols) : "memory");
 }
 
-// Rows of the items that were worked on in pieces: a warp per row.
+// Rows of the items that were worked on in pieces: a CTA takes 16 rows of an item, a warp two of them.
 template <typename T> __global__ void __launch_bounds__(256) k_chunk_join(const ChunkArgs k) {
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const ZcPagedArgs& a = k.a;
   const ChunkHead hd = *k.ws.head;
-  const int lane = threadIdx.x & 31;
-  const long long n = (long long)hd.n_join * a.h_kv * kItemRows;
-  for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) >> 5; i < n; i += (long long)gridDim.x * 8) {
-    const int row = (int)(i % kItemRows), g = row / kM, in = row % kM;
-    const long long job = i / kItemRows;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long n = (long long)hd.n_join * a.h_kv * (kItemRows / 16);
+  for (long long i = blockIdx.x; i < n; i += gridDim.x) {
+    const long long job = i / (kItemRows / 16);
+    const int row16 = (int)(i - job * (kItemRows / 16)) * 16;
     const int kv = (int)(job / hd.n_join);
     const ChunkJoin j = k.ws.joins[job - (long long)kv * hd.n_join];
     const Chunk c = load_chunk(a, j.r);
-    const int tok_in = in / a.G, tok = j.tok0 + g * k.tpt + tok_in;
-    if (tok_in >= k.tpt || tok >= c.n) continue;
-    const long long at = (long long)(c.row0 + tok) * a.h_q + kv * a.G + (in - tok_in * a.G);
-    join_row<T>(a.out, a.lse, at, lane, j.n, [&](int q) {
-      return k.ws.parts + (((long long)kv * hd.slots_per_head + j.slot + q) * kItemRows + row) * kPartStride;
-    });
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int row = row16 + warp + 8 * u, g = row / kM, in = row % kM;
+      const int tok_in = in / a.G, tok = j.tok0 + g * k.tpt + tok_in;
+      if (tok_in >= k.tpt || tok >= c.n) continue;
+      const long long at = (long long)(c.row0 + tok) * a.h_q + kv * a.G + (in - tok_in * a.G);
+      join_row<T>(a.out, a.lse, at, lane, j.n, [&](int q) {
+        return k.ws.parts + (((long long)kv * hd.slots_per_head + j.slot + q) * kItemRows + row) * kPartStride;
+      });
+    }
   }
 }
 
@@ -696,16 +982,31 @@ bool make_q_map(CUtensorMap* map, const void* q, int dtype, int h_q, int G, long
   return zc_encode_map(map, dtype, 4, q, dims, strides, box);
 }
 
+// Dense K or V as (channels, tokens, KV heads, batch rows), boxes of 64 channels x 64 tokens.
+bool make_dense_map(CUtensorMap* map, const void* x, const zc_config& cfg, int l, const int64_t* ks) {
+  const cuuint64_t dims[4] = {ZC_D, (cuuint64_t)l, (cuuint64_t)cfg.n_kv_heads, (cuuint64_t)cfg.batch};
+  const long long s[3] = {ks[2], cfg.n_kv_heads > 1 ? ks[1] : ZC_D, cfg.batch > 1 ? ks[0] : ZC_D};
+  cuuint64_t strides[3];
+  for (int i = 0; i < 3; ++i) {
+    if (s[i] <= 0 || (s[i] & 7)) return false;
+    strides[i] = (cuuint64_t)s[i] * 2;
+  }
+  const cuuint32_t box[4] = {64, kN, 1, 1};
+  return zc_encode_map(map, cfg.dtype, 4, x, dims, strides, box);
+}
+
 template <typename T>
 int launch_chunk(zc_pages* p, const ChunkArgs& k, const CUtensorMap& qmap, cudaStream_t st) {
   cudaError_t e = ready<T, true>();
   if (e != cudaSuccess) return e;
-  k_chunk_plan<<<1, kPlanThreads, 0, st>>>(k, p->n_sm);
+  // one thread per item or request where they are few: the sums over the block then pass through few warps
+  const long long most = std::max<long long>(k.a.n_req, k.a.n_rows / (2 * k.tpt) + k.a.n_req);
+  k_chunk_plan<<<1, most <= 128 ? 128 : most <= 512 ? 512 : kPlanThreads, 0, st>>>(k, p->n_sm);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  e = zc_launch_early(k_chunk_attention<T, true>, dim3(p->n_sm), dim3(kThreads), kSmem, st, k, qmap, p->k128, p->v128);
+  e = zc_launch_early(k_chunk_attention<T, true>, dim3(p->n_sm), dim3(kThreads), kSmem, st, k, qmap, p->k64, p->v64);
   if (e != cudaSuccess) return e;
-  e = zc_launch_early(k_chunk_join<T>, dim3(2 * p->n_sm), dim3(256), 0, st, k);
+  e = zc_launch_early(k_chunk_join<T>, dim3(8 * p->n_sm), dim3(256), 0, st, k);
   p->launches += 3;
   return e;
 }
@@ -756,8 +1057,7 @@ int zc_launch_prefill_window(zc_cache* c, const void* Q, const void* K, const vo
   memset(&kmap, 0, sizeof(kmap));
   memset(&vmap, 0, sizeof(vmap));
   if (!make_q_map(&qmap, Q, cfg.dtype, cfg.n_q_heads, k.a.G, l, cfg.batch, qs[1], qs[2], qs[0]) ||
-      !make_key_map(&kmap, K, cfg.dtype, l, cfg.n_kv_heads, cfg.batch, ks) ||
-      !make_key_map(&vmap, V, cfg.dtype, l, cfg.n_kv_heads, cfg.batch, ks))
+      !make_dense_map(&kmap, K, cfg, l, ks) || !make_dense_map(&vmap, V, cfg, l, ks))
     return (int)cudaErrorNotSupported;
   const long long n = (long long)k.items * cfg.batch * cfg.n_kv_heads;
   const int grid = n < c->n_sm ? (int)n : c->n_sm;

@@ -490,9 +490,9 @@ bool zc_page_maps(zc_pages* p) {
                               (cuuint64_t)p->cfg.n_pages};
   const cuuint64_t strides[4] = {(cuuint64_t)s[1] * 2, 128, (cuuint64_t)s[2] * 2, (cuuint64_t)s[0] * 2};
   const cuuint32_t small[5] = {64, kBlk, 2, 1, 1};
-  const cuuint32_t large[5] = {64, (cuuint32_t)(p->cfg.page_size < kM ? p->cfg.page_size : kM), 1, 1, 1};
+  const cuuint32_t large[5] = {64, (cuuint32_t)(p->cfg.page_size < 64 ? p->cfg.page_size : 64), 1, 1, 1};
   struct { CUtensorMap* map; void* at; const cuuint32_t* box; } todo[4] = {
-      {&p->k16, p->k, small}, {&p->v16, p->v, small}, {&p->k128, p->k, large}, {&p->v128, p->v, large}};
+      {&p->k16, p->k, small}, {&p->v16, p->v, small}, {&p->k64, p->k, large}, {&p->v64, p->v, large}};
   for (auto& t : todo)
     if (!zc_encode_map(t.map, p->cfg.dtype, 5, t.at, dims, strides, t.box)) return false;
   p->maps_ready = true;

@@ -16,7 +16,7 @@ struct zc_pages {
   int G, page_log2, n_sm;
   bool maps_ready;
   CUtensorMap k16, v16;    // boxes of 16 tokens x 128 elements (two 128-byte halves)
-  CUtensorMap k128, v128;  // boxes of min(page, 128) tokens x 64 elements
+  CUtensorMap k64, v64;    // boxes of min(page, 64) tokens x 64 elements
   long long launches;
 };
 
