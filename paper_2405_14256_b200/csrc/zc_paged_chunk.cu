@@ -8,22 +8,22 @@
 // even and the odd key tiles, and their results meet at the end), and the key tiles (64 keys) that any
 // of its rows sees: those of the first `sinks` tokens, then those of the window.  The CTAs are
 // persistent, one per SM; each works through items until there are none:
-//   warp 2      fetches the items ahead of the others (for pages from a common counter, the longest first)
+//   warp 2      walks the CTA's items ahead of the others
 //   warp 1      the copies: Q by one box per tile half, K and V page by page (a lane per page)
 //   warps 0, 3  the matrix products of group 0 and 1, tcgen05.mma with accumulators in tensor memory:
 //               S_g = Q_g K^T (both K-major in shared memory), 128 x 64, and O_g += P_g V (P_g in tensor
 //               memory over the first half of its S, V with its channels contiguous), 128 x 128
-//   warps 4-7, 8-11  groups 0 and 1, one row per thread: running maximum (O rescaled when it grows by
-//               more than 8, base 2) and sum in fp32, P rounded to the input type, output and log-sum-exp
+//   warps 4-7, 8-11  groups 0 and 1, one row per thread: running maximum (renewed, and O rescaled, when the
+//               weights' sum shows it to be far behind) and sum in fp32, P rounded to the input type, output and
+//               log-sum-exp
 // Each group has two places for S, and S of a key tile is computed two tiles ahead: a group turns one S
 // after the other into P without waiting for a product, and the tensor cores' work hides behind that of
 // the groups (and the other way round).  With 128 keys to a tile and one place for S, the chain product -
 // weights - product left either side idle half of the time (5000 cycles per 256 rows x 128 keys).  The
 // next item's Q and first key tiles arrive while this one's output is written.
-// For pages the list of items is made on the device (k_chunk_plan: lengths stay there).  Where a call has
-// few items for the GPU, those with many key tiles are cut into pieces along the keys, and k_chunk_join
-// puts the pieces together in their order.
-#include <algorithm>
+// For pages the lengths are on the device, and every CTA finds its own share there: the items of all heads,
+// laid end to end with their cost in tiles, are cut into as many equal stretches as there are CTAs.  An item
+// that a border cuts is worked on in pieces along its keys; k_chunk_join puts them together in their order.
 #include <cstring>
 #include "zc_paged.cuh"
 #include "zc_layout.cuh"
@@ -41,32 +41,33 @@ constexpr int kTiles = 2 * kTile + (kKS + kVS) * kKvTile;   // 224 KB
 constexpr int kRingN = 2;                             // items fetched ahead
 constexpr int kRingInts = 24;
 constexpr int kSmem = kTiles + 1024 + 384 + 1024 + kRingN * kRingInts * 4;   // alignment, barriers, (m, sum) of group 1
-constexpr int kPoly = 2;                              // of 8 pairs of weights, those without the exp2 unit
-constexpr float kTau = 8.f;
-constexpr float kNoMax = -1e30f;
+#ifndef KPOLY
+#define KPOLY 0
+#endif
+constexpr int kPoly = KPOLY;                              // of 8 pairs of weights, those without the exp2 unit
+constexpr float kNoMax = -1e30f;                      // running maximum before any key
+constexpr float kTau = 3.f;                           // a new maximum is taken where it exceeds the old by this (base 2)
+constexpr float kBigSum = 1024.f;                     // ... and looked for where a tile's weights sum to more than this
+constexpr float kTopPoly = 16.f;                      // ... or one that the exp2 unit did not compute has this exponent
 constexpr int kPartStride = ZC_PART_STRIDE;           // m, sum, -, -, acc[128]
 constexpr int kItemRows = 2 * kM;
-// Pieces: at most kPieces key-tile ranges of full length over all heads, and no more remainders.
-constexpr int kPieces = 2 * ZC_PAGED_MAX_CTAS;
-constexpr int kMaxSlots = 2 * kPieces;
-constexpr int kPlanThreads = 1024;
-constexpr int kReqShared = 2048;                      // requests whose lengths the planner keeps in shared memory
+constexpr int kMaxItems = 13000;                      // items of a head, and requests, that a call may have: what the
+                                                      // prologue keeps in the tiles' shared memory (16 bytes each)
+constexpr int kItemCost = 6;                          // of an item beside its tiles: Q, first product, output (half tiles)
+constexpr int kMinPiece = 8;                          // tiles; below, joining costs more than the even share gains
 
-// One piece of work: tokens tok0 ... of request r (one item), key tiles t0 .. t1 - 1 of those it sees.
-struct ChunkWork {
-  int r, tok0, t0, t1;
-  int slot;        // -1: the whole item; else its partial results' place among one head's
-  int pad[3];
+// Where a CTA's share begins: item `item` of all heads' (head * items + item of the head), key tile t of it.
+struct Border { int item, t; };
+// The item that the border before CTA c cuts, written by the first such CTA of the item.
+struct ChunkJoin {
+  int on, r, tok0, kv;
+  int first, last;    // CTAs whose shares begin inside the item
+  int pad[2];
 };
-struct ChunkJoin { int r, tok0, slot, n; };
-struct ChunkHead { int n_work, n_join, slots_per_head, next; };   // next: the first item that no CTA has taken
-
 struct ChunkWs {
-  ChunkHead* head;
-  int* item_start;    // [n_req + 1] items before a request
-  ChunkWork* work;
-  ChunkJoin* joins;
-  float* parts;       // [slot][256][132]
+  ChunkJoin* joins;   // [CTA]
+  int* used;          // [CTA] its share is not empty
+  float* parts;       // [CTA][2][256][132]: the piece at its share's start, the one at its end
 };
 
 struct ChunkArgs {
@@ -95,173 +96,158 @@ __device__ __forceinline__ int item_tiles(const ZcPagedArgs& a, const Chunk& c, 
   return zc_seen(c.p0 + tok0, c.p0 + last, a.window, a.sinks, kTileLog2).nb;
 }
 
-// Exclusive sums over the block of two counts at once, and their totals.
-__device__ __forceinline__ int2 block_scan2(int2 v, int2* s_warp, int2* total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warp = blockDim.x >> 5;
-  int2 incl = v;
+// Exclusive sum over the kThreads threads, and the total.
+__device__ __forceinline__ long long block_scan(long long v, long long* s_warp, long long* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long incl = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, incl.x, o), y = __shfl_up_sync(0xffffffffu, incl.y, o);
-    if (lane >= o) {
-      incl.x += x;
-      incl.y += y;
-    }
+    const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += u;
   }
   __syncthreads();
   if (lane == 31) s_warp[warp] = incl;
   __syncthreads();
-  int2 before = make_int2(incl.x - v.x, incl.y - v.y);
-  total->x = total->y = 0;
-  for (int w = 0; w < n_warp; ++w) {
-    const int2 u = s_warp[w];
-    if (w < warp) {
-      before.x += u.x;
-      before.y += u.y;
-    }
-    total->x += u.x;
-    total->y += u.y;
+  long long before = incl - v;
+  *total = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    const long long u = s_warp[w];
+    if (w < warp) before += u;
+    *total += u;
   }
   return before;
 }
 
-// Piece lengths in 64 classes, four to a power of two, the longest class first.
-__device__ __forceinline__ int length_class(int n) {
-  if (n < 4) return 63 - n;
-  const int e = 31 - __clz(n);
-  return max(0, 63 - (4 * e - 4 + ((n >> (e - 2)) & 3)));
+// Cost of an item in half tiles: both groups work on every tile of a wide item, on every second of a narrow one.
+__device__ __forceinline__ int item_width(int ntok, int tpt) { return ntok <= tpt ? 1 : 2; }
+__device__ __forceinline__ int item_cost(int nt, int width) { return nt * width + kItemCost; }
+// The tile at which a border at `off` into an item's cost cuts it: 0 or nt where a piece would be short.
+__device__ __forceinline__ int cut_tile(long long off, int nt, int width) {
+  const long long t = (off - kItemCost / 2) / width;
+  return t < kMinPiece ? 0 : nt - t < kMinPiece ? nt : (int)t;
 }
 
-// The list of work of one KV head (every head has the same), the longest pieces first, and the items
-// that are in pieces.  One CTA; lengths are read here and nowhere on the host.
-__global__ void __launch_bounds__(kPlanThreads, 1) k_chunk_plan(const ChunkArgs k, int n_cta) {
-  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-  __shared__ int2 s_warp[32];
-  __shared__ unsigned long long s_tiles;
-  __shared__ int s_class[64];
-  __shared__ int s_start[kReqShared + 1], s_n[kReqShared], s_p0[kReqShared];
+// This CTA's share of a paged call, found by the whole block in shared memory (16 bytes per request or item).
+struct Share {
+  Border begin, end;
+  int items;          // of a head
+  int r, in_req;      // the begin's request, and the item's number in it
+};
+__device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, long long* s_warp, Border* s_border,
+                                            int n_cta) {
   const ZcPagedArgs& a = k.a;
-  const int tid = threadIdx.x, n_thread = blockDim.x, tpi = 2 * k.tpt;
-  const bool shared = a.n_req <= kReqShared;   // else the items' starts go through the workspace
-  int* start = shared ? s_start : k.ws.item_start;
-  if (tid == 0) s_tiles = 0;
-  for (int i = tid; i < 64; i += n_thread) s_class[i] = 0;
+  const int tid = threadIdx.x, tpi = 2 * k.tpt;
+  int* s_start = reinterpret_cast<int*>(scratch);      // items before a request
+  int* s_n = s_start + a.n_req + 1;
+  int* s_p0 = s_n + a.n_req;
+  int* s_cost = s_p0 + a.n_req;                        // cost of the head's items before an item
   int items = 0;
-  for (int c0 = 0; c0 < a.n_req; c0 += n_thread) {
+  for (int c0 = 0; c0 < a.n_req; c0 += kThreads) {
     const int r = c0 + tid;
-    int n = 0;
+    Chunk c;
+    c.n = c.p0 = 0;
     if (r < a.n_req) {
-      const Chunk c = load_chunk(a, r);
-      n = (c.n + tpi - 1) / tpi;
-      if (shared) {
-        s_n[r] = c.n;
-        s_p0[r] = c.p0;
-      }
+      c = load_chunk(a, r);
+      s_n[r] = c.n;
+      s_p0[r] = c.p0;
     }
-    int2 t;
-    const int2 at = block_scan2(make_int2(n, 0), s_warp, &t);
-    if (r < a.n_req) start[r] = items + at.x;
-    items += t.x;
+    long long t;
+    const long long at = block_scan((c.n + tpi - 1) / tpi, s_warp, &t);
+    // (lengths that contradict the host's bounds cannot lead outside the scratch)
+    if (r < a.n_req) s_start[r] = (int)min((long long)kMaxItems, items + at);
+    items = (int)min((long long)kMaxItems, items + t);
   }
-  if (tid == 0) start[a.n_req] = items;
+  if (tid == 0) s_start[a.n_req] = items;
   __syncthreads();
-  auto item = [&](int i, int* tok0, int* nt) {   // request, first token and key tiles of item i
+  auto request = [&](int i) {
     int lo = 0, hi = a.n_req;
     while (hi - lo > 1) {
       const int m = (lo + hi) >> 1;
-      if (start[m] <= i) lo = m; else hi = m;
+      if (s_start[m] <= i) lo = m; else hi = m;
     }
-    *tok0 = (i - start[lo]) * tpi;
-    Chunk c;
-    if (shared) {
-      c.n = s_n[lo];
-      c.p0 = s_p0[lo];
-    } else {
-      c = load_chunk(a, lo);
-    }
-    *nt = item_tiles(a, c, *tok0, tpi);
     return lo;
   };
-  unsigned long long tiles = 0;
-  for (int i = tid; i < items; i += n_thread) {
-    int tok0, nt;
-    item(i, &tok0, &nt);
-    tiles += nt;
-  }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, o);
-  if ((tid & 31) == 0) atomicAdd(&s_tiles, tiles);
-  __syncthreads();
-  // No piece is longer than half a CTA's even share, so that handing out the longest first leaves the
-  // CTAs about even, and none is shorter than 8 tiles, below which writing and joining the pieces costs
-  // more than it evens out.
-  const long long all = (long long)s_tiles * a.h_kv;
-  long long most = (all + 2 * n_cta - 1) / (2 * n_cta);
-  if (most < 8) most = 8;
-  auto pieces_of = [&](int nt) { return nt <= most ? 1 : (int)((nt + most - 1) / most); };
-  for (int i = tid; i < items; i += n_thread) {
-    int tok0, nt;
-    item(i, &tok0, &nt);
-    const int pieces = pieces_of(nt);
-    atomicAdd(&s_class[length_class((nt + pieces - 1) / pieces)], pieces);
-  }
-  __syncthreads();
-  if (tid < 32) {   // starts of the classes
-    const int x = s_class[2 * tid], y = s_class[2 * tid + 1];
-    int incl = x + y;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, incl, o);
-      if (tid >= o) incl += u;
-    }
-    s_class[2 * tid] = incl - x - y;
-    s_class[2 * tid + 1] = incl - y;
-  }
-  __syncthreads();
-  int n_slot = 0, n_join = 0, n_work = 0;
-  for (int c0 = 0; c0 < items; c0 += n_thread) {
+  auto tiles = [&](int i, int r, int* width) {
+    const int tok0 = (i - s_start[r]) * tpi;
+    Chunk c;
+    c.row0 = 0;
+    c.n = s_n[r];
+    c.p0 = s_p0[r];
+    *width = item_width(min(tpi, c.n - tok0), k.tpt);
+    return item_tiles(a, c, tok0, tpi);
+  };
+  long long head = 0;   // cost of a head
+  for (int c0 = 0; c0 < items; c0 += kThreads) {
     const int i = c0 + tid;
-    int r = 0, tok0 = 0, nt = 0, pieces = 0;
+    int cost = 0;
     if (i < items) {
-      r = item(i, &tok0, &nt);
-      pieces = pieces_of(nt);
+      int width;
+      const int nt = tiles(i, request(i), &width);
+      cost = item_cost(nt, width);
     }
-    // partial results have places by the order of the items: the results do not depend on the schedule
-    int2 t;
-    const bool cut = pieces > 1;
-    const int2 at = block_scan2(make_int2(cut ? pieces : 0, cut ? 1 : 0), s_warp, &t);
-    if (pieces) {
-      const int w = atomicAdd(&s_class[length_class((nt + pieces - 1) / pieces)], pieces);
-      for (int q = 0; q < pieces; ++q) {
-        ChunkWork x;
-        x.r = r;
-        x.tok0 = tok0;
-        x.t0 = (int)((long long)q * nt / pieces);
-        x.t1 = (int)((long long)(q + 1) * nt / pieces);
-        x.slot = cut ? n_slot + at.x + q : -1;
-        x.pad[0] = x.pad[1] = x.pad[2] = 0;
-        k.ws.work[w + q] = x;
+    long long t;
+    const long long at = block_scan(cost, s_warp, &t);
+    if (i < items) s_cost[i] = (int)(head + at);
+    head += t;
+  }
+  if (tid == 0) s_cost[items] = (int)head;
+  __syncthreads();
+  // Borders before this CTA and the next (threads 0 and 1).
+  const int c = blockIdx.x;
+  const long long all = head * a.h_kv;
+  if (tid < 2) {
+    const long long at = all * (c + tid) / n_cta;
+    Border b;
+    ChunkJoin j;
+    j.on = 0;
+    if (at >= all) {
+      b.item = items * a.h_kv;
+      b.t = 0;
+    } else {
+      const int kv = (int)(at / head);
+      const long long in = at - kv * head;
+      int lo = 0, hi = items;
+      while (hi - lo > 1) {
+        const int m = (lo + hi) >> 1;
+        if (s_cost[m] <= in) lo = m; else hi = m;
       }
-      if (cut) {
-        ChunkJoin x;
-        x.r = r;
-        x.tok0 = tok0;
-        x.slot = n_slot + at.x;
-        x.n = pieces;
-        k.ws.joins[n_join + at.y] = x;
+      int width;
+      const int r = request(lo), nt = tiles(lo, r, &width), t = cut_tile(in - s_cost[lo], nt, width);
+      b.item = kv * items + lo + (t > 0 && t == nt ? 1 : 0);
+      b.t = t == nt ? 0 : t;
+      if (tid == 0 && b.t > 0) {
+        // the CTAs around this one whose borders cut the same item
+        const long long start = kv * head + s_cost[lo];
+        auto cuts = [&](int d) {
+          const int u = cut_tile(all * d / n_cta - start, nt, width);
+          return u > 0 && u < nt;
+        };
+        j.first = j.last = c;
+        while (j.first > 1 && cuts(j.first - 1)) --j.first;
+        if (j.first == c) {
+          while (j.last + 1 < n_cta && cuts(j.last + 1)) ++j.last;
+          j.on = 1;
+          j.r = r;
+          j.tok0 = (lo - s_start[r]) * tpi;
+          j.kv = kv;
+        }
       }
     }
-    n_slot += t.x;
-    n_join += t.y;
+    if (tid == 0) k.ws.joins[c] = j;
+    s_border[tid] = b;
   }
-  n_work = items - n_join + n_slot;
-  if (tid == 0) {
-    ChunkHead h;
-    h.n_work = n_work;
-    h.n_join = n_join;
-    h.slots_per_head = n_slot;
-    h.next = n_cta;   // the first n_cta items belong to the CTAs of their number
-    *k.ws.head = h;
-  }
+  __syncthreads();
+  Share s;
+  s.begin = s_border[0];
+  s.end = s_border[1];
+  s.items = items;
+  const int i = items > 0 ? s.begin.item % items : 0;
+  s.r = items > 0 ? request(i) : 0;
+  s.in_req = i - s_start[s.r];
+  if (tid == 0) k.ws.used[c] = s.begin.item < s.end.item || s.begin.t < s.end.t;
+  __syncthreads();   // the scratch is free for the tiles
+  return s;
 }
 
 // Shared-memory descriptor of a B operand whose N dimension is contiguous: rows are keys of 128 bytes
@@ -345,43 +331,30 @@ struct Item {
 };
 static_assert(sizeof(Item) <= kRingInts * 4, "an item fits its place in the ring");
 
-template <bool PAGED>
-__device__ __forceinline__ Item load_item(const ChunkArgs& k, long long idx) {
+// Item of a dense call.
+__device__ __forceinline__ Item dense_item(const ChunkArgs& k, long long idx) {
   const ZcPagedArgs& a = k.a;
+  const int units = a.n_req * a.h_kv, q = (int)(idx / units), unit = (int)(idx - (long long)q * units);
   Item it;
+  it.r = unit / a.h_kv;
+  it.kv = unit - it.r * a.h_kv;
+  it.tok0 = (k.items - 1 - q) * 2 * k.tpt;   // the last, longest rows first
+  it.slot = -1;
+  it.row0 = 0;
+  it.p_first = it.tok0;
+  it.t0 = 0;
+  it.t1 = 1 << 30;
+  return it;
+}
+
+// Fills in what follows from the rows (n tokens in the request) and the first and last key tile asked for.
+__device__ __forceinline__ void finish_item(const ChunkArgs& k, int n, Item& it) {
+  const ZcPagedArgs& a = k.a;
   const int tpi = 2 * k.tpt;
-  int n;
-  if (PAGED) {
-    // all heads of a piece beside each other: the list's order, the longest first, holds for all of them
-    const long long at = idx / a.h_kv;
-    it.kv = (int)(idx - at * a.h_kv);
-    const ChunkWork w = k.ws.work[at];
-    const Chunk c = load_chunk(a, w.r);
-    it.r = w.r;
-    it.tok0 = w.tok0;
-    it.t0 = w.t0;
-    it.t1 = w.t1;
-    it.slot = w.slot;
-    it.row0 = c.row0;
-    it.p_first = c.p0 + w.tok0;
-    n = c.n;
-  } else {
-    const int units = a.n_req * a.h_kv, q = (int)(idx / units), unit = (int)(idx - (long long)q * units);
-    it.r = unit / a.h_kv;
-    it.kv = unit - it.r * a.h_kv;
-    it.tok0 = (k.items - 1 - q) * tpi;   // the last, longest rows first
-    it.slot = -1;
-    it.row0 = 0;
-    it.p_first = it.tok0;
-    n = k.l;
-  }
   it.ntok = min(tpi, n - it.tok0);
   it.narrow = it.ntok <= k.tpt;
   it.s = zc_seen(it.p_first, it.p_first + it.ntok - 1, a.window, a.sinks, kTileLog2);
-  if (!PAGED) {
-    it.t0 = 0;
-    it.t1 = it.s.nb;
-  }
+  it.t1 = min(it.t1, it.s.nb);
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     const int first = it.p_first + g * k.tpt, last = it.p_first + min(it.ntok, (g + 1) * k.tpt) - 1;
@@ -392,7 +365,6 @@ __device__ __forceinline__ Item load_item(const ChunkArgs& k, long long idx) {
     it.ga[g] = it.narrow ? it.t0 : max(it.t0, begin);
     it.ge[g] = it.narrow ? it.t1 : min(it.t1, end);
   }
-  return it;
 }
 
 // bar_wait that says whether the phase completed (false: the bound ran out here or elsewhere).
@@ -440,18 +412,31 @@ __device__ __forceinline__ float2 exp2_poly(float2 x) {
                      __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 
-// The weights of 64 keys, 2^(v * scale - m), packed to the input type, and their sums (of the unrounded
-// values) by two accumulators.  POLY of every 8 pairs take exp2_poly: the exp2 unit, at a quarter of a
-// warp per cycle and quarter of the SM, would otherwise be what the groups wait for.
+// The weights of 64 keys, 2^(v * scale - m), packed to the input type; returns their sum (of the unrounded
+// values).  POLY of every 8 pairs take exp2_poly: the exp2 unit, at a quarter of a warp per cycle and
+// quarter of the SM, would otherwise be what the groups wait for.  top: the largest exponent among those
+// (the exp2 unit's weights become infinite, and the sum with them, where theirs would be wrong).
 template <typename T, int POLY>
-__device__ __forceinline__ void weights(const float* v, float2 scale, float2 neg_m, float2 (&add)[2], uint32_t* w) {
+__device__ __forceinline__ float weights(const float* v, float scale, float m, uint32_t* w, float* top) {
+  const float2 sc = make_float2(scale, scale), neg_m = make_float2(-m, -m);
+  float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+  float t = -INFINITY;
 #pragma unroll
-  for (int c = 0; c < 32; ++c) {
-    const float2 x = fma2(make_float2(v[2 * c], v[2 * c + 1]), scale, neg_m);
-    const float2 p = (c * POLY) % 8 + POLY > 7 && POLY ? exp2_poly(x) : make_float2(zc_exp2(x.x), zc_exp2(x.y));
+  for (int c = 0; c < kN / 2; ++c) {
+    const float2 x = fma2(make_float2(v[2 * c], v[2 * c + 1]), sc, neg_m);
+    float2 p;
+    if (POLY && (c * POLY) % 8 + POLY > 7) {
+      t = max3(t, x.x, x.y);
+      p = exp2_poly(x);
+    } else {
+      p = make_float2(zc_exp2(x.x), zc_exp2(x.y));
+    }
     add[c & 1] = add2(add[c & 1], p);
     w[c] = pack2<T>(p.x, p.y);
   }
+  if (POLY) *top = t;
+  add[0] = add2(add[0], add[1]);
+  return add[0].x + add[0].y;
 }
 
 // The loads that wrote v[0 .. 31] have completed (the operands keep their uses behind the wait).
@@ -541,7 +526,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);
-  asm volatile("griddepcontrol.wait;\n" ::: "memory");   // the list of work (and all that came before it)
+  Share share;
+  if (PAGED) share = find_share(k, base, reinterpret_cast<long long*>(s_ms), reinterpret_cast<Border*>(ring), gridDim.x);
 
   uint32_t n_item = 0;   // items taken from the ring
   // Next item of the ring; a whole warp calls.  False: there are no more (or a wait ran out).
@@ -562,23 +548,68 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
     if (warp == 2) {
       // ---- items ----
-      if (lane == 0) {
-        const long long n_idx = PAGED ? (long long)k.ws.head->n_work * a.h_kv : (long long)k.items * a.n_req * a.h_kv;
-        long long idx = blockIdx.x;
-        for (uint32_t n = 0;; ++n) {
-          Item it;
-          const bool more = idx < n_idx;
-          if (more) it = load_item<PAGED>(k, idx);
-          if (!more) it.r = -1;
-          const uint32_t at = n % kRingN;
-          if (n >= kRingN && !bar_wait_ok(&i_free[at], (n / kRingN - 1) & 1u)) break;
-          int* dst = ring + at * kRingInts;
+      const long long n_idx = (long long)k.items * a.n_req * a.h_kv;   // dense form
+      long long idx = blockIdx.x;
+      Border at = share.begin;
+      int r = share.r, in_req = share.in_req;
+      Chunk c;
+      c.row0 = c.n = c.p0 = 0;
+      if (PAGED && share.items > 0) c = load_chunk(a, r);
+      for (uint32_t n = 0;; ++n) {
+        Item it;
+        it.r = -1;
+        if (PAGED) {
+          if (at.item < share.end.item || (at.item == share.end.item && at.t < share.end.t)) {
+            // (only the share's first item can begin, and only its last can end, inside)
+            it.r = r;
+            it.kv = at.item / share.items;
+            it.tok0 = in_req * 2 * k.tpt;
+            it.row0 = c.row0;
+            it.p_first = c.p0 + it.tok0;
+            it.t0 = at.t;
+            it.t1 = at.item == share.end.item ? share.end.t : 1 << 30;
+            finish_item(k, c.n, it);
+            it.slot = it.t0 > 0 ? 2 * (int)blockIdx.x : it.t1 < it.s.nb ? 2 * (int)blockIdx.x + 1 : -1;
+          }
+        } else if (idx < n_idx) {
+          it = dense_item(k, idx);
+          finish_item(k, k.l, it);
+        }
+        const uint32_t place = n % kRingN;
+        if (n >= kRingN && !bar_wait_ok(&i_free[place], (n / kRingN - 1) & 1u)) break;
+        if (lane == 0) {
+          int* dst = ring + place * kRingInts;
           const int* src = reinterpret_cast<const int*>(&it);
 #pragma unroll
           for (int i = 0; i < (int)(sizeof(Item) / 4); ++i) dst[i] = src[i];
-          bar_arrive(&i_full[at]);
-          if (!more) break;
-          idx = PAGED ? (long long)atomicAdd(&k.ws.head->next, 1) : idx + gridDim.x;
+          bar_arrive(&i_full[place]);
+        }
+        if (it.r < 0) break;
+        if (PAGED) {
+          ++at.item;
+          at.t = 0;
+          if (at.item >= share.end.item && share.end.t == 0) continue;
+          if ((++in_req) * 2 * k.tpt >= c.n) {
+            // the next request with rows (after the last one's, the next head's first), 32 at a time
+            in_req = 0;
+            const bool wrap = at.item % share.items == 0;
+            for (int r0 = wrap ? 0 : r + 1; r0 < a.n_req; r0 += 32) {
+              Chunk x;
+              x.row0 = x.n = x.p0 = 0;
+              if (r0 + lane < a.n_req) x = load_chunk(a, r0 + lane);
+              const unsigned some = __ballot_sync(0xffffffffu, x.n > 0);
+              if (some) {
+                const int src = __ffs(some) - 1;
+                r = r0 + src;
+                c.row0 = __shfl_sync(0xffffffffu, x.row0, src);
+                c.n = __shfl_sync(0xffffffffu, x.n, src);
+                c.p0 = __shfl_sync(0xffffffffu, x.p0, src);
+                break;
+              }
+            }
+          }
+        } else {
+          idx += gridDim.x;
         }
       }
     } else if (warp == 1) {
@@ -734,6 +765,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int ga = g ? it.ga[1] : it.ga[0], ge = g ? it.ge[1] : it.ge[0];
       const int step = it.narrow ? 2 : 1, t_first = it.narrow ? it.t0 + g : ga;
       float m_run = kNoMax, s_run = 0.f;
+      bool unset = true;                                             // a row of the warp has seen no key yet
       for (int t = t_first; t < ge; t += step) {
         const int key0 = it.key0(t);
         const uint32_t place = n_s & 1u, tmem_s = tmem_g + place * kN;
@@ -765,44 +797,53 @@ __global__ void __launch_bounds__(kThreads, 1)
             async_proxy_fence();
           }
         }
-        float mx4[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-        for (int e = 4; e < kN; e += 8)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mx4[i] = e + 4 < kN ? max3(mx4[i], v[e + i], v[e + 4 + i]) : fmaxf(mx4[i], v[e + i]);
-        const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * scale;
-        const bool grow = mx > m_run + kTau;
-        if (__any_sync(0xffffffffu, grow)) {
-          const float alpha = grow ? zc_exp2(m_run - mx) : 1.f;
-          if (t > t_first) {
-            // O has every product up to the tile before once the next tile's S is there (it was issued behind
-            // them), or, at the last tile, once they say so themselves
-            if (t + step < ge) bar_wait(&s_done[2 * g + (n_s & 1u)], (n_s >> 1) & 1u);
-            else bar_wait(&o_last[g], n_last & 1u);
-            tc_fence_after();
-#pragma unroll 1
-            for (int q8 = 0; q8 < 16; ++q8) {
-              float o[8];
-              tmem_ld8(o, tmem_o + 8 * q8);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) o[e] *= alpha;
-              tmem_st8(o, tmem_o + 8 * q8);
-            }
-          }
-          s_run *= alpha;
-          if (grow) m_run = mx;
+        // With the maximum that the row has so far, which as a rule is near enough: no pass over the logits for a
+        // new one.  The sum tells where it is not (a weight above 2^4 at least, 2^10 at most stays unseen).
+        uint32_t w[kN / 2];
+        float sum = 0.f;
+        bool renew = edge || unset;
+        if (!renew) {
+          float top;
+          sum = weights<T, kPoly>(v, scale, m_run, w, &top);
+          renew = __any_sync(0xffffffffu, !(sum <= kBigSum) || top > kTopPoly);
         }
-        const float2 sc2 = make_float2(scale, scale), m2 = make_float2(-m_run, -m_run);
-        float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        uint32_t w[32];
-        if (edge) weights<T, 0>(v, sc2, m2, add, w);   // hidden keys weigh 0 exactly
-        else weights<T, kPoly>(v, sc2, m2, add, w);
+        if (renew) {
+          float mx4[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+          for (int e = 4; e < kN; e += 8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx4[i] = e + 4 < kN ? max3(mx4[i], v[e + i], v[e + 4 + i]) : fmaxf(mx4[i], v[e + i]);
+          const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * scale;
+          const bool grow = mx > m_run + kTau;
+          if (__any_sync(0xffffffffu, grow)) {
+            const float alpha = grow ? zc_exp2(m_run - mx) : 1.f;
+            if (t > t_first) {
+              // O has every product up to the tile before once the next tile's S is there (it was issued behind
+              // them), or, at the last tile, once they say so themselves
+              if (t + step < ge) bar_wait(&s_done[2 * g + (n_s & 1u)], (n_s >> 1) & 1u);
+              else bar_wait(&o_last[g], n_last & 1u);
+              tc_fence_after();
+#pragma unroll 1
+              for (int q8 = 0; q8 < 16; ++q8) {
+                float o[8];
+                tmem_ld8(o, tmem_o + 8 * q8);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] *= alpha;
+                tmem_st8(o, tmem_o + 8 * q8);
+              }
+            }
+            s_run *= alpha;
+            if (grow) m_run = mx;
+          }
+          unset = __any_sync(0xffffffffu, valid && m_run == kNoMax);
+          sum = weights<T, 0>(v, scale, m_run, w, nullptr);   // hidden keys weigh 0 exactly
+        }
         tmem_st32(w, tmem_s);
         asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
         tc_fence_before();
         __syncwarp();
         if (lane == 0) bar_arrive(&p_full[2 * g + place]);
-        s_run += (add[0].x + add[0].y) + (add[1].x + add[1].y);
+        s_run += sum;
       }
       if (ge - t_first > step) ++n_last;   // an item of two or more of this group's tiles
       tile0 += (uint32_t)max(0, it.t1 - it.t0);
@@ -837,7 +878,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const long long at = (PAGED ? 0 : it.r * k.o_req) + (long long)(it.row0 + it.tok0 + tok) * k.o_row + h * k.o_head;
       float* pr = nullptr;
       if (PAGED && it.slot >= 0)
-        pr = k.ws.parts + (((long long)it.kv * k.ws.head->slots_per_head + it.slot) * kItemRows + rows_at * kM + row) * kPartStride;
+        pr = k.ws.parts + ((long long)it.slot * kItemRows + rows_at * kM + row) * kPartStride;
 #pragma unroll 1
       for (int q4 = 0; q4 < 4; ++q4) {
         float o[32];
@@ -906,29 +947,38 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kCols) : "memory");
 }
 
-// Rows of the items that were worked on in pieces: a CTA takes 16 rows of an item, a warp two of them.
+// Rows of the items that were worked on in pieces.  Block (c - 1) * 16 + i: rows 16 i ... of the item that the
+// border before CTA c cuts first; a warp takes two rows.
 template <typename T> __global__ void __launch_bounds__(256) k_chunk_join(const ChunkArgs k) {
+  __shared__ int s_slot[ZC_PAGED_MAX_CTAS + 1], s_count;
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const ZcPagedArgs& a = k.a;
-  const ChunkHead hd = *k.ws.head;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long n = (long long)hd.n_join * a.h_kv * (kItemRows / 16);
-  for (long long i = blockIdx.x; i < n; i += gridDim.x) {
-    const long long job = i / (kItemRows / 16);
-    const int row16 = (int)(i - job * (kItemRows / 16)) * 16;
-    const int kv = (int)(job / hd.n_join);
-    const ChunkJoin j = k.ws.joins[job - (long long)kv * hd.n_join];
-    const Chunk c = load_chunk(a, j.r);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int row = row16 + warp + 8 * u, g = row / kM, in = row % kM;
-      const int tok_in = in / a.G, tok = j.tok0 + g * k.tpt + tok_in;
-      if (tok_in >= k.tpt || tok >= c.n) continue;
-      const long long at = (long long)(c.row0 + tok) * a.h_q + kv * a.G + (in - tok_in * a.G);
-      join_row<T>(a.out, a.lse, at, lane, j.n, [&](int q) {
-        return k.ws.parts + (((long long)kv * hd.slots_per_head + j.slot + q) * kItemRows + row) * kPartStride;
-      });
+  const ChunkJoin j = k.ws.joins[blockIdx.x / 16 + 1];
+  if (!j.on) return;
+  const Chunk c = load_chunk(a, j.r);
+  if (warp == 0) {
+    // the pieces in order: the end of the share before the item's first border, then the starts behind each border
+    int n = 1;
+    if (lane == 0) s_slot[0] = 2 * (j.first - 1) + 1;
+    for (int d = j.first; d <= j.last; d += 32) {
+      const bool on = d + lane <= j.last && k.ws.used[d + lane];
+      const unsigned m = __ballot_sync(0xffffffffu, on);
+      if (on) s_slot[n + __popc(m & ((1u << lane) - 1u))] = 2 * (d + lane);
+      n += __popc(m);
     }
+    if (lane == 0) s_count = n;
+  }
+  __syncthreads();
+  const int n = s_count;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int row = (int)(blockIdx.x % 16) * 16 + warp + 8 * u, g = row / kM, in = row % kM;
+    const int tok_in = in / a.G, tok = j.tok0 + g * k.tpt + tok_in;
+    if (tok_in >= k.tpt || tok >= c.n) continue;
+    const long long at = (long long)(c.row0 + tok) * a.h_q + j.kv * a.G + (in - tok_in * a.G);
+    join_row<T>(a.out, a.lse, at, lane, n,
+                [&](int q) { return k.ws.parts + ((long long)s_slot[q] * kItemRows + row) * kPartStride; });
   }
 }
 
@@ -936,8 +986,7 @@ size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 int tokens_per_tile(int G) { return kM / G; }
 
 // Places of the parts of a call's workspace; returns the bytes.
-size_t carve(char* ws, int G, int h_kv, int n_req, int n_rows, ChunkWs* out) {
-  const size_t items = (size_t)n_rows / (2 * tokens_per_tile(G)) + (size_t)n_req + 1;
+size_t carve(char* ws, ChunkWs* out) {
   size_t off = 0;
   auto take = [&](size_t bytes) {
     char* p = ws + off;
@@ -945,12 +994,9 @@ size_t carve(char* ws, int G, int h_kv, int n_req, int n_rows, ChunkWs* out) {
     return p;
   };
   ChunkWs w;
-  w.head = (ChunkHead*)take(sizeof(ChunkHead));
-  w.item_start = (int*)take(((size_t)n_req + 1) * sizeof(int));
-  w.work = (ChunkWork*)take((items + kMaxSlots) * sizeof(ChunkWork));
-  w.joins = (ChunkJoin*)take((size_t)kMaxSlots * sizeof(ChunkJoin));
-  w.parts = (float*)take((size_t)kMaxSlots * kItemRows * kPartStride * sizeof(float));
-  (void)h_kv;
+  w.joins = (ChunkJoin*)take(ZC_PAGED_MAX_CTAS * sizeof(ChunkJoin));
+  w.used = (int*)take(ZC_PAGED_MAX_CTAS * sizeof(int));
+  w.parts = (float*)take((size_t)ZC_PAGED_MAX_CTAS * 2 * kItemRows * kPartStride * sizeof(float));
   if (out) *out = w;
   return off;
 }
@@ -999,22 +1045,24 @@ template <typename T>
 int launch_chunk(zc_pages* p, const ChunkArgs& k, const CUtensorMap& qmap, cudaStream_t st) {
   cudaError_t e = ready<T, true>();
   if (e != cudaSuccess) return e;
-  // one thread per item or request where they are few: the sums over the block then pass through few warps
-  const long long most = std::max<long long>(k.a.n_req, k.a.n_rows / (2 * k.tpt) + k.a.n_req);
-  k_chunk_plan<<<1, most <= 128 ? 128 : most <= 512 ? 512 : kPlanThreads, 0, st>>>(k, p->n_sm);
+  k_chunk_attention<T, true><<<p->n_sm, kThreads, kSmem, st>>>(k, qmap, p->k64, p->v64);
+  p->launches += 1;
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  e = zc_launch_early(k_chunk_attention<T, true>, dim3(p->n_sm), dim3(kThreads), kSmem, st, k, qmap, p->k64, p->v64);
-  if (e != cudaSuccess) return e;
-  e = zc_launch_early(k_chunk_join<T>, dim3(8 * p->n_sm), dim3(256), 0, st, k);
-  p->launches += 3;
-  return e;
+  if (p->n_sm > 1) {
+    e = zc_launch_early(k_chunk_join<T>, dim3(16 * (p->n_sm - 1)), dim3(256), 0, st, k);
+    if (e != cudaSuccess) return e;
+    p->launches += 1;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace
 
-size_t zc_paged_chunk_workspace(const zc_pages* p, int n_req, int n_rows) {
-  return carve(nullptr, p->G, p->cfg.n_kv_heads, n_req, n_rows, nullptr);
+size_t zc_paged_chunk_workspace() { return carve(nullptr, nullptr); }
+
+bool zc_paged_chunk_fits(int G, int n_req, int n_rows) {
+  return (long long)n_rows / (2 * tokens_per_tile(G)) + n_req <= kMaxItems;
 }
 
 int zc_launch_paged_chunk(zc_pages* p, const ZcPagedArgs& a, char* ws, cudaStream_t st) {
@@ -1022,7 +1070,7 @@ int zc_launch_paged_chunk(zc_pages* p, const ZcPagedArgs& a, char* ws, cudaStrea
   ChunkArgs k;
   memset(&k, 0, sizeof(k));
   k.a = a;
-  carve(ws, a.G, a.h_kv, a.n_req, a.n_rows, &k.ws);
+  carve(ws, &k.ws);
   k.tpt = tokens_per_tile(a.G);
   k.o_row = (long long)a.h_q * ZC_D;
   k.o_head = ZC_D;

@@ -468,7 +468,7 @@ int launch(zc_pages* p, const ZcPagedArgs& a, float* parts, JoinDesc* descs, cud
 
 }  // namespace
 
-size_t zc_paged_decode_workspace(const zc_pages*) {
+size_t zc_paged_decode_workspace() {
   return (size_t)ZC_PAGED_MAX_CTAS * (2 * ZC_PAGED_ROWS * kJoinStride * 4 + sizeof(JoinDesc));
 }
 

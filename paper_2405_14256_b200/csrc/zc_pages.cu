@@ -242,11 +242,8 @@ int zc_pages_workspace(const zc_page_config* cfg, int n_req, int n_rows, size_t*
   const int rc = check_page_config(cfg);
   if (rc) return rc;
   if (n_req < 0 || n_rows < 0 || !workspace_bytes) return ZC_EINVAL;
-  zc_pages p;
-  memset(&p, 0, sizeof(p));
-  p.cfg = *cfg;
-  p.G = cfg->n_q_heads / cfg->n_kv_heads;
-  const size_t a = zc_paged_decode_workspace(&p), b = zc_paged_chunk_workspace(&p, n_req, n_rows);
+  if (!zc_paged_chunk_fits(cfg->n_q_heads / cfg->n_kv_heads, n_req, n_rows)) return ZC_ECAPACITY;
+  const size_t a = zc_paged_decode_workspace(), b = zc_paged_chunk_workspace();
   *workspace_bytes = a > b ? a : b;
   return ZC_OK;
 }
@@ -373,8 +370,8 @@ int zc_paged_attention(zc_pages* p, const void* q, const int64_t q_strides[2], c
   a.out = out;
   a.lse = row_lse;
   const bool few = (long long)max_rows * p->G <= ZC_PAGED_ROWS;
-  const size_t need = few ? zc_paged_decode_workspace(p) : zc_paged_chunk_workspace(p, n_req, n_rows);
-  if (workspace_bytes < need) return ZC_ECAPACITY;
+  if (workspace_bytes < (few ? zc_paged_decode_workspace() : zc_paged_chunk_workspace())) return ZC_ECAPACITY;
+  if (!few && !zc_paged_chunk_fits(p->G, n_req, n_rows)) return ZC_ECAPACITY;
   const int e = few ? zc_launch_paged_decode(p, a, (char*)workspace, (cudaStream_t)stream)
                     : zc_launch_paged_chunk(p, a, (char*)workspace, (cudaStream_t)stream);
   return zc_cuda_status(e);

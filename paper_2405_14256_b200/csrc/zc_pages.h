@@ -57,9 +57,10 @@ __host__ __device__ static inline ZcSeen zc_seen(int p_first, int p_last, int wi
   return s;
 }
 
-// Workspace of one call: [list of work items | merge jobs | partial results].
-size_t zc_paged_decode_workspace(const zc_pages* p);
-size_t zc_paged_chunk_workspace(const zc_pages* p, int n_req, int n_rows);
+// Workspace of one call: what the joining kernel is told, and the partial results it joins.
+size_t zc_paged_decode_workspace();
+size_t zc_paged_chunk_workspace();
+bool zc_paged_chunk_fits(int G, int n_req, int n_rows);   // the call's items fit the chunk kernel's shared memory
 int zc_launch_paged_decode(zc_pages* p, const ZcPagedArgs& a, char* ws, cudaStream_t st);
 int zc_launch_paged_chunk(zc_pages* p, const ZcPagedArgs& a, char* ws, cudaStream_t st);
 int zc_launch_prefill_window(zc_cache* c, const void* Q, const void* K, const void* V, int l, const int64_t* qs,

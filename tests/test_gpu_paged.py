@@ -378,8 +378,8 @@ def test_wrong_tensors_are_refused(zc):
         with pytest.raises((zc.ZipCacheError, ValueError)):
             pool.attention(kw["q"], kw["table"], kw["row_start"], kw["kv_len"], n)
     with pytest.raises(zc.ZipCacheError, match="capacity"):
-        big = torch.zeros(200000, 8, D, dtype=torch.float16, device=DEV)
-        pool.attention(big, table, row_start, kv_len, 200000)
+        big = torch.zeros(900000, 8, D, dtype=torch.float16, device=DEV)
+        pool.attention(big, table, row_start, kv_len, 900000)
     with pytest.raises(zc.ZipCacheError):
         pool.write(q[:, :2].bfloat16(), q[:, :2].bfloat16(), i32([0, 1, 2]))
     with pytest.raises(zc.ZipCacheError):

@@ -51,9 +51,12 @@ def test_a_stride_of_an_extent_of_one_does_not_matter(zc):
     assert zc.zc_pages_workspace(config(zc, n_pages=1, strides=(0, 8 * 128, 128)), 8, 64) > 0
 
 
-def test_workspace_grows_with_the_call(zc):
-    small, large = zc.zc_pages_workspace(config(zc), 1, 1), zc.zc_pages_workspace(config(zc), 4096, 1 << 20)
-    assert 0 < small < large
+def test_workspace_of_the_largest_calls(zc):
+    # G = 4: 64 rows to an item
+    assert zc.zc_pages_workspace(config(zc), 13000, 0) == zc.zc_pages_workspace(config(zc), 1, 12999 * 64) > 0
+    for n_req, n_rows in [(13001, 0), (1, 13000 * 64), (13000, 64)]:
+        with pytest.raises(zc.ZipCacheError, match="capacity"):
+            zc.zc_pages_workspace(config(zc), n_req, n_rows)
     for n_req, n_rows in [(-1, 4), (4, -1)]:
         with pytest.raises(zc.ZipCacheError, match="invalid argument"):
             zc.zc_pages_workspace(config(zc), n_req, n_rows)
