@@ -8,8 +8,9 @@
 // even and the odd key tiles, and their results meet at the end), and the key tiles (64 keys) that any
 // of its rows sees: those of the first `sinks` tokens, then those of the window.  The CTAs are
 // persistent, one per SM; each works through items until there are none:
-//   warp 2      walks the CTA's items ahead of the others
-//   warp 1      the copies: Q by one box per tile half, K and V page by page (a lane per page)
+//   warp 2      walks the CTA's items, one ahead of the others, and copies V
+//   warp 1      copies Q (a box per half of a tile's channels) and K, as warp 2 V, page by page: a box per
+//               page of 64 tokens or more, a lane per page and a box per half of the channels below that
 //   warps 0, 3  the matrix products of group 0 and 1, tcgen05.mma with accumulators in tensor memory:
 //               S_g = Q_g K^T (both K-major in shared memory), 128 x 64, and O_g += P_g V (P_g in tensor
 //               memory over the first half of its S, V with its channels contiguous), 128 x 128
@@ -35,9 +36,10 @@ constexpr int kN = 64;                                // keys of a tile
 constexpr int kTileLog2 = 6;
 constexpr int kKvTile = kN * ZC_D * 2;                // 16 KB: [2][64][128 B]
 constexpr int kKvBlock = kN * 128;
-constexpr int kKS = 5, kVS = 5;                       // key and value buffers
+constexpr int kKS = 4, kVS = 5;                       // key and value buffers
 constexpr uint32_t kCols = 512;                       // S_0 twice | S_1 twice | O_0 | O_1
-constexpr int kTiles = 2 * kTile + (kKS + kVS) * kKvTile;   // 224 KB
+constexpr int kOutTile = 32 * 64;                     // a warp's 32 rows x 32 channels on their way out
+constexpr int kTiles = 2 * kTile + (kKS + kVS) * kKvTile + 8 * kOutTile;   // 224 KB
 constexpr int kRingN = 2;                             // items fetched ahead
 constexpr int kRingInts = 24;
 constexpr int kSmem = kTiles + 1024 + 384 + 1024 + kRingN * kRingInts * 4;   // alignment, barriers, (m, sum) of group 1
@@ -49,8 +51,10 @@ constexpr float kNoMax = -1e30f;                      // running maximum before 
 constexpr float kTau = 3.f;                           // a new maximum is taken where it exceeds the old by this (base 2)
 constexpr float kBigSum = 1024.f;                     // ... and looked for where a tile's weights sum to more than this
 constexpr float kTopPoly = 16.f;                      // ... or one that the exp2 unit did not compute has this exponent
-constexpr int kPartStride = ZC_PART_STRIDE;           // m, sum, -, -, acc[128]
 constexpr int kItemRows = 2 * kM;
+// A piece's partial result: 32 x 256 groups of 4 channels, [group of channels][row], so that the threads that
+// own neighbouring rows write neighbouring 16 bytes; then (maximum, sum) [row].
+constexpr int kPartBytes = kItemRows * ZC_D * 4 + kItemRows * 8;
 constexpr int kMaxItems = 13000;                      // items of a head, and requests, that a call may have: what the
                                                       // prologue keeps in the tiles' shared memory (16 bytes each)
 constexpr int kItemCost = 6;                          // of an item beside its tiles: Q, first product, output (half tiles)
@@ -67,7 +71,7 @@ struct ChunkJoin {
 struct ChunkWs {
   ChunkJoin* joins;   // [CTA]
   int* used;          // [CTA] its share is not empty
-  float* parts;       // [CTA][2][256][132]: the piece at its share's start, the one at its end
+  char* parts;        // [CTA][2]: the piece at its share's start, the one at its end
 };
 
 struct ChunkArgs {
@@ -304,15 +308,12 @@ __device__ __forceinline__ void tmem_st8(const float* v, uint32_t taddr) {
                "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
-// One box of 64 channels of a dense tensor: half kb of the channels, from (head, token) of batch row b on;
-// the maps of Q have the heads inside the tokens, those of K and V (swapped) the tokens inside the heads.
-__device__ __forceinline__ void q_copy(const CUtensorMap* map, uint32_t dst, uint64_t* bar, int kb, int head, int tok,
-                                       int b, bool swapped = false) {
+// Q rows of one tile half: 64 channels x G heads x tokens, from (channel half kb, head, token) of batch row b on.
+__device__ __forceinline__ void q_copy(const CUtensorMap* map, uint32_t dst, uint64_t* bar, int kb, int head, int tok, int b) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
       "[%6];\n" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(kb * 64), "r"(swapped ? tok : head), "r"(swapped ? head : tok), "r"(b),
-      "r"(zc_smem_u32(bar))
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(kb * 64), "r"(head), "r"(tok), "r"(b), "r"(zc_smem_u32(bar))
       : "memory");
 }
 __device__ __forceinline__ void expect_bytes(uint64_t* bar, uint32_t bytes) {
@@ -483,8 +484,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* o_done = o_last + 2;            // [2] the group's last P V of an item completed
   uint64_t* i_full = o_done + 2;            // [kRingN] an item is in the ring
   uint64_t* i_free = i_full + kRingN;       // [kRingN] all roles have read it
-  uint64_t* m_free = i_free + kRingN;       // the groups' meeting over a narrow item is over
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(m_free + 1);
+  uint64_t* m_free = i_free + kRingN;       // [2] the groups' meeting over a narrow item is over (in turn)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(m_free + 2);
   float2* s_ms = reinterpret_cast<float2*>(base + kTiles + 384);                    // [128] narrow items: group 1's (m, sum)
   int* ring = reinterpret_cast<int*>(base + kTiles + 384 + 1024);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -492,7 +493,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (tid == 0) {
     bar_init(q_full, 1);
     bar_init(q_free, 2);
-    bar_init(m_free, 1);
+    bar_init(&m_free[0], 1);
+    bar_init(&m_free[1], 1);
     for (int i = 0; i < kKS; ++i) {
       bar_init(&k_full[i], 1);
       bar_init(&k_free[i], 2);
@@ -511,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < kRingN; ++i) {
       bar_init(&i_full[i], 1);
-      bar_init(&i_free[i], 11);   // copies, two warps for the products, eight worker warps
+      bar_init(&i_free[i], 11);   // Q and K, two warps for the products, eight worker warps
     }
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
@@ -546,8 +548,53 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
+    // The key (or value) tiles of an item through their ring; the whole warp calls.
+    uint32_t stage = 0, phase = 1;   // of this warp's stream; the first wait for a free place succeeds at once
+    auto stream = [&](const Item& it, const CUtensorMap* map, uint32_t at, uint64_t* full, uint64_t* free, uint32_t places) {
+      const int rows = PAGED ? min(kN, 1 << a.page_log2) : kN;
+      // page ids: lane i holds that of page base + i, and of the 32 pages behind those
+      int base = -64, now = -1, next = -1;
+      auto table_at = [&](int page) { return page < a.table_width ? a.table[(long long)it.r * a.table_width + page] : -1; };
+#pragma unroll 1
+      for (int t = it.t0; t < it.t1; ++t) {
+        const int key0 = it.key0(t);
+        int page = it.r, row = key0;   // dense form: a batch row is a page
+        bool on = lane == 0;
+        uint32_t bytes = kKvTile;
+        if (PAGED) {
+          const int page0 = key0 >> a.page_log2, b = page0 & ~31;
+          if (b != base) {
+            now = b == base + 32 ? next : table_at(b + lane);
+            next = table_at(b + 32 + lane);
+            base = b;
+          }
+          const int id = __shfl_sync(0xffffffffu, now, (page0 + lane) & 31);
+          page = id >= 0 && id < a.n_pages ? id : a.n_pages;   // beyond the pool: arrives as zeros
+          row = key0 & ((1 << a.page_log2) - 1);
+          if (rows < kN) {
+            // lane i brings the i-th page of the tile, if any row of the item sees a key of it
+            const int pk0 = key0 + lane * rows;
+            on = lane < kN / rows && (pk0 < it.s.sink_n || (pk0 < it.s.hi && pk0 + rows > it.s.lo));
+            bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, on)) * (uint32_t)rows * (ZC_D * 2);
+          }
+        }
+        bar_wait(&free[stage], phase);
+        if (lane == 0) expect_bytes(&full[stage], bytes);
+        __syncwarp();
+        if (on) {
+          const uint32_t dst = at + stage * kKvTile + lane * rows * 128;
+          page_copy(map, dst, &full[stage], row, 0, it.kv, page);
+          if (rows < kN) page_copy(map, dst + kKvBlock, &full[stage], row, 1, it.kv, page);
+        }
+        __syncwarp();
+        if (++stage == places) {
+          stage = 0;
+          phase ^= 1u;
+        }
+      }
+    };
     if (warp == 2) {
-      // ---- items ----
+      // ---- items, and V ----
       const long long n_idx = (long long)k.items * a.n_req * a.h_kv;   // dense form
       long long idx = blockIdx.x;
       Border at = share.begin;
@@ -555,28 +602,53 @@ __global__ void __launch_bounds__(kThreads, 1)
       Chunk c;
       c.row0 = c.n = c.p0 = 0;
       if (PAGED && share.items > 0) c = load_chunk(a, r);
-      for (uint32_t n = 0;; ++n) {
-        Item it;
+      auto find_item = [&](Item& it) {   // the share's next item; r < 0: there is none
         it.r = -1;
-        if (PAGED) {
-          if (at.item < share.end.item || (at.item == share.end.item && at.t < share.end.t)) {
-            // (only the share's first item can begin, and only its last can end, inside)
-            it.r = r;
-            it.kv = at.item / share.items;
-            it.tok0 = in_req * 2 * k.tpt;
-            it.row0 = c.row0;
-            it.p_first = c.p0 + it.tok0;
-            it.t0 = at.t;
-            it.t1 = at.item == share.end.item ? share.end.t : 1 << 30;
-            finish_item(k, c.n, it);
-            it.slot = it.t0 > 0 ? 2 * (int)blockIdx.x : it.t1 < it.s.nb ? 2 * (int)blockIdx.x + 1 : -1;
+        if (!PAGED) {
+          if (idx < n_idx) {
+            it = dense_item(k, idx);
+            finish_item(k, k.l, it);
+            idx += gridDim.x;
           }
-        } else if (idx < n_idx) {
-          it = dense_item(k, idx);
-          finish_item(k, k.l, it);
+          return;
         }
+        if (at.item > share.end.item || (at.item == share.end.item && at.t >= share.end.t)) return;
+        // (only the share's first item can begin, and only its last can end, inside)
+        it.r = r;
+        it.kv = at.item / share.items;
+        it.tok0 = in_req * 2 * k.tpt;
+        it.row0 = c.row0;
+        it.p_first = c.p0 + it.tok0;
+        it.t0 = at.t;
+        it.t1 = at.item == share.end.item ? share.end.t : 1 << 30;
+        finish_item(k, c.n, it);
+        it.slot = it.t0 > 0 ? 2 * (int)blockIdx.x : it.t1 < it.s.nb ? 2 * (int)blockIdx.x + 1 : -1;
+        ++at.item;
+        at.t = 0;
+        if (at.item > share.end.item || (at.item == share.end.item && share.end.t == 0)) return;
+        if ((++in_req) * 2 * k.tpt >= c.n) {
+          // the next request with rows (after the last one's, the next head's first), 32 at a time
+          in_req = 0;
+          for (int r0 = at.item % share.items == 0 ? 0 : r + 1; r0 < a.n_req; r0 += 32) {
+            Chunk x;
+            x.row0 = x.n = x.p0 = 0;
+            if (r0 + lane < a.n_req) x = load_chunk(a, r0 + lane);
+            const unsigned some = __ballot_sync(0xffffffffu, x.n > 0);
+            if (some) {
+              const int src = __ffs(some) - 1;
+              r = r0 + src;
+              c.row0 = __shfl_sync(0xffffffffu, x.row0, src);
+              c.n = __shfl_sync(0xffffffffu, x.n, src);
+              c.p0 = __shfl_sync(0xffffffffu, x.p0, src);
+              break;
+            }
+          }
+        }
+      };
+      uint32_t n = 0;   // items announced
+      auto announce = [&](const Item& it) {
         const uint32_t place = n % kRingN;
-        if (n >= kRingN && !bar_wait_ok(&i_free[place], (n / kRingN - 1) & 1u)) break;
+        if (n >= kRingN && !bar_wait_ok(&i_free[place], (n / kRingN - 1) & 1u)) return false;
         if (lane == 0) {
           int* dst = ring + place * kRingInts;
           const int* src = reinterpret_cast<const int*>(&it);
@@ -584,71 +656,29 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int i = 0; i < (int)(sizeof(Item) / 4); ++i) dst[i] = src[i];
           bar_arrive(&i_full[place]);
         }
-        if (it.r < 0) break;
-        if (PAGED) {
-          ++at.item;
-          at.t = 0;
-          if (at.item >= share.end.item && share.end.t == 0) continue;
-          if ((++in_req) * 2 * k.tpt >= c.n) {
-            // the next request with rows (after the last one's, the next head's first), 32 at a time
-            in_req = 0;
-            const bool wrap = at.item % share.items == 0;
-            for (int r0 = wrap ? 0 : r + 1; r0 < a.n_req; r0 += 32) {
-              Chunk x;
-              x.row0 = x.n = x.p0 = 0;
-              if (r0 + lane < a.n_req) x = load_chunk(a, r0 + lane);
-              const unsigned some = __ballot_sync(0xffffffffu, x.n > 0);
-              if (some) {
-                const int src = __ffs(some) - 1;
-                r = r0 + src;
-                c.row0 = __shfl_sync(0xffffffffu, x.row0, src);
-                c.n = __shfl_sync(0xffffffffu, x.n, src);
-                c.p0 = __shfl_sync(0xffffffffu, x.p0, src);
-                break;
-              }
-            }
-          }
-        } else {
-          idx += gridDim.x;
-        }
+        __syncwarp();
+        ++n;
+        return true;
+      };
+      Item it, then;
+      find_item(it);
+      bool ok = announce(it);
+      while (ok && it.r >= 0) {
+        find_item(then);
+        ok = announce(then);
+        stream(it, &vmap, v_addr, v_full, v_free, kVS);
+        it = then;
       }
     } else if (warp == 1) {
-      // ---- copies ----
-      uint32_t k_n = 0, v_n = 0, item = 0, meetings = 0;   // tiles, items with tiles, narrow ones among them so far
-      // The n-th tile of keys (or values) into its place; the whole warp calls.
-      auto kv_tile = [&](const Item& it, int t, const CUtensorMap* map, uint32_t at, uint64_t* full, uint64_t* free,
-                         uint32_t places, uint32_t n) {
-        const uint32_t s = n % places;
-        const int key0 = it.key0(t);
-        if (PAGED) {
-          // lane i brings the i-th page of the tile, if any row of the item sees a key of it
-          const int rows = min(kN, 1 << a.page_log2), pk0 = key0 + lane * rows;
-          const bool on = lane < kN / rows && (pk0 < it.s.sink_n || (pk0 < it.s.hi && pk0 + rows > it.s.lo));
-          const int page = on ? a.table[(long long)it.r * a.table_width + (pk0 >> a.page_log2)] : 0;
-          const int pg = page >= 0 && page < a.n_pages ? page : a.n_pages;   // beyond the pool: arrives as zeros
-          const int row = pk0 & ((1 << a.page_log2) - 1);
-          const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, on)) * (uint32_t)rows * (ZC_D * 2);
-          if (lane == 0) {
-            if (n >= places) bar_wait(&free[s], (n / places - 1) & 1u);
-            expect_bytes(&full[s], bytes);
-          }
-          __syncwarp();
-          if (on)
-            for (int kb = 0; kb < 2; ++kb)
-              page_copy(map, at + s * kKvTile + kb * kKvBlock + lane * rows * 128, &full[s], row, kb, it.kv, pg);
-        } else if (lane == 0) {
-          if (n >= places) bar_wait(&free[s], (n / places - 1) & 1u);
-          expect_bytes(&full[s], kKvTile);
-          for (int kb = 0; kb < 2; ++kb) q_copy(map, at + s * kKvTile + kb * kKvBlock, &full[s], kb, it.kv, key0, it.r, true);
-        }
-      };
-      bool met = true;                             // the last item's meeting is waited for (or it had none)
+      // ---- Q and K ----
+      uint32_t item = 0, meetings = 0, met = 0;   // items with tiles, narrow ones, meetings waited for
       Item it;
       while (next_item(it)) {
         if (it.t0 >= it.t1) continue;
+        if (item > 0) bar_wait(q_free, (item - 1) & 1u);
+        // a wide item needs the second Q tile's place, where the groups meet over narrow ones
+        for (; met + (it.narrow ? 1u : 0u) < meetings; ++met) bar_wait(&m_free[met & 1u], (met >> 1) & 1u);
         if (lane == 0) {
-          if (item > 0) bar_wait(q_free, (item - 1) & 1u);
-          if (!met) bar_wait(m_free, (meetings - 1) & 1u);
           const int tiles = it.narrow ? 1 : 2;
           expect_bytes(q_full, (uint32_t)(tiles * k.tpt * a.G * ZC_D * 2));
           for (int g = 0; g < tiles; ++g)
@@ -656,20 +686,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               q_copy(&qmap, q_addr + g * kTile + kb * kKBlock, q_full, kb, it.kv * a.G,
                      it.row0 + it.tok0 + g * k.tpt, PAGED ? 0 : it.r);
         }
+        __syncwarp();
         ++item;
-        met = !it.narrow;
         meetings += it.narrow ? 1u : 0u;
-        // keys run two tiles ahead of the values, as their products do
-        for (int t = it.t0 - 2; t < it.t1; ++t) {
-          if (t >= it.t0) {
-            kv_tile(it, t, &vmap, v_addr, v_full, v_free, kVS, v_n);
-            ++v_n;
-          }
-          if (t + 2 < it.t1) {
-            kv_tile(it, t + 2, &kmap, k_addr, k_full, k_free, kKS, k_n);
-            ++k_n;
-          }
-        }
+        stream(it, &kmap, k_addr, k_full, k_free, kKS);
       }
     } else {
       // ---- matrix products of group g ----
@@ -753,7 +773,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
     const uint32_t tmem_g = tmem + lane_off + (uint32_t)g * kM, tmem_o = tmem + lane_off + (uint32_t)(2 + g) * kM;
     const float scale = kLog2e * rsqrtf((float)ZC_D);
-    uint32_t tile0 = 0, n_s = 0, n_o = 0, n_last = 0;
+    uint32_t tile0 = 0, n_s = 0, n_o = 0, n_last = 0, meetings = 0;
     Item it;
     while (next_item(it)) {
       const int rows_at = it.narrow ? 0 : g;                         // which tile of rows
@@ -858,8 +878,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool other = meet && it.t0 + 1 < it.t1;                  // group 1 has a share of a narrow item
       float f_own = 1.f, f_other = 0.f;
       if (meet) {
-        // group 1's sums and its O, 32 channels at a time through two halves of the second Q tile's place, to
-        // group 0 (which has read a half by the time the other half's values are announced)
+        // group 1's sums, and its O by halves, to group 0
         if (g == 1) s_ms[row] = make_float2(m_run, s_run);
         groups_sync();
         if (g == 0 && other) {
@@ -876,9 +895,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float inv = some ? 1.f / s_run : 0.f;
       const int h = it.kv * a.G + head_in;
       const long long at = (PAGED ? 0 : it.r * k.o_req) + (long long)(it.row0 + it.tok0 + tok) * k.o_row + h * k.o_head;
-      float* pr = nullptr;
-      if (PAGED && it.slot >= 0)
-        pr = k.ws.parts + ((long long)it.slot * kItemRows + rows_at * kM + row) * kPartStride;
+      char* part = PAGED && it.slot >= 0 ? k.ws.parts + (long long)it.slot * kPartBytes : nullptr;
+      const int prow = rows_at * kM + row;
+      // Output rows leave through the warp's 2 KB of shared memory, 32 channels at a time, so that a store writes 64
+      // bytes of each of eight rows: lane i then has rows i / 4 + 8 j, whose places it asks the owners for.
+      const unsigned writers = __ballot_sync(0xffffffffu, writer);
+      long long at_j[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) at_j[j] = __shfl_sync(0xffffffffu, at, (lane >> 2) + 8 * j);
+      char* stage = base + 2 * kTile + (kKS + kVS) * kKvTile + (warp - 4) * kOutTile;
 #pragma unroll 1
       for (int q4 = 0; q4 < 4; ++q4) {
         float o[32];
@@ -890,13 +915,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int e = 0; e < 32; ++e) o[e] = 0.f;
         }
         if (other) {
-          float4* xr = reinterpret_cast<float4*>(base + kTile) + row * 16 + 8 * (q4 & 1);   // 64 channels a row
+          // through the place of the second Q tile: 128 rows x 32 channels, twice
+          float4* xr = reinterpret_cast<float4*>(base + kTile) + row * 16 + 8 * (q4 & 1);
           if (g == 1) {
 #pragma unroll
             for (int c = 0; c < 8; ++c) xr[c ^ (row & 7)] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
             async_proxy_fence();
           }
-          groups_sync();
+          groups_sync();   // (group 0 has read the half before last by now)
           if (g == 0) {
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
@@ -908,33 +934,40 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         }
-        if (writer) {
-          if (!pr) {
-            T* orow = reinterpret_cast<T*>(a.out) + at + 32 * q4;
-#pragma unroll
-            for (int c4 = 0; c4 < 4; ++c4) {
-              uint4 w = make_uint4(pack2<T>(o[8 * c4] * inv, o[8 * c4 + 1] * inv),
-                                   pack2<T>(o[8 * c4 + 2] * inv, o[8 * c4 + 3] * inv),
-                                   pack2<T>(o[8 * c4 + 4] * inv, o[8 * c4 + 5] * inv),
-                                   pack2<T>(o[8 * c4 + 6] * inv, o[8 * c4 + 7] * inv));
-              if (!some) w = make_uint4(0, 0, 0, 0);
-              *reinterpret_cast<uint4*>(orow + 8 * c4) = w;
-            }
-          } else {
+        if (part) {
+          if (writer)
 #pragma unroll
             for (int c = 0; c < 8; ++c)
-              *reinterpret_cast<float4*>(pr + 4 + 32 * q4 + 4 * c) =
+              reinterpret_cast<float4*>(part)[(8 * q4 + c) * kItemRows + prow] =
                   make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+        } else if (writers) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint4 w = make_uint4(pack2<T>(o[8 * c] * inv, o[8 * c + 1] * inv), pack2<T>(o[8 * c + 2] * inv, o[8 * c + 3] * inv),
+                                 pack2<T>(o[8 * c + 4] * inv, o[8 * c + 5] * inv), pack2<T>(o[8 * c + 6] * inv, o[8 * c + 7] * inv));
+            if (!some) w = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = w;
           }
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int src = (lane >> 2) + 8 * j;
+            const uint4 w = *reinterpret_cast<const uint4*>(stage + src * 64 + (((lane & 3) ^ ((src >> 1) & 3)) << 4));
+            if ((writers >> src) & 1u)
+              *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.out) + at_j[j] + 32 * q4 + 8 * (lane & 3)) = w;
+          }
+          __syncwarp();
         }
       }
       if (writer) {
-        if (!pr && a.lse) a.lse[at / ZC_D] = some ? m_run + log2f(s_run) : -INFINITY;
-        if (pr) *reinterpret_cast<float4*>(pr) = make_float4(m_run, any ? s_run : 0.f, 0.f, 0.f);
+        if (!part && a.lse) a.lse[at / ZC_D] = some ? m_run + log2f(s_run) : -INFINITY;
+        if (part)
+          reinterpret_cast<float2*>(part + kItemRows * ZC_D * 4)[prow] = make_float2(m_run, any ? s_run : 0.f);
       }
       if (meet) {
         groups_sync();   // the second Q tile's place and the sums are free
-        if (tid == 128) bar_arrive(m_free);
+        if (tid == 128) bar_arrive(&m_free[meetings & 1u]);
+        ++meetings;
       }
       // this row's O is in registers or memory: the next item's products may overwrite it
       tc_fence_before();
@@ -948,7 +981,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Rows of the items that were worked on in pieces.  Block (c - 1) * 16 + i: rows 16 i ... of the item that the
-// border before CTA c cuts first; a warp takes two rows.
+// border before CTA c cuts first; a thread takes eight channels of a row.
 template <typename T> __global__ void __launch_bounds__(256) k_chunk_join(const ChunkArgs k) {
   __shared__ int s_slot[ZC_PAGED_MAX_CTAS + 1], s_count;
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
@@ -971,15 +1004,39 @@ template <typename T> __global__ void __launch_bounds__(256) k_chunk_join(const 
   }
   __syncthreads();
   const int n = s_count;
+  const int row = (int)(blockIdx.x % 16) * 16 + (threadIdx.x & 15), cg = threadIdx.x >> 4;
+  const int g = row / kM, in = row % kM, tok_in = in / a.G, tok = j.tok0 + g * k.tpt + tok_in;
+  if (tok_in >= k.tpt || tok >= c.n) return;
+  auto sums = [&](int q) {
+    return reinterpret_cast<const float2*>(k.ws.parts + (long long)s_slot[q] * kPartBytes + kItemRows * ZC_D * 4)[row];
+  };
+  float m = -1e30f;
+#pragma unroll 4
+  for (int q = 0; q < n; ++q) m = fmaxf(m, sums(q).x);
+  float sum = 0.f;
+  float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 2
+  for (int q = 0; q < n; ++q) {
+    const float4* p = reinterpret_cast<const float4*>(k.ws.parts + (long long)s_slot[q] * kPartBytes) + row;
+    const float2 ms = sums(q);
+    const float4 x[2] = {p[cg * kItemRows], p[(cg + 16) * kItemRows]};
+    const float f = zc_exp2(ms.x - m);
+    sum = fmaf(ms.y, f, sum);
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int row = (int)(blockIdx.x % 16) * 16 + warp + 8 * u, g = row / kM, in = row % kM;
-    const int tok_in = in / a.G, tok = j.tok0 + g * k.tpt + tok_in;
-    if (tok_in >= k.tpt || tok >= c.n) continue;
-    const long long at = (long long)(c.row0 + tok) * a.h_q + j.kv * a.G + (in - tok_in * a.G);
-    join_row<T>(a.out, a.lse, at, lane, n,
-                [&](int q) { return k.ws.parts + ((long long)s_slot[q] * kItemRows + row) * kPartStride; });
+    for (int u = 0; u < 2; ++u) {
+      acc[u].x = fmaf(x[u].x, f, acc[u].x);
+      acc[u].y = fmaf(x[u].y, f, acc[u].y);
+      acc[u].z = fmaf(x[u].z, f, acc[u].z);
+      acc[u].w = fmaf(x[u].w, f, acc[u].w);
+    }
   }
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const long long at = (long long)(c.row0 + tok) * a.h_q + j.kv * a.G + (in - tok_in * a.G);
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.out) + at * ZC_D + 4 * (cg + 16 * u)) =
+        make_uint2(pack2<T>(acc[u].x * inv, acc[u].y * inv), pack2<T>(acc[u].z * inv, acc[u].w * inv));
+  if (a.lse && cg == 0) a.lse[at] = sum > 0.f ? m + log2f(sum) : -INFINITY;
 }
 
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
@@ -996,7 +1053,7 @@ size_t carve(char* ws, ChunkWs* out) {
   ChunkWs w;
   w.joins = (ChunkJoin*)take(ZC_PAGED_MAX_CTAS * sizeof(ChunkJoin));
   w.used = (int*)take(ZC_PAGED_MAX_CTAS * sizeof(int));
-  w.parts = (float*)take((size_t)ZC_PAGED_MAX_CTAS * 2 * kItemRows * kPartStride * sizeof(float));
+  w.parts = take((size_t)ZC_PAGED_MAX_CTAS * 2 * kPartBytes);
   if (out) *out = w;
   return off;
 }
@@ -1028,17 +1085,18 @@ bool make_q_map(CUtensorMap* map, const void* q, int dtype, int h_q, int G, long
   return zc_encode_map(map, dtype, 4, q, dims, strides, box);
 }
 
-// Dense K or V as (channels, tokens, KV heads, batch rows), boxes of 64 channels x 64 tokens.
+// Dense K or V as pages: a batch row is a page of l tokens (64 channels, token, half of the channels, KV head,
+// batch row), boxes of 64 tokens.
 bool make_dense_map(CUtensorMap* map, const void* x, const zc_config& cfg, int l, const int64_t* ks) {
-  const cuuint64_t dims[4] = {ZC_D, (cuuint64_t)l, (cuuint64_t)cfg.n_kv_heads, (cuuint64_t)cfg.batch};
-  const long long s[3] = {ks[2], cfg.n_kv_heads > 1 ? ks[1] : ZC_D, cfg.batch > 1 ? ks[0] : ZC_D};
-  cuuint64_t strides[3];
-  for (int i = 0; i < 3; ++i) {
+  const cuuint64_t dims[5] = {64, (cuuint64_t)l, 2, (cuuint64_t)cfg.n_kv_heads, (cuuint64_t)cfg.batch};
+  const long long s[4] = {ks[2], 64, cfg.n_kv_heads > 1 ? ks[1] : ZC_D, cfg.batch > 1 ? ks[0] : ZC_D};
+  cuuint64_t strides[4];
+  for (int i = 0; i < 4; ++i) {
     if (s[i] <= 0 || (s[i] & 7)) return false;
     strides[i] = (cuuint64_t)s[i] * 2;
   }
-  const cuuint32_t box[4] = {64, kN, 1, 1};
-  return zc_encode_map(map, cfg.dtype, 4, x, dims, strides, box);
+  const cuuint32_t box[5] = {64, kN, 2, 1, 1};
+  return zc_encode_map(map, cfg.dtype, 5, x, dims, strides, box);
 }
 
 template <typename T>

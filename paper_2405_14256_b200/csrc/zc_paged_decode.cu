@@ -490,7 +490,9 @@ bool zc_page_maps(zc_pages* p) {
                               (cuuint64_t)p->cfg.n_pages};
   const cuuint64_t strides[4] = {(cuuint64_t)s[1] * 2, 128, (cuuint64_t)s[2] * 2, (cuuint64_t)s[0] * 2};
   const cuuint32_t small[5] = {64, kBlk, 2, 1, 1};
-  const cuuint32_t large[5] = {64, (cuuint32_t)(p->cfg.page_size < 64 ? p->cfg.page_size : 64), 1, 1, 1};
+  // a tile of 64 keys from one page comes with both halves of its channels, from several pages half by half
+  const bool one = p->cfg.page_size >= 64;
+  const cuuint32_t large[5] = {64, (cuuint32_t)(one ? 64 : p->cfg.page_size), one ? 2u : 1u, 1, 1};
   struct { CUtensorMap* map; void* at; const cuuint32_t* box; } todo[4] = {
       {&p->k16, p->k, small}, {&p->v16, p->v, small}, {&p->k64, p->k, large}, {&p->v64, p->v, large}};
   for (auto& t : todo)

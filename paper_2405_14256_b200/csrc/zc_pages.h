@@ -16,7 +16,7 @@ struct zc_pages {
   int G, page_log2, n_sm;
   bool maps_ready;
   CUtensorMap k16, v16;    // boxes of 16 tokens x 128 elements (two 128-byte halves)
-  CUtensorMap k64, v64;    // boxes of min(page, 64) tokens x 64 elements
+  CUtensorMap k64, v64;    // boxes of min(page, 64) tokens x 64 elements (x 2 halves from 64 on)
   long long launches;
 };
 
