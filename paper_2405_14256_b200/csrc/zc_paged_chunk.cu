@@ -43,14 +43,9 @@ constexpr int kTiles = 2 * kTile + (kKS + kVS) * kKvTile + 8 * kOutTile;   // 22
 constexpr int kRingN = 2;                             // items fetched ahead
 constexpr int kRingInts = 24;
 constexpr int kSmem = kTiles + 1024 + 384 + 1024 + kRingN * kRingInts * 4;   // alignment, barriers, (m, sum) of group 1
-#ifndef KPOLY
-#define KPOLY 0
-#endif
-constexpr int kPoly = KPOLY;                              // of 8 pairs of weights, those without the exp2 unit
 constexpr float kNoMax = -1e30f;                      // running maximum before any key
 constexpr float kTau = 3.f;                           // a new maximum is taken where it exceeds the old by this (base 2)
 constexpr float kBigSum = 1024.f;                     // ... and looked for where a tile's weights sum to more than this
-constexpr float kTopPoly = 16.f;                      // ... or one that the exp2 unit did not compute has this exponent
 constexpr int kItemRows = 2 * kM;
 // A piece's partial result: 32 x 256 groups of 4 channels, [group of channels][row], so that the threads that
 // own neighbouring rows write neighbouring 16 bytes; then (maximum, sum) [row].
@@ -395,47 +390,19 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;\n" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// 2^x of two values without the exp2 unit: x = n + f with n the nearest whole number (the low bits of
-// x + 1.5 * 2^23), 2^f by the polynomial of degree 5 whose largest relative error on |f| <= 1/2 is least
-// (7.5e-8, found by the Remez exchange), n added to the exponent.  x is held at -126 or more.
-__device__ __forceinline__ float2 exp2_poly(float2 x) {
-  x.x = fmaxf(x.x, -126.f);
-  x.y = fmaxf(x.y, -126.f);
-  const float2 big = make_float2(12582912.f, 12582912.f), neg = make_float2(-12582912.f, -12582912.f);
-  const float2 t = add2(x, big), n = add2(t, neg);
-  const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
-  float2 p = fma2(f, make_float2(1.32764721678e-3f, 1.32764721678e-3f), make_float2(9.67554133102e-3f, 9.67554133102e-3f));
-  p = fma2(p, f, make_float2(5.55071327288e-2f, 5.55071327288e-2f));
-  p = fma2(p, f, make_float2(0.24022119724f, 0.24022119724f));
-  p = fma2(p, f, make_float2(0.693146967065f, 0.693146967065f));
-  p = fma2(p, f, make_float2(1.00000007165f, 1.00000007165f));
-  return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
-                     __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
-}
-
 // The weights of 64 keys, 2^(v * scale - m), packed to the input type; returns their sum (of the unrounded
-// values).  POLY of every 8 pairs take exp2_poly: the exp2 unit, at a quarter of a warp per cycle and
-// quarter of the SM, would otherwise be what the groups wait for.  top: the largest exponent among those
-// (the exp2 unit's weights become infinite, and the sum with them, where theirs would be wrong).
-template <typename T, int POLY>
-__device__ __forceinline__ float weights(const float* v, float scale, float m, uint32_t* w, float* top) {
+// values).  All exponentials go through the exp2 unit: a quarter of them by a polynomial on the FMA pipe
+// instead measured the same to 7 % slower.
+template <typename T> __device__ __forceinline__ float weights(const float* v, float scale, float m, uint32_t* w) {
   const float2 sc = make_float2(scale, scale), neg_m = make_float2(-m, -m);
   float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-  float t = -INFINITY;
 #pragma unroll
   for (int c = 0; c < kN / 2; ++c) {
     const float2 x = fma2(make_float2(v[2 * c], v[2 * c + 1]), sc, neg_m);
-    float2 p;
-    if (POLY && (c * POLY) % 8 + POLY > 7) {
-      t = max3(t, x.x, x.y);
-      p = exp2_poly(x);
-    } else {
-      p = make_float2(zc_exp2(x.x), zc_exp2(x.y));
-    }
+    const float2 p = make_float2(zc_exp2(x.x), zc_exp2(x.y));
     add[c & 1] = add2(add[c & 1], p);
     w[c] = pack2<T>(p.x, p.y);
   }
-  if (POLY) *top = t;
   add[0] = add2(add[0], add[1]);
   return add[0].x + add[0].y;
 }
@@ -823,9 +790,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         float sum = 0.f;
         bool renew = edge || unset;
         if (!renew) {
-          float top;
-          sum = weights<T, kPoly>(v, scale, m_run, w, &top);
-          renew = __any_sync(0xffffffffu, !(sum <= kBigSum) || top > kTopPoly);
+          sum = weights<T>(v, scale, m_run, w);
+          renew = __any_sync(0xffffffffu, !(sum <= kBigSum));
         }
         if (renew) {
           float mx4[4] = {v[0], v[1], v[2], v[3]};
@@ -856,7 +822,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (grow) m_run = mx;
           }
           unset = __any_sync(0xffffffffu, valid && m_run == kNoMax);
-          sum = weights<T, 0>(v, scale, m_run, w, nullptr);   // hidden keys weigh 0 exactly
+          sum = weights<T>(v, scale, m_run, w);
         }
         tmem_st32(w, tmem_s);
         asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
