@@ -292,9 +292,11 @@ typedef struct zc_pages zc_pages; /* small host-side handle */
 
 /* Device scratch [host] that zc_paged_attention needs for calls of up to n_req requests and n_rows rows
  * (partial results of rows whose keys several CTAs share).  ZC_ECAPACITY when one call cannot take so many:
- * n_req + n_rows / (2 * floor(128 / G)) may be 13000, G = n_q_heads / n_kv_heads.  The scratch needs no
- * initialisation and nothing in it survives a call; it must not be used by calls that may run at the same
+ * n_req + n_rows / (2 * floor(128 / G)) may be 13000, G = n_q_heads / n_kv_heads.  Its first
+ * ZC_PAGES_SYNC_BYTES must be zero before its first use (every call leaves them zero again); nothing else
+ * in it needs initialisation or survives a call.  It must not be used by calls that may run at the same
  * time (other streams, graphs replayed side by side). */
+#define ZC_PAGES_SYNC_BYTES 1024
 int zc_pages_workspace(const zc_page_config* cfg, int n_req, int n_rows, size_t* workspace_bytes);
 /* Handle over caller-owned pages K, V [device, 16-byte aligned].  No device work is enqueued. */
 int zc_pages_init(void* k_pages, void* v_pages, const zc_page_config* cfg, zc_pages** out);

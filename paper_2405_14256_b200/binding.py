@@ -18,6 +18,7 @@ ZC_FLAG_OUT_F32 = 4
 ZC_FLAG_PARAMS_F16 = 8
 ZC_FLAG_GROUP_ALL_HEADS = 16
 ZC_K_CST, ZC_K_CHANNEL = 0, 1
+ZC_PAGES_SYNC_BYTES = 1024
 ZC_SCOPE_KV_HEAD, ZC_SCOPE_TOKEN = 0, 1
 
 
@@ -160,6 +161,18 @@ def _stream(stream) -> int:
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
+
+
+_I64x2, _I64x3 = C.c_int64 * 2, C.c_int64 * 3
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(device_index: int, stream) -> int:
+    """_stream for a device known to be current, without building a torch.cuda.Stream."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device_index)
+    return _stream(stream)
 
 
 def zc_strerror(status: int) -> str:
@@ -372,21 +385,11 @@ def _want(t, name: str, shape, dtype, contiguous: bool = True) -> None:
                             f"{t.dtype} {tuple(t.shape)} with strides {t.stride()}")
 
 
-class _OnDevice:
-    """The library works on the calling thread's current device: makes `device` current for the
-    call when another one is, and picks its current stream unless one is given."""
-
-    def __init__(self, device):
-        self.device = device
-
-    def __enter__(self):
-        self.other = torch.cuda.current_device()
-        if self.other != self.device.index:
-            torch.cuda.set_device(self.device)
-
-    def __exit__(self, *exc):
-        if self.other != self.device.index:
-            torch.cuda.set_device(self.other)
+def _want_i32(t, name: str, n: int) -> None:
+    """Refuses anything but n contiguous int32 values on a GPU."""
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ZipCacheError(f"{name}: expected {n} contiguous int32 values on a GPU, got {t.dtype} {tuple(t.shape)} "
+                            f"with strides {t.stride()} on {t.device}")
 
 
 def _cuda_device(device) -> torch.device:
@@ -403,24 +406,29 @@ class StepTables:
 
     def __init__(self, n_req: int, n_rows: int, device="cuda:0"):
         self.device = _cuda_device(device)
-        self.n_req, self.n_rows = n_req, n_rows
+        self.n_req, self.n_rows, self._index = n_req, n_rows, self.device.index
         new = lambda n: torch.zeros(n, dtype=torch.int32, device=self.device)  # noqa: E731
         self.kv_len, self.row_start, self.slots, self.pos = new(n_req), new(n_req + 1), new(n_rows), new(n_rows)
         self.free_state = new(3)
-        self._on = _OnDevice(self.device)
 
     def build(self, page_size: int, past, fresh, free_pages, free_state, table, stream=None) -> "StepTables":
         """past, fresh [n_req], free_pages [any], free_state [3] (next, end, -) and table [n_req, width]
         (extended in place), all int32 on this object's device."""
-        i32 = torch.int32
-        _want(past, "past", (self.n_req,), i32)
-        _want(fresh, "fresh", (self.n_req,), i32)
-        _want(free_pages, "free_pages", (free_pages.numel(),), i32)
-        _want(free_state, "free_state", (3,), i32)
-        _want(table, "table", (self.n_req, table.shape[-1]), i32)
-        with self._on:
-            zc_page_tables(page_size, past, fresh, free_pages, free_state, table, self.kv_len, self.row_start,
-                           self.slots, self.pos, self.free_state, stream)
+        if _current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.build(page_size, past, fresh, free_pages, free_state, table, stream)
+        n = self.n_req
+        _want_i32(past, "past", n)
+        _want_i32(fresh, "fresh", n)
+        _want_i32(free_pages, "free_pages", free_pages.numel())
+        _want_i32(free_state, "free_state", 3)
+        width = table.size(-1)
+        _want_i32(table, "table", n * width)
+        _check(lib().zc_page_tables(page_size, n, past.data_ptr(), fresh.data_ptr(), free_pages.data_ptr(),
+                                    free_pages.numel(), free_state.data_ptr(), table.data_ptr(), width,
+                                    self.kv_len.data_ptr(), self.row_start.data_ptr(), self.n_rows,
+                                    self.slots.data_ptr(), self.pos.data_ptr(), self.free_state.data_ptr(),
+                                    _stream_of(self._index, stream)), "zc_page_tables")
         return self
 
 
@@ -428,7 +436,8 @@ class PagedKV:
     """Keys and values at full precision in pages: a handle over the caller's tensors, both
     [n_pages, page_size, n_kv_heads, 128] with any strides of the first three dimensions (for pages
     stored [n_pages, n_kv_heads, page_size, 128] pass .transpose(1, 2)).  Holds the workspace of
-    attention calls of up to max_req requests and max_rows rows."""
+    attention calls of up to max_req requests and max_rows rows; one that is given (to share it among
+    the handles of a stream) must have its first ZC_PAGES_SYNC_BYTES zeroed once."""
 
     def __init__(self, k_pages, v_pages, n_q_heads: int, max_req: int = 256, max_rows: int = 8192,
                  workspace: Optional[torch.Tensor] = None):
@@ -443,14 +452,16 @@ class PagedKV:
         self.cfg = ZcPageConfig.make(k_pages.dtype, n_q_heads, n_kv, page_size, n_pages, k_pages.stride()[:3], d)
         self.k_pages, self.v_pages = k_pages, v_pages
         self.dtype, self.page_size, self.n_q_heads, self.n_kv_heads = k_pages.dtype, page_size, n_q_heads, n_kv
+        self._index = self.device.index
         self.workspace_bytes = zc_pages_workspace(self.cfg, max_req, max_rows)
-        self._on = _OnDevice(self.device)
         if workspace is None:
             workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
-        if workspace.numel() * workspace.element_size() < self.workspace_bytes:
+            workspace[:ZC_PAGES_SYNC_BYTES].zero_()
+        self._ws_bytes = workspace.numel() * workspace.element_size()
+        if self._ws_bytes < self.workspace_bytes:
             raise ZipCacheError("shared workspace too small")
         self.workspace = workspace
-        with self._on:
+        with torch.cuda.device(self._index):
             self.handle = zc_pages_init(k_pages, v_pages, self.cfg)
 
     def close(self):
@@ -464,29 +475,42 @@ class PagedKV:
         except Exception:
             pass
 
+    def _rows(self, t, name: str, n: int, heads: int) -> None:
+        """Refuses anything but [n, heads, 128] of the pages' type with contiguous channels."""
+        if t.dtype is not self.dtype or t.dim() != 3 or t.size(0) != n or t.size(1) != heads or t.size(2) != 128 \
+                or t.stride(2) != 1:
+            raise ZipCacheError(f"{name}: expected {self.dtype} {(n, heads, 128)} with contiguous channels, got "
+                                f"{t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+
     def write(self, k_rows, v_rows, slots, stream=None):
         """Rows [n, n_kv_heads, 128] into slots [n] (int32; negative: skipped)."""
-        shape = (slots.numel(), self.n_kv_heads, 128)
-        _want(slots, "slots", shape[:1], torch.int32)
-        _want(k_rows, "k_rows", shape, self.dtype, contiguous=False)
-        _want(v_rows, "v_rows", shape, self.dtype, contiguous=False)
-        if k_rows.stride(2) != 1:
-            raise ZipCacheError("the channels of a row must be contiguous")
-        with self._on:
-            zc_page_write(self.handle, k_rows, v_rows, slots, stream)
+        if _current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.write(k_rows, v_rows, slots, stream)
+        n = slots.numel()
+        _want_i32(slots, "slots", n)
+        self._rows(k_rows, "k_rows", n, self.n_kv_heads)
+        self._rows(v_rows, "v_rows", n, self.n_kv_heads)
+        strides = k_rows.stride()
+        if strides != v_rows.stride():
+            raise ZipCacheError("k_rows and v_rows must share strides")
+        _check(lib().zc_page_write(self.handle, k_rows.data_ptr(), v_rows.data_ptr(), _I64x2(strides[0], strides[1]),
+                                   slots.data_ptr(), n, _stream_of(self._index, stream)), "zc_page_write")
 
     def read(self, table, l: int, K=None, V=None, stream=None):
         """The first l tokens of every request in table [n_req, width]: K, V [n_req, n_kv_heads, l, 128]."""
-        shape = (table.shape[0], self.n_kv_heads, l, 128)
+        if _current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.read(table, l, K, V, stream)
         _want(table, "table", (table.shape[0], table.shape[-1]), torch.int32)
+        shape = (table.shape[0], self.n_kv_heads, l, 128)
         K = torch.empty(shape, dtype=self.dtype, device=self.device) if K is None else K
         V = torch.empty(shape, dtype=self.dtype, device=self.device) if V is None else V
         _want(K, "K", shape, self.dtype, contiguous=False)
         _want(V, "V", shape, self.dtype, contiguous=False)
         if K.stride(3) != 1:
             raise ZipCacheError("the channels of a row must be contiguous")
-        with self._on:
-            zc_page_read(self.handle, table, l, K, V, stream)
+        zc_page_read(self.handle, table, l, K, V, stream)
         return K, V
 
     def attention(self, q, table, row_start, kv_len, max_rows: int, window: int = 0, sinks: int = 0, out=None,
@@ -495,22 +519,30 @@ class PagedKV:
         row_start[r + 1] - 1 are the last of kv_len[r] tokens), to the cached keys and values: out like q
         (contiguous) and the rows' base-2 log-sum-exp [n_rows, n_q_heads].  max_rows bounds a request's
         rows; window > 0 keeps the last `window` tokens and the first `sinks` ones visible."""
-        n_req, i32 = kv_len.numel(), torch.int32
-        _want(q, "q", (q.shape[0], self.n_q_heads, 128), self.dtype, contiguous=False)
-        _want(kv_len, "kv_len", (n_req,), i32)
-        _want(row_start, "row_start", (n_req + 1,), i32)
-        _want(table, "table", (n_req, table.shape[-1]), i32)
-        if q.stride(2) != 1:
-            raise ZipCacheError("the channels of a row must be contiguous")
+        if _current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.attention(q, table, row_start, kv_len, max_rows, window, sinks, out, row_lse, stream)
+        n_req, n, heads = kv_len.numel(), q.size(0), self.n_q_heads
+        self._rows(q, "q", n, heads)
+        _want_i32(kv_len, "kv_len", n_req)
+        _want_i32(row_start, "row_start", n_req + 1)
+        width = table.size(-1)
+        _want_i32(table, "table", n_req * width)
         if out is None:
-            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+            out = torch.empty((n, heads, 128), dtype=self.dtype, device=self.device)
+        else:
+            self._rows(out, "out", n, heads)
+            if not out.is_contiguous():
+                raise ZipCacheError("out must be contiguous")
         if row_lse is None:
-            row_lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device)
-        _want(out, "out", q.shape, self.dtype)
-        _want(row_lse, "row_lse", q.shape[:2], torch.float32)
-        with self._on:
-            zc_paged_attention(self.handle, q, table, row_start, kv_len, max_rows, window, sinks, out, row_lse,
-                               self.workspace, stream)
+            row_lse = torch.empty((n, heads), dtype=torch.float32, device=self.device)
+        elif row_lse.dtype is not torch.float32 or row_lse.numel() != n * heads or not row_lse.is_contiguous():
+            _want(row_lse, "row_lse", (n, heads), torch.float32)
+        strides = q.stride()
+        _check(lib().zc_paged_attention(self.handle, q.data_ptr(), _I64x2(strides[0], strides[1]), table.data_ptr(), width,
+                                        row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
+                                        out.data_ptr(), row_lse.data_ptr(), self.workspace.data_ptr(), self._ws_bytes,
+                                        _stream_of(self._index, stream)), "zc_paged_attention")
         return out, row_lse
 
 

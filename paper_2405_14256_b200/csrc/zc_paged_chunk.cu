@@ -1010,7 +1010,7 @@ int tokens_per_tile(int G) { return kM / G; }
 
 // Places of the parts of a call's workspace; returns the bytes.
 size_t carve(char* ws, ChunkWs* out) {
-  size_t off = 0;
+  size_t off = ZC_PAGES_SYNC_BYTES;   // the single-token kernel's counters stay as they are
   auto take = [&](size_t bytes) {
     char* p = ws + off;
     off += round_up(bytes);

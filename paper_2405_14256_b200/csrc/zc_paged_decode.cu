@@ -12,8 +12,9 @@
 //                                         would be) and transposed in registers
 // Running maximum and sum per row in fp32; O is rescaled only when a row's maximum grows by more than
 // 8 (base 2).  At the end of a unit's steps the eight warps' results meet in shared memory.  A unit
-// that one CTA holds whole is written out; one that a share's border cuts goes to the workspace, and
-// k_paged_join puts its pieces together in the order of the CTAs (the result does not depend on timing).
+// that one CTA holds whole is written out; the pieces of one that a share's border cuts go to the workspace,
+// and the CTA that brings the last of them puts them together, in the order of the CTAs (the result does not
+// depend on timing).  It knows by a counter per unit, zero before and after every call.
 #include <cstring>
 #include "zc_pages.h"
 #include "zc_layout.cuh"
@@ -29,16 +30,11 @@ constexpr int kStages = 3;
 constexpr int kRing = kDecWarps * kStages * 2 * kHalf; // 192 KB
 constexpr int kJoinStride = ZC_PART_STRIDE;            // m, sum, -, -, acc[128]
 constexpr int kJoinBytes = kDecWarps * 8 * kJoinStride * 4;
-constexpr int kScanBytes = kDecWarps * 8 + 16;
+constexpr int kScanBytes = kDecWarps * 8 + 80;        // warps' sums; where the share begins
 constexpr int kDecSmem = kRing + kJoinBytes + kDecWarps * kStages * 8 + kScanBytes + 1024;   // 1 KB: alignment
 constexpr float kNoMax = -1e30f;                       // running maximum before any key
+static_assert(ZC_PAGED_MAX_CTAS * 4 <= ZC_PAGES_SYNC_BYTES, "a counter per CTA");
 constexpr float kTau = 8.f;
-
-// What k_paged_join needs to know about the unit that a CTA's share begins inside.
-struct JoinDesc {
-  int on, first_cta, last_cta, kv, row0, rows;
-  int first_slot, pad;
-};
 
 struct Req {
   int row0, n, p0;   // first row, rows, position of the first
@@ -54,6 +50,17 @@ __device__ __forceinline__ int load_req(const ZcPagedArgs& a, int r, Req* q) {
   q->p0 = kv - (e1 - e0);
   q->s = zc_seen(q->p0, q->p0 + q->n - 1, a.window, a.sinks, kBlkLog2);
   return q->n > 0 ? max(1, (q->s.nb + kDecWarps - 1) / kDecWarps) : 0;
+}
+
+static_assert(sizeof(Req) + 16 <= 80, "the share's first request fits its place");
+
+// a * b / c; the quotient of 32-bit numbers where they fit (a <= 160).
+__device__ __forceinline__ long long muldiv(int a, long long b, int c) {
+  return b < (1 << 24) ? (long long)((uint32_t)a * (uint32_t)b / (uint32_t)c) : a * b / c;
+}
+// The CTA whose share holds step s of `total` in g shares.
+__device__ __forceinline__ int share_of(long long s, long long total, int g) {
+  return total < (1 << 24) ? (int)((((uint32_t)s + 1u) * (uint32_t)g - 1u) / (uint32_t)total) : (int)(((s + 1) * g - 1) / total);
 }
 
 // One unit's steps a .. b - 1 inside a CTA's share.
@@ -98,7 +105,7 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t add
 // NT: groups of 8 rows
 template <typename T, int NT>
 __global__ void __launch_bounds__(kDecThreads, 1)
-    k_paged_decode(const ZcPagedArgs a, float* __restrict__ parts, JoinDesc* __restrict__ descs,
+    k_paged_decode(const ZcPagedArgs a, float* __restrict__ parts, unsigned* __restrict__ arrived,
                    const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
   extern __shared__ __align__(1024) char smem_raw[];
   const uint32_t raw_u = zc_smem_u32(smem_raw);
@@ -107,88 +114,91 @@ __global__ void __launch_bounds__(kDecThreads, 1)
   float* s_join = reinterpret_cast<float*>(base + kRing);
   uint64_t* bars = reinterpret_cast<uint64_t*>(base + kRing + kJoinBytes);
   long long* s_sum = reinterpret_cast<long long*>(bars + kDecWarps * kStages);
-  volatile long long& s_off = *reinterpret_cast<volatile long long*>(s_sum + kDecWarps);
-  volatile int& s_req = *reinterpret_cast<volatile int*>(s_sum + kDecWarps + 1);
+  int* s_first = reinterpret_cast<int*>(s_sum + kDecWarps);   // the share's first request: number, steps, steps before, -, Req
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  // the joining kernel may be brought in beside this one; it waits for this grid's end
-  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   if (tid < kDecWarps * kStages) bar_init(&bars[tid], 1);
+  if (tid == 64) {
+    asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&kmap)));
+    asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&vmap)));
+  }
   asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
 
   // ---- this CTA's share ----
   long long sum = 0;
-  int mine = 0;
+  int mine = 0;   // steps of this thread's request (of the last one, where there are more requests than threads)
+  Req mq;
   for (int r = tid; r < a.n_req; r += kDecThreads) {
-    Req q;
-    mine = load_req(a, r, &q);
+    mine = load_req(a, r, &mq);
     sum += mine;
   }
+  long long incl = sum;
 #pragma unroll
-  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (lane == 0) s_sum[warp] = sum;
-  if (tid == 0) s_req = -1;
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 31) s_sum[warp] = incl;
   __syncthreads();
-  long long total = 0;
+  long long total = 0, off = incl - sum;   // off: steps of the requests before this thread's (if it has one)
 #pragma unroll
-  for (int w = 0; w < kDecWarps; ++w) total += s_sum[w];
+  for (int w = 0; w < kDecWarps; ++w) {
+    if (w < warp) off += s_sum[w];
+    total += s_sum[w];
+  }
   total *= a.h_kv;
-  const long long g = min((long long)gridDim.x, total);   // CTAs with work
-  const long long c = blockIdx.x;
-  if (c >= g) {
-    if (tid == 0) descs[c].on = 0;
-    return;
-  }
-  const long long begin = c * total / g, end = (c + 1) * total / g;
-  long long before = 0;
-  for (int c0 = 0; c0 < a.n_req; c0 += kDecThreads) {
-    if (a.n_req > kDecThreads) {
-      Req q;
-      mine = c0 + tid < a.n_req ? load_req(a, c0 + tid, &q) : 0;
-    } else if (tid >= a.n_req) mine = 0;
-    int incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += u;
-    }
-    __syncthreads();
-    if (lane == 31) s_sum[warp] = incl;
-    __syncthreads();
-    long long off = before + incl - mine;
-#pragma unroll
-    for (int w = 0; w < kDecWarps; ++w) {
-      if (w < warp) off += s_sum[w];
-      before += s_sum[w];
-    }
+  const int g = (int)min((long long)gridDim.x, total);   // CTAs with work
+  const int c = blockIdx.x;
+  if (c >= g) return;
+  const long long begin = muldiv(c, total, g), end = muldiv(c + 1, total, g);
+  auto found = [&](int r) {
     if (mine > 0 && begin >= off * a.h_kv && begin < (off + mine) * a.h_kv) {
-      s_req = c0 + tid;
-      s_off = begin - off * a.h_kv;
+      s_first[0] = r;
+      s_first[1] = mine;
+      *reinterpret_cast<long long*>(s_first + 2) = begin - off * a.h_kv;
+      *reinterpret_cast<Req*>(s_first + 4) = mq;
     }
-    __syncthreads();
-    if (s_req >= 0) break;
+  };
+  if (a.n_req <= kDecThreads) {
+    found(tid);
+  } else {
+    long long before = 0;
+    for (int c0 = 0; c0 < a.n_req; c0 += kDecThreads) {
+      mine = c0 + tid < a.n_req ? load_req(a, c0 + tid, &mq) : 0;
+      incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += u;
+      }
+      __syncthreads();
+      if (lane == 31) s_sum[warp] = incl;
+      __syncthreads();
+      off = before + incl - mine;
+#pragma unroll
+      for (int w = 0; w < kDecWarps; ++w) {
+        if (w < warp) off += s_sum[w];
+        before += s_sum[w];
+      }
+      found(c0 + tid);
+      if (begin < before * a.h_kv) break;   // the same for all threads
+    }
   }
+  __syncthreads();
   Seg seg;
-  seg.r = s_req;
-  seg.steps = load_req(a, seg.r, &seg.q);
-  const long long in_req = s_off;
-  seg.kv = (int)(in_req / seg.steps);
-  seg.a = (int)(in_req % seg.steps);
+  seg.r = s_first[0];
+  seg.steps = s_first[1];
+  seg.q = *reinterpret_cast<const Req*>(s_first + 4);
+  const long long in_req = *reinterpret_cast<const long long*>(s_first + 2);
+  if (in_req < (1LL << 31)) {
+    seg.kv = (int)((uint32_t)in_req / (uint32_t)seg.steps);
+    seg.a = (int)((uint32_t)in_req - (uint32_t)seg.kv * (uint32_t)seg.steps);
+  } else {
+    seg.kv = (int)(in_req / seg.steps);
+    seg.a = (int)(in_req - (long long)seg.kv * seg.steps);
+  }
   seg.b = (int)min((long long)seg.steps, seg.a + (end - begin));
   seg.left = (end - begin) - (seg.b - seg.a);
-  if (tid == 0) {
-    JoinDesc d;
-    const long long u0 = begin - seg.a;
-    d.first_cta = (int)(((u0 + 1) * g - 1) / total);
-    d.last_cta = (int)(((u0 + seg.steps) * g - 1) / total);
-    d.on = seg.a > 0 && c == d.first_cta + 1;
-    // the first CTA's piece is its last segment: slot 1, unless its share begins with the unit
-    d.first_slot = (long long)d.first_cta * total / g < u0 ? 1 : 0;
-    d.kv = seg.kv;
-    d.row0 = seg.q.row0;
-    d.rows = seg.q.n * a.G;
-    d.pad = 0;
-    descs[c] = d;
-  }
+  long long unit0 = begin - seg.a;   // the unit's first step among all
 
   // ---- copies: lane 0 of every warp, running ahead of the warp's own blocks ----
   Seg ps = seg;
@@ -420,31 +430,34 @@ __global__ void __launch_bounds__(kDecThreads, 1)
         }
       }
     }
+    if (!whole) {
+      // pieces: the end of the first CTA's share (or all of it), then the starts of the others'
+      const int c0 = share_of(unit0, total, g), c1 = share_of(unit0 + seg.steps - 1, total, g);
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) s_first[0] = atomicAdd(&arrived[c0], 1u) == (unsigned)(c1 - c0);
+      __syncthreads();
+      if (s_first[0]) {
+        __threadfence();
+        const int slot0 = 2 * c0 + (muldiv(c0, total, g) < unit0 ? 1 : 0);
+        for (int row = warp; row < rows; row += kDecWarps) {
+          const int tok = row / a.G;
+          const long long at = (long long)(seg.q.row0 + tok) * a.h_q + seg.kv * a.G + (row - tok * a.G);
+          join_row<T>(a.out, a.lse, at, lane, c1 - c0 + 1, [&](int i) {
+            return parts + ((long long)(i == 0 ? slot0 : 2 * (c0 + i)) * ZC_PAGED_ROWS + row) * kJoinStride;
+          });
+        }
+        if (tid == 0) arrived[c0] = 0;   // as the next call wants it
+      }
+    }
     first_seg = false;
+    unit0 += seg.steps;
     if (!seg_next(a, seg)) break;
   }
 }
 
-// Block c - 1: the unit that the border before CTA c cuts first.  A warp takes a row.
-template <typename T>
-__global__ void __launch_bounds__(256) k_paged_join(const ZcPagedArgs a, const float* __restrict__ parts,
-                                                    const JoinDesc* __restrict__ descs) {
-  asm volatile("griddepcontrol.wait;\n" ::: "memory");
-  const JoinDesc d = descs[blockIdx.x + 1];
-  if (!d.on) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int row = warp; row < d.rows; row += 8) {
-    const int tok = row / a.G;
-    const long long at = (long long)(d.row0 + tok) * a.h_q + d.kv * a.G + (row - tok * a.G);
-    join_row<T>(a.out, a.lse, at, lane, d.last_cta - d.first_cta + 1, [&](int i) {
-      const long long slot = 2LL * (d.first_cta + i) + (i == 0 ? d.first_slot : 0);
-      return parts + (slot * ZC_PAGED_ROWS + row) * kJoinStride;
-    });
-  }
-}
-
 template <typename T, int NT>
-int launch(zc_pages* p, const ZcPagedArgs& a, float* parts, JoinDesc* descs, cudaStream_t st) {
+int launch(zc_pages* p, const ZcPagedArgs& a, float* parts, unsigned* arrived, cudaStream_t st) {
   static bool once[64] = {};   // per device: the attribute belongs to the device's copy of the kernel
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -454,32 +467,27 @@ int launch(zc_pages* p, const ZcPagedArgs& a, float* parts, JoinDesc* descs, cud
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) once[dev] = true;
   }
-  k_paged_decode<T, NT><<<p->n_sm, kDecThreads, kDecSmem, st>>>(a, parts, descs, p->k16, p->v16);
+  k_paged_decode<T, NT><<<p->n_sm, kDecThreads, kDecSmem, st>>>(a, parts, arrived, p->k16, p->v16);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   p->launches += 1;
-  if (p->n_sm > 1) {
-    e = zc_launch_early(k_paged_join<T>, dim3(p->n_sm - 1), dim3(256), 0, st, a, (const float*)parts, (const JoinDesc*)descs);
-    if (e != cudaSuccess) return e;
-    p->launches += 1;
-  }
   return cudaSuccess;
 }
 
 }  // namespace
 
 size_t zc_paged_decode_workspace() {
-  return (size_t)ZC_PAGED_MAX_CTAS * (2 * ZC_PAGED_ROWS * kJoinStride * 4 + sizeof(JoinDesc));
+  return ZC_PAGES_SYNC_BYTES + (size_t)ZC_PAGED_MAX_CTAS * 2 * ZC_PAGED_ROWS * kJoinStride * 4;
 }
 
 int zc_launch_paged_decode(zc_pages* p, const ZcPagedArgs& a, char* ws, cudaStream_t st) {
   if (!zc_page_maps(p)) return (int)cudaErrorNotSupported;
-  JoinDesc* descs = (JoinDesc*)ws;
-  float* parts = (float*)(ws + (size_t)ZC_PAGED_MAX_CTAS * sizeof(JoinDesc));
+  unsigned* arrived = (unsigned*)ws;
+  float* parts = (float*)(ws + ZC_PAGES_SYNC_BYTES);
   const bool one = a.max_rows * a.G <= 8;
   if (p->cfg.dtype == ZC_F16)
-    return one ? launch<__half, 1>(p, a, parts, descs, st) : launch<__half, 2>(p, a, parts, descs, st);
-  return one ? launch<__nv_bfloat16, 1>(p, a, parts, descs, st) : launch<__nv_bfloat16, 2>(p, a, parts, descs, st);
+    return one ? launch<__half, 1>(p, a, parts, arrived, st) : launch<__half, 2>(p, a, parts, arrived, st);
+  return one ? launch<__nv_bfloat16, 1>(p, a, parts, arrived, st) : launch<__nv_bfloat16, 2>(p, a, parts, arrived, st);
 }
 
 // Tensor maps of the pages: (64 channels, token of the page, half of the channels, KV head, page).
