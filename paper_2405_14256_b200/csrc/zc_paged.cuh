@@ -38,29 +38,6 @@ __device__ __forceinline__ void store_row(void* out, float* lse, long long at, i
   if (lse && lane == 0) lse[at] = sum > 0.f ? m + log2f(sum) : -INFINITY;
 }
 
-// One row from its n pieces (each: maximum, sum, -, -, 128 accumulated channels), in their order.
-template <typename T, typename At>
-__device__ __forceinline__ void join_row(void* out, float* lse, long long at, int lane, int n, At piece) {
-  float m = -1e30f;
-  for (int i = lane; i < n; i += 32) m = fmaxf(m, piece(i)[0]);
-#pragma unroll
-  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  float sum = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const float* p = piece(i);
-    const float f = zc_exp2(p[0] - m);
-    const float4 x = *reinterpret_cast<const float4*>(p + 4 + 4 * lane);
-    sum = fmaf(p[1], f, sum);
-    acc.x = fmaf(x.x, f, acc.x);
-    acc.y = fmaf(x.y, f, acc.y);
-    acc.z = fmaf(x.z, f, acc.z);
-    acc.w = fmaf(x.w, f, acc.w);
-  }
-  store_row<T>(out, lse, at, lane, m, sum, acc);
-}
-
 // Tensor map in the 128-byte swizzle; strides in bytes.  False when the driver's entry point is missing
 // or refuses the tensor.
 inline bool zc_encode_map(CUtensorMap* map, int dtype, int rank, const void* at, const cuuint64_t* dims,

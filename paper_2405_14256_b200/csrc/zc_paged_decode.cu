@@ -3,7 +3,7 @@
 //
 // The visible keys of every (request, KV head) are cut into steps of 128 (eight blocks of 16); all
 // steps of the call, laid end to end, are dealt out to the CTAs in equal, consecutive shares, so that
-// ragged lengths do not matter.  A CTA is eight warps; warp w takes block w of each step through a ring
+// ragged lengths do not matter (units of a few steps stay whole).  A CTA is eight warps; warp w takes block w of each step through a ring
 // of its own (bulk tensor copies of 16 keys and 16 values, 8 KB a stage), so that no warp waits for
 // another inside a share.  Per block, with the query rows as the N dimension of the tensor-core tiles:
 //   S^T (16 keys x 8 rows) = K Q^T        A = keys from shared memory, B = rows kept in registers
@@ -26,12 +26,17 @@ namespace {
 constexpr int kDecWarps = 8, kDecThreads = 32 * kDecWarps;
 constexpr int kBlkLog2 = 4, kBlk = 1 << kBlkLog2;      // keys of a block
 constexpr int kHalf = kBlk * ZC_D * 2;                 // 4 KB: keys (or values) of a stage, [2][16][128 B]
-constexpr int kStages = 3;
-constexpr int kRing = kDecWarps * kStages * 2 * kHalf; // 192 KB
+constexpr int kStages = 2;                              // 3 measured 229 against 216 us (32 x 2048-4096 tokens, 32 KV heads)
+constexpr int kRing = kDecWarps * kStages * 2 * kHalf;  // 128 KB
 constexpr int kJoinStride = ZC_PART_STRIDE;            // m, sum, -, -, acc[128]
 constexpr int kJoinBytes = kDecWarps * 8 * kJoinStride * 4;
-constexpr int kScanBytes = kDecWarps * 8 + 80;        // warps' sums; where the share begins
+constexpr int kScanBytes = kDecWarps * 8 + 2 * 80;    // warps' sums; the units of the share's two borders
 constexpr int kDecSmem = kRing + kJoinBytes + kDecWarps * kStages * 8 + kScanBytes + 1024;   // 1 KB: alignment
+// A cut costs a partial result, its announcement and a join, and a share that straddles two units pays most of it
+// twice.  So units of up to 5 steps are never cut (32 requests of 300-500 tokens, 8 KV heads: 13.7 us, cut 16.5),
+// and no piece is shorter than half a share or 3 steps (one request of 8000 tokens: 14.7 us, else 19.2).
+constexpr int kWhole = 5;
+constexpr int kLeast = 3;
 constexpr float kNoMax = -1e30f;                       // running maximum before any key
 static_assert(ZC_PAGED_MAX_CTAS * 4 <= ZC_PAGES_SYNC_BYTES, "a counter per CTA");
 constexpr float kTau = 8.f;
@@ -52,15 +57,22 @@ __device__ __forceinline__ int load_req(const ZcPagedArgs& a, int r, Req* q) {
   return q->n > 0 ? max(1, (q->s.nb + kDecWarps - 1) / kDecWarps) : 0;
 }
 
-static_assert(sizeof(Req) + 16 <= 80, "the share's first request fits its place");
-
 // a * b / c; the quotient of 32-bit numbers where they fit (a <= 160).
 __device__ __forceinline__ long long muldiv(int a, long long b, int c) {
   return b < (1 << 24) ? (long long)((uint32_t)a * (uint32_t)b / (uint32_t)c) : a * b / c;
 }
-// The CTA whose share holds step s of `total` in g shares.
-__device__ __forceinline__ int share_of(long long s, long long total, int g) {
-  return total < (1 << 24) ? (int)((((uint32_t)s + 1u) * (uint32_t)g - 1u) / (uint32_t)total) : (int)(((s + 1) * g - 1) / total);
+
+// A border between two shares: the unit (request, KV head) that it lies in, and the step it falls on, moved to the
+// unit's start or end where the unit is too short to be cut.
+struct Place {
+  int r, steps, kv, step;
+  long long unit0;   // the unit's first step among all
+  Req q;
+};
+static_assert(sizeof(Place) <= 80, "two borders fit their place");
+__device__ __forceinline__ int cut_step(long long off, int steps, int least) {
+  if (steps <= kWhole) return 2 * off < steps ? 0 : steps;
+  return off < least ? 0 : steps - off < least ? steps : (int)off;
 }
 
 // One unit's steps a .. b - 1 inside a CTA's share.
@@ -114,7 +126,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
   float* s_join = reinterpret_cast<float*>(base + kRing);
   uint64_t* bars = reinterpret_cast<uint64_t*>(base + kRing + kJoinBytes);
   long long* s_sum = reinterpret_cast<long long*>(bars + kDecWarps * kStages);
-  int* s_first = reinterpret_cast<int*>(s_sum + kDecWarps);   // the share's first request: number, steps, steps before, -, Req
+  Place* s_place = reinterpret_cast<Place*>(s_sum + kDecWarps);   // [2] where the share begins, where it ends
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid < kDecWarps * kStages) bar_init(&bars[tid], 1);
   if (tid == 64) {
@@ -146,18 +158,32 @@ __global__ void __launch_bounds__(kDecThreads, 1)
     total += s_sum[w];
   }
   total *= a.h_kv;
-  const int g = (int)min((long long)gridDim.x, total);   // CTAs with work
+  const int g = (int)min((long long)gridDim.x, total);   // shares; no two borders on the same step
   const int c = blockIdx.x;
   if (c >= g) return;
-  const long long begin = muldiv(c, total, g), end = muldiv(c + 1, total, g);
-  auto found = [&](int r) {
-    if (mine > 0 && begin >= off * a.h_kv && begin < (off + mine) * a.h_kv) {
-      s_first[0] = r;
-      s_first[1] = mine;
-      *reinterpret_cast<long long*>(s_first + 2) = begin - off * a.h_kv;
-      *reinterpret_cast<Req*>(s_first + 4) = mq;
+  const int least = total >= (long long)g * 2 * kLeast ? kLeast : max(1, (int)((total + g) / (2 * g)));
+  const long long border[2] = {muldiv(c, total, g), muldiv(c + 1, total, g)};
+  auto found = [&](int r) {   // this thread's request, if a border lies in it
+    if (mine <= 0) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const long long in = border[i] - off * a.h_kv;
+      if (in < 0 || in >= (long long)mine * a.h_kv) continue;
+      Place p;
+      p.r = r;
+      p.steps = mine;
+      p.kv = in < (1LL << 31) ? (int)((uint32_t)in / (uint32_t)mine) : (int)(in / mine);
+      const long long in_unit = in - (long long)p.kv * mine;
+      p.unit0 = border[i] - in_unit;
+      p.step = cut_step(in_unit, mine, least);
+      p.q = mq;
+      s_place[i] = p;
     }
   };
+  if (tid == 0 && c + 1 == g) {   // the last share ends behind the last unit
+    s_place[1].unit0 = total;
+    s_place[1].step = 0;
+  }
   if (a.n_req <= kDecThreads) {
     found(tid);
   } else {
@@ -180,25 +206,27 @@ __global__ void __launch_bounds__(kDecThreads, 1)
         before += s_sum[w];
       }
       found(c0 + tid);
-      if (begin < before * a.h_kv) break;   // the same for all threads
+      if (border[1] < before * a.h_kv) break;   // the same for all threads
     }
   }
   __syncthreads();
+  long long unit0 = s_place[0].unit0;   // of the segment's unit: its first step among all
   Seg seg;
-  seg.r = s_first[0];
-  seg.steps = s_first[1];
-  seg.q = *reinterpret_cast<const Req*>(s_first + 4);
-  const long long in_req = *reinterpret_cast<const long long*>(s_first + 2);
-  if (in_req < (1LL << 31)) {
-    seg.kv = (int)((uint32_t)in_req / (uint32_t)seg.steps);
-    seg.a = (int)((uint32_t)in_req - (uint32_t)seg.kv * (uint32_t)seg.steps);
+  seg.r = s_place[0].r;
+  seg.kv = s_place[0].kv;
+  seg.steps = s_place[0].steps;
+  seg.q = s_place[0].q;
+  seg.a = s_place[0].step;
+  const long long begin = unit0 + seg.a, end = s_place[1].unit0 + s_place[1].step;
+  if (begin >= end) return;
+  if (seg.a == seg.steps) {   // the border was moved to the unit's end: the share begins with the next unit
+    unit0 += seg.steps;
+    seg.left = end - begin;
+    seg_next(a, seg);
   } else {
-    seg.kv = (int)(in_req / seg.steps);
-    seg.a = (int)(in_req - (long long)seg.kv * seg.steps);
+    seg.b = (int)min((long long)seg.steps, seg.a + (end - begin));
+    seg.left = (end - begin) - (seg.b - seg.a);
   }
-  seg.b = (int)min((long long)seg.steps, seg.a + (end - begin));
-  seg.left = (end - begin) - (seg.b - seg.a);
-  long long unit0 = begin - seg.a;   // the unit's first step among all
 
   // ---- copies: lane 0 of every warp, running ahead of the warp's own blocks ----
   Seg ps = seg;
@@ -242,11 +270,29 @@ __global__ void __launch_bounds__(kDecThreads, 1)
 #pragma unroll
   for (int i = 0; i < kStages; ++i) issue(i);
 
+  // The eight warps' results of the row that this warp takes, joined in their order.
+  auto meet = [&](float& m, float& sum, float4& acc) {
+    m = kNoMax;
+#pragma unroll
+    for (int w = 0; w < kDecWarps; ++w) m = fmaxf(m, s_join[(w * 8 + warp) * kJoinStride]);
+    sum = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kDecWarps; ++w) {
+      const float* jr = s_join + (w * 8 + warp) * kJoinStride;
+      const float f = zc_exp2(jr[0] - m);
+      const float4 x = *reinterpret_cast<const float4*>(jr + 4 + 4 * lane);
+      sum = fmaf(jr[1], f, sum);
+      acc.x = fmaf(x.x, f, acc.x);
+      acc.y = fmaf(x.y, f, acc.y);
+      acc.z = fmaf(x.z, f, acc.z);
+      acc.w = fmaf(x.w, f, acc.w);
+    }
+  };
   const float scale = kLog2e * rsqrtf((float)ZC_D);
   const int quad = lane & 3, oct = lane >> 2;
   int stage = 0;
   uint32_t phase = 0;
-  bool first_seg = true;
   for (;;) {
     const int rows = seg.q.n * a.G;
     // this unit's query rows as B fragments: row = oct + 8 nt, two consecutive channels a register
@@ -376,7 +422,8 @@ __global__ void __launch_bounds__(kDecThreads, 1)
     }
     // ---- the eight warps' results of this unit ----
     const bool whole = seg.a == 0 && seg.b == seg.steps;
-    float* slot = parts + (2 * c + (first_seg ? 0 : 1)) * (long long)ZC_PAGED_ROWS * kJoinStride;
+    // (a CTA has one piece at most that does not begin with its unit, and one that does and does not end with it)
+    float* slot = parts + (2 * c + (seg.a > 0 ? 0 : 1)) * (long long)ZC_PAGED_ROWS * kJoinStride;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       if (8 * nt >= rows) break;
@@ -400,22 +447,9 @@ __global__ void __launch_bounds__(kDecThreads, 1)
       __syncthreads();
       const int row = 8 * nt + warp;
       if (row < rows) {
-        float mt = kNoMax;
-#pragma unroll
-        for (int w = 0; w < kDecWarps; ++w) mt = fmaxf(mt, s_join[(w * 8 + warp) * kJoinStride]);
-        float total_s = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < kDecWarps; ++w) {
-          const float* jr = s_join + (w * 8 + warp) * kJoinStride;
-          const float f = zc_exp2(jr[0] - mt);
-          const float4 x = *reinterpret_cast<const float4*>(jr + 4 + 4 * lane);
-          total_s = fmaf(jr[1], f, total_s);
-          acc.x = fmaf(x.x, f, acc.x);
-          acc.y = fmaf(x.y, f, acc.y);
-          acc.z = fmaf(x.z, f, acc.z);
-          acc.w = fmaf(x.w, f, acc.w);
-        }
+        float mt, total_s;
+        float4 acc;
+        meet(mt, total_s, acc);
         if (whole) {
           const int tok = row / a.G;
           const long long at = (long long)(seg.q.row0 + tok) * a.h_q + seg.kv * a.G + (row - tok * a.G);
@@ -431,26 +465,84 @@ __global__ void __launch_bounds__(kDecThreads, 1)
       }
     }
     if (!whole) {
-      // pieces: the end of the first CTA's share (or all of it), then the starts of the others'
-      const int c0 = share_of(unit0, total, g), c1 = share_of(unit0 + seg.steps - 1, total, g);
+      // The CTAs whose shares begin inside the unit; the one before the first of them has its first steps.
       __threadfence();
       __syncthreads();
-      if (tid == 0) s_first[0] = atomicAdd(&arrived[c0], 1u) == (unsigned)(c1 - c0);
+      if (tid == 0) {
+        auto cuts = [&](int d) {
+          if (d < 1 || d >= g) return false;
+          const long long in = muldiv(d, total, g) - unit0;
+          if (in <= 0 || in >= seg.steps) return false;
+          const int t = cut_step(in, seg.steps, least);
+          return t > 0 && t < seg.steps;
+        };
+        int c0 = c, c1 = c;
+        if (seg.a > 0)
+          while (cuts(c0 - 1)) --c0;
+        while (cuts(c1 + 1)) ++c1;
+        if (seg.a > 0) --c0;
+        s_place[0].r = c0;
+        s_place[0].kv = c1;
+        s_place[0].step = atomicAdd(&arrived[c0], 1u) == (unsigned)(c1 - c0);
+      }
       __syncthreads();
-      if (s_first[0]) {
+      if (s_place[0].step) {
         __threadfence();
-        const int slot0 = 2 * c0 + (muldiv(c0, total, g) < unit0 ? 1 : 0);
-        for (int row = warp; row < rows; row += kDecWarps) {
-          const int tok = row / a.G;
-          const long long at = (long long)(seg.q.row0 + tok) * a.h_q + seg.kv * a.G + (row - tok * a.G);
-          join_row<T>(a.out, a.lse, at, lane, c1 - c0 + 1, [&](int i) {
-            return parts + ((long long)(i == 0 ? slot0 : 2 * (c0 + i)) * ZC_PAGED_ROWS + row) * kJoinStride;
-          });
+        const int c0 = s_place[0].r, n = s_place[0].kv - c0 + 1;
+#pragma unroll 1
+        for (int r0 = 0; r0 < rows; r0 += 8) {
+          // warp w takes pieces w, w + 8, ... of eight rows; then the warps' results meet as a unit's do
+          __syncthreads();
+          for (int r = 0; r < 8 && r0 + r < rows; r += 4) {
+            float2 ms[4];
+            float4 acc[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              ms[u] = make_float2(kNoMax, 0.f);
+              acc[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            for (int i = warp; i < n; i += kDecWarps) {
+              const float* pr = parts + ((long long)(2 * (c0 + i) + (i == 0 ? 1 : 0)) * ZC_PAGED_ROWS + r0 + r) * kJoinStride;
+              float2 pm[4];
+              float4 x[4];
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+                if (r0 + r + u < rows) {
+                  pm[u] = __ldcg(reinterpret_cast<const float2*>(pr + u * kJoinStride));
+                  x[u] = __ldcg(reinterpret_cast<const float4*>(pr + u * kJoinStride + 4 + 4 * lane));
+                }
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+                if (r0 + r + u < rows) {
+                  const float top = fmaxf(ms[u].x, pm[u].x), fo = zc_exp2(ms[u].x - top), fn = zc_exp2(pm[u].x - top);
+                  ms[u] = make_float2(top, fmaf(ms[u].y, fo, pm[u].y * fn));
+                  acc[u] = make_float4(fmaf(acc[u].x, fo, x[u].x * fn), fmaf(acc[u].y, fo, x[u].y * fn),
+                                       fmaf(acc[u].z, fo, x[u].z * fn), fmaf(acc[u].w, fo, x[u].w * fn));
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              float* jr = s_join + (warp * 8 + r + u) * kJoinStride;
+              if (lane == 0) {
+                jr[0] = ms[u].x;
+                jr[1] = ms[u].y;
+              }
+              *reinterpret_cast<float4*>(jr + 4 + 4 * lane) = acc[u];
+            }
+          }
+          __syncthreads();
+          const int row = r0 + warp;
+          if (row < rows) {
+            float m8, sum8;
+            float4 acc8;
+            meet(m8, sum8, acc8);
+            const int tok = row / a.G;
+            store_row<T>(a.out, a.lse, (long long)(seg.q.row0 + tok) * a.h_q + seg.kv * a.G + (row - tok * a.G), lane, m8, sum8, acc8);
+          }
         }
         if (tid == 0) arrived[c0] = 0;   // as the next call wants it
       }
     }
-    first_seg = false;
     unit0 += seg.steps;
     if (!seg_next(a, seg)) break;
   }
