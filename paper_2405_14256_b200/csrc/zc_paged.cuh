@@ -18,6 +18,12 @@ template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, fl
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// a * b / c; the quotient of 32-bit numbers where they fit (a <= ZC_PAGED_MAX_CTAS).
+static_assert(ZC_PAGED_MAX_CTAS < 256, "a * b < 2^32");
+__device__ __forceinline__ long long zc_muldiv(int a, long long b, int c) {
+  return b < (1 << 24) ? (long long)((uint32_t)a * (uint32_t)b / (uint32_t)c) : a * b / c;
+}
+
 // One box of a page: rows `row` ... of it, half `half` of the channels on.
 __device__ __forceinline__ void page_copy(const CUtensorMap* map, uint32_t dst, uint64_t* bar, int row, int half,
                                           int head, int page) {

@@ -42,7 +42,7 @@ constexpr int kOutTile = 32 * 64;                     // a warp's 32 rows x 32 c
 constexpr int kTiles = 2 * kTile + (kKS + kVS) * kKvTile + 8 * kOutTile;   // 224 KB
 constexpr int kRingN = 2;                             // items fetched ahead
 constexpr int kRingInts = 24;
-constexpr int kSmem = kTiles + 1024 + 384 + 1024 + kRingN * kRingInts * 4;   // alignment, barriers, (m, sum) of group 1
+constexpr int kSmem = kTiles + 1024 + 448 + 1024 + kRingN * kRingInts * 4;   // alignment, barriers, (m, sum) of group 1
 constexpr float kNoMax = -1e30f;                      // running maximum before any key
 constexpr float kTau = 3.f;                           // a new maximum is taken where it exceeds the old by this (base 2)
 constexpr float kBigSum = 1024.f;                     // ... and looked for where a tile's weights sum to more than this
@@ -52,8 +52,8 @@ constexpr int kItemRows = 2 * kM;
 constexpr int kPartBytes = kItemRows * ZC_D * 4 + kItemRows * 8;
 constexpr int kMaxItems = 13000;                      // items of a head, and requests, that a call may have: what the
                                                       // prologue keeps in the tiles' shared memory (16 bytes each)
-constexpr int kItemCost = 6;                          // of an item beside its tiles: Q, first product, output (half tiles)
-constexpr int kMinPiece = 8;                          // tiles; below, joining costs more than the even share gains
+constexpr int kItemCost = 9;                          // of an item beside its tiles: Q, first product, output (half tiles)
+constexpr int kMinPiece = 4;                          // tiles; below, joining costs more than the even share gains
 
 // Where a CTA's share begins: item `item` of all heads' (head * items + item of the head), key tile t of it.
 struct Border { int item, t; };
@@ -95,13 +95,13 @@ __device__ __forceinline__ int item_tiles(const ZcPagedArgs& a, const Chunk& c, 
   return zc_seen(c.p0 + tok0, c.p0 + last, a.window, a.sinks, kTileLog2).nb;
 }
 
-// Exclusive sum over the kThreads threads, and the total.
-__device__ __forceinline__ long long block_scan(long long v, long long* s_warp, long long* total) {
+// Exclusive sum over the kThreads threads, and the total (a warp's values sum to less than 2^31).
+__device__ __forceinline__ long long block_scan(int v, long long* s_warp, long long* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long incl = v;
+  int incl = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+    const int u = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += u;
   }
   __syncthreads();
@@ -119,7 +119,7 @@ __device__ __forceinline__ long long block_scan(long long v, long long* s_warp, 
 }
 
 // Cost of an item in half tiles: both groups work on every tile of a wide item, on every second of a narrow one.
-__device__ __forceinline__ int item_width(int ntok, int tpt) { return ntok <= tpt ? 1 : 2; }
+__device__ __forceinline__ int item_width(int ntok, int tpt) { return ntok <= tpt ? 2 : 3; }
 __device__ __forceinline__ int item_cost(int nt, int width) { return nt * width + kItemCost; }
 // The tile at which a border at `off` into an item's cost cuts it: 0 or nt where a piece would be short.
 __device__ __forceinline__ int cut_tile(long long off, int nt, int width) {
@@ -133,7 +133,14 @@ struct Share {
   int items;          // of a head
   int r, in_req;      // the begin's request, and the item's number in it
 };
-__device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, long long* s_warp, Border* s_border,
+// What is found for all threads: the borders, and the item that the first of them lies in.
+struct Found {
+  Border border[2];
+  long long start, all;   // the item's cost before it, and the cost of everything
+  int nt, width, r, in_req, kv;
+};
+static_assert(sizeof(Found) <= 64, "it fits between the barriers and the sums");
+__device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, long long* s_warp, Found* s_found,
                                             int n_cta) {
   const ZcPagedArgs& a = k.a;
   const int tid = threadIdx.x, tpi = 2 * k.tpt;
@@ -196,56 +203,80 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
   const int c = blockIdx.x;
   const long long all = head * a.h_kv;
   if (tid < 2) {
-    const long long at = all * (c + tid) / n_cta;
+    const long long at = zc_muldiv(c + tid, all, n_cta);
     Border b;
-    ChunkJoin j;
-    j.on = 0;
-    if (at >= all) {
-      b.item = items * a.h_kv;
-      b.t = 0;
-    } else {
-      const int kv = (int)(at / head);
+    b.item = items * a.h_kv;
+    b.t = 0;
+    Found f;
+    f.start = f.all = all;
+    f.nt = f.width = f.r = f.in_req = f.kv = 0;
+    if (at < all) {
+      const int kv = all < (1 << 24) ? (int)((uint32_t)at / (uint32_t)head) : (int)(at / head);
       const long long in = at - kv * head;
       int lo = 0, hi = items;
       while (hi - lo > 1) {
         const int m = (lo + hi) >> 1;
         if (s_cost[m] <= in) lo = m; else hi = m;
       }
-      int width;
-      const int r = request(lo), nt = tiles(lo, r, &width), t = cut_tile(in - s_cost[lo], nt, width);
-      b.item = kv * items + lo + (t > 0 && t == nt ? 1 : 0);
-      b.t = t == nt ? 0 : t;
-      if (tid == 0 && b.t > 0) {
-        // the CTAs around this one whose borders cut the same item
-        const long long start = kv * head + s_cost[lo];
-        auto cuts = [&](int d) {
-          const int u = cut_tile(all * d / n_cta - start, nt, width);
-          return u > 0 && u < nt;
-        };
-        j.first = j.last = c;
-        while (j.first > 1 && cuts(j.first - 1)) --j.first;
-        if (j.first == c) {
-          while (j.last + 1 < n_cta && cuts(j.last + 1)) ++j.last;
-          j.on = 1;
-          j.r = r;
-          j.tok0 = (lo - s_start[r]) * tpi;
-          j.kv = kv;
-        }
+      const int r = request(lo), nt = tiles(lo, r, &f.width), t = cut_tile(in - s_cost[lo], nt, f.width);
+      b.item = kv * items + lo;
+      b.t = t;
+      f.start = kv * head + s_cost[lo];
+      f.nt = nt;
+      f.r = r;
+      f.in_req = lo - s_start[r];
+      f.kv = kv;
+      if (t > 0 && t == nt) {   // the next item
+        b.item += 1;
+        b.t = 0;
+        const int next = lo + 1 < items ? lo + 1 : 0;
+        f.r = request(next);
+        f.in_req = next - s_start[f.r];
       }
     }
-    if (tid == 0) k.ws.joins[c] = j;
-    s_border[tid] = b;
+    s_found->border[tid] = b;
+    if (tid == 0) {
+      s_found->start = f.start;
+      s_found->all = f.all;
+      s_found->nt = f.nt;
+      s_found->width = f.width;
+      s_found->r = f.r;
+      s_found->in_req = f.in_req;
+      s_found->kv = f.kv;
+    }
   }
+  async_proxy_fence();   // the scratch's place is the tiles' from here on, whose copies come by the other proxy
   __syncthreads();
   Share s;
-  s.begin = s_border[0];
-  s.end = s_border[1];
+  s.begin = s_found->border[0];
+  s.end = s_found->border[1];
   s.items = items;
-  const int i = items > 0 ? s.begin.item % items : 0;
-  s.r = items > 0 ? request(i) : 0;
-  s.in_req = i - s_start[s.r];
-  if (tid == 0) k.ws.used[c] = s.begin.item < s.end.item || s.begin.t < s.end.t;
-  __syncthreads();   // the scratch is free for the tiles
+  s.r = s_found->r;
+  s.in_req = s_found->in_req;
+  if (tid == kThreads - 1) {
+    // (a thread that has nothing to do yet) what k_chunk_join is to know of the border before this CTA
+    const Found f = *s_found;
+    ChunkJoin j;
+    j.on = 0;
+    if (s.begin.t > 0) {
+      // the CTAs around this one whose borders cut the same item
+      auto cuts = [&](int d) {
+        const int u = cut_tile(zc_muldiv(d, f.all, n_cta) - f.start, f.nt, f.width);
+        return u > 0 && u < f.nt;
+      };
+      j.first = j.last = c;
+      while (j.first > 1 && cuts(j.first - 1)) --j.first;
+      if (j.first == c) {
+        while (j.last + 1 < n_cta && cuts(j.last + 1)) ++j.last;
+        j.on = 1;
+        j.r = f.r;
+        j.tok0 = f.in_req * tpi;
+        j.kv = f.kv;
+      }
+    }
+    k.ws.joins[c] = j;
+    k.ws.used[c] = s.begin.item < s.end.item || s.begin.t < s.end.t;
+  }
   return s;
 }
 
@@ -453,8 +484,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* i_free = i_full + kRingN;       // [kRingN] all roles have read it
   uint64_t* m_free = i_free + kRingN;       // [2] the groups' meeting over a narrow item is over (in turn)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(m_free + 2);
-  float2* s_ms = reinterpret_cast<float2*>(base + kTiles + 384);                    // [128] narrow items: group 1's (m, sum)
-  int* ring = reinterpret_cast<int*>(base + kTiles + 384 + 1024);
+  float2* s_ms = reinterpret_cast<float2*>(base + kTiles + 448);                    // [128] narrow items: group 1's (m, sum)
+  int* ring = reinterpret_cast<int*>(base + kTiles + 448 + 1024);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   if (tid == 0) {
@@ -496,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);
   Share share;
-  if (PAGED) share = find_share(k, base, reinterpret_cast<long long*>(s_ms), reinterpret_cast<Border*>(ring), gridDim.x);
+  if (PAGED) share = find_share(k, base, reinterpret_cast<long long*>(s_ms), reinterpret_cast<Found*>(base + kTiles + 384), gridDim.x);
 
   uint32_t n_item = 0;   // items taken from the ring
   // Next item of the ring; a whole warp calls.  False: there are no more (or a wait ran out).

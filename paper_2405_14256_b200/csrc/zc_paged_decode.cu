@@ -57,11 +57,6 @@ __device__ __forceinline__ int load_req(const ZcPagedArgs& a, int r, Req* q) {
   return q->n > 0 ? max(1, (q->s.nb + kDecWarps - 1) / kDecWarps) : 0;
 }
 
-// a * b / c; the quotient of 32-bit numbers where they fit (a <= 160).
-__device__ __forceinline__ long long muldiv(int a, long long b, int c) {
-  return b < (1 << 24) ? (long long)((uint32_t)a * (uint32_t)b / (uint32_t)c) : a * b / c;
-}
-
 // A border between two shares: the unit (request, KV head) that it lies in, and the step it falls on, moved to the
 // unit's start or end where the unit is too short to be cut.
 struct Place {
@@ -162,7 +157,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
   const int c = blockIdx.x;
   if (c >= g) return;
   const int least = total >= (long long)g * 2 * kLeast ? kLeast : max(1, (int)((total + g) / (2 * g)));
-  const long long border[2] = {muldiv(c, total, g), muldiv(c + 1, total, g)};
+  const long long border[2] = {zc_muldiv(c, total, g), zc_muldiv(c + 1, total, g)};
   auto found = [&](int r) {   // this thread's request, if a border lies in it
     if (mine <= 0) return;
 #pragma unroll
@@ -471,7 +466,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
       if (tid == 0) {
         auto cuts = [&](int d) {
           if (d < 1 || d >= g) return false;
-          const long long in = muldiv(d, total, g) - unit0;
+          const long long in = zc_muldiv(d, total, g) - unit0;
           if (in <= 0 || in >= seg.steps) return false;
           const int t = cut_step(in, seg.steps, least);
           return t > 0 && t < seg.steps;
