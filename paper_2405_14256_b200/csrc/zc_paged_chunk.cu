@@ -735,6 +735,37 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < min(n, ahead); ++i) keys(i);
 #pragma unroll 1
         for (int i = 0; i < n; ++i) {
+          // Tiles in the midst of a wide item, the same work with nothing to decide: what this warp does beside its
+          // products is what a step takes longer than they do.
+          if (!narrow && i == ga + 1) {
+            const int mid_end = min(ge - 2, n - 3);
+#pragma unroll 1
+            for (; i < mid_end; ++i) {
+              const uint32_t place = n_p & 1u;
+              const uint64_t vd = v_desc + (uint64_t)(vs * (kKvTile >> 4)), kd = k_desc + (uint64_t)(ks * (kKvTile >> 4));
+              uint64_t *kf = &k_full[ks], *vf = &v_full[vs], *pf = &p_full[2 * g + place];
+              if (!bar_try(kf, kp)) bar_wait(kf, kp);
+              if (!bar_try(vf, vp)) bar_wait(vf, vp);
+              if (!bar_try(pf, (n_p >> 1) & 1u)) bar_wait(pf, (n_p >> 1) & 1u);
+              tc_fence_after();
+              if (elect_one()) {
+                mma_pv(tm_o, tm_s + place * kN, vd, idesc_pv, true);
+                mma_commit(vf + kVS);    // v_free
+                mma_s(tm_s + place * kN, qd, kd, idesc_s);
+                mma_commit(&s_done[2 * g + place]);
+                mma_commit(kf + kKS);    // k_free
+              }
+              __syncwarp();
+              ++n_p;
+              ++n_s;
+              const bool kw = ks + 1 == kKS, vw = vs + 1 == kVS;
+              ks = kw ? 0 : ks + 1;
+              vs = vw ? 0 : vs + 1;
+              kp ^= kw ? 1u : 0u;
+              vp ^= vw ? 1u : 0u;
+            }
+            if (i >= n) break;
+          }
           bar_wait(&v_full[vs], vp);
           const uint64_t vd = v_desc + (uint64_t)(vs * (kKvTile >> 4));
           const bool on = mine(i);
