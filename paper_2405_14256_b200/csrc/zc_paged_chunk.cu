@@ -52,7 +52,9 @@ constexpr int kItemRows = 2 * kM;
 constexpr int kPartBytes = kItemRows * ZC_D * 4 + kItemRows * 8;
 constexpr int kMaxItems = 13000;                      // items of a head, and requests, that a call may have: what the
                                                       // prologue keeps in the tiles' shared memory (16 bytes each)
-constexpr int kItemCost = 9;                          // of an item beside its tiles: Q, first product, output (half tiles)
+// Costs as measured over mixed calls, in 220 cycles: a tile of a wide item (both groups work on it), of a narrow one
+// (the groups take turns), an item beside its tiles (Q, first product, output, masks).
+constexpr int kWideTile = 7, kNarrowTile = 5, kItemCost = 25;
 constexpr int kMinPiece = 4;                          // tiles; below, joining costs more than the even share gains
 
 // Where a CTA's share begins: item `item` of all heads' (head * items + item of the head), key tile t of it.
@@ -118,8 +120,7 @@ __device__ __forceinline__ long long block_scan(int v, long long* s_warp, long l
   return before;
 }
 
-// Cost of an item in half tiles: both groups work on every tile of a wide item, on every second of a narrow one.
-__device__ __forceinline__ int item_width(int ntok, int tpt) { return ntok <= tpt ? 2 : 3; }
+__device__ __forceinline__ int item_width(int ntok, int tpt) { return ntok <= tpt ? kNarrowTile : kWideTile; }
 __device__ __forceinline__ int item_cost(int nt, int width) { return nt * width + kItemCost; }
 // The tile at which a border at `off` into an item's cost cuts it: 0 or nt where a piece would be short.
 __device__ __forceinline__ int cut_tile(long long off, int nt, int width) {
@@ -183,6 +184,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
     *width = item_width(min(tpi, c.n - tok0), k.tpt);
     return item_tiles(a, c, tok0, tpi);
   };
+  const int most = 0x7fffffff / max(items, 1);   // a head's cost stays in 31 bits
   long long head = 0;   // cost of a head
   for (int c0 = 0; c0 < items; c0 += kThreads) {
     const int i = c0 + tid;
@@ -190,7 +192,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
     if (i < items) {
       int width;
       const int nt = tiles(i, request(i), &width);
-      cost = item_cost(nt, width);
+      cost = min(item_cost(nt, width), most);
     }
     long long t;
     const long long at = block_scan(cost, s_warp, &t);
@@ -456,6 +458,8 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
   return p != 0;
 }
+// Bits 0 .. n - 1 of 64.
+__device__ __forceinline__ uint64_t below(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 __device__ __forceinline__ void groups_sync() { asm volatile("bar.sync 1, 256;\n" ::: "memory"); }   // both groups
 
@@ -470,9 +474,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   char* base = smem_raw + (base_u - raw_u);
   const uint32_t q_addr = base_u, k_addr = base_u + 2 * kTile, v_addr = k_addr + kKS * kKvTile;
   uint64_t* bars = reinterpret_cast<uint64_t*>(base + kTiles);
-  uint64_t* q_full = bars;                  // an item's Q tiles landed
-  uint64_t* q_free = bars + 1;              // both groups' last S of an item completed
-  uint64_t* k_full = bars + 2;              // [kKS] key tile landed
+  uint64_t* q_full = bars;                  // [3] Q of a wide item's group 0 landed, of its group 1, of a narrow item
+  uint64_t* q_free = bars + 3;              // group 1's last S of a narrow item completed
+  uint64_t* k_full = bars + 4;              // [kKS] key tile landed
   uint64_t* k_free = k_full + kKS;          // [kKS] both groups are through with that tile
   uint64_t* v_full = k_free + kKS;          // [kVS] value tile landed
   uint64_t* v_free = v_full + kVS;          // [kVS] both groups are through with that tile
@@ -489,8 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   if (tid == 0) {
-    bar_init(q_full, 1);
-    bar_init(q_free, 2);
+    for (int i = 0; i < 4; ++i) bar_init(&q_full[i], 1);   // q_free too
     bar_init(&m_free[0], 1);
     bar_init(&m_free[1], 1);
     for (int i = 0; i < kKS; ++i) {
@@ -511,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < kRingN; ++i) {
       bar_init(&i_full[i], 1);
-      bar_init(&i_free[i], 11);   // Q and K, two warps for the products, eight worker warps
+      bar_init(&i_free[i], 11);   // K, two warps for the products, eight worker warps
     }
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
@@ -593,8 +596,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     if (warp == 2) {
       // ---- items, and V ----
-      const long long n_idx = (long long)k.items * a.n_req * a.h_kv;   // dense form
-      long long idx = blockIdx.x;
+      // Dense form: the items longest first, every other round of the CTAs backwards, so that each gets about the
+      // same sum (a causal prompt of 8192: 486 us in rounds all one way, 444 us so; window of 4096: 369 -> 347 us).
+      const long long n_idx = (long long)k.items * a.n_req * a.h_kv;
+      long long idx = blockIdx.x, round = 0;
+      bool back = false;
       Border at = share.begin;
       int r = share.r, in_req = share.in_req;
       Chunk c;
@@ -606,7 +612,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (idx < n_idx) {
             it = dense_item(k, idx);
             finish_item(k, k.l, it);
-            idx += gridDim.x;
+            round += gridDim.x;
+            back = !back;
+            idx = round + (back ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
           }
           return;
         }
@@ -668,24 +676,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         it = then;
       }
     } else if (warp == 1) {
-      // ---- Q and K ----
-      uint32_t item = 0, meetings = 0, met = 0;   // items with tiles, narrow ones, meetings waited for
+      // ---- K ----
+      uint32_t meetings = 0, met = 0;   // narrow items with tiles, meetings of them waited for
       Item it;
       while (next_item(it)) {
         if (it.t0 >= it.t1) continue;
-        if (item > 0) bar_wait(q_free, (item - 1) & 1u);
-        // a wide item needs the second Q tile's place, where the groups meet over narrow ones
+        // a wide item's second Q tile goes where the groups meet over narrow ones
         for (; met + (it.narrow ? 1u : 0u) < meetings; ++met) bar_wait(&m_free[met & 1u], (met >> 1) & 1u);
-        if (lane == 0) {
-          const int tiles = it.narrow ? 1 : 2;
-          expect_bytes(q_full, (uint32_t)(tiles * k.tpt * a.G * ZC_D * 2));
-          for (int g = 0; g < tiles; ++g)
-            for (int kb = 0; kb < 2; ++kb)
-              q_copy(&qmap, q_addr + g * kTile + kb * kKBlock, q_full, kb, it.kv * a.G,
-                     it.row0 + it.tok0 + g * k.tpt, PAGED ? 0 : it.r);
-        }
-        __syncwarp();
-        ++item;
         meetings += it.narrow ? 1u : 0u;
         stream(it, &kmap, k_addr, k_full, k_free, kKS);
       }
@@ -699,7 +696,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t idesc_s = (instr_desc<T>() & ~(0x3Fu << 17)) | ((uint32_t)(kN >> 3) << 17);
       const uint32_t idesc_pv = instr_desc<T>() | (1u << 16);   // B with its N dimension contiguous
       const uint64_t q_desc = smem_desc(q_addr), k_desc = smem_desc(k_addr), v_desc = desc_mn(v_addr);
-      uint32_t item = 0, n_s = 0, n_p = 0;                 // items so far; tiles of the group whose S / P V is issued
+      uint32_t n_s = 0, n_p = 0;                           // tiles of the group whose S / P V is issued
+      uint32_t n_wide = 0, n_narrow = 0; // wide and narrow items so far
+      bool met = false;                                    // the item before was a narrow one
       uint32_t ks = 0, kp = 0, vs = 0, vp = 0;             // place and phase of the next key and value tile
       Item it;
       while (next_item(it)) {
@@ -720,7 +719,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               mma_commit(&s_done[2 * g + place]);
             }
             mma_commit(&k_free[ks]);
-            if (i + 1 == n) mma_commit(q_free);
+            if (i + 1 == n && narrow && g == 1) mma_commit(q_free);
           }
           __syncwarp();
           n_s += on ? 1u : 0u;
@@ -729,8 +728,24 @@ __global__ void __launch_bounds__(kThreads, 1)
             kp ^= 1u;
           }
         };
-        bar_wait(q_full, item & 1u);
-        ++item;
+        // Q of the group's rows, brought by the warp that multiplies it: the products that read the place are through
+        // (each S has come back as P), but those of group 1 with a narrow item's rows, which both groups read.  Where
+        // group 1's tile goes the groups may be meeting still: not once the item's first key tile is there.
+        uint64_t* q_bar = &q_full[narrow ? 2 : g];
+        if (!narrow || g == 0) {
+          if (met && g == 0) bar_wait(q_free, (n_narrow - 1) & 1u);
+          if (met && g == 1) bar_wait(&k_full[ks], kp);
+          if (elect_one()) {
+            expect_bytes(q_bar, (uint32_t)(k.tpt * a.G * ZC_D * 2));
+            for (int kb = 0; kb < 2; ++kb)
+              q_copy(&qmap, q_addr + g * kTile + kb * kKBlock, q_bar, kb, it.kv * a.G, it.row0 + it.tok0 + g * k.tpt,
+                     PAGED ? 0 : it.r);
+          }
+          __syncwarp();
+        }
+        bar_wait(q_bar, (narrow ? n_narrow : n_wide) & 1u);
+        if (narrow) ++n_narrow; else ++n_wide;
+        met = narrow;
 #pragma unroll 1
         for (int i = 0; i < min(n, ahead); ++i) keys(i);
 #pragma unroll 1
@@ -829,10 +844,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool edge = key0 + kN - 1 > first || (key0 <= last - a.window && key0 + kN > a.sinks);
         if (edge) {
           // the tile crosses the diagonal, the window's edge or the end of the sinks
-          const int e_hi = pos - key0, e_lo = max(pos - a.window, -1) - key0, e_sink = a.sinks - key0;
+          const uint64_t seen = below(pos + 1 - key0) & (~below(pos + 1 - a.window - key0) | below(a.sinks - key0));
+          const uint32_t seen2[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
 #pragma unroll
           for (int e = 0; e < kN; ++e)
-            if (!(e <= e_hi && (e > e_lo || e < e_sink))) v[e] = -INFINITY;
+            if (!((seen2[e >> 5] >> (e & 31)) & 1u)) v[e] = -INFINITY;
           // values that no row of the item sees may hold anything (a weight of 0 times NaN is NaN)
           if (key0 + kN > it.s.hi || (key0 < it.s.lo && key0 + kN > it.s.sink_n)) {
             const uint32_t tile = tile0 + (uint32_t)(t - it.t0), vs = tile % kVS;
