@@ -61,9 +61,10 @@ constexpr int kMinPiece = 4;                          // tiles; below, joining c
 struct Border { int item, t; };
 // The item that the border before CTA c cuts, written by the first such CTA of the item.
 struct ChunkJoin {
-  int on, r, tok0, kv;
+  int on, tok0, kv;
   int first, last;    // CTAs whose shares begin inside the item
-  int pad[2];
+  int row0, n;        // the request's first row, and its rows
+  int pad;
 };
 struct ChunkWs {
   ChunkJoin* joins;   // [CTA]
@@ -270,8 +271,10 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
       while (j.first > 1 && cuts(j.first - 1)) --j.first;
       if (j.first == c) {
         while (j.last + 1 < n_cta && cuts(j.last + 1)) ++j.last;
+        const Chunk q = load_chunk(a, f.r);
         j.on = 1;
-        j.r = f.r;
+        j.row0 = q.row0;
+        j.n = q.n;
         j.tok0 = f.in_req * tpi;
         j.kv = f.kv;
       }
@@ -491,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   float2* s_ms = reinterpret_cast<float2*>(base + kTiles + 448);                    // [128] narrow items: group 1's (m, sum)
   int* ring = reinterpret_cast<int*>(base + kTiles + 448 + 1024);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  zc_let_next_start();
   if (tid == 0) {
     for (int i = 0; i < 4; ++i) bar_init(&q_full[i], 1);   // q_free too
     bar_init(&m_free[0], 1);
@@ -529,6 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);
+  zc_wait_for_last();
   Share share;
   if (PAGED) share = find_share(k, base, reinterpret_cast<long long*>(s_ms), reinterpret_cast<Found*>(base + kTiles + 384), gridDim.x);
 
@@ -1028,14 +1032,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 // border before CTA c cuts first; a thread takes eight channels of a row.
 template <typename T> __global__ void __launch_bounds__(256) k_chunk_join(const ChunkArgs k) {
   __shared__ int s_slot[ZC_PAGED_MAX_CTAS + 1], s_count;
-  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  zc_let_next_start();
+  zc_wait_for_last();
   const ZcPagedArgs& a = k.a;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const ChunkJoin j = k.ws.joins[blockIdx.x / 16 + 1];
   if (!j.on) return;
-  const Chunk c = load_chunk(a, j.r);
-  if (warp == 0) {
-    // the pieces in order: the end of the share before the item's first border, then the starts behind each border
+  // the pieces in order: the end of the share before the item's first border, then the starts behind each border;
+  // as a rule there is one border
+  if (warp == 0 && j.last > j.first) {
     int n = 1;
     if (lane == 0) s_slot[0] = 2 * (j.first - 1) + 1;
     for (int d = j.first; d <= j.last; d += 32) {
@@ -1046,36 +1051,46 @@ template <typename T> __global__ void __launch_bounds__(256) k_chunk_join(const 
     }
     if (lane == 0) s_count = n;
   }
-  __syncthreads();
-  const int n = s_count;
+  if (j.last > j.first) __syncthreads();
+  const int n = j.last > j.first ? s_count : 2;
   const int row = (int)(blockIdx.x % 16) * 16 + (threadIdx.x & 15), cg = threadIdx.x >> 4;
   const int g = row / kM, in = row % kM, tok_in = in / a.G, tok = j.tok0 + g * k.tpt + tok_in;
-  if (tok_in >= k.tpt || tok >= c.n) return;
-  auto sums = [&](int q) {
-    return reinterpret_cast<const float2*>(k.ws.parts + (long long)s_slot[q] * kPartBytes + kItemRows * ZC_D * 4)[row];
+  if (tok_in >= k.tpt || tok >= j.n) return;
+  auto piece = [&](int q) {
+    return k.ws.parts + (long long)(j.last > j.first ? s_slot[q] : 2 * j.first - 1 + q) * kPartBytes;
   };
-  float m = -1e30f;
+  auto sums = [&](int q) { return reinterpret_cast<const float2*>(piece(q) + kItemRows * ZC_D * 4)[row]; };
+  struct Part { float4 x[2]; };
+  auto channels = [&](int q) {
+    const float4* p = reinterpret_cast<const float4*>(piece(q)) + row;
+    Part r = {{p[cg * kItemRows], p[(cg + 16) * kItemRows]}};
+    return r;
+  };
+  // the first two pieces (there always are) on their way together
+  const float2 ms0 = sums(0), ms1 = sums(1);
+  const Part p0 = channels(0), p1 = channels(1);
+  float m = fmaxf(ms0.x, ms1.x);
 #pragma unroll 4
-  for (int q = 0; q < n; ++q) m = fmaxf(m, sums(q).x);
+  for (int q = 2; q < n; ++q) m = fmaxf(m, sums(q).x);
   float sum = 0.f;
   float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-#pragma unroll 2
-  for (int q = 0; q < n; ++q) {
-    const float4* p = reinterpret_cast<const float4*>(k.ws.parts + (long long)s_slot[q] * kPartBytes) + row;
-    const float2 ms = sums(q);
-    const float4 x[2] = {p[cg * kItemRows], p[(cg + 16) * kItemRows]};
+  auto take = [&](float2 ms, const Part& p) {
     const float f = zc_exp2(ms.x - m);
     sum = fmaf(ms.y, f, sum);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      acc[u].x = fmaf(x[u].x, f, acc[u].x);
-      acc[u].y = fmaf(x[u].y, f, acc[u].y);
-      acc[u].z = fmaf(x[u].z, f, acc[u].z);
-      acc[u].w = fmaf(x[u].w, f, acc[u].w);
+      acc[u].x = fmaf(p.x[u].x, f, acc[u].x);
+      acc[u].y = fmaf(p.x[u].y, f, acc[u].y);
+      acc[u].z = fmaf(p.x[u].z, f, acc[u].z);
+      acc[u].w = fmaf(p.x[u].w, f, acc[u].w);
     }
-  }
+  };
+  take(ms0, p0);
+  take(ms1, p1);
+#pragma unroll 2
+  for (int q = 2; q < n; ++q) take(sums(q), channels(q));
   const float inv = sum > 0.f ? 1.f / sum : 0.f;
-  const long long at = (long long)(c.row0 + tok) * a.h_q + j.kv * a.G + (in - tok_in * a.G);
+  const long long at = (long long)(j.row0 + tok) * a.h_q + j.kv * a.G + (in - tok_in * a.G);
 #pragma unroll
   for (int u = 0; u < 2; ++u)
     *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.out) + at * ZC_D + 4 * (cg + 16 * u)) =
@@ -1147,10 +1162,9 @@ template <typename T>
 int launch_chunk(zc_pages* p, const ChunkArgs& k, const CUtensorMap& qmap, cudaStream_t st) {
   cudaError_t e = ready<T, true>();
   if (e != cudaSuccess) return e;
-  k_chunk_attention<T, true><<<p->n_sm, kThreads, kSmem, st>>>(k, qmap, p->k64, p->v64);
-  p->launches += 1;
-  e = cudaGetLastError();
+  e = zc_launch_early(k_chunk_attention<T, true>, dim3(p->n_sm), dim3(kThreads), kSmem, st, k, qmap, p->k64, p->v64);
   if (e != cudaSuccess) return e;
+  p->launches += 1;
   if (p->n_sm > 1) {
     e = zc_launch_early(k_chunk_join<T>, dim3(16 * (p->n_sm - 1)), dim3(256), 0, st, k);
     if (e != cudaSuccess) return e;
@@ -1215,14 +1229,14 @@ int zc_launch_prefill_window(zc_cache* c, const void* Q, const void* K, const vo
   if (cfg.dtype == ZC_F16) {
     e = ready<__half, false>();
     if (e != cudaSuccess) return e;
-    k_chunk_attention<__half, false><<<grid, kThreads, kSmem, st>>>(k, qmap, kmap, vmap);
+    e = zc_launch_early(k_chunk_attention<__half, false>, dim3(grid), dim3(kThreads), kSmem, st, k, qmap, kmap, vmap);
   } else {
     e = ready<__nv_bfloat16, false>();
     if (e != cudaSuccess) return e;
-    k_chunk_attention<__nv_bfloat16, false><<<grid, kThreads, kSmem, st>>>(k, qmap, kmap, vmap);
+    e = zc_launch_early(k_chunk_attention<__nv_bfloat16, false>, dim3(grid), dim3(kThreads), kSmem, st, k, qmap, kmap, vmap);
   }
   c->launches += 1;
-  return (int)cudaGetLastError();
+  return (int)e;
 }
 
 int zc_paged_chunk_error_code(int* out) { return (int)cudaMemcpyFromSymbol(out, g_zc_tc_error, sizeof(int)); }

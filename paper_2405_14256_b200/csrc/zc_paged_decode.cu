@@ -129,6 +129,8 @@ __global__ void __launch_bounds__(kDecThreads, 1)
     asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&vmap)));
   }
   asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  zc_let_next_start();
+  zc_wait_for_last();
 
   // ---- this CTA's share ----
   long long sum = 0;
@@ -554,8 +556,7 @@ int launch(zc_pages* p, const ZcPagedArgs& a, float* parts, unsigned* arrived, c
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) once[dev] = true;
   }
-  k_paged_decode<T, NT><<<p->n_sm, kDecThreads, kDecSmem, st>>>(a, parts, arrived, p->k16, p->v16);
-  e = cudaGetLastError();
+  e = zc_launch_early(k_paged_decode<T, NT>, dim3(p->n_sm), dim3(kDecThreads), kDecSmem, st, a, parts, arrived, p->k16, p->v16);
   if (e != cudaSuccess) return e;
   p->launches += 1;
   return cudaSuccess;

@@ -2,7 +2,7 @@
 // lengths, and the copies between dense rows and pages.
 #include <string.h>
 #include <new>
-#include "zc_pages.h"
+#include "zc_paged.cuh"
 
 namespace {
 
@@ -23,8 +23,8 @@ __device__ __forceinline__ long long warp_incl(long long v, int lane) {
 // the grid.  A row's page comes from the table where the request held it before, and straight from
 // the free list where this call grants it, so no CTA waits for another's table entries.
 __global__ void __launch_bounds__(kTabThreads) k_page_tables(
-    int page_log2, int n_req, const int32_t* __restrict__ past, const int32_t* __restrict__ fresh,
-    const int32_t* __restrict__ free_pages, int n_free, const int32_t* __restrict__ free_state,
+    int page_log2, int n_req, const int32_t* past, const int32_t* fresh, const int32_t* free_pages, int n_free,
+    const int32_t* free_state,
     int32_t* table, int width, int32_t* __restrict__ kv_len, int32_t* __restrict__ row_start, int n_rows,
     int32_t* __restrict__ slots, int32_t* __restrict__ pos, int32_t* __restrict__ free_out) {
   __shared__ long long s_row[kTabChunk + 1], s_page[kTabChunk + 1];
@@ -32,6 +32,7 @@ __global__ void __launch_bounds__(kTabThreads) k_page_tables(
   __shared__ long long s_warp[3][kTabThreads / 32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int psize = 1 << page_log2;
+  zc_wait_for_last();
   const long long next = free_state[0] > 0 ? free_state[0] : 0;
   const long long end = free_state[1] < n_free ? free_state[1] : n_free;
   long long rows_before = 0, pages_before = 0, wanted = 0;
@@ -143,10 +144,12 @@ constexpr int kCopyThreads = 256, kUnroll = 4;
 
 __global__ void __launch_bounds__(kCopyThreads) k_page_write(
     char* __restrict__ kp, char* __restrict__ vp, long long sp, long long st, long long sh, int page_log2,
-    int n_pages, int h_kv, const char* __restrict__ kr, const char* __restrict__ vr, long long rs_row,
-    long long rs_head, const int32_t* __restrict__ slots, long long n_pieces) {
+    int n_pages, int h_kv, const char* kr, const char* vr, long long rs_row, long long rs_head,
+    const int32_t* slots, long long n_pieces) {
   const int part = (threadIdx.x & 15) * 16, group = threadIdx.x >> 4;
   const long long first = ((long long)blockIdx.x * kUnroll) * (kCopyThreads / 16) + group;
+  zc_let_next_start();
+  zc_wait_for_last();
   uint4 k[kUnroll], v[kUnroll];
   char* kd[kUnroll];
   long long off[kUnroll];
@@ -177,13 +180,15 @@ __global__ void __launch_bounds__(kCopyThreads) k_page_write(
 
 // grid.y: (request, head); the pieces of a CTA are consecutive tokens.
 __global__ void __launch_bounds__(kCopyThreads) k_page_read(
-    const char* __restrict__ kp, const char* __restrict__ vp, long long sp, long long st, long long sh, int page_log2,
-    int n_pages, int h_kv, const int32_t* __restrict__ table, int width, int l, char* __restrict__ K,
+    const char* kp, const char* vp, long long sp, long long st, long long sh, int page_log2,
+    int n_pages, int h_kv, const int32_t* table, int width, int l, char* __restrict__ K,
     char* __restrict__ V, long long ds_req, long long ds_head, long long ds_tok, int blocks_per_head) {
   const int part = (threadIdx.x & 15) * 16, group = threadIdx.x >> 4;
   const int unit = blockIdx.x / blocks_per_head, blk = blockIdx.x % blocks_per_head;
   const int r = unit / h_kv, head = unit % h_kv;
   const long long t0 = (long long)blk * kUnroll * (kCopyThreads / 16) + group;
+  zc_let_next_start();
+  zc_wait_for_last();
   uint4 k[kUnroll], v[kUnroll];
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
@@ -293,10 +298,9 @@ int zc_page_tables(int page_size, int n_req, const int32_t* past, const int32_t*
   // a CTA per 1024 rows or 64 requests, whichever asks for more; at most two per SM
   const int want = zc_ceil_div(n_rows, 1024) > zc_ceil_div(n_req, 64) ? zc_ceil_div(n_rows, 1024) : zc_ceil_div(n_req, 64);
   const int grid = want > 296 ? 296 : want;
-  k_page_tables<<<grid, kTabThreads, 0, (cudaStream_t)stream>>>(log2, n_req, past, fresh, free_pages, n_free, free_state,
-                                                              table, table_width, kv_len, row_start, n_rows, slots, pos,
-                                                              free_out);
-  return zc_cuda_status((int)cudaGetLastError());
+  return zc_cuda_status((int)zc_launch_early(k_page_tables, dim3(grid), dim3(kTabThreads), 0, (cudaStream_t)stream, log2,
+                                             n_req, past, fresh, free_pages, n_free, free_state, table, table_width,
+                                             kv_len, row_start, n_rows, slots, pos, free_out));
 }
 
 int zc_page_write(zc_pages* p, const void* k_rows, const void* v_rows, const int64_t row_strides[2],
@@ -311,11 +315,12 @@ int zc_page_write(zc_pages* p, const void* k_rows, const void* v_rows, const int
   const long long grid = (pieces + kUnroll * (kCopyThreads / 16) - 1) / (kUnroll * (kCopyThreads / 16));
   if (grid > 0x7fffffffLL) return ZC_EINVAL;
   const int64_t* s = p->cfg.strides;
-  k_page_write<<<(int)grid, kCopyThreads, 0, (cudaStream_t)stream>>>(
-      p->k, p->v, 2 * s[0], 2 * s[1], 2 * s[2], p->page_log2, p->cfg.n_pages, p->cfg.n_kv_heads, (const char*)k_rows,
-      (const char*)v_rows, 2 * row_strides[0], 2 * row_strides[1], slots, pieces);
+  const cudaError_t e = zc_launch_early(
+      k_page_write, dim3((int)grid), dim3(kCopyThreads), 0, (cudaStream_t)stream, p->k, p->v, 2 * s[0], 2 * s[1], 2 * s[2],
+      p->page_log2, p->cfg.n_pages, p->cfg.n_kv_heads, (const char*)k_rows, (const char*)v_rows, 2 * row_strides[0],
+      2 * row_strides[1], slots, pieces);
   p->launches += 1;
-  return zc_cuda_status((int)cudaGetLastError());
+  return zc_cuda_status((int)e);
 }
 
 int zc_page_read(zc_pages* p, const int32_t* table, int table_width, int n_req, int l, void* K, void* V,
@@ -329,11 +334,12 @@ int zc_page_read(zc_pages* p, const int32_t* table, int table_width, int n_req, 
   const long long grid = (long long)per_head * n_req * p->cfg.n_kv_heads;
   if (grid > 0x7fffffffLL) return ZC_EINVAL;
   const int64_t* s = p->cfg.strides;
-  k_page_read<<<(int)grid, kCopyThreads, 0, (cudaStream_t)stream>>>(
-      p->k, p->v, 2 * s[0], 2 * s[1], 2 * s[2], p->page_log2, p->cfg.n_pages, p->cfg.n_kv_heads, table, table_width, l,
-      (char*)K, (char*)V, 2 * kv_strides[0], 2 * kv_strides[1], 2 * kv_strides[2], per_head);
+  const cudaError_t e = zc_launch_early(
+      k_page_read, dim3((int)grid), dim3(kCopyThreads), 0, (cudaStream_t)stream, p->k, p->v, 2 * s[0], 2 * s[1], 2 * s[2],
+      p->page_log2, p->cfg.n_pages, p->cfg.n_kv_heads, table, table_width, l, (char*)K, (char*)V, 2 * kv_strides[0],
+      2 * kv_strides[1], 2 * kv_strides[2], per_head);
   p->launches += 1;
-  return zc_cuda_status((int)cudaGetLastError());
+  return zc_cuda_status((int)e);
 }
 
 int zc_paged_attention(zc_pages* p, const void* q, const int64_t q_strides[2], const int32_t* table, int table_width,
