@@ -385,11 +385,17 @@ def _want(t, name: str, shape, dtype, contiguous: bool = True) -> None:
                             f"{t.dtype} {tuple(t.shape)} with strides {t.stride()}")
 
 
-def _want_i32(t, name: str, n: int) -> None:
-    """Refuses anything but n contiguous int32 values on a GPU."""
-    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
-        raise ZipCacheError(f"{name}: expected {n} contiguous int32 values on a GPU, got {t.dtype} {tuple(t.shape)} "
-                            f"with strides {t.stride()} on {t.device}")
+def _want_i32(t, name: str, n: int, index: int) -> None:
+    """Refuses anything but n contiguous int32 values on GPU `index`."""
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != index:
+        raise ZipCacheError(f"{name}: expected {n} contiguous int32 values on cuda:{index}, got {t.dtype} "
+                            f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
+
+
+def _want_on(t, name: str, index: int) -> None:
+    """Refuses a tensor that is not on GPU `index`."""
+    if t.get_device() != index:
+        raise ZipCacheError(f"{name}: expected a tensor on cuda:{index}, got one on {t.device}")
 
 
 def _cuda_device(device) -> torch.device:
@@ -418,12 +424,12 @@ class StepTables:
             with torch.cuda.device(self._index):
                 return self.build(page_size, past, fresh, free_pages, free_state, table, stream)
         n = self.n_req
-        _want_i32(past, "past", n)
-        _want_i32(fresh, "fresh", n)
-        _want_i32(free_pages, "free_pages", free_pages.numel())
-        _want_i32(free_state, "free_state", 3)
+        _want_i32(past, "past", n, self._index)
+        _want_i32(fresh, "fresh", n, self._index)
+        _want_i32(free_pages, "free_pages", free_pages.numel(), self._index)
+        _want_i32(free_state, "free_state", 3, self._index)
         width = table.size(-1)
-        _want_i32(table, "table", n * width)
+        _want_i32(table, "table", n * width, self._index)
         _check(lib().zc_page_tables(page_size, n, past.data_ptr(), fresh.data_ptr(), free_pages.data_ptr(),
                                     free_pages.numel(), free_state.data_ptr(), table.data_ptr(), width,
                                     self.kv_len.data_ptr(), self.row_start.data_ptr(), self.n_rows,
@@ -446,6 +452,8 @@ class PagedKV:
             raise ZipCacheError("pages must be [n_pages, page_size, n_kv_heads, 128], the last dimension contiguous, "
                                 "K and V with the same strides")
         _want(v_pages, "v_pages", k_pages.shape, k_pages.dtype, contiguous=False)
+        _want_on(k_pages, "k_pages", self.device.index)
+        _want_on(v_pages, "v_pages", self.device.index)
         if k_pages.dtype not in (torch.float16, torch.bfloat16):
             raise ZipCacheError("pages must be float16 or bfloat16")
         n_pages, page_size, n_kv, d = k_pages.shape
@@ -457,6 +465,9 @@ class PagedKV:
         if workspace is None:
             workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
             workspace[:ZC_PAGES_SYNC_BYTES].zero_()
+        _want_on(workspace, "workspace", self._index)
+        if not workspace.is_contiguous():
+            raise ZipCacheError("the workspace must be contiguous")
         self._ws_bytes = workspace.numel() * workspace.element_size()
         if self._ws_bytes < self.workspace_bytes:
             raise ZipCacheError("shared workspace too small")
@@ -476,11 +487,11 @@ class PagedKV:
             pass
 
     def _rows(self, t, name: str, n: int, heads: int) -> None:
-        """Refuses anything but [n, heads, 128] of the pages' type with contiguous channels."""
+        """Refuses anything but [n, heads, 128] of the pages' type and device with contiguous channels."""
         if t.dtype is not self.dtype or t.dim() != 3 or t.size(0) != n or t.size(1) != heads or t.size(2) != 128 \
-                or t.stride(2) != 1:
-            raise ZipCacheError(f"{name}: expected {self.dtype} {(n, heads, 128)} with contiguous channels, got "
-                                f"{t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+                or t.stride(2) != 1 or t.get_device() != self._index:
+            raise ZipCacheError(f"{name}: expected {self.dtype} {(n, heads, 128)} with contiguous channels on "
+                                f"{self.device}, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
     def write(self, k_rows, v_rows, slots, stream=None):
         """Rows [n, n_kv_heads, 128] into slots [n] (int32; negative: skipped)."""
@@ -488,7 +499,7 @@ class PagedKV:
             with torch.cuda.device(self._index):
                 return self.write(k_rows, v_rows, slots, stream)
         n = slots.numel()
-        _want_i32(slots, "slots", n)
+        _want_i32(slots, "slots", n, self._index)
         self._rows(k_rows, "k_rows", n, self.n_kv_heads)
         self._rows(v_rows, "v_rows", n, self.n_kv_heads)
         strides = k_rows.stride()
@@ -508,6 +519,8 @@ class PagedKV:
         V = torch.empty(shape, dtype=self.dtype, device=self.device) if V is None else V
         _want(K, "K", shape, self.dtype, contiguous=False)
         _want(V, "V", shape, self.dtype, contiguous=False)
+        for t, name in ((table, "table"), (K, "K"), (V, "V")):
+            _want_on(t, name, self._index)
         if K.stride(3) != 1:
             raise ZipCacheError("the channels of a row must be contiguous")
         zc_page_read(self.handle, table, l, K, V, stream)
@@ -524,10 +537,10 @@ class PagedKV:
                 return self.attention(q, table, row_start, kv_len, max_rows, window, sinks, out, row_lse, stream)
         n_req, n, heads = kv_len.numel(), q.size(0), self.n_q_heads
         self._rows(q, "q", n, heads)
-        _want_i32(kv_len, "kv_len", n_req)
-        _want_i32(row_start, "row_start", n_req + 1)
+        _want_i32(kv_len, "kv_len", n_req, self._index)
+        _want_i32(row_start, "row_start", n_req + 1, self._index)
         width = table.size(-1)
-        _want_i32(table, "table", n_req * width)
+        _want_i32(table, "table", n_req * width, self._index)
         if out is None:
             out = torch.empty((n, heads, 128), dtype=self.dtype, device=self.device)
         else:
@@ -536,8 +549,10 @@ class PagedKV:
                 raise ZipCacheError("out must be contiguous")
         if row_lse is None:
             row_lse = torch.empty((n, heads), dtype=torch.float32, device=self.device)
-        elif row_lse.dtype is not torch.float32 or row_lse.numel() != n * heads or not row_lse.is_contiguous():
-            _want(row_lse, "row_lse", (n, heads), torch.float32)
+        else:
+            if row_lse.dtype is not torch.float32 or row_lse.numel() != n * heads or not row_lse.is_contiguous():
+                _want(row_lse, "row_lse", (n, heads), torch.float32)
+            _want_on(row_lse, "row_lse", self._index)
         strides = q.stride()
         _check(lib().zc_paged_attention(self.handle, q.data_ptr(), _I64x2(strides[0], strides[1]), table.data_ptr(), width,
                                         row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
@@ -629,12 +644,23 @@ class ZipCache:
         """prefill_attention under a sliding window: a row sees the last `window` tokens up to itself and
         the first `sinks` ones.  out and row_lse may be given (contiguous)."""
         l = K.shape[2]
+        index = _cuda_device(self.device).index
+        if _current_device() != index:
+            with torch.cuda.device(index):
+                return self.prefill_attention_window(Q, K, V, window, sinks, out, row_lse, stream)
+        for t, name, heads in ((Q, "Q", self.n_q_heads), (K, "K", self.n_kv_heads), (V, "V", self.n_kv_heads)):
+            _want(t, name, (self.batch, heads, l, 128), self.dtype, contiguous=False)
+            _want_on(t, name, index)
+            if t.stride(3) != 1:
+                raise ZipCacheError(f"{name}: the channels of a row must be contiguous")
         if out is None:
             out = torch.empty((self.batch, self.n_q_heads, l, 128), dtype=self.dtype, device=self.device)
         if row_lse is None:
             row_lse = torch.empty((self.batch, self.n_q_heads, l), dtype=torch.float32, device=self.device)
         _want(out, "out", (self.batch, self.n_q_heads, l, 128), self.dtype)
         _want(row_lse, "row_lse", (self.batch, self.n_q_heads, l), torch.float32)
+        _want_on(out, "out", index)
+        _want_on(row_lse, "row_lse", index)
         zc_prefill_attention_window(self.handle, Q, K, V, l, window, sinks, out, row_lse, stream)
         return out, row_lse
 

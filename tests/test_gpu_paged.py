@@ -390,6 +390,90 @@ def test_wrong_tensors_are_refused(zc):
         zc.PagedKV(pool.k_pages, pool.v_pages.bfloat16(), 8)
 
 
+def test_tensors_on_another_device_are_refused(zc):
+    """Host tensors: the pointers would mean nothing to the kernels."""
+    pool, (q, table, row_start, kv_len, n), out, lse = attention_case(zc, "fp16", 8, 2, 16, [40], [3])
+    for i in range(4):
+        args = [q, table, row_start, kv_len]
+        args[i] = args[i].cpu()
+        with pytest.raises(zc.ZipCacheError):
+            pool.attention(*args, n)
+    for kw in (dict(out=out.cpu()), dict(row_lse=lse.cpu())):
+        with pytest.raises(zc.ZipCacheError):
+            pool.attention(q, table, row_start, kv_len, n, **kw)
+    rows, slots = q[:, :2].contiguous(), i32([0, 1, 2])
+    for args in ((rows.cpu(), rows, slots), (rows, rows.cpu(), slots), (rows, rows, slots.cpu())):
+        with pytest.raises(zc.ZipCacheError):
+            pool.write(*args)
+    dense = torch.empty(1, 2, 16, D, dtype=torch.float16)
+    with pytest.raises(zc.ZipCacheError):
+        pool.read(table, 16, dense, dense)
+    with pytest.raises(zc.ZipCacheError):
+        pool.read(table.cpu(), 16)
+    with pytest.raises(zc.ZipCacheError):
+        zc.PagedKV(pool.k_pages, pool.v_pages.cpu(), 8)
+    with pytest.raises(zc.ZipCacheError):
+        zc.PagedKV(pool.k_pages, pool.v_pages, 8, workspace=torch.zeros(pool.workspace_bytes, dtype=torch.uint8))
+    step = zc.StepTables(1, 3)
+    with pytest.raises(zc.ZipCacheError):
+        step.build(16, kv_len.cpu(), kv_len, kv_len, i32([0, 1, 0]), table)
+    cache = zc.ZipCache(torch.float16, 1, 8, 2, 16, 1, 0.4, device=DEV)
+    x = torch.zeros(1, 8, 16, D, dtype=torch.float16, device=DEV)
+    for args in ((x.cpu(), x[:, :2], x[:, :2]), (x, x[:, :2].cpu(), x[:, :2]), (x, x[:, :2], x[:, :2].cpu()),
+                 (x.float(), x[:, :2], x[:, :2]), (x, x, x)):
+        with pytest.raises(zc.ZipCacheError):
+            cache.prefill_attention_window(*args, 4)
+    settled(zc)
+
+
+@pytest.mark.parametrize("max_new", [1, 70])
+def test_steps_issued_without_a_pause(zc, max_new):
+    """Tables, write and attention over the same buffers, step after step with nothing waited for: each kernel starts
+    while the one before runs, and must see all that it wrote.  The same steps with a pause after every call give
+    the bits to match."""
+    dt, hq, hkv, page, n_req, steps = torch.bfloat16, 8, 2, 16, 5, 12
+    n_pages, width = 600, 120
+    rng = np.random.RandomState(max_new)
+    plan = [i32(rng.randint(0, max_new + 1, n_req)) for _ in range(steps)]
+    gen = torch.Generator(device=DEV).manual_seed(max_new)
+    q = torch.randn(steps, n_req * max_new, hq, D, generator=gen, device=DEV).to(dt)
+    kr, vr = (torch.randn(steps, n_req * max_new, hkv, D, generator=gen, device=DEV).to(dt) for _ in range(2))
+    free = i32(rng.permutation(n_pages))
+
+    def run(pause):
+        k, v = (torch.zeros(n_pages, page, hkv, D, dtype=dt, device=DEV) for _ in range(2))
+        pool = zc.PagedKV(k, v, hq, max_req=n_req, max_rows=n_req * max_new)
+        turn = [zc.StepTables(n_req, n_req * max_new) for _ in range(2)]
+        past, state, table = i32([0] * n_req), i32([0, n_pages, 0]), i32(np.full((n_req, width), -1))
+        out, lse = torch.zeros_like(q), torch.zeros(steps, n_req * max_new, hq, device=DEV)
+        settled(zc)
+        for i in range(steps):
+            step = turn[i & 1]
+            for call in (lambda: step.build(page, past, plan[i], free, state, table),
+                         lambda: pool.write(kr[i], vr[i], step.slots),
+                         lambda: pool.attention(q[i], table, step.row_start, step.kv_len, max_new, out=out[i],
+                                                row_lse=lse[i])):
+                call()
+                if pause:
+                    torch.cuda.synchronize()
+            past, state = step.kv_len, step.free_state
+        settled(zc)
+        return k, v, table, state, out, lse
+
+    want = run(True)
+    for _ in range(5):
+        for g, w in zip(run(False), want):
+            assert torch.equal(g, w)
+
+
+def test_many_short_and_long_chunks(zc):
+    """Items of one and of two tiles of rows in every order, through one place of Q after the other."""
+    rng = np.random.RandomState(12)
+    new = [int(n) for n in rng.choice([1, 2, 7, 31, 32, 33, 63, 64, 65, 100, 130], 48)]
+    past = [int(p) for p in rng.randint(0, 700, 48)]
+    attention_case(zc, "bf16", 8, 2, 16, past, new, seed=4)
+
+
 # ---------------------------------------------------------------- a window over dense tensors
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 @pytest.mark.parametrize("b,hq,hkv,l,window,sinks", [
@@ -413,6 +497,22 @@ def test_windowed_prompt(zc, dtype, b, hq, hkv, l, window, sinks):
             t_out, t_lse = ref.tolerances(dt, o, mean_abs, largest, seen, total, vmax)
             assert ((out[r, h].double() - o).abs() <= t_out).all(), (r, h)
             assert ((lse[r, h].double() - ls).abs() <= t_lse).all(), (r, h)
+
+
+@pytest.mark.parametrize("window", [90, 5000])
+def test_a_prompt_in_several_rounds_of_the_grid(zc, window):
+    """352 items of different lengths: two full rounds of the CTAs and a part of one."""
+    l, h = 2600, 32
+    gen = torch.Generator(device=DEV).manual_seed(window)
+    q, k, v = (torch.randn(1, h, l, D, generator=gen, device=DEV).half() for _ in range(3))
+    cache = zc.ZipCache(torch.float16, 1, h, h, l, 1, 0.4, device=DEV)
+    out, lse = cache.prefill_attention_window(q, k, v, window, 2)
+    settled(zc)
+    for i in range(h):
+        o, ls, mean_abs, largest, seen, total = ref.attend(q[0, i], k[0, i], v[0, i], 0, window, 2)
+        t_out, t_lse = ref.tolerances(torch.float16, o, mean_abs, largest, seen, total, v.abs().max().double())
+        assert ((out[0, i].double() - o).abs() <= t_out).all(), i
+        assert ((lse[0, i].double() - ls).abs() <= t_lse).all(), i
 
 
 def test_a_window_of_the_whole_prompt_is_no_window(zc):
