@@ -273,7 +273,10 @@ int zc_decode_attention_noalloc(zc_cache* c, const void* q, void* out, int is_pr
  * complete, zc_page_read (its rows as the dense tensors zc_prefill_compress takes).
  * All lengths and tables are read on the device, so that a step can be captured in a CUDA graph
  * and replayed with other lengths of the same n_req / n_rows.  The calling thread's current device
- * must be the one that holds the buffers. */
+ * must be the one that holds the buffers.
+ * The kernels are launched while the stream's kernel before them still runs and wait for it before
+ * they touch memory, so calls on one stream see each other's results as usual.  They are none of the
+ * calls that ZC_FLAG_OVERLAP_CALLS lets a decode call overlap: let them complete before such a call. */
 typedef struct {
   int32_t struct_size;    /* sizeof(zc_page_config) */
   int32_t dtype;          /* ZC_F16 | ZC_BF16 */

@@ -3,6 +3,7 @@ marshalling only.  Every step of the path runs in the library's kernels."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -164,6 +165,14 @@ def _stream(stream) -> int:
 
 
 _I64x2, _I64x3 = C.c_int64 * 2, C.c_int64 * 3
+
+
+@functools.lru_cache(maxsize=256)
+def _strides2(a: int, b: int):
+    """Two strides as the library takes them (it only reads them)."""
+    return _I64x2(a, b)
+
+
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -428,7 +437,7 @@ class StepTables:
         _want_i32(fresh, "fresh", n, self._index)
         _want_i32(free_pages, "free_pages", free_pages.numel(), self._index)
         _want_i32(free_state, "free_state", 3, self._index)
-        width = table.size(-1)
+        width = table.shape[-1]
         _want_i32(table, "table", n * width, self._index)
         _check(lib().zc_page_tables(page_size, n, past.data_ptr(), fresh.data_ptr(), free_pages.data_ptr(),
                                     free_pages.numel(), free_state.data_ptr(), table.data_ptr(), width,
@@ -486,12 +495,13 @@ class PagedKV:
         except Exception:
             pass
 
-    def _rows(self, t, name: str, n: int, heads: int) -> None:
-        """Refuses anything but [n, heads, 128] of the pages' type and device with contiguous channels."""
-        if t.dtype is not self.dtype or t.dim() != 3 or t.size(0) != n or t.size(1) != heads or t.size(2) != 128 \
-                or t.stride(2) != 1 or t.get_device() != self._index:
+    def _rows(self, t, name: str, n: int, heads: int) -> tuple:
+        """The strides of t; refuses anything but [n, heads, 128] of the pages' type and device with contiguous channels."""
+        strides = t.stride()
+        if t.dtype is not self.dtype or t.shape != (n, heads, 128) or strides[2] != 1 or t.get_device() != self._index:
             raise ZipCacheError(f"{name}: expected {self.dtype} {(n, heads, 128)} with contiguous channels on "
-                                f"{self.device}, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+                                f"{self.device}, got {t.dtype} {tuple(t.shape)} with strides {strides} on {t.device}")
+        return strides
 
     def write(self, k_rows, v_rows, slots, stream=None):
         """Rows [n, n_kv_heads, 128] into slots [n] (int32; negative: skipped)."""
@@ -500,12 +510,10 @@ class PagedKV:
                 return self.write(k_rows, v_rows, slots, stream)
         n = slots.numel()
         _want_i32(slots, "slots", n, self._index)
-        self._rows(k_rows, "k_rows", n, self.n_kv_heads)
-        self._rows(v_rows, "v_rows", n, self.n_kv_heads)
-        strides = k_rows.stride()
-        if strides != v_rows.stride():
+        strides = self._rows(k_rows, "k_rows", n, self.n_kv_heads)
+        if strides != self._rows(v_rows, "v_rows", n, self.n_kv_heads):
             raise ZipCacheError("k_rows and v_rows must share strides")
-        _check(lib().zc_page_write(self.handle, k_rows.data_ptr(), v_rows.data_ptr(), _I64x2(strides[0], strides[1]),
+        _check(lib().zc_page_write(self.handle, k_rows.data_ptr(), v_rows.data_ptr(), _strides2(strides[0], strides[1]),
                                    slots.data_ptr(), n, _stream_of(self._index, stream)), "zc_page_write")
 
     def read(self, table, l: int, K=None, V=None, stream=None):
@@ -535,11 +543,11 @@ class PagedKV:
         if _current_device() != self._index:
             with torch.cuda.device(self._index):
                 return self.attention(q, table, row_start, kv_len, max_rows, window, sinks, out, row_lse, stream)
-        n_req, n, heads = kv_len.numel(), q.size(0), self.n_q_heads
-        self._rows(q, "q", n, heads)
+        n_req, n, heads = kv_len.numel(), q.shape[0], self.n_q_heads
+        strides = self._rows(q, "q", n, heads)
         _want_i32(kv_len, "kv_len", n_req, self._index)
         _want_i32(row_start, "row_start", n_req + 1, self._index)
-        width = table.size(-1)
+        width = table.shape[-1]
         _want_i32(table, "table", n_req * width, self._index)
         if out is None:
             out = torch.empty((n, heads, 128), dtype=self.dtype, device=self.device)
@@ -553,8 +561,7 @@ class PagedKV:
             if row_lse.dtype is not torch.float32 or row_lse.numel() != n * heads or not row_lse.is_contiguous():
                 _want(row_lse, "row_lse", (n, heads), torch.float32)
             _want_on(row_lse, "row_lse", self._index)
-        strides = q.stride()
-        _check(lib().zc_paged_attention(self.handle, q.data_ptr(), _I64x2(strides[0], strides[1]), table.data_ptr(), width,
+        _check(lib().zc_paged_attention(self.handle, q.data_ptr(), _strides2(strides[0], strides[1]), table.data_ptr(), width,
                                         row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
                                         out.data_ptr(), row_lse.data_ptr(), self.workspace.data_ptr(), self._ws_bytes,
                                         _stream_of(self._index, stream)), "zc_paged_attention")

@@ -9,9 +9,10 @@
 // of its rows sees: those of the first `sinks` tokens, then those of the window.  The CTAs are
 // persistent, one per SM; each works through items until there are none:
 //   warp 2      walks the CTA's items, one ahead of the others, and copies V
-//   warp 1      copies Q (a box per half of a tile's channels) and K, as warp 2 V, page by page: a box per
-//               page of 64 tokens or more, a lane per page and a box per half of the channels below that
-//   warps 0, 3  the matrix products of group 0 and 1, tcgen05.mma with accumulators in tensor memory:
+//   warp 1      copies K, as warp 2 V, page by page: a box per page of 64 tokens or more, a lane per page and a
+//               box per half of the channels below that
+//   warps 0, 3  copy Q (a box per half of a tile's channels) and issue the matrix products of group 0 and 1,
+//               tcgen05.mma with accumulators in tensor memory:
 //               S_g = Q_g K^T (both K-major in shared memory), 128 x 64, and O_g += P_g V (P_g in tensor
 //               memory over the first half of its S, V with its channels contiguous), 128 x 128
 //   warps 4-7, 8-11  groups 0 and 1, one row per thread: running maximum (renewed, and O rescaled, when the
@@ -20,10 +21,15 @@
 // Each group has two places for S, and S of a key tile is computed two tiles ahead: a group turns one S
 // after the other into P without waiting for a product, and the tensor cores' work hides behind that of
 // the groups (and the other way round).  With 128 keys to a tile and one place for S, the chain product -
-// weights - product left either side idle half of the time (5000 cycles per 256 rows x 128 keys).  The
-// next item's Q and first key tiles arrive while this one's output is written.
+// weights - product left either side idle half of the time (5000 cycles per 256 rows x 128 keys; now 3300).
+// The next item's Q and first key tiles arrive while this one's output is written.
+//   What it takes (1.7 GHz): 1650 cycles per wide tile, of which the tensor cores alone need 1140 and the exp2 unit
+// 1020; about 5500 more per item (its first and last tiles' masks, the last product, 3000 for the output).  A chunk
+// of 2048 tokens over 30000, 32 query heads over 8: 860-900 us, 1150-1210 TFLOP/s; a prompt of 8192 under a window
+// of 4096: 355 us, 1160 TFLOP/s.  Measured and not kept: 16 worker warps, two to a row (1 to 4 % slower); one place
+// for S and two for P (the same); the next S fetched into registers ahead (1.3 times as long).
 // For pages the lengths are on the device, and every CTA finds its own share there: the items of all heads,
-// laid end to end with their cost in tiles, are cut into as many equal stretches as there are CTAs.  An item
+// laid end to end with their costs, are cut into as many equal stretches as there are CTAs.  An item
 // that a border cuts is worked on in pieces along its keys; k_chunk_join puts them together in their order.
 #include <cstring>
 #include "zc_paged.cuh"
@@ -55,7 +61,7 @@ constexpr int kMaxItems = 13000;                      // items of a head, and re
 // Costs as measured over mixed calls, in 220 cycles: a tile of a wide item (both groups work on it), of a narrow one
 // (the groups take turns), an item beside its tiles (Q, first product, output, masks).
 constexpr int kWideTile = 7, kNarrowTile = 5, kItemCost = 25;
-constexpr int kMinPiece = 4;                          // tiles; below, joining costs more than the even share gains
+constexpr int kMinPiece = 4;                          // tiles; a shorter piece goes to its neighbour
 
 // Where a CTA's share begins: item `item` of all heads' (head * items + item of the head), key tile t of it.
 struct Border { int item, t; };
@@ -121,6 +127,7 @@ __device__ __forceinline__ long long block_scan(int v, long long* s_warp, long l
   return before;
 }
 
+// Cost of one of an item's tiles, and of the item.
 __device__ __forceinline__ int item_width(int ntok, int tpt) { return ntok <= tpt ? kNarrowTile : kWideTile; }
 __device__ __forceinline__ int item_cost(int nt, int width) { return nt * width + kItemCost; }
 // The tile at which a border at `off` into an item's cost cuts it: 0 or nt where a piece would be short.

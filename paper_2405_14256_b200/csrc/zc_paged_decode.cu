@@ -3,9 +3,9 @@
 //
 // The visible keys of every (request, KV head) are cut into steps of 128 (eight blocks of 16); all
 // steps of the call, laid end to end, are dealt out to the CTAs in equal, consecutive shares, so that
-// ragged lengths do not matter (units of a few steps stay whole).  A CTA is eight warps; warp w takes block w of each step through a ring
-// of its own (bulk tensor copies of 16 keys and 16 values, 8 KB a stage), so that no warp waits for
-// another inside a share.  Per block, with the query rows as the N dimension of the tensor-core tiles:
+// ragged lengths do not matter (units of a few steps stay whole).  A CTA is eight warps; warp w takes block w
+// of each step through a ring of its own (bulk tensor copies of 16 keys and 16 values, 8 KB a stage), so that
+// no warp waits for another inside a share.  Per block, with the query rows as the N dimension of the tensor-core tiles:
 //   S^T (16 keys x 8 rows) = K Q^T        A = keys from shared memory, B = rows kept in registers
 //   O^T (128 x 8 rows)    += V^T P^T      A = values read transposed, B = P^T = 2^(S - m), rounded to
 //                                         the input type (half a step relative, as a stored weight
@@ -15,6 +15,9 @@
 // that one CTA holds whole is written out; the pieces of one that a share's border cuts go to the workspace,
 // and the CTA that brings the last of them puts them together, in the order of the CTAs (the result does not
 // depend on timing).  It knows by a counter per unit, zero before and after every call.
+//   32 requests of 2048-4096 tokens, 32 KV heads: 222 us, 6.7 TB/s; a window of 4096 over 16 requests, 8 KV heads:
+// 47.5 us, 5.7 TB/s; 4 requests of 200-512 tokens: 7.0 us, of which launch, lengths and tables, one round trip to the
+// keys and the join are all.
 #include <cstring>
 #include "zc_pages.h"
 #include "zc_layout.cuh"
