@@ -550,7 +550,7 @@ class PagedKV:
         width = table.shape[-1]
         _want_i32(table, "table", n_req * width, self._index)
         if out is None:
-            out = torch.empty((n, heads, 128), dtype=self.dtype, device=self.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         else:
             self._rows(out, "out", n, heads)
             if not out.is_contiguous():

@@ -25,8 +25,8 @@
 // The next item's Q and first key tiles arrive while this one's output is written.
 //   What it takes (1.7 GHz): 1650 cycles per wide tile, of which the tensor cores alone need 1140 and the exp2 unit
 // 1020; about 5500 more per item (its first and last tiles' masks, the last product, 3000 for the output).  A chunk
-// of 2048 tokens over 30000, 32 query heads over 8: 860-900 us, 1150-1210 TFLOP/s; a prompt of 8192 under a window
-// of 4096: 355 us, 1160 TFLOP/s.  Measured and not kept: 16 worker warps, two to a row (1 to 4 % slower); one place
+// of 2048 tokens over 30000, 32 query heads over 8: 887 us, 1170 TFLOP/s; a prompt of 8192 under a window
+// of 4096: 353 us, 1170 TFLOP/s.  Measured and not kept: 16 worker warps, two to a row (1 to 4 % slower); one place
 // for S and two for P (the same); the next S fetched into registers ahead (1.3 times as long).
 // For pages the lengths are on the device, and every CTA finds its own share there: the items of all heads,
 // laid end to end with their costs, are cut into as many equal stretches as there are CTAs.  An item

@@ -354,6 +354,54 @@ def test_a_captured_step_replays_with_other_lengths(zc, few):
                 assert ((lse[a:e, h].double() - l).abs() <= t_lse).all()
 
 
+@pytest.mark.parametrize("max_new", [1, 40])
+def test_a_captured_step_forked_over_two_streams(zc, max_new):
+    """Copies, a fill and the write on a second stream between the captured calls: what a call waits for may be a
+    kernel, a copy or several of them."""
+    pool, (q, table, row_start, kv_len, n), out, lse = attention_case(zc, "bf16", 8, 2, 16, [500, 20], [max_new] * 2)
+    n_rows = q.shape[0]
+    slots = i32(np.concatenate([np.asarray([int(table[r, p // 16]) * 16 + p % 16 for p in range(k - max_new, k)])
+                                for r, k in enumerate(kv_len.tolist())]))
+    rows = torch.randn(2, n_rows, 2, D, device=DEV).to(q.dtype)
+    k_in, v_in, q_in = rows[0].clone(), rows[1].clone(), torch.zeros_like(q)
+    got, got_lse = torch.empty_like(out), torch.empty_like(lse)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def one_step():
+        forked, joined = torch.cuda.Event(), torch.cuda.Event()
+        k_in.zero_()
+        forked.record(a)
+        b.wait_event(forked)
+        with torch.cuda.stream(b):
+            k_in.copy_(rows[0])
+            pool.write(k_in, v_in, slots)
+            joined.record(b)
+        got.fill_(7.0)
+        q_in.copy_(q)
+        a.wait_event(joined)
+        pool.attention(q_in, table, row_start, kv_len, n, out=got, row_lse=got_lse)
+
+    with torch.cuda.stream(a):
+        one_step()
+        a.synchronize()
+        want, want_lse = got.clone(), got_lse.clone()
+        pool.write(rows[0], rows[1], slots)
+        first, first_lse = pool.attention(q, table, row_start, kv_len, n)
+        a.synchronize()
+        assert torch.equal(first, want) and torch.equal(first_lse, want_lse)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=a):
+            one_step()
+    for _ in range(5):
+        pool.k_pages.view(-1, 2, D)[slots.long()] = 0
+        got.zero_()
+        q_in.zero_()
+        settled(zc)
+        graph.replay()
+        settled(zc)
+        assert torch.equal(got, want) and torch.equal(got_lse, want_lse)
+
+
 def test_two_streams_with_workspaces_of_their_own(zc):
     a, args_a, out_a, lse_a = attention_case(zc, "fp16", 8, 2, 16, [4000, 100], [30, 60], seed=1)
     b, args_b, out_b, lse_b = attention_case(zc, "fp16", 8, 2, 16, [2000, 900, 1], [1, 1, 1], seed=2)
