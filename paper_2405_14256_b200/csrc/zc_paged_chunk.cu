@@ -131,10 +131,17 @@ __device__ __forceinline__ long long block_scan(int v, long long* s_warp, long l
 __device__ __forceinline__ int item_width(int ntok, int tpt) { return ntok <= tpt ? kNarrowTile : kWideTile; }
 __device__ __forceinline__ int item_cost(int nt, int width) { return nt * width + kItemCost; }
 // The tile at which a border at `off` into an item's cost cuts it: 0 or nt where a piece would be short.
-__device__ __forceinline__ int cut_tile(long long off, int nt, int width) {
-  const long long t = (off - kItemCost / 2) / width;
-  return t < kMinPiece ? 0 : nt - t < kMinPiece ? nt : (int)t;
+__device__ __forceinline__ int cut_tile(long long off, int nt, int width, int grain) {
+  off -= kItemCost / 2;
+  if (off <= 0) return 0;
+  // (nt is below 2^24: beyond 31 bits the border lies behind the item)
+  const int cost = (int)min(off, 0x7fffffffLL), t = (width == kWideTile ? cost / kWideTile : cost / kNarrowTile) & -grain;
+  return t < kMinPiece ? 0 : nt - t < kMinPiece ? nt : t;
 }
+
+// Shares of fewer than eight tiles are cut at every fourth tile only: a piece of one or two costs more than they do (one
+// chunk of 40 tokens, 32 heads over 8: over 1000 21.3 -> 19.0 us, over 4000 27.5 -> 23.6; shares of 25 tiles would lose 4 %).
+__device__ __forceinline__ int cut_grain(long long all, int n_cta) { return all < 8LL * kWideTile * n_cta ? kMinPiece : 1; }
 
 // This CTA's share of a paged call, found by the whole block in shared memory (16 bytes per request or item).
 struct Share {
@@ -228,7 +235,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
         const int m = (lo + hi) >> 1;
         if (s_cost[m] <= in) lo = m; else hi = m;
       }
-      const int r = request(lo), nt = tiles(lo, r, &f.width), t = cut_tile(in - s_cost[lo], nt, f.width);
+      const int r = request(lo), nt = tiles(lo, r, &f.width), t = cut_tile(in - s_cost[lo], nt, f.width, cut_grain(all, n_cta));
       b.item = kv * items + lo;
       b.t = t;
       f.start = kv * head + s_cost[lo];
@@ -271,7 +278,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
     if (s.begin.t > 0) {
       // the CTAs around this one whose borders cut the same item
       auto cuts = [&](int d) {
-        const int u = cut_tile(zc_muldiv(d, f.all, n_cta) - f.start, f.nt, f.width);
+        const int u = cut_tile(zc_muldiv(d, f.all, n_cta) - f.start, f.nt, f.width, cut_grain(f.all, n_cta));
         return u > 0 && u < f.nt;
       };
       j.first = j.last = c;
