@@ -319,7 +319,9 @@ void zc_pages_free(zc_pages* p);
  *                .. row_start[r + 1] - 1 of the step's row-wise tensors
  *   slots, pos   n_rows: slot and position of every row; slot -1 for a token whose page is missing;
  *                both -1 for rows behind the last request's (padding)
- *   free_out     3: {next + pages taken, end, pages missing}; not the buffer of free_state (ZC_EINVAL)
+ *   free_out     3: {next + pages taken, end, pages missing}
+ * No output may overlap past, fresh, free_pages or free_state (ZC_EINVAL): a step whose lengths feed the
+ * next one's takes two sets of outputs in turn.
  * A step with pages missing must not be carried on with as it is: free pages and build it again. */
 int zc_page_tables(int page_size, int n_req, const int32_t* past, const int32_t* fresh,
                    const int32_t* free_pages, int n_free, const int32_t* free_state, int32_t* table,

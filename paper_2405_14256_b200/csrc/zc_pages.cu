@@ -218,6 +218,10 @@ __global__ void __launch_bounds__(kCopyThreads) k_page_read(
 }
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+template <typename... P> bool aligned4(const P*... p) { return (((uintptr_t)p | ...) & 3) == 0; }
+
+struct Ints { const int32_t* at; long long n; };
+bool overlap(const Ints& a, const Ints& b) { return a.n && b.n && a.at < b.at + b.n && b.at < a.at + a.n; }
 
 int page_log2_of(int page_size) {
   for (int i = 4; i <= 8; ++i)
@@ -296,7 +300,15 @@ int zc_page_tables(int page_size, int n_req, const int32_t* past, const int32_t*
   if (log2 < 0 || n_req < 1 || n_rows < 0 || n_free < 0 || table_width < 1) return ZC_EINVAL;
   if ((long long)table_width << log2 > ZC_NO_WINDOW) return ZC_EINVAL;
   if (!past || !fresh || !free_state || !table || !kv_len || !row_start || !free_out) return ZC_EINVAL;
-  if ((n_free && !free_pages) || (n_rows && (!slots || !pos)) || free_state == free_out) return ZC_EINVAL;
+  if ((n_free && !free_pages) || (n_rows && (!slots || !pos))) return ZC_EINVAL;
+  if (!aligned4(past, fresh, free_pages, free_state, table, kv_len, row_start, slots, pos, free_out)) return ZC_EALIGN;
+  // every CTA reads all lengths, some after others have written their results
+  const Ints in[4] = {{past, n_req}, {fresh, n_req}, {free_pages, n_free}, {free_state, 3}};
+  const Ints out[6] = {{table, (long long)n_req * table_width}, {kv_len, n_req}, {row_start, n_req + 1LL},
+                       {slots, n_rows}, {pos, n_rows}, {free_out, 3}};
+  for (const Ints& i : in)
+    for (const Ints& o : out)
+      if (overlap(i, o)) return ZC_EINVAL;
   // a CTA per 1024 rows or 64 requests, whichever asks for more; at most two per SM
   const int want = zc_ceil_div(n_rows, 1024) > zc_ceil_div(n_req, 64) ? zc_ceil_div(n_rows, 1024) : zc_ceil_div(n_req, 64);
   const int grid = want > 296 ? 296 : want;
@@ -310,7 +322,7 @@ int zc_page_write(zc_pages* p, const void* k_rows, const void* v_rows, const int
   if (!p || n_rows < 0 || !row_strides) return ZC_EINVAL;
   if (n_rows == 0) return ZC_OK;
   if (!k_rows || !v_rows || !slots) return ZC_EINVAL;
-  if (!aligned16(k_rows) || !aligned16(v_rows)) return ZC_EALIGN;
+  if (!aligned16(k_rows) || !aligned16(v_rows) || !aligned4(slots)) return ZC_EALIGN;
   for (int i = 0; i < 2; ++i)
     if (row_strides[i] < 0 || row_strides[i] % 8) return ZC_EINVAL;
   const long long pieces = (long long)n_rows * p->cfg.n_kv_heads;
@@ -329,7 +341,7 @@ int zc_page_read(zc_pages* p, const int32_t* table, int table_width, int n_req, 
                  const int64_t kv_strides[3], zc_stream_t stream) {
   if (!p || !table || !K || !V || !kv_strides || table_width < 1 || n_req < 1 || l < 1) return ZC_EINVAL;
   if ((long long)l > (long long)table_width << p->page_log2) return ZC_ECAPACITY;
-  if (!aligned16(K) || !aligned16(V)) return ZC_EALIGN;
+  if (!aligned16(K) || !aligned16(V) || !aligned4(table)) return ZC_EALIGN;
   for (int i = 0; i < 3; ++i)
     if (kv_strides[i] < 0 || kv_strides[i] % 8) return ZC_EINVAL;
   const int per_head = zc_ceil_div(l, kUnroll * (kCopyThreads / 16));
@@ -352,7 +364,8 @@ int zc_paged_attention(zc_pages* p, const void* q, const int64_t q_strides[2], c
   if (n_req == 0 || n_rows == 0 || max_rows == 0) return ZC_OK;
   if (!q || !table || !row_start || !kv_len || !out || !workspace || table_width < 1) return ZC_EINVAL;
   if ((long long)table_width << p->page_log2 > ZC_NO_WINDOW || n_rows > ZC_NO_WINDOW) return ZC_EINVAL;
-  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || ((uintptr_t)row_lse & 3)) return ZC_EALIGN;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || !aligned4(row_lse, table, row_start, kv_len))
+    return ZC_EALIGN;
   for (int i = 0; i < 2; ++i)
     if (q_strides[i] < 0 || q_strides[i] % 8 || q_strides[i] >= (1LL << 39)) return ZC_EINVAL;
   if ((p->cfg.n_q_heads > 1 && q_strides[1] < ZC_D) || (n_rows > 1 && q_strides[0] < ZC_D)) return ZC_EINVAL;

@@ -79,13 +79,22 @@ def test_tables_refusals(zc):
     f = zc.lib().zc_page_tables
     names = ["page_size", "n_req", "past", "fresh", "free_pages", "n_free", "free_state", "table", "width", "kv_len",
              "row_start", "n_rows", "slots", "pos", "free_out"]
-    good = dict(page_size=16, n_req=4, past=FAKE, fresh=FAKE, free_pages=FAKE, n_free=8, free_state=FAKE, table=FAKE,
-                width=4, kv_len=FAKE, row_start=FAKE, n_rows=10, slots=FAKE, pos=FAKE, free_out=C.c_void_p(0x30000))
+    at = {n: C.c_void_p(0x10000 + 0x1000 * i) for i, n in enumerate(names)}
+    good = {**at, **dict(page_size=16, n_req=4, n_free=8, width=4, n_rows=10)}
     for bad in [dict(page_size=0), dict(page_size=24), dict(n_req=0), dict(n_rows=-1), dict(n_free=-1), dict(width=0),
-                dict(width=1 << 27), dict(free_out=FAKE)] + [
+                dict(width=1 << 27)] + [
             {n: None} for n in names if n not in ("page_size", "n_req", "n_free", "width", "n_rows")]:
         kw = {**good, **bad}
         assert f(*[kw[n] for n in names], None) == EINVAL, bad
+    inputs, outputs = ("past", "fresh", "free_pages", "free_state"), ("table", "kv_len", "row_start", "slots", "pos", "free_out")
+    for i in inputs:
+        for o in outputs:
+            for shift in (-8, 0, 8):   # outputs that begin, or end, inside an input
+                kw = {**good, o: C.c_void_p(at[i].value + shift)}
+                assert f(*[kw[n] for n in names], None) == EINVAL, (i, o, shift)
+    for n in inputs + outputs:
+        kw = {**good, n: C.c_void_p(at[n].value + 2)}
+        assert f(*[kw[n] for n in names], None) == EALIGN, n
 
 
 def test_write_and_read_refusals(zc, pages):
@@ -98,6 +107,7 @@ def test_write_and_read_refusals(zc, pages):
     assert lib.zc_page_write(pages, FAKE, FAKE, bad_rs, FAKE, 3, None) == EINVAL
     assert lib.zc_page_write(pages, FAKE, FAKE, None, FAKE, 3, None) == EINVAL
     assert lib.zc_page_write(pages, FAKE, ODD, rs, FAKE, 3, None) == EALIGN
+    assert lib.zc_page_write(pages, FAKE, FAKE, rs, C.c_void_p(0x20002), 3, None) == EALIGN
     assert lib.zc_page_write(pages, None, None, rs, None, 0, None) == 0          # nothing to do
     ks, bad_ks = (C.c_int64 * 3)(8 * 640 * 128, 640 * 128, 128), (C.c_int64 * 3)(8, 4, 128)
     assert lib.zc_page_read(pages, FAKE, 10, 2, 641, FAKE, FAKE, ks, None) == ECAPACITY
@@ -106,6 +116,7 @@ def test_write_and_read_refusals(zc, pages):
     assert lib.zc_page_read(pages, None, 10, 2, 64, FAKE, FAKE, ks, None) == EINVAL
     assert lib.zc_page_read(pages, FAKE, 10, 2, 64, FAKE, FAKE, bad_ks, None) == EINVAL
     assert lib.zc_page_read(pages, FAKE, 10, 2, 64, ODD, FAKE, ks, None) == EALIGN
+    assert lib.zc_page_read(pages, C.c_void_p(0x20002), 10, 2, 64, FAKE, FAKE, ks, None) == EALIGN
     assert lib.zc_page_read(None, FAKE, 10, 2, 64, FAKE, FAKE, ks, None) == EINVAL
     assert lib.zc_pages_launch_count(pages) == 0
 
@@ -127,7 +138,8 @@ def test_attention_refusals(zc, pages):
         assert call(**bad) == EINVAL, bad
     for n in ("q", "out", "ws"):
         assert call(**{n: ODD}) == EALIGN, n
-    assert call(lse=C.c_void_p(0x20002)) == EALIGN
+    for n in ("lse", "table", "row_start", "kv_len"):
+        assert call(**{n: C.c_void_p(0x20002)}) == EALIGN, n
     assert call(ws_bytes=1024) == ECAPACITY and call(ws_bytes=1024, max_rows=1) == ECAPACITY
     # nothing to do
     assert call(n_req=0) == 0 and call(n_rows=0) == 0 and call(max_rows=0) == 0
