@@ -881,13 +881,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         // With the maximum that the row has so far, which as a rule is near enough: no pass over the logits for a
-        // new one.  The sum tells where it is not (a weight above 2^4 at least, 2^10 at most stays unseen).
+        // new one.  The sum tells where it is not (a weight above 2^4 at least, 2^10 at most stays unseen).  Only the
+        // item's rows have a say: the tile's other rows hold another request's queries or what was there before, and
+        // a new maximum changes how the weights round.
         uint32_t w[kN / 2];
         float sum = 0.f;
         bool renew = edge || unset;
         if (!renew) {
           sum = weights<T>(v, scale, m_run, w);
-          renew = __any_sync(0xffffffffu, !(sum <= kBigSum));
+          renew = __any_sync(0xffffffffu, valid && !(sum <= kBigSum));
         }
         if (renew) {
           float mx4[4] = {v[0], v[1], v[2], v[3]};
@@ -896,7 +898,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int i = 0; i < 4; ++i) mx4[i] = e + 4 < kN ? max3(mx4[i], v[e + i], v[e + 4 + i]) : fmaxf(mx4[i], v[e + i]);
           const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * scale;
-          const bool grow = mx > m_run + kTau;
+          const bool grow = valid && mx > m_run + kTau;
           if (__any_sync(0xffffffffu, grow)) {
             const float alpha = grow ? zc_exp2(m_run - mx) : 1.f;
             if (t > t_first) {
