@@ -24,6 +24,13 @@ __device__ __forceinline__ long long zc_muldiv(int a, long long b, int c) {
   return b < (1 << 24) ? (long long)((uint32_t)a * (uint32_t)b / (uint32_t)c) : a * b / c;
 }
 
+// bar_wait of a whole warp, with one answer for all lanes: a lane whose wait ran out must not part from the others.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
+  return __all_sync(0xffffffffu, bar_wait(bar, parity));
+}
+// Before a warp leaves: what it asked for has arrived (or the bound has run out once more).
+__device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) { (void)bar_wait(bar, parity); }
+
 // One box of a page: rows `row` ... of it, half `half` of the channels on.
 __device__ __forceinline__ void page_copy(const CUtensorMap* map, uint32_t dst, uint64_t* bar, int row, int half,
                                           int head, int page) {

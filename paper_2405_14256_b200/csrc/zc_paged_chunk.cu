@@ -23,6 +23,9 @@
 // the groups (and the other way round).  With 128 keys to a tile and one place for S, the chain product -
 // weights - product left either side idle half of the time (5000 cycles per 256 rows x 128 keys; now 3300).
 // The next item's Q and first key tiles arrive while this one's output is written.
+//   Every wait is bounded, also that of the two groups for each other.  Warps 0 to 3 leave where one runs out: they
+// issue nothing more, wait (with the bound) for their own copies and products in flight, and meet the others at the
+// kernel's end; a worker warp goes on with void values until no more items come.
 //   What it takes (1.7 GHz): 1650 cycles per wide tile, of which the tensor cores alone need 1140 and the exp2 unit
 // 1020; about 5500 more per item (its first and last tiles' masks, the last product, 3000 for the output).  A chunk
 // of 2048 tokens over 30000, 32 query heads over 8: 887 us, 1170 TFLOP/s; a prompt of 8192 under a window
@@ -413,12 +416,6 @@ __device__ __forceinline__ void finish_item(const ChunkArgs& k, int n, Item& it)
   }
 }
 
-// bar_wait that says whether the phase completed (false: the bound ran out here or elsewhere).
-__device__ __forceinline__ bool bar_wait_ok(uint64_t* bar, uint32_t parity) {
-  bar_wait(bar, parity);
-  return bar_try(bar, parity);
-}
-
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   float2 d;
   asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
@@ -478,7 +475,6 @@ __device__ __forceinline__ bool elect_one() {
 // Bits 0 .. n - 1 of 64.
 __device__ __forceinline__ uint64_t below(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
-__device__ __forceinline__ void groups_sync() { asm volatile("bar.sync 1, 256;\n" ::: "memory"); }   // both groups
 
 template <typename T, bool PAGED>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -504,7 +500,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* i_full = o_done + 2;            // [kRingN] an item is in the ring
   uint64_t* i_free = i_full + kRingN;       // [kRingN] all roles have read it
   uint64_t* m_free = i_free + kRingN;       // [2] the groups' meeting over a narrow item is over (in turn)
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(m_free + 2);
+  uint64_t* meet_bar = m_free + 2;          // the groups' eight warps meet over a narrow item
+  uint64_t* drained = meet_bar + 1;         // [2] all products of the group completed
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 2);
+  uint32_t* meet_slot = tmem_slot + 1;      // meetings that all eight warps have come to; ~0: there are no more
   float2* s_ms = reinterpret_cast<float2*>(base + kTiles + 448);                    // [128] narrow items: group 1's (m, sum)
   int* ring = reinterpret_cast<int*>(base + kTiles + 448 + 1024);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -513,6 +512,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < 4; ++i) bar_init(&q_full[i], 1);   // q_free too
     bar_init(&m_free[0], 1);
     bar_init(&m_free[1], 1);
+    bar_init(meet_bar, 8);
+    *meet_slot = 0;
     for (int i = 0; i < kKS; ++i) {
       bar_init(&k_full[i], 1);
       bar_init(&k_free[i], 2);
@@ -528,6 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       bar_init(&o_last[g], 1);
       bar_init(&o_done[g], 1);
+      bar_init(&drained[g], 1);
     }
     for (int i = 0; i < kRingN; ++i) {
       bar_init(&i_full[i], 1);
@@ -554,7 +556,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   // Next item of the ring; a whole warp calls.  False: there are no more (or a wait ran out).
   auto next_item = [&](Item& it) {
     const uint32_t at = n_item % kRingN;
-    if (!bar_wait_ok(&i_full[at], (n_item / kRingN) & 1u)) return false;
+    if (!warp_wait(&i_full[at], (n_item / kRingN) & 1u)) return false;
     const int* src = ring + at * kRingInts;
     int* dst = reinterpret_cast<int*>(&it);
 #pragma unroll
@@ -567,7 +569,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
-    // The key (or value) tiles of an item through their ring; the whole warp calls.
+    // The key (or value) tiles of an item through their ring; the whole warp calls.  False: a wait ran out.
     uint32_t stage = 0, phase = 1;   // of this warp's stream; the first wait for a free place succeeds at once
     auto stream = [&](const Item& it, const CUtensorMap* map, uint32_t at, uint64_t* full, uint64_t* free, uint32_t places) {
       const int rows = PAGED ? min(kN, 1 << a.page_log2) : kN;
@@ -597,7 +599,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, on)) * (uint32_t)rows * (ZC_D * 2);
           }
         }
-        bar_wait(&free[stage], phase);
+        if (!warp_wait(&free[stage], phase)) return false;
         if (lane == 0) expect_bytes(&full[stage], bytes);
         __syncwarp();
         if (on) {
@@ -611,6 +613,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           phase ^= 1u;
         }
       }
+      return true;
+    };
+    // The places before `stage` were filled in this round of the ring, the others in the one before (or never).
+    auto landed = [&](uint64_t* full, uint32_t places) {
+      for (uint32_t i = 0; i < places; ++i) drain(&full[i], i < stage ? phase ^ 1u : phase);
     };
     if (warp == 2) {
       // ---- items, and V ----
@@ -672,7 +679,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t n = 0;   // items announced
       auto announce = [&](const Item& it) {
         const uint32_t place = n % kRingN;
-        if (n >= kRingN && !bar_wait_ok(&i_free[place], (n / kRingN - 1) & 1u)) return false;
+        if (n >= kRingN && !warp_wait(&i_free[place], (n / kRingN - 1) & 1u)) return false;
         if (lane == 0) {
           int* dst = ring + place * kRingInts;
           const int* src = reinterpret_cast<const int*>(&it);
@@ -689,21 +696,23 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = announce(it);
       while (ok && it.r >= 0) {
         find_item(then);
-        ok = announce(then);
-        stream(it, &vmap, v_addr, v_full, v_free, kVS);
+        ok = announce(then) && stream(it, &vmap, v_addr, v_full, v_free, kVS);
         it = then;
       }
+      landed(v_full, kVS);
     } else if (warp == 1) {
       // ---- K ----
       uint32_t meetings = 0, met = 0;   // narrow items with tiles, meetings of them waited for
+      bool ok = true;
       Item it;
-      while (next_item(it)) {
+      while (ok && next_item(it)) {
         if (it.t0 >= it.t1) continue;
         // a wide item's second Q tile goes where the groups meet over narrow ones
-        for (; met + (it.narrow ? 1u : 0u) < meetings; ++met) bar_wait(&m_free[met & 1u], (met >> 1) & 1u);
+        for (; ok && met + (it.narrow ? 1u : 0u) < meetings; ++met) ok = warp_wait(&m_free[met & 1u], (met >> 1) & 1u);
         meetings += it.narrow ? 1u : 0u;
-        stream(it, &kmap, k_addr, k_full, k_free, kKS);
+        ok = ok && stream(it, &kmap, k_addr, k_full, k_free, kKS);
       }
+      landed(k_full, kKS);
     } else {
       // ---- matrix products of group g ----
       // Per tile: O += P V, then the group's S two of its tiles on, into the place that this P leaves.  Each
@@ -718,8 +727,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t n_wide = 0, n_narrow = 0; // wide and narrow items so far
       bool met = false;                                    // the item before was a narrow one
       uint32_t ks = 0, kp = 0, vs = 0, vp = 0;             // place and phase of the next key and value tile
+      uint64_t* q_last = nullptr;                          // barrier and phase of the last Q copy issued
+      uint32_t q_last_phase = 0;
+      bool ok = true;                                      // no wait has run out
       Item it;
-      while (next_item(it)) {
+      while (ok && next_item(it)) {
         const int t0 = uniform(it.t0), n = uniform(it.t1) - t0, narrow = uniform(it.narrow);
         const int ga = uniform(g ? it.ga[1] : it.ga[0]) - t0, ge = uniform(g ? it.ge[1] : it.ge[0]) - t0;
         if (n <= 0) continue;
@@ -727,7 +739,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t qd = q_desc + (uint64_t)((narrow ? 0 : g) * (kTile >> 4));
         auto mine = [&](int i) { return narrow ? (i & 1) == g : i >= ga && i < ge; };
         auto keys = [&](int i) {        // the item's key tile i: its S, and the tile's release
-          bar_wait(&k_full[ks], kp);
+          ok = warp_wait(&k_full[ks], kp);
+          if (!ok) return;
           const uint64_t kd = k_desc + (uint64_t)(ks * (kKvTile >> 4));
           const uint32_t place = n_s & 1u;
           const bool on = mine(i);
@@ -750,9 +763,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         // (each S has come back as P), but those of group 1 with a narrow item's rows, which both groups read.  Where
         // group 1's tile goes the groups may be meeting still: not once the item's first key tile is there.
         uint64_t* q_bar = &q_full[narrow ? 2 : g];
+        const uint32_t q_phase = (narrow ? n_narrow : n_wide) & 1u;
         if (!narrow || g == 0) {
-          if (met && g == 0) bar_wait(q_free, (n_narrow - 1) & 1u);
-          if (met && g == 1) bar_wait(&k_full[ks], kp);
+          if (met) ok = g == 0 ? warp_wait(q_free, (n_narrow - 1) & 1u) : warp_wait(&k_full[ks], kp);
+          if (!ok) break;
+          q_last = q_bar;
+          q_last_phase = q_phase;
           if (elect_one()) {
             expect_bytes(q_bar, (uint32_t)(k.tpt * a.G * ZC_D * 2));
             for (int kb = 0; kb < 2; ++kb)
@@ -761,13 +777,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           __syncwarp();
         }
-        bar_wait(q_bar, (narrow ? n_narrow : n_wide) & 1u);
+        ok = warp_wait(q_bar, q_phase);
         if (narrow) ++n_narrow; else ++n_wide;
         met = narrow;
 #pragma unroll 1
-        for (int i = 0; i < min(n, ahead); ++i) keys(i);
+        for (int i = 0; ok && i < min(n, ahead); ++i) keys(i);
 #pragma unroll 1
-        for (int i = 0; i < n; ++i) {
+        for (int i = 0; ok && i < n; ++i) {
           // Tiles in the midst of a wide item, the same work with nothing to decide: what this warp does beside its
           // products is what a step takes longer than they do.
           if (!narrow && i == ga + 1) {
@@ -777,11 +793,11 @@ __global__ void __launch_bounds__(kThreads, 1)
               const uint32_t place = n_p & 1u;
               const uint64_t vd = v_desc + (uint64_t)(vs * (kKvTile >> 4)), kd = k_desc + (uint64_t)(ks * (kKvTile >> 4));
               uint64_t *kf = &k_full[ks], *vf = &v_full[vs], *pf = &p_full[2 * g + place];
-              if (!bar_try(kf, kp)) bar_wait(kf, kp);
-              if (!bar_try(vf, vp)) bar_wait(vf, vp);
-              if (!bar_try(pf, (n_p >> 1) & 1u)) bar_wait(pf, (n_p >> 1) & 1u);
+              const bool k_in = bar_try(kf, kp) || bar_wait(kf, kp), v_in = bar_try(vf, vp) || bar_wait(vf, vp);
+              const bool p_in = bar_try(pf, (n_p >> 1) & 1u) || bar_wait(pf, (n_p >> 1) & 1u);
+              const bool in = k_in && v_in && p_in;
               tc_fence_after();
-              if (elect_one()) {
+              if (elect_one() && in) {
                 mma_pv(tm_o, tm_s + place * kN, vd, idesc_pv, true);
                 mma_commit(vf + kVS);    // v_free
                 mma_s(tm_s + place * kN, qd, kd, idesc_s);
@@ -796,10 +812,13 @@ __global__ void __launch_bounds__(kThreads, 1)
               vs = vw ? 0 : vs + 1;
               kp ^= kw ? 1u : 0u;
               vp ^= vw ? 1u : 0u;
+              ok = __all_sync(0xffffffffu, in);   // (behind the products: nothing waits for the vote)
+              if (!ok) break;
             }
-            if (i >= n) break;
+            if (!ok || i >= n) break;
           }
-          bar_wait(&v_full[vs], vp);
+          ok = warp_wait(&v_full[vs], vp);
+          if (!ok) break;
           const uint64_t vd = v_desc + (uint64_t)(vs * (kKvTile >> 4));
           const bool on = mine(i);
           if (on) {
@@ -807,7 +826,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool first = narrow ? i < 2 : i == ga;
             const bool last = narrow ? i + step >= n : i + 1 == ge;
             const bool last_but_one = !last && (narrow ? i + 2 * step >= n : i + 2 == ge);
-            bar_wait(&p_full[2 * g + place], (n_p >> 1) & 1u);
+            ok = warp_wait(&p_full[2 * g + place], (n_p >> 1) & 1u);
+            if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
               mma_pv(tm_o, tm_s + place * kN, vd, idesc_pv, !first);
@@ -827,6 +847,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (i + ahead < n) keys(i + ahead);
         }
       }
+      if (q_last) drain(q_last, q_last_phase);
+      if (n_s > 0) {
+        if (elect_one()) mma_commit(&drained[g]);
+        __syncwarp();
+        drain(&drained[g], 0);
+      }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
@@ -836,6 +862,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t tmem_g = tmem + lane_off + (uint32_t)g * kM, tmem_o = tmem + lane_off + (uint32_t)(2 + g) * kM;
     const float scale = kLog2e * rsqrtf((float)ZC_D);
     uint32_t tile0 = 0, n_s = 0, n_o = 0, n_last = 0, meetings = 0;
+    // Both groups meet over a narrow item: a hardware barrier, which cannot be given up.  So they first agree that all
+    // eight warps are here: whoever settles the count first, by the bounded wait's success or by its end, settles it for
+    // all (a warp that left, or whose wait ran out, is never waited for; ~0 stays).
+    auto groups_sync = [&]() { asm volatile("bar.sync 1, 256;\n" ::: "memory"); };
+    auto all_here = [&]() {
+      __syncwarp();
+      if (lane == 0) bar_arrive(meet_bar);
+      const bool here = bar_wait(meet_bar, meetings & 1u);
+      uint32_t to = here ? meetings + 1u : ~0u;
+      if (lane == 0) {
+        const uint32_t was = atomicCAS(meet_slot, meetings, to);
+        if (was != meetings) to = was;
+      }
+      return __shfl_sync(0xffffffffu, to, 0) == meetings + 1u;
+    };
     Item it;
     while (next_item(it)) {
       const int rows_at = it.narrow ? 0 : g;                         // which tile of rows
@@ -938,13 +979,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         ++n_o;
         tc_fence_after();
       }
-      const bool meet = it.narrow && it.t0 < it.t1;
-      const bool other = meet && it.t0 + 1 < it.t1;                  // group 1 has a share of a narrow item
+      bool meet = it.narrow && it.t0 < it.t1;
       float f_own = 1.f, f_other = 0.f;
+      if (meet && g == 1) s_ms[row] = make_float2(m_run, s_run);
+      if (meet) meet = all_here();
+      const bool other = meet && it.t0 + 1 < it.t1;                  // group 1 has a share of a narrow item
       if (meet) {
         // group 1's sums, and its O by halves, to group 0
-        if (g == 1) s_ms[row] = make_float2(m_run, s_run);
-        groups_sync();
         if (g == 0 && other) {
           const float2 o = s_ms[row];
           const float m = fmaxf(m_run, o.x);

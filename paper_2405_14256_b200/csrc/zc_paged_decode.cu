@@ -252,6 +252,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
   };
   const uint32_t ring = base_u + warp * kStages * 2 * kHalf;
   uint64_t* full = bars + warp * kStages;
+  bool ok = true;   // no wait of the warp has run out
   auto issue = [&](int stage) {
     if (pkey < 0) return;
     if (lane == 0) {
@@ -328,12 +329,13 @@ __global__ void __launch_bounds__(kDecThreads, 1)
       m[nt][0] = m[nt][1] = kNoMax;
       s[nt][0] = s[nt][1] = 0.f;
     }
-    for (int step = seg.a; step < seg.b; ++step) {
+    for (int step = seg.a; ok && step < seg.b; ++step) {
       const int vb = step * kDecWarps + warp;
       if (vb >= seg.q.s.nb) break;
       const int key0 = (vb < seg.q.s.nsb ? vb : seg.q.s.wb0 + vb - seg.q.s.nsb) << kBlkLog2;
       const uint32_t kt = ring + stage * 2 * kHalf, vt = kt + kHalf;
-      bar_wait(&full[stage], phase);
+      ok = warp_wait(&full[stage], phase);
+      if (!ok) break;   // nothing more is copied; the unit's other warps are met below
       // ---- S^T = K Q^T ----
       float sc[NT][4];
 #pragma unroll
@@ -546,6 +548,8 @@ __global__ void __launch_bounds__(kDecThreads, 1)
     unit0 += seg.steps;
     if (!seg_next(a, seg)) break;
   }
+  if (!ok)   // the copies that were on their way
+    for (int i = 0; i < kStages; ++i) drain(&full[i], i < stage ? phase ^ 1u : phase);
 }
 
 template <typename T, int NT>

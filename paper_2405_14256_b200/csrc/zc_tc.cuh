@@ -75,12 +75,17 @@ __device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-__device__ __forceinline__ void bar_wait(uint64_t* bar, uint32_t parity) {
+// True: the phase has completed.  False: the wait ran out, here or elsewhere.
+__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
   for (int spins = 0; !bar_try(bar, parity); ++spins) {
-    if (spins > kSpinLimit) { atomicExch(&g_zc_tc_error, 1); break; }
+    if (spins > kSpinLimit) {
+      atomicExch(&g_zc_tc_error, 1);
+      return false;
+    }
     // once a wait has run out somewhere the results are void: do not add to the delay
-    if ((spins & 1023) == 1023 && *reinterpret_cast<volatile int*>(&g_zc_tc_error)) break;
+    if ((spins & 1023) == 1023 && *reinterpret_cast<volatile int*>(&g_zc_tc_error)) return false;
   }
+  return true;
 }
 __device__ __forceinline__ void tmem_ld32_nowait(float* v, uint32_t taddr) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
