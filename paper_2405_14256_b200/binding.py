@@ -184,6 +184,46 @@ def _stream_of(device_index: int, stream) -> int:
     return _stream(stream)
 
 
+def _stream_object(device_index: int, raw: int):
+    """The torch.cuda.Stream of a raw handle."""
+    return torch.cuda.ExternalStream(raw, device_index) if raw else torch.cuda.default_stream(device_index)
+
+
+def _new(shape, dtype, device, stream):
+    """A tensor that a kernel on `stream` writes and the current stream's work will read: it comes from that stream's
+    memory, and is not given to another before the current stream's work so far is done when it is freed."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    device = _cuda_device(device)
+    current = torch.cuda.current_stream(device)
+    if _stream(stream) == current.cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(_stream_object(device.index, _stream(stream))):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(current)
+    return t
+
+
+class _Buffers:
+    """Buffers that an object keeps for its calls, whatever stream a call runs on."""
+
+    def _keep(self, *buffers):
+        """Called once they are made: whatever their memory was used for on the current stream, and their first
+        fill, is over before a call on any stream can touch them.  (Made under capture, they belong to that graph.)"""
+        self._kept = buffers
+        self._home = _raw_stream(self._index) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+        self._others = set()
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().synchronize()
+
+    def _used_on(self, raw: int):
+        """A call runs on a stream that is not the buffers' own: freed, they wait for its work so far."""
+        if raw not in self._others:
+            self._others.add(raw)
+            for t in self._kept:
+                t.record_stream(_stream_object(self._index, raw))
+
+
 def zc_strerror(status: int) -> str:
     return lib().zc_strerror(status).decode()
 
@@ -414,17 +454,21 @@ def _cuda_device(device) -> torch.device:
     return torch.device("cuda", torch.cuda.current_device() if device.index is None else device.index)
 
 
-class StepTables:
+class StepTables(_Buffers):
     """The buffers of one serving step's lengths and slots (zc_page_tables): kv_len [n_req],
-    row_start [n_req + 1], slots and pos [n_rows], free_state [3], all int32.  Reused from step to
-    step; two steps whose free_state feeds the next one's take two of these in turn."""
+    row_start [n_req + 1], slots and pos [n_rows], free_state [3], all int32, undefined before the
+    first build.  Made once (the constructor waits for the current stream's work) and reused from step to
+    step; two steps whose free_state feeds the next one's take two of these in turn.  build may run on any
+    stream; readers on another one are ordered behind it by the caller."""
 
     def __init__(self, n_req: int, n_rows: int, device="cuda:0"):
         self.device = _cuda_device(device)
         self.n_req, self.n_rows, self._index = n_req, n_rows, self.device.index
-        new = lambda n: torch.zeros(n, dtype=torch.int32, device=self.device)  # noqa: E731
-        self.kv_len, self.row_start, self.slots, self.pos = new(n_req), new(n_req + 1), new(n_rows), new(n_rows)
-        self.free_state = new(3)
+        new = lambda n: torch.empty(n, dtype=torch.int32, device=self.device)  # noqa: E731
+        with torch.cuda.device(self._index):
+            self.kv_len, self.row_start, self.slots, self.pos = new(n_req), new(n_req + 1), new(n_rows), new(n_rows)
+            self.free_state = new(3)
+            self._keep(self.kv_len, self.row_start, self.slots, self.pos, self.free_state)
 
     def build(self, page_size: int, past, fresh, free_pages, free_state, table, stream=None) -> "StepTables":
         """past, fresh [n_req], free_pages [any], free_state [3] (next, end, -) and table [n_req, width]
@@ -439,20 +483,25 @@ class StepTables:
         _want_i32(free_state, "free_state", 3, self._index)
         width = table.shape[-1]
         _want_i32(table, "table", n * width, self._index)
+        raw = _stream_of(self._index, stream)
+        if raw != self._home:
+            self._used_on(raw)
         _check(lib().zc_page_tables(page_size, n, past.data_ptr(), fresh.data_ptr(), free_pages.data_ptr(),
                                     free_pages.numel(), free_state.data_ptr(), table.data_ptr(), width,
                                     self.kv_len.data_ptr(), self.row_start.data_ptr(), self.n_rows,
-                                    self.slots.data_ptr(), self.pos.data_ptr(), self.free_state.data_ptr(),
-                                    _stream_of(self._index, stream)), "zc_page_tables")
+                                    self.slots.data_ptr(), self.pos.data_ptr(), self.free_state.data_ptr(), raw),
+               "zc_page_tables")
         return self
 
 
-class PagedKV:
+class PagedKV(_Buffers):
     """Keys and values at full precision in pages: a handle over the caller's tensors, both
     [n_pages, page_size, n_kv_heads, 128] with any strides of the first three dimensions (for pages
     stored [n_pages, n_kv_heads, page_size, 128] pass .transpose(1, 2)).  Holds the workspace of
     attention calls of up to max_req requests and max_rows rows; one that is given (to share it among
-    the handles of a stream) must have its first ZC_PAGES_SYNC_BYTES zeroed once."""
+    the handles of a stream) must have its first ZC_PAGES_SYNC_BYTES zeroed once.  A handle's calls may run on
+    any stream (the constructor waits for the current one's work), attention calls on one at a time.  Tensors
+    that a call allocates may be used on the current stream, behind what orders it after `stream`."""
 
     def __init__(self, k_pages, v_pages, n_q_heads: int, max_req: int = 256, max_rows: int = 8192,
                  workspace: Optional[torch.Tensor] = None):
@@ -472,8 +521,9 @@ class PagedKV:
         self._index = self.device.index
         self.workspace_bytes = zc_pages_workspace(self.cfg, max_req, max_rows)
         if workspace is None:
-            workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
-            workspace[:ZC_PAGES_SYNC_BYTES].zero_()
+            with torch.cuda.device(self._index):
+                workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
+                workspace[:ZC_PAGES_SYNC_BYTES].zero_()
         _want_on(workspace, "workspace", self._index)
         if not workspace.is_contiguous():
             raise ZipCacheError("the workspace must be contiguous")
@@ -482,6 +532,7 @@ class PagedKV:
             raise ZipCacheError("shared workspace too small")
         self.workspace = workspace
         with torch.cuda.device(self._index):
+            self._keep(workspace)
             self.handle = zc_pages_init(k_pages, v_pages, self.cfg)
 
     def close(self):
@@ -523,8 +574,8 @@ class PagedKV:
                 return self.read(table, l, K, V, stream)
         _want(table, "table", (table.shape[0], table.shape[-1]), torch.int32)
         shape = (table.shape[0], self.n_kv_heads, l, 128)
-        K = torch.empty(shape, dtype=self.dtype, device=self.device) if K is None else K
-        V = torch.empty(shape, dtype=self.dtype, device=self.device) if V is None else V
+        K = _new(shape, self.dtype, self.device, stream) if K is None else K
+        V = _new(shape, self.dtype, self.device, stream) if V is None else V
         _want(K, "K", shape, self.dtype, contiguous=False)
         _want(V, "V", shape, self.dtype, contiguous=False)
         for t, name in ((table, "table"), (K, "K"), (V, "V")):
@@ -550,21 +601,25 @@ class PagedKV:
         width = table.shape[-1]
         _want_i32(table, "table", n_req * width, self._index)
         if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format) if stream is None else \
+                _new(q.shape, q.dtype, self.device, stream)
         else:
             self._rows(out, "out", n, heads)
             if not out.is_contiguous():
                 raise ZipCacheError("out must be contiguous")
         if row_lse is None:
-            row_lse = torch.empty((n, heads), dtype=torch.float32, device=self.device)
+            row_lse = _new((n, heads), torch.float32, self.device, stream)
         else:
             if row_lse.dtype is not torch.float32 or row_lse.numel() != n * heads or not row_lse.is_contiguous():
                 _want(row_lse, "row_lse", (n, heads), torch.float32)
             _want_on(row_lse, "row_lse", self._index)
+        raw = _stream_of(self._index, stream)
+        if raw != self._home:
+            self._used_on(raw)
         _check(lib().zc_paged_attention(self.handle, q.data_ptr(), _strides2(strides[0], strides[1]), table.data_ptr(), width,
                                         row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
                                         out.data_ptr(), row_lse.data_ptr(), self.workspace.data_ptr(), self._ws_bytes,
-                                        _stream_of(self._index, stream)), "zc_paged_attention")
+                                        raw), "zc_paged_attention")
         return out, row_lse
 
 
@@ -642,8 +697,8 @@ class ZipCache:
     def prefill_attention(self, Q, K, V, stream=None):
         """Causal attention output O and the rows' log-sum-exp (Alg. 2's attention-output line)."""
         l = K.shape[2]
-        O = torch.empty((self.batch, self.n_q_heads, l, 128), dtype=self.dtype, device=self.device)
-        lse = torch.empty((self.batch, self.n_q_heads, l), dtype=torch.float32, device=self.device)
+        O = _new((self.batch, self.n_q_heads, l, 128), self.dtype, self.device, stream)
+        lse = _new((self.batch, self.n_q_heads, l), torch.float32, self.device, stream)
         zc_prefill_attention(self.handle, Q, K, V, l, O, lse, stream)
         return O, lse
 
@@ -661,9 +716,9 @@ class ZipCache:
             if t.stride(3) != 1:
                 raise ZipCacheError(f"{name}: the channels of a row must be contiguous")
         if out is None:
-            out = torch.empty((self.batch, self.n_q_heads, l, 128), dtype=self.dtype, device=self.device)
+            out = _new((self.batch, self.n_q_heads, l, 128), self.dtype, self.device, stream)
         if row_lse is None:
-            row_lse = torch.empty((self.batch, self.n_q_heads, l), dtype=torch.float32, device=self.device)
+            row_lse = _new((self.batch, self.n_q_heads, l), torch.float32, self.device, stream)
         _want(out, "out", (self.batch, self.n_q_heads, l, 128), self.dtype)
         _want(row_lse, "row_lse", (self.batch, self.n_q_heads, l), torch.float32)
         _want_on(out, "out", index)
@@ -679,7 +734,7 @@ class ZipCache:
 
     def decode_attention(self, q, is_probe_step=False, out=None, stream=None):
         if out is None:
-            out = torch.empty(q.shape, dtype=self.out_dtype, device=q.device)
+            out = _new(q.shape, self.out_dtype, q.device, stream)
         zc_decode_attention(self.handle, q, out, is_probe_step, self.workspace, stream)
         return out
 

@@ -84,3 +84,110 @@ def test_the_same_bits_whatever_ran_before(zc, hq, hkv):
         o, l = pool.attention(*args)
         settled(zc)
         assert torch.equal(o, out) and torch.equal(l, lse), fill
+
+
+# ---------------------------------------------------------------- streams
+def busy(stream, ms=40):
+    """Keeps a stream occupied for some time."""
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(int(ms * 1.9e6))
+
+
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_the_first_call_on_another_stream_than_the_constructor_s(zc, own_stream):
+    """The construction stream has long work in flight; a call at once on another stream, current or passed, must not
+    meet counters that are not zero yet nor have its tables overwritten."""
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    new, lengths = [1, 1, 1], [4000, 3000, 50]
+    k, v = ref.make_pages(gen, 450, 16, 2, torch.float16, False, DEV)
+    q = torch.randn(3, 8, D, generator=gen, device=DEV).half()
+    free, table = i32(np.random.RandomState(1).permutation(450)), i32(np.full((3, 250), -1))
+    past, fresh, state = i32([n - 1 for n in lengths]), i32(new), i32([0, 450, 0])
+    zeros = i32([0] * 3)
+    first = zc.StepTables(3, sum(lengths))
+    first.build(16, zeros, past, free, state, table)               # the cached tokens' pages
+    state = first.free_state.clone()
+    plain, step = zc.PagedKV(k, v, 8, max_req=3, max_rows=3), zc.StepTables(3, 3)
+    step.build(16, past, fresh, free, state, table)
+    out, lse = plain.attention(q, table, step.row_start, step.kv_len, 1)
+    settled(zc)
+    # memory of the workspace's and the tables' sizes holds something else than zeros when it is taken again
+    junk = [torch.full((plain.workspace_bytes,), 0xFF, dtype=torch.uint8, device=DEV)] + [
+        torch.full((n,), -1, dtype=torch.int32, device=DEV) for n in (3, 4, 3, 3, 3)]
+    want = [t.clone() for t in (step.kv_len, step.row_start, step.slots, step.pos, step.free_state)]
+    del plain, junk
+    torch.cuda.synchronize()
+    home, side = torch.cuda.Stream(), torch.cuda.Stream()
+    busy(home)
+    with torch.cuda.stream(home):
+        pool, other = zc.PagedKV(k, v, 8, max_req=3, max_rows=3), zc.StepTables(3, 3)
+        if own_stream:
+            other.build(16, past, fresh, free, state, table, stream=side)
+            o, l = pool.attention(q, table, other.row_start, other.kv_len, 1, stream=side)
+    if not own_stream:
+        with torch.cuda.stream(side):
+            other.build(16, past, fresh, free, state, table)
+            o, l = pool.attention(q, table, other.row_start, other.kv_len, 1)
+    settled(zc)
+    for got, w in zip((other.kv_len, other.row_start, other.slots, other.pos, other.free_state), want):
+        assert torch.equal(got, w)
+    assert torch.equal(o, out) and torch.equal(l, lse)
+
+
+def test_allocated_outputs_belong_to_the_stream_that_writes_them(zc):
+    """Memory that the current stream still uses, or will hand out again at once, is not what a call on another
+    stream writes to."""
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    pool, table = pool_of(zc, gen, torch.float16, 8, 2, 16, [900, 40], 8)
+    q = torch.randn(4, 8, D, generator=gen, device=DEV).half()
+    cache = zc.ZipCache(torch.float16, 1, 8, 2, 64, 1, 0.4, device=DEV)
+    x = torch.randn(1, 12, 64, D, generator=gen, device=DEV).half()
+    calls = {
+        "attention": lambda **kw: pool.attention(q, table, i32([0, 2, 4]), i32([900, 40]), 2, **kw),
+        "read": lambda **kw: pool.read(table, 40, **kw),
+        "window": lambda **kw: cache.prefill_attention_window(x[:, :8], x[:, 8:10], x[:, 10:], 9, **kw),
+        "prompt": lambda **kw: cache.prefill_attention(x[:, :8], x[:, 8:10], x[:, 10:], **kw),
+    }
+    side = torch.cuda.Stream()
+    for name, call in calls.items():
+        plain = [t.clone() for t in call()]
+        torch.cuda.synchronize()
+        held = [torch.empty_like(t) for t in plain]
+        places = {t.data_ptr() for t in held}
+        busy(torch.cuda.current_stream(), 20)
+        for t in held:
+            t.fill_(3.0)
+        del held, t                       # free for the current stream, whose fill is still to come
+        got = call(stream=side)
+        assert not places & {t.data_ptr() for t in got}, name
+        torch.cuda.synchronize()
+        for g, w in zip(got, plain):
+            assert torch.equal(g, w), name
+        busy(side, 20)
+        got = call(stream=side)
+        places = {t.data_ptr() for t in got}
+        del got, g                        # freed while the side stream has yet to write them
+        held = [torch.empty_like(t) for t in plain]
+        assert not places & {t.data_ptr() for t in held}, name
+        torch.cuda.synchronize()
+        del held
+    settled(zc)
+
+
+def test_a_dropped_handle_s_workspace_waits_for_the_streams_that_used_it(zc):
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    pool, table = pool_of(zc, gen, torch.float16, 8, 2, 16, [900, 40], 8)
+    q = torch.randn(4, 8, D, generator=gen, device=DEV).half()
+    step = zc.StepTables(2, 4)
+    args = (q, table, i32([0, 2, 4]), i32([900, 40]), 2)
+    some = (i32([898, 38]), i32([2, 2]), i32([0]), i32([0, 0, 0]), table.clone())
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    busy(side)
+    pool.attention(*args, stream=side)
+    step.build(16, *some, stream=side)
+    size, at, slots = pool.workspace_bytes, pool.workspace.data_ptr(), step.slots.data_ptr()
+    del pool, step
+    again = [torch.empty(size, dtype=torch.uint8, device=DEV), torch.empty(4, dtype=torch.int32, device=DEV)]
+    assert again[0].data_ptr() != at and again[1].data_ptr() != slots
+    settled(zc)
