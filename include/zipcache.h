@@ -291,7 +291,8 @@ typedef struct {
                              the three is accepted. */
 } zc_page_config;
 
-typedef struct zc_pages zc_pages; /* small host-side handle */
+typedef struct zc_pages zc_pages; /* small host-side handle; several host threads may use one at the same time (with
+                                     workspaces and streams of their own), until zc_pages_free */
 
 /* Device scratch [host] that zc_paged_attention needs for calls of up to n_req requests and n_rows rows
  * (partial results of rows whose keys several CTAs share).  ZC_ECAPACITY when one call cannot take so many:

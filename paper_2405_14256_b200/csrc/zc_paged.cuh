@@ -75,6 +75,19 @@ inline bool zc_encode_map(CUtensorMap* map, int dtype, int rank, const void* at,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The opt-in to large shared memory, once per device (a bit of `allowed`) and kernel; any host thread may come first.
+template <typename Kernel>
+cudaError_t zc_allow_smem(Kernel kernel, int bytes, std::atomic<unsigned long long>* allowed) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (dev < 64 && (allowed->load(std::memory_order_acquire) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev < 64) allowed->fetch_or(bit, std::memory_order_release);
+  return e;
+}
+
 // Kernels of this file's users come one behind the other, many of them of a few microseconds: each is launched while
 // the one before still runs, and waits, before its first access to global memory, until that one has completed
 // (their inputs are not declared __restrict__: a read of constant memory might be moved ahead of the wait).

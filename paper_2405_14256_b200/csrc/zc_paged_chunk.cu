@@ -1175,15 +1175,9 @@ size_t carve(char* ws, ChunkWs* out) {
 }
 
 template <typename T, bool PAGED>
-cudaError_t ready() {   // the shared memory the kernel asks for, once per device
-  static bool once[64] = {};
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev >= 0 && dev < 64 && once[dev]) return cudaSuccess;
-  e = cudaFuncSetAttribute(k_chunk_attention<T, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-  if (e == cudaSuccess && dev >= 0 && dev < 64) once[dev] = true;
-  return e;
+cudaError_t ready() {   // the shared memory the kernel asks for
+  static std::atomic<unsigned long long> allowed{0};
+  return zc_allow_smem(k_chunk_attention<T, PAGED>, kSmem, &allowed);
 }
 
 // Q as (channels, query heads, tokens, batch rows), boxes of 64 channels x G heads x tpt tokens.

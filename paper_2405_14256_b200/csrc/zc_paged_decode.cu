@@ -554,15 +554,9 @@ __global__ void __launch_bounds__(kDecThreads, 1)
 
 template <typename T, int NT>
 int launch(zc_pages* p, const ZcPagedArgs& a, float* parts, unsigned* arrived, cudaStream_t st) {
-  static bool once[64] = {};   // per device: the attribute belongs to the device's copy of the kernel
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  static std::atomic<unsigned long long> allowed{0};
+  cudaError_t e = zc_allow_smem(k_paged_decode<T, NT>, kDecSmem, &allowed);
   if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= 64 || !once[dev]) {
-    e = cudaFuncSetAttribute(k_paged_decode<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDecSmem);
-    if (e != cudaSuccess) return e;
-    if (dev >= 0 && dev < 64) once[dev] = true;
-  }
   e = zc_launch_early(k_paged_decode<T, NT>, dim3(p->n_sm), dim3(kDecThreads), kDecSmem, st, a, parts, arrived, p->k16, p->v16);
   if (e != cudaSuccess) return e;
   p->launches += 1;
@@ -587,7 +581,9 @@ int zc_launch_paged_decode(zc_pages* p, const ZcPagedArgs& a, char* ws, cudaStre
 
 // Tensor maps of the pages: (64 channels, token of the page, half of the channels, KV head, page).
 bool zc_page_maps(zc_pages* p) {
-  if (p->maps_ready) return true;
+  if (p->maps_ready.load(std::memory_order_acquire)) return true;
+  std::lock_guard<std::mutex> lock(p->maps_guard);
+  if (p->maps_ready.load(std::memory_order_relaxed)) return true;   // another thread's first call
   const int64_t* s = p->cfg.strides;
   const cuuint64_t dims[5] = {64, (cuuint64_t)p->cfg.page_size, 2, (cuuint64_t)p->cfg.n_kv_heads,
                               (cuuint64_t)p->cfg.n_pages};
@@ -600,7 +596,7 @@ bool zc_page_maps(zc_pages* p) {
       {&p->k16, p->k, small}, {&p->v16, p->v, small}, {&p->k64, p->k, large}, {&p->v64, p->v, large}};
   for (auto& t : todo)
     if (!zc_encode_map(t.map, p->cfg.dtype, 5, t.at, dims, strides, t.box)) return false;
-  p->maps_ready = true;
+  p->maps_ready.store(true, std::memory_order_release);
   return true;
 }
 

@@ -1,6 +1,5 @@
 // Full-precision pages: host API (argument checks, handle), block tables and slot maps from request
 // lengths, and the copies between dense rows and pages.
-#include <string.h>
 #include <new>
 #include "zc_paged.cuh"
 
@@ -268,7 +267,6 @@ int zc_pages_init(void* k_pages, void* v_pages, const zc_page_config* cfg, zc_pa
   if (!aligned16(k_pages) || !aligned16(v_pages)) return ZC_EALIGN;
   zc_pages* p = new (std::nothrow) zc_pages();
   if (!p) return ZC_EINVAL;
-  memset(p, 0, sizeof(*p));
   p->cfg = *cfg;
   // an extent of 1 may come with any stride: the tensor maps want one that is valid
   const long long extent[3] = {cfg->n_pages, cfg->page_size, cfg->n_kv_heads};
@@ -290,7 +288,7 @@ int zc_pages_init(void* k_pages, void* v_pages, const zc_page_config* cfg, zc_pa
 
 void zc_pages_free(zc_pages* p) { delete p; }
 
-int64_t zc_pages_launch_count(const zc_pages* p) { return p ? p->launches : 0; }
+int64_t zc_pages_launch_count(const zc_pages* p) { return p ? p->launches.load() : 0; }
 
 int zc_page_tables(int page_size, int n_req, const int32_t* past, const int32_t* fresh, const int32_t* free_pages,
                    int n_free, const int32_t* free_state, int32_t* table, int table_width, int32_t* kv_len,

@@ -2,6 +2,8 @@
 // given, and the arithmetic of visible keys that the host, the planner and the kernels share.
 #pragma once
 #include <cuda.h>
+#include <atomic>
+#include <mutex>
 #include "zc_internal.h"
 
 #define ZC_PAGE_MAX_G 16            // most query heads per KV head
@@ -9,15 +11,17 @@
 #define ZC_PAGED_MAX_CTAS 160       // CTAs the workspace is sized for
 #define ZC_NO_WINDOW (1 << 30)      // positions stay below it
 
+// Several host threads may call with one handle.  The tensor maps are made by the first call that needs them.
 struct zc_pages {
   zc_page_config cfg;
   char* k;
   char* v;
   int G, page_log2, n_sm;
-  bool maps_ready;
+  std::atomic<bool> maps_ready;
+  std::mutex maps_guard;
   CUtensorMap k16, v16;    // boxes of 16 tokens x 128 elements (two 128-byte halves)
   CUtensorMap k64, v64;    // boxes of min(page, 64) tokens x 64 elements (x 2 halves from 64 on)
-  long long launches;
+  std::atomic<long long> launches;
 };
 
 // One attention call, as the kernels see it.

@@ -191,3 +191,44 @@ def test_a_dropped_handle_s_workspace_waits_for_the_streams_that_used_it(zc):
     again = [torch.empty(size, dtype=torch.uint8, device=DEV), torch.empty(4, dtype=torch.int32, device=DEV)]
     assert again[0].data_ptr() != at and again[1].data_ptr() != slots
     settled(zc)
+
+
+def test_first_calls_of_several_threads_on_one_handle(zc):
+    """The handle's tensor maps are made by whichever call comes first; each thread has a stream and a workspace."""
+    from concurrent.futures import ThreadPoolExecutor
+    from threading import Barrier
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    n, gate, lib = 4, Barrier(4), zc.lib()
+    table, n_pages = ref.make_table(np.random.RandomState(9), [300, 40], 16)
+    k, v = ref.make_pages(gen, n_pages, 16, 2, torch.float16, False, DEV)
+    table = i32(table)
+    q = torch.randn(42, 8, D, generator=gen, device=DEV).half()
+    steps = [(i32([0, 1, 2]), 1), (i32([0, 30, 42]), 30)]
+    lengths = i32([300, 40])
+    plain = zc.PagedKV(k, v, 8, max_req=2, max_rows=42)
+    want = [plain.attention(q, table, rs, lengths, m) for rs, m in steps]
+    streams = [torch.cuda.Stream() for _ in range(n)]
+    works = [torch.zeros_like(plain.workspace) for _ in range(n)]
+    settled(zc)
+
+    def first(i, pool):
+        rs, m = steps[i % 2]
+        out, lse = torch.zeros_like(q), torch.zeros(42, 8, device=DEV)
+        torch.cuda.synchronize()
+        gate.wait()
+        from paper_2405_14256_b200 import binding
+        code = lib.zc_paged_attention(pool.handle, q.data_ptr(), binding._strides2(8 * D, D), table.data_ptr(), table.shape[1],
+                                      rs.data_ptr(), lengths.data_ptr(), 2, 42, m, 0, 0, out.data_ptr(), lse.data_ptr(),
+                                      works[i].data_ptr(), works[i].numel(), streams[i].cuda_stream)
+        streams[i].synchronize()
+        return code, out, lse
+
+    with ThreadPoolExecutor(n) as threads:
+        for _ in range(25):
+            pool = zc.PagedKV(k, v, 8, max_req=2, max_rows=42, workspace=works[0])
+            for i, (code, out, lse) in enumerate(threads.map(lambda i: first(i, pool), range(n))):
+                rows = int(steps[i % 2][0][2])
+                assert code == 0
+                assert torch.equal(out[:rows], want[i % 2][0][:rows]) and torch.equal(lse[:rows], want[i % 2][1][:rows])
+            assert zc.zc_pages_launch_count(pool.handle) == 2 * 1 + 2 * 2
+    settled(zc)
