@@ -1,6 +1,7 @@
 // Device helpers that the paged attention kernels share: tensor-map copies of page rows, output rows,
 // the joining of partial results, and launches that may start beside the kernel they follow.
 #pragma once
+#include <cfloat>
 #include "zc_pages.h"
 #include "zc_tc.cuh"
 
@@ -23,6 +24,11 @@ static_assert(ZC_PAGED_MAX_CTAS < 256, "a * b < 2^32");
 __device__ __forceinline__ long long zc_muldiv(int a, long long b, int c) {
   return b < (1 << 24) ? (long long)((uint32_t)a * (uint32_t)b / (uint32_t)c) : a * b / c;
 }
+
+constexpr float kNoMax = -FLT_MAX;                     // running maximum before any key
+// The weights' exponents are (q.k) * scale - m, m the scaled maximum rounded to fp32: off by 2^-24 of m, for all of a row's keys
+// alike, which cancels up to here (a shift of 4 at most).  Beyond, the maximum's own q.k is taken off before the scaling.
+constexpr float kFarMax = 67108864.f;
 
 // bar_wait of a whole warp, with one answer for all lanes: a lane whose wait ran out must not part from the others.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {

@@ -52,7 +52,6 @@ constexpr int kTiles = 2 * kTile + (kKS + kVS) * kKvTile + 8 * kOutTile;   // 22
 constexpr int kRingN = 2;                             // items fetched ahead
 constexpr int kRingInts = 24;
 constexpr int kSmem = kTiles + 1024 + 448 + 1024 + kRingN * kRingInts * 4;   // alignment, barriers, (m, sum) of group 1
-constexpr float kNoMax = -1e30f;                      // running maximum before any key
 constexpr float kTau = 3.f;                           // a new maximum is taken where it exceeds the old by this (base 2)
 constexpr float kBigSum = 1024.f;                     // ... and looked for where a tile's weights sum to more than this
 constexpr int kItemRows = 2 * kM;
@@ -888,7 +887,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int ga = g ? it.ga[1] : it.ga[0], ge = g ? it.ge[1] : it.ge[0];
       const int step = it.narrow ? 2 : 1, t_first = it.narrow ? it.t0 + g : ga;
       float m_run = kNoMax, s_run = 0.f;
-      bool unset = true;                                             // a row of the warp has seen no key yet
+      bool unset = true;     // a row of the warp has seen no key yet, or has its maximum beyond kFarMax
       for (int t = t_first; t < ge; t += step) {
         const int key0 = it.key0(t);
         const uint32_t place = n_s & 1u, tmem_s = tmem_g + place * kN;
@@ -938,7 +937,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int e = 4; e < kN; e += 8)
 #pragma unroll
             for (int i = 0; i < 4; ++i) mx4[i] = e + 4 < kN ? max3(mx4[i], v[e + i], v[e + 4 + i]) : fmaxf(mx4[i], v[e + i]);
-          const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * scale;
+          const float top = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]), mx = top * scale;
           const bool grow = valid && mx > m_run + kTau;
           if (__any_sync(0xffffffffu, grow)) {
             const float alpha = grow ? zc_exp2(m_run - mx) : 1.f;
@@ -960,8 +959,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             s_run *= alpha;
             if (grow) m_run = mx;
           }
-          unset = __any_sync(0xffffffffu, valid && m_run == kNoMax);
-          sum = weights<T>(v, scale, m_run, w);
+          unset = __any_sync(0xffffffffu, valid && !(fabsf(m_run) < kFarMax));
+          float less = m_run;
+          if (unset && __any_sync(0xffffffffu, valid && !(fabsf(m_run) < kFarMax) && m_run != kNoMax)) {
+            // the maximum's q.k waits where outputs leave from
+            if (valid && !(fabsf(m_run) < kFarMax) && m_run != kNoMax) {
+              float* keep = reinterpret_cast<float*>(base + 2 * kTile + (kKS + kVS) * kKvTile + (warp - 4) * kOutTile) + lane;
+              if (grow) *keep = top;
+#pragma unroll
+              for (int e = 0; e < kN; ++e) v[e] -= *keep;
+              less = 0.f;
+            }
+          }
+          sum = weights<T>(v, scale, less, w);
         }
         tmem_st32(w, tmem_s);
         asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");

@@ -40,7 +40,6 @@ constexpr int kDecSmem = kRing + kJoinBytes + kDecWarps * kStages * 8 + kScanByt
 // and no piece is shorter than half a share or 3 steps (one request of 8000 tokens: 14.7 us, else 19.2).
 constexpr int kWhole = 5;
 constexpr int kLeast = 3;
-constexpr float kNoMax = -1e30f;                       // running maximum before any key
 static_assert(ZC_PAGED_MAX_CTAS * 4 <= ZC_PAGES_SYNC_BYTES, "a counter per CTA");
 constexpr float kTau = 8.f;
 
@@ -319,7 +318,8 @@ __global__ void __launch_bounds__(kDecThreads, 1)
         pos[nt][e] = row < rows ? seg.q.p0 + row / a.G : -1;
       }
     const int p_last = seg.q.p0 + seg.q.n - 1;
-    float o[NT][8][4], m[NT][2], s[NT][2];
+    float o[NT][8][4], m[NT][2], s[NT][2], raw[NT][2];   // raw: q.k of the maximum
+    bool far = false;                                    // a row of the warp has its maximum beyond kFarMax
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -327,6 +327,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
       m[nt][0] = m[nt][1] = kNoMax;
+      raw[nt][0] = raw[nt][1] = 0.f;
       s[nt][0] = s[nt][1] = 0.f;
     }
     for (int step = seg.a; ok && step < seg.b; ++step) {
@@ -379,15 +380,21 @@ __global__ void __launch_bounds__(kDecThreads, 1)
         float mx[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          mx[e] = fmaxf(sc[nt][e], sc[nt][e + 2]) * scale;
+          mx[e] = fmaxf(sc[nt][e], sc[nt][e + 2]);
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], x));
         }
+        const float top[2] = {mx[0], mx[1]};
+        mx[0] *= scale;
+        mx[1] *= scale;
         const bool grow0 = mx[0] > m[nt][0] + kTau, grow1 = mx[1] > m[nt][1] + kTau;
         if (__any_sync(0xffffffffu, grow0 || grow1)) {
           const float al0 = grow0 ? zc_exp2(m[nt][0] - mx[0]) : 1.f, al1 = grow1 ? zc_exp2(m[nt][1] - mx[1]) : 1.f;
           if (grow0) m[nt][0] = mx[0];
           if (grow1) m[nt][1] = mx[1];
+          if (grow0) raw[nt][0] = top[0];
+          if (grow1) raw[nt][1] = top[1];
+          far = far || __any_sync(0xffffffffu, !(fmaxf(grow0 ? fabsf(mx[0]) : 0.f, grow1 ? fabsf(mx[1]) : 0.f) < kFarMax));
           s[nt][0] *= al0;
           s[nt][1] *= al1;
 #pragma unroll
@@ -398,8 +405,14 @@ __global__ void __launch_bounds__(kDecThreads, 1)
             o[nt][i][3] *= al1;
           }
         }
-        const float p0 = zc_exp2(fmaf(sc[nt][0], scale, -m[nt][0])), p1 = zc_exp2(fmaf(sc[nt][1], scale, -m[nt][1]));
-        const float p2 = zc_exp2(fmaf(sc[nt][2], scale, -m[nt][0])), p3 = zc_exp2(fmaf(sc[nt][3], scale, -m[nt][1]));
+        float less[2] = {m[nt][0], m[nt][1]};
+        if (far) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[nt][e] -= raw[nt][e & 1];
+          less[0] = less[1] = 0.f;
+        }
+        const float p0 = zc_exp2(fmaf(sc[nt][0], scale, -less[0])), p1 = zc_exp2(fmaf(sc[nt][1], scale, -less[1]));
+        const float p2 = zc_exp2(fmaf(sc[nt][2], scale, -less[0])), p3 = zc_exp2(fmaf(sc[nt][3], scale, -less[1]));
         s[nt][0] += p0 + p2;
         s[nt][1] += p1 + p3;
         pf[nt][0] = movmatrix_trans(pack2<T>(p0, p1));    // keys 0-7 of the block

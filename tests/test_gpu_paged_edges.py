@@ -232,3 +232,47 @@ def test_first_calls_of_several_threads_on_one_handle(zc):
                 assert torch.equal(out[:rows], want[i % 2][0][:rows]) and torch.equal(lse[:rows], want[i % 2][1][:rows])
             assert zc.zc_pages_launch_count(pool.handle) == 2 * 1 + 2 * 2
     settled(zc)
+
+
+# ---------------------------------------------------------------- logits that are not mild
+@pytest.mark.parametrize("new", [1, 4, 60])
+@pytest.mark.parametrize("dtype,power,sign", [("bf16", 55, -1), ("bf16", 59, -1), ("bf16", 55, 1), ("bf16", 16, -1),
+                                              ("fp16", 14, -1), ("fp16", 14, 1), ("fp16", 11, 1)])
+def test_rows_whose_logits_are_all_far_from_zero(zc, dtype, power, sign, new):
+    """fp16 reaches logits of 2e9 and bf16 of 1e34.  Keys are so far apart then that nearly always a row's weight lies on
+    its largest logit alone: the output is that value, and the log-sum-exp is that logit.
+    From logits of 2^26 on the largest one's weight is 2^0 and the output exact.  Below, it is 2^x with x the rounding
+    of the maximum, so that the weight is off by u, half a step of the type, against the sum (fp32: 2^-20 with the
+    division), and the output is rounded once more: (1 + u)^2 (1 + 2^-20) - 1 of its size, 2^-25 where fp16 is not normal."""
+    dt, lengths = TYPES[dtype], [1500, 700]
+    u = torch.finfo(dt).eps / 2
+    gen = torch.Generator(device=DEV).manual_seed(power + new)
+    table, n_pages = ref.make_table(np.random.RandomState(power), lengths, 16)
+    size = lambda *shape: torch.rand(shape, generator=gen, device=DEV) * 0.5 + 0.5  # noqa: E731
+    k = (sign * size(n_pages, 16, 2, D) * 2.0 ** power).to(dt)
+    v = torch.randn(n_pages, 16, 2, D, generator=gen, device=DEV).to(dt)
+    q = (size(2 * new, 8, D) * 2.0 ** power).to(dt)
+    pool = zc.PagedKV(k, v, 8, max_req=2, max_rows=2 * new)
+    out, lse = pool.attention(q, i32(table), i32([0, new, 2 * new]), i32(lengths), new)
+    settled(zc)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    checked = 0
+    for r, n in enumerate(lengths):
+        kk, vv = ref.rows_of_request(k, v, table[r], n)
+        for h in range(8):
+            logit = q[r * new:(r + 1) * new, h].double() @ kk[:, h // 4].double().T * (math.log2(math.e) / math.sqrt(D))
+            assert (sign * logit).min() > 2.0 ** (2 * power) * 2
+            hidden = torch.arange(n, device=DEV)[None] > torch.arange(n - new, n, device=DEV)[:, None]
+            two, at = logit.masked_fill(hidden, -math.inf).topk(2, dim=1)
+            # an fp32 logit is off by 136 * 2^-24 of its size (all terms have one sign): rows where the two largest
+            # are further apart than twice that have one answer
+            off = 136 * 2.0 ** -24 * two[:, 0].abs()
+            sure = two[:, 0] - two[:, 1] > 2 * off + 64
+            checked += int(sure.sum())
+            rows = slice(r * new, (r + 1) * new)
+            got, want = out[rows, h][sure].double(), vv[at[:, 0], h // 4][sure].double()
+            far = two[sure, 0].abs()[:, None] > 2.0 ** 26 * (1 + 2.0 ** -10)
+            slack = (2 * u + u * u + 2.0 ** -19) * want.abs() + 2.0 ** -25
+            assert ((got - want).abs() <= torch.where(far, torch.zeros_like(slack), slack)).all()
+            assert ((lse[rows, h].double() - two[:, 0]).abs() <= off + 2.0 ** -22 * two[:, 0].abs()).all()
+    assert checked > 8 * new      # (of 16 * new rows)
