@@ -276,3 +276,119 @@ def test_rows_whose_logits_are_all_far_from_zero(zc, dtype, power, sign, new):
             assert ((got - want).abs() <= torch.where(far, torch.zeros_like(slack), slack)).all()
             assert ((lse[rows, h].double() - two[:, 0]).abs() <= off + 2.0 ** -22 * two[:, 0].abs()).all()
     assert checked > 8 * new      # (of 16 * new rows)
+
+
+def compare(zc, dt, q, k, v, table, row_start, lengths, max_rows, window=0, sinks=0):
+    """One call against the 64-bit reference, every row."""
+    hq, hkv = q.shape[1], k.shape[2]
+    pool = zc.PagedKV(k, v, hq, max_req=len(lengths), max_rows=q.shape[0])
+    out, lse = pool.attention(q, i32(table), i32(row_start), i32(lengths), max_rows, window=window, sinks=sinks)
+    settled(zc)
+    compare_rows(dt, out, lse, q, k, v, table, row_start, lengths, window, sinks)
+
+
+def compare_rows(dt, out, lse, q, k, v, table, row_start, lengths, window=0, sinks=0, rows=None):
+    hq, hkv = q.shape[1], k.shape[2]
+    for r, n in enumerate(lengths):
+        a, e = row_start[r], row_start[r + 1]
+        some = e - a if rows is None else min(e - a, rows)
+        if some == 0:
+            continue
+        kk, vv = ref.rows_of_request(k, v, table[r], n)
+        for h in range(hq):
+            o, l, mean_abs, largest, seen, total = ref.attend(q[a:a + some, h], kk[:, h // (hq // hkv)], vv[:, h // (hq // hkv)],
+                                                              n - (e - a), window, sinks)
+            t_out, t_lse = ref.tolerances(dt, o, mean_abs, largest, seen, total, vv.abs().max().double())
+            off = (out[a:a + some, h].double() - o).abs() - t_out
+            assert off.max() <= 0, (r, h, off.max().item())
+            off = (lse[a:a + some, h].double() - l).abs() - t_lse
+            assert off.max() <= 0, (r, h, off.max().item())
+
+
+SHAPES = ["rising", "falling", "steps", "spike inside", "spike in the last block", "spike past 2^128", "two spikes", "wide"]
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("new,window,sinks", [([1, 1, 1], 0, 0), ([4, 1, 3], 700, 4), ([70, 200, 33], 0, 0), ([300, 20, 64], 900, 4)])
+def test_maxima_that_are_renewed(zc, dtype, shape, new, window, sinks):
+    """Logits that grow along the cache, or leap: every row's queries share a component c, and keys have multiples of it."""
+    dt, hq, hkv, page = TYPES[dtype], 8, 2, 16
+    lengths = [2300, 700, 330]
+    gen = torch.Generator(device=DEV).manual_seed(len(shape) + sum(new))
+    table, n_pages = ref.make_table(np.random.RandomState(3), lengths, page)
+    k, v = ref.make_pages(gen, n_pages, page, hkv, dt, False, DEV)
+    c = torch.randn(D, generator=gen, device=DEV)
+    q = (torch.randn(sum(new), hq, D, generator=gen, device=DEV) * 0.5 + c).to(dt)
+    # a key with m * c beside its noise has a logit of about 16 m (base 2)
+    for r, n in enumerate(lengths):
+        t = torch.arange(n, device=DEV)
+        m = torch.zeros(n, device=DEV)
+        if shape == "rising":
+            m = 6.0 * t / n
+        elif shape == "falling":
+            m = 6.0 * (n - t) / n
+        elif shape == "steps":
+            m = (t // 64 % 7).float() * 0.5
+        elif shape == "wide":
+            m = torch.randn(n, generator=gen, device=DEV) * 1.5
+        elif shape == "spike in the last block":
+            m[n - 1 - new[r]] = 4.0
+        elif shape == "spike past 2^128":
+            m[n - n // 3] = 12.0
+        else:
+            m[n // 2 + 5] = 3.0
+            if shape == "two spikes":
+                m[n - n // 4] = 5.0
+                m[3] = -9.0
+        ids = torch.as_tensor(table[r], device=DEV).long()[t // page]
+        k[ids, t % page] += (m[:, None] * c)[:, None].to(dt)
+    compare(zc, dt, q, k, v, table, [0] + np.cumsum(new).tolist(), lengths, max(new), window, sinks)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("shape", ["rising", "spike", "spike past 2^128"])
+@pytest.mark.parametrize("window,sinks", [(5000, 0), (700, 4)])
+def test_maxima_that_are_renewed_in_a_windowed_prompt(zc, dtype, shape, window, sinks):
+    dt, hq, hkv, l = TYPES[dtype], 4, 2, 1500
+    gen = torch.Generator(device=DEV).manual_seed(len(shape))
+    c = torch.randn(D, generator=gen, device=DEV)
+    q = (torch.randn(1, hq, l, D, generator=gen, device=DEV) * 0.5 + c).to(dt)
+    t = torch.arange(l, device=DEV)
+    m = 6.0 * t / l if shape == "rising" else (t == 700) * (3.0 if shape == "spike" else 12.0)
+    k = (torch.randn(1, hkv, l, D, generator=gen, device=DEV) + m[:, None] * c).to(dt)
+    v = torch.randn(1, hkv, l, D, generator=gen, device=DEV).to(dt)
+    cache = zc.ZipCache(dt, 1, hq, hkv, l, 1, 0.4, device=DEV)
+    out, lse = cache.prefill_attention_window(q, k, v, window, sinks)
+    settled(zc)
+    for h in range(hq):
+        o, ls, mean_abs, largest, seen, total = ref.attend(q[0, h], k[0, h // 2], v[0, h // 2], 0, window, sinks)
+        t_out, t_lse = ref.tolerances(dt, o, mean_abs, largest, seen, total, v.abs().max().double())
+        assert ((out[0, h].double() - o).abs() <= t_out).all(), h
+        assert ((lse[0, h].double() - ls).abs() <= t_lse).all(), h
+
+
+# ---------------------------------------------------------------- what the documentation allows
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("new,bound", [([1, 3, 2], 2), ([40, 9, 130, 64], 64), ([5, 300, 1], 33)])
+def test_a_request_with_more_rows_than_the_bound(zc, dtype, new, bound):
+    """The first `bound` rows of a request are right, the others may be left; nothing else is touched."""
+    dt, hq, hkv = TYPES[dtype], 8, 2
+    lengths = [n + 77 * (i + 1) for i, n in enumerate(new)]
+    gen = torch.Generator(device=DEV).manual_seed(bound)
+    table, n_pages = ref.make_table(np.random.RandomState(4), lengths, 16)
+    k, v = ref.make_pages(gen, n_pages, 16, hkv, dt, False, DEV)
+    rows = [0] + np.cumsum(new).tolist()
+    q = torch.randn(rows[-1] + 7, hq, D, generator=gen, device=DEV).to(dt)
+    out, lse = torch.full_like(q, 9.0), torch.full((rows[-1] + 7, hq), 9.0, device=DEV)
+    pool = zc.PagedKV(k, v, hq, max_req=len(new), max_rows=rows[-1] + 7)
+    pool.attention(q, i32(table), i32(rows), i32(lengths), bound, out=out, row_lse=lse)
+    settled(zc)
+    compare_rows(dt, out, lse, q, k, v, table, rows, lengths, rows=bound)
+    for r, n in enumerate(new):
+        left = slice(rows[r] + bound, rows[r + 1])
+        if n > bound:
+            right = pool.attention(q, i32(table), i32(rows), i32(lengths), max(new))
+            same = (out[left] == 9).all(-1) | (out[left] == right[0][left]).all(-1)
+            assert same.all()
+    assert (out[rows[-1]:] == 9).all() and (lse[rows[-1]:] == 9).all()
