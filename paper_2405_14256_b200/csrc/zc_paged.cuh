@@ -19,6 +19,15 @@ template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, fl
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// The two values that pack2 rounded, as they are held.
+template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t w);
+template <> __device__ __forceinline__ float2 unpack2<__half>(uint32_t w) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t w) {
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
 // a * b / c; the quotient of 32-bit numbers where they fit (a <= ZC_PAGED_MAX_CTAS).
 static_assert(ZC_PAGED_MAX_CTAS < 256, "a * b < 2^32");
 __device__ __forceinline__ long long zc_muldiv(int a, long long b, int c) {

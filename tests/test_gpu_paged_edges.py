@@ -392,3 +392,32 @@ def test_a_request_with_more_rows_than_the_bound(zc, dtype, new, bound):
             same = (out[left] == 9).all(-1) | (out[left] == right[0][left]).all(-1)
             assert same.all()
     assert (out[rows[-1]:] == 9).all() and (lse[rows[-1]:] == 9).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("hq,hkv,new,lengths", [(8, 2, [1, 1, 1], [900, 4000, 130]), (8, 1, [2, 1], [3000, 77]), (4, 4, [1, 1], [2000, 16])])
+def test_single_tokens_are_off_by_the_output_s_rounding_alone(zc, dtype, hq, hkv, new, lengths):
+    """A weight goes to the tensor cores as its value of the type and the rest of it, together off by u * u of it (u half
+    a step; fp16: 2^-25 at least, where the rest is not normal).  So the output's bound has u of its own size and no u
+    of the weighted values; the other terms are those of zc_paged_ref.tolerances."""
+    dt = TYPES[dtype]
+    u = torch.finfo(dt).eps / 2
+    gen = torch.Generator(device=DEV).manual_seed(hq + len(new))
+    table, n_pages = ref.make_table(np.random.RandomState(6), lengths, 16)
+    k, v = ref.make_pages(gen, n_pages, 16, hkv, dt, False, DEV)
+    v.abs_()                                     # outputs as large as the weighted values: nothing cancels
+    rows = [0] + np.cumsum(new).tolist()
+    q = torch.randn(rows[-1], hq, D, generator=gen, device=DEV).to(dt)
+    pool = zc.PagedKV(k, v, hq, max_req=len(new), max_rows=rows[-1])
+    out, lse = pool.attention(q, i32(table), i32(rows), i32(lengths), max(new))
+    settled(zc)
+    for r, n in enumerate(lengths):
+        a, e = rows[r], rows[r + 1]
+        kk, vv = ref.rows_of_request(k, v, table[r], n)
+        for h in range(hq):
+            o, l, mean_abs, largest, seen, total = ref.attend(q[a:e, h], kk[:, h // (hq // hkv)], vv[:, h // (hq // hkv)], n - (e - a), 0, 0)
+            logit = 136 * 2.0 ** -24 * largest
+            bound = (u * u + 2 * math.log(2) * logit + 2.0 ** -18)[:, None] * mean_abs + u * o.abs() + 2.0 ** -24
+            if dt == torch.float16:
+                bound = bound + (seen * 2.0 ** -25 * vv.abs().max().double() / total.clamp(min=1.0))[:, None]
+            assert ((out[a:e, h].double() - o).abs() <= bound).all(), (r, h, ((out[a:e, h].double() - o).abs() / bound).max().item())
