@@ -117,7 +117,9 @@ __global__ void __launch_bounds__(kTabThreads) k_page_tables(
         }
       }
       pos[row] = (int)p;
-      slots[row] = page >= 0 ? (int)(((long long)page << page_log2) + (p & (psize - 1))) : -1;
+      // (a page whose slots pass 31 bits is in no pool)
+      const bool some = page >= 0 && page <= (0x7fffffff >> page_log2);
+      slots[row] = some ? (page << page_log2) + (int)(p & (psize - 1)) : -1;
     }
     rows_before += rt;
     pages_before += pt;

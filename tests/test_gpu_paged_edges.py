@@ -421,3 +421,19 @@ def test_single_tokens_are_off_by_the_output_s_rounding_alone(zc, dtype, hq, hkv
             if dt == torch.float16:
                 bound = bound + (seen * 2.0 ** -25 * vv.abs().max().double() / total.clamp(min=1.0))[:, None]
             assert ((out[a:e, h].double() - o).abs() <= bound).all(), (r, h, ((out[a:e, h].double() - o).abs() / bound).max().item())
+
+
+@pytest.mark.parametrize("page", [16, 256])
+def test_a_page_id_that_no_pool_has_gives_no_slot(zc, page):
+    """A page whose slots pass 2^31 - 1 cannot exist; its tokens have no slot instead of one of another page."""
+    last = 2 ** 31 // page - 1                        # the largest page id that a pool can have
+    ids = [last, last + 1, 2 ** 32 // page, 2 ** 31 - 1, 3]
+    ids = [i for i in ids if i < 2 ** 31]
+    n = len(ids) * page
+    step, table = zc.StepTables(2, n + 1), i32([[5] + [-7] * len(ids), [last + 1, -7] + [-7] * (len(ids) - 1)])
+    step.build(page, i32([page, page - 1]), i32([n, 1]), i32(ids), i32([0, len(ids), 0]), table)
+    torch.cuda.synchronize()
+    want = [i * page + t if i <= last else -1 for i in ids for t in range(page)] + [-1]
+    assert step.slots.tolist() == want
+    assert step.pos.tolist() == [page + i for i in range(n)] + [page - 1]
+    assert table[0].tolist() == [5] + ids
