@@ -437,3 +437,48 @@ def test_a_page_id_that_no_pool_has_gives_no_slot(zc, page):
     assert step.slots.tolist() == want
     assert step.pos.tolist() == [page + i for i in range(n)] + [page - 1]
     assert table[0].tolist() == [5] + ids
+
+
+def test_the_functions_beside_the_classes(zc):
+    """zc_page_tables, zc_page_write, zc_page_read and zc_paged_attention take the tensors as they are, on a handle of
+    zc_pages_init: what the classes give, bit for bit."""
+    dt, hq, hkv, page = torch.bfloat16, 8, 2, 16
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    past, new, n_pages, width = [100, 33], [3, 50], 40, 12
+    rows = sum(new)
+    k, v = ref.make_pages(gen, n_pages, page, hkv, dt, False, DEV)
+    joint = torch.randn(rows, hq + 2 * hkv, D, generator=gen, device=DEV).to(dt)
+    q, kr, vr = joint[:, :hq], joint[:, hq:hq + hkv], joint[:, hq + hkv:]
+    held = np.full((2, width), -1, dtype=np.int32)
+    held[0, :7], held[1, :3] = range(7), range(7, 10)
+    free, state = i32(range(10, n_pages)), i32([0, n_pages - 10, 0])
+    a_table, b_table = i32(held), i32(held)
+    step = zc.StepTables(2, rows)
+    step.build(page, i32(past), i32(new), free, state, a_table)
+    pool = zc.PagedKV(k.clone(), v.clone(), hq, max_req=2, max_rows=rows)
+    pool.write(kr, vr, step.slots)
+    out, lse = pool.attention(q, a_table, step.row_start, step.kv_len, max(new), 40, 4)
+    dense = pool.read(a_table, 80)
+
+    cfg = zc.ZcPageConfig.make(dt, hq, hkv, page, n_pages, k.stride()[:3])
+    work = torch.zeros(zc.zc_pages_workspace(cfg, 2, rows), dtype=torch.uint8, device=DEV)
+    made = [torch.full((n,), -9, dtype=torch.int32, device=DEV) for n in (2, 3, rows, rows, 3)]
+    out2, lse2 = torch.empty_like(out), torch.empty_like(lse)
+    dense2 = [torch.empty_like(t) for t in dense]
+    handle = zc.zc_pages_init(k, v, cfg)
+    try:
+        zc.zc_page_tables(page, i32(past), i32(new), free, state, b_table, *made)
+        zc.zc_page_write(handle, kr, vr, made[2])
+        zc.zc_paged_attention(handle, q, b_table, made[1], made[0], max(new), 40, 4, out2, lse2, work)
+        zc.zc_page_read(handle, b_table, 80, *dense2)
+        settled(zc)
+        assert zc.zc_pages_launch_count(handle) == zc.zc_pages_launch_count(pool.handle) == 4
+        with pytest.raises(zc.ZipCacheError, match="strides"):
+            zc.zc_page_write(handle, kr, vr.contiguous(), made[2])
+    finally:
+        zc.zc_pages_free(handle)
+    assert torch.equal(a_table, b_table) and torch.equal(out, out2) and torch.equal(lse, lse2)
+    for a, b in zip((step.kv_len, step.row_start, step.slots, step.pos, step.free_state), made):
+        assert torch.equal(a, b)
+    assert torch.equal(pool.k_pages, k) and torch.equal(pool.v_pages, v)
+    assert torch.equal(dense[0], dense2[0]) and torch.equal(dense[1], dense2[1])
