@@ -295,7 +295,9 @@ typedef struct zc_pages zc_pages; /* small host-side handle; several host thread
                                      workspaces and streams of their own), until zc_pages_free */
 
 /* Device scratch [host] that zc_paged_attention needs for calls of up to n_req requests and n_rows rows
- * (partial results of rows whose keys several CTAs share).  ZC_ECAPACITY when one call cannot take so many:
+ * (partial results of rows whose keys several CTAs share; 43 MB for every admitted pair, since the CTAs and the rows
+ * that each holds at once bound it: handles whose calls follow one another on a stream can share one, and
+ * zc_page_write and zc_page_read need none).  ZC_ECAPACITY when one call cannot take so many:
  * n_req + n_rows / (2 * floor(128 / G)) may be 13000, G = n_q_heads / n_kv_heads.  Its first
  * ZC_PAGES_SYNC_BYTES must be zero before its first use (every call leaves them zero again); nothing else
  * in it needs initialisation or survives a call.  It must not be used by calls that may run at the same

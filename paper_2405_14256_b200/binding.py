@@ -500,10 +500,13 @@ class PagedKV(_Buffers):
     """Keys and values at full precision in pages: a handle over the caller's tensors, both
     [n_pages, page_size, n_kv_heads, 128] with any strides of the first three dimensions (for pages
     stored [n_pages, n_kv_heads, page_size, 128] pass .transpose(1, 2)).  Holds the workspace of
-    attention calls of up to max_req requests and max_rows rows; one that is given (to share it among
-    the handles of a stream) must have its first ZC_PAGES_SYNC_BYTES zeroed once.  A handle's calls may run on
-    any stream (the constructor waits for the current one's work), attention calls on one at a time.  Tensors
-    that a call allocates may be used on the current stream, behind what orders it after `stream`."""
+    attention calls of up to max_req requests and max_rows rows: 43 MB whatever they are, so handles whose
+    calls follow one another on a stream (the layers of a model) best share one: pass the first one's
+    .workspace.  One made by the caller must have its first ZC_PAGES_SYNC_BYTES zeroed once.  With max_req or
+    max_rows 0 and none given there is no workspace, and the handle is for write and read alone.  A handle's calls
+    may run on any stream (the constructor waits for the current one's work), attention calls that share a workspace
+    on one at a time.  Tensors that a call allocates may be used on the current stream, behind what orders it after
+    `stream`."""
 
     def __init__(self, k_pages, v_pages, n_q_heads: int, max_req: int = 256, max_rows: int = 8192,
                  workspace: Optional[torch.Tensor] = None):
@@ -522,19 +525,21 @@ class PagedKV(_Buffers):
         self.dtype, self.page_size, self.n_q_heads, self.n_kv_heads = k_pages.dtype, page_size, n_q_heads, n_kv
         self._index = self.device.index
         self.workspace_bytes = zc_pages_workspace(self.cfg, max_req, max_rows)
-        if workspace is None:
+        if workspace is None and max_req > 0 and max_rows > 0:
             with torch.cuda.device(self._index):
                 workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
                 workspace[:ZC_PAGES_SYNC_BYTES].zero_()
-        _want_on(workspace, "workspace", self._index)
-        if not workspace.is_contiguous():
-            raise ZipCacheError("the workspace must be contiguous")
-        self._ws_bytes = workspace.numel() * workspace.element_size()
-        if self._ws_bytes < self.workspace_bytes:
-            raise ZipCacheError("shared workspace too small")
+        self._ws_bytes = 0
+        if workspace is not None:
+            _want_on(workspace, "workspace", self._index)
+            if not workspace.is_contiguous():
+                raise ZipCacheError("the workspace must be contiguous")
+            self._ws_bytes = workspace.numel() * workspace.element_size()
+            if self._ws_bytes < self.workspace_bytes:
+                raise ZipCacheError("shared workspace too small")
         self.workspace = workspace
         with torch.cuda.device(self._index):
-            self._keep(workspace)
+            self._keep(*(() if workspace is None else (workspace,)))
             self.handle = zc_pages_init(k_pages, v_pages, self.cfg)
 
     def close(self):
@@ -596,6 +601,8 @@ class PagedKV(_Buffers):
         if _current_device() != self._index:
             with torch.cuda.device(self._index):
                 return self.attention(q, table, row_start, kv_len, max_rows, window, sinks, out, row_lse, stream)
+        if self.workspace is None:
+            raise ZipCacheError("this handle has no workspace for attention (max_req or max_rows was 0)")
         n_req, n, heads = kv_len.numel(), q.shape[0], self.n_q_heads
         strides = self._rows(q, "q", n, heads)
         _want_i32(kv_len, "kv_len", n_req, self._index)

@@ -482,3 +482,24 @@ def test_the_functions_beside_the_classes(zc):
         assert torch.equal(a, b)
     assert torch.equal(pool.k_pages, k) and torch.equal(pool.v_pages, v)
     assert torch.equal(dense[0], dense2[0]) and torch.equal(dense[1], dense2[1])
+
+
+@pytest.mark.parametrize("kw", [dict(max_rows=0), dict(max_req=0)])
+def test_a_handle_that_only_copies_holds_no_workspace(zc, kw):
+    table, n_pages = ref.make_table(np.random.RandomState(0), [30], 16)
+    k, v = ref.make_pages(torch.Generator(device=DEV).manual_seed(1), n_pages, 16, 2, torch.float16, False, DEV)
+    before = torch.cuda.memory_allocated()
+    pool = zc.PagedKV(k, v, 4, **kw)
+    assert torch.cuda.memory_allocated() == before and pool.workspace is None
+    rows = torch.randn(2, 2, D, device=DEV).half()
+    pool.write(rows, rows, i32([table[0, 0] * 16 + 3, table[0, 1] * 16]))
+    K, V = pool.read(i32(table), 30)
+    settled(zc)
+    assert torch.equal(K[0, :, 3], rows[0]) and torch.equal(V[0, :, 16], rows[1])
+    q = torch.zeros(1, 4, D, dtype=torch.float16, device=DEV)
+    with pytest.raises(zc.ZipCacheError, match="workspace"):
+        pool.attention(q, i32(table), i32([0, 1]), i32([30]), 1)
+    shared = zc.PagedKV(k, v, 4, workspace=zc.PagedKV(k, v, 4).workspace, **kw)
+    out, lse = shared.attention(q, i32(table), i32([0, 1]), i32([30]), 1)
+    settled(zc)
+    assert torch.isfinite(out).all()
