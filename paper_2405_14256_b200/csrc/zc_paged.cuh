@@ -1,5 +1,5 @@
-// Device helpers that the paged attention kernels share: tensor-map copies of page rows, output rows,
-// the joining of partial results, and launches that may start beside the kernel they follow.
+// What the paged kernels share: bounded waits of a warp, tensor-map copies of page rows, output rows, tensor maps, and
+// launches that may start beside the kernel they follow.
 #pragma once
 #include <cfloat>
 #include "zc_pages.h"
@@ -8,16 +8,6 @@
 bool zc_page_maps(zc_pages* p);   // encodes the handle's tensor maps (once); false: not supported
 
 namespace {
-
-template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
-template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 
 // The two values that pack2 rounded, as they are held.
 template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t w);
@@ -106,7 +96,8 @@ cudaError_t zc_allow_smem(Kernel kernel, int bytes, std::atomic<unsigned long lo
 // Kernels of this file's users come one behind the other, many of them of a few microseconds: each is launched while
 // the one before still runs, and waits, before its first access to global memory, until that one has completed
 // (their inputs are not declared __restrict__: a read of constant memory might be moved ahead of the wait).
-// Calls one after the other: 2 to 3 us each of launch and prologue less, which of 8 to 50 us is 5 to 10 %.
+// Calls one after the other: 2 to 4 us each of launch and prologue less (write of 8 x 4096 rows 43.0 -> 40.7 us, read
+// 45.4 -> 43.2, windowed single tokens 50.4 -> 48.2, windowed chunks 102 -> 98).
 __device__ __forceinline__ void zc_let_next_start() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
 __device__ __forceinline__ void zc_wait_for_last() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
 template <typename... KArgs, typename... Args>

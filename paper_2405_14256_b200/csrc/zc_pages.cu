@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kCopyThreads) k_page_write(
     }
 }
 
-// grid.y: (request, head); the pieces of a CTA are consecutive tokens.
+// Block: (request, head) * blocks_per_head + block of 64 consecutive tokens of it.
 __global__ void __launch_bounds__(kCopyThreads) k_page_read(
     const char* kp, const char* vp, long long sp, long long st, long long sh, int page_log2,
     int n_pages, int h_kv, const int32_t* table, int width, int l, char* __restrict__ K,

@@ -1,5 +1,5 @@
 // Internal declarations of the full-precision pages: the host handle, what the attention kernels are
-// given, and the arithmetic of visible keys that the host, the planner and the kernels share.
+// given, and the arithmetic of visible keys that the kernels share.
 #pragma once
 #include <cuda.h>
 #include <atomic>
@@ -47,7 +47,7 @@ struct ZcSeen {
   int sink_n;      // keys 0 .. sink_n - 1 lie in front of it and are seen as well
   int nsb, wb0, nb;
 };
-__host__ __device__ static inline ZcSeen zc_seen(int p_first, int p_last, int window, int sinks, int log2) {
+__device__ static inline ZcSeen zc_seen(int p_first, int p_last, int window, int sinks, int log2) {
   ZcSeen s;
   s.hi = p_last + 1 > 0 ? p_last + 1 : 0;
   const int lo = p_first - window + 1;
@@ -61,7 +61,7 @@ __host__ __device__ static inline ZcSeen zc_seen(int p_first, int p_last, int wi
   return s;
 }
 
-// Workspace of one call: what the joining kernel is told, and the partial results it joins.
+// Workspace of one call: arrival counters, what the joining kernel is told, and the partial results that are joined.
 size_t zc_paged_decode_workspace();
 size_t zc_paged_chunk_workspace();
 bool zc_paged_chunk_fits(int G, int n_req, int n_rows);   // the call's items fit the chunk kernel's shared memory
