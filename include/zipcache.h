@@ -333,8 +333,8 @@ int zc_page_tables(int page_size, int n_req, const int32_t* past, const int32_t*
 
 /* New rows into pages: k_rows, v_rows [device] n_rows x h_kv x d of cfg.dtype, row_strides [host] =
  * strides of (row, head) in elements (multiples of 8), d contiguous; row i goes to slots[i] [device].
- * Rows whose slot is negative (or beyond the pages) are skipped.  Two rows with the same slot:
- * either may win.  n_rows = 0 is a no-op. */
+ * Rows whose slot is negative (or beyond the pages) are skipped.  Two rows with the same slot leave either's value
+ * in each 16 bytes of it, head by head and in K and V apart: a mixture of both.  n_rows = 0 is a no-op. */
 int zc_page_write(zc_pages* p, const void* k_rows, const void* v_rows, const int64_t row_strides[2],
                   const int32_t* slots, int n_rows, zc_stream_t stream);
 
@@ -367,7 +367,8 @@ int zc_paged_attention(zc_pages* p, const void* q, const int64_t q_strides[2], c
 
 /* zc_prefill_attention with a sliding window: row i sees the keys j <= i with j > i - window, and the
  * first `sinks` tokens (j < sinks); window >= 1, sinks >= 0.  Arguments, outputs and errors as there.
- * row_lse belongs to the windowed rows: zc_prefill_compress_lse wants zc_prefill_attention's. */
+ * row_lse belongs to the windowed rows: zc_prefill_compress_lse wants zc_prefill_attention's, and decode attention over
+ * a compressed cache knows no window. */
 int zc_prefill_attention_window(zc_cache* c, const void* Q, const void* K, const void* V, int l,
                                 const int64_t q_strides[3], const int64_t kv_strides[3], int window,
                                 int sinks, void* O, float* row_lse, zc_stream_t stream);

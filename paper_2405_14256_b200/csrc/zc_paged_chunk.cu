@@ -28,8 +28,10 @@
 // kernel's end; a worker warp goes on with void values until no more items come.
 //   What it takes (1.7 GHz): 1650 cycles per wide tile, of which the tensor cores alone need 1140 and the exp2 unit
 // 1020; about 5500 more per item (its first and last tiles' masks, the last product, 3000 for the output).  A chunk
-// of 2048 tokens over 30000, 32 query heads over 8: 887 us, 1170 TFLOP/s; a prompt of 8192 under a window
-// of 4096: 353 us, 1170 TFLOP/s.  Measured and not kept: 16 worker warps, two to a row (1 to 4 % slower); one place
+// of 2048 tokens over 30000, 32 query heads over 8: 887-901 us, 1160 TFLOP/s, a few calls after a pause (1.7 to 1.9 GHz);
+// 1000-1060 us, 1000 TFLOP/s, call after call at the power limit.  A prompt of 8192 under a window of 4096: 353-374 and
+// 394-416 us, 1130 and 1020 TFLOP/s.  P is rounded to the input type (the sum is of the unrounded weights): 0.0022
+// of a bf16 output's norm, 0.0016 of which is the output's own rounding.  Measured and not kept: 16 worker warps, two to a row (1 to 4 % slower); one place
 // for S and two for P (the same); the next S fetched into registers ahead (1.3 times as long).
 // For pages the lengths are on the device, and every CTA finds its own share there: the items of all heads,
 // laid end to end with their costs, are cut into as many equal stretches as there are CTAs.  An item

@@ -17,8 +17,8 @@
 // that one CTA holds whole is written out; the pieces of one that a share's border cuts go to the workspace,
 // and the CTA that brings the last of them puts them together, in the order of the CTAs (the result does not
 // depend on timing).  It knows by a counter per unit, zero before and after every call.
-//   32 requests of 2048-4096 tokens, 32 KV heads: 222 us, 6.7 TB/s; a window of 4096 over 16 requests, 8 KV heads:
-// 47.5 us, 5.7 TB/s; 4 requests of 200-512 tokens: 7.0 us, of which launch, lengths and tables, one round trip to the
+//   32 requests of 2048-4096 tokens, 32 KV heads: 219-224 us, 6.7 TB/s; a window of 4096 over 16 requests, 8 KV heads:
+// 48.2 us, 5.6 TB/s; 4 requests of 200-512 tokens: 7.6 us, of which launch, lengths and tables, one round trip to the
 // keys and the join are all.
 #include <cstring>
 #include "zc_pages.h"
