@@ -458,7 +458,7 @@ def _cuda_device(device) -> torch.device:
 
 class StepTables(_Buffers):
     """The buffers of one serving step's lengths and slots (zc_page_tables): kv_len [n_req],
-    row_start [n_req + 1], slots and pos [n_rows], free_state [3], all int32, undefined before the
+    row_start [n_req + 1], slots and pos [n_rows], free_state [3], all int32, zero before the
     first build.  Made once (the constructor waits for the current stream's work) and reused from step to
     step; two steps whose free_state feeds the next one's take two of these in turn.  build may run on any
     stream; readers on another one are ordered behind it by the caller."""
@@ -466,7 +466,7 @@ class StepTables(_Buffers):
     def __init__(self, n_req: int, n_rows: int, device="cuda:0"):
         self.device = _cuda_device(device)
         self.n_req, self.n_rows, self._index = n_req, n_rows, self.device.index
-        new = lambda n: torch.empty(n, dtype=torch.int32, device=self.device)  # noqa: E731
+        new = lambda n: torch.zeros(n, dtype=torch.int32, device=self.device)  # noqa: E731
         with torch.cuda.device(self._index):
             self.kv_len, self.row_start, self.slots, self.pos = new(n_req), new(n_req + 1), new(n_rows), new(n_rows)
             self.free_state = new(3)

@@ -503,3 +503,16 @@ def test_a_handle_that_only_copies_holds_no_workspace(zc, kw):
     out, lse = shared.attention(q, i32(table), i32([0, 1]), i32([30]), 1)
     settled(zc)
     assert torch.isfinite(out).all()
+
+
+def test_step_buffers_begin_as_zeros(zc):
+    junk = torch.full((1 << 20,), -1, dtype=torch.int32, device=DEV)
+    del junk
+    home = torch.cuda.Stream()
+    busy(home, 5)
+    with torch.cuda.stream(home):
+        step = zc.StepTables(3, 700)
+    # (no stream of the reader's has been ordered behind the constructor's)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        for t in (step.kv_len, step.row_start, step.slots, step.pos, step.free_state):
+            assert (t == 0).all()
