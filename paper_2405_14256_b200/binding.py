@@ -207,11 +207,12 @@ def _new(shape, dtype, device, stream):
 class _Buffers:
     """Buffers that an object keeps for its calls, whatever stream a call runs on."""
 
-    def _keep(self, *buffers):
+    def _keep(self, *buffers, own: bool = True):
         """Called once they are made: whatever their memory was used for on the current stream, and their first
-        fill, is over before a call on any stream can touch them.  (Made under capture, they belong to that graph.)"""
+        fill, is over before a call on any stream can touch them.  (Made under capture, they belong to that graph.)
+        own: their memory comes from the current stream; a given buffer's may come from any."""
         self._kept = buffers
-        self._home = _raw_stream(self._index) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+        self._home = _stream_of(self._index, None) if own else None
         self._others = set()
         if not torch.cuda.is_current_stream_capturing():
             torch.cuda.current_stream().synchronize()
@@ -525,7 +526,8 @@ class PagedKV(_Buffers):
         self.dtype, self.page_size, self.n_q_heads, self.n_kv_heads = k_pages.dtype, page_size, n_q_heads, n_kv
         self._index = self.device.index
         self.workspace_bytes = zc_pages_workspace(self.cfg, max_req, max_rows)
-        if workspace is None and max_req > 0 and max_rows > 0:
+        given = workspace is not None
+        if not given and max_req > 0 and max_rows > 0:
             with torch.cuda.device(self._index):
                 workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
                 workspace[:ZC_PAGES_SYNC_BYTES].zero_()
@@ -539,7 +541,7 @@ class PagedKV(_Buffers):
                 raise ZipCacheError("shared workspace too small")
         self.workspace = workspace
         with torch.cuda.device(self._index):
-            self._keep(*(() if workspace is None else (workspace,)))
+            self._keep(*(() if workspace is None else (workspace,)), own=not given)
             self.handle = zc_pages_init(k_pages, v_pages, self.cfg)
 
     def close(self):

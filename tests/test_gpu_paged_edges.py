@@ -516,3 +516,23 @@ def test_step_buffers_begin_as_zeros(zc):
     with torch.cuda.stream(torch.cuda.Stream()):
         for t in (step.kv_len, step.row_start, step.slots, step.pos, step.free_state):
             assert (t == 0).all()
+
+
+def test_a_shared_workspace_waits_for_the_streams_of_all_handles(zc):
+    """Made by a handle on one stream, used by another handle on that one's own stream."""
+    gen = torch.Generator(device=DEV).manual_seed(13)
+    pool, table = pool_of(zc, gen, torch.float16, 8, 2, 16, [900, 40], 8)
+    q = torch.randn(4, 8, D, generator=gen, device=DEV).half()
+    args = (q, table, i32([0, 2, 4]), i32([900, 40]), 2)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        other = zc.PagedKV(pool.k_pages, pool.v_pages, 8, max_req=2, max_rows=8, workspace=pool.workspace)
+    torch.cuda.synchronize()
+    busy(side)
+    with torch.cuda.stream(side):
+        other.attention(*args)
+    size, at = pool.workspace_bytes, pool.workspace.data_ptr()
+    del pool, other
+    again = torch.empty(size, dtype=torch.uint8, device=DEV)
+    assert again.data_ptr() != at
+    settled(zc)
