@@ -365,6 +365,79 @@ int zc_paged_attention(zc_pages* p, const void* q, const int64_t q_strides[2], c
                        int n_rows, int max_rows, int window, int sinks, void* out, float* row_lse,
                        void* workspace, size_t workspace_bytes, zc_stream_t stream);
 
+/* zc_paged_attention for requests that begin alike: n_groups groups of consecutive requests, group g the requests
+ * group_start[g] .. group_start[g + 1] - 1, the first shared_len[g] tokens of which are the same ones (a system prompt, a
+ * document): their tables list the same pages for them, or copies of the same rows where a page is not filled by them.
+ * Those keys and values are read once for all rows of the group, through the table of its first request, instead of
+ * once per request.  group_start [device] n_groups + 1 ascending, shared_len [device] n_groups; requests in no group, and
+ * groups too short to be worth it (down to groups of one), are attended like any.  At most 4096 groups (ZC_ECAPACITY).
+ * Of a group's shared tokens those count that lie before every new row of its requests.
+ *   max_rows * G must be at most 16 (ZC_EINVAL): generated tokens, one or a few per request; a chunk reads each
+ *   key once for 128 / G of its tokens as it is, and is zc_paged_attention's.
+ *   scores [device or NULL]: as zc_paged_attention_scored, with shared_len in place of first (0 for requests in no
+ *   group), and logits likewise.
+ *   workspace: of zc_pages_shared_workspace for the call's n_req and n_rows (or more), zeroed in front as zc_pages_workspace
+ *   says, whose calls it serves as well.
+ * Results are zc_paged_attention's up to rounding: the order in which keys are added up is another one. */
+int zc_paged_attention_shared(zc_pages* p, const void* q, const int64_t q_strides[2], const int32_t* table,
+                              int table_width, const int32_t* row_start, const int32_t* kv_len, int n_req, int n_rows,
+                              int max_rows, const int32_t* group_start, const int32_t* shared_len, int n_groups,
+                              float* scores, void* out, float* row_lse, void* workspace, size_t workspace_bytes,
+                              void* logits, size_t logits_bytes, zc_stream_t stream);
+int zc_pages_shared_workspace(const zc_page_config* cfg, int n_req, int n_rows, size_t* workspace_bytes);
+
+/* ---- thinning out ---------------------------------------------------------------------------
+ * A request that may not grow keeps the tokens that attention has used.  zc_paged_attention_scored adds up every
+ * cached token's weight, zc_page_select lists, per KV head, the tokens to keep by it, zc_page_compact moves their rows
+ * to the front of the request's pages and gives the pages behind them back.  Afterwards the request has kept_len tokens
+ * in its old order, and goes on as any other (its next token's position in the text is the caller's to know). */
+
+/* zc_paged_attention that also adds up the weights of the cached tokens: for token j of request r and KV head h
+ *   A[j, h] = sum over the request's rows i that see j, and the query heads of h, of 2^(s_ij - row_lse_i),
+ * s the scaled logits (base 2).  Tokens that came with this call (the last n_r of kv_len[r]) start from A, older ones
+ * add it to the score they have; so a slot needs no clearing before a new token takes it.
+ *   scores [device, 16-byte aligned] n_pages x h_kv x page_size floats, contiguous, indexed by slot as the pages are;
+ *   first [device or NULL] n_req: tokens before first[r] have no score (pages that other requests share, say), theirs
+ *   are left as they were, as are those of tokens that no row of the call sees.  A slot that two requests of the call
+ *   score ends with either's sum.  row_lse must be given.  Sums are fp32, of fp32 weights, in a fixed order.
+ *   logits [device, 16-byte aligned]: scratch of calls whose max_rows * G is at most 16 (zc_scores_workspace for that
+ *   max_rows; none for others, NULL then).  Nothing in it survives a call; it must not be used by calls that may run at
+ *   the same time.
+ * Everything else as zc_paged_attention, whose outputs it gives bit for bit. */
+int zc_paged_attention_scored(zc_pages* p, const void* q, const int64_t q_strides[2], const int32_t* table,
+                              int table_width, const int32_t* row_start, const int32_t* kv_len, int n_req, int n_rows,
+                              int max_rows, int window, int sinks, const int32_t* first, float* scores, void* out,
+                              float* row_lse, void* workspace, size_t workspace_bytes, void* logits,
+                              size_t logits_bytes, zc_stream_t stream);
+/* Bytes [host] of the logits' scratch: 4 per slot, query head and row. */
+int zc_scores_workspace(const zc_page_config* cfg, int max_rows, size_t* bytes);
+
+/* Which tokens a request keeps, per KV head: the first first[r] ones (NULL: 0), the last `recent` ones, and of those
+ * between the ones with the highest scores, as many as make keep[r] tokens in all (at most max_keep; equal scores: the
+ * lower position; a NaN is below every number).  keep, first [device] n_req; negative values count as 0.
+ *   kept [device] n_req x h_kv x max_keep int32: positions, ascending, -1 behind them;  kept_len [device] n_req: how
+ *   many, the same for all heads.
+ * first[r] + recent tokens are kept even where keep[r] is less.  A request that has no more than its keep[r], or whose
+ * first and recent tokens alone are more than max_keep, stays as it is: kept_len[r] = kv_len[r] (of which kept lists
+ * max_keep at most).  Outputs may not overlap inputs. */
+int zc_page_select(zc_pages* p, const int32_t* table, int table_width, const int32_t* kv_len, int n_req,
+                   const float* scores, const int32_t* keep, int recent, const int32_t* first, int32_t* kept,
+                   int max_keep, int32_t* kept_len, zc_stream_t stream);
+
+/* Moves, in K, V and (unless NULL) scores, the rows of the kept tokens to the first kept_len[r] slots of their request,
+ * head by head, in place: token i of KV head h is then the one that was token kept[r][h][i].  kept [device] n_req x h_kv
+ * x max_keep, the first kept_len[r] of each ascending in [0, kv_len[r]) (zc_page_select's, or a list of the caller's;
+ * others give undefined rows of that request, no fault); requests with kept_len[r] >= kv_len[r], or above max_keep, are
+ * left alone.  What lies behind the kept tokens is left as it is.  All pages of a request's kv_len[r] tokens must be
+ * its own, but those whose tokens all stay where they are (pages of a shared beginning that first[r] covers).
+ * The pages behind the kept tokens, request by request, are put back in front of the free ones, where zc_page_tables
+ * took them from: free_pages [device] n_free, free_state, free_out [device] 3 as there: free_out = {next - pages, end,
+ * pages that found no room in front of next: 0 where all came from this list}.  All three NULL: none.  The table is
+ * left as it is; its entries behind the kept tokens' pages mean nothing any more.  Outputs may not overlap inputs. */
+int zc_page_compact(zc_pages* p, const int32_t* table, int table_width, const int32_t* kv_len, int n_req,
+                    const int32_t* kept, int max_keep, const int32_t* kept_len, float* scores, int32_t* free_pages,
+                    int n_free, const int32_t* free_state, int32_t* free_out, zc_stream_t stream);
+
 /* zc_prefill_attention with a sliding window: row i sees the keys j <= i with j > i - window, and the
  * first `sinks` tokens (j < sinks); window >= 1, sinks >= 0.  Arguments, outputs and errors as there.
  * row_lse belongs to the windowed rows: zc_prefill_compress_lse wants zc_prefill_attention's, and decode attention over

@@ -14,6 +14,8 @@ from .binding import (  # noqa: F401
     zc_export_segment, zc_segment_tokens, zc_num_segments, zc_tail_tokens,
     zc_decode_bytes, zc_launch_count, zc_strerror, zc_device_status, ZipCache,
     zc_order_model_reset, zc_order_model_call,
-    ZcPageConfig, PagedKV, StepTables, zc_pages_workspace, zc_pages_init, zc_pages_free, zc_pages_launch_count,
+    ZC_PAGES_SYNC_BYTES, ZcPageConfig, PagedKV, StepTables, zc_pages_workspace, zc_pages_init, zc_pages_free, zc_pages_launch_count,
     zc_page_tables, zc_page_write, zc_page_read, zc_paged_attention, zc_prefill_attention_window,
+    zc_paged_attention_scored, zc_scores_workspace, zc_paged_attention_shared, zc_pages_shared_workspace,
+    zc_page_select, zc_page_compact,
 )

@@ -104,6 +104,20 @@ _SIGS = {
     "zc_paged_attention": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p, C.c_int,
                                      C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int,
                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "zc_paged_attention_scored": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p, C.c_int,
+                                            C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int,
+                                            C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                            C.c_void_p, C.c_size_t, C.c_void_p]),
+    "zc_scores_workspace": (C.c_int, [C.POINTER(ZcPageConfig), C.c_int, C.POINTER(C.c_size_t)]),
+    "zc_paged_attention_shared": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p, C.c_int,
+                                            C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
+                                            C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                            C.c_void_p, C.c_size_t, C.c_void_p]),
+    "zc_pages_shared_workspace": (C.c_int, [C.POINTER(ZcPageConfig), C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "zc_page_select": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int,
+                                 C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]),
+    "zc_page_compact": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]),
     "zc_prefill_attention_window": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
                                               C.POINTER(C.c_int64), C.POINTER(C.c_int64), C.c_int, C.c_int,
                                               C.c_void_p, C.c_void_p, C.c_void_p]),
@@ -413,6 +427,55 @@ def zc_paged_attention(handle, q, table, row_start, kv_len, max_rows: int, windo
            "zc_paged_attention")
 
 
+def zc_scores_workspace(cfg: ZcPageConfig, max_rows: int) -> int:
+    nbytes = C.c_size_t(0)
+    _check(lib().zc_scores_workspace(C.byref(cfg), max_rows, C.byref(nbytes)), "zc_scores_workspace")
+    return nbytes.value
+
+
+def zc_pages_shared_workspace(cfg: ZcPageConfig, n_req: int, n_rows: int) -> int:
+    nbytes = C.c_size_t(0)
+    _check(lib().zc_pages_shared_workspace(C.byref(cfg), n_req, n_rows, C.byref(nbytes)), "zc_pages_shared_workspace")
+    return nbytes.value
+
+
+def _nbytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def zc_paged_attention_scored(handle, q, table, row_start, kv_len, max_rows: int, window: int, sinks: int, first, scores,
+                              out, row_lse, workspace, logits, stream=None) -> None:
+    qs = (C.c_int64 * 2)(*q.stride()[:2])
+    _check(lib().zc_paged_attention_scored(handle, _ptr(q), qs, _ptr(table), table.shape[1], _ptr(row_start),
+                                           _ptr(kv_len), kv_len.numel(), q.shape[0], max_rows, window, sinks, _ptr(first),
+                                           _ptr(scores), _ptr(out), _ptr(row_lse), _ptr(workspace), _nbytes(workspace),
+                                           _ptr(logits), _nbytes(logits), _stream(stream)), "zc_paged_attention_scored")
+
+
+def zc_paged_attention_shared(handle, q, table, row_start, kv_len, max_rows: int, group_start, shared_len, scores, out,
+                              row_lse, workspace, logits, stream=None) -> None:
+    qs = (C.c_int64 * 2)(*q.stride()[:2])
+    _check(lib().zc_paged_attention_shared(handle, _ptr(q), qs, _ptr(table), table.shape[1], _ptr(row_start),
+                                           _ptr(kv_len), kv_len.numel(), q.shape[0], max_rows, _ptr(group_start),
+                                           _ptr(shared_len), shared_len.numel(), _ptr(scores), _ptr(out), _ptr(row_lse),
+                                           _ptr(workspace), _nbytes(workspace), _ptr(logits), _nbytes(logits),
+                                           _stream(stream)), "zc_paged_attention_shared")
+
+
+def zc_page_select(handle, table, kv_len, scores, keep, recent: int, first, kept, kept_len, stream=None) -> None:
+    _check(lib().zc_page_select(handle, _ptr(table), table.shape[1], _ptr(kv_len), kv_len.numel(), _ptr(scores), _ptr(keep),
+                                recent, _ptr(first), _ptr(kept), kept.shape[2], _ptr(kept_len), _stream(stream)),
+           "zc_page_select")
+
+
+def zc_page_compact(handle, table, kv_len, kept, kept_len, scores=None, free_pages=None, free_state=None, free_out=None,
+                    stream=None) -> None:
+    _check(lib().zc_page_compact(handle, _ptr(table), table.shape[1], _ptr(kv_len), kv_len.numel(), _ptr(kept),
+                                 kept.shape[2], _ptr(kept_len), _ptr(scores), _ptr(free_pages),
+                                 0 if free_pages is None else free_pages.numel(), _ptr(free_state), _ptr(free_out),
+                                 _stream(stream)), "zc_page_compact")
+
+
 ORDER_FIELDS = ("epoch_start", "e", "need_start", "need_end", "slot", "tag", "record", "drain")
 
 
@@ -507,10 +570,15 @@ class PagedKV(_Buffers):
     max_rows 0 and none given there is no workspace, and the handle is for write and read alone.  A handle's calls
     may run on any stream (the constructor waits for the current one's work), attention calls that share a workspace
     on one at a time.  Tensors that a call allocates may be used on the current stream, behind what orders it after
-    `stream`."""
+    `stream`.
+    shared: the workspace serves attention_shared as well, for max_req requests and max_rows rows (about 1 KB more for each
+    of these rows and query heads).  scored_rows: room for the logits of attention_scored and attention_shared calls of up
+    to so many rows per request (4 bytes per slot, query head and row, in .logits, which handles over pages of one shape
+    share as they share a workspace: pass the first one's); calls of more than 16 / G rows need none."""
 
     def __init__(self, k_pages, v_pages, n_q_heads: int, max_req: int = 256, max_rows: int = 8192,
-                 workspace: Optional[torch.Tensor] = None):
+                 workspace: Optional[torch.Tensor] = None, shared: bool = False, scored_rows: int = 0,
+                 logits: Optional[torch.Tensor] = None):
         self.device = _cuda_device(k_pages.device)
         if k_pages.dim() != 4 or k_pages.stride(3) != 1 or k_pages.stride() != v_pages.stride():
             raise ZipCacheError("pages must be [n_pages, page_size, n_kv_heads, 128], the last dimension contiguous, "
@@ -525,7 +593,7 @@ class PagedKV(_Buffers):
         self.k_pages, self.v_pages = k_pages, v_pages
         self.dtype, self.page_size, self.n_q_heads, self.n_kv_heads = k_pages.dtype, page_size, n_q_heads, n_kv
         self._index = self.device.index
-        self.workspace_bytes = zc_pages_workspace(self.cfg, max_req, max_rows)
+        self.workspace_bytes = (zc_pages_shared_workspace if shared else zc_pages_workspace)(self.cfg, max_req, max_rows)
         given = workspace is not None
         if not given and max_req > 0 and max_rows > 0:
             with torch.cuda.device(self._index):
@@ -540,8 +608,18 @@ class PagedKV(_Buffers):
             if self._ws_bytes < self.workspace_bytes:
                 raise ZipCacheError("shared workspace too small")
         self.workspace = workspace
+        self.scored_rows = int(scored_rows)
+        need, given_logits = zc_scores_workspace(self.cfg, self.scored_rows), logits is not None
+        if not given_logits and need > 0:
+            with torch.cuda.device(self._index):
+                logits = torch.empty(need, dtype=torch.uint8, device=self.device)
+        if logits is not None:
+            _want_on(logits, "logits", self._index)
+            if not logits.is_contiguous() or _nbytes(logits) < need:
+                raise ZipCacheError("shared logits too small, or not contiguous")
+        self.logits = logits
         with torch.cuda.device(self._index):
-            self._keep(*(() if workspace is None else (workspace,)), own=not given)
+            self._keep(*(t for t in (workspace, logits) if t is not None), own=not (given or given_logits))
             self.handle = zc_pages_init(k_pages, v_pages, self.cfg)
 
     def close(self):
@@ -603,6 +681,15 @@ class PagedKV(_Buffers):
         if _current_device() != self._index:
             with torch.cuda.device(self._index):
                 return self.attention(q, table, row_start, kv_len, max_rows, window, sinks, out, row_lse, stream)
+        n_req, n, width, strides, out, row_lse, raw = self._call(q, table, row_start, kv_len, out, row_lse, stream)
+        _check(lib().zc_paged_attention(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
+                                        row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
+                                        out.data_ptr(), row_lse.data_ptr(), self.workspace.data_ptr(), self._ws_bytes,
+                                        raw), "zc_paged_attention")
+        return out, row_lse
+
+    def _call(self, q, table, row_start, kv_len, out, row_lse, stream) -> tuple:
+        """What attention calls share: their checks, outputs and stream."""
         if self.workspace is None:
             raise ZipCacheError("this handle has no workspace for attention (max_req or max_rows was 0)")
         n_req, n, heads = kv_len.numel(), q.shape[0], self.n_q_heads
@@ -627,11 +714,131 @@ class PagedKV(_Buffers):
         raw = _stream_of(self._index, stream)
         if raw != self._home:
             self._used_on(raw)
-        _check(lib().zc_paged_attention(self.handle, q.data_ptr(), _strides2(strides[0], strides[1]), table.data_ptr(), width,
-                                        row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
-                                        out.data_ptr(), row_lse.data_ptr(), self.workspace.data_ptr(), self._ws_bytes,
-                                        raw), "zc_paged_attention")
+        return n_req, n, width, _strides2(strides[0], strides[1]), out, row_lse, raw
+
+    def _want_scores(self, scores) -> None:
+        shape = (self.cfg.n_pages, self.n_kv_heads, self.page_size)
+        if scores.dtype is not torch.float32 or scores.shape != shape or not scores.is_contiguous() \
+                or scores.get_device() != self._index:
+            raise ZipCacheError(f"scores: expected contiguous float32 {shape} on {self.device}, got {scores.dtype} "
+                                f"{tuple(scores.shape)} with strides {scores.stride()} on {scores.device}")
+
+    def _logits_for(self, max_rows: int) -> tuple:
+        """The logits' scratch (address, bytes) of a call that scores."""
+        if max_rows > self.scored_rows and max_rows * (self.n_q_heads // self.n_kv_heads) <= 16:
+            raise ZipCacheError(f"this handle has room for the logits of {self.scored_rows} rows per request (scored_rows)")
+        return (0, 0) if self.logits is None else (self.logits.data_ptr(), _nbytes(self.logits))
+
+    def attention_scored(self, q, table, row_start, kv_len, max_rows: int, scores, first=None, window: int = 0,
+                         sinks: int = 0, out=None, row_lse=None, stream=None):
+        """attention that also adds up the weight of every cached token, over the request's rows and the query heads of a KV
+        head, in scores [n_pages, n_kv_heads, page_size] (float32, contiguous): the call's new tokens start from it, older
+        ones add it to what they have; tokens before first[r] (int32 [n_req]; None: 0) have no score."""
+        if _current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.attention_scored(q, table, row_start, kv_len, max_rows, scores, first, window, sinks, out,
+                                             row_lse, stream)
+        self._want_scores(scores)
+        if first is not None:
+            _want_i32(first, "first", kv_len.numel(), self._index)
+        logits, size = self._logits_for(min(max_rows, q.shape[0]))
+        n_req, n, width, strides, out, row_lse, raw = self._call(q, table, row_start, kv_len, out, row_lse, stream)
+        _check(lib().zc_paged_attention_scored(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
+                                               row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
+                                               _ptr(first), scores.data_ptr(), out.data_ptr(), row_lse.data_ptr(),
+                                               self.workspace.data_ptr(), self._ws_bytes, logits, size, raw),
+               "zc_paged_attention_scored")
         return out, row_lse
+
+    def attention_shared(self, q, table, row_start, kv_len, max_rows: int, group_start, shared_len, scores=None, out=None,
+                         row_lse=None, stream=None):
+        """attention of generated tokens (max_rows * G at most 16) for groups of consecutive requests that begin alike:
+        group g, the requests group_start[g] .. group_start[g + 1] - 1, shares its first shared_len[g] tokens, whose keys
+        and values are read once for all of them (int32 [n_groups + 1] and [n_groups]).  scores: as attention_scored's,
+        with the shared tokens for `first`.  For handles made with shared=True."""
+        if _current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.attention_shared(q, table, row_start, kv_len, max_rows, group_start, shared_len, scores, out,
+                                             row_lse, stream)
+        n_groups = shared_len.numel()
+        _want_i32(shared_len, "shared_len", n_groups, self._index)
+        _want_i32(group_start, "group_start", n_groups + 1, self._index)
+        logits = size = 0
+        if scores is not None:
+            self._want_scores(scores)
+            logits, size = self._logits_for(min(max_rows, q.shape[0]))
+        n_req, n, width, strides, out, row_lse, raw = self._call(q, table, row_start, kv_len, out, row_lse, stream)
+        _check(lib().zc_paged_attention_shared(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
+                                               row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows,
+                                               group_start.data_ptr(), shared_len.data_ptr(), n_groups, _ptr(scores),
+                                               out.data_ptr(), row_lse.data_ptr(), self.workspace.data_ptr(),
+                                               self._ws_bytes, logits, size, raw), "zc_paged_attention_shared")
+        return out, row_lse
+
+    def select(self, table, kv_len, scores, keep, recent: int = 0, first=None, max_keep: int = 0, kept=None, kept_len=None,
+               stream=None):
+        """The tokens that each request keeps, per KV head: the first first[r] ones, the last `recent` ones, and by score as
+        many between them as make keep[r] in all (int32 [n_req] each; equal scores: the lower position).  Returns
+        kept [n_req, n_kv_heads, max_keep] (int32 positions, ascending, -1 behind them; max_keep from a given kept, or as
+        said) and kept_len [n_req], the requests' new lengths; what has no more than its keep stays as it is."""
+        if _current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.select(table, kv_len, scores, keep, recent, first, max_keep, kept, kept_len, stream)
+        n_req = kv_len.numel()
+        _want_i32(kv_len, "kv_len", n_req, self._index)
+        _want_i32(keep, "keep", n_req, self._index)
+        width = table.shape[-1]
+        _want_i32(table, "table", n_req * width, self._index)
+        if first is not None:
+            _want_i32(first, "first", n_req, self._index)
+        self._want_scores(scores)
+        if kept is None:
+            kept = _new((n_req, self.n_kv_heads, max_keep), torch.int32, self.device, stream)
+        elif kept.dim() != 3 or kept.shape[:2] != (n_req, self.n_kv_heads):
+            raise ZipCacheError(f"kept: expected [{n_req}, {self.n_kv_heads}, max_keep], got {tuple(kept.shape)}")
+        _want_i32(kept, "kept", kept.numel(), self._index)
+        if kept_len is None:
+            kept_len = _new((n_req,), torch.int32, self.device, stream)
+        _want_i32(kept_len, "kept_len", n_req, self._index)
+        _check(lib().zc_page_select(self.handle, table.data_ptr(), width, kv_len.data_ptr(), n_req, scores.data_ptr(),
+                                    keep.data_ptr(), recent, _ptr(first), kept.data_ptr(), kept.shape[2],
+                                    kept_len.data_ptr(), _stream_of(self._index, stream)), "zc_page_select")
+        return kept, kept_len
+
+    def compact(self, table, kv_len, kept, kept_len, scores=None, free_pages=None, free_state=None, free_out=None,
+                stream=None):
+        """Moves the rows (and scores) of the kept tokens to the front of each request's pages, in place; the requests go on
+        with kept_len tokens.  The pages behind them go back in front of the free ones (free_pages, free_state as
+        StepTables.build's; returns free_out [3], the new state) unless these are None."""
+        if _current_device() != self._index:
+            with torch.cuda.device(self._index):
+                return self.compact(table, kv_len, kept, kept_len, scores, free_pages, free_state, free_out, stream)
+        n_req = kv_len.numel()
+        _want_i32(kv_len, "kv_len", n_req, self._index)
+        _want_i32(kept_len, "kept_len", n_req, self._index)
+        width = table.shape[-1]
+        _want_i32(table, "table", n_req * width, self._index)
+        if kept.dim() != 3 or kept.shape[:2] != (n_req, self.n_kv_heads):
+            raise ZipCacheError(f"kept: expected [{n_req}, {self.n_kv_heads}, max_keep], got {tuple(kept.shape)}")
+        _want_i32(kept, "kept", kept.numel(), self._index)
+        if scores is not None:
+            self._want_scores(scores)
+        n_free = 0
+        if free_pages is not None:
+            n_free = free_pages.numel()
+            _want_i32(free_pages, "free_pages", n_free, self._index)
+            if free_state is None:
+                raise ZipCacheError("free_pages come with free_state")
+            _want_i32(free_state, "free_state", 3, self._index)
+            if free_out is None:
+                free_out = _new((3,), torch.int32, self.device, stream)
+            _want_i32(free_out, "free_out", 3, self._index)
+        elif free_state is not None or free_out is not None:
+            raise ZipCacheError("free_state and free_out come with free_pages")
+        _check(lib().zc_page_compact(self.handle, table.data_ptr(), width, kv_len.data_ptr(), n_req, kept.data_ptr(),
+                                     kept.shape[2], kept_len.data_ptr(), _ptr(scores), _ptr(free_pages), n_free,
+                                     _ptr(free_state), _ptr(free_out), _stream_of(self._index, stream)), "zc_page_compact")
+        return free_out
 
 
 class ZipCache:

@@ -608,7 +608,9 @@ int zc_device_status(int* code) {
   int paged = 0, chunk = 0;
   ZC_CUDA(zc_paged_decode_error_code(&paged));
   ZC_CUDA(zc_paged_chunk_error_code(&chunk));
-  if (*code == 0 && (paged || chunk)) *code = 4;
+  int weights = 0;
+  ZC_CUDA(zc_paged_weights_error_code(&weights));
+  if (*code == 0 && (paged || chunk || weights)) *code = 4;
   int dbg_c = 0, dbg_d = 0;   // bounds-checked build only: 100 + the first failed check
   ZC_CUDA(zc_debug_code_compress(&dbg_c));
   ZC_CUDA(zc_debug_code_decode(&dbg_d));

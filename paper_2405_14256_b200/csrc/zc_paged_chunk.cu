@@ -37,7 +37,7 @@
 // laid end to end with their costs, are cut into as many equal stretches as there are CTAs.  An item
 // that a border cuts is worked on in pieces along its keys; k_chunk_join puts them together in their order.
 #include <cstring>
-#include "zc_paged.cuh"
+#include "zc_paged_tc.cuh"
 #include "zc_layout.cuh"
 
 namespace {
@@ -65,6 +65,7 @@ constexpr int kMaxItems = 13000;                      // items of a head, and re
 // Costs as measured over mixed calls, in 220 cycles: a tile of a wide item (both groups work on it), of a narrow one
 // (the groups take turns), an item beside its tiles (Q, first product, output, masks).
 constexpr int kWideTile = 7, kNarrowTile = 5, kItemCost = 25;
+constexpr int kWorthSharing = 512;                    // keys that are not read again, from which on a group is one
 constexpr int kMinPiece = 4;                          // tiles; a shorter piece goes to its neighbour
 
 // Where a CTA's share begins: item `item` of all heads' (head * items + item of the head), key tile t of it.
@@ -82,27 +83,33 @@ struct ChunkWs {
   char* parts;        // [CTA][2]: the piece at its share's start, the one at its end
 };
 
+// What a call is about: batch rows of dense tensors, requests' chunks in pages, or groups of requests whose rows all see
+// the same first keys (no mask; every item's result is partial and joined with the rows' own keys elsewhere).
+enum { kDense = 0, kPages = 1, kGroups = 2 };
+constexpr int kMaxGroups = ZC_PAGED_MAX_GROUPS;
+
 struct ChunkArgs {
   ZcPagedArgs a;
   ChunkWs ws;
+  ZcGroups gr;                         // kGroups
   long long o_req, o_row, o_head;      // elements: out; the log-sum-exp's are these / 128
   int tpt;                             // tokens per tile
   int l, items;                        // dense form: tokens per batch row, items per (batch row, KV head)
 };
 
-// A request's chunk as the kernels see it.
-struct Chunk { int row0, n, p0; };
-__device__ __forceinline__ Chunk load_chunk(const ZcPagedArgs& a, int r) {
-  const int e0 = min(max(a.row_start[r], 0), a.n_rows);
-  const int e1 = min(max(a.row_start[r + 1], e0), a.n_rows);
-  const long long cap = (long long)a.table_width << a.page_log2;
-  const int kv = (int)min((long long)max(a.kv_len[r], 0), cap);
+// A group's rows (those of its requests, which follow one another) and how many keys they share, as find_share has left it.
+__device__ __forceinline__ int group_border(const ChunkArgs& k, int g) { return min(max(k.gr.start[g], 0), k.a.n_req); }
+__device__ __forceinline__ Chunk load_group(const ChunkArgs& k, int g) {
+  const ZcPagedArgs& a = k.a;
+  const int r0 = group_border(k, g), r1 = max(r0, group_border(k, g + 1));
+  const int e0 = min(max(a.row_start[r0], 0), a.n_rows), e1 = min(max(a.row_start[r1], e0), a.n_rows);
   Chunk c;
   c.row0 = e0;
-  c.n = min(e1 - e0, a.max_rows);
-  c.p0 = kv - (e1 - e0);
+  c.p0 = k.gr.keys[g];
+  c.n = c.p0 > 0 ? e1 - e0 : 0;
   return c;
 }
+
 __device__ __forceinline__ int item_tiles(const ZcPagedArgs& a, const Chunk& c, int tok0, int tpi) {
   const int last = min(tok0 + tpi, c.n) - 1;
   return zc_seen(c.p0 + tok0, c.p0 + last, a.window, a.sinks, kTileLog2).nb;
@@ -147,6 +154,61 @@ __device__ __forceinline__ int cut_tile(long long off, int nt, int width, int gr
 // chunk of 40 tokens, 32 heads over 8: over 1000 21.3 -> 19.0 us, over 4000 27.5 -> 23.6; shares of 25 tiles would lose 4 %).
 __device__ __forceinline__ int cut_grain(long long all, int n_cta) { return all < 8LL * kWideTile * n_cta ? kMinPiece : 1; }
 
+// How many keys each group shares: at most what the caller says and what lies before every row of its requests, in whole
+// tiles (the keys behind them are the requests' own, as far as this call goes); none where that does not pay: an item
+// costs about 25 * 220 cycles beside its tiles, the single-token kernel 20 cycles a key and request.  Every CTA finds
+// all of it and leaves it where it reads it again; whoever writes, writes the same.
+__device__ __forceinline__ void find_groups(const ChunkArgs& k, int* scratch) {
+  const ZcPagedArgs& a = k.a;
+  const int tid = threadIdx.x, n = k.gr.n;
+  int* s_border = scratch;          // requests before a group
+  int* s_keys = s_border + n + 1;
+  int* s_count = s_keys + n;        // its requests that have rows
+  const long long cap = (long long)a.table_width << a.page_log2;
+  for (int g = tid; g <= n; g += kThreads) {
+    s_border[g] = group_border(k, g);
+    if (g < n) {
+      s_keys[g] = (int)min((long long)max(k.gr.shared[g], 0), cap);
+      s_count[g] = 0;
+    }
+  }
+  __syncthreads();
+  for (int r = tid; r < a.n_req; r += kThreads) {
+    const Chunk c = load_chunk(a, r);
+    if (c.n <= 0 || r < s_border[0] || r >= s_border[n]) continue;
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+      const int m = (lo + hi) >> 1;
+      if (s_border[m] <= r) lo = m; else hi = m;
+    }
+    atomicMin(&s_keys[lo], c.p0);
+    atomicAdd(&s_count[lo], 1);
+  }
+  __syncthreads();
+  for (int g = tid; g < n; g += kThreads) {
+    const int keys = max(s_keys[g], 0) & -kN;
+    k.gr.keys[g] = (long long)(s_count[g] - 1) * keys >= kWorthSharing ? keys : 0;
+  }
+  __syncthreads();   // (a thread reads what another of its CTA has written)
+}
+// What the kernels behind this one are to know of a request: its group's keys, its first row among the group's, the group's
+// first item.
+__device__ __forceinline__ void tell_requests(const ChunkArgs& k, const int* s_start, int n_cta) {
+  const ZcPagedArgs& a = k.a;
+  for (int r = blockIdx.x + threadIdx.x * n_cta; r < a.n_req; r += kThreads * n_cta) {
+    int4 info = make_int4(0, 0, 0, 0);
+    if (r >= group_border(k, 0) && r < group_border(k, k.gr.n)) {
+      int lo = 0, hi = k.gr.n;
+      while (hi - lo > 1) {
+        const int m = (lo + hi) >> 1;
+        if (group_border(k, m) <= r) lo = m; else hi = m;
+      }
+      info = make_int4(k.gr.keys[lo], max(0, min(max(a.row_start[r], 0), a.n_rows) - load_group(k, lo).row0), s_start[lo], 0);
+    }
+    k.gr.info[r] = info;
+  }
+}
+
 // This CTA's share of a paged call, found by the whole block in shared memory (16 bytes per request or item).
 struct Share {
   Border begin, end;
@@ -160,34 +222,39 @@ struct Found {
   int nt, width, r, in_req, kv;
 };
 static_assert(sizeof(Found) <= 64, "it fits between the barriers and the sums");
+template <int FORM>
 __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, long long* s_warp, Found* s_found,
                                             int n_cta) {
   const ZcPagedArgs& a = k.a;
   const int tid = threadIdx.x, tpi = 2 * k.tpt;
+  const int n_req = FORM == kGroups ? k.gr.n : a.n_req;   // (groups take the requests' place below)
   int* s_start = reinterpret_cast<int*>(scratch);      // items before a request
-  int* s_n = s_start + a.n_req + 1;
-  int* s_p0 = s_n + a.n_req;
-  int* s_cost = s_p0 + a.n_req;                        // cost of the head's items before an item
+  int* s_n = s_start + n_req + 1;
+  int* s_p0 = s_n + n_req;
+  int* s_cost = s_p0 + n_req;                          // cost of the head's items before an item
+  if (FORM == kGroups) find_groups(k, s_cost);
   int items = 0;
-  for (int c0 = 0; c0 < a.n_req; c0 += kThreads) {
+  for (int c0 = 0; c0 < n_req; c0 += kThreads) {
     const int r = c0 + tid;
     Chunk c;
     c.n = c.p0 = 0;
-    if (r < a.n_req) {
-      c = load_chunk(a, r);
+    if (r < n_req) {
+      c = FORM == kGroups ? load_group(k, r) : load_chunk(a, r);
       s_n[r] = c.n;
       s_p0[r] = c.p0;
     }
     long long t;
     const long long at = block_scan((c.n + tpi - 1) / tpi, s_warp, &t);
     // (lengths that contradict the host's bounds cannot lead outside the scratch)
-    if (r < a.n_req) s_start[r] = (int)min((long long)kMaxItems, items + at);
-    items = (int)min((long long)kMaxItems, items + t);
+    const long long most = FORM == kGroups ? k.gr.most : kMaxItems;
+    if (r < n_req) s_start[r] = (int)min(most, items + at);
+    items = (int)min(most, items + t);
   }
-  if (tid == 0) s_start[a.n_req] = items;
+  if (tid == 0) s_start[n_req] = items;
   __syncthreads();
+  if (FORM == kGroups) tell_requests(k, s_start, n_cta);
   auto request = [&](int i) {
-    int lo = 0, hi = a.n_req;
+    int lo = 0, hi = n_req;
     while (hi - lo > 1) {
       const int m = (lo + hi) >> 1;
       if (s_start[m] <= i) lo = m; else hi = m;
@@ -201,6 +268,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
     c.n = s_n[r];
     c.p0 = s_p0[r];
     *width = item_width(min(tpi, c.n - tok0), k.tpt);
+    if (FORM == kGroups) return c.p0 >> kTileLog2;
     return item_tiles(a, c, tok0, tpi);
   };
   const int most = 0x7fffffff / max(items, 1);   // a head's cost stays in 31 bits
@@ -289,7 +357,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
       while (j.first > 1 && cuts(j.first - 1)) --j.first;
       if (j.first == c) {
         while (j.last + 1 < n_cta && cuts(j.last + 1)) ++j.last;
-        const Chunk q = load_chunk(a, f.r);
+        const Chunk q = FORM == kGroups ? load_group(k, f.r) : load_chunk(a, f.r);
         j.on = 1;
         j.row0 = q.row0;
         j.n = q.n;
@@ -334,18 +402,6 @@ __device__ __forceinline__ void mma_pv(uint32_t tmem_o, uint32_t tmem_p, uint64_
         "r"(tmem_p + 8u * ks), "l"(db + (uint64_t)((ks * 16 * 128) >> 4)), "r"(idesc), "r"((accumulate || ks > 0) ? 1u : 0u)
         : "memory");
 }
-// Q rows of one tile half: 64 channels x G heads x tokens, from (channel half kb, head, token) of batch row b on.
-__device__ __forceinline__ void q_copy(const CUtensorMap* map, uint32_t dst, uint64_t* bar, int kb, int head, int tok, int b) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
-      "[%6];\n" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(kb * 64), "r"(head), "r"(tok), "r"(b), "r"(zc_smem_u32(bar))
-      : "memory");
-}
-__device__ __forceinline__ void expect_bytes(uint64_t* bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(zc_smem_u32(bar)), "r"(bytes) : "memory");
-}
-
 // An item as the fetching warp hands it to the other roles.
 struct Item {
   int r, kv, tok0, ntok;      // request (dense form: batch row), KV head, tokens; r < 0: no more items
@@ -394,22 +450,6 @@ __device__ __forceinline__ void finish_item(const ChunkArgs& k, int n, Item& it)
   }
 }
 
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
-      " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 d, a, b;\n"
-      " mov.b64 {%0, %1}, d;\n}\n"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;\n" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -432,33 +472,26 @@ template <typename T> __device__ __forceinline__ float weights(const float* v, f
   return add[0].x + add[0].y;
 }
 
-// The loads that wrote v[0 .. 31] have completed (the operands keep their uses behind the wait).
-__device__ __forceinline__ void tmem_wait32(float* v) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;\n"
-               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
-                 "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
-                 "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
-                 "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
-               :
-               : "memory");
+// The same for a group's item: all rows see all of its keys.
+__device__ __forceinline__ void finish_group_item(const ChunkArgs& k, const Chunk& c, Item& it) {
+  it.ntok = min(2 * k.tpt, c.n - it.tok0);
+  it.narrow = it.ntok <= k.tpt;
+  it.s.lo = it.s.sink_n = it.s.nsb = it.s.wb0 = 0;
+  it.s.hi = c.p0;
+  it.s.nb = c.p0 >> kTileLog2;
+  it.t1 = min(it.t1, it.s.nb);
+  it.ga[0] = it.ga[1] = it.t0;
+  it.ge[0] = it.ge[1] = it.t1;
 }
-// One thread of the (converged) warp, the same each time.  What it issues is computed by the whole warp
-// from values that are the same in all lanes: the operands of tcgen05.mma then live in uniform registers
-// instead of being moved there one by one (75 against 48 cycles from one 128 x 64 x 16 product to the next).
-__device__ __forceinline__ bool elect_one() {
-  uint32_t p;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
-  return p != 0;
-}
+
 // Bits 0 .. n - 1 of 64.
 __device__ __forceinline__ uint64_t below(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
-__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
-
-template <typename T, bool PAGED>
+template <typename T, int FORM>
 __global__ void __launch_bounds__(kThreads, 1)
     k_chunk_attention(const ChunkArgs k, const __grid_constant__ CUtensorMap qmap,
                       const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
   extern __shared__ __align__(1024) char smem_raw[];
+  constexpr bool PAGED = FORM != kDense;
   const ZcPagedArgs& a = k.a;
   const uint32_t raw_u = zc_smem_u32(smem_raw);
   const uint32_t base_u = (raw_u + 1023u) & ~1023u;
@@ -528,7 +561,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);
   zc_wait_for_last();
   Share share;
-  if (PAGED) share = find_share(k, base, reinterpret_cast<long long*>(s_ms), reinterpret_cast<Found*>(base + kTiles + 384), gridDim.x);
+  if (PAGED) share = find_share<FORM>(k, base, reinterpret_cast<long long*>(s_ms), reinterpret_cast<Found*>(base + kTiles + 384), gridDim.x);
 
   uint32_t n_item = 0;   // items taken from the ring
   // Next item of the ring; a whole warp calls.  False: there are no more (or a wait ran out).
@@ -608,7 +641,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       int r = share.r, in_req = share.in_req;
       Chunk c;
       c.row0 = c.n = c.p0 = 0;
-      if (PAGED && share.items > 0) c = load_chunk(a, r);
+      auto load = [&](int i) { return FORM == kGroups ? load_group(k, i) : load_chunk(a, i); };
+      if (PAGED && share.items > 0) c = load(r);
       auto find_item = [&](Item& it) {   // the share's next item; r < 0: there is none
         it.r = -1;
         if (!PAGED) {
@@ -623,25 +657,30 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (at.item > share.end.item || (at.item == share.end.item && at.t >= share.end.t)) return;
         // (only the share's first item can begin, and only its last can end, inside)
-        it.r = r;
+        it.r = FORM == kGroups ? group_border(k, r) : r;   // the first request's table has the group's pages
         it.kv = at.item / share.items;
         it.tok0 = in_req * 2 * k.tpt;
         it.row0 = c.row0;
         it.p_first = c.p0 + it.tok0;
         it.t0 = at.t;
         it.t1 = at.item == share.end.item ? share.end.t : 1 << 30;
-        finish_item(k, c.n, it);
+        if (FORM == kGroups) finish_group_item(k, c, it);
+        else finish_item(k, c.n, it);
         it.slot = it.t0 > 0 ? 2 * (int)blockIdx.x : it.t1 < it.s.nb ? 2 * (int)blockIdx.x + 1 : -1;
+        // where the item's result will be: with its rows, or in pieces from the next CTA's border on
+        if (FORM == kGroups && it.t0 == 0 && lane == 0)
+          k.gr.cut[(long long)(at.item - it.kv * share.items) * a.h_kv + it.kv] = it.slot >= 0 ? (int)blockIdx.x + 1 : 0;
         ++at.item;
         at.t = 0;
         if (at.item > share.end.item || (at.item == share.end.item && share.end.t == 0)) return;
         if ((++in_req) * 2 * k.tpt >= c.n) {
           // the next request with rows (after the last one's, the next head's first), 32 at a time
           in_req = 0;
-          for (int r0 = at.item % share.items == 0 ? 0 : r + 1; r0 < a.n_req; r0 += 32) {
+          const int n_req = FORM == kGroups ? k.gr.n : a.n_req;
+          for (int r0 = at.item % share.items == 0 ? 0 : r + 1; r0 < n_req; r0 += 32) {
             Chunk x;
             x.row0 = x.n = x.p0 = 0;
-            if (r0 + lane < a.n_req) x = load_chunk(a, r0 + lane);
+            if (r0 + lane < n_req) x = load(r0 + lane);
             const unsigned some = __ballot_sync(0xffffffffu, x.n > 0);
             if (some) {
               const int src = __ffs(some) - 1;
@@ -878,7 +917,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int h = 0; h < 2; ++h) tmem_ld32_nowait(v + 32 * h, tmem_s + 32 * h);
 #pragma unroll
         for (int h = 0; h < 2; ++h) tmem_wait32(v + 32 * h);
-        const bool edge = key0 + kN - 1 > first || (key0 <= last - a.window && key0 + kN > a.sinks);
+        const bool edge = FORM != kGroups && (key0 + kN - 1 > first || (key0 <= last - a.window && key0 + kN > a.sinks));
         if (edge) {
           // the tile crosses the diagonal, the window's edge or the end of the sinks
           const uint64_t seen = below(pos + 1 - key0) & (~below(pos + 1 - a.window - key0) | below(a.sinks - key0));
@@ -990,6 +1029,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int h = it.kv * a.G + head_in;
       const long long at = (PAGED ? 0 : it.r * k.o_req) + (long long)(it.row0 + it.tok0 + tok) * k.o_row + h * k.o_head;
       char* part = PAGED && it.slot >= 0 ? k.ws.parts + (long long)it.slot * kPartBytes : nullptr;
+      float* whole = FORM == kGroups ? k.gr.rows + at / ZC_D * ZC_PART_STRIDE : nullptr;   // (maximum, sum, -, -, 128 sums)
       const int prow = rows_at * kM + row;
       // Output rows leave through the warp's 2 KB of shared memory, 32 channels at a time, so that a store writes 64
       // bytes of each of eight rows: lane i then has rows i / 4 + 8 j, whose places it asks the owners for.
@@ -1034,6 +1074,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int c = 0; c < 8; ++c)
               reinterpret_cast<float4*>(part)[(8 * q4 + c) * kItemRows + prow] =
                   make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+        } else if (FORM == kGroups) {
+          if (writer)
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+              *reinterpret_cast<float4*>(whole + 4 + 32 * q4 + 4 * c) =
+                  make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
         } else if (writers) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -1054,7 +1100,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (writer) {
-        if (!part && a.lse) a.lse[at / ZC_D] = some ? m_run + log2f(s_run) : -INFINITY;
+        if (FORM == kGroups && !part) *reinterpret_cast<float2*>(whole) = make_float2(m_run, any ? s_run : 0.f);
+        else if (!part && a.lse) a.lse[at / ZC_D] = some ? m_run + log2f(s_run) : -INFINITY;
         if (part)
           reinterpret_cast<float2*>(part + kItemRows * ZC_D * 4)[prow] = make_float2(m_run, any ? s_run : 0.f);
       }
@@ -1144,9 +1191,60 @@ template <typename T> __global__ void __launch_bounds__(256) k_chunk_join(const 
   if (a.lse && cg == 0) a.lse[at] = sum > 0.f ? m + log2f(sum) : -INFINITY;
 }
 
-size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
-int tokens_per_tile(int G) { return kM / G; }
+// The rows of groups: what they have from the shared keys, whole or in pieces, and from their own.  A warp has a row, a
+// lane four channels of it.
+template <typename T> __global__ void __launch_bounds__(256) k_group_join(const ChunkArgs k, const float* own, int n_cta) {
+  zc_let_next_start();
+  zc_wait_for_last();
+  const ZcPagedArgs& a = k.a;
+  const int lane = threadIdx.x & 31;
+  const long long idx = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int per_req = a.max_rows * a.h_q, r = (int)(idx / per_req), in = (int)(idx - (long long)r * per_req);
+  if (r >= a.n_req) return;
+  const int t = in / a.h_q, head = in - t * a.h_q;
+  const int4 info = k.gr.info[r];
+  const Chunk c = load_chunk(a, r);
+  if (t >= c.n || info.x <= 0) return;
+  const long long at = (long long)(c.row0 + t) * a.h_q + head;
+  const float* mine = own + at * ZC_PART_STRIDE;
+  const float2 ms0 = *reinterpret_cast<const float2*>(mine);
+  const float4 x0 = *reinterpret_cast<const float4*>(mine + 4 + 4 * lane);
+  const int kv = head / a.G, tok = info.y + t, tpi = 2 * k.tpt, item = tok / tpi;
+  const int tok_in = tok - item * tpi, half = tok_in >= k.tpt;
+  const int prow = half * kM + (tok_in - half * k.tpt) * a.G + head - kv * a.G;
+  if (info.z + item >= k.gr.most) return;   // (lengths that contradict one another)
+  int cut = k.gr.cut[(long long)(info.z + item) * a.h_kv + kv];
+  if (cut < 0 || cut >= n_cta) cut = 0;   // (only where a wait has run out)
+  float m = ms0.x, sum = ms0.y;
+  float4 acc = x0;
+  auto take = [&](float2 ms, float4 x) {
+    const float top = fmaxf(m, ms.x), fo = zc_exp2(m - top), fn = zc_exp2(ms.x - top);
+    m = top;
+    sum = fmaf(sum, fo, ms.y * fn);
+    acc.x = fmaf(acc.x, fo, x.x * fn);
+    acc.y = fmaf(acc.y, fo, x.y * fn);
+    acc.z = fmaf(acc.z, fo, x.z * fn);
+    acc.w = fmaf(acc.w, fo, x.w * fn);
+  };
+  auto piece = [&](int slot) {
+    const char* p = k.ws.parts + (long long)slot * kPartBytes;
+    take(reinterpret_cast<const float2*>(p + kItemRows * ZC_D * 4)[prow],
+         reinterpret_cast<const float4*>(p)[lane * kItemRows + prow]);
+  };
+  if (cut == 0) {
+    const float* w = k.gr.rows + at * ZC_PART_STRIDE;
+    take(*reinterpret_cast<const float2*>(w), *reinterpret_cast<const float4*>(w + 4 + 4 * lane));
+  } else {
+    const int last = min(k.ws.joins[cut].last, n_cta - 1);
+    piece(2 * (cut - 1) + 1);
+#pragma unroll 4
+    for (int d = cut; d <= last; ++d)
+      if (k.ws.used[d]) piece(2 * d);
+  }
+  store_row<T>(a.out, a.lse, at, lane, m, sum, acc);
+}
 
+size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 // Places of the parts of a call's workspace; returns the bytes.
 size_t carve(char* ws, ChunkWs* out) {
   size_t off = ZC_PAGES_SYNC_BYTES;   // the single-token kernel's counters stay as they are
@@ -1163,25 +1261,10 @@ size_t carve(char* ws, ChunkWs* out) {
   return off;
 }
 
-template <typename T, bool PAGED>
+template <typename T, int FORM>
 cudaError_t ready() {   // the shared memory the kernel asks for
   static std::atomic<unsigned long long> allowed{0};
-  return zc_allow_smem(k_chunk_attention<T, PAGED>, kSmem, &allowed);
-}
-
-// Q as (channels, query heads, tokens, batch rows), boxes of 64 channels x G heads x tpt tokens.
-bool make_q_map(CUtensorMap* map, const void* q, int dtype, int h_q, int G, long long tokens, int batch,
-                long long s_head, long long s_tok, long long s_batch) {
-  const cuuint64_t dims[4] = {ZC_D, (cuuint64_t)h_q, (cuuint64_t)tokens, (cuuint64_t)batch};
-  // an extent of 1 may come with any stride: the map wants one that is valid
-  const long long s[3] = {h_q > 1 ? s_head : ZC_D, tokens > 1 ? s_tok : ZC_D, batch > 1 ? s_batch : ZC_D};
-  cuuint64_t strides[3];
-  for (int i = 0; i < 3; ++i) {
-    if (s[i] <= 0 || (s[i] & 7)) return false;
-    strides[i] = (cuuint64_t)s[i] * 2;
-  }
-  const cuuint32_t box[4] = {64, (cuuint32_t)G, (cuuint32_t)tokens_per_tile(G), 1};
-  return zc_encode_map(map, dtype, 4, q, dims, strides, box);
+  return zc_allow_smem(k_chunk_attention<T, FORM>, kSmem, &allowed);
 }
 
 // Dense K or V as pages: a batch row is a page of l tokens (64 channels, token, half of the channels, KV head,
@@ -1200,9 +1283,9 @@ bool make_dense_map(CUtensorMap* map, const void* x, const zc_config& cfg, int l
 
 template <typename T>
 int launch_chunk(zc_pages* p, const ChunkArgs& k, const CUtensorMap& qmap, cudaStream_t st) {
-  cudaError_t e = ready<T, true>();
+  cudaError_t e = ready<T, kPages>();
   if (e != cudaSuccess) return e;
-  e = zc_launch_early(k_chunk_attention<T, true>, dim3(p->n_sm), dim3(kThreads), kSmem, st, k, qmap, p->k64, p->v64);
+  e = zc_launch_early(k_chunk_attention<T, kPages>, dim3(p->n_sm), dim3(kThreads), kSmem, st, k, qmap, p->k64, p->v64);
   if (e != cudaSuccess) return e;
   p->launches += 1;
   if (p->n_sm > 1) {
@@ -1213,7 +1296,86 @@ int launch_chunk(zc_pages* p, const ChunkArgs& k, const CUtensorMap& qmap, cudaS
   return cudaSuccess;
 }
 
+template <typename T>
+cudaError_t launch_groups(zc_pages* p, const ChunkArgs& k, const CUtensorMap& qmap, cudaStream_t st) {
+  const cudaError_t e = ready<T, kGroups>();
+  if (e != cudaSuccess) return e;
+  return zc_launch_early(k_chunk_attention<T, kGroups>, dim3(p->n_sm), dim3(kThreads), kSmem, st, k, qmap, p->k64, p->v64);
+}
+
+// Items that a head can have: whole ones, and a part of one for each request.
+int most_items(int G, int n_req, int n_rows) { return n_rows / (2 * tokens_per_tile(G)) + n_req; }
+
+// Places of the parts of a shared call's workspace, behind a chunk call's; returns the bytes.
+size_t carve_groups(const zc_page_config& c, int n_req, int n_rows, char* ws, ZcGroups* gr, char** own, char** parts) {
+  const int G = c.n_q_heads / c.n_kv_heads;
+  size_t off = carve(nullptr, nullptr);
+  auto take = [&](size_t bytes) {
+    char* p = ws + off;
+    off += round_up(bytes);
+    return p;
+  };
+  char* p0 = take(zc_paged_decode_workspace());
+  int4* info = (int4*)take((size_t)n_req * sizeof(int4));
+  int* keys = (int*)take(kMaxGroups * sizeof(int));
+  int* cut = (int*)take((size_t)most_items(G, n_req, n_rows) * c.n_kv_heads * sizeof(int));
+  const size_t rows = (size_t)n_rows * c.n_q_heads * ZC_PART_STRIDE * 4;
+  float* shared_rows = (float*)take(rows);
+  char* own_rows = take(rows);
+  if (gr) {
+    gr->info = info;
+    gr->keys = keys;
+    gr->cut = cut;
+    gr->rows = shared_rows;
+    *own = own_rows;
+    *parts = p0;
+  }
+  return off;
+}
+
 }  // namespace
+
+size_t zc_paged_shared_workspace(const zc_page_config& c, int n_req, int n_rows) {
+  return carve_groups(c, n_req, n_rows, nullptr, nullptr, nullptr, nullptr);
+}
+
+int zc_launch_paged_shared(zc_pages* p, const ZcPagedArgs& a, const int32_t* group_start, const int32_t* shared_len,
+                           int n_groups, float* logits, char* ws, cudaStream_t st) {
+  if (!zc_page_maps(p)) return (int)cudaErrorNotSupported;
+  ChunkArgs k;
+  memset(&k, 0, sizeof(k));
+  k.a = a;
+  carve(ws, &k.ws);
+  ZcDecodeMore more = {};
+  char* own = nullptr;
+  carve_groups(p->cfg, a.n_req, a.n_rows, ws, &k.gr, &own, &more.parts);
+  k.gr.start = group_start;
+  k.gr.shared = shared_len;
+  k.gr.n = n_groups;
+  k.gr.most = most_items(a.G, a.n_req, a.n_rows);
+  k.tpt = tokens_per_tile(a.G);
+  k.o_row = (long long)a.h_q * ZC_D;
+  k.o_head = ZC_D;
+  CUtensorMap qmap;
+  memset(&qmap, 0, sizeof(qmap));
+  if (!make_q_map(&qmap, a.q, p->cfg.dtype, a.h_q, a.G, a.n_rows, 1, a.qs_head, a.qs_row, 0))
+    return (int)cudaErrorNotSupported;
+  const bool half = p->cfg.dtype == ZC_F16;
+  cudaError_t e = half ? launch_groups<__half>(p, k, qmap, st) : launch_groups<__nv_bfloat16>(p, k, qmap, st);
+  if (e != cudaSuccess) return (int)e;
+  p->launches += 1;
+  more.logits = logits;
+  more.info = k.gr.info;
+  more.rows = (float*)own;
+  e = (cudaError_t)zc_launch_paged_decode(p, a, more, ws, st);
+  if (e != cudaSuccess) return (int)e;
+  const long long blocks = ((long long)a.n_req * a.max_rows * a.h_q + 7) / 8;
+  if (blocks > 0x7fffffffLL) return (int)cudaErrorInvalidConfiguration;
+  e = half ? zc_launch_early(k_group_join<__half>, dim3((unsigned)blocks), dim3(256), 0, st, k, (float*)own, p->n_sm)
+           : zc_launch_early(k_group_join<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, st, k, (float*)own, p->n_sm);
+  if (e == cudaSuccess) p->launches += 1;
+  return (int)e;
+}
 
 size_t zc_paged_chunk_workspace() { return carve(nullptr, nullptr); }
 
@@ -1267,13 +1429,13 @@ int zc_launch_prefill_window(zc_cache* c, const void* Q, const void* K, const vo
   const int grid = n < c->n_sm ? (int)n : c->n_sm;
   cudaError_t e;
   if (cfg.dtype == ZC_F16) {
-    e = ready<__half, false>();
+    e = ready<__half, kDense>();
     if (e != cudaSuccess) return e;
-    e = zc_launch_early(k_chunk_attention<__half, false>, dim3(grid), dim3(kThreads), kSmem, st, k, qmap, kmap, vmap);
+    e = zc_launch_early(k_chunk_attention<__half, kDense>, dim3(grid), dim3(kThreads), kSmem, st, k, qmap, kmap, vmap);
   } else {
-    e = ready<__nv_bfloat16, false>();
+    e = ready<__nv_bfloat16, kDense>();
     if (e != cudaSuccess) return e;
-    e = zc_launch_early(k_chunk_attention<__nv_bfloat16, false>, dim3(grid), dim3(kThreads), kSmem, st, k, qmap, kmap, vmap);
+    e = zc_launch_early(k_chunk_attention<__nv_bfloat16, kDense>, dim3(grid), dim3(kThreads), kSmem, st, k, qmap, kmap, vmap);
   }
   c->launches += 1;
   return (int)e;

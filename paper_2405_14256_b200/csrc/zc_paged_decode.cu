@@ -49,7 +49,8 @@ struct Req {
   int row0, n, p0;   // first row, rows, position of the first
   ZcSeen s;
 };
-__device__ __forceinline__ int load_req(const ZcPagedArgs& a, int r, Req* q) {
+template <int MODE>
+__device__ __forceinline__ int load_req(const ZcPagedArgs& a, const ZcDecodeMore& more, int r, Req* q) {
   const int e0 = min(max(a.row_start[r], 0), a.n_rows);
   const int e1 = min(max(a.row_start[r + 1], e0), a.n_rows);
   const long long cap = (long long)a.table_width << a.page_log2;
@@ -58,6 +59,11 @@ __device__ __forceinline__ int load_req(const ZcPagedArgs& a, int r, Req* q) {
   q->n = min(e1 - e0, a.max_rows);
   q->p0 = kv - (e1 - e0);
   q->s = zc_seen(q->p0, q->p0 + q->n - 1, a.window, a.sinks, kBlkLog2);
+  if (MODE & ZC_DEC_SHARED) {   // the keys before are the group's (a multiple of the block, and before every row)
+    q->s.lo = more.info[r].x;
+    q->s.wb0 = q->s.lo >> kBlkLog2;
+    q->s.nb = max(0, q->s.nb - q->s.wb0);
+  }
   return q->n > 0 ? max(1, (q->s.nb + kDecWarps - 1) / kDecWarps) : 0;
 }
 
@@ -80,13 +86,14 @@ struct Seg {
   long long left;   // steps of the share after this segment
   Req q;
 };
-__device__ __forceinline__ bool seg_next(const ZcPagedArgs& a, Seg& g) {
+template <int MODE>
+__device__ __forceinline__ bool seg_next(const ZcPagedArgs& a, const ZcDecodeMore& more, Seg& g) {
   if (g.left <= 0) return false;
   if (++g.kv == a.h_kv) {
     g.kv = 0;
     do {
       if (++g.r >= a.n_req) return false;
-      g.steps = load_req(a, g.r, &g.q);
+      g.steps = load_req<MODE>(a, more, g.r, &g.q);
     } while (g.steps == 0);
   }
   g.a = 0;
@@ -113,10 +120,11 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t add
                : "memory");
 }
 
-// NT: groups of 8 rows
-template <typename T, int NT>
+// NT: groups of 8 rows.  MODE: ZC_DEC_WEIGHTS, the logits are kept for zc_launch_score_add; ZC_DEC_SHARED, a request's first
+// keys are another kernel's, and its rows' results go to where the two are joined.
+template <typename T, int NT, int MODE>
 __global__ void __launch_bounds__(kDecThreads, 1)
-    k_paged_decode(const ZcPagedArgs a, float* __restrict__ parts, unsigned* __restrict__ arrived,
+    k_paged_decode(const ZcPagedArgs a, const ZcDecodeMore more, float* __restrict__ parts, unsigned* __restrict__ arrived,
                    const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
   extern __shared__ __align__(1024) char smem_raw[];
   const uint32_t raw_u = zc_smem_u32(smem_raw);
@@ -141,7 +149,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
   int mine = 0;   // steps of this thread's request (of the last one, where there are more requests than threads)
   Req mq;
   for (int r = tid; r < a.n_req; r += kDecThreads) {
-    mine = load_req(a, r, &mq);
+    mine = load_req<MODE>(a, more, r, &mq);
     sum += mine;
   }
   long long incl = sum;
@@ -190,7 +198,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
   } else {
     long long before = 0;
     for (int c0 = 0; c0 < a.n_req; c0 += kDecThreads) {
-      mine = c0 + tid < a.n_req ? load_req(a, c0 + tid, &mq) : 0;
+      mine = c0 + tid < a.n_req ? load_req<MODE>(a, more, c0 + tid, &mq) : 0;
       incl = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -223,7 +231,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
   if (seg.a == seg.steps) {   // the border was moved to the unit's end: the share begins with the next unit
     unit0 += seg.steps;
     seg.left = end - begin;
-    seg_next(a, seg);
+    seg_next<MODE>(a, more, seg);
   } else {
     seg.b = (int)min((long long)seg.steps, seg.a + (end - begin));
     seg.left = (end - begin) - (seg.b - seg.a);
@@ -244,7 +252,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
           return;
         }
       }
-      if (!seg_next(a, ps)) {
+      if (!seg_next<MODE>(a, more, ps)) {
         pkey = -1;
         return;
       }
@@ -254,8 +262,10 @@ __global__ void __launch_bounds__(kDecThreads, 1)
   const uint32_t ring = base_u + warp * kStages * 2 * kHalf;
   uint64_t* full = bars + warp * kStages;
   bool ok = true;   // no wait of the warp has run out
+  int held[2] = {0, 0};   // pages of the blocks in the two stages
   auto issue = [&](int stage) {
     if (pkey < 0) return;
+    if (MODE & ZC_DEC_WEIGHTS) held[0] = stage == 0 ? ppage : held[0], held[1] = stage == 1 ? ppage : held[1];
     if (lane == 0) {
       const int page = ppage >= 0 && ppage < a.n_pages ? ppage : a.n_pages;   // beyond the pool: arrives as zeros
       const int row = pkey & ((1 << a.page_log2) - 1);
@@ -289,6 +299,16 @@ __global__ void __launch_bounds__(kDecThreads, 1)
       acc.y = fmaf(x.y, f, acc.y);
       acc.z = fmaf(x.z, f, acc.z);
       acc.w = fmaf(x.w, f, acc.w);
+    }
+  };
+  // A row's result: the output, or what is joined with that over the group's keys.
+  auto put = [&](const Req& q, long long at, float m, float sum, float4 acc) {
+    if ((MODE & ZC_DEC_SHARED) && q.s.lo > 0) {
+      float* to = more.rows + at * kJoinStride;
+      if (lane == 0) *reinterpret_cast<float2*>(to) = make_float2(m, sum);
+      *reinterpret_cast<float4*>(to + 4 + 4 * lane) = acc;
+    } else {
+      store_row<T>(a.out, a.lse, at, lane, m, sum, acc);
     }
   };
   const float scale = kLog2e * rsqrtf((float)ZC_D);
@@ -374,6 +394,21 @@ __global__ void __launch_bounds__(kDecThreads, 1)
         }
         async_proxy_fence();   // the stage's next copy is ordered behind these stores
         __syncwarp();
+      }
+      // ---- the logits, for the keys' weights: [page][KV head][token][row] ----
+      if (MODE & ZC_DEC_WEIGHTS) {
+        const int page = stage == 0 ? held[0] : held[1], per = a.max_rows * a.G;
+        if (page >= 0 && page < a.n_pages) {
+          float* at = more.logits + ((((long long)page * a.h_kv + seg.kv) << a.page_log2) +
+                                     (key0 & ((1 << a.page_log2) - 1)) + oct) * per;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int row = 8 * nt + 2 * quad + (e & 1);
+              if (row < rows) at[(e >> 1) * 8 * per + row] = sc[nt][e] * scale;
+            }
+        }
       }
       // ---- running maximum and sum ----
       uint32_t pf[NT][2], rest[NT][2];
@@ -483,7 +518,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
         if (whole) {
           const int tok = row / a.G;
           const long long at = (long long)(seg.q.row0 + tok) * a.h_q + seg.kv * a.G + (row - tok * a.G);
-          store_row<T>(a.out, a.lse, at, lane, mt, total_s, acc);
+          put(seg.q, at, mt, total_s, acc);
         } else {
           float* pr = slot + row * kJoinStride;
           if (lane == 0) {
@@ -567,28 +602,44 @@ __global__ void __launch_bounds__(kDecThreads, 1)
             float4 acc8;
             meet(m8, sum8, acc8);
             const int tok = row / a.G;
-            store_row<T>(a.out, a.lse, (long long)(seg.q.row0 + tok) * a.h_q + seg.kv * a.G + (row - tok * a.G), lane, m8, sum8, acc8);
+            put(seg.q, (long long)(seg.q.row0 + tok) * a.h_q + seg.kv * a.G + (row - tok * a.G), m8, sum8, acc8);
           }
         }
         if (tid == 0) arrived[c0] = 0;   // as the next call wants it
       }
     }
     unit0 += seg.steps;
-    if (!seg_next(a, seg)) break;
+    if (!seg_next<MODE>(a, more, seg)) break;
   }
   if (!ok)   // the copies that were on their way
     for (int i = 0; i < kStages; ++i) drain(&full[i], i < stage ? phase ^ 1u : phase);
 }
 
-template <typename T, int NT>
-int launch(zc_pages* p, const ZcPagedArgs& a, float* parts, unsigned* arrived, cudaStream_t st) {
+template <typename T, int NT, int MODE>
+int launch(zc_pages* p, const ZcPagedArgs& a, const ZcDecodeMore& more, float* parts, unsigned* arrived, cudaStream_t st) {
   static std::atomic<unsigned long long> allowed{0};
-  cudaError_t e = zc_allow_smem(k_paged_decode<T, NT>, kDecSmem, &allowed);
+  cudaError_t e = zc_allow_smem(k_paged_decode<T, NT, MODE>, kDecSmem, &allowed);
   if (e != cudaSuccess) return e;
-  e = zc_launch_early(k_paged_decode<T, NT>, dim3(p->n_sm), dim3(kDecThreads), kDecSmem, st, a, parts, arrived, p->k16, p->v16);
+  e = zc_launch_early(k_paged_decode<T, NT, MODE>, dim3(p->n_sm), dim3(kDecThreads), kDecSmem, st, a, more, parts, arrived,
+                      p->k16, p->v16);
   if (e != cudaSuccess) return e;
   p->launches += 1;
   return cudaSuccess;
+}
+
+template <typename T, int MODE>
+int launch_rows(zc_pages* p, const ZcPagedArgs& a, const ZcDecodeMore& more, float* parts, unsigned* arrived, cudaStream_t st) {
+  return a.max_rows * a.G <= 8 ? launch<T, 1, MODE>(p, a, more, parts, arrived, st)
+                               : launch<T, 2, MODE>(p, a, more, parts, arrived, st);
+}
+
+template <typename T>
+int launch_mode(zc_pages* p, const ZcPagedArgs& a, const ZcDecodeMore& more, float* parts, unsigned* arrived, cudaStream_t st) {
+  if (more.info)
+    return more.logits ? launch_rows<T, ZC_DEC_SHARED | ZC_DEC_WEIGHTS>(p, a, more, parts, arrived, st)
+                       : launch_rows<T, ZC_DEC_SHARED>(p, a, more, parts, arrived, st);
+  return more.logits ? launch_rows<T, ZC_DEC_WEIGHTS>(p, a, more, parts, arrived, st)
+                     : launch_rows<T, 0>(p, a, more, parts, arrived, st);
 }
 
 }  // namespace
@@ -597,14 +648,12 @@ size_t zc_paged_decode_workspace() {
   return ZC_PAGES_SYNC_BYTES + (size_t)ZC_PAGED_MAX_CTAS * 2 * ZC_PAGED_ROWS * kJoinStride * 4;
 }
 
-int zc_launch_paged_decode(zc_pages* p, const ZcPagedArgs& a, char* ws, cudaStream_t st) {
+int zc_launch_paged_decode(zc_pages* p, const ZcPagedArgs& a, const ZcDecodeMore& more, char* ws, cudaStream_t st) {
   if (!zc_page_maps(p)) return (int)cudaErrorNotSupported;
   unsigned* arrived = (unsigned*)ws;
-  float* parts = (float*)(ws + ZC_PAGES_SYNC_BYTES);
-  const bool one = a.max_rows * a.G <= 8;
-  if (p->cfg.dtype == ZC_F16)
-    return one ? launch<__half, 1>(p, a, parts, arrived, st) : launch<__half, 2>(p, a, parts, arrived, st);
-  return one ? launch<__nv_bfloat16, 1>(p, a, parts, arrived, st) : launch<__nv_bfloat16, 2>(p, a, parts, arrived, st);
+  float* parts = (float*)(more.parts ? more.parts : ws + ZC_PAGES_SYNC_BYTES);
+  return p->cfg.dtype == ZC_F16 ? launch_mode<__half>(p, a, more, parts, arrived, st)
+                                : launch_mode<__nv_bfloat16>(p, a, more, parts, arrived, st);
 }
 
 // Tensor maps of the pages: (64 channels, token of the page, half of the channels, KV head, page).
@@ -620,8 +669,9 @@ bool zc_page_maps(zc_pages* p) {
   // a tile of 64 keys from one page comes with both halves of its channels, from several pages half by half
   const bool one = p->cfg.page_size >= 64;
   const cuuint32_t large[5] = {64, (cuuint32_t)(one ? 64 : p->cfg.page_size), one ? 2u : 1u, 1, 1};
-  struct { CUtensorMap* map; void* at; const cuuint32_t* box; } todo[4] = {
-      {&p->k16, p->k, small}, {&p->v16, p->v, small}, {&p->k64, p->k, large}, {&p->v64, p->v, large}};
+  const cuuint32_t tall[5] = {64, (cuuint32_t)(p->cfg.page_size < 128 ? p->cfg.page_size : 128), 1, 1, 1};
+  struct { CUtensorMap* map; void* at; const cuuint32_t* box; } todo[5] = {
+      {&p->k16, p->k, small}, {&p->v16, p->v, small}, {&p->k64, p->k, large}, {&p->v64, p->v, large}, {&p->k128, p->k, tall}};
   for (auto& t : todo)
     if (!zc_encode_map(t.map, p->cfg.dtype, 5, t.at, dims, strides, t.box)) return false;
   p->maps_ready.store(true, std::memory_order_release);

@@ -246,6 +246,50 @@ int check_page_config(const zc_page_config* c) {
   return ZC_OK;
 }
 
+// The checks that attention calls share, and what the kernels are given; n_req = 0 in *out: there is nothing to do.
+int paged_args(zc_pages* p, const void* q, const int64_t q_strides[2], const int32_t* table, int table_width,
+               const int32_t* row_start, const int32_t* kv_len, int n_req, int n_rows, int max_rows, int window, int sinks,
+               void* out, float* row_lse, void* workspace, ZcPagedArgs* args) {
+  args->n_req = 0;
+  if (!p || !q_strides || n_req < 0 || n_rows < 0 || max_rows < 0 || window < 0 || sinks < 0) return ZC_EINVAL;
+  if (n_req == 0 || n_rows == 0 || max_rows == 0) return ZC_OK;
+  if (!q || !table || !row_start || !kv_len || !out || !workspace || table_width < 1) return ZC_EINVAL;
+  if ((long long)table_width << p->page_log2 > ZC_NO_WINDOW || n_rows > ZC_NO_WINDOW) return ZC_EINVAL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || !aligned4(row_lse, table, row_start, kv_len))
+    return ZC_EALIGN;
+  for (int i = 0; i < 2; ++i)
+    if (q_strides[i] < 0 || q_strides[i] % 8 || q_strides[i] >= (1LL << 39)) return ZC_EINVAL;
+  if ((p->cfg.n_q_heads > 1 && q_strides[1] < ZC_D) || (n_rows > 1 && q_strides[0] < ZC_D)) return ZC_EINVAL;
+  ZcPagedArgs& a = *args;
+  a.table = table;
+  a.row_start = row_start;
+  a.kv_len = kv_len;
+  a.table_width = table_width;
+  a.n_req = n_req;
+  a.n_rows = n_rows;
+  a.max_rows = max_rows < n_rows ? max_rows : n_rows;
+  a.page_log2 = p->page_log2;
+  a.n_pages = p->cfg.n_pages;
+  a.h_q = p->cfg.n_q_heads;
+  a.h_kv = p->cfg.n_kv_heads;
+  a.G = p->G;
+  a.window = window == 0 || window > ZC_NO_WINDOW ? ZC_NO_WINDOW : window;
+  a.sinks = sinks;
+  a.q = q;
+  a.qs_row = q_strides[0];
+  a.qs_head = q_strides[1];
+  a.out = out;
+  a.lse = row_lse;
+  return ZC_OK;
+}
+// Whether a call is the single-token kernel's.
+bool few_rows(const ZcPagedArgs& a) { return (long long)a.max_rows * a.G <= ZC_PAGED_ROWS; }
+// A logit of every slot, query head and row, where a call is.
+size_t logits_bytes(const zc_page_config& c, int max_rows) {
+  const int G = c.n_q_heads / c.n_kv_heads;
+  return (long long)max_rows * G <= ZC_PAGED_ROWS ? (size_t)c.n_pages * c.page_size * c.n_q_heads * max_rows * 4 : 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -360,41 +404,90 @@ int zc_paged_attention(zc_pages* p, const void* q, const int64_t q_strides[2], c
                        const int32_t* row_start, const int32_t* kv_len, int n_req, int n_rows, int max_rows,
                        int window, int sinks, void* out, float* row_lse, void* workspace, size_t workspace_bytes,
                        zc_stream_t stream) {
-  if (!p || !q_strides || n_req < 0 || n_rows < 0 || max_rows < 0 || window < 0 || sinks < 0) return ZC_EINVAL;
-  if (n_req == 0 || n_rows == 0 || max_rows == 0) return ZC_OK;
-  if (!q || !table || !row_start || !kv_len || !out || !workspace || table_width < 1) return ZC_EINVAL;
-  if ((long long)table_width << p->page_log2 > ZC_NO_WINDOW || n_rows > ZC_NO_WINDOW) return ZC_EINVAL;
-  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || !aligned4(row_lse, table, row_start, kv_len))
-    return ZC_EALIGN;
-  for (int i = 0; i < 2; ++i)
-    if (q_strides[i] < 0 || q_strides[i] % 8 || q_strides[i] >= (1LL << 39)) return ZC_EINVAL;
-  if ((p->cfg.n_q_heads > 1 && q_strides[1] < ZC_D) || (n_rows > 1 && q_strides[0] < ZC_D)) return ZC_EINVAL;
-  if (max_rows > n_rows) max_rows = n_rows;
   ZcPagedArgs a;
-  a.table = table;
-  a.row_start = row_start;
-  a.kv_len = kv_len;
-  a.table_width = table_width;
-  a.n_req = n_req;
-  a.n_rows = n_rows;
-  a.max_rows = max_rows;
-  a.page_log2 = p->page_log2;
-  a.n_pages = p->cfg.n_pages;
-  a.h_q = p->cfg.n_q_heads;
-  a.h_kv = p->cfg.n_kv_heads;
-  a.G = p->G;
-  a.window = window == 0 || window > ZC_NO_WINDOW ? ZC_NO_WINDOW : window;
-  a.sinks = sinks;
-  a.q = q;
-  a.qs_row = q_strides[0];
-  a.qs_head = q_strides[1];
-  a.out = out;
-  a.lse = row_lse;
-  const bool few = (long long)max_rows * p->G <= ZC_PAGED_ROWS;
+  const int rc = paged_args(p, q, q_strides, table, table_width, row_start, kv_len, n_req, n_rows, max_rows, window, sinks,
+                            out, row_lse, workspace, &a);
+  if (rc != ZC_OK || a.n_req == 0) return rc;
+  const bool few = few_rows(a);
   if (workspace_bytes < (few ? zc_paged_decode_workspace() : zc_paged_chunk_workspace())) return ZC_ECAPACITY;
   if (!few && !zc_paged_chunk_fits(p->G, n_req, n_rows)) return ZC_ECAPACITY;
-  const int e = few ? zc_launch_paged_decode(p, a, (char*)workspace, (cudaStream_t)stream)
+  const int e = few ? zc_launch_paged_decode(p, a, ZcDecodeMore(), (char*)workspace, (cudaStream_t)stream)
                     : zc_launch_paged_chunk(p, a, (char*)workspace, (cudaStream_t)stream);
+  return zc_cuda_status(e);
+}
+
+int zc_scores_workspace(const zc_page_config* cfg, int max_rows, size_t* bytes) {
+  const int rc = check_page_config(cfg);
+  if (rc) return rc;
+  if (max_rows < 0 || !bytes) return ZC_EINVAL;
+  *bytes = logits_bytes(*cfg, max_rows);
+  return ZC_OK;
+}
+
+int zc_paged_attention_scored(zc_pages* p, const void* q, const int64_t q_strides[2], const int32_t* table,
+                              int table_width, const int32_t* row_start, const int32_t* kv_len, int n_req, int n_rows,
+                              int max_rows, int window, int sinks, const int32_t* first, float* scores, void* out,
+                              float* row_lse, void* workspace, size_t workspace_bytes, void* logits,
+                              size_t logits_size, zc_stream_t stream) {
+  ZcPagedArgs a;
+  const int rc = paged_args(p, q, q_strides, table, table_width, row_start, kv_len, n_req, n_rows, max_rows, window, sinks,
+                            out, row_lse, workspace, &a);
+  if (rc != ZC_OK || a.n_req == 0) return rc;
+  if (!scores || !row_lse) return ZC_EINVAL;
+  if (!aligned16(scores) || !aligned4(first) || !aligned16(logits)) return ZC_EALIGN;
+  const bool few = few_rows(a);
+  if (few && !logits) return ZC_EINVAL;
+  if (workspace_bytes < (few ? zc_paged_decode_workspace() : zc_paged_chunk_workspace())) return ZC_ECAPACITY;
+  if (few ? logits_size < logits_bytes(p->cfg, a.max_rows) : !zc_paged_chunk_fits(p->G, n_req, n_rows)) return ZC_ECAPACITY;
+  const cudaStream_t st = (cudaStream_t)stream;
+  int e;
+  if (few) {
+    ZcDecodeMore more = {};
+    more.logits = (float*)logits;
+    e = zc_launch_paged_decode(p, a, more, (char*)workspace, st);
+    if (e == cudaSuccess) e = zc_launch_score_add(p, a, (float*)logits, scores, first, nullptr, nullptr, 0, st);
+  } else {
+    e = zc_launch_paged_chunk(p, a, (char*)workspace, st);
+    if (e == cudaSuccess) e = zc_launch_chunk_weights(p, a, scores, first, (char*)workspace, st);
+  }
+  return zc_cuda_status(e);
+}
+
+int zc_pages_shared_workspace(const zc_page_config* cfg, int n_req, int n_rows, size_t* workspace_bytes) {
+  const int rc = zc_pages_workspace(cfg, n_req, n_rows, workspace_bytes);
+  if (rc) return rc;
+  *workspace_bytes = zc_paged_shared_workspace(*cfg, n_req, n_rows);
+  return ZC_OK;
+}
+
+int zc_paged_attention_shared(zc_pages* p, const void* q, const int64_t q_strides[2], const int32_t* table,
+                              int table_width, const int32_t* row_start, const int32_t* kv_len, int n_req, int n_rows,
+                              int max_rows, const int32_t* group_start, const int32_t* shared_len, int n_groups,
+                              float* scores, void* out, float* row_lse, void* workspace, size_t workspace_bytes,
+                              void* logits, size_t logits_size, zc_stream_t stream) {
+  ZcPagedArgs a;
+  if (n_groups < 0 || (n_groups > 0 && (!group_start || !shared_len))) return ZC_EINVAL;
+  const int rc = paged_args(p, q, q_strides, table, table_width, row_start, kv_len, n_req, n_rows, max_rows, 0, 0, out,
+                            row_lse, workspace, &a);
+  if (rc != ZC_OK || a.n_req == 0) return rc;
+  if (!few_rows(a)) return ZC_EINVAL;
+  if (scores && (!row_lse || !logits)) return ZC_EINVAL;
+  if (!aligned4(group_start, shared_len) || !aligned16(scores) || !aligned16(logits)) return ZC_EALIGN;
+  if (n_groups > ZC_PAGED_MAX_GROUPS || !zc_paged_chunk_fits(p->G, n_req, n_rows)) return ZC_ECAPACITY;
+  if (workspace_bytes < zc_paged_shared_workspace(p->cfg, n_req, n_rows)) return ZC_ECAPACITY;
+  if (scores && logits_size < logits_bytes(p->cfg, a.max_rows)) return ZC_ECAPACITY;
+  const cudaStream_t st = (cudaStream_t)stream;
+  float* kept = scores ? (float*)logits : nullptr;
+  int e;
+  if (n_groups > 0) {
+    e = zc_launch_paged_shared(p, a, group_start, shared_len, n_groups, kept, (char*)workspace, st);
+  } else {
+    ZcDecodeMore more = {};
+    more.logits = kept;
+    e = zc_launch_paged_decode(p, a, more, (char*)workspace, st);
+  }
+  if (scores && e == cudaSuccess)
+    e = zc_launch_score_add(p, a, kept, scores, nullptr, group_start, shared_len, n_groups, st);
   return zc_cuda_status(e);
 }
 
