@@ -415,6 +415,7 @@ int zc_scores_workspace(const zc_page_config* cfg, int max_rows, size_t* bytes);
 /* Which tokens a request keeps, per KV head: the first first[r] ones (NULL: 0), the last `recent` ones, and of those
  * between the ones with the highest scores, as many as make keep[r] tokens in all (at most max_keep; equal scores: the
  * lower position; a NaN is below every number).  keep, first [device] n_req; negative values count as 0.
+ *   scores as zc_paged_attention_scored leaves them (16-byte aligned);
  *   kept [device] n_req x h_kv x max_keep int32: positions, ascending, -1 behind them;  kept_len [device] n_req: how
  *   many, the same for all heads.
  * first[r] + recent tokens are kept even where keep[r] is less.  A request that has no more than its keep[r], or whose

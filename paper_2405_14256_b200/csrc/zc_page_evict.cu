@@ -11,37 +11,64 @@ __device__ __forceinline__ int clamp_len(int n, int width, int page_log2) {
 
 // ---------------------------------------------------------------- selection
 // One CTA per (request, KV head).  The candidates' scores become whole numbers of the same order and stay in shared
-// memory (49152 of them; the rest is fetched again where it is needed).  The k-th largest is found digit by digit (11,
-// 11 and 10 bits) in a histogram of 2048 places; then every warp counts its own stretch of positions, and writes the
-// kept ones behind those of the warps before it, so that the list ascends.  Of the candidates equal to the k-th the
-// first ones are kept.  Bound: latency (one read of the scores, three scans of the histogram).
+// memory (as many as there is room for; the rest is fetched again where it is needed), four consecutive ones a thread.  The k-th highest is
+// found digit by digit (11, 11 and 10 bits) in a histogram of 2048 places; then every thread counts its own stretch of
+// positions, and writes the kept ones behind those of the threads before it, so that the list ascends.  Of the candidates
+// equal to the k-th the first ones are kept.  Candidates of the first digit found, where they are few, go to a list that
+// the other two digits are found in.  Bound: issue slots.
 constexpr int kBins = 2048;
-constexpr int kSelMost = 49152;
+constexpr int kListMost = 1024;
+constexpr int kSelectRoom = 226 * 1024, kSelectFixed = 14 * 1024;   // an SM's shared memory; a CTA's beside the keys
 
-// NaN below everything, -0 as 0.
+// A whole number in the scores' order: NaN below everything, -0 as 0.
 __device__ __forceinline__ uint32_t score_key(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
-  if (x != x) return 0u;
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+  const uint32_t k = u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
+  return (u << 1) > 0xff000000u ? 0u : k;
+}
+
+// Exclusive sums of a and b over the block's threads; returns the whole sums.
+template <int THREADS>
+__device__ __forceinline__ int2 block_before(int& a, int& b, int2* s_warp) {
+  constexpr int kWarps = THREADS / 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = a, y = b;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, x, o), v = __shfl_up_sync(0xffffffffu, y, o);
+    if (lane >= o) {
+      x += u;
+      y += v;
+    }
+  }
+  if (lane == 31) s_warp[warp] = make_int2(x, y);
+  __syncthreads();
+  // (every warp sums the warps before it)
+  const int2 w = lane < kWarps ? s_warp[lane] : make_int2(0, 0);
+  a = x - a + __reduce_add_sync(0xffffffffu, lane < warp ? w.x : 0);
+  b = y - b + __reduce_add_sync(0xffffffffu, lane < warp ? w.y : 0);
+  return make_int2(__reduce_add_sync(0xffffffffu, w.x), __reduce_add_sync(0xffffffffu, w.y));
 }
 
 struct SelectArgs {
   const int32_t *table, *kv_len, *keep, *first;
   const float* scores;
   int32_t *kept, *kept_len;
-  int width, page_log2, n_pages, h_kv, recent, max_keep, held;   // held: keys that shared memory has room for
+  int width, page_log2, n_pages, h_kv, recent, max_keep, held;   // held: fours that shared memory has room for
 };
 
 template <int THREADS>
-__global__ void __launch_bounds__(THREADS) k_page_select(const SelectArgs a) {
+__global__ void __launch_bounds__(THREADS, 2048 / THREADS) k_page_select(const SelectArgs a) {
   constexpr int kWarps = THREADS / 32, kPer = kBins / THREADS;
-  extern __shared__ uint32_t s_keys[];
+  extern __shared__ uint4 s_keys[];
   __shared__ int s_hist[kBins];
-  __shared__ int s_warp[2][kWarps];
-  __shared__ int s_digit, s_left;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  __shared__ uint32_t s_list[kListMost];
+  __shared__ int2 s_warp[kWarps];
+  __shared__ int s_digit, s_left, s_in, s_listed;
+  const int tid = threadIdx.x;
   const int r = blockIdx.x / a.h_kv, head = blockIdx.x - r * a.h_kv;
   zc_let_next_start();
+  for (int i = tid; i < kBins; i += THREADS) s_hist[i] = 0;
   zc_wait_for_last();
   const int n = clamp_len(a.kv_len[r], a.width, a.page_log2);
   const int first = a.first ? min(max(a.first[r], 0), n) : 0;
@@ -56,61 +83,64 @@ __global__ void __launch_bounds__(THREADS) k_page_select(const SelectArgs a) {
     for (int i = tid; i < min(n, a.max_keep); i += THREADS) kept[i] = i;
     return;
   }
-  const int c0 = first, nc = n - recent - first;   // candidates: nc positions from c0 on
-  int want = budget - first - recent;              // of which so many stay, fewer than nc
+  for (int i = tid; i < first; i += THREADS) kept[i] = i;
+  for (int i = tid; i < recent; i += THREADS) kept[len - recent + i] = n - recent + i;
+  const int c0 = first, c1 = n - recent;           // candidates: positions c0 .. c1 - 1
+  int want = budget - first - recent;              // of which so many stay, fewer than there are
+  if (want == 0) return;
   const int32_t* table = a.table + (long long)r * a.width;
-  auto fetch = [&](int i) {
-    const int t = c0 + i, page = table[t >> a.page_log2];
-    if (page < 0 || page >= a.n_pages) return 0u;
-    return score_key(a.scores[(((long long)page * a.h_kv + head) << a.page_log2) + (t & ((1 << a.page_log2) - 1))]);
+  const int mask = (1 << a.page_log2) - 1;
+  const uint32_t page_bytes = 4u << a.page_log2;
+  const int q0 = c0 >> 2, q1 = (c1 + 3) >> 2;      // in fours, which lie on one page
+  auto fetch = [&](int q) {
+    const int t = 4 * q, page = table[t >> a.page_log2];
+    if (page < 0 || page >= a.n_pages) return make_uint4(0u, 0u, 0u, 0u);
+    // (h_kv scores to a token: the numbers of all (page, head) stay in 32 bits)
+    const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const char*>(a.scores) +
+                                                      (uint64_t)((uint32_t)page * (uint32_t)a.h_kv + head) * page_bytes +
+                                                      4u * (t & mask));
+    const uint4 u = make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w));
+    if (max(max(u.x, u.y), max(u.z, u.w)) <= 0x7f800000u)      // as sums of weights are: no sign, no NaN
+      return make_uint4(u.x | 0x80000000u, u.y | 0x80000000u, u.z | 0x80000000u, u.w | 0x80000000u);
+    return make_uint4(score_key(v.x), score_key(v.y), score_key(v.z), score_key(v.w));
   };
-  auto key = [&](int i) { return i < a.held ? s_keys[i] : fetch(i); };
-  // ---- the want-th largest key ----
-  uint32_t found = 0;
-  int shift = 21;
-#pragma unroll 1
-  for (int pass = 0; pass < 3 && want > 0; ++pass) {
-    const int bits = pass < 2 ? 11 : 10;
-    for (int i = tid; i < kBins; i += THREADS) s_hist[i] = 0;
-    __syncthreads();
-    auto count = [&](bool on, uint32_t k) {
-      // many tokens of one weight (none yet, say) are one addition of the warp's
-      const uint32_t bin = (k >> shift) & ((1u << bits) - 1);
-      const unsigned some = __ballot_sync(0xffffffffu, on);
-      if (some == 0xffffffffu) {
-        int same;
-        __match_all_sync(0xffffffffu, bin, &same);
-        if (same) {
-          if (lane == 0) atomicAdd(&s_hist[bin], 32);
-          return;
-        }
-      }
-      if (on) atomicAdd(&s_hist[bin], 1);
-    };
-    if (pass == 0) {
-      constexpr int kUnroll = 8;
-      for (int i0 = 0; i0 < nc; i0 += kUnroll * THREADS) {
-        uint32_t k[kUnroll];
+  // which of a four are candidates (all, but at the ends)
+  auto members = [&](int q) {
+    unsigned in = 15u;
+    if (q == q0) in &= 15u << (c0 - 4 * q);
+    if (q == q1 - 1) in &= 15u >> (4 * q1 - c1);
+    return in;
+  };
+  auto keys = [&](int q) { return q - q0 < a.held ? s_keys[q - q0] : fetch(q); };
+  // ---- the want-th highest key ----
+  __syncthreads();
+  for (int qa = q0; qa < q1; qa += 2 * THREADS) {
+    uint4 k[2];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          const int i = i0 + u * THREADS + tid;
-          k[u] = i < nc ? fetch(i) : 0u;
-        }
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          const int i = i0 + u * THREADS + tid;
-          if (i0 + u * THREADS >= nc) break;
-          if (i < nc && i < a.held) s_keys[i] = k[u];
-          count(i < nc, k[u]);
-        }
-      }
-    } else {
-      for (int i0 = 0; i0 < nc; i0 += THREADS) {
-        const int i = i0 + tid;
-        const uint32_t k = i < nc ? key(i) : 0u;
-        count(i < nc && (k >> (shift + bits)) == (found >> (shift + bits)), k);
-      }
+    for (int u = 0; u < 2; ++u) {
+      const int q = qa + u * THREADS + tid;
+      if (q < q1) k[u] = fetch(q);
     }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int q = qa + u * THREADS + tid;
+      if (q >= q1) continue;
+      if (q - q0 < a.held) s_keys[q - q0] = k[u];
+      const unsigned in = members(q);
+      const uint32_t bin[4] = {k[u].x >> 21, k[u].y >> 21, k[u].z >> 21, k[u].w >> 21};
+      if (in == 15u && bin[0] == bin[1] && bin[0] == bin[2] && bin[0] == bin[3]) {
+        atomicAdd(&s_hist[bin[0]], 4);               // (tokens that have no weight yet, say)
+        continue;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if ((in >> j) & 1u) atomicAdd(&s_hist[bin[j]], 1);
+    }
+  }
+  uint32_t found = 0;
+  int shift = 21, listed = 0;
+#pragma unroll 1
+  for (int pass = 0;; ++pass) {
     __syncthreads();
     // places from the top: thread t has the kPer places below those of thread t - 1
     int mine[kPer], sum = 0;
@@ -119,79 +149,94 @@ __global__ void __launch_bounds__(THREADS) k_page_select(const SelectArgs a) {
       mine[j] = s_hist[kBins - 1 - (tid * kPer + j)];
       sum += mine[j];
     }
-    int incl = sum;
+    int above = sum, unused = 0;
+    block_before<THREADS>(above, unused, s_warp);
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += u;
-    }
-    if (lane == 31) s_warp[0][warp] = incl;
-    __syncthreads();
-    int above = incl - sum;
+    for (int j = 0; j < kPer; ++j) s_hist[kBins - 1 - (tid * kPer + j)] = 0;
+    if (above < want && want <= above + sum) {
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w)
-      if (w < warp) above += s_warp[0][w];
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      if (above < want && want <= above + mine[j]) {
-        s_digit = kBins - 1 - (tid * kPer + j);
-        s_left = want - above;
+      for (int j = 0; j < kPer; ++j) {
+        if (above < want && want <= above + mine[j]) {
+          s_digit = kBins - 1 - (tid * kPer + j);
+          s_left = want - above;
+          s_in = mine[j];
+        }
+        above += mine[j];
       }
-      above += mine[j];
     }
+    if (tid == 0) s_listed = 0;
     __syncthreads();
     found |= (uint32_t)s_digit << shift;
     want = s_left;   // so many of the keys that begin like this one stay
-    shift -= pass == 0 ? 11 : 10;
-  }
-  // ---- the positions, in order: warp w has candidates from w * stretch on ----
-  const bool some = budget > first + recent;       // else no candidate stays
-  const int stretch = (nc + THREADS - 1) / THREADS * 32;
-  const int b = min(nc, warp * stretch), e = min(nc, b + stretch);
-  int gt = 0, eq = 0;
-  if (some) {
-    for (int i0 = b; i0 < e; i0 += 32) {
-      const uint32_t k = i0 + lane < e ? key(i0 + lane) : 0u;
-      const bool in = i0 + lane < e;
-      gt += __popc(__ballot_sync(0xffffffffu, in && k > found));
-      eq += __popc(__ballot_sync(0xffffffffu, in && k == found));
-    }
-    if (lane == 0) {
-      s_warp[0][warp] = gt;
-      s_warp[1][warp] = eq;
-    }
-    __syncthreads();
-    gt = eq = 0;
+    if (pass == 2) break;
+    const int was = shift, next = pass == 0 ? 10 : 0;
+    auto count = [&](uint32_t k) { atomicAdd(&s_hist[(k >> next) & (pass == 0 ? 2047u : 1023u)], 1); };
+    if (listed) {
+      for (int i = tid; i < listed; i += THREADS)
+        if ((s_list[i] >> was) == (found >> was)) count(s_list[i]);
+    } else {
+      const bool list = s_in <= kListMost;
+      for (int q = q0 + tid; q < q1; q += THREADS) {
+        const uint4 four = keys(q);
+        const uint32_t k[4] = {four.x, four.y, four.z, four.w};
+        unsigned like = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w)
-      if (w < warp) {
-        gt += s_warp[0][w];
-        eq += s_warp[1][w];
+        for (int j = 0; j < 4; ++j) like |= (unsigned)((k[j] ^ found) >> was == 0u) << j;
+        like &= members(q);
+        for (; like; like &= like - 1) {
+          const int j = __ffs(like) - 1;
+          const uint32_t x = j & 2 ? (j & 1 ? k[3] : k[2]) : (j & 1 ? k[1] : k[0]);
+          if (list) s_list[atomicAdd(&s_listed, 1)] = x;
+          count(x);
+        }
       }
-    for (int i0 = b; i0 < e; i0 += 32) {
-      const bool in = i0 + lane < e;
-      const uint32_t k = in ? key(i0 + lane) : 0u;
-      const unsigned g = __ballot_sync(0xffffffffu, in && k > found), q = __ballot_sync(0xffffffffu, in && k == found);
-      const unsigned before = (1u << lane) - 1u;
-      const int eq_here = eq + __popc(q & before), at = first + gt + __popc(g & before) + min(eq_here, want);
-      if (in && (k > found || (k == found && eq_here < want))) kept[at] = c0 + i0 + lane;
-      gt += __popc(g);
-      eq += __popc(q);
+      __syncthreads();
+      if (list) listed = s_listed;
     }
+    shift = next;
   }
-  for (int i = tid; i < first; i += THREADS) kept[i] = i;
-  for (int i = tid; i < recent; i += THREADS) kept[len - recent + i] = n - recent + i;
+  // ---- the positions, in order: thread t has `per` fours from the t * per-th on, as bits of a word ----
+  const int per = min(7, ((q1 - q0 + THREADS - 1) / THREADS) | 1);   // (odd: no conflicts in shared memory)
+  int at0 = first, eq0 = 0;   // places taken by higher ones before these fours; equal ones before them
+  for (int s0 = q0; s0 < q1; s0 += THREADS * per) {
+    const int b = min(q1, s0 + tid * per), cnt = min(q1 - b, per);
+    unsigned higher = 0, same = 0;
+    for (int i = 0; i < cnt; ++i) {
+      const uint4 four = keys(b + i);
+      const unsigned in = members(b + i);
+      unsigned g = (unsigned)(four.x > found) | (unsigned)(four.y > found) << 1 | (unsigned)(four.z > found) << 2 |
+                   (unsigned)(four.w > found) << 3;
+      unsigned e = (unsigned)(four.x == found) | (unsigned)(four.y == found) << 1 | (unsigned)(four.z == found) << 2 |
+                   (unsigned)(four.w == found) << 3;
+      higher |= (g & in) << (4 * i);
+      same |= (e & in) << (4 * i);
+    }
+    int gt = __popc(higher), eq = __popc(same);
+    const int2 all = block_before<THREADS>(gt, eq, s_warp);
+    const int room = want - eq0 - eq;                         // of the equal ones, the first stay
+    while (__popc(same) > max(room, 0)) same &= ~(0x80000000u >> __clz(same));
+    int at = at0 + gt + min(eq0 + eq, want);
+    for (unsigned m = higher | same; m; m &= m - 1) kept[at++] = 4 * b + __ffs(m) - 1;
+    at0 += all.x;
+    eq0 += all.y;
+    __syncthreads();   // (the sums' place is free)
+  }
 }
 
 // ---------------------------------------------------------------- compaction
 // Row i of a request's kept ones goes to position i, from a position that is never smaller: what is written in a round
-// (rows of consecutive i) has been read in it or in one before, and no later round reads there.  So a round is: every
-// thread of the cluster has its pieces of rows in registers; the cluster meets; all write.  K and V of a (request, KV
-// head) are clusters of their own; a cluster is 1 to 8 CTAs, as many as fill the GPU: with few requests the rounds
-// would otherwise follow one another in a few CTAs.  Bound: HBM (a row that moves is read once and written once).
-constexpr int kMoveThreads = 256, kMoveUnroll = 8;
-constexpr int kMoveRows = kMoveThreads / 16 * kMoveUnroll;   // rows of a CTA's round
-constexpr int kMoveCluster = 8;
+// (rows of consecutive i) has been read in it or in one before, and no later round reads there.  So the rows pass through
+// shared memory in rounds: a round's rows are written when all of the CTA's threads have theirs, while the next three
+// rounds' are on their way.  K and V of a (request, KV head) are CTAs of their own, and where these do not fill the GPU, so
+// are the halves or quarters of the channels, which need not wait for one another either.  The places of 2048 rows are found
+// at once: found round by round, two dependent reads each, they held the rows up (16 requests of 5000-8192 tokens to 2048,
+// 8 KV heads: 76 us, whether the rows lay scattered or side by side).
+// Bound: HBM (a row that moves is read once and written once).
+constexpr int kMoveThreads = 256, kMoveStages = 4, kMoveSteps = 4;
+constexpr int kMoveStage = kMoveSteps * kMoveThreads * 16;   // bytes of a round
+constexpr int kMoveSeg = 2048;                               // rows whose places are known
+constexpr int kMoveSmem = kMoveStages * kMoveStage + 2 * kMoveSeg * 8;
+constexpr uint64_t kNowhere = ~0ull;
 
 struct CompactArgs {
   char *k, *v;
@@ -201,7 +246,7 @@ struct CompactArgs {
   int32_t* free_pages;             // may be null
   const int32_t* free_state;
   int32_t* free_out;
-  int n_free, n_req, width, page_log2, n_pages, h_kv, max_keep, cluster;
+  int n_free, n_req, width, page_log2, n_pages, h_kv, max_keep;
 };
 
 // A request's tokens and those that it keeps; false: it stays as it is.
@@ -217,95 +262,147 @@ __device__ __forceinline__ int pages_left_over(const CompactArgs& a, int r) {
   return ((n + size - 1) >> a.page_log2) - ((len + size - 1) >> a.page_log2);
 }
 
-__global__ void __launch_bounds__(kMoveThreads) k_page_compact(const CompactArgs a) {
+// The pages behind the kept tokens of request r, put back in front of the free ones.
+__device__ __forceinline__ void give_back(const CompactArgs& a, int r) {
   __shared__ int s_sum[2];
-  const int part = (threadIdx.x & 15) * 16, group = threadIdx.x >> 4;
-  const int rank = blockIdx.x % a.cluster, c = blockIdx.x / a.cluster;
-  const int unit = c >> 1, r = unit / a.h_kv, head = unit - r * a.h_kv;
-  const bool values = c & 1;
-  zc_let_next_start();
-  zc_wait_for_last();
-  const int32_t* table = a.table + (long long)r * a.width;
-  // ---- the pages behind the kept tokens, put back in front of the free ones: one CTA per request ----
-  if (a.free_pages && values && head == 0 && rank == 0) {
-    if (threadIdx.x < 2) s_sum[threadIdx.x] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.n_req; i += kMoveThreads) {
-      const int gone = pages_left_over(a, i);
-      if (gone) {
-        atomicAdd(&s_sum[1], gone);
-        if (i < r) atomicAdd(&s_sum[0], gone);
-      }
-    }
-    __syncthreads();
-    const int total = s_sum[1], mine = pages_left_over(a, r);
-    const int next = min(max(a.free_state[0], 0), a.n_free);
-    const int at = next - total + s_sum[0];
-    const int stay = mine ? (max(a.kept_len[r], 0) + (1 << a.page_log2) - 1) >> a.page_log2 : 0;
-    for (int i = threadIdx.x; i < mine; i += kMoveThreads)
-      if (at + i >= 0) a.free_pages[at + i] = table[stay + i];
-    if (r == 0 && threadIdx.x == 0) {
-      a.free_out[0] = max(0, next - total);
-      a.free_out[1] = min(a.free_state[1], a.n_free);
-      a.free_out[2] = max(0, total - next);
+  if (threadIdx.x < 2) s_sum[threadIdx.x] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < a.n_req; i += kMoveThreads) {
+    const int gone = pages_left_over(a, i);
+    if (gone) {
+      atomicAdd(&s_sum[1], gone);
+      if (i < r) atomicAdd(&s_sum[0], gone);
     }
   }
-  // ---- the rows ----
+  __syncthreads();
+  const int total = s_sum[1], mine = pages_left_over(a, r);
+  const int next = min(max(a.free_state[0], 0), a.n_free);
+  const int at = next - total + s_sum[0];
+  const int stay = mine ? (max(a.kept_len[r], 0) + (1 << a.page_log2) - 1) >> a.page_log2 : 0;
+  for (int i = threadIdx.x; i < mine; i += kMoveThreads)
+    if (at + i >= 0) a.free_pages[at + i] = a.table[(long long)r * a.width + stay + i];
+  if (r == 0 && threadIdx.x == 0) {
+    a.free_out[0] = max(0, next - total);
+    a.free_out[1] = min(a.free_state[1], a.n_free);
+    a.free_out[2] = max(0, total - next);
+  }
+}
+
+// Block: ((request, KV head) * 2 + tensor) * PARTS + part of the channels; behind them one per request for its pages.
+template <int PARTS>
+__global__ void __launch_bounds__(kMoveThreads, 2) k_page_compact(const CompactArgs a) {
+  constexpr int kLanes = 16 / PARTS, kAtOnce = kMoveThreads / kLanes;   // threads to a row's part, rows to a step
+  constexpr int kRows = kMoveSteps * kAtOnce;                           // of a round
+  extern __shared__ char s_move[];                                      // [stage][step][thread] 16 bytes
+  uint64_t* s_from = reinterpret_cast<uint64_t*>(s_move + kMoveStages * kMoveStage);
+  uint64_t* s_to = s_from + kMoveSeg;
+  const int work = 2 * PARTS * a.n_req * a.h_kv;
+  zc_let_next_start();
+  zc_wait_for_last();
+  if ((int)blockIdx.x >= work) {
+    give_back(a, blockIdx.x - work);
+    return;
+  }
+  const int tid = threadIdx.x, group = tid / kLanes;
+  const int part = blockIdx.x % PARTS, c = blockIdx.x / PARTS;
+  const int unit = c >> 1, r = unit / a.h_kv, head = unit - r * a.h_kv;
+  const bool values = c & 1;
   int n, len;
-  if (!load_kept(a, r, &n, &len)) return;   // (the whole cluster's)
+  if (!load_kept(a, r, &n, &len)) return;
+  const int32_t* table = a.table + (long long)r * a.width;
   const int32_t* kept = a.kept + (long long)unit * a.max_keep;
-  char* pool = (values ? a.v : a.k) + head * a.sh + part;
+  char* pool = (values ? a.v : a.k) + head * a.sh + part * (256 / PARTS) + (tid % kLanes) * 16;
   const int mask = (1 << a.page_log2) - 1;
   const bool weighs = a.scores && !values && part == 0;
-  const int step = a.cluster * kMoveRows;
+  const uint32_t score_bytes = 4u << a.page_log2;
+  auto score_at = [&](int page, int row) {
+    return reinterpret_cast<float*>(reinterpret_cast<char*>(a.scores) +
+                                    (uint64_t)((uint32_t)page * (uint32_t)a.h_kv + head) * score_bytes + 4u * row);
+  };
 #pragma unroll 1
-  for (int i0 = rank * kMoveRows; i0 - rank * kMoveRows < len; i0 += step) {
-    int src[kMoveUnroll], from[kMoveUnroll];
-    uint4 x[kMoveUnroll];
-    float s[kMoveUnroll];
+  for (int seg = 0; seg < len; seg += kMoveSeg) {
+    const int cnt = min(kMoveSeg, len - seg);
+    __syncthreads();   // the segment before has been written
+    constexpr int kPer = kMoveSeg / kMoveThreads;
+    int src[kPer], page[kPer], to[kPer];
 #pragma unroll
-    for (int u = 0; u < kMoveUnroll; ++u) {
-      const int i = i0 + u * (kMoveThreads / 16) + group;
-      src[u] = i < len ? kept[i] : -1;
-      if (src[u] == i || src[u] >= n) src[u] = -1;   // stays where it is
+    for (int u = 0; u < kPer; ++u) {
+      const int i = u * kMoveThreads + tid;
+      src[u] = i < cnt ? kept[seg + i] : -1;
+      to[u] = i < cnt ? table[(seg + i) >> a.page_log2] : -1;
+      if (src[u] == seg + i || src[u] >= n || to[u] < 0 || to[u] >= a.n_pages) src[u] = -1;   // stays where it is
     }
 #pragma unroll
-    for (int u = 0; u < kMoveUnroll; ++u) {
-      from[u] = src[u] >= 0 ? table[src[u] >> a.page_log2] : -1;
-      if (from[u] >= a.n_pages) from[u] = -1;
+    for (int u = 0; u < kPer; ++u) {
+      page[u] = src[u] >= 0 ? table[src[u] >> a.page_log2] : -1;
+      if (page[u] >= a.n_pages) page[u] = -1;
     }
 #pragma unroll
-    for (int u = 0; u < kMoveUnroll; ++u)
-      if (from[u] >= 0) {
-        x[u] = *reinterpret_cast<const uint4*>(pool + from[u] * a.sp + (src[u] & mask) * a.st);
-        if (weighs) s[u] = a.scores[(((long long)from[u] * a.h_kv + head) << a.page_log2) + (src[u] & mask)];
+    for (int u = 0; u < kPer; ++u) {
+      const int i = u * kMoveThreads + tid;
+      if (i >= cnt) break;
+      s_from[i] = page[u] >= 0 ? (uint32_t)page[u] * (uint64_t)a.sp + (uint32_t)(src[u] & mask) * (uint64_t)a.st : kNowhere;
+      s_to[i] = (uint32_t)max(to[u], 0) * (uint64_t)a.sp + (uint32_t)((seg + i) & mask) * (uint64_t)a.st;
+    }
+    float score[kPer];
+    if (weighs)
+#pragma unroll
+      for (int u = 0; u < kPer; ++u)
+        if (page[u] >= 0) score[u] = *score_at(page[u], src[u] & mask);
+    __syncthreads();
+    if (weighs)
+#pragma unroll
+      for (int u = 0; u < kPer; ++u)
+        if (page[u] >= 0) *score_at(to[u], (seg + u * kMoveThreads + tid) & mask) = score[u];
+    auto ask = [&](int round) {
+      char* at = s_move + (round % kMoveStages) * kMoveStage + tid * 16;
+#pragma unroll
+      for (int t = 0; t < kMoveSteps; ++t) {
+        const int i = round * kRows + t * kAtOnce + group;
+        const uint64_t from = i < cnt ? s_from[i] : kNowhere;
+        if (from != kNowhere) zc_cp_async16(at + t * (kMoveThreads * 16), pool + from);
       }
-    if (a.cluster > 1) {
-      __syncwarp();
-      asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-    } else {
-      __syncthreads();
-    }
+    };
+    const int rounds = (cnt + kRows - 1) / kRows;
 #pragma unroll
-    for (int u = 0; u < kMoveUnroll; ++u)
-      if (from[u] >= 0) {
-        const int i = i0 + u * (kMoveThreads / 16) + group, page = table[i >> a.page_log2];
-        if (page >= 0 && page < a.n_pages) {
-          *reinterpret_cast<uint4*>(pool + page * a.sp + (i & mask) * a.st) = x[u];
-          if (weighs) a.scores[(((long long)page * a.h_kv + head) << a.page_log2) + (i & mask)] = s[u];
-        }
+    for (int i = 0; i < kMoveStages - 1; ++i) {
+      if (i < rounds) ask(i);
+      zc_cp_async_commit();
+    }
+#pragma unroll 1
+    for (int round = 0; round < rounds; ++round) {
+      if (round + kMoveStages - 1 < rounds) ask(round + kMoveStages - 1);
+      zc_cp_async_commit();
+      zc_cp_async_wait<kMoveStages - 1>();
+      __syncthreads();   // every thread has its pieces of this round
+      const char* at = s_move + (round % kMoveStages) * kMoveStage + tid * 16;
+#pragma unroll
+      for (int t = 0; t < kMoveSteps; ++t) {
+        const int i = round * kRows + t * kAtOnce + group;
+        if (i < cnt && s_from[i] != kNowhere)
+          *reinterpret_cast<uint4*>(pool + s_to[i]) = *reinterpret_cast<const uint4*>(at + t * (kMoveThreads * 16));
       }
+    }
   }
 }
 
 template <int THREADS>
 cudaError_t launch_select(const SelectArgs& a, int units, cudaStream_t st) {
   static std::atomic<unsigned long long> allowed{0};
-  cudaError_t e = zc_allow_smem(k_page_select<THREADS>, kSelMost * 4, &allowed);
+  const cudaError_t e = zc_allow_smem(k_page_select<THREADS>, kSelectRoom - kSelectFixed, &allowed);
   if (e != cudaSuccess) return e;
-  return zc_launch_early(k_page_select<THREADS>, dim3(units), dim3(THREADS), (size_t)a.held * 4, st, a);
+  return zc_launch_early(k_page_select<THREADS>, dim3(units), dim3(THREADS), (size_t)a.held * 16, st, a);
+}
+template <int PARTS>
+cudaError_t launch_compact(const CompactArgs& a, cudaStream_t st) {
+  static std::atomic<unsigned long long> allowed{0};
+  const cudaError_t e = zc_allow_smem(k_page_compact<PARTS>, kMoveSmem, &allowed);
+  if (e != cudaSuccess) return e;
+  const int grid = 2 * PARTS * a.n_req * a.h_kv + (a.free_pages ? a.n_req : 0);
+  return zc_launch_early(k_page_compact<PARTS>, dim3((unsigned)grid), dim3(kMoveThreads), kMoveSmem, st, a);
 }
 
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 inline bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 struct Span { const void* at; long long bytes; };
 bool overlap(const Span& a, const Span& b) {
@@ -325,7 +422,7 @@ int zc_page_select(zc_pages* p, const int32_t* table, int table_width, const int
   if (!table || !kv_len || !scores || !keep || (!kept && max_keep) || !kept_len || table_width < 1) return ZC_EINVAL;
   const long long cap = (long long)table_width << p->page_log2, units = (long long)n_req * p->cfg.n_kv_heads;
   if (cap > ZC_NO_WINDOW || units > 0x7fffffffLL) return ZC_EINVAL;
-  if (!aligned4(table) || !aligned4(kv_len) || !aligned4(scores) || !aligned4(keep) || !aligned4(first) ||
+  if (!aligned4(table) || !aligned4(kv_len) || !aligned16(scores) || !aligned4(keep) || !aligned4(first) ||
       !aligned4(kept) || !aligned4(kept_len))
     return ZC_EALIGN;
   const Span in[5] = {{table, 4LL * n_req * table_width}, {kv_len, 4LL * n_req}, {keep, 4LL * n_req},
@@ -349,9 +446,13 @@ int zc_page_select(zc_pages* p, const int32_t* table, int table_width, const int
   a.h_kv = p->cfg.n_kv_heads;
   a.recent = recent;
   a.max_keep = max_keep;
-  a.held = (int)(cap < kSelMost ? cap : kSelMost);
-  const cudaError_t e = cap <= 2048 ? launch_select<256>(a, (int)units, (cudaStream_t)stream)
-                                    : launch_select<512>(a, (int)units, (cudaStream_t)stream);
+  // as many keys in shared memory as leave room for the CTAs that an SM has to take, four at most (2048 threads)
+  const long long per_sm = (units + p->n_sm - 1) / p->n_sm;
+  const long long room = (kSelectRoom / (per_sm < 4 ? per_sm : 4) - kSelectFixed) / 16;
+  const long long fours = cap / 4 + 1;   // (the candidates may begin inside a four)
+  a.held = (int)(fours < room ? fours : room);
+  const cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = cap <= 2048 ? launch_select<256>(a, (int)units, st) : launch_select<512>(a, (int)units, st);
   p->launches += 1;
   return zc_cuda_status((int)e);
 }
@@ -365,7 +466,7 @@ int zc_page_compact(zc_pages* p, const int32_t* table, int table_width, const in
   const bool lists = free_pages || free_state || free_out;
   if (lists && (!free_pages || !free_state || !free_out)) return ZC_EINVAL;
   const long long units = (long long)n_req * p->cfg.n_kv_heads;
-  if ((long long)table_width << p->page_log2 > ZC_NO_WINDOW || units * 2 * kMoveCluster > 0x7fffffffLL) return ZC_EINVAL;
+  if ((long long)table_width << p->page_log2 > ZC_NO_WINDOW || units * 9 > 0x7fffffffLL) return ZC_EINVAL;
   if (!aligned4(table) || !aligned4(kv_len) || !aligned4(kept) || !aligned4(kept_len) || !aligned4(scores) ||
       !aligned4(free_pages) || !aligned4(free_state) || !aligned4(free_out))
     return ZC_EALIGN;
@@ -400,21 +501,13 @@ int zc_page_compact(zc_pages* p, const int32_t* table, int table_width, const in
   a.n_pages = p->cfg.n_pages;
   a.h_kv = p->cfg.n_kv_heads;
   a.max_keep = max_keep;
-  a.cluster = 1;
-  while (a.cluster < kMoveCluster && 2 * units * a.cluster < 2 * p->n_sm) a.cluster *= 2;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(2 * units * a.cluster));
-  cfg.blockDim = dim3(kMoveThreads);
-  cfg.stream = (cudaStream_t)stream;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)a.cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = a.cluster > 1 ? 2 : 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_page_compact, (const CompactArgs)a);
+  // Whole rows where K and V of all units come to about two CTAs per SM, else as many parts as give that (measured at
+  // 2048 of 8192 tokens, whole rows / halves / quarters: 128 units 58 / 62 / 70 us, 64 units 38 / 30 / 36; 8 units, 16384 of
+  // 32768 tokens, 167 / 105 / 96).
+  const cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = 5 * units >= 4 * p->n_sm   ? launch_compact<1>(a, st)
+                        : 5 * units >= 2 * p->n_sm ? launch_compact<2>(a, st)
+                                                   : launch_compact<4>(a, st);
   p->launches += 1;
   return zc_cuda_status((int)e);
 }
