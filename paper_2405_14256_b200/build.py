@@ -14,9 +14,9 @@ LIB = os.path.join(HERE, "libzipcache.so")
 LIB_DEBUG = os.path.join(HERE, "libzipcache_debug.so")   # bounds-checked build (-DZC_DEBUG)
 SOURCES = ["zc_host.cu", "zc_scores.cu", "zc_compress.cu", "zc_decode.cu", "zc_order.cu",
            "zc_export.cu", "zc_attention.cu", "zc_pages.cu", "zc_paged_decode.cu", "zc_paged_chunk.cu",
-           "zc_paged_weights.cu", "zc_page_evict.cu"]
+           "zc_paged_own.cu", "zc_paged_weights.cu", "zc_page_evict.cu"]
 HEADERS = ["zc_internal.h", "zc_layout.cuh", "zc_mma.cuh", "zc_order.h", "zc_paged.cuh",
-           "zc_paged_tc.cuh", "zc_pages.h",
+           "zc_paged_block.cuh", "zc_paged_groups.cuh", "zc_paged_tc.cuh", "zc_pages.h",
            "zc_quant.cuh", "zc_tc.cuh"]
 
 

@@ -610,7 +610,9 @@ int zc_device_status(int* code) {
   ZC_CUDA(zc_paged_chunk_error_code(&chunk));
   int weights = 0;
   ZC_CUDA(zc_paged_weights_error_code(&weights));
-  if (*code == 0 && (paged || chunk || weights)) *code = 4;
+  int own = 0;
+  ZC_CUDA(zc_paged_own_error_code(&own));
+  if (*code == 0 && (paged || chunk || weights || own)) *code = 4;
   int dbg_c = 0, dbg_d = 0;   // bounds-checked build only: 100 + the first failed check
   ZC_CUDA(zc_debug_code_compress(&dbg_c));
   ZC_CUDA(zc_debug_code_decode(&dbg_d));

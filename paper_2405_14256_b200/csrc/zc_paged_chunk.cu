@@ -37,7 +37,7 @@
 // laid end to end with their costs, are cut into as many equal stretches as there are CTAs.  An item
 // that a border cuts is worked on in pieces along its keys; k_chunk_join puts them together in their order.
 #include <cstring>
-#include "zc_paged_tc.cuh"
+#include "zc_paged_groups.cuh"
 #include "zc_layout.cuh"
 
 namespace {
@@ -60,12 +60,9 @@ constexpr int kItemRows = 2 * kM;
 // A piece's partial result: 32 x 256 groups of 4 channels, [group of channels][row], so that the threads that
 // own neighbouring rows write neighbouring 16 bytes; then (maximum, sum) [row].
 constexpr int kPartBytes = kItemRows * ZC_D * 4 + kItemRows * 8;
+static_assert(kItemRows == ZC_CHUNK_PART_ROWS && kPartBytes == ZC_CHUNK_PART_BYTES, "as the joining kernel of groups reads them");
 constexpr int kMaxItems = 13000;                      // items of a head, and requests, that a call may have: what the
                                                       // prologue keeps in the tiles' shared memory (16 bytes each)
-// Costs as measured over mixed calls, in 220 cycles: a tile of a wide item (both groups work on it), of a narrow one
-// (the groups take turns), an item beside its tiles (Q, first product, output, masks).
-constexpr int kWideTile = 7, kNarrowTile = 5, kItemCost = 25;
-constexpr int kWorthSharing = 512;                    // keys that are not read again, from which on a group is one
 constexpr int kMinPiece = 4;                          // tiles; a shorter piece goes to its neighbour
 
 // Where a CTA's share begins: item `item` of all heads' (head * items + item of the head), key tile t of it.
@@ -86,7 +83,6 @@ struct ChunkWs {
 // What a call is about: batch rows of dense tensors, requests' chunks in pages, or groups of requests whose rows all see
 // the same first keys (no mask; every item's result is partial and joined with the rows' own keys elsewhere).
 enum { kDense = 0, kPages = 1, kGroups = 2 };
-constexpr int kMaxGroups = ZC_PAGED_MAX_GROUPS;
 
 struct ChunkArgs {
   ZcPagedArgs a;
@@ -98,18 +94,15 @@ struct ChunkArgs {
 };
 
 // A group's rows (those of its requests, which follow one another) and how many keys they share, as find_share has left it.
-__device__ __forceinline__ int group_border(const ChunkArgs& k, int g) { return min(max(k.gr.start[g], 0), k.a.n_req); }
 __device__ __forceinline__ Chunk load_group(const ChunkArgs& k, int g) {
   const ZcPagedArgs& a = k.a;
-  const int r0 = group_border(k, g), r1 = max(r0, group_border(k, g + 1));
-  const int e0 = min(max(a.row_start[r0], 0), a.n_rows), e1 = min(max(a.row_start[r1], e0), a.n_rows);
   Chunk c;
-  c.row0 = e0;
   c.p0 = k.gr.keys[g];
-  c.n = c.p0 > 0 ? e1 - e0 : 0;
+  const int r0 = group_border(a, k.gr, g), r1 = group_border(a, k.gr, g + 1);
+  c.row0 = min(max(a.row_start[r0], 0), a.n_rows);
+  c.n = c.p0 > 0 ? min(max(a.row_start[r1], 0), a.n_rows) - c.row0 : 0;
   return c;
 }
-
 __device__ __forceinline__ int item_tiles(const ZcPagedArgs& a, const Chunk& c, int tok0, int tpi) {
   const int last = min(tok0 + tpi, c.n) - 1;
   return zc_seen(c.p0 + tok0, c.p0 + last, a.window, a.sinks, kTileLog2).nb;
@@ -154,72 +147,19 @@ __device__ __forceinline__ int cut_tile(long long off, int nt, int width, int gr
 // chunk of 40 tokens, 32 heads over 8: over 1000 21.3 -> 19.0 us, over 4000 27.5 -> 23.6; shares of 25 tiles would lose 4 %).
 __device__ __forceinline__ int cut_grain(long long all, int n_cta) { return all < 8LL * kWideTile * n_cta ? kMinPiece : 1; }
 
-// How many keys each group shares: at most what the caller says and what lies before every row of its requests, in whole
-// tiles (the keys behind them are the requests' own, as far as this call goes); none where that does not pay: an item
-// costs about 25 * 220 cycles beside its tiles, the single-token kernel 20 cycles a key and request.  Every CTA finds
-// all of it and leaves it where it reads it again; whoever writes, writes the same.
-__device__ __forceinline__ void find_groups(const ChunkArgs& k, int* scratch) {
-  const ZcPagedArgs& a = k.a;
-  const int tid = threadIdx.x, n = k.gr.n;
-  int* s_border = scratch;          // requests before a group
-  int* s_keys = s_border + n + 1;
-  int* s_count = s_keys + n;        // its requests that have rows
-  const long long cap = (long long)a.table_width << a.page_log2;
-  for (int g = tid; g <= n; g += kThreads) {
-    s_border[g] = group_border(k, g);
-    if (g < n) {
-      s_keys[g] = (int)min((long long)max(k.gr.shared[g], 0), cap);
-      s_count[g] = 0;
-    }
-  }
-  __syncthreads();
-  for (int r = tid; r < a.n_req; r += kThreads) {
-    const Chunk c = load_chunk(a, r);
-    if (c.n <= 0 || r < s_border[0] || r >= s_border[n]) continue;
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-      const int m = (lo + hi) >> 1;
-      if (s_border[m] <= r) lo = m; else hi = m;
-    }
-    atomicMin(&s_keys[lo], c.p0);
-    atomicAdd(&s_count[lo], 1);
-  }
-  __syncthreads();
-  for (int g = tid; g < n; g += kThreads) {
-    const int keys = max(s_keys[g], 0) & -kN;
-    k.gr.keys[g] = (long long)(s_count[g] - 1) * keys >= kWorthSharing ? keys : 0;
-  }
-  __syncthreads();   // (a thread reads what another of its CTA has written)
-}
-// What the kernels behind this one are to know of a request: its group's keys, its first row among the group's, the group's
-// first item.
-__device__ __forceinline__ void tell_requests(const ChunkArgs& k, const int* s_start, int n_cta) {
-  const ZcPagedArgs& a = k.a;
-  for (int r = blockIdx.x + threadIdx.x * n_cta; r < a.n_req; r += kThreads * n_cta) {
-    int4 info = make_int4(0, 0, 0, 0);
-    if (r >= group_border(k, 0) && r < group_border(k, k.gr.n)) {
-      int lo = 0, hi = k.gr.n;
-      while (hi - lo > 1) {
-        const int m = (lo + hi) >> 1;
-        if (group_border(k, m) <= r) lo = m; else hi = m;
-      }
-      info = make_int4(k.gr.keys[lo], max(0, min(max(a.row_start[r], 0), a.n_rows) - load_group(k, lo).row0), s_start[lo], 0);
-    }
-    k.gr.info[r] = info;
-  }
-}
-
 // This CTA's share of a paged call, found by the whole block in shared memory (16 bytes per request or item).
 struct Share {
   Border begin, end;
   int items;          // of a head
   int r, in_req;      // the begin's request, and the item's number in it
+  Chunk c;            // that request's (or group's) rows
 };
 // What is found for all threads: the borders, and the item that the first of them lies in.
 struct Found {
   Border border[2];
   long long start, all;   // the item's cost before it, and the cost of everything
   int nt, width, r, in_req, kv;
+  Chunk c;
 };
 static_assert(sizeof(Found) <= 64, "it fits between the barriers and the sums");
 template <int FORM>
@@ -228,18 +168,25 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
   const ZcPagedArgs& a = k.a;
   const int tid = threadIdx.x, tpi = 2 * k.tpt;
   const int n_req = FORM == kGroups ? k.gr.n : a.n_req;   // (groups take the requests' place below)
-  int* s_start = reinterpret_cast<int*>(scratch);      // items before a request
+  // (the groups' tables have been made in front of the scratch)
+  const GroupTables gt(scratch, k.gr.n, a.n_req);
+  int* s_start = reinterpret_cast<int*>(scratch) + (FORM == kGroups ? GroupTables::kInts : 0);   // items before a request
   int* s_n = s_start + n_req + 1;
   int* s_p0 = s_n + n_req;
   int* s_cost = s_p0 + n_req;                          // cost of the head's items before an item
-  if (FORM == kGroups) find_groups(k, s_cost);
   int items = 0;
   for (int c0 = 0; c0 < n_req; c0 += kThreads) {
     const int r = c0 + tid;
     Chunk c;
     c.n = c.p0 = 0;
     if (r < n_req) {
-      c = FORM == kGroups ? load_group(k, r) : load_chunk(a, r);
+      if (FORM == kGroups) {
+        c.p0 = gt.keys[r];
+        c.n = c.p0 > 0 ? gt.row[r + 1] - gt.row[r] : 0;
+        k.gr.keys[r] = c.p0;   // (every CTA leaves the same where it reads it again)
+      } else {
+        c = load_chunk(a, r);
+      }
       s_n[r] = c.n;
       s_p0[r] = c.p0;
     }
@@ -252,7 +199,14 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
   }
   if (tid == 0) s_start[n_req] = items;
   __syncthreads();
-  if (FORM == kGroups) tell_requests(k, s_start, n_cta);
+  if (FORM == kGroups) {
+    // what the joining kernel is to know of a request: its group's keys, its first row among the group's, the first item
+    if (blockIdx.x == 0 && tid == 0) *k.gr.head = n_cta;
+    for (int r = blockIdx.x + tid * n_cta; r < a.n_req; r += kThreads * n_cta) {
+      const int g = gt.group_of(r);
+      k.gr.info[r] = g < 0 ? make_int4(0, 0, 0, 0) : make_int4(gt.keys[g], max(0, gt.chunk(a, r).row0 - gt.row[g]), s_start[g], 0);
+    }
+  }
   auto request = [&](int i) {
     int lo = 0, hi = n_req;
     while (hi - lo > 1) {
@@ -299,6 +253,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
     Found f;
     f.start = f.all = all;
     f.nt = f.width = f.r = f.in_req = f.kv = 0;
+    f.c.row0 = f.c.n = f.c.p0 = 0;
     if (at < all) {
       const int kv = all < (1 << 24) ? (int)((uint32_t)at / (uint32_t)head) : (int)(at / head);
       const long long in = at - kv * head;
@@ -322,6 +277,11 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
         f.r = request(next);
         f.in_req = next - s_start[f.r];
       }
+      if (tid == 0) {
+        f.c.n = s_n[f.r];
+        f.c.p0 = s_p0[f.r];
+        f.c.row0 = FORM == kGroups ? gt.row[f.r] : load_chunk(a, f.r).row0;
+      }
     }
     s_found->border[tid] = b;
     if (tid == 0) {
@@ -332,6 +292,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
       s_found->r = f.r;
       s_found->in_req = f.in_req;
       s_found->kv = f.kv;
+      s_found->c = f.c;
     }
   }
   async_proxy_fence();   // the scratch's place is the tiles' from here on, whose copies come by the other proxy
@@ -342,6 +303,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
   s.items = items;
   s.r = s_found->r;
   s.in_req = s_found->in_req;
+  s.c = s_found->c;
   if (tid == kThreads - 1) {
     // (a thread that has nothing to do yet) what k_chunk_join is to know of the border before this CTA
     const Found f = *s_found;
@@ -357,15 +319,18 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
       while (j.first > 1 && cuts(j.first - 1)) --j.first;
       if (j.first == c) {
         while (j.last + 1 < n_cta && cuts(j.last + 1)) ++j.last;
-        const Chunk q = FORM == kGroups ? load_group(k, f.r) : load_chunk(a, f.r);
         j.on = 1;
-        j.row0 = q.row0;
-        j.n = q.n;
+        if (FORM != kGroups) {
+          const Chunk q = load_chunk(a, f.r);
+          j.row0 = q.row0;
+          j.n = q.n;
+        }
         j.tok0 = f.in_req * tpi;
         j.kv = f.kv;
       }
     }
     k.ws.joins[c] = j;
+    if (FORM == kGroups) k.gr.last[c] = j.on ? j.last : c;
     k.ws.used[c] = s.begin.item < s.end.item || s.begin.t < s.end.t;
   }
   return s;
@@ -518,7 +483,20 @@ __global__ void __launch_bounds__(kThreads, 1)
   float2* s_ms = reinterpret_cast<float2*>(base + kTiles + 448);                    // [128] narrow items: group 1's (m, sum)
   int* ring = reinterpret_cast<int*>(base + kTiles + 448 + 1024);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  zc_let_next_start();
+  int n_cta = gridDim.x;
+  if (FORM == kGroups) {
+    // The kernel behind this one, of the requests' own keys, does not wait for it: it takes the CTAs that are not needed
+    // here.  So it may start only once what came before both is complete.
+    zc_wait_for_last();
+    zc_let_next_start();
+    n_cta = plan_groups<kThreads>(a, k.gr, GroupTables(base, k.gr.n, a.n_req), k.tpt, gridDim.x);
+    if (blockIdx.x == 0 && tid == 0) *reinterpret_cast<volatile int*>(k.gr.told) = 1 + n_cta;
+    if (n_cta == 0)
+      for (int r = blockIdx.x + tid * gridDim.x; r < a.n_req; r += kThreads * gridDim.x) k.gr.info[r] = make_int4(0, 0, 0, 0);
+    if ((int)blockIdx.x >= n_cta) return;
+  } else {
+    zc_let_next_start();
+  }
   if (tid == 0) {
     for (int i = 0; i < 4; ++i) bar_init(&q_full[i], 1);   // q_free too
     bar_init(&m_free[0], 1);
@@ -559,9 +537,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);
-  zc_wait_for_last();
+  if (FORM != kGroups) zc_wait_for_last();
   Share share;
-  if (PAGED) share = find_share<FORM>(k, base, reinterpret_cast<long long*>(s_ms), reinterpret_cast<Found*>(base + kTiles + 384), gridDim.x);
+  if (PAGED) share = find_share<FORM>(k, base, reinterpret_cast<long long*>(s_ms), reinterpret_cast<Found*>(base + kTiles + 384), n_cta);
 
   uint32_t n_item = 0;   // items taken from the ring
   // Next item of the ring; a whole warp calls.  False: there are no more (or a wait ran out).
@@ -642,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       Chunk c;
       c.row0 = c.n = c.p0 = 0;
       auto load = [&](int i) { return FORM == kGroups ? load_group(k, i) : load_chunk(a, i); };
-      if (PAGED && share.items > 0) c = load(r);
+      if (PAGED && share.items > 0) c = share.c;
       auto find_item = [&](Item& it) {   // the share's next item; r < 0: there is none
         it.r = -1;
         if (!PAGED) {
@@ -657,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (at.item > share.end.item || (at.item == share.end.item && at.t >= share.end.t)) return;
         // (only the share's first item can begin, and only its last can end, inside)
-        it.r = FORM == kGroups ? group_border(k, r) : r;   // the first request's table has the group's pages
+        it.r = FORM == kGroups ? group_border(a, k.gr, r) : r;   // the first request's table has the group's pages
         it.kv = at.item / share.items;
         it.tok0 = in_req * 2 * k.tpt;
         it.row0 = c.row0;
@@ -1191,59 +1169,6 @@ template <typename T> __global__ void __launch_bounds__(256) k_chunk_join(const 
   if (a.lse && cg == 0) a.lse[at] = sum > 0.f ? m + log2f(sum) : -INFINITY;
 }
 
-// The rows of groups: what they have from the shared keys, whole or in pieces, and from their own.  A warp has a row, a
-// lane four channels of it.
-template <typename T> __global__ void __launch_bounds__(256) k_group_join(const ChunkArgs k, const float* own, int n_cta) {
-  zc_let_next_start();
-  zc_wait_for_last();
-  const ZcPagedArgs& a = k.a;
-  const int lane = threadIdx.x & 31;
-  const long long idx = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int per_req = a.max_rows * a.h_q, r = (int)(idx / per_req), in = (int)(idx - (long long)r * per_req);
-  if (r >= a.n_req) return;
-  const int t = in / a.h_q, head = in - t * a.h_q;
-  const int4 info = k.gr.info[r];
-  const Chunk c = load_chunk(a, r);
-  if (t >= c.n || info.x <= 0) return;
-  const long long at = (long long)(c.row0 + t) * a.h_q + head;
-  const float* mine = own + at * ZC_PART_STRIDE;
-  const float2 ms0 = *reinterpret_cast<const float2*>(mine);
-  const float4 x0 = *reinterpret_cast<const float4*>(mine + 4 + 4 * lane);
-  const int kv = head / a.G, tok = info.y + t, tpi = 2 * k.tpt, item = tok / tpi;
-  const int tok_in = tok - item * tpi, half = tok_in >= k.tpt;
-  const int prow = half * kM + (tok_in - half * k.tpt) * a.G + head - kv * a.G;
-  if (info.z + item >= k.gr.most) return;   // (lengths that contradict one another)
-  int cut = k.gr.cut[(long long)(info.z + item) * a.h_kv + kv];
-  if (cut < 0 || cut >= n_cta) cut = 0;   // (only where a wait has run out)
-  float m = ms0.x, sum = ms0.y;
-  float4 acc = x0;
-  auto take = [&](float2 ms, float4 x) {
-    const float top = fmaxf(m, ms.x), fo = zc_exp2(m - top), fn = zc_exp2(ms.x - top);
-    m = top;
-    sum = fmaf(sum, fo, ms.y * fn);
-    acc.x = fmaf(acc.x, fo, x.x * fn);
-    acc.y = fmaf(acc.y, fo, x.y * fn);
-    acc.z = fmaf(acc.z, fo, x.z * fn);
-    acc.w = fmaf(acc.w, fo, x.w * fn);
-  };
-  auto piece = [&](int slot) {
-    const char* p = k.ws.parts + (long long)slot * kPartBytes;
-    take(reinterpret_cast<const float2*>(p + kItemRows * ZC_D * 4)[prow],
-         reinterpret_cast<const float4*>(p)[lane * kItemRows + prow]);
-  };
-  if (cut == 0) {
-    const float* w = k.gr.rows + at * ZC_PART_STRIDE;
-    take(*reinterpret_cast<const float2*>(w), *reinterpret_cast<const float4*>(w + 4 + 4 * lane));
-  } else {
-    const int last = min(k.ws.joins[cut].last, n_cta - 1);
-    piece(2 * (cut - 1) + 1);
-#pragma unroll 4
-    for (int d = cut; d <= last; ++d)
-      if (k.ws.used[d]) piece(2 * d);
-  }
-  store_row<T>(a.out, a.lse, at, lane, m, sum, acc);
-}
-
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 // Places of the parts of a call's workspace; returns the bytes.
 size_t carve(char* ws, ChunkWs* out) {
@@ -1303,11 +1228,11 @@ cudaError_t launch_groups(zc_pages* p, const ChunkArgs& k, const CUtensorMap& qm
   return zc_launch_early(k_chunk_attention<T, kGroups>, dim3(p->n_sm), dim3(kThreads), kSmem, st, k, qmap, p->k64, p->v64);
 }
 
-// Items that a head can have: whole ones, and a part of one for each request.
-int most_items(int G, int n_req, int n_rows) { return n_rows / (2 * tokens_per_tile(G)) + n_req; }
+// Items that a head can have: whole ones, and a part of one for each group.
+int most_items(int G, int n_groups, int n_rows) { return n_rows / (2 * tokens_per_tile(G)) + n_groups; }
 
 // Places of the parts of a shared call's workspace, behind a chunk call's; returns the bytes.
-size_t carve_groups(const zc_page_config& c, int n_req, int n_rows, char* ws, ZcGroups* gr, char** own, char** parts) {
+size_t carve_groups(const zc_page_config& c, int n_req, int n_rows, char* ws, ZcGroups* gr) {
   const int G = c.n_q_heads / c.n_kv_heads;
   size_t off = carve(nullptr, nullptr);
   auto take = [&](size_t bytes) {
@@ -1315,28 +1240,27 @@ size_t carve_groups(const zc_page_config& c, int n_req, int n_rows, char* ws, Zc
     off += round_up(bytes);
     return p;
   };
-  char* p0 = take(zc_paged_decode_workspace());
-  int4* info = (int4*)take((size_t)n_req * sizeof(int4));
-  int* keys = (int*)take(kMaxGroups * sizeof(int));
-  int* cut = (int*)take((size_t)most_items(G, n_req, n_rows) * c.n_kv_heads * sizeof(int));
-  const size_t rows = (size_t)n_rows * c.n_q_heads * ZC_PART_STRIDE * 4;
-  float* shared_rows = (float*)take(rows);
-  char* own_rows = take(rows);
-  if (gr) {
-    gr->info = info;
-    gr->keys = keys;
-    gr->cut = cut;
-    gr->rows = shared_rows;
-    *own = own_rows;
-    *parts = p0;
-  }
+  ZcGroups g;
+  memset(&g, 0, sizeof(g));
+  g.told = (int*)ws + ZC_PAGED_MAX_CTAS + 2;
+  g.head = (int*)take(sizeof(int));
+  g.keys = (int*)take(kMaxGroups * sizeof(int));
+  g.last = (int*)take(ZC_PAGED_MAX_CTAS * sizeof(int));
+  g.info = (int4*)take((size_t)n_req * sizeof(int4));
+  g.own = (int4*)take((size_t)n_req * sizeof(int4));
+  g.cut = (int*)take((size_t)most_items(G, n_req, n_rows) * c.n_kv_heads * sizeof(int));
+  const size_t row = (size_t)c.n_q_heads * ZC_PART_STRIDE * 4;
+  g.rows = (float*)take(n_rows * row);
+  g.own_most = 2 * n_rows + 512;
+  g.own_rows = (float*)take(g.own_most * row);
+  if (gr) *gr = g;
   return off;
 }
 
 }  // namespace
 
 size_t zc_paged_shared_workspace(const zc_page_config& c, int n_req, int n_rows) {
-  return carve_groups(c, n_req, n_rows, nullptr, nullptr, nullptr, nullptr);
+  return carve_groups(c, n_req, n_rows, nullptr, nullptr);
 }
 
 int zc_launch_paged_shared(zc_pages* p, const ZcPagedArgs& a, const int32_t* group_start, const int32_t* shared_len,
@@ -1346,13 +1270,13 @@ int zc_launch_paged_shared(zc_pages* p, const ZcPagedArgs& a, const int32_t* gro
   memset(&k, 0, sizeof(k));
   k.a = a;
   carve(ws, &k.ws);
-  ZcDecodeMore more = {};
-  char* own = nullptr;
-  carve_groups(p->cfg, a.n_req, a.n_rows, ws, &k.gr, &own, &more.parts);
+  carve_groups(p->cfg, a.n_req, a.n_rows, ws, &k.gr);
   k.gr.start = group_start;
   k.gr.shared = shared_len;
   k.gr.n = n_groups;
-  k.gr.most = most_items(a.G, a.n_req, a.n_rows);
+  k.gr.most = most_items(a.G, n_groups < a.n_req ? n_groups : a.n_req, a.n_rows);
+  k.gr.used = k.ws.used;
+  k.gr.parts = k.ws.parts;
   k.tpt = tokens_per_tile(a.G);
   k.o_row = (long long)a.h_q * ZC_D;
   k.o_head = ZC_D;
@@ -1360,21 +1284,11 @@ int zc_launch_paged_shared(zc_pages* p, const ZcPagedArgs& a, const int32_t* gro
   memset(&qmap, 0, sizeof(qmap));
   if (!make_q_map(&qmap, a.q, p->cfg.dtype, a.h_q, a.G, a.n_rows, 1, a.qs_head, a.qs_row, 0))
     return (int)cudaErrorNotSupported;
-  const bool half = p->cfg.dtype == ZC_F16;
-  cudaError_t e = half ? launch_groups<__half>(p, k, qmap, st) : launch_groups<__nv_bfloat16>(p, k, qmap, st);
+  const cudaError_t e = p->cfg.dtype == ZC_F16 ? launch_groups<__half>(p, k, qmap, st)
+                                               : launch_groups<__nv_bfloat16>(p, k, qmap, st);
   if (e != cudaSuccess) return (int)e;
   p->launches += 1;
-  more.logits = logits;
-  more.info = k.gr.info;
-  more.rows = (float*)own;
-  e = (cudaError_t)zc_launch_paged_decode(p, a, more, ws, st);
-  if (e != cudaSuccess) return (int)e;
-  const long long blocks = ((long long)a.n_req * a.max_rows * a.h_q + 7) / 8;
-  if (blocks > 0x7fffffffLL) return (int)cudaErrorInvalidConfiguration;
-  e = half ? zc_launch_early(k_group_join<__half>, dim3((unsigned)blocks), dim3(256), 0, st, k, (float*)own, p->n_sm)
-           : zc_launch_early(k_group_join<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, st, k, (float*)own, p->n_sm);
-  if (e == cudaSuccess) p->launches += 1;
-  return (int)e;
+  return zc_launch_own_keys(p, a, k.gr, k.tpt, logits, st);
 }
 
 size_t zc_paged_chunk_workspace() { return carve(nullptr, nullptr); }

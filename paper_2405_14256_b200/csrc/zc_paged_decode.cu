@@ -21,16 +21,11 @@
 // 48.2 us, 5.6 TB/s; 4 requests of 200-512 tokens: 7.6 us, of which launch, lengths and tables, one round trip to the
 // keys and the join are all.
 #include <cstring>
-#include "zc_pages.h"
-#include "zc_layout.cuh"
-#include "zc_tc.cuh"
-#include "zc_paged.cuh"
+#include "zc_paged_block.cuh"
 
 namespace {
 
 constexpr int kDecWarps = 8, kDecThreads = 32 * kDecWarps;
-constexpr int kBlkLog2 = 4, kBlk = 1 << kBlkLog2;      // keys of a block
-constexpr int kHalf = kBlk * ZC_D * 2;                 // 4 KB: keys (or values) of a stage, [2][16][128 B]
 constexpr int kStages = 2;                              // 3 measured 229 against 216 us (32 x 2048-4096 tokens, 32 KV heads)
 constexpr int kRing = kDecWarps * kStages * 2 * kHalf;  // 128 KB
 constexpr int kJoinStride = ZC_PART_STRIDE;            // m, sum, -, -, acc[128]
@@ -43,14 +38,11 @@ constexpr int kDecSmem = kRing + kJoinBytes + kDecWarps * kStages * 8 + kScanByt
 constexpr int kWhole = 5;
 constexpr int kLeast = 3;
 static_assert(ZC_PAGED_MAX_CTAS * 4 <= ZC_PAGES_SYNC_BYTES, "a counter per CTA");
-constexpr float kTau = 8.f;
-
 struct Req {
   int row0, n, p0;   // first row, rows, position of the first
   ZcSeen s;
 };
-template <int MODE>
-__device__ __forceinline__ int load_req(const ZcPagedArgs& a, const ZcDecodeMore& more, int r, Req* q) {
+__device__ __forceinline__ int load_req(const ZcPagedArgs& a, int r, Req* q) {
   const int e0 = min(max(a.row_start[r], 0), a.n_rows);
   const int e1 = min(max(a.row_start[r + 1], e0), a.n_rows);
   const long long cap = (long long)a.table_width << a.page_log2;
@@ -59,11 +51,6 @@ __device__ __forceinline__ int load_req(const ZcPagedArgs& a, const ZcDecodeMore
   q->n = min(e1 - e0, a.max_rows);
   q->p0 = kv - (e1 - e0);
   q->s = zc_seen(q->p0, q->p0 + q->n - 1, a.window, a.sinks, kBlkLog2);
-  if (MODE & ZC_DEC_SHARED) {   // the keys before are the group's (a multiple of the block, and before every row)
-    q->s.lo = more.info[r].x;
-    q->s.wb0 = q->s.lo >> kBlkLog2;
-    q->s.nb = max(0, q->s.nb - q->s.wb0);
-  }
   return q->n > 0 ? max(1, (q->s.nb + kDecWarps - 1) / kDecWarps) : 0;
 }
 
@@ -86,14 +73,13 @@ struct Seg {
   long long left;   // steps of the share after this segment
   Req q;
 };
-template <int MODE>
-__device__ __forceinline__ bool seg_next(const ZcPagedArgs& a, const ZcDecodeMore& more, Seg& g) {
+__device__ __forceinline__ bool seg_next(const ZcPagedArgs& a, Seg& g) {
   if (g.left <= 0) return false;
   if (++g.kv == a.h_kv) {
     g.kv = 0;
     do {
       if (++g.r >= a.n_req) return false;
-      g.steps = load_req<MODE>(a, more, g.r, &g.q);
+      g.steps = load_req(a, g.r, &g.q);
     } while (g.steps == 0);
   }
   g.a = 0;
@@ -102,29 +88,10 @@ __device__ __forceinline__ bool seg_next(const ZcPagedArgs& a, const ZcDecodeMor
   return true;
 }
 
-__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
-  uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
-  return y;
-}
-__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr)
-               : "memory");
-}
-__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr)
-               : "memory");
-}
-
-// NT: groups of 8 rows.  MODE: ZC_DEC_WEIGHTS, the logits are kept for zc_launch_score_add; ZC_DEC_SHARED, a request's first
-// keys are another kernel's, and its rows' results go to where the two are joined.
-template <typename T, int NT, int MODE>
+// NT: groups of 8 rows.  WEIGHTS: the logits are kept for zc_launch_score_add.
+template <typename T, int NT, bool WEIGHTS>
 __global__ void __launch_bounds__(kDecThreads, 1)
-    k_paged_decode(const ZcPagedArgs a, const ZcDecodeMore more, float* __restrict__ parts, unsigned* __restrict__ arrived,
+    k_paged_decode(const ZcPagedArgs a, float* logits, float* __restrict__ parts, unsigned* __restrict__ arrived,
                    const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
   extern __shared__ __align__(1024) char smem_raw[];
   const uint32_t raw_u = zc_smem_u32(smem_raw);
@@ -149,7 +116,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
   int mine = 0;   // steps of this thread's request (of the last one, where there are more requests than threads)
   Req mq;
   for (int r = tid; r < a.n_req; r += kDecThreads) {
-    mine = load_req<MODE>(a, more, r, &mq);
+    mine = load_req(a, r, &mq);
     sum += mine;
   }
   long long incl = sum;
@@ -198,7 +165,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
   } else {
     long long before = 0;
     for (int c0 = 0; c0 < a.n_req; c0 += kDecThreads) {
-      mine = c0 + tid < a.n_req ? load_req<MODE>(a, more, c0 + tid, &mq) : 0;
+      mine = c0 + tid < a.n_req ? load_req(a, c0 + tid, &mq) : 0;
       incl = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -231,7 +198,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
   if (seg.a == seg.steps) {   // the border was moved to the unit's end: the share begins with the next unit
     unit0 += seg.steps;
     seg.left = end - begin;
-    seg_next<MODE>(a, more, seg);
+    seg_next(a, seg);
   } else {
     seg.b = (int)min((long long)seg.steps, seg.a + (end - begin));
     seg.left = (end - begin) - (seg.b - seg.a);
@@ -252,7 +219,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
           return;
         }
       }
-      if (!seg_next<MODE>(a, more, ps)) {
+      if (!seg_next(a, ps)) {
         pkey = -1;
         return;
       }
@@ -265,7 +232,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
   int held[2] = {0, 0};   // pages of the blocks in the two stages
   auto issue = [&](int stage) {
     if (pkey < 0) return;
-    if (MODE & ZC_DEC_WEIGHTS) held[0] = stage == 0 ? ppage : held[0], held[1] = stage == 1 ? ppage : held[1];
+    if (WEIGHTS) held[0] = stage == 0 ? ppage : held[0], held[1] = stage == 1 ? ppage : held[1];
     if (lane == 0) {
       const int page = ppage >= 0 && ppage < a.n_pages ? ppage : a.n_pages;   // beyond the pool: arrives as zeros
       const int row = pkey & ((1 << a.page_log2) - 1);
@@ -301,57 +268,18 @@ __global__ void __launch_bounds__(kDecThreads, 1)
       acc.w = fmaf(x.w, f, acc.w);
     }
   };
-  // A row's result: the output, or what is joined with that over the group's keys.
-  auto put = [&](const Req& q, long long at, float m, float sum, float4 acc) {
-    if ((MODE & ZC_DEC_SHARED) && q.s.lo > 0) {
-      float* to = more.rows + at * kJoinStride;
-      if (lane == 0) *reinterpret_cast<float2*>(to) = make_float2(m, sum);
-      *reinterpret_cast<float4*>(to + 4 + 4 * lane) = acc;
-    } else {
-      store_row<T>(a.out, a.lse, at, lane, m, sum, acc);
-    }
-  };
-  const float scale = kLog2e * rsqrtf((float)ZC_D);
   const int quad = lane & 3, oct = lane >> 2;
   int stage = 0;
   uint32_t phase = 0;
   for (;;) {
     const int rows = seg.q.n * a.G;
-    // this unit's query rows as B fragments: row = oct + 8 nt, two consecutive channels a register
     uint32_t qf[NT][8][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int row = oct + 8 * nt, tok = row / a.G;
-      const T* qp = reinterpret_cast<const T*>(a.q) + (long long)(seg.q.row0 + tok) * a.qs_row +
-                    (long long)(seg.kv * a.G + (row - tok * a.G)) * a.qs_head + 2 * quad;
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        qf[nt][ks][0] = row < rows ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks) : 0u;
-        qf[nt][ks][1] = row < rows ? *reinterpret_cast<const uint32_t*>(qp + 16 * ks + 8) : 0u;
-      }
-    }
-    // positions of this thread's rows (rows 2 quad, 2 quad + 1 of each group of 8)
     int pos[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int row = 8 * nt + 2 * quad + e;
-        pos[nt][e] = row < rows ? seg.q.p0 + row / a.G : -1;
-      }
+    load_rows<T, NT>(a, seg.q.row0, seg.kv, rows, qf);
+    row_positions<NT>(a, seg.q.p0, rows, pos);
     const int p_last = seg.q.p0 + seg.q.n - 1;
-    float o[NT][8][4], m[NT][2], s[NT][2], raw[NT][2];   // raw: q.k of the maximum
-    bool far = false;                                    // a row of the warp has its maximum beyond kFarMax
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
-      m[nt][0] = m[nt][1] = kNoMax;
-      raw[nt][0] = raw[nt][1] = 0.f;
-      s[nt][0] = s[nt][1] = 0.f;
-    }
+    RowState<NT> x;
+    x.clear();
     for (int step = seg.a; ok && step < seg.b; ++step) {
       const int vb = step * kDecWarps + warp;
       if (vb >= seg.q.s.nb) break;
@@ -359,125 +287,12 @@ __global__ void __launch_bounds__(kDecThreads, 1)
       const uint32_t kt = ring + stage * 2 * kHalf, vt = kt + kHalf;
       ok = warp_wait(&full[stage], phase);
       if (!ok) break;   // nothing more is copied; the unit's other warps are met below
-      // ---- S^T = K Q^T ----
-      float sc[NT][4];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sc[nt][e] = 0.f;
-      const int lrow = lane & 15;                         // matrices 0, 2: keys 0-7; 1, 3: keys 8-15
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        const int chunk = 2 * ks + (lane >> 4);
-        uint32_t kf[4];
-        ldmatrix_x4(kf, kt + (chunk >> 3) * (kBlk * 128) + lrow * 128 + (((chunk & 7) ^ (lrow & 7)) << 4));
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) zc_mma16816<T>(sc[nt], kf, qf[nt][ks][0], qf[nt][ks][1]);
+      float* keep = nullptr;
+      if (WEIGHTS) {
+        const int page = stage == 0 ? held[0] : held[1];
+        if (page >= 0 && page < a.n_pages) keep = logits_of(logits, a, page, seg.kv, key0);
       }
-      // ---- masks: only blocks at a border ----
-      if (key0 + kBlk - 1 > seg.q.p0 || (key0 <= p_last - a.window && key0 + kBlk > a.sinks)) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int key = key0 + oct + 8 * (e >> 1), p = pos[nt][e & 1];
-            const bool seen = key <= p && (key > p - a.window || key < a.sinks);
-            if (!seen) sc[nt][e] = -INFINITY;
-          }
-        // values that no row sees may hold anything (2^-inf = 0 times NaN is NaN): zeros in their place
-        const int vr = lane >> 1, vkey = key0 + vr;
-        const bool dead = vkey >= seg.q.s.hi || (vkey < seg.q.s.lo && vkey >= seg.q.s.sink_n);
-        if (dead) {
-          char* at = base + (vt - base_u) + (lane & 1) * (kBlk * 128) + vr * 128;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(at + 16 * i) = make_uint4(0, 0, 0, 0);
-        }
-        async_proxy_fence();   // the stage's next copy is ordered behind these stores
-        __syncwarp();
-      }
-      // ---- the logits, for the keys' weights: [page][KV head][token][row] ----
-      if (MODE & ZC_DEC_WEIGHTS) {
-        const int page = stage == 0 ? held[0] : held[1], per = a.max_rows * a.G;
-        if (page >= 0 && page < a.n_pages) {
-          float* at = more.logits + ((((long long)page * a.h_kv + seg.kv) << a.page_log2) +
-                                     (key0 & ((1 << a.page_log2) - 1)) + oct) * per;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int row = 8 * nt + 2 * quad + (e & 1);
-              if (row < rows) at[(e >> 1) * 8 * per + row] = sc[nt][e] * scale;
-            }
-        }
-      }
-      // ---- running maximum and sum ----
-      uint32_t pf[NT][2], rest[NT][2];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float mx[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          mx[e] = fmaxf(sc[nt][e], sc[nt][e + 2]);
-#pragma unroll
-          for (int x = 4; x < 32; x <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], x));
-        }
-        const float top[2] = {mx[0], mx[1]};
-        mx[0] *= scale;
-        mx[1] *= scale;
-        const bool grow0 = mx[0] > m[nt][0] + kTau, grow1 = mx[1] > m[nt][1] + kTau;
-        if (__any_sync(0xffffffffu, grow0 || grow1)) {
-          const float al0 = grow0 ? zc_exp2(m[nt][0] - mx[0]) : 1.f, al1 = grow1 ? zc_exp2(m[nt][1] - mx[1]) : 1.f;
-          if (grow0) m[nt][0] = mx[0];
-          if (grow1) m[nt][1] = mx[1];
-          if (grow0) raw[nt][0] = top[0];
-          if (grow1) raw[nt][1] = top[1];
-          far = far || __any_sync(0xffffffffu, !(fmaxf(grow0 ? fabsf(mx[0]) : 0.f, grow1 ? fabsf(mx[1]) : 0.f) < kFarMax));
-          s[nt][0] *= al0;
-          s[nt][1] *= al1;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            o[nt][i][0] *= al0;
-            o[nt][i][1] *= al1;
-            o[nt][i][2] *= al0;
-            o[nt][i][3] *= al1;
-          }
-        }
-        float less[2] = {m[nt][0], m[nt][1]};
-        if (far) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc[nt][e] -= raw[nt][e & 1];
-          less[0] = less[1] = 0.f;
-        }
-        const float p0 = zc_exp2(fmaf(sc[nt][0], scale, -less[0])), p1 = zc_exp2(fmaf(sc[nt][1], scale, -less[1]));
-        const float p2 = zc_exp2(fmaf(sc[nt][2], scale, -less[0])), p3 = zc_exp2(fmaf(sc[nt][3], scale, -less[1]));
-        s[nt][0] += p0 + p2;
-        s[nt][1] += p1 + p3;
-        const uint32_t w0 = pack2<T>(p0, p1), w1 = pack2<T>(p2, p3);   // keys 0-7 of the block, keys 8-15
-        const float2 h0 = unpack2<T>(w0), h1 = unpack2<T>(w1);
-        pf[nt][0] = movmatrix_trans(w0);
-        pf[nt][1] = movmatrix_trans(w1);
-        rest[nt][0] = movmatrix_trans(pack2<T>(p0 - h0.x, p1 - h0.y));
-        rest[nt][1] = movmatrix_trans(pack2<T>(p2 - h1.x, p3 - h1.y));
-      }
-      // ---- O^T += V^T P^T ----
-      const int vrow = (lane & 7) + ((lane >> 4) << 3);   // matrices 0, 1: keys 0-7; 2, 3: keys 8-15
-#pragma unroll
-      for (int m2 = 0; m2 < 8; m2 += 2) {   // two tiles of channels at a time, so that no product waits for the one before
-        uint32_t vf[2][4];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int chunk = 2 * (m2 + u) + ((lane >> 3) & 1);
-          ldmatrix_x4_trans(vf[u], vt + (chunk >> 3) * (kBlk * 128) + vrow * 128 + (((chunk & 7) ^ (vrow & 7)) << 4));
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) zc_mma16816<T>(o[nt][m2 + u], vf[u], pf[nt][0], pf[nt][1]);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) zc_mma16816<T>(o[nt][m2 + u], vf[u], rest[nt][0], rest[nt][1]);
-      }
+      attend_block<T, NT, WEIGHTS>(x, qf, pos, kt, vt, base + (vt - base_u), key0, seg.q.p0, p_last, seg.q.s, a, rows, keep);
       __syncwarp();
       issue(stage);
       if (++stage == kStages) {
@@ -495,18 +310,18 @@ __global__ void __launch_bounds__(kDecThreads, 1)
       __syncthreads();   // the join area is free
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float t = s[nt][e];
+        float t = x.s[nt][e];
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) t += __shfl_xor_sync(0xffffffffu, t, x);
         float* jr = s_join + (warp * 8 + 2 * quad + e) * kJoinStride;
         if (oct == 0) {
-          jr[0] = m[nt][e];
+          jr[0] = x.m[nt][e];
           jr[1] = t;
         }
 #pragma unroll
         for (int mt = 0; mt < 8; ++mt) {
-          jr[4 + 16 * mt + oct] = o[nt][mt][e];
-          jr[4 + 16 * mt + oct + 8] = o[nt][mt][e + 2];
+          jr[4 + 16 * mt + oct] = x.o[nt][mt][e];
+          jr[4 + 16 * mt + oct + 8] = x.o[nt][mt][e + 2];
         }
       }
       __syncthreads();
@@ -518,7 +333,7 @@ __global__ void __launch_bounds__(kDecThreads, 1)
         if (whole) {
           const int tok = row / a.G;
           const long long at = (long long)(seg.q.row0 + tok) * a.h_q + seg.kv * a.G + (row - tok * a.G);
-          put(seg.q, at, mt, total_s, acc);
+          store_row<T>(a.out, a.lse, at, lane, mt, total_s, acc);
         } else {
           float* pr = slot + row * kJoinStride;
           if (lane == 0) {
@@ -602,44 +417,34 @@ __global__ void __launch_bounds__(kDecThreads, 1)
             float4 acc8;
             meet(m8, sum8, acc8);
             const int tok = row / a.G;
-            put(seg.q, (long long)(seg.q.row0 + tok) * a.h_q + seg.kv * a.G + (row - tok * a.G), m8, sum8, acc8);
+            store_row<T>(a.out, a.lse, (long long)(seg.q.row0 + tok) * a.h_q + seg.kv * a.G + (row - tok * a.G), lane, m8, sum8, acc8);
           }
         }
         if (tid == 0) arrived[c0] = 0;   // as the next call wants it
       }
     }
     unit0 += seg.steps;
-    if (!seg_next<MODE>(a, more, seg)) break;
+    if (!seg_next(a, seg)) break;
   }
   if (!ok)   // the copies that were on their way
     for (int i = 0; i < kStages; ++i) drain(&full[i], i < stage ? phase ^ 1u : phase);
 }
 
-template <typename T, int NT, int MODE>
-int launch(zc_pages* p, const ZcPagedArgs& a, const ZcDecodeMore& more, float* parts, unsigned* arrived, cudaStream_t st) {
+template <typename T, int NT, bool WEIGHTS>
+int launch(zc_pages* p, const ZcPagedArgs& a, float* logits, float* parts, unsigned* arrived, cudaStream_t st) {
   static std::atomic<unsigned long long> allowed{0};
-  cudaError_t e = zc_allow_smem(k_paged_decode<T, NT, MODE>, kDecSmem, &allowed);
+  cudaError_t e = zc_allow_smem(k_paged_decode<T, NT, WEIGHTS>, kDecSmem, &allowed);
   if (e != cudaSuccess) return e;
-  e = zc_launch_early(k_paged_decode<T, NT, MODE>, dim3(p->n_sm), dim3(kDecThreads), kDecSmem, st, a, more, parts, arrived,
+  e = zc_launch_early(k_paged_decode<T, NT, WEIGHTS>, dim3(p->n_sm), dim3(kDecThreads), kDecSmem, st, a, logits, parts, arrived,
                       p->k16, p->v16);
   if (e != cudaSuccess) return e;
   p->launches += 1;
   return cudaSuccess;
 }
 
-template <typename T, int MODE>
-int launch_rows(zc_pages* p, const ZcPagedArgs& a, const ZcDecodeMore& more, float* parts, unsigned* arrived, cudaStream_t st) {
-  return a.max_rows * a.G <= 8 ? launch<T, 1, MODE>(p, a, more, parts, arrived, st)
-                               : launch<T, 2, MODE>(p, a, more, parts, arrived, st);
-}
-
-template <typename T>
-int launch_mode(zc_pages* p, const ZcPagedArgs& a, const ZcDecodeMore& more, float* parts, unsigned* arrived, cudaStream_t st) {
-  if (more.info)
-    return more.logits ? launch_rows<T, ZC_DEC_SHARED | ZC_DEC_WEIGHTS>(p, a, more, parts, arrived, st)
-                       : launch_rows<T, ZC_DEC_SHARED>(p, a, more, parts, arrived, st);
-  return more.logits ? launch_rows<T, ZC_DEC_WEIGHTS>(p, a, more, parts, arrived, st)
-                     : launch_rows<T, 0>(p, a, more, parts, arrived, st);
+template <typename T, int NT>
+int launch_mode(zc_pages* p, const ZcPagedArgs& a, float* logits, float* parts, unsigned* arrived, cudaStream_t st) {
+  return logits ? launch<T, NT, true>(p, a, logits, parts, arrived, st) : launch<T, NT, false>(p, a, logits, parts, arrived, st);
 }
 
 }  // namespace
@@ -648,12 +453,15 @@ size_t zc_paged_decode_workspace() {
   return ZC_PAGES_SYNC_BYTES + (size_t)ZC_PAGED_MAX_CTAS * 2 * ZC_PAGED_ROWS * kJoinStride * 4;
 }
 
-int zc_launch_paged_decode(zc_pages* p, const ZcPagedArgs& a, const ZcDecodeMore& more, char* ws, cudaStream_t st) {
+int zc_launch_paged_decode(zc_pages* p, const ZcPagedArgs& a, float* logits, char* ws, cudaStream_t st) {
   if (!zc_page_maps(p)) return (int)cudaErrorNotSupported;
   unsigned* arrived = (unsigned*)ws;
-  float* parts = (float*)(more.parts ? more.parts : ws + ZC_PAGES_SYNC_BYTES);
-  return p->cfg.dtype == ZC_F16 ? launch_mode<__half>(p, a, more, parts, arrived, st)
-                                : launch_mode<__nv_bfloat16>(p, a, more, parts, arrived, st);
+  float* parts = (float*)(ws + ZC_PAGES_SYNC_BYTES);
+  const bool one = a.max_rows * a.G <= 8;
+  if (p->cfg.dtype == ZC_F16)
+    return one ? launch_mode<__half, 1>(p, a, logits, parts, arrived, st) : launch_mode<__half, 2>(p, a, logits, parts, arrived, st);
+  return one ? launch_mode<__nv_bfloat16, 1>(p, a, logits, parts, arrived, st)
+             : launch_mode<__nv_bfloat16, 2>(p, a, logits, parts, arrived, st);
 }
 
 // Tensor maps of the pages: (64 channels, token of the page, half of the channels, KV head, page).

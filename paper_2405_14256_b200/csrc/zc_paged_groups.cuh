@@ -1,0 +1,161 @@
+// Groups of requests that begin alike: what the kernel of the shared keys and that of the requests' own keys both work out
+// from the lengths, each for itself, before they run side by side.
+#pragma once
+#include "zc_paged_tc.cuh"
+
+namespace {
+
+constexpr int kMaxGroups = ZC_PAGED_MAX_GROUPS;
+constexpr int kShareTile = 64;      // shared keys are taken in whole tiles of the chunk kernel
+// Keys that are not read again, from which on a group is one: an item costs about 25 * 220 cycles beside its tiles, the
+// single-token kernel 20 cycles a key and request.
+constexpr int kWorthSharing = 512;
+// Costs as measured, in 220 cycles: a tile of a wide item (both groups of warps work on it), of a narrow one (they take
+// turns), an item beside its tiles (Q, first product, output, masks); of the single-token kernel a step of 128 keys, and a
+// (request, KV head) beside its steps.
+constexpr int kWideTile = 7, kNarrowTile = 5, kItemCost = 25;
+constexpr int kOwnStep = 5, kOwnUnit = 3;
+constexpr int kPlanReq = 768;       // requests whose lengths are kept in shared memory; those of more are read again
+
+// What is known of the groups and the requests, in shared memory.
+struct GroupTables {
+  int *border, *row;          // [n + 1] first request of a group, its first row
+  int *keys, *count;          // [n] keys that it shares (0: none), its requests that have rows
+  int *first, *kv;            // [n_req + 1], [n_req] a request's first row, its tokens (n_req <= kPlanReq)
+  long long* sums;            // [4] costs of the shared and of the own keys, own keys, items of a KV head
+  int n;
+  bool held;
+  static constexpr int kInts = 4 * kMaxGroups + 8 + 2 * kPlanReq + 3;   // (8 of them the sums)
+  __device__ __forceinline__ GroupTables(void* at, int n_groups, int n_req) {
+    sums = reinterpret_cast<long long*>(at);
+    border = reinterpret_cast<int*>(sums + 4);
+    row = border + kMaxGroups + 1;
+    keys = row + kMaxGroups + 1;
+    count = keys + kMaxGroups;
+    first = count + kMaxGroups;
+    kv = first + kPlanReq + 1;
+    n = n_groups;
+    held = n_req <= kPlanReq;
+  }
+  __device__ __forceinline__ int group_of(int r) const {   // -1: none
+    if (r < border[0] || r >= border[n]) return -1;
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+      const int m = (lo + hi) >> 1;
+      if (border[m] <= r) lo = m; else hi = m;
+    }
+    return lo;
+  }
+  __device__ __forceinline__ int keys_of(int r) const {
+    const int g = group_of(r);
+    return g < 0 ? 0 : keys[g];
+  }
+  __device__ __forceinline__ Chunk chunk(const ZcPagedArgs& a, int r) const {   // load_chunk's
+    if (!held) return load_chunk(a, r);
+    const int e0 = first[r], e1 = max(first[r + 1], e0);
+    Chunk c;
+    c.row0 = e0;
+    c.n = min(e1 - e0, a.max_rows);
+    c.p0 = kv[r] - (e1 - e0);
+    return c;
+  }
+};
+__device__ __forceinline__ int group_border(const ZcPagedArgs& a, const ZcGroups& gr, int g) {
+  return min(max(gr.start[g], 0), a.n_req);
+}
+
+// *sum += v of all threads of the block's warps (64-bit additions in shared memory retry until nobody else is at it: one to
+// a warp; one to a thread took 4 us of 64 threads, 10 of 128).
+__device__ __forceinline__ void add_all(long long* sum, long long v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if ((threadIdx.x & 31) == 0 && v) atomicAdd(reinterpret_cast<unsigned long long*>(sum), (unsigned long long)v);
+}
+
+// How many keys each group shares: at most what the caller says and what lies before every row of its requests, in whole
+// tiles (the keys behind them are the requests' own, as far as this call goes); none where that does not pay.  Returns how
+// many of the n_cta CTAs that share the GPU are the shared keys' (0: there are none): as many as their cost is of all.
+template <int THREADS>
+__device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups& gr, const GroupTables& t, int tpt, int n_cta) {
+  const int tid = threadIdx.x, n = t.n;
+  const long long cap = (long long)a.table_width << a.page_log2;
+  // (everything that is read, in one round trip)
+  for (int g = tid; g <= n; g += THREADS) {
+    t.border[g] = group_border(a, gr, g);
+    if (g < n) {
+      t.keys[g] = (int)min((long long)max(gr.shared[g], 0), cap);
+      t.count[g] = 0;
+    }
+  }
+  if (t.held)
+    for (int r = tid; r <= a.n_req; r += THREADS) {
+      t.first[r] = min(max(a.row_start[r], 0), a.n_rows);
+      if (r < a.n_req) t.kv[r] = (int)min((long long)max(a.kv_len[r], 0), cap);
+    }
+  if (tid < 4) t.sums[tid] = 0;
+  __syncthreads();
+  for (int g = tid; g <= n; g += THREADS)
+    t.row[g] = t.held ? t.first[t.border[g]] : min(max(a.row_start[t.border[g]], 0), a.n_rows);
+  for (int r0 = 0; r0 < a.n_req; r0 += THREADS) {
+    const int r = r0 + tid;
+    Chunk c;
+    c.n = c.p0 = 0;
+    if (r < a.n_req) c = t.chunk(a, r);
+    const int g = c.n > 0 ? t.group_of(r) : -1;
+    // (a warp's requests are one group's as a rule: one of its threads speaks for all)
+    const int top = __reduce_max_sync(0xffffffffu, g);
+    if (__all_sync(0xffffffffu, g == top || g < 0)) {
+      const int least = __reduce_min_sync(0xffffffffu, g < 0 ? 0x7fffffff : c.p0);
+      const int count = __popc(__ballot_sync(0xffffffffu, g >= 0));
+      if (top >= 0 && (tid & 31) == 0) {
+        atomicMin(&t.keys[top], least);
+        atomicAdd(&t.count[top], count);
+      }
+    } else if (g >= 0) {
+      atomicMin(&t.keys[g], c.p0);
+      atomicAdd(&t.count[g], 1);
+    }
+  }
+  __syncthreads();
+  long long cost = 0, items = 0;
+  for (int g = tid; g < n; g += THREADS) {
+    const int keys = max(t.keys[g], 0) & -kShareTile, rows = t.row[g + 1] - t.row[g], tpi = 2 * tpt;
+    const bool on = rows > 0 && n_cta > 1 && (long long)(t.count[g] - 1) * keys >= kWorthSharing;
+    t.keys[g] = on ? keys : 0;
+    if (!on) continue;
+    const int tiles = keys / kShareTile, whole = rows / tpi, rest = rows - whole * tpi;
+    cost += (long long)whole * (tiles * kWideTile + kItemCost);
+    items += whole + (rest > 0);
+    if (rest) cost += tiles * (rest <= tpt ? kNarrowTile : kWideTile) + kItemCost;
+  }
+  add_all(&t.sums[0], cost);
+  add_all(&t.sums[3], items);
+  __syncthreads();
+  long long own = 0, own_keys = 0;
+  for (int r = tid; r < a.n_req; r += THREADS) {
+    const Chunk c = t.chunk(a, r);
+    if (c.n <= 0) continue;
+    const int keys = c.p0 + c.n - t.keys_of(r);
+    own += (long long)max(1, (keys + 127) >> 7) * kOwnStep + kOwnUnit;
+    own_keys += max(0, keys);
+  }
+  add_all(&t.sums[1], own);
+  add_all(&t.sums[2], own_keys);
+  __syncthreads();
+  const long long shared = t.sums[0], all = shared + t.sums[1];
+  if (shared == 0) return 0;
+  // (to 24 bits, so that the quotient is one of 32)
+  const int shift = max(0, 40 - __clzll(all));
+  const uint32_t x = (uint32_t)(shared >> shift), y = (uint32_t)(all >> shift);
+  uint32_t mine = min((uint32_t)n_cta - 1u, max(1u, ((uint32_t)n_cta * x + y / 2) / y));
+  // as many for each item, where there are more CTAs than items: a share that straddles two items has both their ends
+  const long long all_items = t.sums[3] * a.h_kv;
+  if (all_items <= mine) {
+    const uint32_t n = (uint32_t)all_items, each = (mine + n / 2) / n;
+    mine = n * each < (uint32_t)n_cta ? n * each : n * (each - 1);
+    if (mine == 0) mine = (uint32_t)n_cta - 1u;
+  }
+  return (int)mine;
+}
+
+}  // namespace

@@ -1,0 +1,474 @@
+// Attention of requests that begin alike (few rows each): their own keys, behind those that their group shares, and the
+// joining of the two.
+//
+// k_own_keys runs beside the kernel of the shared keys, on the SMs that that one leaves (zc_paged_groups.cuh).  Own parts
+// are short as a rule, so a piece of up to a few blocks of 16 keys is one warp's alone: no warp waits for another, and
+// nothing is joined inside a CTA (eight warps to a unit, whose results meet in shared memory: 5 us of a CTA per (request, KV
+// head) of some 300 keys).  The pieces of all requests and KV heads are dealt out to the warps in turn; a warp works out 32
+// of them at a time, a lane each, and runs through their blocks with a ring of three stages (16 keys and 16 values each,
+// bulk tensor copies), ahead of itself across pieces.  Every piece leaves (maximum, sum, 128 sums) per row.
+// k_own_join puts a row's pieces and its group's together, in their order.  Bound: HBM, every own key and value once.
+#include <cstring>
+#include "zc_paged_block.cuh"
+#include "zc_paged_groups.cuh"
+
+namespace {
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kStages = 3;
+constexpr int kRing = kWarps * kStages * 2 * kHalf;    // 96 KB: two CTAs to an SM
+constexpr int kBatch = 32;                             // pieces that a warp knows
+constexpr int kLeastPiece = 64;                        // keys
+constexpr int kPiecesPerWarp = 12;                     // as many as to make the shares about equal
+constexpr int kStride = ZC_PART_STRIDE;
+
+struct Piece {
+  int r, kv, row0, n, p0;     // request (-1: no more), KV head, its rows, the position of the first
+  int key0, key1;             // keys: whole blocks, the last one's end may lie behind the request's
+  int lo, base;               // first own key of the request; the piece's first row among all pieces' rows
+};
+constexpr int kPieceInts = 9;   // (odd: lanes write without conflicts)
+static_assert(sizeof(Piece) == kPieceInts * 4, "a piece");
+constexpr int kSmem = kRing + kWarps * kStages * 8 + kWarps * kBatch * kPieceInts * 4 + 64 + 1024;   // 1 KB: alignment
+static_assert(GroupTables::kInts * 4 <= kRing, "the groups' tables, before the first copy");
+// Of each request (kPlanReq of them at most; else in global memory): pieces before its own, rows of pieces before, its
+// group's keys.
+constexpr int kOwnSmem = kSmem + 3 * kPlanReq * 4;
+
+struct OwnArgs {
+  ZcPagedArgs a;
+  ZcGroups gr;
+  int tpt, n_sm;
+  float* logits;
+};
+
+__device__ __forceinline__ int own_keys(const Chunk& c, int shared) { return max(0, c.p0 + c.n - shared); }
+// Pieces of a request; one at least (of no key, where its rows see none).
+__device__ __forceinline__ int own_pieces(const Chunk& c, int shared, int len) {
+  return c.n > 0 ? max(1, (own_keys(c, shared) + len - 1) / len) : 0;
+}
+
+// Sum over the block, for all threads.
+__device__ __forceinline__ int block_sum(int v, int* s_warp) {
+  v = __reduce_add_sync(0xffffffffu, v);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) v += s_warp[w];
+  return v;
+}
+
+// The requests' pieces, for every CTA by itself: how long they are, and how many lie before each request's (left in global
+// memory, by every CTA the same, where it reads them again).  Returns their number for one KV head.
+__device__ __forceinline__ int plan_pieces(const OwnArgs& k, const GroupTables& t, int n_warps, int* s_warp, int* s_own,
+                                           int* length) {
+  const ZcPagedArgs& a = k.a;
+  const int tid = threadIdx.x;
+  // as long as makes a few for each warp, and no more than there is room for (their rows are k.gr.own_most at most; a
+  // piece per request always fits)
+  const double per = (double)t.sums[2] * a.h_kv / (n_warps * kPiecesPerWarp);
+  int len = max(kLeastPiece, ((int)min((double)ZC_NO_WINDOW, per) + kBlk - 1) & -kBlk);
+  for (;;) {
+    int rows = 0;
+    for (int r = tid; r < a.n_req; r += kThreads) {
+      const Chunk c = t.chunk(a, r);
+      const long long mine = (long long)own_pieces(c, t.keys_of(r), len) * c.n;
+      rows = (int)min((long long)k.gr.own_most + 1, rows + mine);
+    }
+    if (block_sum(min(rows, 0x7fffffff / kThreads), s_warp) <= k.gr.own_most || len >= ZC_NO_WINDOW) break;
+    len *= 2;
+  }
+  *length = len;
+  int pieces = 0, rows = 0;
+  for (int c0 = 0; c0 < a.n_req; c0 += kThreads) {
+    const int r = c0 + tid;
+    int np = 0, nr = 0, shared = 0;
+    if (r < a.n_req) {
+      const Chunk c = t.chunk(a, r);
+      shared = t.keys_of(r);
+      np = own_pieces(c, shared, len);
+      nr = np * c.n;
+    }
+    int x = np, y = nr;
+    const int lane = tid & 31, warp = tid >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, x, o), v = __shfl_up_sync(0xffffffffu, y, o);
+      if (lane >= o) {
+        x += u;
+        y += v;
+      }
+    }
+    __syncthreads();
+    if (lane == 31) {
+      s_warp[warp] = x;
+      s_warp[kWarps + warp] = y;
+    }
+    __syncthreads();
+    int before = pieces, rows_before = rows;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) {
+        before += s_warp[w];
+        rows_before += s_warp[kWarps + w];
+      }
+      pieces += s_warp[w];
+      rows += s_warp[kWarps + w];
+    }
+    if (r < a.n_req) {
+      const int4 own = make_int4(before + x - np, rows_before + y - nr, shared, np);
+      if (t.held) {
+        s_own[r] = own.x;
+        s_own[kPlanReq + r] = own.y;
+        s_own[2 * kPlanReq + r] = own.z;
+      }
+      if (!t.held || blockIdx.x == 0) k.gr.own[r] = own;
+    }
+  }
+  __syncthreads();   // (a thread reads what others of its CTA have written)
+  return pieces;
+}
+
+template <typename T, int NT, bool WEIGHTS>
+__global__ void __launch_bounds__(kThreads, 2)
+    k_own_keys(const OwnArgs k, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
+  extern __shared__ __align__(1024) char smem_raw[];
+  const ZcPagedArgs& a = k.a;
+  const uint32_t raw_u = zc_smem_u32(smem_raw);
+  const uint32_t base_u = (raw_u + 1023u) & ~1023u;
+  char* base = smem_raw + (base_u - raw_u);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(base + kRing);
+  int* s_pieces = reinterpret_cast<int*>(bars + kWarps * kStages);
+  int* s_warp = s_pieces + kWarps * kBatch * kPieceInts;
+  int* s_own = s_warp + 16;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid < kWarps * kStages) bar_init(&bars[tid], 1);
+  if (tid == 64) {
+    asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&kmap)));
+    asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&vmap)));
+  }
+  asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  zc_let_next_start();
+  // This kernel does not wait for the one of the shared keys, whose CTAs started once all before them was complete; it takes
+  // the SMs that that one leaves.  Its first CTA waits at its end, so that what comes behind waits for both.
+  // (CTAs that find no SM before others leave theirs are not needed as a rule, and need not work that out)
+  const int told = *reinterpret_cast<volatile int*>(k.gr.told);
+  if (told > 0 && blockIdx.x > 0 && (int)blockIdx.x >= 2 * (k.n_sm - (told - 1))) return;
+  const GroupTables tables(base, k.gr.n, a.n_req);
+  const int sms = k.n_sm - plan_groups<kThreads>(a, k.gr, tables, k.tpt, k.n_sm);
+  const int n_warps = 2 * sms * kWarps, wid = blockIdx.x * kWarps + warp;
+  int len;
+  const long long total = (long long)plan_pieces(k, tables, n_warps, s_warp, s_own, &len) * a.h_kv;
+  const bool held = tables.held;
+  async_proxy_fence();   // the tables' place is the ring's from here on, whose copies come by the other proxy
+  __syncthreads();
+
+  if (wid < n_warps) {
+    // ---- pieces: 32 at a time, a lane each ----
+    int* mine = s_pieces + warp * kBatch * kPieceInts;
+    auto find = [&](int first) {
+      const long long i = wid + (long long)(first + lane) * n_warps;
+      Piece p;
+      p.r = -1;
+      if (i < total) {
+        const int idx = (int)(i / a.h_kv);
+        p.kv = (int)(i - (long long)idx * a.h_kv);
+        int lo = 0, hi = a.n_req;   // the last request that has its first piece at or before this one
+        while (hi - lo > 1) {
+          const int m = (lo + hi) >> 1;
+          if ((held ? s_own[m] : k.gr.own[m].x) <= idx) lo = m; else hi = m;
+        }
+        const int4 own = held ? make_int4(s_own[lo], s_own[kPlanReq + lo], s_own[2 * kPlanReq + lo], 0) : k.gr.own[lo];
+        const Chunk c = load_chunk(a, lo);
+        p.r = lo;
+        p.row0 = c.row0;
+        p.n = c.n;
+        p.p0 = c.p0;
+        p.lo = own.z;
+        p.key0 = own.z + (idx - own.x) * len;
+        p.key1 = (int)min((long long)p.key0 + len, (long long)own.z + own_keys(c, own.z));
+        p.base = own.y + (idx - own.x) * c.n;
+        if (p.base < 0 || (long long)p.base + p.n > k.gr.own_most) p.r = -1;   // (lengths that contradict one another)
+      }
+      __syncwarp();
+      int* to = mine + lane * kPieceInts;
+      const int* src = reinterpret_cast<const int*>(&p);
+#pragma unroll
+      for (int e = 0; e < kPieceInts; ++e) to[e] = src[e];
+      __syncwarp();
+    };
+    auto piece = [&](int i) {
+      Piece p;
+      int* to = reinterpret_cast<int*>(&p);
+      const int* src = mine + i * kPieceInts;
+#pragma unroll
+      for (int e = 0; e < kPieceInts; ++e) to[e] = src[e];
+      return p;
+    };
+    const uint32_t ring = base_u + warp * kStages * 2 * kHalf;
+    uint64_t* full = bars + warp * kStages;
+    bool ok = true;      // no wait of the warp has run out
+    int stage = 0;
+    uint32_t phase = 0;
+    const int quad = lane & 3, oct = lane >> 2;
+    for (int first = 0; wid + (long long)first * n_warps < total; first += kBatch) {
+      find(first);
+      // ---- copies, running ahead of the warp's own blocks within these pieces ----
+      int pi = 0, pkey = 0, at_key = -1, at_kv = 0, page = 0;   // the next block: its page id is asked for now and used then
+      Piece pp = piece(0);
+      pkey = pp.key0;
+      auto fetch = [&]() {
+        for (;;) {
+          if (pi == kBatch || pp.r < 0) {
+            at_key = -1;
+            return;
+          }
+          if (pkey < pp.key1) {
+            at_key = pkey;
+            at_kv = pp.kv;
+            page = a.table[(long long)pp.r * a.table_width + (pkey >> a.page_log2)];
+            pkey += kBlk;
+            return;
+          }
+          if (++pi < kBatch) {
+            pp = piece(pi);
+            pkey = pp.key0;
+          }
+        }
+      };
+      int held[kStages];   // pages of the blocks in the stages
+#pragma unroll
+      for (int i = 0; i < kStages; ++i) held[i] = -1;
+      auto issue = [&](int s) {
+        if (at_key < 0) return;
+#pragma unroll
+        for (int i = 0; i < kStages; ++i)
+          if (WEIGHTS && i == s) held[i] = page;
+        if (lane == 0) {
+          const int id = page >= 0 && page < a.n_pages ? page : a.n_pages;   // beyond the pool: arrives as zeros
+          const int row = at_key & ((1 << a.page_log2) - 1);
+          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(zc_smem_u32(&full[s])),
+                       "r"(2 * kHalf)
+                       : "memory");
+          const uint32_t dst = ring + s * 2 * kHalf;
+          page_copy(&kmap, dst, &full[s], row, 0, at_kv, id);
+          page_copy(&vmap, dst + kHalf, &full[s], row, 0, at_kv, id);
+        }
+        fetch();
+      };
+      fetch();
+#pragma unroll
+      for (int i = 0; i < kStages; ++i)
+        if (ok) issue((stage + i) % kStages);
+      // ---- the pieces, their query rows asked for one ahead ----
+      Piece p = piece(0);
+      uint32_t qf[NT][8][2], qn[NT][8][2];
+      load_rows<T, NT>(a, p.row0, p.kv, p.n * a.G, qn);
+#pragma unroll 1
+      for (int i = 0; i < kBatch && p.r >= 0; ++i) {
+        const Piece now = p;
+        const int rows = now.n * a.G, p_last = now.p0 + now.n - 1;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks) {
+            qf[nt][ks][0] = qn[nt][ks][0];
+            qf[nt][ks][1] = qn[nt][ks][1];
+          }
+        if (i + 1 < kBatch) p = piece(i + 1);
+        if (i + 1 < kBatch && p.r >= 0) load_rows<T, NT>(a, p.row0, p.kv, p.n * a.G, qn);
+        int pos[NT][2];
+        row_positions<NT>(a, now.p0, rows, pos);
+        ZcSeen seen;
+        seen.lo = now.lo;
+        seen.hi = p_last + 1;
+        seen.sink_n = seen.nsb = seen.wb0 = seen.nb = 0;
+        RowState<NT> x;
+        x.clear();
+#pragma unroll 1
+        for (int key0 = now.key0; ok && key0 < now.key1; key0 += kBlk) {
+          ok = warp_wait(&full[stage], phase);
+          if (!ok) break;   // nothing more is copied
+          const uint32_t kt = ring + stage * 2 * kHalf, vt = kt + kHalf;
+          float* keep = nullptr;
+          if (WEIGHTS) {
+            int id = -1;
+#pragma unroll
+            for (int s = 0; s < kStages; ++s)
+              if (s == stage) id = held[s];
+            if (id >= 0 && id < a.n_pages) keep = logits_of(k.logits, a, id, now.kv, key0);
+          }
+          attend_block<T, NT, WEIGHTS>(x, qf, pos, kt, vt, base + (vt - base_u), key0, now.p0, p_last, seen, a, rows, keep);
+          __syncwarp();
+          issue(stage);
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+        // ---- what the piece's rows have ----
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float sum = x.s[nt][e];
+#pragma unroll
+            for (int s = 4; s < 32; s <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+            const int row = 8 * nt + 2 * quad + e, tok = row / a.G;
+            if (row >= rows) continue;
+            float* to = k.gr.own_rows +
+                        ((long long)(now.base + tok) * a.h_q + now.kv * a.G + row - tok * a.G) * kStride;
+            if (oct == 0) *reinterpret_cast<float2*>(to) = make_float2(x.m[nt][e], sum);
+#pragma unroll
+            for (int mt = 0; mt < 8; ++mt) {
+              to[4 + 16 * mt + oct] = x.o[nt][mt][e];
+              to[4 + 16 * mt + oct + 8] = x.o[nt][mt][e + 2];
+            }
+          }
+      }
+    }
+    if (!ok)   // the copies that were on their way
+      for (int i = 0; i < kStages; ++i) drain(&full[i], i < stage ? phase ^ 1u : phase);
+  }
+  if (blockIdx.x == 0) zc_wait_for_last();
+}
+
+// A row's pieces of its own keys, and of its group's, to its output.  A warp has a quarter of the channels of eight
+// consecutive rows (token * G + head) of a request and KV head, a lane twice four channels of one of them, so that four
+// lanes read 64 consecutive bytes of a row and eight 128 of a piece of the group's, and several pieces are on their way at a
+// time; a warp to all channels of a row, or of eight, took 17 to 19 us of 64 rows and 32 heads.
+struct JoinArgs {
+  ZcPagedArgs a;
+  ZcGroups gr;
+  int tpt, per_unit;                // per_unit: warps to a (request, KV head), four to eight rows
+};
+template <typename T> __global__ void __launch_bounds__(256) k_own_join(const JoinArgs k) {
+  zc_let_next_start();
+  zc_wait_for_last();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *k.gr.told = 0;   // as the next call wants it
+  const ZcPagedArgs& a = k.a;
+  const int lane = threadIdx.x & 31;
+  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int blk = (int)(w % k.per_unit), unit = (int)(w / k.per_unit);
+  const int r = unit / a.h_kv, kv = unit - r * a.h_kv;
+  if (r >= a.n_req) return;
+  const Chunk c = load_chunk(a, r);
+  const int4 own = k.gr.own[r], info = k.gr.info[r];
+  const int row = (blk >> 2) * 8 + (lane & 7), cg = 8 * (blk & 3) + (lane >> 3);   // this lane's groups of channels: cg, cg + 4
+  const int t = row / a.G, head = kv * a.G + row - t * a.G;
+  if (t >= c.n || own.y < 0 || own.y + (long long)own.w * c.n > k.gr.own_most) return;
+  float m = kNoMax, sum = 0.f;
+  float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+  auto take = [&](float2 ms, float4 x, float4 y) {
+    const float top = fmaxf(m, ms.x), fo = zc_exp2(m - top), fn = zc_exp2(ms.x - top);
+    m = top;
+    sum = fmaf(sum, fo, ms.y * fn);
+    acc[0] = make_float4(fmaf(acc[0].x, fo, x.x * fn), fmaf(acc[0].y, fo, x.y * fn), fmaf(acc[0].z, fo, x.z * fn), fmaf(acc[0].w, fo, x.w * fn));
+    acc[1] = make_float4(fmaf(acc[1].x, fo, y.x * fn), fmaf(acc[1].y, fo, y.y * fn), fmaf(acc[1].z, fo, y.z * fn), fmaf(acc[1].w, fo, y.w * fn));
+  };
+  // the group's keys: where their result is
+  const int n_cta = *k.gr.head;
+  const int tok = info.y + t, tpi = 2 * k.tpt, in_group = tok / tpi, tok_in = tok - in_group * tpi;
+  const int item = info.z + in_group, half = tok_in >= k.tpt;
+  const int prow = half * kM + (tok_in - half * k.tpt) * a.G + head - kv * a.G;
+  const bool shared = info.x > 0 && item < k.gr.most;   // (beyond: lengths that contradict one another)
+  const int cut = shared ? k.gr.cut[(long long)item * a.h_kv + kv] : 0;
+  const bool pieces = shared && cut > 0 && cut < n_cta;
+  const int last = pieces ? min(k.gr.last[cut], n_cta - 1) : 0;
+  // own keys, four pieces at a time
+  const float* from = k.gr.own_rows + ((long long)(own.y + t) * a.h_q + head) * kStride;
+  const long long next = (long long)c.n * a.h_q * kStride;
+  for (int p0 = 0; p0 < own.w; p0 += 4) {
+    float2 ms[4];
+    float4 x[4], y[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (p0 + u < own.w) {
+        const float* at = from + (p0 + u) * next;
+        ms[u] = *reinterpret_cast<const float2*>(at);
+        x[u] = *reinterpret_cast<const float4*>(at + 4 + 4 * cg);
+        y[u] = *reinterpret_cast<const float4*>(at + 4 + 4 * (cg + 4));
+      }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (p0 + u < own.w) take(ms[u], x[u], y[u]);
+  }
+  if (pieces) {
+    // in order: the end of the share before the item's first border, then the starts behind each border
+    for (int d0 = cut - 1; d0 <= last; d0 += 4) {
+      float2 ms[4];
+      float4 x[4], y[4];
+      bool on[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (d0 + u <= last) {
+          const int d = d0 + u;
+          const char* at = k.gr.parts + (long long)(d < cut ? 2 * d + 1 : 2 * d) * ZC_CHUNK_PART_BYTES;
+          on[u] = d < cut || k.gr.used[d];
+          ms[u] = reinterpret_cast<const float2*>(at + ZC_CHUNK_PART_ROWS * ZC_D * 4)[prow];
+          x[u] = reinterpret_cast<const float4*>(at)[cg * ZC_CHUNK_PART_ROWS + prow];
+          y[u] = reinterpret_cast<const float4*>(at)[(cg + 4) * ZC_CHUNK_PART_ROWS + prow];
+        }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (d0 + u <= last && on[u]) take(ms[u], x[u], y[u]);
+    }
+  } else if (shared) {
+    const float* at = k.gr.rows + ((long long)(c.row0 + t) * a.h_q + head) * kStride;
+    take(*reinterpret_cast<const float2*>(at), *reinterpret_cast<const float4*>(at + 4 + 4 * cg),
+         *reinterpret_cast<const float4*>(at + 4 + 4 * (cg + 4)));
+  }
+  const long long at = (long long)(c.row0 + t) * a.h_q + head;
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+    *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.out) + at * ZC_D + 4 * (cg + 4 * j)) =
+        make_uint2(pack2<T>(acc[j].x * inv, acc[j].y * inv), pack2<T>(acc[j].z * inv, acc[j].w * inv));
+  if (a.lse && cg == 0) a.lse[at] = sum > 0.f ? m + log2f(sum) : -INFINITY;
+}
+
+template <typename T, int NT, bool WEIGHTS>
+cudaError_t launch(zc_pages* p, const OwnArgs& k, cudaStream_t st) {
+  static std::atomic<unsigned long long> allowed{0};
+  const cudaError_t e = zc_allow_smem(k_own_keys<T, NT, WEIGHTS>, kOwnSmem, &allowed);
+  if (e != cudaSuccess) return e;
+  return zc_launch_early(k_own_keys<T, NT, WEIGHTS>, dim3(2 * k.n_sm), dim3(kThreads), kOwnSmem, st, k, p->k16, p->v16);
+}
+template <typename T, int NT> cudaError_t launch_mode(zc_pages* p, const OwnArgs& k, cudaStream_t st) {
+  return k.logits ? launch<T, NT, true>(p, k, st) : launch<T, NT, false>(p, k, st);
+}
+template <typename T> cudaError_t launch_rows(zc_pages* p, const OwnArgs& k, cudaStream_t st) {
+  return k.a.max_rows * k.a.G <= 8 ? launch_mode<T, 1>(p, k, st) : launch_mode<T, 2>(p, k, st);
+}
+
+}  // namespace
+
+int zc_launch_own_keys(zc_pages* p, const ZcPagedArgs& a, const ZcGroups& gr, int tpt, float* logits, cudaStream_t st) {
+  OwnArgs k;
+  memset(&k, 0, sizeof(k));
+  k.a = a;
+  k.gr = gr;
+  k.tpt = tpt;
+  k.n_sm = p->n_sm;
+  k.logits = logits;
+  const bool half = p->cfg.dtype == ZC_F16;
+  cudaError_t e = half ? launch_rows<__half>(p, k, st) : launch_rows<__nv_bfloat16>(p, k, st);
+  if (e != cudaSuccess) return (int)e;
+  p->launches += 1;
+  JoinArgs j;
+  memset(&j, 0, sizeof(j));
+  j.a = a;
+  j.gr = gr;
+  j.tpt = tpt;
+  j.per_unit = (a.max_rows * a.G + 7) / 8 * 4;
+  const long long warps = (long long)a.n_req * a.h_kv * j.per_unit, blocks = (warps + 7) / 8;
+  if (warps > 0x7fffffffLL) return (int)cudaErrorInvalidConfiguration;
+  e = half ? zc_launch_early(k_own_join<__half>, dim3((unsigned)blocks), dim3(256), 0, st, j)
+           : zc_launch_early(k_own_join<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, st, j);
+  if (e == cudaSuccess) p->launches += 1;
+  return (int)e;
+}
+
+int zc_paged_own_error_code(int* out) { return (int)cudaMemcpyFromSymbol(out, g_zc_tc_error, sizeof(int)); }

@@ -411,7 +411,7 @@ int zc_paged_attention(zc_pages* p, const void* q, const int64_t q_strides[2], c
   const bool few = few_rows(a);
   if (workspace_bytes < (few ? zc_paged_decode_workspace() : zc_paged_chunk_workspace())) return ZC_ECAPACITY;
   if (!few && !zc_paged_chunk_fits(p->G, n_req, n_rows)) return ZC_ECAPACITY;
-  const int e = few ? zc_launch_paged_decode(p, a, ZcDecodeMore(), (char*)workspace, (cudaStream_t)stream)
+  const int e = few ? zc_launch_paged_decode(p, a, nullptr, (char*)workspace, (cudaStream_t)stream)
                     : zc_launch_paged_chunk(p, a, (char*)workspace, (cudaStream_t)stream);
   return zc_cuda_status(e);
 }
@@ -442,9 +442,7 @@ int zc_paged_attention_scored(zc_pages* p, const void* q, const int64_t q_stride
   const cudaStream_t st = (cudaStream_t)stream;
   int e;
   if (few) {
-    ZcDecodeMore more = {};
-    more.logits = (float*)logits;
-    e = zc_launch_paged_decode(p, a, more, (char*)workspace, st);
+    e = zc_launch_paged_decode(p, a, (float*)logits, (char*)workspace, st);
     if (e == cudaSuccess) e = zc_launch_score_add(p, a, (float*)logits, scores, first, nullptr, nullptr, 0, st);
   } else {
     e = zc_launch_paged_chunk(p, a, (char*)workspace, st);
@@ -479,12 +477,14 @@ int zc_paged_attention_shared(zc_pages* p, const void* q, const int64_t q_stride
   const cudaStream_t st = (cudaStream_t)stream;
   float* kept = scores ? (float*)logits : nullptr;
   int e;
-  if (n_groups > 0) {
+  // What sharing can save at most, by the table's width, against what its kernels take beside their keys: about 15 us, in
+  // which 90 MB are read (8 requests behind 1000 tokens, 8 KV heads: 22 us shared, 10 as any).
+  const int spare = n_req - (n_groups < n_req ? n_groups : n_req);
+  const double saved = (double)spare * ((long long)table_width << p->page_log2) * p->cfg.n_kv_heads * (4.0 * ZC_D);
+  if (n_groups > 0 && saved > 90e6) {
     e = zc_launch_paged_shared(p, a, group_start, shared_len, n_groups, kept, (char*)workspace, st);
   } else {
-    ZcDecodeMore more = {};
-    more.logits = kept;
-    e = zc_launch_paged_decode(p, a, more, (char*)workspace, st);
+    e = zc_launch_paged_decode(p, a, kept, (char*)workspace, st);
   }
   if (scores && e == cudaSuccess)
     e = zc_launch_score_add(p, a, kept, scores, nullptr, group_start, shared_len, n_groups, st);

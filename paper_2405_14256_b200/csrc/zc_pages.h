@@ -9,7 +9,7 @@
 #define ZC_PAGE_MAX_G 16            // most query heads per KV head
 #define ZC_PAGED_ROWS 16            // rows (tokens x query heads of a KV head) the single-token kernel takes
 #define ZC_PAGED_MAX_CTAS 160       // CTAs the workspace is sized for
-static_assert(ZC_PAGED_MAX_CTAS * 4 + 8 <= ZC_PAGES_SYNC_BYTES, "a counter per CTA, and two of the weights' kernel");
+static_assert(ZC_PAGED_MAX_CTAS * 4 + 12 <= ZC_PAGES_SYNC_BYTES, "a counter per CTA, two of the weights' kernel, ZcGroups::told");
 #define ZC_NO_WINDOW (1 << 30)      // positions stay below it
 
 // Several host threads may call with one handle.  The tensor maps are made by the first call that needs them.
@@ -63,37 +63,41 @@ __device__ static inline ZcSeen zc_seen(int p_first, int p_last, int window, int
   return s;
 }
 
-// What the single-token kernel is given beside its arguments, in two modes that can go together.
-#define ZC_DEC_WEIGHTS 1
-#define ZC_DEC_SHARED 2
-struct ZcDecodeMore {
-  float* logits;           // ZC_DEC_WEIGHTS: [page][KV head][token][max_rows * G], scaled, base 2; else null
-  const int4* info;        // ZC_DEC_SHARED: of each request, x = the keys from the first on that are its group's; else null
-  float* rows;             // ZC_DEC_SHARED: (maximum, sum, -, -, 128 sums) of each (row, query head)
-  char* parts;             // partial results elsewhere than behind the counters; or null
-};
-
-// Groups of requests with the same first keys, as the chunk kernel and those behind it see them.
-#define ZC_PAGED_MAX_GROUPS 4096
+// Groups of requests with the same first keys, as the kernels of the shared and of the own keys and the joining one see them.
+#define ZC_PAGED_MAX_GROUPS 1024
+#define ZC_CHUNK_PART_ROWS 256                                   // a piece of the chunk kernel: [channels / 4][row] float4,
+#define ZC_CHUNK_PART_BYTES (ZC_CHUNK_PART_ROWS * (128 * 4 + 8))   // then (maximum, sum) [row]
 struct ZcGroups {
   const int32_t* start;    // [n + 1] the groups' requests
   const int32_t* shared;   // [n] tokens that a group's tables begin with alike
-  int n, most;             // groups; items that there is room for
-  int* keys;               // [n] how many of them the call reads once
-  int4* info;              // [request] (keys, first row among the group's, the group's first item, -)
-  int* cut;                // [item][KV head] 0: the result is with the rows; c: in pieces, whose second is CTA c's
-  float* rows;             // (maximum, sum, -, -, 128 sums) of each (row, query head) over the shared keys
+  int n, most;             // groups; items of a KV head that there is room for
+  // the shared keys' kernel
+  int* told;               // 1 + the CTAs that work on them, once one of them knows; zero before and after every call
+  int* head;               // how many these are
+  int* keys;               // [n] how many of the shared tokens the call reads once
+  int4* info;              // [request] (its group's keys, its first row among the group's, the group's first item, -)
+  int* cut;                // [item][KV head] 0: the result is with the rows; c: in pieces, the second CTA c's
+  int* last;               // [CTA] the last of the CTAs that have pieces of the item that the border before this one cuts
+  const int* used;         // [CTA] its share is not empty
+  const char* parts;       // [CTA][2] pieces
+  float* rows;             // (maximum, sum, -, -, 128 sums) of each (row, query head)
+  // the own keys' kernel
+  int4* own;               // [request] (pieces before its own, rows of pieces before, its group's keys, its pieces)
+  int own_most;            // rows of pieces that there is room for
+  float* own_rows;         // (maximum, sum, -, -, 128 sums) of each (row of a piece, query head)
 };
 
 // Workspace of one call: arrival counters, what the joining kernel is told, and the partial results that are joined.
 size_t zc_paged_decode_workspace();
 size_t zc_paged_chunk_workspace();
 bool zc_paged_chunk_fits(int G, int n_req, int n_rows);   // the call's items fit the chunk kernel's shared memory
-int zc_launch_paged_decode(zc_pages* p, const ZcPagedArgs& a, const ZcDecodeMore& more, char* ws, cudaStream_t st);
+// logits: where they are kept, [page][KV head][token][max_rows * G], scaled, base 2; or null.
+int zc_launch_paged_decode(zc_pages* p, const ZcPagedArgs& a, float* logits, char* ws, cudaStream_t st);
 int zc_launch_paged_chunk(zc_pages* p, const ZcPagedArgs& a, char* ws, cudaStream_t st);
 size_t zc_paged_shared_workspace(const zc_page_config& c, int n_req, int n_rows);
 int zc_launch_paged_shared(zc_pages* p, const ZcPagedArgs& a, const int32_t* group_start, const int32_t* shared_len,
                            int n_groups, float* logits, char* ws, cudaStream_t st);
+int zc_launch_own_keys(zc_pages* p, const ZcPagedArgs& a, const ZcGroups& gr, int tpt, float* logits, cudaStream_t st);
 // group_start, shared_len, n_groups: tokens before a group's shared_len have no score; else first (may be null) says so.
 int zc_launch_score_add(zc_pages* p, const ZcPagedArgs& a, const float* logits, float* scores, const int32_t* first,
                         const int32_t* group_start, const int32_t* shared_len, int n_groups, cudaStream_t st);
@@ -103,3 +107,4 @@ int zc_launch_prefill_window(zc_cache* c, const void* Q, const void* K, const vo
 int zc_paged_decode_error_code(int* out);
 int zc_paged_chunk_error_code(int* out);
 int zc_paged_weights_error_code(int* out);
+int zc_paged_own_error_code(int* out);

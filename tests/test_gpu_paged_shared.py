@@ -31,6 +31,14 @@ def settled(zc):
     assert zc.zc_device_status() == 0
 
 
+def widened(table, page, hkv, n_groups):
+    """The table with so many more (empty) columns that sharing may pay by its width: calls that cannot save 90 MB of reads
+    are attended like any."""
+    spare = len(table) - min(n_groups, len(table))
+    width = int(1e8 / max(1, spare * hkv * 512 * page)) + 1
+    return np.pad(table, ((0, 0), (0, max(0, width - table.shape[1]))), constant_values=-1)
+
+
 def check_rows(dt, q, k, v, table, row_start, kv, out, lse):
     hq, hkv = q.shape[1], k.shape[2]
     vmax = v.abs().max().double()
@@ -52,11 +60,13 @@ def check_rows(dt, q, k, v, table, row_start, kv, out, lse):
 
 
 def shared_case(zc, dtype, hq, hkv, page, groups, shared, own, new=1, alone=0, heads_first=False, pad_rows=0, scored=False,
-                said=None, kv_len=None, seed=0):
+                said=None, kv_len=None, seed=0, wide=True):
     """groups requests with these shared lengths and own lengths behind them (new tokens included); said: what the caller
     claims to be shared, where that is another number."""
     rng, gen, dt = np.random.RandomState(seed), torch.Generator(device=DEV).manual_seed(seed + 1), TYPES[dtype]
     table, kv, starts, n_pages, copies = er.make_groups(rng, page, groups, shared, own, alone)
+    if wide:
+        table = widened(table, page, hkv, len(groups))
     k, v = ref.make_pages(gen, n_pages, page, hkv, dt, heads_first, DEV)
     for src, dst, rows in copies:
         for pool in (k, v):
@@ -131,6 +141,29 @@ def test_groups(zc, dtype, kw):
     shared_case(zc, dtype, **kw)
 
 
+@pytest.mark.parametrize("kw", [CASES[0], CASES[6], CASES[7]])
+def test_groups_that_cannot_save_much(zc, kw):
+    """Narrow tables: attended like any, by one kernel."""
+    shared_case(zc, "bf16", scored=True, wide=False, **kw)
+    pool, args, out, lse = shared_case(zc, "fp16", wide=False, **kw)
+    o, l = pool.attention(*args[:5])
+    settled(zc)
+    end = int(args[2][-1])
+    assert torch.equal(out[:end], o[:end]) and torch.equal(lse[:end], l[:end])
+    before = zc.zc_pages_launch_count(pool.handle)
+    pool.attention_shared(*args)
+    assert zc.zc_pages_launch_count(pool.handle) == before + 1
+    settled(zc)
+
+
+def test_own_parts_of_every_length(zc):
+    """Pieces of the own keys: from one block to more than there is room for at the shortest, more than a warp's batch."""
+    shared_case(zc, "fp16", 8, 2, 64, groups=[5], shared=[512], own=[30000, 1, 16, 17, 64])
+    shared_case(zc, "bf16", 4, 4, 16, groups=[40], shared=[512], own=[1 + 37 * i for i in range(40)], seed=3)
+    shared_case(zc, "fp16", 2, 1, 16, groups=[900], shared=[640], own=[1 + i % 130 for i in range(900)], seed=4)     # > kPlanReq requests
+    shared_case(zc, "fp16", 32, 32, 16, groups=[9, 9], shared=[700, 64], own=[500] * 18, seed=5)
+
+
 @pytest.mark.parametrize("kw", [CASES[0], CASES[2], CASES[3], CASES[6], CASES[7], CASES[13], CASES[11]])
 def test_groups_with_scores(zc, kw):
     shared_case(zc, "bf16", scored=True, **kw)
@@ -186,6 +219,7 @@ def test_maxima_far_apart_between_shared_and_own_keys(zc, dtype):
     for loud_own in (False, True):
         rng, gen, dt = np.random.RandomState(1), torch.Generator(device=DEV).manual_seed(2), TYPES[dtype]
         table, kv, starts, n_pages, copies = er.make_groups(rng, 16, [4], [640], [30, 31, 1, 200])
+        table = widened(table, 16, 2, 1)
         k, v = ref.make_pages(gen, n_pages, 16, 2, dt, False, DEV)
         own_pages = torch.as_tensor(np.unique(table[:, 40:][table[:, 40:] >= 0]), device=DEV).long()
         shared_pages = torch.as_tensor(np.unique(table[:, :40]), device=DEV).long()
@@ -205,7 +239,7 @@ def test_a_run_of_it_all(zc):
     gen = torch.Generator(device=DEV).manual_seed(11)
     shared, groups = [320, 96], [4, 3]
     starts, n_req = [0, 4, 7], 7
-    n_pages, width = 260, 40
+    n_pages, width = 260, 1300
     k = torch.full((n_pages, page, hkv, D), math.nan, dtype=dt, device=DEV)
     v = k.clone()
     scores = torch.full((n_pages, hkv, page), math.nan, device=DEV)

@@ -67,7 +67,7 @@ def test_scored_attention_refuses(zc, pages, bad, code):
 @pytest.mark.parametrize("bad,code", [
     (dict(starts=None), EINVAL), (dict(shared=None), EINVAL), (dict(n_groups=-1), EINVAL), (dict(max_rows=5, n_rows=20), EINVAL),
     (dict(logits=None), EINVAL), (dict(lse=None), EINVAL), (dict(starts=ODD), EALIGN), (dict(shared=ODD), EALIGN),
-    (dict(scores=HALF), EALIGN), (dict(n_groups=4097), ECAPACITY), (dict(ws_bytes=43 << 20), ECAPACITY),
+    (dict(scores=HALF), EALIGN), (dict(n_groups=1025), ECAPACITY), (dict(ws_bytes=43 << 20), ECAPACITY),
     (dict(logits_bytes=100), ECAPACITY), (dict(n_req=13001, n_rows=13001), ECAPACITY)])
 def test_shared_attention_refuses(zc, pages, bad, code):
     assert zc.lib().zc_paged_attention_shared(pages, *{**SHARED, **bad}.values()) == code
