@@ -507,6 +507,13 @@ def _want_i32(t, name: str, n: int, index: int) -> None:
                             f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
+def _at_i32(t, name: str, n: int, index: int) -> int:
+    """The address of n contiguous int32 values on GPU `index`; anything else is refused."""
+    if t.dtype is not torch.int32 or t.numel() != n or t.get_device() != index or not t.is_contiguous():
+        _want_i32(t, name, n, index)
+    return t.data_ptr()
+
+
 def _want_on(t, name: str, index: int) -> None:
     """Refuses a tensor that is not on GPU `index`."""
     if t.get_device() != index:
@@ -618,6 +625,8 @@ class PagedKV(_Buffers):
             if not logits.is_contiguous() or _nbytes(logits) < need:
                 raise ZipCacheError("shared logits too small, or not contiguous")
         self.logits = logits
+        self._logits = (0, 0) if logits is None else (logits.data_ptr(), _nbytes(logits))
+        self._score_shape, self._group = torch.Size((n_pages, n_kv, page_size)), n_q_heads // n_kv
         with torch.cuda.device(self._index):
             self._keep(*(t for t in (workspace, logits) if t is not None), own=not (given or given_logits))
             self.handle = zc_pages_init(k_pages, v_pages, self.cfg)
@@ -716,18 +725,19 @@ class PagedKV(_Buffers):
             self._used_on(raw)
         return n_req, n, width, _strides2(strides[0], strides[1]), out, row_lse, raw
 
-    def _want_scores(self, scores) -> None:
-        shape = (self.cfg.n_pages, self.n_kv_heads, self.page_size)
-        if scores.dtype is not torch.float32 or scores.shape != shape or not scores.is_contiguous() \
+    def _at_scores(self, scores) -> int:
+        """The address of scores; anything but contiguous float32 [n_pages, n_kv_heads, page_size] is refused."""
+        if scores.dtype is not torch.float32 or scores.shape != self._score_shape or not scores.is_contiguous() \
                 or scores.get_device() != self._index:
-            raise ZipCacheError(f"scores: expected contiguous float32 {shape} on {self.device}, got {scores.dtype} "
-                                f"{tuple(scores.shape)} with strides {scores.stride()} on {scores.device}")
+            raise ZipCacheError(f"scores: expected contiguous float32 {tuple(self._score_shape)} on {self.device}, got "
+                                f"{scores.dtype} {tuple(scores.shape)} with strides {scores.stride()} on {scores.device}")
+        return scores.data_ptr()
 
     def _logits_for(self, max_rows: int) -> tuple:
         """The logits' scratch (address, bytes) of a call that scores."""
-        if max_rows > self.scored_rows and max_rows * (self.n_q_heads // self.n_kv_heads) <= 16:
+        if max_rows > self.scored_rows and max_rows * self._group <= 16:
             raise ZipCacheError(f"this handle has room for the logits of {self.scored_rows} rows per request (scored_rows)")
-        return (0, 0) if self.logits is None else (self.logits.data_ptr(), _nbytes(self.logits))
+        return self._logits
 
     def attention_scored(self, q, table, row_start, kv_len, max_rows: int, scores, first=None, window: int = 0,
                          sinks: int = 0, out=None, row_lse=None, stream=None):
@@ -738,14 +748,13 @@ class PagedKV(_Buffers):
             with torch.cuda.device(self._index):
                 return self.attention_scored(q, table, row_start, kv_len, max_rows, scores, first, window, sinks, out,
                                              row_lse, stream)
-        self._want_scores(scores)
-        if first is not None:
-            _want_i32(first, "first", kv_len.numel(), self._index)
+        at_scores = self._at_scores(scores)
+        at_first = 0 if first is None else _at_i32(first, "first", kv_len.numel(), self._index)
         logits, size = self._logits_for(min(max_rows, q.shape[0]))
         n_req, n, width, strides, out, row_lse, raw = self._call(q, table, row_start, kv_len, out, row_lse, stream)
         _check(lib().zc_paged_attention_scored(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
                                                row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
-                                               _ptr(first), scores.data_ptr(), out.data_ptr(), row_lse.data_ptr(),
+                                               at_first, at_scores, out.data_ptr(), row_lse.data_ptr(),
                                                self.workspace.data_ptr(), self._ws_bytes, logits, size, raw),
                "zc_paged_attention_scored")
         return out, row_lse
@@ -760,17 +769,16 @@ class PagedKV(_Buffers):
             with torch.cuda.device(self._index):
                 return self.attention_shared(q, table, row_start, kv_len, max_rows, group_start, shared_len, scores, out,
                                              row_lse, stream)
-        n_groups = shared_len.numel()
-        _want_i32(shared_len, "shared_len", n_groups, self._index)
-        _want_i32(group_start, "group_start", n_groups + 1, self._index)
-        logits = size = 0
+        n_groups, index = shared_len.numel(), self._index
+        at_shared, at_start = _at_i32(shared_len, "shared_len", n_groups, index), _at_i32(group_start, "group_start", n_groups + 1, index)
+        logits = size = at_scores = 0
         if scores is not None:
-            self._want_scores(scores)
+            at_scores = self._at_scores(scores)
             logits, size = self._logits_for(min(max_rows, q.shape[0]))
         n_req, n, width, strides, out, row_lse, raw = self._call(q, table, row_start, kv_len, out, row_lse, stream)
         _check(lib().zc_paged_attention_shared(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
                                                row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows,
-                                               group_start.data_ptr(), shared_len.data_ptr(), n_groups, _ptr(scores),
+                                               at_start, at_shared, n_groups, at_scores,
                                                out.data_ptr(), row_lse.data_ptr(), self.workspace.data_ptr(),
                                                self._ws_bytes, logits, size, raw), "zc_paged_attention_shared")
         return out, row_lse
@@ -784,25 +792,21 @@ class PagedKV(_Buffers):
         if _current_device() != self._index:
             with torch.cuda.device(self._index):
                 return self.select(table, kv_len, scores, keep, recent, first, max_keep, kept, kept_len, stream)
-        n_req = kv_len.numel()
-        _want_i32(kv_len, "kv_len", n_req, self._index)
-        _want_i32(keep, "keep", n_req, self._index)
-        width = table.shape[-1]
-        _want_i32(table, "table", n_req * width, self._index)
-        if first is not None:
-            _want_i32(first, "first", n_req, self._index)
-        self._want_scores(scores)
+        n_req, width, index = kv_len.numel(), table.shape[-1], self._index
         if kept is None:
             kept = _new((n_req, self.n_kv_heads, max_keep), torch.int32, self.device, stream)
-        elif kept.dim() != 3 or kept.shape[:2] != (n_req, self.n_kv_heads):
+        elif kept.dim() == 3:
+            max_keep = kept.shape[2]
+        if kept.dim() != 3 or kept.shape[1] != self.n_kv_heads:
             raise ZipCacheError(f"kept: expected [{n_req}, {self.n_kv_heads}, max_keep], got {tuple(kept.shape)}")
-        _want_i32(kept, "kept", kept.numel(), self._index)
         if kept_len is None:
-            kept_len = _new((n_req,), torch.int32, self.device, stream)
-        _want_i32(kept_len, "kept_len", n_req, self._index)
-        _check(lib().zc_page_select(self.handle, table.data_ptr(), width, kv_len.data_ptr(), n_req, scores.data_ptr(),
-                                    keep.data_ptr(), recent, _ptr(first), kept.data_ptr(), kept.shape[2],
-                                    kept_len.data_ptr(), _stream_of(self._index, stream)), "zc_page_select")
+            kept_len = torch.empty_like(kv_len) if stream is None else _new((n_req,), torch.int32, self.device, stream)
+        _check(lib().zc_page_select(self.handle, _at_i32(table, "table", n_req * width, index), width,
+                                    _at_i32(kv_len, "kv_len", n_req, index), n_req, self._at_scores(scores),
+                                    _at_i32(keep, "keep", n_req, index), recent,
+                                    0 if first is None else _at_i32(first, "first", n_req, index),
+                                    _at_i32(kept, "kept", n_req * self.n_kv_heads * max_keep, index), max_keep,
+                                    _at_i32(kept_len, "kept_len", n_req, index), _stream_of(index, stream)), "zc_page_select")
         return kept, kept_len
 
     def compact(self, table, kv_len, kept, kept_len, scores=None, free_pages=None, free_state=None, free_out=None,
@@ -813,31 +817,27 @@ class PagedKV(_Buffers):
         if _current_device() != self._index:
             with torch.cuda.device(self._index):
                 return self.compact(table, kv_len, kept, kept_len, scores, free_pages, free_state, free_out, stream)
-        n_req = kv_len.numel()
-        _want_i32(kv_len, "kv_len", n_req, self._index)
-        _want_i32(kept_len, "kept_len", n_req, self._index)
-        width = table.shape[-1]
-        _want_i32(table, "table", n_req * width, self._index)
-        if kept.dim() != 3 or kept.shape[:2] != (n_req, self.n_kv_heads):
+        n_req, width, index = kv_len.numel(), table.shape[-1], self._index
+        if kept.dim() != 3 or kept.shape[1] != self.n_kv_heads:
             raise ZipCacheError(f"kept: expected [{n_req}, {self.n_kv_heads}, max_keep], got {tuple(kept.shape)}")
-        _want_i32(kept, "kept", kept.numel(), self._index)
-        if scores is not None:
-            self._want_scores(scores)
-        n_free = 0
+        max_keep = kept.shape[2]
+        at_free = n_free = at_state = at_out = 0
         if free_pages is not None:
-            n_free = free_pages.numel()
-            _want_i32(free_pages, "free_pages", n_free, self._index)
             if free_state is None:
                 raise ZipCacheError("free_pages come with free_state")
-            _want_i32(free_state, "free_state", 3, self._index)
             if free_out is None:
                 free_out = _new((3,), torch.int32, self.device, stream)
-            _want_i32(free_out, "free_out", 3, self._index)
+            n_free = free_pages.numel()
+            at_free, at_state = _at_i32(free_pages, "free_pages", n_free, index), _at_i32(free_state, "free_state", 3, index)
+            at_out = _at_i32(free_out, "free_out", 3, index)
         elif free_state is not None or free_out is not None:
             raise ZipCacheError("free_state and free_out come with free_pages")
-        _check(lib().zc_page_compact(self.handle, table.data_ptr(), width, kv_len.data_ptr(), n_req, kept.data_ptr(),
-                                     kept.shape[2], kept_len.data_ptr(), _ptr(scores), _ptr(free_pages), n_free,
-                                     _ptr(free_state), _ptr(free_out), _stream_of(self._index, stream)), "zc_page_compact")
+        _check(lib().zc_page_compact(self.handle, _at_i32(table, "table", n_req * width, index), width,
+                                     _at_i32(kv_len, "kv_len", n_req, index), n_req,
+                                     _at_i32(kept, "kept", n_req * self.n_kv_heads * max_keep, index), max_keep,
+                                     _at_i32(kept_len, "kept_len", n_req, index),
+                                     0 if scores is None else self._at_scores(scores), at_free, n_free, at_state, at_out,
+                                     _stream_of(index, stream)), "zc_page_compact")
         return free_out
 
 

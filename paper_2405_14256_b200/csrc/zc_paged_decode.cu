@@ -108,8 +108,11 @@ __global__ void __launch_bounds__(kDecThreads, 1)
     asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&vmap)));
   }
   asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
-  zc_let_next_start();
+  // (what adds the weights up reads the lengths and old scores before it waits for this kernel: it may start only once what
+  // came before is complete)
+  if (!WEIGHTS) zc_let_next_start();
   zc_wait_for_last();
+  if (WEIGHTS) zc_let_next_start();
 
   // ---- this CTA's share ----
   long long sum = 0;

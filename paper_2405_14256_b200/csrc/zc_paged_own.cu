@@ -346,15 +346,17 @@ struct JoinArgs {
 };
 template <typename T> __global__ void __launch_bounds__(256) k_own_join(const JoinArgs k) {
   zc_let_next_start();
-  zc_wait_for_last();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *k.gr.told = 0;   // as the next call wants it
   const ZcPagedArgs& a = k.a;
   const int lane = threadIdx.x & 31;
   const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int blk = (int)(w % k.per_unit), unit = (int)(w / k.per_unit);
   const int r = unit / a.h_kv, kv = unit - r * a.h_kv;
-  if (r >= a.n_req) return;
-  const Chunk c = load_chunk(a, r);
+  Chunk c;
+  c.row0 = c.n = c.p0 = 0;
+  if (r < a.n_req) c = load_chunk(a, r);   // (what came before the two kernels is complete)
+  zc_wait_for_last();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *k.gr.told = 0;   // as the next call wants it
+  if (c.n <= 0) return;
   const int4 own = k.gr.own[r], info = k.gr.info[r];
   const int row = (blk >> 2) * 8 + (lane & 7), cg = 8 * (blk & 3) + (lane >> 3);   // this lane's groups of channels: cg, cg + 4
   const int t = row / a.G, head = kv * a.G + row - t * a.G;

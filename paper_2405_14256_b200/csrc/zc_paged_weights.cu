@@ -12,8 +12,9 @@
 namespace {
 
 // ---------------------------------------------------------------- single tokens
-// A thread has four consecutive slots of a page and KV head, whose R logits each lie beside each other.  Bound: HBM, or
-// L2 where the logits are still there.
+// A thread has four consecutive slots of a page and KV head, whose R logits each lie beside each other.  What the kernels
+// before it do not write (lengths, tables, old scores) is read for the first of its slots before it waits for them: they
+// start it only when all that came before them is complete.  Bound: HBM, or L2 where the logits are still there.
 constexpr int kAddThreads = 256;
 
 struct AddArgs {
@@ -31,9 +32,8 @@ __global__ void __launch_bounds__(kAddThreads) k_score_add(const AddArgs w) {
   const ZcPagedArgs& a = w.a;
   const int r = blockIdx.x / w.per_req, part = blockIdx.x - r * w.per_req;
   zc_let_next_start();
-  zc_wait_for_last();
   const Chunk c = load_chunk(a, r);
-  if (c.n <= 0) return;   // (the whole block)
+  if (c.n <= 0) return zc_wait_for_last();   // (the whole block; what comes behind waits for this kernel alone)
   const int per = R ? R : a.max_rows * a.G, rows = c.n * a.G;
   int first = w.first ? max(w.first[r], 0) : 0;
   if (w.n_groups > 0) {
@@ -50,6 +50,7 @@ __global__ void __launch_bounds__(kAddThreads) k_score_add(const AddArgs w) {
   const int fb = first >> a.page_log2;                            // pages without a score
   const int skip = min(s.nb, min(fb, s.nsb) + max(0, fb - s.wb0));
   const long long total = (long long)(s.nb - skip) * per_page;
+  bool waited = false;
   for (long long idx = (long long)part * kAddThreads + threadIdx.x; idx < total;
        idx += (long long)w.per_req * kAddThreads) {
     const int nth = total < (1LL << 32) ? (int)((uint32_t)idx / (uint32_t)per_page) : (int)(idx / per_page);
@@ -64,6 +65,8 @@ __global__ void __launch_bounds__(kAddThreads) k_score_add(const AddArgs w) {
     const float* lse = a.lse + (long long)c.row0 * a.h_q + head * a.G;
     float4* at = reinterpret_cast<float4*>(w.scores + slot);
     const float4 old = *at;
+    if (!waited) zc_wait_for_last();
+    waited = true;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](int k, int row, float x) {
       const int tok = row / a.G, p = c.p0 + tok;
@@ -105,6 +108,7 @@ __global__ void __launch_bounds__(kAddThreads) k_score_add(const AddArgs w) {
         if (key + k >= first && ((key + k >= s.lo && key + k < s.hi) || key + k < s.sink_n)) one[k] = now[k];
     }
   }
+  if (!waited) zc_wait_for_last();
 }
 
 // ---------------------------------------------------------------- chunks
@@ -124,7 +128,9 @@ constexpr int kKeys = 2 * kM;                          // keys of an item
 constexpr int kKeysLog2 = 8;
 constexpr int kKBufs = 2, kQBufs = 2, kLBufs = 4, kRing = 2;
 constexpr int kTiles = (2 * kKBufs + kQBufs) * kTile;  // 192 KB
-constexpr int kRowsBytes = kLBufs * kM * 8;            // minus the log-sum-exp, position
+constexpr int kRowsBytes = kLBufs * (kM * 8 + 4);      // minus the log-sum-exp, position; mild
+// Up to here a logit's rounding makes no weight more than 2^0.07; beyond, weights are held to 1.
+constexpr float kMild = 1048576.f;
 constexpr int kItemInts = 16;
 constexpr int kSmem = kTiles + 1024 + 512 + kRowsBytes + kRing * kItemInts * 4;
 constexpr uint32_t kCols = 512;
@@ -146,6 +152,40 @@ struct WItem {
   int first, two;             // two: the second tile has keys
 };
 static_assert(sizeof(WItem) <= kItemInts * 4, "an item fits its place in the ring");
+
+// 2^x of two numbers on the FMA pipe, x <= 2^20: x is rounded to a whole number n by adding 1.5 * 2^23, whose lower bits
+// then hold n, and the rest, of -1/2 .. 1/2, goes through a polynomial of degree 5 (least largest relative error, fitted by
+// reweighted least squares: 1.6e-7 with these fp32 coefficients); n is added to the exponent.  Below 2^-126: 2^-126.
+__device__ __forceinline__ float2 exp2_fma(float2 x) {
+  const float2 big = make_float2(12582912.f, 12582912.f), back = make_float2(-12582912.f, -12582912.f);
+  x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
+  const float2 t = add2(x, big), n = add2(t, back);
+  const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
+  float2 p = fma2(make_float2(0.0013276470f, 0.0013276470f), f, make_float2(0.0096755410f, 0.0096755410f));
+  p = fma2(p, f, make_float2(0.055507131f, 0.055507131f));
+  p = fma2(p, f, make_float2(0.24022120f, 0.24022120f));
+  p = fma2(p, f, make_float2(0.69314694f, 0.69314694f));
+  p = fma2(p, f, make_float2(1.00000012f, 1.00000012f));
+  return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
+                     __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+// add += the weights 2^(v * scale + less) of 32 columns; kFmaPairs of eight pairs of them on the FMA pipe, since the exp2 unit
+// alone would take eight cycles of a warp's for each, and the instructions beside it two.
+constexpr int kFmaPairs = 2;
+__device__ __forceinline__ void sum_weights(const float* v, const float4* less, float scale, float2 (&add)[2]) {
+  const float2 sc = make_float2(scale, scale);
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    const float4 l = less[c];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float2 x = fma2(make_float2(v[4 * c + 2 * h], v[4 * c + 2 * h + 1]), sc, h ? make_float2(l.z, l.w) : make_float2(l.x, l.y));
+      const int pair = (2 * c + h) & 7;
+      const float2 e = (pair * kFmaPairs) % 8 < kFmaPairs ? exp2_fma(x) : make_float2(zc_exp2(x.x), zc_exp2(x.y));
+      add[h] = add2(add[h], e);
+    }
+  }
+}
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -171,7 +211,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
   float* s_lse = reinterpret_cast<float*>(base + kTiles + 512);          // [kLBufs][kM]
   int* s_pos = reinterpret_cast<int*>(s_lse + kLBufs * kM);              // [kLBufs][kM]
-  int* ring = s_pos + kLBufs * kM;
+  int* s_mild = s_pos + kLBufs * kM;                                     // [kLBufs] no row's is beyond kMild
+  int* ring = s_mild + kLBufs;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   zc_let_next_start();
   if (tid == 0) {
@@ -419,11 +460,16 @@ __global__ void __launch_bounds__(kThreads, 1)
           less[i] = on ? -w.lse[(long long)(it.row0 + tok) * a.h_q + it.kv * a.G + col - in * a.G] : -INFINITY;
           pos[i] = on ? it.p0 + tok : -1;
         }
+        bool mild = true;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mild = mild && (fabsf(less[i]) < kMild || pos[i] < 0);
+        mild = __all_sync(0xffffffffu, mild);
         const uint32_t at = n_l % kLBufs;
         ok = n_l < kLBufs || warp_wait(&l_free[at], (n_l / kLBufs - 1) & 1u);
         if (!ok) break;
         *reinterpret_cast<float4*>(s_lse + at * kM + 4 * lane) = make_float4(less[0], less[1], less[2], less[3]);
         *reinterpret_cast<int4*>(s_pos + at * kM + 4 * lane) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+        if (lane == 0) s_mild[at] = mild;
         __syncwarp();
         if (lane == 0) bar_arrive(&l_full[at]);
       }
@@ -458,31 +504,36 @@ __global__ void __launch_bounds__(kThreads, 1)
           // pairs that are not to be counted: rows behind the request's, rows before the key, keys behind the window
           const int tok0 = t * w.tpt, p_first = it.p0 + tok0, p_last = it.p0 + min(it.n, tok0 + w.tpt) - 1;
           const bool edge = tok0 + w.tpt > it.n || first_key + kM - 1 > p_first ||
-                            (first_key <= p_last - a.window && first_key + kM > a.sinks);
+                            (first_key <= p_last - a.window && first_key + kM > a.sinks) || !s_mild[lb];
           float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          const float2 sc = make_float2(scale, scale);
+          const float4* less = reinterpret_cast<const float4*>(s_lse + lb * kM);
+          auto released = [&]() {   // the group has read its S
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(&s_free[2 * g + place]);
+          };
+          if (!edge) {
+            // 32 columns at a time, the next ones' loads under these ones' exponentials
+            float v[2][32];
+            tmem_ld32_nowait(v[0], tmem_s);
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+              tmem_wait32(v[q4 & 1]);
+              if (q4 < 3) tmem_ld32_nowait(v[(q4 + 1) & 1], tmem_s + 32 * (q4 + 1));
+              else released();
+              sum_weights(v[q4 & 1], less + 8 * q4, scale, add);
+            }
+          } else {
+            const int4* where = reinterpret_cast<const int4*>(s_pos + lb * kM);
 #pragma unroll 1
-          for (int q4 = 0; q4 < 4; ++q4) {
-            float v[32];
-            tmem_ld32_nowait(v, tmem_s + 32 * q4);
-            tmem_wait32(v);
-            const float4* less = reinterpret_cast<const float4*>(s_lse + lb * kM + 32 * q4);
-            // (a weight is at most 1: beyond 2^24 the logits' rounding alone would make it more)
-            if (!edge) {
+            for (int q4 = 0; q4 < 4; ++q4) {
+              float v[32];
+              tmem_ld32_nowait(v, tmem_s + 32 * q4);
+              tmem_wait32(v);
 #pragma unroll
               for (int c = 0; c < 8; ++c) {
-                const float4 l = less[c];
-                const float2 x = fma2(make_float2(v[4 * c], v[4 * c + 1]), sc, make_float2(l.x, l.y));
-                const float2 y = fma2(make_float2(v[4 * c + 2], v[4 * c + 3]), sc, make_float2(l.z, l.w));
-                add[0] = add2(add[0], make_float2(zc_exp2(fminf(x.x, 0.f)), zc_exp2(fminf(x.y, 0.f))));
-                add[1] = add2(add[1], make_float2(zc_exp2(fminf(y.x, 0.f)), zc_exp2(fminf(y.y, 0.f))));
-              }
-            } else {
-              const int4* where = reinterpret_cast<const int4*>(s_pos + lb * kM + 32 * q4);
-#pragma unroll
-              for (int c = 0; c < 8; ++c) {
-                const float4 l = less[c];
-                const int4 p = where[c];
+                const float4 l = less[8 * q4 + c];
+                const int4 p = where[8 * q4 + c];
                 auto one = [&](float x, float m, int at_pos) {
                   const bool seen = key <= at_pos && (key > at_pos - a.window || key < a.sinks);
                   return seen ? zc_exp2(fminf(fmaf(x, scale, m), 0.f)) : 0.f;
@@ -491,10 +542,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 add[1] = add2(add[1], make_float2(one(v[4 * c + 2], l.z, p.z), one(v[4 * c + 3], l.w, p.w)));
               }
             }
+            released();
           }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) bar_arrive(&s_free[2 * g + place]);
           const float2 both = add2(add[0], add[1]);
           sum += both.x + both.y;
         }
