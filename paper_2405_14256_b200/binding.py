@@ -614,7 +614,8 @@ class PagedKV(_Buffers):
             self._ws_bytes = workspace.numel() * workspace.element_size()
             if self._ws_bytes < self.workspace_bytes:
                 raise ZipCacheError("shared workspace too small")
-        self.workspace = workspace
+        self.workspace, self._ws_at = workspace, 0 if workspace is None else workspace.data_ptr()
+        self._lib = lib()
         self.scored_rows = int(scored_rows)
         need, given_logits = zc_scores_workspace(self.cfg, self.scored_rows), logits is not None
         if not given_logits and need > 0:
@@ -660,7 +661,7 @@ class PagedKV(_Buffers):
         strides = self._rows(k_rows, "k_rows", n, self.n_kv_heads)
         if strides != self._rows(v_rows, "v_rows", n, self.n_kv_heads):
             raise ZipCacheError("k_rows and v_rows must share strides")
-        _check(lib().zc_page_write(self.handle, k_rows.data_ptr(), v_rows.data_ptr(), _strides2(strides[0], strides[1]),
+        _check(self._lib.zc_page_write(self.handle, k_rows.data_ptr(), v_rows.data_ptr(), _strides2(strides[0], strides[1]),
                                    slots.data_ptr(), n, _stream_of(self._index, stream)), "zc_page_write")
 
     def read(self, table, l: int, K=None, V=None, stream=None):
@@ -691,9 +692,9 @@ class PagedKV(_Buffers):
             with torch.cuda.device(self._index):
                 return self.attention(q, table, row_start, kv_len, max_rows, window, sinks, out, row_lse, stream)
         n_req, n, width, strides, out, row_lse, raw = self._call(q, table, row_start, kv_len, out, row_lse, stream)
-        _check(lib().zc_paged_attention(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
+        _check(self._lib.zc_paged_attention(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
                                         row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
-                                        out.data_ptr(), row_lse.data_ptr(), self.workspace.data_ptr(), self._ws_bytes,
+                                        out.data_ptr(), row_lse.data_ptr(), self._ws_at, self._ws_bytes,
                                         raw), "zc_paged_attention")
         return out, row_lse
 
@@ -752,10 +753,10 @@ class PagedKV(_Buffers):
         at_first = 0 if first is None else _at_i32(first, "first", kv_len.numel(), self._index)
         logits, size = self._logits_for(min(max_rows, q.shape[0]))
         n_req, n, width, strides, out, row_lse, raw = self._call(q, table, row_start, kv_len, out, row_lse, stream)
-        _check(lib().zc_paged_attention_scored(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
+        _check(self._lib.zc_paged_attention_scored(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
                                                row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
                                                at_first, at_scores, out.data_ptr(), row_lse.data_ptr(),
-                                               self.workspace.data_ptr(), self._ws_bytes, logits, size, raw),
+                                               self._ws_at, self._ws_bytes, logits, size, raw),
                "zc_paged_attention_scored")
         return out, row_lse
 
@@ -776,7 +777,7 @@ class PagedKV(_Buffers):
             at_scores = self._at_scores(scores)
             logits, size = self._logits_for(min(max_rows, q.shape[0]))
         n_req, n, width, strides, out, row_lse, raw = self._call(q, table, row_start, kv_len, out, row_lse, stream)
-        _check(lib().zc_paged_attention_shared(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
+        _check(self._lib.zc_paged_attention_shared(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
                                                row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows,
                                                at_start, at_shared, n_groups, at_scores,
                                                out.data_ptr(), row_lse.data_ptr(), self.workspace.data_ptr(),
@@ -801,7 +802,7 @@ class PagedKV(_Buffers):
             raise ZipCacheError(f"kept: expected [{n_req}, {self.n_kv_heads}, max_keep], got {tuple(kept.shape)}")
         if kept_len is None:
             kept_len = torch.empty_like(kv_len) if stream is None else _new((n_req,), torch.int32, self.device, stream)
-        _check(lib().zc_page_select(self.handle, _at_i32(table, "table", n_req * width, index), width,
+        _check(self._lib.zc_page_select(self.handle, _at_i32(table, "table", n_req * width, index), width,
                                     _at_i32(kv_len, "kv_len", n_req, index), n_req, self._at_scores(scores),
                                     _at_i32(keep, "keep", n_req, index), recent,
                                     0 if first is None else _at_i32(first, "first", n_req, index),
@@ -832,7 +833,7 @@ class PagedKV(_Buffers):
             at_out = _at_i32(free_out, "free_out", 3, index)
         elif free_state is not None or free_out is not None:
             raise ZipCacheError("free_state and free_out come with free_pages")
-        _check(lib().zc_page_compact(self.handle, _at_i32(table, "table", n_req * width, index), width,
+        _check(self._lib.zc_page_compact(self.handle, _at_i32(table, "table", n_req * width, index), width,
                                      _at_i32(kv_len, "kv_len", n_req, index), n_req,
                                      _at_i32(kept, "kept", n_req * self.n_kv_heads * max_keep, index), max_keep,
                                      _at_i32(kept_len, "kept_len", n_req, index),

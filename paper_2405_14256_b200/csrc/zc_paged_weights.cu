@@ -120,10 +120,12 @@ __global__ void __launch_bounds__(kAddThreads) k_score_add(const AddArgs w) {
 //   warp 0      walks the items (a counter deals them out, long ones first), copies K (a lane per page) and Q
 //   warp 1      issues the products, into two places of tensor memory per group
 //   warp 2      brings the rows' log-sum-exp and positions to shared memory
-//   warps 4-7, 8-11  groups 0 and 1, a key per thread
+//   warps 4-7, 8-11  groups 0 and 1, a key per thread: columns 0-63 of every tile
+//   warps 12-15, 16-19  columns 64-127, whose sum the key's first thread gets at the item's end
+// (With all 128 columns a thread, and two warps to a scheduler, the exp2 unit was 65 % busy.)
 // Every wait is bounded; warps 0 to 2 leave where one runs out and wait for what they have in flight, the groups go on
 // with void values until no more items come.  The blocks' warps meet at the kernel's end only.
-constexpr int kThreads = 384;
+constexpr int kThreads = 640;
 constexpr int kKeys = 2 * kM;                          // keys of an item
 constexpr int kKeysLog2 = 8;
 constexpr int kKBufs = 2, kQBufs = 2, kLBufs = 4, kRing = 2;
@@ -132,7 +134,8 @@ constexpr int kRowsBytes = kLBufs * (kM * 8 + 4);      // minus the log-sum-exp,
 // Up to here a logit's rounding makes no weight more than 2^0.07; beyond, weights are held to 1.
 constexpr float kMild = 1048576.f;
 constexpr int kItemInts = 16;
-constexpr int kSmem = kTiles + 1024 + 512 + kRowsBytes + kRing * kItemInts * 4;
+constexpr int kPartBytes = 2 * kKeys * 4;              // sums of the second halves of the columns, of two items
+constexpr int kSmem = kTiles + 1024 + 512 + kPartBytes + kRowsBytes + kRing * kItemInts * 4;
 constexpr uint32_t kCols = 512;
 
 struct WeightArgs {
@@ -202,14 +205,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* q_full = k_free + kKBufs;        // [kQBufs]
   uint64_t* q_free = q_full + kQBufs;        // [kQBufs]
   uint64_t* l_full = q_free + kQBufs;        // [kLBufs] a tile's log-sum-exps
-  uint64_t* l_free = l_full + kLBufs;        // [kLBufs] all eight warps are through with them
+  uint64_t* l_free = l_full + kLBufs;        // [kLBufs] all sixteen warps are through with them
   uint64_t* s_done = l_free + kLBufs;        // [2][2] S_g in place
   uint64_t* s_free = s_done + 4;             // [2][2] the group has read it
   uint64_t* i_full = s_free + 4;             // [kRing]
   uint64_t* i_free = i_full + kRing;         // [kRing]
-  uint64_t* drained = i_free + kRing;
+  uint64_t* x_full = i_free + kRing;         // [2][2] group g's second halves have left their sums, of every other item
+  uint64_t* x_free = x_full + 4;             // [2][2] its first halves have read them
+  uint64_t* drained = x_free + 4;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
-  float* s_lse = reinterpret_cast<float*>(base + kTiles + 512);          // [kLBufs][kM]
+  float* s_part = reinterpret_cast<float*>(base + kTiles + 512);         // [2][kKeys]
+  float* s_lse = s_part + 2 * kKeys;                                     // [kLBufs][kM]
   int* s_pos = reinterpret_cast<int*>(s_lse + kLBufs * kM);              // [kLBufs][kM]
   int* s_mild = s_pos + kLBufs * kM;                                     // [kLBufs] no row's is beyond kMild
   int* ring = s_mild + kLBufs;
@@ -226,15 +232,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < kLBufs; ++i) {
       bar_init(&l_full[i], 1);
-      bar_init(&l_free[i], 8);
+      bar_init(&l_free[i], 16);
     }
     for (int i = 0; i < 4; ++i) {
       bar_init(&s_done[i], 1);
-      bar_init(&s_free[i], 4);
+      bar_init(&s_free[i], 8);
+      bar_init(&x_full[i], 4);
+      bar_init(&x_free[i], 4);
     }
     for (int i = 0; i < kRing; ++i) {
       bar_init(&i_full[i], 1);
-      bar_init(&i_free[i], 10);   // the products, the log-sum-exps, eight worker warps
+      bar_init(&i_free[i], 18);   // the products, the log-sum-exps, sixteen worker warps
     }
     bar_init(drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -475,16 +483,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
   } else if (warp >= 4) {
-    const int g = (warp >> 2) - 1, quarter = warp & 3, row = quarter * 32 + lane;
-    const uint32_t tmem_g = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)g * 2 * kM;
+    const int g = (warp >> 2) - 1 & 1, half = warp >= 12, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t tmem_g = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)g * 2 * kM + 64u * half;
     const float scale = kLog2e * rsqrtf((float)ZC_D);
-    uint32_t n_l = 0, n_s = 0;
+    uint32_t n_l = 0, n_s = 0, n_x = 0;
     WItem it;
     while (next_item(it)) {
       const int first_key = it.key0 + g * kM, key = first_key + row;
       const bool work = g == 0 || it.two;
       // this thread's slot, and what it has; asked for now, used at the item's end
-      const bool mine = key >= it.first && ((key >= it.lo && key < it.hi) || key < it.sink_n);
+      const bool mine = half == 0 && key >= it.first && ((key >= it.lo && key < it.hi) || key < it.sink_n);
       float* at = nullptr;
       if (mine) {
         const int page = a.table[(long long)it.r * a.table_width + (key >> a.page_log2)];
@@ -506,34 +514,25 @@ __global__ void __launch_bounds__(kThreads, 1)
           const bool edge = tok0 + w.tpt > it.n || first_key + kM - 1 > p_first ||
                             (first_key <= p_last - a.window && first_key + kM > a.sinks) || !s_mild[lb];
           float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          const float4* less = reinterpret_cast<const float4*>(s_lse + lb * kM);
-          auto released = [&]() {   // the group has read its S
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(&s_free[2 * g + place]);
-          };
-          if (!edge) {
-            // 32 columns at a time, the next ones' loads under these ones' exponentials
-            float v[2][32];
-            tmem_ld32_nowait(v[0], tmem_s);
+          const float4* less = reinterpret_cast<const float4*>(s_lse + lb * kM + 64 * half);
+          const int4* where = reinterpret_cast<const int4*>(s_pos + lb * kM + 64 * half);
 #pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) {
-              tmem_wait32(v[q4 & 1]);
-              if (q4 < 3) tmem_ld32_nowait(v[(q4 + 1) & 1], tmem_s + 32 * (q4 + 1));
-              else released();
-              sum_weights(v[q4 & 1], less + 8 * q4, scale, add);
+          for (int h = 0; h < 2; ++h) {
+            float v[32];
+            tmem_ld32_nowait(v, tmem_s + 32 * h);
+            tmem_wait32(v);
+            if (h == 1) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) bar_arrive(&s_free[2 * g + place]);   // this warp has read its S
             }
-          } else {
-            const int4* where = reinterpret_cast<const int4*>(s_pos + lb * kM);
-#pragma unroll 1
-            for (int q4 = 0; q4 < 4; ++q4) {
-              float v[32];
-              tmem_ld32_nowait(v, tmem_s + 32 * q4);
-              tmem_wait32(v);
+            if (!edge) {
+              sum_weights(v, less + 8 * h, scale, add);
+            } else {
 #pragma unroll
               for (int c = 0; c < 8; ++c) {
-                const float4 l = less[8 * q4 + c];
-                const int4 p = where[8 * q4 + c];
+                const float4 l = less[8 * h + c];
+                const int4 p = where[8 * h + c];
                 auto one = [&](float x, float m, int at_pos) {
                   const bool seen = key <= at_pos && (key > at_pos - a.window || key < a.sinks);
                   return seen ? zc_exp2(fminf(fmaf(x, scale, m), 0.f)) : 0.f;
@@ -542,7 +541,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                 add[1] = add2(add[1], make_float2(one(v[4 * c + 2], l.z, p.z), one(v[4 * c + 3], l.w, p.w)));
               }
             }
-            released();
           }
           const float2 both = add2(add[0], add[1]);
           sum += both.x + both.y;
@@ -550,7 +548,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) bar_arrive(&l_free[lb]);
       }
-      if (at) *at = old + sum;
+      if (!work) continue;
+      const uint32_t x = 2 * g + (n_x & 1u);
+      float* part = s_part + (n_x & 1u) * kKeys + g * kM + row;
+      if (half) {
+        if (n_x >= 2) bar_wait(&x_free[x], (n_x / 2 - 1) & 1u);
+        *part = sum;
+        __syncwarp();
+        if (lane == 0) bar_arrive(&x_full[x]);
+      } else {
+        bar_wait(&x_full[x], (n_x / 2) & 1u);
+        sum += *part;
+        __syncwarp();
+        if (lane == 0) bar_arrive(&x_free[x]);
+        if (at) *at = old + sum;
+      }
+      ++n_x;
     }
   }
   tc_fence_before();
