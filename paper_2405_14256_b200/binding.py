@@ -578,8 +578,8 @@ class PagedKV(_Buffers):
     may run on any stream (the constructor waits for the current one's work), attention calls that share a workspace
     on one at a time.  Tensors that a call allocates may be used on the current stream, behind what orders it after
     `stream`.
-    shared: the workspace serves attention_shared as well, for max_req requests and max_rows rows (about 1 KB more for each
-    of these rows and query heads).  scored_rows: room for the logits of attention_scored and attention_shared calls of up
+    shared: the workspace serves attention_shared as well, for max_req requests and max_rows rows (1.6 KB more for each of
+    these rows and query heads, so max_rows is best no more than the generated tokens of a step).  scored_rows: room for the logits of attention_scored and attention_shared calls of up
     to so many rows per request (4 bytes per slot, query head and row, in .logits, which handles over pages of one shape
     share as they share a workspace: pass the first one's); calls of more than 16 / G rows need none."""
 

@@ -465,8 +465,7 @@ int zc_launch_own_keys(zc_pages* p, const ZcPagedArgs& a, const ZcGroups& gr, in
   j.gr = gr;
   j.tpt = tpt;
   j.per_unit = (a.max_rows * a.G + 7) / 8 * 4;
-  const long long warps = (long long)a.n_req * a.h_kv * j.per_unit, blocks = (warps + 7) / 8;
-  if (warps > 0x7fffffffLL) return (int)cudaErrorInvalidConfiguration;
+  const long long blocks = ((long long)a.n_req * a.h_kv * j.per_unit + 7) / 8;
   e = half ? zc_launch_early(k_own_join<__half>, dim3((unsigned)blocks), dim3(256), 0, st, j)
            : zc_launch_early(k_own_join<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, st, j);
   if (e == cudaSuccess) p->launches += 1;

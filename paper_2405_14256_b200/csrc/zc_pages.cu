@@ -468,7 +468,7 @@ int zc_paged_attention_shared(zc_pages* p, const void* q, const int64_t q_stride
   const int rc = paged_args(p, q, q_strides, table, table_width, row_start, kv_len, n_req, n_rows, max_rows, 0, 0, out,
                             row_lse, workspace, &a);
   if (rc != ZC_OK || a.n_req == 0) return rc;
-  if (!few_rows(a)) return ZC_EINVAL;
+  if (!few_rows(a) || (long long)n_req * a.h_kv * ZC_PAGED_ROWS > 0x7fffffffLL) return ZC_EINVAL;
   if (scores && (!row_lse || !logits)) return ZC_EINVAL;
   if (!aligned4(group_start, shared_len) || !aligned16(scores) || !aligned16(logits)) return ZC_EALIGN;
   if (n_groups > ZC_PAGED_MAX_GROUPS || !zc_paged_chunk_fits(p->G, n_req, n_rows)) return ZC_ECAPACITY;
@@ -478,7 +478,7 @@ int zc_paged_attention_shared(zc_pages* p, const void* q, const int64_t q_stride
   float* kept = scores ? (float*)logits : nullptr;
   int e;
   // What sharing can save at most, by the table's width, against what its kernels take beside their keys: about 15 us, in
-  // which 90 MB are read (8 requests behind 1000 tokens, 8 KV heads: 22 us shared, 10 as any).
+  // which 90 MB are read (8 requests behind 1000 tokens, 8 KV heads: 22 us shared, 14 as any).
   const int spare = n_req - (n_groups < n_req ? n_groups : n_req);
   const double saved = (double)spare * ((long long)table_width << p->page_log2) * p->cfg.n_kv_heads * (4.0 * ZC_D);
   if (n_groups > 0 && saved > 90e6) {

@@ -193,6 +193,43 @@ def test_huge_logits_give_weights_of_at_most_one(zc):
         assert torch.isfinite(scores).all() and scores.min() >= 0 and scores.max() <= new * hq // hkv
 
 
+@pytest.mark.parametrize("new,bound", [([1, 3, 2], 2), ([40, 9, 130, 64], 64)])
+def test_a_request_with_more_rows_than_the_bound(zc, new, bound):
+    """What it does to its own scores is not said; the others' are as without it."""
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    lengths = [n + 300 for n in new]
+    table, n_pages = ref.make_table(np.random.RandomState(8), lengths, 16)
+    k, v = ref.make_pages(gen, n_pages, 16, 2, torch.float16, False, DEV)
+    q = torch.randn(sum(new), 8, D, generator=gen, device=DEV).half()
+    row_start = [0] + np.cumsum(new).tolist()
+    pool = zc.PagedKV(k, v, 8, max_req=len(new), max_rows=sum(new), scored_rows=4)
+    got, want = (torch.zeros((n_pages, 2, 16), device=DEV) for _ in range(2))
+    pool.attention_scored(q, i32(table), i32(row_start), i32(lengths), bound, got)
+    pool.attention_scored(q, i32(table), i32(row_start), i32(lengths), max(new), want)
+    settled(zc)
+    assert torch.isfinite(got).all()
+    for r, n in enumerate(new):
+        if n <= bound:
+            ids = torch.as_tensor(table[r], device=DEV).long()
+            ids = ids[ids >= 0]
+            # (the same weights, added up by another kernel where the bound decides which)
+            assert (got[ids] - want[ids]).abs().max() <= 2.0 ** -16 * n * 4
+
+
+def test_lengths_beyond_the_table(zc):
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    table, n_pages = ref.make_table(np.random.RandomState(9), [112, 112], 16, 7)
+    k, v = ref.make_pages(gen, n_pages, 16, 2, torch.float16, False, DEV)
+    for new in (1, 40):
+        q = torch.randn(2 * new, 8, D, generator=gen, device=DEV).half()
+        pool = zc.PagedKV(k, v, 8, max_req=2, max_rows=2 * new, scored_rows=1)
+        got, want = (torch.zeros((n_pages, 2, 16), device=DEV) for _ in range(2))
+        pool.attention_scored(q, i32(table), i32([0, new, 2 * new]), i32([5000, 2 ** 31 - 1]), new, got)
+        pool.attention_scored(q, i32(table), i32([0, new, 2 * new]), i32([112, 112]), new, want)
+        settled(zc)
+        assert torch.equal(got, want)
+
+
 def test_a_captured_step_and_another_stream(zc):
     pool, args, _, before = scored_case(zc, "fp16", 8, 2, 16, [100, 900, 33], [1, 2, 1])
     q, table, row_start, kv, most = args

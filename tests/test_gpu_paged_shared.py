@@ -132,6 +132,8 @@ CASES = [
     dict(hq=8, hkv=2, page=16, groups=[2] * 60, shared=[400 + i for i in range(60)], own=[3] * 120),       # many groups
     dict(hq=8, hkv=8, page=64, groups=[130], shared=[200], own=[3] * 130),
     dict(hq=4, hkv=2, page=16, groups=[4], shared=[600], own=[1] * 4, new=[4, 3, 2, 1], kv_len=[2, 601, 601, 601]),   # rows that see nothing
+    dict(hq=7, hkv=1, page=16, groups=[19], shared=[900], own=[5 + i for i in range(19)]),                 # G = 7: 126 of 128 rows
+    dict(hq=10, hkv=2, page=128, groups=[6, 30], shared=[3000, 129], own=[200] * 36, new=[3, 1, 2] * 12),  # G = 5, 15 rows
 ]
 
 
@@ -195,6 +197,53 @@ def test_calls_repeat_bit_for_bit_and_serve_other_calls(zc):
         assert torch.equal(want[0], o2) and torch.equal(want[1], l2)
     check_rows(torch.float16, q, *(torch.nan_to_num(t) for t in (pool.k_pages, pool.v_pages)), table.cpu().numpy(),
                row_start.tolist(), kv2.tolist(), o2, l2)
+
+
+def test_more_rows_than_the_bound_and_lengths_beyond_the_table(zc):
+    """A request with more rows than the caller vouched for does not disturb the others, nor does one whose length passes
+    the table's end."""
+    hq, hkv, page = 8, 2, 16
+    rng, gen = np.random.RandomState(5), torch.Generator(device=DEV).manual_seed(6)
+    table, kv, starts, n_pages, copies = er.make_groups(rng, page, [5], [800], [40, 30, 64, 50, 20])
+    table = widened(table, page, hkv, 1)
+    k, v = ref.make_pages(gen, n_pages, page, hkv, torch.bfloat16, False, DEV)
+    new = [1, 2, 5, 1, 2]
+    row_start = [0] + np.cumsum(new).tolist()
+    q = torch.randn(row_start[-1], hq, D, generator=gen, device=DEV).to(torch.bfloat16)
+    scores = torch.zeros((n_pages, hkv, page), device=DEV)
+    pool = zc.PagedKV(k, v, hq, max_req=5, max_rows=row_start[-1], shared=True, scored_rows=2)
+    out, lse = pool.attention_shared(q, i32(table), i32(row_start), i32(kv), 2, i32(starts), i32([800]), scores=scores)
+    settled(zc)
+    ok = [0, 1, 3, 4]
+    check_rows(torch.bfloat16, q, k, v, table, [row_start[r] for r in range(6)], [kv[r] if r in ok else 0 for r in range(5)],
+               out.index_fill(0, torch.arange(3, 8, device=DEV), 0.0), lse.index_fill(0, torch.arange(3, 8, device=DEV), -math.inf))
+    assert torch.isfinite(scores).all()
+    narrow = i32(table[:, :53].copy())           # 848 tokens: 840 and 864 are requests 0 and 2
+    pool.attention_shared(q, narrow, i32(row_start), i32([2 ** 30, 830, 900, 850, 820]), 2, i32(starts), i32([800]), scores=scores)
+    settled(zc)
+
+
+def test_streams_and_no_groups_with_scores(zc):
+    pool, args, out, lse = shared_case(zc, "bf16", 8, 2, 64, [6], [2000], [40] * 6, scored=True)
+    q, table, row_start, kv, most, starts, said = args
+    side = torch.cuda.Stream()
+    scores = torch.zeros(pool.k_pages.shape[0], 2, 64, device=DEV)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(int(2e7))
+    o, l = pool.attention_shared(*args, scores=scores, stream=side)
+    side.synchronize()
+    assert torch.equal(o, out) and torch.equal(l, lse)
+    kept, length = pool.select(table, kv, scores, i32([2010] * 6), 4, first=i32([2000] * 6), max_keep=2010, stream=side)
+    free, state = i32([0] * 50), i32([40, 50, 0])
+    after = pool.compact(table, kv, kept, length, scores, free, state, stream=side)
+    side.synchronize()
+    assert length.tolist() == [2010] * 6 and after.tolist() == [40, 50, 0]      # (the last page holds 2010 and 2040 alike)
+    one, two = torch.zeros_like(scores), torch.zeros_like(scores)
+    pool.attention_shared(q, table, row_start, kv, 1, i32([0]), i32([]), scores=one)
+    pool.attention_scored(q, table, row_start, kv, 1, two)
+    settled(zc)
+    own = table[:, 31].long()                    # (a slot that several requests score ends with one's sum)
+    assert torch.equal(one[own], two[own]) and one[own].max() > 0
 
 
 def test_no_groups_and_borders_that_contradict(zc):
