@@ -222,7 +222,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
     c.n = s_n[r];
     c.p0 = s_p0[r];
     *width = item_width(min(tpi, c.n - tok0), k.tpt);
-    if (FORM == kGroups) return c.p0 >> kTileLog2;
+    if (FORM == kGroups) return (c.p0 + kN - 1) >> kTileLog2;
     return item_tiles(a, c, tok0, tpi);
   };
   const int most = 0x7fffffff / max(items, 1);   // a head's cost stays in 31 bits
@@ -443,7 +443,7 @@ __device__ __forceinline__ void finish_group_item(const ChunkArgs& k, const Chun
   it.narrow = it.ntok <= k.tpt;
   it.s.lo = it.s.sink_n = it.s.nsb = it.s.wb0 = 0;
   it.s.hi = c.p0;
-  it.s.nb = c.p0 >> kTileLog2;
+  it.s.nb = (c.p0 + kN - 1) >> kTileLog2;
   it.t1 = min(it.t1, it.s.nb);
   it.ga[0] = it.ga[1] = it.t0;
   it.ge[0] = it.ge[1] = it.t1;
@@ -877,7 +877,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int rows_at = it.narrow ? 0 : g;                         // which tile of rows
       const int tok = rows_at * k.tpt + tok_in;                      // token of the item
       const bool valid = tok_in < k.tpt && tok < it.ntok;
-      const int pos = valid ? it.p_first + tok : -1;
+      const int pos = valid ? (FORM == kGroups ? it.s.hi - 1 : it.p_first + tok) : -1;   // (all of a group's see all its keys)
       const int first = it.p_first + rows_at * k.tpt;
       const int last = it.p_first + min(it.ntok, (rows_at + 1) * k.tpt) - 1;
       const int ga = g ? it.ga[1] : it.ga[0], ge = g ? it.ge[1] : it.ge[0];
@@ -895,7 +895,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int h = 0; h < 2; ++h) tmem_ld32_nowait(v + 32 * h, tmem_s + 32 * h);
 #pragma unroll
         for (int h = 0; h < 2; ++h) tmem_wait32(v + 32 * h);
-        const bool edge = FORM != kGroups && (key0 + kN - 1 > first || (key0 <= last - a.window && key0 + kN > a.sinks));
+        const bool edge = FORM == kGroups ? key0 + kN > it.s.hi
+                                          : key0 + kN - 1 > first || (key0 <= last - a.window && key0 + kN > a.sinks);
         if (edge) {
           // the tile crosses the diagonal, the window's edge or the end of the sinks
           const uint64_t seen = below(pos + 1 - key0) & (~below(pos + 1 - a.window - key0) | below(a.sinks - key0));

@@ -6,10 +6,13 @@
 namespace {
 
 constexpr int kMaxGroups = ZC_PAGED_MAX_GROUPS;
-constexpr int kShareTile = 64;      // shared keys are taken in whole tiles of the chunk kernel
+constexpr int kShareStep = 16;      // shared keys are taken in whole blocks of the own keys' kernel
+constexpr int kShareTile = 64;      // keys of a tile of the chunk kernel
 // Keys that are not read again, from which on a group is one: an item costs about 25 * 220 cycles beside its tiles, the
-// single-token kernel 20 cycles a key and request.
+// own keys' kernel 20 cycles a key and request.  And of all groups and KV heads together, from which on any is: the shared
+// keys' kernel takes some 10 us however few they are, in which 50 MB are read.
 constexpr int kWorthSharing = 512;
+constexpr long long kWorthAll = 100000;
 // Costs as measured, in 220 cycles: a tile of a wide item (both groups of warps work on it), of a narrow one (they take
 // turns), an item beside its tiles (Q, first product, output, masks); of the single-token kernel a step of 128 keys, and a
 // (request, KV head) beside its steps.
@@ -22,13 +25,13 @@ struct GroupTables {
   int *border, *row;          // [n + 1] first request of a group, its first row
   int *keys, *count;          // [n] keys that it shares (0: none), its requests that have rows
   int *first, *kv;            // [n_req + 1], [n_req] a request's first row, its tokens (n_req <= kPlanReq)
-  long long* sums;            // [4] costs of the shared and of the own keys, own keys, items of a KV head
+  long long* sums;            // [5] costs of the shared and of the own keys, own keys, items of a KV head, keys spared
   int n;
   bool held;
-  static constexpr int kInts = 4 * kMaxGroups + 8 + 2 * kPlanReq + 3;   // (8 of them the sums)
+  static constexpr int kInts = 4 * kMaxGroups + 8 + 2 * kPlanReq + 5;   // (10 of them the sums)
   __device__ __forceinline__ GroupTables(void* at, int n_groups, int n_req) {
     sums = reinterpret_cast<long long*>(at);
-    border = reinterpret_cast<int*>(sums + 4);
+    border = reinterpret_cast<int*>(sums + 5);
     row = border + kMaxGroups + 1;
     keys = row + kMaxGroups + 1;
     count = keys + kMaxGroups;
@@ -73,7 +76,7 @@ __device__ __forceinline__ void add_all(long long* sum, long long v) {
 }
 
 // How many keys each group shares: at most what the caller says and what lies before every row of its requests, in whole
-// tiles (the keys behind them are the requests' own, as far as this call goes); none where that does not pay.  Returns how
+// blocks of 16 (the keys behind them are the requests' own, as far as this call goes); none where that does not pay.  Returns how
 // many of the n_cta CTAs that share the GPU are the shared keys' (0: there are none): as many as their cost is of all.
 template <int THREADS>
 __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups& gr, const GroupTables& t, int tpt, int n_cta) {
@@ -92,7 +95,7 @@ __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups&
       t.first[r] = min(max(a.row_start[r], 0), a.n_rows);
       if (r < a.n_req) t.kv[r] = (int)min((long long)max(a.kv_len[r], 0), cap);
     }
-  if (tid < 4) t.sums[tid] = 0;
+  if (tid < 5) t.sums[tid] = 0;
   __syncthreads();
   for (int g = tid; g <= n; g += THREADS)
     t.row[g] = t.held ? t.first[t.border[g]] : min(max(a.row_start[t.border[g]], 0), a.n_rows);
@@ -117,20 +120,28 @@ __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups&
     }
   }
   __syncthreads();
-  long long cost = 0, items = 0;
+  long long cost = 0, items = 0, spared = 0;
   for (int g = tid; g < n; g += THREADS) {
-    const int keys = max(t.keys[g], 0) & -kShareTile, rows = t.row[g + 1] - t.row[g], tpi = 2 * tpt;
-    const bool on = rows > 0 && n_cta > 1 && (long long)(t.count[g] - 1) * keys >= kWorthSharing;
+    const int keys = max(t.keys[g], 0) & -kShareStep, rows = t.row[g + 1] - t.row[g], tpi = 2 * tpt;
+    const long long mine = (long long)(t.count[g] - 1) * keys;
+    const bool on = rows > 0 && n_cta > 1 && mine >= kWorthSharing;
     t.keys[g] = on ? keys : 0;
     if (!on) continue;
-    const int tiles = keys / kShareTile, whole = rows / tpi, rest = rows - whole * tpi;
+    spared += mine;
+    const int tiles = (keys + kShareTile - 1) / kShareTile, whole = rows / tpi, rest = rows - whole * tpi;
     cost += (long long)whole * (tiles * kWideTile + kItemCost);
     items += whole + (rest > 0);
     if (rest) cost += tiles * (rest <= tpt ? kNarrowTile : kWideTile) + kItemCost;
   }
   add_all(&t.sums[0], cost);
   add_all(&t.sums[3], items);
+  add_all(&t.sums[4], spared);
   __syncthreads();
+  if (t.sums[4] * a.h_kv < kWorthAll) {
+    for (int g = tid; g < n; g += THREADS) t.keys[g] = 0;
+    if (tid == 0) t.sums[0] = 0;
+    __syncthreads();
+  }
   long long own = 0, own_keys = 0;
   for (int r = tid; r < a.n_req; r += THREADS) {
     const Chunk c = t.chunk(a, r);
@@ -148,10 +159,13 @@ __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups&
   const int shift = max(0, 40 - __clzll(all));
   const uint32_t x = (uint32_t)(shared >> shift), y = (uint32_t)(all >> shift);
   uint32_t mine = min((uint32_t)n_cta - 1u, max(1u, ((uint32_t)n_cta * x + y / 2) / y));
-  // as many for each item, where there are more CTAs than items: a share that straddles two items has both their ends
+  // as many for each item, where there are more CTAs than items: a share that straddles two items has both their ends.
+  // And no more than 2 sqrt(tiles of an item), beyond 8: a piece more takes the joining kernel a quarter as long as a tile.
   const long long all_items = t.sums[3] * a.h_kv;
   if (all_items <= mine) {
-    const uint32_t n = (uint32_t)all_items, each = (mine + n / 2) / n;
+    const uint32_t n = (uint32_t)all_items, tiles = (uint32_t)min(1LL << 24, t.sums[0] / t.sums[3]) / kWideTile;
+    uint32_t each = (mine + n / 2) / n;
+    while (each > 8 && each * each > 4 * tiles) --each;
     mine = n * each < (uint32_t)n_cta ? n * each : n * (each - 1);
     if (mine == 0) mine = (uint32_t)n_cta - 1u;
   }

@@ -335,16 +335,18 @@ __global__ void __launch_bounds__(kThreads, 2)
   if (blockIdx.x == 0) zc_wait_for_last();
 }
 
-// A row's pieces of its own keys, and of its group's, to its output.  A warp has a quarter of the channels of eight
-// consecutive rows (token * G + head) of a request and KV head, a lane twice four channels of one of them, so that four
-// lanes read 64 consecutive bytes of a row and eight 128 of a piece of the group's, and several pieces are on their way at a
-// time; a warp to all channels of a row, or of eight, took 17 to 19 us of 64 rows and 32 heads.
+// A row's pieces of its own keys, and of its group's, to its output.  A warp has ROWS consecutive rows (token * G + head) of
+// a request and KV head, 32 / ROWS lanes to a row, a lane one or two groups of four channels (with eight or four rows the
+// channels are four or two warps'), and four pieces on their way at a time.  A warp to all channels of a row, piece by
+// piece, or of eight rows, took 17 to 19 us of 64 rows and 32 heads; eight rows to a warp with one row to a unit 25 us of 131
+// rows and 32 heads.
 struct JoinArgs {
   ZcPagedArgs a;
   ZcGroups gr;
-  int tpt, per_unit;                // per_unit: warps to a (request, KV head), four to eight rows
+  int tpt, per_unit;                // per_unit: warps to a (request, KV head)
 };
-template <typename T> __global__ void __launch_bounds__(256) k_own_join(const JoinArgs k) {
+template <typename T, int ROWS> __global__ void __launch_bounds__(256) k_own_join(const JoinArgs k) {
+  constexpr int kLanes = 32 / ROWS, kVec = ROWS == 1 ? 1 : 2, kParts = 32 / (kLanes * kVec);   // groups of channels: 32
   zc_let_next_start();
   const ZcPagedArgs& a = k.a;
   const int lane = threadIdx.x & 31;
@@ -358,17 +360,22 @@ template <typename T> __global__ void __launch_bounds__(256) k_own_join(const Jo
   if (blockIdx.x == 0 && threadIdx.x == 0) *k.gr.told = 0;   // as the next call wants it
   if (c.n <= 0) return;
   const int4 own = k.gr.own[r], info = k.gr.info[r];
-  const int row = (blk >> 2) * 8 + (lane & 7), cg = 8 * (blk & 3) + (lane >> 3);   // this lane's groups of channels: cg, cg + 4
+  const int row = blk / kParts * ROWS + lane % ROWS;
+  const int cg = blk % kParts * (kLanes * kVec) + lane / ROWS;   // this lane's groups of channels: cg, cg + kLanes
   const int t = row / a.G, head = kv * a.G + row - t * a.G;
   if (t >= c.n || own.y < 0 || own.y + (long long)own.w * c.n > k.gr.own_most) return;
   float m = kNoMax, sum = 0.f;
-  float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-  auto take = [&](float2 ms, float4 x, float4 y) {
+  float4 acc[kVec];
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto take = [&](float2 ms, const float4 (&x)[kVec]) {
     const float top = fmaxf(m, ms.x), fo = zc_exp2(m - top), fn = zc_exp2(ms.x - top);
     m = top;
     sum = fmaf(sum, fo, ms.y * fn);
-    acc[0] = make_float4(fmaf(acc[0].x, fo, x.x * fn), fmaf(acc[0].y, fo, x.y * fn), fmaf(acc[0].z, fo, x.z * fn), fmaf(acc[0].w, fo, x.w * fn));
-    acc[1] = make_float4(fmaf(acc[1].x, fo, y.x * fn), fmaf(acc[1].y, fo, y.y * fn), fmaf(acc[1].z, fo, y.z * fn), fmaf(acc[1].w, fo, y.w * fn));
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      acc[j] = make_float4(fmaf(acc[j].x, fo, x[j].x * fn), fmaf(acc[j].y, fo, x[j].y * fn), fmaf(acc[j].z, fo, x[j].z * fn),
+                           fmaf(acc[j].w, fo, x[j].w * fn));
   };
   // the group's keys: where their result is
   const int n_cta = *k.gr.head;
@@ -384,24 +391,24 @@ template <typename T> __global__ void __launch_bounds__(256) k_own_join(const Jo
   const long long next = (long long)c.n * a.h_q * kStride;
   for (int p0 = 0; p0 < own.w; p0 += 4) {
     float2 ms[4];
-    float4 x[4], y[4];
+    float4 x[4][kVec];
 #pragma unroll
     for (int u = 0; u < 4; ++u)
       if (p0 + u < own.w) {
         const float* at = from + (p0 + u) * next;
         ms[u] = *reinterpret_cast<const float2*>(at);
-        x[u] = *reinterpret_cast<const float4*>(at + 4 + 4 * cg);
-        y[u] = *reinterpret_cast<const float4*>(at + 4 + 4 * (cg + 4));
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) x[u][j] = *reinterpret_cast<const float4*>(at + 4 + 4 * (cg + kLanes * j));
       }
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (p0 + u < own.w) take(ms[u], x[u], y[u]);
+      if (p0 + u < own.w) take(ms[u], x[u]);
   }
   if (pieces) {
     // in order: the end of the share before the item's first border, then the starts behind each border
     for (int d0 = cut - 1; d0 <= last; d0 += 4) {
       float2 ms[4];
-      float4 x[4], y[4];
+      float4 x[4][kVec];
       bool on[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u)
@@ -410,25 +417,42 @@ template <typename T> __global__ void __launch_bounds__(256) k_own_join(const Jo
           const char* at = k.gr.parts + (long long)(d < cut ? 2 * d + 1 : 2 * d) * ZC_CHUNK_PART_BYTES;
           on[u] = d < cut || k.gr.used[d];
           ms[u] = reinterpret_cast<const float2*>(at + ZC_CHUNK_PART_ROWS * ZC_D * 4)[prow];
-          x[u] = reinterpret_cast<const float4*>(at)[cg * ZC_CHUNK_PART_ROWS + prow];
-          y[u] = reinterpret_cast<const float4*>(at)[(cg + 4) * ZC_CHUNK_PART_ROWS + prow];
+#pragma unroll
+          for (int j = 0; j < kVec; ++j)
+            x[u][j] = reinterpret_cast<const float4*>(at)[(cg + kLanes * j) * ZC_CHUNK_PART_ROWS + prow];
         }
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if (d0 + u <= last && on[u]) take(ms[u], x[u], y[u]);
+        if (d0 + u <= last && on[u]) take(ms[u], x[u]);
     }
   } else if (shared) {
     const float* at = k.gr.rows + ((long long)(c.row0 + t) * a.h_q + head) * kStride;
-    take(*reinterpret_cast<const float2*>(at), *reinterpret_cast<const float4*>(at + 4 + 4 * cg),
-         *reinterpret_cast<const float4*>(at + 4 + 4 * (cg + 4)));
+    float4 x[kVec];
+    const float2 ms = *reinterpret_cast<const float2*>(at);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) x[j] = *reinterpret_cast<const float4*>(at + 4 + 4 * (cg + kLanes * j));
+    take(ms, x);
   }
   const long long at = (long long)(c.row0 + t) * a.h_q + head;
   const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
-    *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.out) + at * ZC_D + 4 * (cg + 4 * j)) =
+  for (int j = 0; j < kVec; ++j)
+    *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.out) + at * ZC_D + 4 * (cg + kLanes * j)) =
         make_uint2(pack2<T>(acc[j].x * inv, acc[j].y * inv), pack2<T>(acc[j].z * inv, acc[j].w * inv));
   if (a.lse && cg == 0) a.lse[at] = sum > 0.f ? m + log2f(sum) : -INFINITY;
+}
+
+template <typename T, int ROWS> cudaError_t launch_join(const JoinArgs& j, cudaStream_t st) {
+  JoinArgs k = j;
+  constexpr int kParts = ROWS == 8 ? 4 : ROWS == 4 ? 2 : 1;
+  k.per_unit = (j.a.max_rows * j.a.G + ROWS - 1) / ROWS * kParts;
+  const long long blocks = ((long long)k.a.n_req * k.a.h_kv * k.per_unit + 7) / 8;
+  return zc_launch_early(k_own_join<T, ROWS>, dim3((unsigned)blocks), dim3(256), 0, st, k);
+}
+template <typename T> cudaError_t launch_join_rows(const JoinArgs& j, cudaStream_t st) {
+  const int rows = j.a.max_rows * j.a.G;
+  return rows > 4 ? launch_join<T, 8>(j, st) : rows > 2 ? launch_join<T, 4>(j, st) : rows > 1 ? launch_join<T, 2>(j, st)
+                                                                                              : launch_join<T, 1>(j, st);
 }
 
 template <typename T, int NT, bool WEIGHTS>
@@ -464,10 +488,7 @@ int zc_launch_own_keys(zc_pages* p, const ZcPagedArgs& a, const ZcGroups& gr, in
   j.a = a;
   j.gr = gr;
   j.tpt = tpt;
-  j.per_unit = (a.max_rows * a.G + 7) / 8 * 4;
-  const long long blocks = ((long long)a.n_req * a.h_kv * j.per_unit + 7) / 8;
-  e = half ? zc_launch_early(k_own_join<__half>, dim3((unsigned)blocks), dim3(256), 0, st, j)
-           : zc_launch_early(k_own_join<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, st, j);
+  e = half ? launch_join_rows<__half>(j, st) : launch_join_rows<__nv_bfloat16>(j, st);
   if (e == cudaSuccess) p->launches += 1;
   return (int)e;
 }

@@ -68,11 +68,15 @@ __global__ void __launch_bounds__(kAddThreads) k_score_add(const AddArgs w) {
     if (!waited) zc_wait_for_last();
     waited = true;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    auto add = [&](int k, int row, float x) {
-      const int tok = row / a.G, p = c.p0 + tok;
-      const bool seen = key + k <= p && (key + k > p - a.window || key + k < a.sinks);
-      // (a weight is at most 1: beyond 2^24 the logits' rounding alone would make it more)
-      if (seen) sum[k] += zc_exp2(fminf(x - lse[(long long)tok * a.h_q + row - tok * a.G], 0.f));
+    auto add = [&](int row, const float (&x)[4]) {
+      const int tok = a.max_rows == 1 ? 0 : row / a.G, p = c.p0 + tok;
+      const float less = lse[(long long)tok * a.h_q + row - tok * a.G];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const bool seen = key + k <= p && (key + k > p - a.window || key + k < a.sinks);
+        // (a weight is at most 1: beyond 2^24 the logits' rounding alone would make it more)
+        if (seen) sum[k] += zc_exp2(fminf(x[k] - less, 0.f));
+      }
     };
     if (R) {
       float x[R ? 4 * R : 1];
@@ -80,13 +84,16 @@ __global__ void __launch_bounds__(kAddThreads) k_score_add(const AddArgs w) {
 #pragma unroll
       for (int i = 0; i < R; ++i) *reinterpret_cast<float4*>(x + 4 * i) = from[i];
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int row = 0; row < R; ++row)
-          if (row < rows) add(k, row, x[k * R + row]);
+      for (int row = 0; row < R; ++row) {
+        const float of[4] = {x[row], x[R + row], x[2 * R + row], x[3 * R + row]};
+        if (row < rows) add(row, of);
+      }
     } else {
-      for (int k = 0; k < 4; ++k)
-        for (int row = 0; row < rows; ++row) add(k, row, w.logits[(slot + k) * per + row]);
+      for (int row = 0; row < rows; ++row) {
+        const float* from = w.logits + slot * per + row;
+        const float of[4] = {from[0], from[per], from[2 * per], from[3 * per]};
+        add(row, of);
+      }
     }
     const float was[4] = {old.x, old.y, old.z, old.w};
     float now[4];
@@ -152,9 +159,14 @@ struct WItem {
   int row0, n, p0;
   int qa, qe;                 // tiles of rows
   int lo, hi, sink_n;         // keys that any row sees
-  int first, two;             // two: the second tile has keys
+  int first, two;             // two: the second tile has keys that a row sees
 };
 static_assert(sizeof(WItem) <= kItemInts * 4, "an item fits its place in the ring");
+// Whether any row of tile t (tpt tokens) sees a key of the item's tile g; the tiles that no row of it does cost nothing.
+__device__ __forceinline__ bool tile_seen(const WItem& it, const ZcPagedArgs& a, int tpt, int t, int g) {
+  const int key = it.key0 + g * kM, p_first = it.p0 + t * tpt, p_last = it.p0 + min(it.n, (t + 1) * tpt) - 1;
+  return key < it.hi && key <= p_last && (key + kM - 1 > p_first - a.window || key < a.sinks);
+}
 
 // 2^x of two numbers on the FMA pipe, x <= 2^20: x is rounded to a whole number n by adding 1.5 * 2^23, whose lower bits
 // then hold n, and the rest, of -1/2 .. 1/2, goes through a polynomial of degree 5 (least largest relative error, fitted by
@@ -422,13 +434,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     while (ok && next_item(it)) {
       const uint32_t kb = n_k % kKBufs;
       ok = warp_wait(&k_full[kb], (n_k / kKBufs) & 1u);
-      const int cnt = uniform(it.qe - it.qa), two = uniform(it.two);
+      const int cnt = uniform(it.qe - it.qa);
       for (int t = 0; ok && t < cnt; ++t, ++n_q) {
         const uint32_t qb = n_q % kQBufs;
         ok = warp_wait(&q_full[qb], (n_q / kQBufs) & 1u);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          if (g && !two) continue;
+          if (!uniform(tile_seen(it, a, w.tpt, it.qa + t, g))) continue;
           const uint32_t place = n_s[g] & 1u;
           ok = ok && (n_s[g] < 2 || warp_wait(&s_free[2 * g + place], (n_s[g] / 2 - 1) & 1u));
           if (!ok) break;
@@ -491,6 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     while (next_item(it)) {
       const int first_key = it.key0 + g * kM, key = first_key + row;
       const bool work = g == 0 || it.two;
+      const int window = key < a.sinks ? 0x7fffffff : a.window;   // a sink is seen from everywhere behind it
       // this thread's slot, and what it has; asked for now, used at the item's end
       const bool mine = half == 0 && key >= it.first && ((key >= it.lo && key < it.hi) || key < it.sink_n);
       float* at = nullptr;
@@ -504,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int t = it.qa; t < it.qe; ++t, ++n_l) {
         const uint32_t lb = n_l % kLBufs;
         bar_wait(&l_full[lb], (n_l / kLBufs) & 1u);
-        if (work) {
+        if (tile_seen(it, a, w.tpt, t, g)) {
           const uint32_t place = n_s & 1u, tmem_s = tmem_g + place * kM;
           bar_wait(&s_done[2 * g + place], (n_s >> 1) & 1u);
           ++n_s;
@@ -534,7 +547,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float4 l = less[8 * h + c];
                 const int4 p = where[8 * h + c];
                 auto one = [&](float x, float m, int at_pos) {
-                  const bool seen = key <= at_pos && (key > at_pos - a.window || key < a.sinks);
+                  const bool seen = at_pos >= key && at_pos - key < window;   // (-1: no row)
                   return seen ? zc_exp2(fminf(fmaf(x, scale, m), 0.f)) : 0.f;
                 };
                 add[0] = add2(add[0], make_float2(one(v[4 * c], l.x, p.x), one(v[4 * c + 1], l.y, p.y)));
