@@ -19,7 +19,7 @@ constexpr int kStages = 3;
 constexpr int kRing = kWarps * kStages * 2 * kHalf;    // 96 KB: two CTAs to an SM
 constexpr int kBatch = 32;                             // pieces that a warp knows
 constexpr int kLeastPiece = 64;                        // keys
-constexpr int kPiecesPerWarp = 12;                     // as many as to make the shares about equal
+constexpr int kPiecesPerWarp = 4;                      // as many as to make the shares about equal (12: 6 us more at 128 on 30000)
 constexpr int kStride = ZC_PART_STRIDE;
 
 struct Piece {
