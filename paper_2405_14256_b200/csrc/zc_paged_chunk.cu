@@ -1252,8 +1252,9 @@ size_t carve_groups(const zc_page_config& c, int n_req, int n_rows, char* ws, Zc
   g.cut = (int*)take((size_t)most_items(G, n_req, n_rows) * c.n_kv_heads * sizeof(int));
   const size_t row = (size_t)c.n_q_heads * ZC_PART_STRIDE * 4;
   g.rows = (float*)take(n_rows * row);
-  g.own_most = 2 * n_rows + 512;
-  g.own_rows = (float*)take(g.own_most * row);
+  g.own_line = (long long*)take(2 * sizeof(long long));
+  // (a request's rows, and as many again for each warp, where the next one goes on)
+  g.own_rows = (float*)take(n_rows * row + (size_t)kOwnWarps * ZC_PAGED_MAX_CTAS * ZC_PAGED_ROWS * ZC_PART_STRIDE * 4);
   if (gr) *gr = g;
   return off;
 }

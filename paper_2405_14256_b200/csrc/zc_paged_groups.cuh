@@ -14,24 +14,27 @@ constexpr int kShareTile = 64;      // keys of a tile of the chunk kernel
 constexpr int kWorthSharing = 512;
 constexpr long long kWorthAll = 100000;
 // Costs as measured, in 220 cycles: a tile of a wide item (both groups of warps work on it), of a narrow one (they take
-// turns), an item beside its tiles (Q, first product, output, masks); of the single-token kernel a step of 128 keys, and a
-// (request, KV head) beside its steps.
+// turns), an item beside its tiles (Q, first product, output, masks); of the own keys' kernel 128 keys, and a
+// (request, KV head) beside them.
 constexpr int kWideTile = 7, kNarrowTile = 5, kItemCost = 25;
-constexpr int kOwnStep = 5, kOwnUnit = 3;
+constexpr int kOwnStep = 4, kOwnUnit = 2;
 constexpr int kPlanReq = 768;       // requests whose lengths are kept in shared memory; those of more are read again
+
+// Warps of the own keys' kernel on an SM.
+constexpr int kOwnWarps = 8;
 
 // What is known of the groups and the requests, in shared memory.
 struct GroupTables {
   int *border, *row;          // [n + 1] first request of a group, its first row
   int *keys, *count;          // [n] keys that it shares (0: none), its requests that have rows
   int *first, *kv;            // [n_req + 1], [n_req] a request's first row, its tokens (n_req <= kPlanReq)
-  long long* sums;            // [5] costs of the shared and of the own keys, own keys, items of a KV head, keys spared
+  long long* sums;            // [4] costs of the shared and of the own keys, items of a KV head, keys spared
   int n;
   bool held;
-  static constexpr int kInts = 4 * kMaxGroups + 8 + 2 * kPlanReq + 5;   // (10 of them the sums)
+  static constexpr int kInts = 4 * kMaxGroups + 8 + 2 * kPlanReq + 3;   // (8 of them the sums)
   __device__ __forceinline__ GroupTables(void* at, int n_groups, int n_req) {
     sums = reinterpret_cast<long long*>(at);
-    border = reinterpret_cast<int*>(sums + 5);
+    border = reinterpret_cast<int*>(sums + 4);
     row = border + kMaxGroups + 1;
     keys = row + kMaxGroups + 1;
     count = keys + kMaxGroups;
@@ -95,7 +98,7 @@ __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups&
       t.first[r] = min(max(a.row_start[r], 0), a.n_rows);
       if (r < a.n_req) t.kv[r] = (int)min((long long)max(a.kv_len[r], 0), cap);
     }
-  if (tid < 5) t.sums[tid] = 0;
+  if (tid < 4) t.sums[tid] = 0;
   __syncthreads();
   for (int g = tid; g <= n; g += THREADS)
     t.row[g] = t.held ? t.first[t.border[g]] : min(max(a.row_start[t.border[g]], 0), a.n_rows);
@@ -134,24 +137,22 @@ __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups&
     if (rest) cost += tiles * (rest <= tpt ? kNarrowTile : kWideTile) + kItemCost;
   }
   add_all(&t.sums[0], cost);
-  add_all(&t.sums[3], items);
-  add_all(&t.sums[4], spared);
+  add_all(&t.sums[2], items);
+  add_all(&t.sums[3], spared);
   __syncthreads();
-  if (t.sums[4] * a.h_kv < kWorthAll) {
+  if (t.sums[3] * a.h_kv < kWorthAll) {
     for (int g = tid; g < n; g += THREADS) t.keys[g] = 0;
     if (tid == 0) t.sums[0] = 0;
     __syncthreads();
   }
-  long long own = 0, own_keys = 0;
+  long long own = 0;
   for (int r = tid; r < a.n_req; r += THREADS) {
     const Chunk c = t.chunk(a, r);
     if (c.n <= 0) continue;
     const int keys = c.p0 + c.n - t.keys_of(r);
     own += (long long)max(1, (keys + 127) >> 7) * kOwnStep + kOwnUnit;
-    own_keys += max(0, keys);
   }
   add_all(&t.sums[1], own);
-  add_all(&t.sums[2], own_keys);
   __syncthreads();
   const long long shared = t.sums[0], all = shared + t.sums[1];
   if (shared == 0) return 0;
@@ -159,15 +160,18 @@ __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups&
   const int shift = max(0, 40 - __clzll(all));
   const uint32_t x = (uint32_t)(shared >> shift), y = (uint32_t)(all >> shift);
   uint32_t mine = min((uint32_t)n_cta - 1u, max(1u, ((uint32_t)n_cta * x + y / 2) / y));
-  // as many for each item, where there are more CTAs than items: a share that straddles two items has both their ends.
-  // And no more than 2 sqrt(tiles of an item), beyond 8: a piece more takes the joining kernel a quarter as long as a tile.
-  const long long all_items = t.sums[3] * a.h_kv;
+  // As many for each item, where there are more CTAs than items: a share that straddles two items has both their ends.
+  // Of the two numbers next to an equal one, that which ends sooner: rounded, 16 items on 148 SMs went from 6 CTAs each to
+  // 7, and the own keys of 128 requests from 52 SMs to 36 (95 -> 142 us).  And no more than 2 sqrt(tiles of an item),
+  // beyond 8: a piece more takes the joining kernel a quarter as long as a tile.
+  const long long all_items = t.sums[2] * a.h_kv;
   if (all_items <= mine) {
-    const uint32_t n = (uint32_t)all_items, tiles = (uint32_t)min(1LL << 24, t.sums[0] / t.sums[3]) / kWideTile;
-    uint32_t each = (mine + n / 2) / n;
+    const uint32_t n = (uint32_t)all_items, tiles = (uint32_t)min(1LL << 24, t.sums[0] / t.sums[2]) / kWideTile;
+    uint32_t each = mine / n;
+    const long long left = (long long)n_cta - n * (each + 1);
+    if (left > 0 && x * left > (long long)(y - x) * (n * each)) ++each;
     while (each > 8 && each * each > 4 * tiles) --each;
-    mine = n * each < (uint32_t)n_cta ? n * each : n * (each - 1);
-    if (mine == 0) mine = (uint32_t)n_cta - 1u;
+    mine = n * each;
   }
   return (int)mine;
 }

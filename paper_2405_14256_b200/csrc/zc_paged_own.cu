@@ -2,11 +2,14 @@
 // joining of the two.
 //
 // k_own_keys runs beside the kernel of the shared keys, on the SMs that that one leaves (zc_paged_groups.cuh).  Own parts
-// are short as a rule, so a piece of up to a few blocks of 16 keys is one warp's alone: no warp waits for another, and
+// are short as a rule, so a piece of some blocks of 16 keys is one warp's alone: no warp waits for another, and
 // nothing is joined inside a CTA (eight warps to a unit, whose results meet in shared memory: 5 us of a CTA per (request, KV
-// head) of some 300 keys).  The pieces of all requests and KV heads are dealt out to the warps in turn; a warp works out 32
-// of them at a time, a lane each, and runs through their blocks with a ring of three stages (16 keys and 16 values each,
-// bulk tensor copies), ahead of itself across pieces.  Every piece leaves (maximum, sum, 128 sums) per row.
+// head) of some 300 keys).  The blocks of all KV heads and requests lie on one line, each (KV head, request) with what a
+// piece costs beside its blocks, and every warp has an equal stretch of it: the end of one request's, whole ones, the
+// beginning of another's (pieces of one length dealt out to the warps in turn left half of them idle at the end: 108 us for
+// 128 requests of up to 2048 own keys behind 30000, 95 so).  A warp works out 32 of its pieces at a time, a lane each, and
+// runs through their blocks with a ring of three stages (16 keys and 16 values each, bulk tensor copies), ahead of itself
+// across pieces.  Every piece leaves (maximum, sum, 128 sums) per row.
 // k_own_join puts a row's pieces and its group's together, in their order.  Bound: HBM, every own key and value once.
 #include <cstring>
 #include "zc_paged_block.cuh"
@@ -15,24 +18,25 @@
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
+static_assert(kOwnWarps == 2 * kWarps, "two CTAs to an SM");
 constexpr int kStages = 3;
 constexpr int kRing = kWarps * kStages * 2 * kHalf;    // 96 KB: two CTAs to an SM
 constexpr int kBatch = 32;                             // pieces that a warp knows
-constexpr int kLeastPiece = 64;                        // keys
-constexpr int kPiecesPerWarp = 4;                      // as many as to make the shares about equal (12: 6 us more at 128 on 30000)
+constexpr int kPieceCost = 4;                          // what a piece costs beside its blocks, in blocks
+constexpr int kLeastStretch = 4 + kPieceCost;          // of a warp, in blocks
 constexpr int kStride = ZC_PART_STRIDE;
 
 struct Piece {
   int r, kv, row0, n, p0;     // request (-1: no more), KV head, its rows, the position of the first
   int key0, key1;             // keys: whole blocks, the last one's end may lie behind the request's
-  int lo, base;               // first own key of the request; the piece's first row among all pieces' rows
+  int lo, base;               // first own key of the request; where the piece's rows are among all pieces' rows
 };
 constexpr int kPieceInts = 9;   // (odd: lanes write without conflicts)
 static_assert(sizeof(Piece) == kPieceInts * 4, "a piece");
 constexpr int kSmem = kRing + kWarps * kStages * 8 + kWarps * kBatch * kPieceInts * 4 + 64 + 1024;   // 1 KB: alignment
 static_assert(GroupTables::kInts * 4 <= kRing, "the groups' tables, before the first copy");
-// Of each request (kPlanReq of them at most; else in global memory): pieces before its own, rows of pieces before, its
-// group's keys.
+// Of each request (kPlanReq of them at most; else in global memory): where its blocks begin on a KV head's line (64 bits),
+// its group's keys.
 constexpr int kOwnSmem = kSmem + 3 * kPlanReq * 4;
 
 struct OwnArgs {
@@ -43,93 +47,52 @@ struct OwnArgs {
 };
 
 __device__ __forceinline__ int own_keys(const Chunk& c, int shared) { return max(0, c.p0 + c.n - shared); }
-// Pieces of a request; one at least (of no key, where its rows see none).
-__device__ __forceinline__ int own_pieces(const Chunk& c, int shared, int len) {
-  return c.n > 0 ? max(1, (own_keys(c, shared) + len - 1) / len) : 0;
+// A request's length on the line, in blocks; the piece that it has in any case, of no key maybe, costs as well.
+__device__ __forceinline__ int own_length(const Chunk& c, int shared) {
+  return c.n > 0 ? (int)(((long long)own_keys(c, shared) + kBlk - 1) / kBlk) + kPieceCost : 0;
 }
 
-// Sum over the block, for all threads.
-__device__ __forceinline__ int block_sum(int v, int* s_warp) {
-  v = __reduce_add_sync(0xffffffffu, v);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) v += s_warp[w];
-  return v;
-}
-
-// The requests' pieces, for every CTA by itself: how long they are, and how many lie before each request's (left in global
-// memory, by every CTA the same, where it reads them again).  Returns their number for one KV head.
-__device__ __forceinline__ int plan_pieces(const OwnArgs& k, const GroupTables& t, int n_warps, int* s_warp, int* s_own,
-                                           int* length) {
+// Where each request's blocks begin on a KV head's line, for every CTA by itself (left in global memory, by every CTA the
+// same, where it reads them again).  Returns the line's length.
+__device__ __forceinline__ long long plan_line(const OwnArgs& k, const GroupTables& t, long long* s_warp, long long* s_at,
+                                               int* s_shared) {
   const ZcPagedArgs& a = k.a;
-  const int tid = threadIdx.x;
-  // as long as makes a few for each warp, and no more than there is room for (their rows are k.gr.own_most at most; a
-  // piece per request always fits)
-  const double per = (double)t.sums[2] * a.h_kv / (n_warps * kPiecesPerWarp);
-  int len = max(kLeastPiece, ((int)min((double)ZC_NO_WINDOW, per) + kBlk - 1) & -kBlk);
-  for (;;) {
-    int rows = 0;
-    for (int r = tid; r < a.n_req; r += kThreads) {
-      const Chunk c = t.chunk(a, r);
-      const long long mine = (long long)own_pieces(c, t.keys_of(r), len) * c.n;
-      rows = (int)min((long long)k.gr.own_most + 1, rows + mine);
-    }
-    if (block_sum(min(rows, 0x7fffffff / kThreads), s_warp) <= k.gr.own_most || len >= ZC_NO_WINDOW) break;
-    len *= 2;
-  }
-  *length = len;
-  int pieces = 0, rows = 0;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  long long line = 0;
   for (int c0 = 0; c0 < a.n_req; c0 += kThreads) {
     const int r = c0 + tid;
-    int np = 0, nr = 0, shared = 0;
+    int length = 0, shared = 0;
     if (r < a.n_req) {
-      const Chunk c = t.chunk(a, r);
       shared = t.keys_of(r);
-      np = own_pieces(c, shared, len);
-      nr = np * c.n;
+      length = own_length(t.chunk(a, r), shared);
     }
-    int x = np, y = nr;
-    const int lane = tid & 31, warp = tid >> 5;
+    long long x = length;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, x, o), v = __shfl_up_sync(0xffffffffu, y, o);
-      if (lane >= o) {
-        x += u;
-        y += v;
-      }
+      const long long u = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += u;
     }
     __syncthreads();
-    if (lane == 31) {
-      s_warp[warp] = x;
-      s_warp[kWarps + warp] = y;
-    }
+    if (lane == 31) s_warp[warp] = x;
     __syncthreads();
-    int before = pieces, rows_before = rows;
+    long long before = line + x - length;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) {
-        before += s_warp[w];
-        rows_before += s_warp[kWarps + w];
-      }
-      pieces += s_warp[w];
-      rows += s_warp[kWarps + w];
+      if (w < warp) before += s_warp[w];
+      line += s_warp[w];
     }
     if (r < a.n_req) {
-      const int4 own = make_int4(before + x - np, rows_before + y - nr, shared, np);
       if (t.held) {
-        s_own[r] = own.x;
-        s_own[kPlanReq + r] = own.y;
-        s_own[2 * kPlanReq + r] = own.z;
+        s_at[r] = before;
+        s_shared[r] = shared;
       }
-      if (!t.held || blockIdx.x == 0) k.gr.own[r] = own;
+      if (!t.held || blockIdx.x == 0) k.gr.own[r] = make_int4((int)before, (int)(before >> 32), shared, length);
     }
   }
   __syncthreads();   // (a thread reads what others of its CTA have written)
-  return pieces;
+  return line;
 }
+__device__ __forceinline__ long long line_at(const int4& own) { return (long long)own.y << 32 | (uint32_t)own.x; }
 
 template <typename T, int NT, bool WEIGHTS>
 __global__ void __launch_bounds__(kThreads, 2)
@@ -141,8 +104,9 @@ __global__ void __launch_bounds__(kThreads, 2)
   char* base = smem_raw + (base_u - raw_u);
   uint64_t* bars = reinterpret_cast<uint64_t*>(base + kRing);
   int* s_pieces = reinterpret_cast<int*>(bars + kWarps * kStages);
-  int* s_warp = s_pieces + kWarps * kBatch * kPieceInts;
-  int* s_own = s_warp + 16;
+  long long* s_warp = reinterpret_cast<long long*>(s_pieces + kWarps * kBatch * kPieceInts);
+  long long* s_at = s_warp + 8;
+  int* s_shared = reinterpret_cast<int*>(s_at + kPlanReq);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid < kWarps * kStages) bar_init(&bars[tid], 1);
   if (tid == 64) {
@@ -158,9 +122,13 @@ __global__ void __launch_bounds__(kThreads, 2)
   if (told > 0 && blockIdx.x > 0 && (int)blockIdx.x >= 2 * (k.n_sm - (told - 1))) return;
   const GroupTables tables(base, k.gr.n, a.n_req);
   const int sms = k.n_sm - plan_groups<kThreads>(a, k.gr, tables, k.tpt, k.n_sm);
-  const int n_warps = 2 * sms * kWarps, wid = blockIdx.x * kWarps + warp;
-  int len;
-  const long long total = (long long)plan_pieces(k, tables, n_warps, s_warp, s_own, &len) * a.h_kv;
+  const int n_warps = sms * kOwnWarps, wid = blockIdx.x * kWarps + warp;
+  const long long line = plan_line(k, tables, s_warp, s_at, s_shared), total = line * a.h_kv;
+  const long long stretch = max((long long)kLeastStretch, (total + n_warps - 1) / n_warps);
+  if (blockIdx.x == 0 && tid == 0) {
+    k.gr.own_line[0] = line;
+    k.gr.own_line[1] = stretch;
+  }
   const bool held = tables.held;
   async_proxy_fence();   // the tables' place is the ring's from here on, whose copies come by the other proxy
   __syncthreads();
@@ -168,35 +136,50 @@ __global__ void __launch_bounds__(kThreads, 2)
   if (wid < n_warps) {
     // ---- pieces: 32 at a time, a lane each ----
     int* mine = s_pieces + warp * kBatch * kPieceInts;
-    auto find = [&](int first) {
-      const long long i = wid + (long long)(first + lane) * n_warps;
+    long long x0 = min(total, wid * stretch);
+    const long long x1 = min(total, x0 + stretch);
+    auto find = [&]() {   // those from x0 on
+      const int kv0 = (int)(x0 / line);
+      const long long rem = x0 - kv0 * line;
+      int lo = 0, hi = a.n_req;   // the last request that begins at or before this place
+      while (hi - lo > 1) {
+        const int m = (lo + hi) >> 1;
+        if ((held ? s_at[m] : line_at(k.gr.own[m])) <= rem) lo = m; else hi = m;
+      }
+      const int unit = kv0 * a.n_req + lo + lane;
       Piece p;
       p.r = -1;
-      if (i < total) {
-        const int idx = (int)(i / a.h_kv);
-        p.kv = (int)(i - (long long)idx * a.h_kv);
-        int lo = 0, hi = a.n_req;   // the last request that has its first piece at or before this one
-        while (hi - lo > 1) {
-          const int m = (lo + hi) >> 1;
-          if ((held ? s_own[m] : k.gr.own[m].x) <= idx) lo = m; else hi = m;
+      p.kv = unit / a.n_req;
+      const int r = unit - p.kv * a.n_req;
+      long long end = 0;
+      if (p.kv < a.h_kv) {
+        const Chunk c = load_chunk(a, r);
+        const int4 own = held ? make_int4(0, 0, s_shared[r], 0) : k.gr.own[r];
+        const long long at = p.kv * line + (held ? s_at[r] : line_at(own)), from = max(at, x0);
+        end = min(at + own_length(c, own.z), x1);
+        if (from < end) {
+          p.r = r;
+          p.row0 = c.row0;
+          p.n = c.n;
+          p.p0 = c.p0;
+          p.lo = own.z;
+          p.key0 = own.z + kBlk * max(0, (int)(from - at) - kPieceCost);
+          p.key1 = (int)min((long long)own.z + kBlk * (long long)max(0, (int)(end - at) - kPieceCost),
+                            (long long)own.z + own_keys(c, own.z));
+          // (each next piece is the next warp's or of the next rows: no two have the same place)
+          p.base = (p.kv * a.n_rows + c.row0) * a.G + wid * ZC_PAGED_ROWS;
         }
-        const int4 own = held ? make_int4(s_own[lo], s_own[kPlanReq + lo], s_own[2 * kPlanReq + lo], 0) : k.gr.own[lo];
-        const Chunk c = load_chunk(a, lo);
-        p.r = lo;
-        p.row0 = c.row0;
-        p.n = c.n;
-        p.p0 = c.p0;
-        p.lo = own.z;
-        p.key0 = own.z + (idx - own.x) * len;
-        p.key1 = (int)min((long long)p.key0 + len, (long long)own.z + own_keys(c, own.z));
-        p.base = own.y + (idx - own.x) * c.n;
-        if (p.base < 0 || (long long)p.base + p.n > k.gr.own_most) p.r = -1;   // (lengths that contradict one another)
       }
+      const unsigned on = __ballot_sync(0xffffffffu, p.r >= 0);
       __syncwarp();
-      int* to = mine + lane * kPieceInts;
-      const int* src = reinterpret_cast<const int*>(&p);
+      if (lane >= __popc(on)) mine[lane * kPieceInts] = -1;
+      if (p.r >= 0) {
+        int* to = mine + __popc(on & ((1u << lane) - 1u)) * kPieceInts;
+        const int* src = reinterpret_cast<const int*>(&p);
 #pragma unroll
-      for (int e = 0; e < kPieceInts; ++e) to[e] = src[e];
+        for (int e = 0; e < kPieceInts; ++e) to[e] = src[e];
+      }
+      x0 = on ? __shfl_sync(0xffffffffu, end, 31 - __clz(on)) : x1;
       __syncwarp();
     };
     auto piece = [&](int i) {
@@ -213,8 +196,8 @@ __global__ void __launch_bounds__(kThreads, 2)
     int stage = 0;
     uint32_t phase = 0;
     const int quad = lane & 3, oct = lane >> 2;
-    for (int first = 0; wid + (long long)first * n_warps < total; first += kBatch) {
-      find(first);
+    while (x0 < x1) {
+      find();
       // ---- copies, running ahead of the warp's own blocks within these pieces ----
       int pi = 0, pkey = 0, at_key = -1, at_kv = 0, page = 0;   // the next block: its page id is asked for now and used then
       Piece pp = piece(0);
@@ -316,10 +299,9 @@ __global__ void __launch_bounds__(kThreads, 2)
             float sum = x.s[nt][e];
 #pragma unroll
             for (int s = 4; s < 32; s <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
-            const int row = 8 * nt + 2 * quad + e, tok = row / a.G;
+            const int row = 8 * nt + 2 * quad + e;
             if (row >= rows) continue;
-            float* to = k.gr.own_rows +
-                        ((long long)(now.base + tok) * a.h_q + now.kv * a.G + row - tok * a.G) * kStride;
+            float* to = k.gr.own_rows + (long long)(now.base + row) * kStride;
             if (oct == 0) *reinterpret_cast<float2*>(to) = make_float2(x.m[nt][e], sum);
 #pragma unroll
             for (int mt = 0; mt < 8; ++mt) {
@@ -363,7 +345,10 @@ template <typename T, int ROWS> __global__ void __launch_bounds__(256) k_own_joi
   const int row = blk / kParts * ROWS + lane % ROWS;
   const int cg = blk % kParts * (kLanes * kVec) + lane / ROWS;   // this lane's groups of channels: cg, cg + kLanes
   const int t = row / a.G, head = kv * a.G + row - t * a.G;
-  if (t >= c.n || own.y < 0 || own.y + (long long)own.w * c.n > k.gr.own_most) return;
+  if (t >= c.n) return;
+  // its pieces: the warps that have a part of its stretch of the line
+  const long long at0 = kv * k.gr.own_line[0] + line_at(own), stretch = k.gr.own_line[1];
+  const int w0 = (int)(at0 / stretch), n_own = (int)((at0 + own.w - 1) / stretch) - w0 + 1;
   float m = kNoMax, sum = 0.f;
   float4 acc[kVec];
 #pragma unroll
@@ -387,14 +372,14 @@ template <typename T, int ROWS> __global__ void __launch_bounds__(256) k_own_joi
   const bool pieces = shared && cut > 0 && cut < n_cta;
   const int last = pieces ? min(k.gr.last[cut], n_cta - 1) : 0;
   // own keys, four pieces at a time
-  const float* from = k.gr.own_rows + ((long long)(own.y + t) * a.h_q + head) * kStride;
-  const long long next = (long long)c.n * a.h_q * kStride;
-  for (int p0 = 0; p0 < own.w; p0 += 4) {
+  const float* from = k.gr.own_rows + ((long long)(kv * a.n_rows + c.row0) * a.G + w0 * ZC_PAGED_ROWS + row) * kStride;
+  constexpr int next = ZC_PAGED_ROWS * kStride;
+  for (int p0 = 0; p0 < n_own; p0 += 4) {
     float2 ms[4];
     float4 x[4][kVec];
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (p0 + u < own.w) {
+      if (p0 + u < n_own) {
         const float* at = from + (p0 + u) * next;
         ms[u] = *reinterpret_cast<const float2*>(at);
 #pragma unroll
@@ -402,7 +387,7 @@ template <typename T, int ROWS> __global__ void __launch_bounds__(256) k_own_joi
       }
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (p0 + u < own.w) take(ms[u], x[u]);
+      if (p0 + u < n_own) take(ms[u], x[u]);
   }
   if (pieces) {
     // in order: the end of the share before the item's first border, then the starts behind each border

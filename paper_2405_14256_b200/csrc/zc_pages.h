@@ -82,9 +82,10 @@ struct ZcGroups {
   const char* parts;       // [CTA][2] pieces
   float* rows;             // (maximum, sum, -, -, 128 sums) of each (row, query head)
   // the own keys' kernel
-  int4* own;               // [request] (pieces before its own, rows of pieces before, its group's keys, its pieces)
-  int own_most;            // rows of pieces that there is room for
-  float* own_rows;         // (maximum, sum, -, -, 128 sums) of each (row of a piece, query head)
+  int4* own;               // [request] (where its blocks begin on a KV head's line: low and high word, its group's keys,
+                           // its length on the line)
+  long long* own_line;     // a KV head's line, a warp's stretch of all of them
+  float* own_rows;         // (maximum, sum, -, -, 128 sums) of each row of each piece
 };
 
 // Workspace of one call: arrival counters, what the joining kernel is told, and the partial results that are joined.
