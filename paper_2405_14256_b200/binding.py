@@ -578,10 +578,11 @@ class PagedKV(_Buffers):
     may run on any stream (the constructor waits for the current one's work), attention calls that share a workspace
     on one at a time.  Tensors that a call allocates may be used on the current stream, behind what orders it after
     `stream`.
-    shared: the workspace serves attention_shared as well, for max_req requests and max_rows rows (1.6 KB more for each of
-    these rows and query heads, so max_rows is best no more than the generated tokens of a step).  scored_rows: room for the logits of attention_scored and attention_shared calls of up
-    to so many rows per request (4 bytes per slot, query head and row, in .logits, which handles over pages of one shape
-    share as they share a workspace: pass the first one's); calls of more than 16 / G rows need none."""
+    shared: the workspace serves attention_shared as well, for max_req requests and max_rows rows (11 MB more, and 1.1 KB
+    for each of these rows and query heads, so max_rows is best no more than the generated tokens of a step).
+    scored_rows: room for the logits of attention_scored and attention_shared calls of up to so many rows per request
+    (4 bytes per slot, query head and row, in .logits, which handles over pages of one shape share as they share a
+    workspace: pass the first one's); calls of more than 16 / G rows need none."""
 
     def __init__(self, k_pages, v_pages, n_q_heads: int, max_req: int = 256, max_rows: int = 8192,
                  workspace: Optional[torch.Tensor] = None, shared: bool = False, scored_rows: int = 0,
@@ -662,7 +663,7 @@ class PagedKV(_Buffers):
         if strides != self._rows(v_rows, "v_rows", n, self.n_kv_heads):
             raise ZipCacheError("k_rows and v_rows must share strides")
         _check(self._lib.zc_page_write(self.handle, k_rows.data_ptr(), v_rows.data_ptr(), _strides2(strides[0], strides[1]),
-                                   slots.data_ptr(), n, _stream_of(self._index, stream)), "zc_page_write")
+                                       slots.data_ptr(), n, _stream_of(self._index, stream)), "zc_page_write")
 
     def read(self, table, l: int, K=None, V=None, stream=None):
         """The first l tokens of every request in table [n_req, width]: K, V [n_req, n_kv_heads, l, 128]."""
@@ -693,9 +694,9 @@ class PagedKV(_Buffers):
                 return self.attention(q, table, row_start, kv_len, max_rows, window, sinks, out, row_lse, stream)
         n_req, n, width, strides, out, row_lse, raw = self._call(q, table, row_start, kv_len, out, row_lse, stream)
         _check(self._lib.zc_paged_attention(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
-                                        row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
-                                        out.data_ptr(), row_lse.data_ptr(), self._ws_at, self._ws_bytes,
-                                        raw), "zc_paged_attention")
+                                            row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
+                                            out.data_ptr(), row_lse.data_ptr(), self._ws_at, self._ws_bytes,
+                                            raw), "zc_paged_attention")
         return out, row_lse
 
     def _call(self, q, table, row_start, kv_len, out, row_lse, stream) -> tuple:
@@ -754,9 +755,9 @@ class PagedKV(_Buffers):
         logits, size = self._logits_for(min(max_rows, q.shape[0]))
         n_req, n, width, strides, out, row_lse, raw = self._call(q, table, row_start, kv_len, out, row_lse, stream)
         _check(self._lib.zc_paged_attention_scored(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
-                                               row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
-                                               at_first, at_scores, out.data_ptr(), row_lse.data_ptr(),
-                                               self._ws_at, self._ws_bytes, logits, size, raw),
+                                                   row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows, window, sinks,
+                                                   at_first, at_scores, out.data_ptr(), row_lse.data_ptr(),
+                                                   self._ws_at, self._ws_bytes, logits, size, raw),
                "zc_paged_attention_scored")
         return out, row_lse
 
@@ -771,17 +772,18 @@ class PagedKV(_Buffers):
                 return self.attention_shared(q, table, row_start, kv_len, max_rows, group_start, shared_len, scores, out,
                                              row_lse, stream)
         n_groups, index = shared_len.numel(), self._index
-        at_shared, at_start = _at_i32(shared_len, "shared_len", n_groups, index), _at_i32(group_start, "group_start", n_groups + 1, index)
+        at_shared = _at_i32(shared_len, "shared_len", n_groups, index)
+        at_start = _at_i32(group_start, "group_start", n_groups + 1, index)
         logits = size = at_scores = 0
         if scores is not None:
             at_scores = self._at_scores(scores)
             logits, size = self._logits_for(min(max_rows, q.shape[0]))
         n_req, n, width, strides, out, row_lse, raw = self._call(q, table, row_start, kv_len, out, row_lse, stream)
         _check(self._lib.zc_paged_attention_shared(self.handle, q.data_ptr(), strides, table.data_ptr(), width,
-                                               row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows,
-                                               at_start, at_shared, n_groups, at_scores,
-                                               out.data_ptr(), row_lse.data_ptr(), self.workspace.data_ptr(),
-                                               self._ws_bytes, logits, size, raw), "zc_paged_attention_shared")
+                                                   row_start.data_ptr(), kv_len.data_ptr(), n_req, n, max_rows,
+                                                   at_start, at_shared, n_groups, at_scores,
+                                                   out.data_ptr(), row_lse.data_ptr(), self.workspace.data_ptr(),
+                                                   self._ws_bytes, logits, size, raw), "zc_paged_attention_shared")
         return out, row_lse
 
     def select(self, table, kv_len, scores, keep, recent: int = 0, first=None, max_keep: int = 0, kept=None, kept_len=None,
@@ -803,11 +805,11 @@ class PagedKV(_Buffers):
         if kept_len is None:
             kept_len = torch.empty_like(kv_len) if stream is None else _new((n_req,), torch.int32, self.device, stream)
         _check(self._lib.zc_page_select(self.handle, _at_i32(table, "table", n_req * width, index), width,
-                                    _at_i32(kv_len, "kv_len", n_req, index), n_req, self._at_scores(scores),
-                                    _at_i32(keep, "keep", n_req, index), recent,
-                                    0 if first is None else _at_i32(first, "first", n_req, index),
-                                    _at_i32(kept, "kept", n_req * self.n_kv_heads * max_keep, index), max_keep,
-                                    _at_i32(kept_len, "kept_len", n_req, index), _stream_of(index, stream)), "zc_page_select")
+                                        _at_i32(kv_len, "kv_len", n_req, index), n_req, self._at_scores(scores),
+                                        _at_i32(keep, "keep", n_req, index), recent,
+                                        0 if first is None else _at_i32(first, "first", n_req, index),
+                                        _at_i32(kept, "kept", n_req * self.n_kv_heads * max_keep, index), max_keep,
+                                        _at_i32(kept_len, "kept_len", n_req, index), _stream_of(index, stream)), "zc_page_select")
         return kept, kept_len
 
     def compact(self, table, kv_len, kept, kept_len, scores=None, free_pages=None, free_state=None, free_out=None,
@@ -834,11 +836,11 @@ class PagedKV(_Buffers):
         elif free_state is not None or free_out is not None:
             raise ZipCacheError("free_state and free_out come with free_pages")
         _check(self._lib.zc_page_compact(self.handle, _at_i32(table, "table", n_req * width, index), width,
-                                     _at_i32(kv_len, "kv_len", n_req, index), n_req,
-                                     _at_i32(kept, "kept", n_req * self.n_kv_heads * max_keep, index), max_keep,
-                                     _at_i32(kept_len, "kept_len", n_req, index),
-                                     0 if scores is None else self._at_scores(scores), at_free, n_free, at_state, at_out,
-                                     _stream_of(index, stream)), "zc_page_compact")
+                                         _at_i32(kv_len, "kv_len", n_req, index), n_req,
+                                         _at_i32(kept, "kept", n_req * self.n_kv_heads * max_keep, index), max_keep,
+                                         _at_i32(kept_len, "kept_len", n_req, index),
+                                         0 if scores is None else self._at_scores(scores), at_free, n_free, at_state, at_out,
+                                         _stream_of(index, stream)), "zc_page_compact")
         return free_out
 
 
