@@ -166,6 +166,11 @@ def test_own_parts_of_every_length(zc):
     shared_case(zc, "fp16", 32, 32, 16, groups=[9, 9], shared=[700, 64], own=[500] * 18, seed=5)
 
 
+def test_more_pieces_than_a_warp_knows_at_once(zc):
+    """Long shared keys leave few SMs to 4160 short own parts: some 35 to each of their warps, which know 32 at a time."""
+    shared_case(zc, "fp16", 32, 32, 64, groups=[130], shared=[66000], own=[1 + i % 40 for i in range(130)], seed=6)
+
+
 @pytest.mark.parametrize("kw", [CASES[0], CASES[2], CASES[3], CASES[6], CASES[7], CASES[13], CASES[11]])
 def test_groups_with_scores(zc, kw):
     shared_case(zc, "bf16", scored=True, **kw)
