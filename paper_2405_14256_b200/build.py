@@ -42,7 +42,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     lib = LIB_DEBUG if debug else LIB
     if not force and not _stale(lib):
         return lib
-    cmd = [_nvcc(), "-shared", "-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-lineinfo",
+    cmd = [_nvcc(), "-shared", "--threads", "0", "-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-lineinfo",
            "-gencode", "arch=compute_100a,code=sm_100a",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC,
            "-o", lib] + (["-DZC_DEBUG"] if debug else []) + [os.path.join(CSRC, s) for s in SOURCES]
