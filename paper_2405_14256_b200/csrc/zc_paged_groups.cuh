@@ -79,8 +79,9 @@ __device__ __forceinline__ void add_all(long long* sum, long long v) {
 }
 
 // How many keys each group shares: at most what the caller says and what lies before every row of its requests, in whole
-// blocks of 16 (the keys behind them are the requests' own, as far as this call goes); none where that does not pay.  Returns how
-// many of the n_cta CTAs that share the GPU are the shared keys' (0: there are none): as many as their cost is of all.
+// blocks of 16 (the keys behind them are the requests' own, as far as this call goes); none where that does not pay.
+// Returns how many of the n_cta CTAs that share the GPU are the shared keys' (0: there are none): as many as their cost is
+// of all.
 template <int THREADS>
 __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups& gr, const GroupTables& t, int tpt, int n_cta) {
   const int tid = threadIdx.x, n = t.n;

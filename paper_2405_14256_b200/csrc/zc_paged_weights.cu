@@ -14,7 +14,8 @@ namespace {
 // ---------------------------------------------------------------- single tokens
 // A thread has four consecutive slots of a page and KV head, whose R logits each lie beside each other.  What the kernels
 // before it do not write (lengths, tables, old scores) is read for the first of its slots before it waits for them: they
-// start it only when all that came before them is complete.  Bound: HBM, or L2 where the logits are still there.
+// start it only when all that came before them is complete.  Bound: HBM, or L2 where the logits are still there: 32
+// requests of 2048-4096, 32 heads, 255 us with the attention's, which takes 232 alone; 4 of 200-512, 8 KV heads, 10.3 and 7.4.
 constexpr int kAddThreads = 256;
 
 struct AddArgs {
@@ -130,6 +131,8 @@ __global__ void __launch_bounds__(kAddThreads) k_score_add(const AddArgs w) {
 //   warps 4-7, 8-11  groups 0 and 1, a key per thread: columns 0-63 of every tile
 //   warps 12-15, 16-19  columns 64-127, whose sum the key's first thread gets at the item's end
 // (With all 128 columns a thread, and two warps to a scheduler, the exp2 unit was 65 % busy.)
+// Bound: the exp2 unit (68 % busy), the FMA pipe (53 %) and the issue slots (62 %) together: 289 us for 2048 rows behind 16000
+// tokens, 32 over 8 heads, the tensor cores alone 172.
 // Every wait is bounded; warps 0 to 2 leave where one runs out and wait for what they have in flight, the groups go on
 // with void values until no more items come.  The blocks' warps meet at the kernel's end only.
 constexpr int kThreads = 640;
@@ -185,7 +188,8 @@ __device__ __forceinline__ float2 exp2_fma(float2 x) {
                      __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 // add += the weights 2^(v * scale + less) of 32 columns; kFmaPairs of eight pairs of them on the FMA pipe, since the exp2 unit
-// alone would take eight cycles of a warp's for each, and the instructions beside it two.
+// alone would take eight cycles of a warp's for each, and the instructions beside it two (the call with 0, 1, 2, 3 pairs: 805,
+// 792, 783, 791 us).
 constexpr int kFmaPairs = 2;
 __device__ __forceinline__ void sum_weights(const float* v, const float4* less, float scale, float2 (&add)[2]) {
   const float2 sc = make_float2(scale, scale);
@@ -194,7 +198,8 @@ __device__ __forceinline__ void sum_weights(const float* v, const float4* less, 
     const float4 l = less[c];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float2 x = fma2(make_float2(v[4 * c + 2 * h], v[4 * c + 2 * h + 1]), sc, h ? make_float2(l.z, l.w) : make_float2(l.x, l.y));
+      const float2 x = fma2(make_float2(v[4 * c + 2 * h], v[4 * c + 2 * h + 1]), sc,
+                            h ? make_float2(l.z, l.w) : make_float2(l.x, l.y));
       const int pair = (2 * c + h) & 7;
       const float2 e = (pair * kFmaPairs) % 8 < kFmaPairs ? exp2_fma(x) : make_float2(zc_exp2(x.x), zc_exp2(x.y));
       add[h] = add2(add[h], e);
