@@ -368,8 +368,8 @@ int zc_paged_attention(zc_pages* p, const void* q, const int64_t q_strides[2], c
 /* zc_paged_attention for requests that begin alike: n_groups groups of consecutive requests, group g the requests
  * group_start[g] .. group_start[g + 1] - 1, the first shared_len[g] tokens of which are the same ones (a system prompt, a
  * document): their tables list the same pages for them, or copies of the same rows where a page is not filled by them.
- * Those keys and values are read once for all rows of the group, through the table of its first request, instead of
- * once per request.  group_start [device] n_groups + 1 ascending, shared_len [device] n_groups; requests in no group, and
+ * Those keys and values are read once for all rows of the group, through the table of the first of its requests that has
+ * rows in the call, instead of once per request (tables of requests without rows may hold anything).  group_start [device] n_groups + 1 ascending, shared_len [device] n_groups; requests in no group, and
  * groups too short to be worth it (down to groups of one), are attended like any.  At most 1024 groups (ZC_ECAPACITY).
  * Of a group's shared tokens those count that lie before every new row of its requests.
  *   max_rows * G must be at most 16 (ZC_EINVAL): generated tokens, one or a few per request; a chunk reads each

@@ -184,6 +184,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
         c.p0 = gt.keys[r];
         c.n = c.p0 > 0 ? gt.row[r + 1] - gt.row[r] : 0;
         k.gr.keys[r] = c.p0;   // (every CTA leaves the same where it reads it again)
+        k.gr.lead[r] = gt.lead[r];
       } else {
         c = load_chunk(a, r);
       }
@@ -635,7 +636,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (at.item > share.end.item || (at.item == share.end.item && at.t >= share.end.t)) return;
         // (only the share's first item can begin, and only its last can end, inside)
-        it.r = FORM == kGroups ? group_border(a, k.gr, r) : r;   // the first request's table has the group's pages
+        it.r = FORM == kGroups ? k.gr.lead[r] : r;   // whose table has the item's pages
         it.kv = at.item / share.items;
         it.tok0 = in_req * 2 * k.tpt;
         it.row0 = c.row0;
@@ -1246,6 +1247,7 @@ size_t carve_groups(const zc_page_config& c, int n_req, int n_rows, char* ws, Zc
   g.told = (int*)ws + ZC_PAGED_MAX_CTAS + 2;
   g.head = (int*)take(sizeof(int));
   g.keys = (int*)take(kMaxGroups * sizeof(int));
+  g.lead = (int*)take(kMaxGroups * sizeof(int));
   g.last = (int*)take(ZC_PAGED_MAX_CTAS * sizeof(int));
   g.info = (int4*)take((size_t)n_req * sizeof(int4));
   g.own = (int4*)take((size_t)n_req * sizeof(int4));

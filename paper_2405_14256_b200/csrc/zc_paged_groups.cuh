@@ -26,19 +26,20 @@ constexpr int kOwnWarps = 8;
 // What is known of the groups and the requests, in shared memory.
 struct GroupTables {
   int *border, *row;          // [n + 1] first request of a group, its first row
-  int *keys, *count;          // [n] keys that it shares (0: none), its requests that have rows
+  int *keys, *count, *lead;   // [n] keys that it shares (0: none), its requests that have rows, the first of these
   int *first, *kv;            // [n_req + 1], [n_req] a request's first row, its tokens (n_req <= kPlanReq)
   long long* sums;            // [4] costs of the shared and of the own keys, items of a KV head, keys spared
   int n;
   bool held;
-  static constexpr int kInts = 4 * kMaxGroups + 8 + 2 * kPlanReq + 3;   // (8 of them the sums)
+  static constexpr int kInts = 5 * kMaxGroups + 8 + 2 * kPlanReq + 3;   // (8 of them the sums)
   __device__ __forceinline__ GroupTables(void* at, int n_groups, int n_req) {
     sums = reinterpret_cast<long long*>(at);
     border = reinterpret_cast<int*>(sums + 4);
     row = border + kMaxGroups + 1;
     keys = row + kMaxGroups + 1;
     count = keys + kMaxGroups;
-    first = count + kMaxGroups;
+    lead = count + kMaxGroups;
+    first = lead + kMaxGroups;
     kv = first + kPlanReq + 1;
     n = n_groups;
     held = n_req <= kPlanReq;
@@ -92,6 +93,7 @@ __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups&
     if (g < n) {
       t.keys[g] = (int)min((long long)max(gr.shared[g], 0), cap);
       t.count[g] = 0;
+      t.lead[g] = 0x7fffffff;
     }
   }
   if (t.held)
@@ -113,14 +115,16 @@ __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups&
     const int top = __reduce_max_sync(0xffffffffu, g);
     if (__all_sync(0xffffffffu, g == top || g < 0)) {
       const int least = __reduce_min_sync(0xffffffffu, g < 0 ? 0x7fffffff : c.p0);
-      const int count = __popc(__ballot_sync(0xffffffffu, g >= 0));
+      const unsigned have = __ballot_sync(0xffffffffu, g >= 0);
       if (top >= 0 && (tid & 31) == 0) {
         atomicMin(&t.keys[top], least);
-        atomicAdd(&t.count[top], count);
+        atomicAdd(&t.count[top], __popc(have));
+        atomicMin(&t.lead[top], r + __ffs(have) - 1);
       }
     } else if (g >= 0) {
       atomicMin(&t.keys[g], c.p0);
       atomicAdd(&t.count[g], 1);
+      atomicMin(&t.lead[g], r);
     }
   }
   __syncthreads();

@@ -75,6 +75,7 @@ struct ZcGroups {
   int* told;               // 1 + the CTAs that work on them, once one of them knows; zero before and after every call
   int* head;               // how many these are
   int* keys;               // [n] how many of the shared tokens the call reads once
+  int* lead;               // [n] the request through whose table: the group's first that has rows (others may be anything)
   int4* info;              // [request] (its group's keys, its first row among the group's, the group's first item, -)
   int* cut;                // [item][KV head] 0: the result is with the rows; c: in pieces, the second CTA c's
   int* last;               // [CTA] the last of the CTAs that have pieces of the item that the border before this one cuts
