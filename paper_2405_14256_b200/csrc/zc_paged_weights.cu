@@ -11,6 +11,15 @@
 
 namespace {
 
+// A row without a log-sum-exp that sees keys has a logit that is NaN or +inf, or none above -inf: its weights are NaN.
+__device__ __forceinline__ float or_nan(float lse) { return lse == -INFINITY ? __int_as_float(0x7fffffff) : lse; }
+// min(x, 0), NaN where x is.
+__device__ __forceinline__ float at_most_0(float x) {
+  float y;
+  asm("min.NaN.f32 %0, %1, 0f00000000;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // ---------------------------------------------------------------- single tokens
 // A thread has four consecutive slots of a page and KV head, whose R logits each lie beside each other.  What the kernels
 // before it do not write (lengths, tables, old scores) is read for the first of its slots before it waits for them: they
@@ -71,12 +80,12 @@ __global__ void __launch_bounds__(kAddThreads) k_score_add(const AddArgs w) {
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](int row, const float (&x)[4]) {
       const int tok = a.max_rows == 1 ? 0 : row / a.G, p = c.p0 + tok;
-      const float less = lse[(long long)tok * a.h_q + row - tok * a.G];
+      const float less = or_nan(lse[(long long)tok * a.h_q + row - tok * a.G]);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const bool seen = key + k <= p && (key + k > p - a.window || key + k < a.sinks);
         // (a weight is at most 1: beyond 2^24 the logits' rounding alone would make it more)
-        if (seen) sum[k] += zc_exp2(fminf(x[k] - less, 0.f));
+        if (seen) sum[k] += zc_exp2(at_most_0(x[k] - less));
       }
     };
     if (R) {
@@ -482,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < 4; ++i) {
           const int col = 4 * lane + i, in = col / a.G, tok = t * w.tpt + in;
           const bool on = in < w.tpt && tok < it.n;
-          less[i] = on ? -w.lse[(long long)(it.row0 + tok) * a.h_q + it.kv * a.G + col - in * a.G] : -INFINITY;
+          less[i] = on ? -or_nan(w.lse[(long long)(it.row0 + tok) * a.h_q + it.kv * a.G + col - in * a.G]) : -INFINITY;
           pos[i] = on ? it.p0 + tok : -1;
         }
         bool mild = true;
@@ -553,7 +562,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int4 p = where[8 * h + c];
                 auto one = [&](float x, float m, int at_pos) {
                   const bool seen = at_pos >= key && at_pos - key < window;   // (-1: no row)
-                  return seen ? zc_exp2(fminf(fmaf(x, scale, m), 0.f)) : 0.f;
+                  return seen ? zc_exp2(at_most_0(fmaf(x, scale, m))) : 0.f;
                 };
                 add[0] = add2(add[0], make_float2(one(v[4 * c], l.x, p.x), one(v[4 * c + 1], l.y, p.y)));
                 add[1] = add2(add[1], make_float2(one(v[4 * c + 2], l.z, p.z), one(v[4 * c + 3], l.w, p.w)));

@@ -95,3 +95,124 @@ def test_a_group_goes_on_when_its_first_requests_have_ended(zc, kw, scored, left
         first = [s for s, n in zip(kw["shared"], kw["groups"]) for _ in range(n)]
         want, tol = er.add_weights(before, q, k, table, row_start, kv, first, 0, 0)
         assert ((scores.double() - want).abs() <= tol).all()
+
+
+# ---------------------------------------------------------------- what is not a number
+def poisoned(q, kp, table, row_start, kv_len, window, sinks):
+    """[pages, heads, page] bool: slots that a row sees one of whose logits is NaN or +inf in 64 bits, where its weights are NaN."""
+    n_pages, page, hkv, _ = kp.shape
+    G = q.shape[1] // hkv
+    bad = torch.zeros((n_pages, hkv, page), dtype=torch.bool, device=DEV)
+    for r, n in enumerate(kv_len):
+        a, e = row_start[r], row_start[r + 1]
+        if e <= a or n <= 0:
+            continue
+        k, _ = ref.rows_of_request(kp, kp, table[r], n)
+        j, p0 = torch.arange(n, device=DEV), n - (e - a)
+        i = torch.arange(p0, n, device=DEV)[:, None]
+        seen = (j <= i) & (((i - j) < window) | (j < sinks) if window else torch.ones_like(j, dtype=torch.bool))
+        ids = torch.as_tensor(table[r], device=DEV).long()[j // page]
+        for h in range(hkv):
+            for g in range(G):
+                x = q[a:e, h * G + g].double() @ k[:, h].double().T
+                row = (seen & (x.isnan() | (x == math.inf))).any(1)
+                at = (seen & row[:, None]).any(0)
+                bad[ids[at], h, (j % page)[at]] = True
+    return bad
+
+
+NAN = [
+    # single tokens, few rows, chunks; under a window rows that do not see the key keep their weights
+    dict(hq=8, hkv=2, page=16, past=[100, 300, 33], new=[1, 1, 1]),
+    dict(hq=4, hkv=2, page=16, past=[100, 300, 33], new=[3, 1, 4]),
+    dict(hq=18, hkv=2, page=16, past=[100, 40], new=[1, 1]),
+    dict(hq=8, hkv=2, page=64, past=[100, 300, 3000], new=[1, 1, 1], window=200, sinks=4),
+    dict(hq=8, hkv=2, page=16, past=[100, 300, 0], new=[40, 130, 300]),
+    dict(hq=6, hkv=2, page=64, past=[500, 20], new=[200, 150], window=90, sinks=3),
+]
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("where,value", [("key", math.nan), ("query", math.nan), ("query", math.inf), ("key", math.inf)])
+@pytest.mark.parametrize("kw", NAN)
+def test_weights_of_rows_that_are_not_numbers_are_none(zc, kw, where, value, dtype):
+    """A row with a logit that is no finite number has no softmax: its weights are NaN for every token that it sees, and
+    no other token's score is touched by it."""
+    hq, hkv, page, past, new = (kw[x] for x in ("hq", "hkv", "page", "past", "new"))
+    window, sinks = kw.get("window", 0), kw.get("sinks", 0)
+    rng, gen, dt = np.random.RandomState(1), torch.Generator(device=DEV).manual_seed(2), TYPES[dtype]
+    kv = [p + n for p, n in zip(past, new)]
+    table, n_pages = ref.make_table(rng, kv, page)
+    k, v = ref.make_pages(gen, n_pages, page, hkv, dt, False, DEV)
+    row_start = [0] + np.cumsum(new).tolist()
+    q = torch.randn(row_start[-1], hq, D, generator=gen, device=DEV).to(dt)
+    k2, q2 = k.clone(), q.clone()
+    if where == "key":
+        q[..., 7] = q[..., 7].abs() + 0.5                         # (+inf then makes +inf of every logit)
+        q2 = q.clone()
+        for r, t in ((0, past[0] // 2), (1, kv[1] - 1)):      # in the past, and the newest token's own
+            k2[int(table[r][t // page]), t % page, r % hkv, 7] = value
+    else:
+        q2[0, 0, 5] = value
+        q2[row_start[1] + new[1] // 2, hq - 1, 100] = value
+    start = torch.rand((n_pages, hkv, page), generator=gen, device=DEV)
+    most = max(new)
+    few = most * (hq // hkv) <= 16
+    scores = []
+    for keys, queries in ((k, q), (k2, q2)):
+        pool = zc.PagedKV(keys, v, hq, max_req=len(kv), max_rows=row_start[-1], scored_rows=most if few else 0)
+        s = start.clone()
+        pool.attention_scored(queries, i32(table), i32(row_start), i32(kv), most, s, window=window, sinks=sinks)
+        settled(zc)
+        scores.append(s)
+    clean, got = scores
+    bad = poisoned(q2, k2, table, row_start, kv, window, sinks)
+    assert bad.any() and not bad.all()
+    assert torch.isnan(got[bad]).all()
+    # the same rows weigh the others: each weight off by 2^-18 of it at most in either call, sums by their roundings
+    tol = clean * (2 * 2.0 ** -18 + 2 * (most * (hq // hkv) + 2) * 2.0 ** -24)
+    assert ((got - clean).abs() <= tol)[~bad].all()
+
+
+@pytest.mark.parametrize("past,new", [([100, 30], [1, 2]), ([100, 30], [40, 130])])
+def test_a_logit_of_minus_infinity_is_a_weight_of_zero(zc, past, new):
+    hq, hkv, page = 8, 2, 16
+    gen, dt = torch.Generator(device=DEV).manual_seed(2), torch.bfloat16
+    kv = [p + n for p, n in zip(past, new)]
+    table, n_pages = ref.make_table(np.random.RandomState(1), kv, page)
+    k, v = ref.make_pages(gen, n_pages, page, hkv, dt, False, DEV)
+    row_start = [0] + np.cumsum(new).tolist()
+    q = torch.randn(row_start[-1], hq, D, generator=gen, device=DEV).to(dt)
+    q[..., 7] = q[..., 7].abs() + 0.5
+    at = (int(table[1][1]), 3, 1)                                 # token 19 of request 1, KV head 1
+    k[at][7] = -math.inf
+    start = torch.rand((n_pages, hkv, page), generator=gen, device=DEV)
+    scores = start.clone()
+    pool = zc.PagedKV(k, v, hq, max_req=2, max_rows=row_start[-1], scored_rows=2)
+    pool.attention_scored(q, i32(table), i32(row_start), i32(kv), max(new), scores)
+    settled(zc)
+    want, tol = er.add_weights(start, q, k, table, row_start, kv, [0, 0], 0, 0)
+    assert ((scores.double() - want).abs() <= tol).all()
+    assert scores[at[0], at[2], at[1]] == (start[at[0], at[2], at[1]] if past[1] > 19 else 0)
+
+
+def test_shared_weights_of_rows_that_are_not_numbers(zc):
+    rng, gen, dt = np.random.RandomState(1), torch.Generator(device=DEV).manual_seed(2), torch.bfloat16
+    hq, hkv, page = 8, 2, 16
+    table, kv, starts, n_pages, copies = er.make_groups(rng, page, [6], [960], [30, 1, 70, 5, 16, 17])
+    table = wide(table, page, hkv, 1)
+    k, v = ref.make_pages(gen, n_pages, page, hkv, dt, False, DEV)
+    q = torch.randn(6, hq, D, generator=gen, device=DEV).to(dt)
+    q2 = q.clone()
+    q2[2, 5, 3] = math.nan
+    pool = zc.PagedKV(k, v, hq, max_req=6, max_rows=6, shared=True, scored_rows=1)
+    got = []
+    for x in (q, q2):
+        s = torch.zeros((n_pages, hkv, page), device=DEV)
+        pool.attention_shared(x, i32(table), i32(range(7)), i32(kv), 1, i32(starts), i32([960]), scores=s)
+        settled(zc)
+        got.append(s)
+    bad = torch.zeros_like(got[0], dtype=torch.bool)
+    for t in range(960, kv[2]):
+        bad[int(table[2][t // page]), 1, t % page] = True
+    assert torch.isnan(got[1][bad]).all() and torch.equal(got[0][~bad], got[1][~bad])
