@@ -240,6 +240,7 @@ constexpr int kMoveStage = kMoveSteps * kMoveThreads * 16;   // bytes of a round
 constexpr int kMoveSeg = 2048;                               // rows whose places are known
 constexpr int kMoveSmem = kMoveStages * kMoveStage + 2 * kMoveSeg * 8;
 constexpr uint64_t kNowhere = ~0ull;
+constexpr int kGiveBlocks = 16;                              // that put pages back
 
 struct CompactArgs {
   char *k, *v;
@@ -258,40 +259,68 @@ __device__ __forceinline__ bool load_kept(const CompactArgs& a, int r, int* n, i
   *len = max(a.kept_len[r], 0);
   return *len < *n && *len <= a.max_keep;
 }
-__device__ __forceinline__ int pages_left_over(const CompactArgs& a, int r) {
+// The table's columns of request r whose pages lie behind its kept tokens.
+__device__ __forceinline__ int2 left_over(const CompactArgs& a, int r) {
   int n, len;
-  if (!load_kept(a, r, &n, &len)) return 0;
+  if (!load_kept(a, r, &n, &len)) return make_int2(0, 0);
   const int size = 1 << a.page_log2;
-  return ((n + size - 1) >> a.page_log2) - ((len + size - 1) >> a.page_log2);
+  return make_int2((len + size - 1) >> a.page_log2, (n + size - 1) >> a.page_log2);
 }
 
-// The pages behind the kept tokens of request r, put back in front of the free ones.
-__device__ __forceinline__ void give_back(const CompactArgs& a, int r) {
-  __shared__ int s_sum[2];
-  if (threadIdx.x < 2) s_sum[threadIdx.x] = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < a.n_req; i += kMoveThreads) {
-    const int gone = pages_left_over(a, i);
-    if (gone) {
-      atomicAdd(&s_sum[1], gone);
-      if (i < r) atomicAdd(&s_sum[0], gone);
+// Requests whose pages a block puts back: enough for some 16 blocks at most, each of which counts what comes behind its own.
+__device__ __host__ __forceinline__ int give_share(int n_req) { return (n_req + kGiveBlocks - 1) / kGiveBlocks; }
+// The pages behind the kept tokens, put back in front of the free ones, request by request; entries that are no page (where
+// the free list had run out) are not.  Block i has requests i * share on; a warp counts a request's pages, or stores them,
+// from the last one to the first: the list's end is known beforehand, its beginning is not.
+__device__ __forceinline__ void give_back(const CompactArgs& a, int block) {
+  constexpr int kWarps = kMoveThreads / 32;
+  __shared__ int s_count[kWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int share = give_share(a.n_req), r0 = min(a.n_req, block * share), r1 = min(a.n_req, r0 + share);
+  const int next = min(max(a.free_state[0], 0), a.n_free);
+  auto is_page = [&](int page) { return page >= 0 && page < a.n_pages; };
+  auto all_of = [&](int v) {   // the block's sum
+    v = __reduce_add_sync(0xffffffffu, v);
+    __syncthreads();
+    if (lane == 0) s_count[warp] = v;
+    __syncthreads();
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) sum += s_count[w];
+    return sum;
+  };
+  int behind = 0;   // this thread's
+  for (int r = r1 + warp; r < a.n_req; r += kWarps) {
+    const int2 cols = left_over(a, r);
+    for (int i = cols.x + lane; i < cols.y; i += 32) behind += is_page(a.table[(long long)r * a.width + i]);
+  }
+  int end = next - all_of(behind);   // places from here on are those of requests behind
+  for (int g = r1; g > r0; g -= kWarps) {   // eight requests at a time, the last ones first
+    const int r = g - 1 - warp;
+    const int2 cols = r >= r0 ? left_over(a, r) : make_int2(0, 0);
+    const int32_t* row = a.table + (long long)max(r, 0) * a.width;
+    int mine = 0;
+    for (int i = cols.x + lane; i < cols.y; i += 32) mine += is_page(row[i]);
+    const int sum = all_of(mine);
+    int at = end;
+    for (int w = 0; w < warp; ++w) at -= s_count[w];
+    end -= sum;
+    for (int c = cols.y; c > cols.x; c -= 32) {   // 32 columns, the last of them lane 0's
+      const int i = c - 1 - lane, page = i >= cols.x ? row[i] : -1;
+      const unsigned on = __ballot_sync(0xffffffffu, is_page(page));
+      const int to = at - 1 - __popc(on & ((1u << lane) - 1u));
+      if (is_page(page) && to >= 0) a.free_pages[to] = page;
+      at -= __popc(on);
     }
   }
-  __syncthreads();
-  const int total = s_sum[1], mine = pages_left_over(a, r);
-  const int next = min(max(a.free_state[0], 0), a.n_free);
-  const int at = next - total + s_sum[0];
-  const int stay = mine ? (max(a.kept_len[r], 0) + (1 << a.page_log2) - 1) >> a.page_log2 : 0;
-  for (int i = threadIdx.x; i < mine; i += kMoveThreads)
-    if (at + i >= 0) a.free_pages[at + i] = a.table[(long long)r * a.width + stay + i];
-  if (r == 0 && threadIdx.x == 0) {
-    a.free_out[0] = max(0, next - total);
+  if (block == 0 && threadIdx.x == 0) {
+    a.free_out[0] = max(0, end);
     a.free_out[1] = min(a.free_state[1], a.n_free);
-    a.free_out[2] = max(0, total - next);
+    a.free_out[2] = max(0, -end);
   }
 }
 
-// Block: ((request, KV head) * 2 + tensor) * PARTS + part of the channels; behind them one per request for its pages.
+// Block: ((request, KV head) * 2 + tensor) * PARTS + part of the channels; behind them those that give pages back.
 template <int PARTS>
 __global__ void __launch_bounds__(kMoveThreads, 2) k_page_compact(const CompactArgs a) {
   constexpr int kLanes = 16 / PARTS, kAtOnce = kMoveThreads / kLanes;   // threads to a row's part, rows to a step
@@ -401,7 +430,7 @@ cudaError_t launch_compact(const CompactArgs& a, cudaStream_t st) {
   static std::atomic<unsigned long long> allowed{0};
   const cudaError_t e = zc_allow_smem(k_page_compact<PARTS>, kMoveSmem, &allowed);
   if (e != cudaSuccess) return e;
-  const int grid = 2 * PARTS * a.n_req * a.h_kv + (a.free_pages ? a.n_req : 0);
+  const int share = give_share(a.n_req), grid = 2 * PARTS * a.n_req * a.h_kv + (a.free_pages ? (a.n_req + share - 1) / share : 0);
   return zc_launch_early(k_page_compact<PARTS>, dim3((unsigned)grid), dim3(kMoveThreads), kMoveSmem, st, a);
 }
 

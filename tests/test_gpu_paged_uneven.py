@@ -216,3 +216,69 @@ def test_shared_weights_of_rows_that_are_not_numbers(zc):
     for t in range(960, kv[2]):
         bad[int(table[2][t // page]), 1, t % page] = True
     assert torch.isnan(got[1][bad]).all() and torch.equal(got[0][~bad], got[1][~bad])
+
+
+# ---------------------------------------------------------------- pages that are none
+def freed(table, n_pages, page, kv_len, lens, free, state):
+    """The free list after the pages behind the kept tokens are put back, and its state; entries that are no page are not."""
+    gone = [int(x) for r, (n, m) in enumerate(zip(kv_len, lens)) if m < n
+            for x in table[r][-(-m // page): -(-n // page)] if 0 <= x < n_pages]
+    free, nxt = list(free), min(max(state[0], 0), len(free))
+    for i, p in enumerate(gone):
+        if nxt - len(gone) + i >= 0:
+            free[nxt - len(gone) + i] = p
+    return free, [max(0, nxt - len(gone)), min(state[1], len(free)), max(0, len(gone) - nxt)]
+
+
+@pytest.mark.parametrize("page,lengths,lens,room", [
+    (16, [300, 17, 0, 40, 500], [128, 17, 0, 16, 0], 30), (64, [5000, 700], [1, 640], 200), (16, [160] * 300, [16] * 300, 3000),
+    (16, [160] * 300, [16 * (i % 11) for i in range(300)], 700), (256, [4000], [0], 5), (16, [30000], [9000], 2000),
+    (16, [20, 9000, 33], [4, 0, 0], 600)])
+@pytest.mark.parametrize("holes", [0.0, 0.3, 1.0])
+def test_only_pages_are_given_back(zc, page, lengths, lens, room, holes):
+    rng, gen = np.random.RandomState(len(lengths)), torch.Generator(device=DEV).manual_seed(1)
+    table, n_pages = ref.make_table(rng, lengths, page)
+    table = table.copy()
+    for r, m in enumerate(lens):
+        behind = np.arange(table.shape[1]) >= -(-m // page)
+        hole = behind & (rng.rand(table.shape[1]) < holes)
+        table[r, hole] = rng.choice([-1, n_pages, 2 ** 31 - 1, -2 ** 31], size=int(hole.sum()))
+    k, v = ref.make_pages(gen, n_pages, page, 1, torch.float16, False, DEV)
+    pool = zc.PagedKV(k, v, 1, max_req=0, max_rows=0)
+    most = max(1, max(lens))
+    kept = i32(np.broadcast_to(np.arange(most), (len(lens), 1, most)).copy())
+    free = rng.randint(0, 1000, room).tolist()
+    state = [room - 2, room - 1, 5]
+    dev = i32(free)
+    out = pool.compact(i32(table), i32(lengths), kept, i32(lens), None, dev, i32(state))
+    settled(zc)
+    want, want_state = freed(table, n_pages, page, lengths, lens, free, state)
+    assert dev.tolist() == want and out.tolist() == want_state
+
+
+def test_thinning_out_where_the_pages_have_run_out(zc):
+    """A step asks for more pages than are free; the requests are thinned out as they stand, and the next step's pages come
+    from the list: every page is held once, and none is none."""
+    page, hkv, n_pages, width = 16, 2, 24, 12
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    k, v = ref.make_pages(gen, n_pages, page, hkv, torch.bfloat16, False, DEV)
+    scores = torch.rand((n_pages, hkv, page), generator=gen, device=DEV)
+    pool = zc.PagedKV(k, v, hkv, max_req=0, max_rows=0)
+    free, table = i32(np.random.RandomState(1).permutation(n_pages)), torch.full((3, width), -1, dtype=torch.int32, device=DEV)
+    one, two = zc.StepTables(3, 400), zc.StepTables(3, 400)
+    one.build(page, i32([0, 0, 0]), i32([160, 100, 170]), free, i32([0, n_pages, 0]), table)
+    settled(zc)
+    assert one.free_state.tolist() == [n_pages, n_pages, 4] and (table[2, :11] == -1).sum() == 4
+    keep = i32([64, 100, 60])
+    kept, length = pool.select(table, one.kv_len, scores, keep, recent=8, first=i32([4, 4, 4]), max_keep=100)
+    state = pool.compact(table, one.kv_len, kept, length, scores, free, one.free_state)
+    settled(zc)
+    assert length.tolist() == [64, 100, 60]
+    back = (10 - 4) + (11 - 4 - 4)                   # request 2 held 7 of its 11 pages
+    assert state.tolist() == [n_pages - back, n_pages, 0] and free.min() >= 0
+    two.build(page, length, i32([48, 10, 40]), free, state, table)
+    settled(zc)
+    assert two.free_state.tolist()[2] == 0 and (two.slots[:98] >= 0).all()
+    held = [int(x) for r, n in enumerate(two.kv_len.tolist()) for x in table[r, : -(-n // page)]]
+    left = free[int(two.free_state[0]):].tolist()
+    assert sorted(held + left) == list(range(n_pages))
