@@ -419,9 +419,9 @@ int zc_scores_workspace(const zc_page_config* cfg, int max_rows, size_t* bytes);
  *   scores as zc_paged_attention_scored leaves them (16-byte aligned);
  *   kept [device] n_req x h_kv x max_keep int32: positions, ascending, -1 behind them;  kept_len [device] n_req: how
  *   many, the same for all heads.
- * first[r] + recent tokens are kept even where keep[r] is less.  A request that has no more than its keep[r], or whose
- * first and recent tokens alone are more than max_keep, stays as it is: kept_len[r] = kv_len[r] (of which kept lists
- * max_keep at most).  Outputs may not overlap inputs. */
+ * first[r] + recent tokens are kept even where keep[r] is less.  A request that has no more than its keep[r] (even where
+ * that is more than max_keep), or whose first and recent tokens alone are more than max_keep, stays as it is:
+ * kept_len[r] = kv_len[r] (of which kept lists max_keep at most).  Outputs may not overlap inputs. */
 int zc_page_select(zc_pages* p, const int32_t* table, int table_width, const int32_t* kv_len, int n_req,
                    const float* scores, const int32_t* keep, int recent, const int32_t* first, int32_t* kept,
                    int max_keep, int32_t* kept_len, zc_stream_t stream);

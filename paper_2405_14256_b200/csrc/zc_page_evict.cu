@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) k_page_select(const S
   const int first = a.first ? min(max(a.first[r], 0), n) : 0;
   const int recent = min(a.recent, n - first);
   const int budget = max(min(max(a.keep[r], 0), a.max_keep), first + recent);
-  const bool whole = budget >= n || budget > a.max_keep;   // nothing is evicted
+  const bool whole = a.keep[r] >= n || budget >= n || budget > a.max_keep;   // nothing is evicted
   const int len = whole ? n : budget;
   int32_t* kept = a.kept + (long long)blockIdx.x * a.max_keep;
   if (head == 0 && tid == 0) a.kept_len[r] = len;

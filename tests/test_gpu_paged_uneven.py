@@ -282,3 +282,30 @@ def test_thinning_out_where_the_pages_have_run_out(zc):
     held = [int(x) for r, n in enumerate(two.kv_len.tolist()) for x in table[r, : -(-n // page)]]
     left = free[int(two.free_state[0]):].tolist()
     assert sorted(held + left) == list(range(n_pages))
+
+
+# ---------------------------------------------------------------- budgets and lists
+def test_a_request_within_its_budget_stays_whole_though_the_list_is_shorter(zc):
+    """n <= keep[r] tokens stay, listed as far as the list goes; compaction leaves them; one token more is a selection."""
+    page, hkv = 16, 2
+    lengths, keep = [100, 100, 121, 120, 40, 41, 41], [100, 120, 120, 2 ** 31 - 1, 40, 41, 40]
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    table, n_pages = ref.make_table(np.random.RandomState(1), lengths, page)
+    k, v = ref.make_pages(gen, n_pages, page, hkv, torch.float16, False, DEV)
+    scores = torch.rand((n_pages, hkv, page), generator=gen, device=DEV)
+    pool = zc.PagedKV(k, v, hkv, max_req=0, max_rows=0)
+    kept, length = pool.select(i32(table), i32(lengths), scores, i32(keep), 4, max_keep=40)
+    settled(zc)
+    assert length.tolist() == [100, 100, 40, 120, 40, 41, 40]
+    for r in (0, 1, 3, 4, 5):
+        assert (kept[r].cpu() == torch.arange(40)).all()
+    for r in (2, 6):
+        assert all((kept[r, h, 1:] > kept[r, h, :-1]).all() and kept[r, h, -4:].tolist() == list(range(lengths[r] - 4, lengths[r]))
+                   for h in range(hkv))
+    k2, v2, s2 = k.clone(), v.clone(), scores.clone()
+    free = i32([0] * 30)
+    state = pool.compact(i32(table), i32(lengths), kept, length, scores, free, i32([20, 30, 0]))
+    settled(zc)
+    assert state.tolist() == [20 - 5, 30, 0]              # 121 to 40 tokens: 8 pages to 3; 41 and 40 lie on three
+    still = torch.as_tensor(np.unique(np.concatenate([table[r][: -(-lengths[r] // page)] for r in (0, 1, 3, 4, 5)])), device=DEV).long()
+    assert torch.equal(k[still], k2[still]) and torch.equal(v[still], v2[still]) and torch.equal(scores[still], s2[still])
