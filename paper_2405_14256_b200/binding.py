@@ -786,17 +786,19 @@ class PagedKV(_Buffers):
                                                    self._ws_bytes, logits, size, raw), "zc_paged_attention_shared")
         return out, row_lse
 
-    def select(self, table, kv_len, scores, keep, recent: int = 0, first=None, max_keep: int = 0, kept=None, kept_len=None,
-               stream=None):
+    def select(self, table, kv_len, scores, keep, recent: int = 0, first=None, max_keep: Optional[int] = None, kept=None,
+               kept_len=None, stream=None):
         """The tokens that each request keeps, per KV head: the first first[r] ones, the last `recent` ones, and by score as
         many between them as make keep[r] in all (int32 [n_req] each; equal scores: the lower position).  Returns
-        kept [n_req, n_kv_heads, max_keep] (int32 positions, ascending, -1 behind them; max_keep from a given kept, or as
-        said) and kept_len [n_req], the requests' new lengths; what has no more than its keep stays as it is."""
+        kept [n_req, n_kv_heads, max_keep] (int32 positions, ascending, -1 behind them; max_keep is a given kept's, else
+        it has to be said: no request that is thinned out keeps more) and kept_len [n_req], the requests' new lengths; what has no more than its keep stays as it is."""
         if _current_device() != self._index:
             with torch.cuda.device(self._index):
                 return self.select(table, kv_len, scores, keep, recent, first, max_keep, kept, kept_len, stream)
         n_req, width, index = kv_len.numel(), table.shape[-1], self._index
         if kept is None:
+            if max_keep is None or max_keep < 0:
+                raise ZipCacheError(f"max_keep: expected the lists' length where no kept is given, got {max_keep}")
             kept = _new((n_req, self.n_kv_heads, max_keep), torch.int32, self.device, stream)
         elif kept.dim() == 3:
             max_keep = kept.shape[2]

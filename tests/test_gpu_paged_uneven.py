@@ -309,3 +309,21 @@ def test_a_request_within_its_budget_stays_whole_though_the_list_is_shorter(zc):
     assert state.tolist() == [20 - 5, 30, 0]              # 121 to 40 tokens: 8 pages to 3; 41 and 40 lie on three
     still = torch.as_tensor(np.unique(np.concatenate([table[r][: -(-lengths[r] // page)] for r in (0, 1, 3, 4, 5)])), device=DEV).long()
     assert torch.equal(k[still], k2[still]) and torch.equal(v[still], v2[still]) and torch.equal(scores[still], s2[still])
+
+
+def test_a_selection_says_how_long_its_lists_are(zc):
+    page, hkv = 16, 2
+    table, n_pages = ref.make_table(np.random.RandomState(1), [100], page)
+    k = torch.zeros((n_pages, page, hkv, D), dtype=torch.float16, device=DEV)
+    scores = torch.zeros((n_pages, hkv, page), device=DEV)
+    pool = zc.PagedKV(k, k, hkv, max_req=0, max_rows=0)
+    args = (i32(table), i32([100]), scores, i32([20]))
+    for bad in (dict(), dict(recent=8), dict(max_keep=-1)):
+        with pytest.raises(zc.ZipCacheError, match="max_keep"):
+            pool.select(*args, **bad)
+    kept, length = pool.select(*args, kept=torch.empty((1, hkv, 20), dtype=torch.int32, device=DEV))
+    settled(zc)
+    assert length.tolist() == [20] and kept[0, 0].tolist() == list(range(20))
+    kept, length = pool.select(*args, max_keep=0)          # said so: nothing is kept
+    settled(zc)
+    assert kept.shape == (1, hkv, 0) and length.tolist() == [0]
