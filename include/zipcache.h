@@ -397,10 +397,12 @@ int zc_pages_shared_workspace(const zc_page_config* cfg, int n_req, int n_rows, 
  * s the scaled logits (base 2).  Tokens that came with this call (the last n_r of kv_len[r]) start from A, older ones
  * add it to the score they have; so a slot needs no clearing before a new token takes it.
  *   scores [device, 16-byte aligned] n_pages x h_kv x page_size floats, contiguous, indexed by slot as the pages are;
- *   first [device or NULL] n_req: tokens before first[r] have no score (pages that other requests share, say), theirs
- *   are left as they were, as are those of tokens that no row of the call sees.  A slot that two requests of the call
- *   score ends with either's sum.  row_lse must be given.  Sums are fp32, of fp32 weights, in a fixed order.  A row with
- *   a logit that is NaN or +inf (or with none above -inf) has no weights: the tokens that it sees get NaN.
+ *   first [device or NULL] n_req: tokens before first[r] have no score (pages that other requests of the call share, say),
+ *   theirs are left as they were, as are those of tokens that no row of the call sees.  A slot that two requests of the
+ *   call score ends with a number that is neither's sum, nor the same every time: the logits that single tokens leave are
+ *   one place to a slot.  It lies between 0 and the old score plus either's rows times G; other slots are not touched by it.
+ *   row_lse must be given.  Sums are fp32, of fp32 weights, in a fixed order.  A row with a logit that is NaN or +inf (or
+ *   with none above -inf) has no weights: the tokens that it sees get NaN.
  *   logits [device, 16-byte aligned]: scratch of calls whose max_rows * G is at most 16 (zc_scores_workspace for that
  *   max_rows; none for others, NULL then).  Nothing in it survives a call; it must not be used by calls that may run at
  *   the same time.

@@ -745,7 +745,8 @@ class PagedKV(_Buffers):
                          sinks: int = 0, out=None, row_lse=None, stream=None):
         """attention that also adds up the weight of every cached token, over the request's rows and the query heads of a KV
         head, in scores [n_pages, n_kv_heads, page_size] (float32, contiguous): the call's new tokens start from it, older
-        ones add it to what they have; tokens before first[r] (int32 [n_req]; None: 0) have no score."""
+        ones add it to what they have; tokens before first[r] (int32 [n_req]; None: 0) have no score.  Tokens that requests of
+        the call share belong there: a slot that two of them score ends with neither's sum."""
         if _current_device() != self._index:
             with torch.cuda.device(self._index):
                 return self.attention_scored(q, table, row_start, kv_len, max_rows, scores, first, window, sinks, out,
@@ -766,7 +767,7 @@ class PagedKV(_Buffers):
         """attention of generated tokens (max_rows * G at most 16) for groups of consecutive requests that begin alike:
         group g, the requests group_start[g] .. group_start[g + 1] - 1, shares its first shared_len[g] tokens, whose keys
         and values are read once for all of them (int32 [n_groups + 1] and [n_groups]).  scores: as attention_scored's,
-        with the shared tokens for `first`.  For handles made with shared=True."""
+        with shared_len for `first`, which then says all that the tables share.  For handles made with shared=True."""
         if _current_device() != self._index:
             with torch.cuda.device(self._index):
                 return self.attention_shared(q, table, row_start, kv_len, max_rows, group_start, shared_len, scores, out,

@@ -1,7 +1,8 @@
 // The weight that attention gives every cached token of a call, added up over the request's rows and the query heads of
 // a KV head:  A[j, h] = sum over rows i of 2^(s_ij - lse_i),  s the scaled logits and lse the rows' log-sum-exp, base 2.
 // The step's own tokens begin with it, older ones add it to what they have.  Every sum is formed by one thread in a
-// fixed order, in fp32, and a slot is written by one thread: no atomics, the same bits every time.
+// fixed order, in fp32, and a slot is written by one thread of each request that scores it (one, if the caller leaves shared
+// pages out): no atomics, the same bits every time.
 //
 // Single tokens: the attention kernel has left its logits beside the slots, k_score_add reads them once the log-sum-exp
 // is known (4 bytes per key and query row instead of the key's 256).  Chunks: the logits are computed again on the

@@ -327,3 +327,51 @@ def test_a_selection_says_how_long_its_lists_are(zc):
     kept, length = pool.select(*args, max_keep=0)          # said so: nothing is kept
     settled(zc)
     assert kept.shape == (1, hkv, 0) and length.tolist() == [0]
+
+
+# ---------------------------------------------------------------- slots that two requests score
+@pytest.mark.parametrize("new", [1, 40])
+def test_slots_that_two_requests_score_hold_some_number_and_others_their_own(zc, new):
+    """Pages that requests share belong before `first`.  Where they do not, their slots end with a number of 0 to what the
+    requests' rows could add to the old score; every other slot is as if nothing were shared."""
+    hq, hkv, page, shared = 8, 2, 16, 160
+    rng, gen, dt = np.random.RandomState(5), torch.Generator(device=DEV).manual_seed(6), torch.bfloat16
+    table, kv, starts, n_pages, copies = er.make_groups(rng, page, [4], [shared], [new + 40, new + 3, new, new + 100])
+    k, v = ref.make_pages(gen, n_pages, page, hkv, dt, False, DEV)
+    q = torch.randn(4 * new, hq, D, generator=gen, device=DEV).to(dt)
+    row_start = [new * i for i in range(5)]
+    pool = zc.PagedKV(k, v, hq, max_req=4, max_rows=4 * new, scored_rows=1)
+    start = torch.rand((n_pages, hkv, page), generator=gen, device=DEV)
+    got, want = start.clone(), start.clone()
+    pool.attention_scored(q, i32(table), i32(row_start), i32(kv), new, got)
+    pool.attention_scored(q, i32(table), i32(row_start), i32(kv), new, want, first=i32([shared] * 4))
+    settled(zc)
+    common = torch.zeros(n_pages, dtype=torch.bool, device=DEV)
+    common[torch.as_tensor(table[0, : shared // page], device=DEV).long()] = True
+    assert torch.equal(got[~common], want[~common]) and torch.equal(want[common], start[common])
+    more = (got - start)[common]
+    # (an old score and its sum are off by half a step each)
+    assert more.min() >= -2.0 ** -22 and more.max() <= new * hq // hkv * (1 + 2.0 ** -22)
+
+
+def test_own_tokens_of_a_group_that_shares_more_than_it_says(zc):
+    """said < what the tables share, with scores: outputs are right, and the scores of the slots that are one request's."""
+    hq, hkv, page = 8, 2, 16
+    rng, gen, dt = np.random.RandomState(8), torch.Generator(device=DEV).manual_seed(9), torch.float16
+    table, kv, starts, n_pages, copies = er.make_groups(rng, page, [8], [960], [30 + i for i in range(8)])
+    common = torch.as_tensor(table[0, :60], device=DEV).long()
+    table = wide(table, page, hkv, 1)
+    k, v = ref.make_pages(gen, n_pages, page, hkv, dt, False, DEV)
+    q = torch.randn(8, hq, D, generator=gen, device=DEV).to(dt)
+    pool = zc.PagedKV(k, v, hq, max_req=8, max_rows=8, shared=True, scored_rows=1)
+    start = torch.rand((n_pages, hkv, page), generator=gen, device=DEV)
+    got = start.clone()
+    out, lse = pool.attention_shared(q, i32(table), i32(range(9)), i32(kv), 1, i32(starts), i32([800]), scores=got)
+    settled(zc)
+    want, tol = er.add_weights(start, q, k, table, list(range(9)), kv, [960] * 8, 0, 0)
+    alone = torch.ones(n_pages, dtype=torch.bool, device=DEV)
+    alone[common] = False
+    assert ((got.double() - want).abs() <= tol)[alone].all()
+    assert torch.equal(got[common[:50]], start[common[:50]])             # what the call was told is shared has no score
+    more = (got - start)[common[50:]]
+    assert more.min() >= -2.0 ** -22 and more.max() <= hq // hkv * (1 + 2.0 ** -22)
