@@ -151,7 +151,9 @@ constexpr int kKeysLog2 = 8;
 constexpr int kKBufs = 2, kQBufs = 2, kLBufs = 4, kRing = 2;
 constexpr int kTiles = (2 * kKBufs + kQBufs) * kTile;  // 192 KB
 constexpr int kRowsBytes = kLBufs * (kM * 8 + 4);      // minus the log-sum-exp, position; mild
-// Up to here a logit's rounding makes no weight more than 2^0.07; beyond, weights are held to 1.
+// The logits are the attention kernel's bit for bit, whatever their terms' sizes (the same products in the same order, with
+// keys and rows in each other's place), so that a weight passes 1 by the log-sum-exp's rounding alone, 2^-24 of it: up to
+// here by 2^0.07 at most.  Beyond, weights are held to 1.
 constexpr float kMild = 1048576.f;
 constexpr int kItemInts = 16;
 constexpr int kPartBytes = 2 * kKeys * 4;              // sums of the second halves of the columns, of two items

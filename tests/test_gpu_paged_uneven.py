@@ -218,6 +218,33 @@ def test_shared_weights_of_rows_that_are_not_numbers(zc):
     assert torch.isnan(got[1][bad]).all() and torch.equal(got[0][~bad], got[1][~bad])
 
 
+@pytest.mark.parametrize("dtype,sizes", [("bf16", [0, 6, 10, 12, 14, 16, 20, 26, 40]), ("fp16", [0, 6, 10, 12, 13])])
+@pytest.mark.parametrize("hq,hkv,new", [(8, 2, 300), (5, 1, 70), (4, 4, 129)])
+def test_weights_of_logits_whose_terms_cancel(zc, dtype, sizes, hq, hkv, new):
+    """Terms of up to 2^80 whose sums are small or rounding alone: under a window of one key every weight is 1, off by the
+    log-sum-exp's rounding (2^-24 of it, a 20th where that is held to 1) and 2^-18; with two keys a row's sum to it."""
+    dt, page, G = TYPES[dtype], 64, hq // hkv
+    for size in sizes:
+        gen = torch.Generator(device=DEV).manual_seed(7)
+        table, n_pages = ref.make_table(np.random.RandomState(7), [new], page)
+        k, v = ref.make_pages(gen, n_pages, page, hkv, dt, False, DEV)
+        q = torch.randn((new, hq, D), generator=gen, device=DEV).to(dt)
+        k[..., 3:64] = (torch.randn((n_pages, page, hkv, 61), generator=gen, device=DEV) * 2.0 ** size).to(dt)
+        q[..., 3:64] = (torch.randn((new, hq, 61), generator=gen, device=DEV) * 2.0 ** size).to(dt)
+        k[..., 67:], q[..., 67:] = -k[..., 3:64], q[..., 3:64]
+        pool = zc.PagedKV(k, v, hq, max_req=1, max_rows=new)
+        for window in (1, 2):
+            scores = torch.zeros((n_pages, hkv, page), device=DEV)
+            out, lse = pool.attention_scored(q, i32(table), i32([0, new]), i32([new]), new, scores, window=window)
+            settled(zc)
+            mine = scores[torch.as_tensor(table[0], device=DEV).long()].transpose(1, 2).reshape(-1, hkv)[:new].double()
+            assert torch.isfinite(mine).all() and mine.min() >= 0
+            off = 2.0 ** (min(lse.abs().max().item(), 2.0 ** 20) * 2.0 ** -24) - 1 + 2.0 ** -18
+            assert mine.max() <= window * G * (1 + off)
+            if window == 1 and lse.abs().max() < 2.0 ** 20:
+                assert mine.min() >= G * (1 - off)
+
+
 # ---------------------------------------------------------------- pages that are none
 def freed(table, n_pages, page, kv_len, lens, free, state):
     """The free list after the pages behind the kept tokens are put back, and its state; entries that are no page are not."""
