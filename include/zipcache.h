@@ -436,9 +436,9 @@ int zc_page_select(zc_pages* p, const int32_t* table, int table_width, const int
  * its own, but those whose tokens all stay where they are (pages of a shared beginning that first[r] covers).
  * The pages behind the kept tokens, request by request, are put back in front of the free ones, where zc_page_tables
  * took them from: free_pages [device] n_free, free_state, free_out [device] 3 as there: free_out = {next - pages, end,
- * pages that found no room in front of next: 0 where all came from this list}.  Entries outside [0, n_pages) are none (a step
- * whose pages ran out leaves them) and are not put back.  All three NULL: none.  The table is
- * left as it is; its entries behind the kept tokens' pages mean nothing any more.  Outputs may not overlap inputs. */
+ * pages that found no room in front of next: 0 where all came from this list}.  Entries outside [0, n_pages) are no pages
+ * (a step that ran out of them leaves such) and are not put back.  All three NULL: none.  n_req = 0 is a no-op: free_out is
+ * not written.  The table is left as it is; its entries behind the kept tokens' pages mean nothing any more.  Outputs may not overlap inputs. */
 int zc_page_compact(zc_pages* p, const int32_t* table, int table_width, const int32_t* kv_len, int n_req,
                     const int32_t* kept, int max_keep, const int32_t* kept_len, float* scores, int32_t* free_pages,
                     int n_free, const int32_t* free_state, int32_t* free_out, zc_stream_t stream);

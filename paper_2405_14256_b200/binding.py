@@ -838,12 +838,18 @@ class PagedKV(_Buffers):
             at_out = _at_i32(free_out, "free_out", 3, index)
         elif free_state is not None or free_out is not None:
             raise ZipCacheError("free_state and free_out come with free_pages")
+        raw = _stream_of(index, stream)
+        if n_req == 0 and at_out:        # (nothing for the library to do)
+            with torch.cuda.stream(_stream_object(index, raw)):
+                torch.clamp(free_state, max=n_free, out=free_out)
+                free_out[:1].clamp_(min=0)
+                free_out[2:].zero_()
         _check(self._lib.zc_page_compact(self.handle, _at_i32(table, "table", n_req * width, index), width,
                                          _at_i32(kv_len, "kv_len", n_req, index), n_req,
                                          _at_i32(kept, "kept", n_req * self.n_kv_heads * max_keep, index), max_keep,
                                          _at_i32(kept_len, "kept_len", n_req, index),
                                          0 if scores is None else self._at_scores(scores), at_free, n_free, at_state, at_out,
-                                         _stream_of(index, stream)), "zc_page_compact")
+                                         raw), "zc_page_compact")
         return free_out
 
 

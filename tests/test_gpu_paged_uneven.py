@@ -402,3 +402,18 @@ def test_own_tokens_of_a_group_that_shares_more_than_it_says(zc):
     assert torch.equal(got[common[:50]], start[common[:50]])             # what the call was told is shared has no score
     more = (got - start)[common[50:]]
     assert more.min() >= -2.0 ** -22 and more.max() <= hq // hkv * (1 + 2.0 ** -22)
+
+
+def test_compaction_of_no_requests_says_the_free_list_s_state(zc):
+    k = torch.zeros((4, 16, 2, D), dtype=torch.float16, device=DEV)
+    pool = zc.PagedKV(k, k, 2, max_req=0, max_rows=0)
+    none, table = i32([]), torch.zeros((0, 5), dtype=torch.int32, device=DEV)
+    kept = torch.zeros((0, 2, 8), dtype=torch.int32, device=DEV)
+    side = torch.cuda.Stream()
+    for given, state, want in ((None, [2, 4, 7], [2, 4, 0]), (i32([9, 9, 9]), [-3, 9, 1], [0, 4, 0]), (None, [6, 4, 0], [4, 4, 0])):
+        torch.full((3,), 77, dtype=torch.int32, device=DEV)          # (freed: what an unwritten result would hold)
+        for stream in (None, side):
+            out = pool.compact(table, none, kept, none, None, i32([0, 1, 2, 3]), i32(state), given, stream=stream)
+            settled(zc)
+            assert out.tolist() == want and (given is None or out is given)
+    assert pool.compact(table, none, kept, none) is None
