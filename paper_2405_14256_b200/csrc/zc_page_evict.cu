@@ -325,7 +325,7 @@ template <int PARTS>
 __global__ void __launch_bounds__(kMoveThreads, 2) k_page_compact(const CompactArgs a) {
   constexpr int kLanes = 16 / PARTS, kAtOnce = kMoveThreads / kLanes;   // threads to a row's part, rows to a step
   constexpr int kRows = kMoveSteps * kAtOnce;                           // of a round
-  extern __shared__ char s_move[];                                      // [stage][step][thread] 16 bytes
+  extern __shared__ __align__(16) char s_move[];                        // [stage][step][thread] 16 bytes
   uint64_t* s_from = reinterpret_cast<uint64_t*>(s_move + kMoveStages * kMoveStage);
   uint64_t* s_to = s_from + kMoveSeg;
   const int work = 2 * PARTS * a.n_req * a.h_kv;
