@@ -1288,11 +1288,16 @@ int zc_launch_paged_shared(zc_pages* p, const ZcPagedArgs& a, const int32_t* gro
   memset(&qmap, 0, sizeof(qmap));
   if (!make_q_map(&qmap, a.q, p->cfg.dtype, a.h_q, a.G, a.n_rows, 1, a.qs_head, a.qs_row, 0))
     return (int)cudaErrorNotSupported;
-  const cudaError_t e = p->cfg.dtype == ZC_F16 ? launch_groups<__half>(p, k, qmap, st)
-                                               : launch_groups<__nv_bfloat16>(p, k, qmap, st);
-  if (e != cudaSuccess) return (int)e;
+  // The first kernel sets gr.told, the joining one clears it: what can fail without a launch does so before the first, and
+  // where a launch behind it fails, the word is cleared all the same (left set, it would mislead the next call's kernels).
+  int e = zc_launch_own_keys(p, a, k.gr, k.tpt, logits, false, st);
+  if (e != cudaSuccess) return e;
+  e = p->cfg.dtype == ZC_F16 ? launch_groups<__half>(p, k, qmap, st) : launch_groups<__nv_bfloat16>(p, k, qmap, st);
+  if (e != cudaSuccess) return e;
   p->launches += 1;
-  return zc_launch_own_keys(p, a, k.gr, k.tpt, logits, st);
+  e = zc_launch_own_keys(p, a, k.gr, k.tpt, logits, true, st);
+  if (e != cudaSuccess) cudaMemsetAsync(k.gr.told, 0, sizeof(int), st);
+  return e;
 }
 
 size_t zc_paged_chunk_workspace() { return carve(nullptr, nullptr); }

@@ -441,22 +441,23 @@ template <typename T> cudaError_t launch_join_rows(const JoinArgs& j, cudaStream
 }
 
 template <typename T, int NT, bool WEIGHTS>
-cudaError_t launch(zc_pages* p, const OwnArgs& k, cudaStream_t st) {
+cudaError_t launch(zc_pages* p, const OwnArgs& k, bool go, cudaStream_t st) {
   static std::atomic<unsigned long long> allowed{0};
   const cudaError_t e = zc_allow_smem(k_own_keys<T, NT, WEIGHTS>, kOwnSmem, &allowed);
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess || !go) return e;
   return zc_launch_early(k_own_keys<T, NT, WEIGHTS>, dim3(2 * k.n_sm), dim3(kThreads), kOwnSmem, st, k, p->k16, p->v16);
 }
-template <typename T, int NT> cudaError_t launch_mode(zc_pages* p, const OwnArgs& k, cudaStream_t st) {
-  return k.logits ? launch<T, NT, true>(p, k, st) : launch<T, NT, false>(p, k, st);
+template <typename T, int NT> cudaError_t launch_mode(zc_pages* p, const OwnArgs& k, bool go, cudaStream_t st) {
+  return k.logits ? launch<T, NT, true>(p, k, go, st) : launch<T, NT, false>(p, k, go, st);
 }
-template <typename T> cudaError_t launch_rows(zc_pages* p, const OwnArgs& k, cudaStream_t st) {
-  return k.a.max_rows * k.a.G <= 8 ? launch_mode<T, 1>(p, k, st) : launch_mode<T, 2>(p, k, st);
+template <typename T> cudaError_t launch_rows(zc_pages* p, const OwnArgs& k, bool go, cudaStream_t st) {
+  return k.a.max_rows * k.a.G <= 8 ? launch_mode<T, 1>(p, k, go, st) : launch_mode<T, 2>(p, k, go, st);
 }
 
 }  // namespace
 
-int zc_launch_own_keys(zc_pages* p, const ZcPagedArgs& a, const ZcGroups& gr, int tpt, float* logits, cudaStream_t st) {
+int zc_launch_own_keys(zc_pages* p, const ZcPagedArgs& a, const ZcGroups& gr, int tpt, float* logits, bool go,
+                       cudaStream_t st) {
   OwnArgs k;
   memset(&k, 0, sizeof(k));
   k.a = a;
@@ -465,8 +466,8 @@ int zc_launch_own_keys(zc_pages* p, const ZcPagedArgs& a, const ZcGroups& gr, in
   k.n_sm = p->n_sm;
   k.logits = logits;
   const bool half = p->cfg.dtype == ZC_F16;
-  cudaError_t e = half ? launch_rows<__half>(p, k, st) : launch_rows<__nv_bfloat16>(p, k, st);
-  if (e != cudaSuccess) return (int)e;
+  cudaError_t e = half ? launch_rows<__half>(p, k, go, st) : launch_rows<__nv_bfloat16>(p, k, go, st);
+  if (e != cudaSuccess || !go) return (int)e;
   p->launches += 1;
   JoinArgs j;
   memset(&j, 0, sizeof(j));

@@ -99,7 +99,8 @@ int zc_launch_paged_chunk(zc_pages* p, const ZcPagedArgs& a, char* ws, cudaStrea
 size_t zc_paged_shared_workspace(const zc_page_config& c, int n_req, int n_rows);
 int zc_launch_paged_shared(zc_pages* p, const ZcPagedArgs& a, const int32_t* group_start, const int32_t* shared_len,
                            int n_groups, float* logits, char* ws, cudaStream_t st);
-int zc_launch_own_keys(zc_pages* p, const ZcPagedArgs& a, const ZcGroups& gr, int tpt, float* logits, cudaStream_t st);
+// go: false only asks for the shared memory that the launch needs.
+int zc_launch_own_keys(zc_pages* p, const ZcPagedArgs& a, const ZcGroups& gr, int tpt, float* logits, bool go, cudaStream_t st);
 // group_start, shared_len, n_groups: tokens before a group's shared_len have no score; else first (may be null) says so.
 int zc_launch_score_add(zc_pages* p, const ZcPagedArgs& a, const float* logits, float* scores, const int32_t* first,
                         const int32_t* group_start, const int32_t* shared_len, int n_groups, cudaStream_t st);
