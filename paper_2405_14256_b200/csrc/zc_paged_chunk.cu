@@ -153,12 +153,13 @@ struct Share {
   int items;          // of a head
   int r, in_req;      // the begin's request, and the item's number in it
   Chunk c;            // that request's (or group's) rows
+  int lead;           // groups: the request through whose table
 };
 // What is found for all threads: the borders, and the item that the first of them lies in.
 struct Found {
   Border border[2];
   long long start, all;   // the item's cost before it, and the cost of everything
-  int nt, width, r, in_req, kv;
+  int nt, width, r, in_req, kv;   // (groups: kv is the first item's lead)
   Chunk c;
 };
 static_assert(sizeof(Found) <= 64, "it fits between the barriers and the sums");
@@ -279,6 +280,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
         f.in_req = next - s_start[f.r];
       }
       if (tid == 0) {
+        if (FORM == kGroups) f.kv = gt.lead[f.r];
         f.c.n = s_n[f.r];
         f.c.p0 = s_p0[f.r];
         f.c.row0 = FORM == kGroups ? gt.row[f.r] : load_chunk(a, f.r).row0;
@@ -305,6 +307,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
   s.r = s_found->r;
   s.in_req = s_found->in_req;
   s.c = s_found->c;
+  s.lead = s_found->kv;
   if (tid == kThreads - 1) {
     // (a thread that has nothing to do yet) what k_chunk_join is to know of the border before this CTA
     const Found f = *s_found;
@@ -327,7 +330,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& k, char* scratch, l
           j.n = q.n;
         }
         j.tok0 = f.in_req * tpi;
-        j.kv = f.kv;
+        j.kv = f.kv;   // (k_chunk_join's, which groups do without)
       }
     }
     k.ws.joins[c] = j;
@@ -617,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       long long idx = blockIdx.x, round = 0;
       bool back = false;
       Border at = share.begin;
-      int r = share.r, in_req = share.in_req;
+      int r = share.r, in_req = share.in_req, lead = share.lead;
       Chunk c;
       c.row0 = c.n = c.p0 = 0;
       auto load = [&](int i) { return FORM == kGroups ? load_group(k, i) : load_chunk(a, i); };
@@ -636,7 +639,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (at.item > share.end.item || (at.item == share.end.item && at.t >= share.end.t)) return;
         // (only the share's first item can begin, and only its last can end, inside)
-        it.r = FORM == kGroups ? k.gr.lead[r] : r;   // whose table has the item's pages
+        it.r = FORM == kGroups ? lead : r;   // whose table has the item's pages
         it.kv = at.item / share.items;
         it.tok0 = in_req * 2 * k.tpt;
         it.row0 = c.row0;
@@ -664,6 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (some) {
               const int src = __ffs(some) - 1;
               r = r0 + src;
+              if (FORM == kGroups) lead = k.gr.lead[r];
               c.row0 = __shfl_sync(0xffffffffu, x.row0, src);
               c.n = __shfl_sync(0xffffffffu, x.n, src);
               c.p0 = __shfl_sync(0xffffffffu, x.p0, src);

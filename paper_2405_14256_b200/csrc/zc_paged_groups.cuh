@@ -53,6 +53,18 @@ struct GroupTables {
     }
     return lo;
   }
+  // The first of a group's requests that has rows (a third atomic beside the minimum and the count would take 1.6 us): the
+  // last one that begins where the group's rows do.
+  __device__ __forceinline__ int lead_of(const ZcPagedArgs& a, int g) const {
+    auto row_of = [&](int r) { return held ? first[r] : min(max(a.row_start[r], 0), a.n_rows); };
+    int lo = border[g], hi = border[g + 1];
+    if (row_of(lo + 1) > row[g]) return lo;
+    while (hi - lo > 1) {
+      const int m = (lo + hi) >> 1;
+      if (row_of(m) <= row[g]) lo = m; else hi = m;
+    }
+    return lo;
+  }
   __device__ __forceinline__ int keys_of(int r) const {
     const int g = group_of(r);
     return g < 0 ? 0 : keys[g];
@@ -93,7 +105,6 @@ __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups&
     if (g < n) {
       t.keys[g] = (int)min((long long)max(gr.shared[g], 0), cap);
       t.count[g] = 0;
-      t.lead[g] = 0x7fffffff;
     }
   }
   if (t.held)
@@ -115,16 +126,14 @@ __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups&
     const int top = __reduce_max_sync(0xffffffffu, g);
     if (__all_sync(0xffffffffu, g == top || g < 0)) {
       const int least = __reduce_min_sync(0xffffffffu, g < 0 ? 0x7fffffff : c.p0);
-      const unsigned have = __ballot_sync(0xffffffffu, g >= 0);
+      const int count = __popc(__ballot_sync(0xffffffffu, g >= 0));
       if (top >= 0 && (tid & 31) == 0) {
         atomicMin(&t.keys[top], least);
-        atomicAdd(&t.count[top], __popc(have));
-        atomicMin(&t.lead[top], r + __ffs(have) - 1);
+        atomicAdd(&t.count[top], count);
       }
     } else if (g >= 0) {
       atomicMin(&t.keys[g], c.p0);
       atomicAdd(&t.count[g], 1);
-      atomicMin(&t.lead[g], r);
     }
   }
   __syncthreads();
@@ -135,6 +144,7 @@ __device__ __forceinline__ int plan_groups(const ZcPagedArgs& a, const ZcGroups&
     const bool on = rows > 0 && n_cta > 1 && mine >= kWorthSharing;
     t.keys[g] = on ? keys : 0;
     if (!on) continue;
+    t.lead[g] = t.lead_of(a, g);
     spared += mine;
     const int tiles = (keys + kShareTile - 1) / kShareTile, whole = rows / tpi, rest = rows - whole * tpi;
     cost += (long long)whole * (tiles * kWideTile + kItemCost);
