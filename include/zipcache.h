@@ -378,7 +378,11 @@ int zc_paged_attention(zc_pages* p, const void* q, const int64_t q_strides[2], c
  *   group), and logits likewise.
  *   workspace: of zc_pages_shared_workspace for the call's n_req and n_rows (or more), zeroed in front as zc_pages_workspace
  *   says, whose calls it serves as well.
- * Results are zc_paged_attention's up to rounding: the order in which keys are added up is another one. */
+ * Results are zc_paged_attention's up to rounding: keys are added up in another order, and the weights of keys that are
+ * read once for a group are rounded to the input type (by 2^-8 of them at most in bf16, 2^-11 in fp16), as a chunk's are,
+ * where zc_paged_attention holds those of so few rows in two parts.  So an output is off by as much of the weighted mean of
+ * |v| more, in calls and groups that are large enough to be worth it (by the table's width, the lengths and the number of
+ * requests), and in none that is attended like any. */
 int zc_paged_attention_shared(zc_pages* p, const void* q, const int64_t q_strides[2], const int32_t* table,
                               int table_width, const int32_t* row_start, const int32_t* kv_len, int n_req, int n_rows,
                               int max_rows, const int32_t* group_start, const int32_t* shared_len, int n_groups,

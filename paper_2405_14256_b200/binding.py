@@ -574,7 +574,7 @@ class PagedKV(_Buffers):
     attention calls of up to max_req requests and max_rows rows: 43 MB whatever they are, so handles whose
     calls follow one another on a stream (the layers of a model) best share one: pass the first one's
     .workspace.  One made by the caller must have its first ZC_PAGES_SYNC_BYTES zeroed once.  With max_req or
-    max_rows 0 and none given there is no workspace, and the handle is for write and read alone.  A handle's calls
+    max_rows 0 and none given there is no workspace, and the handle is for all but attention: write, read, select, compact.  A handle's calls
     may run on any stream (the constructor waits for the current one's work), attention calls that share a workspace
     on one at a time.  Tensors that a call allocates may be used on the current stream, behind what orders it after
     `stream`.

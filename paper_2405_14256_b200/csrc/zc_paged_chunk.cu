@@ -425,7 +425,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 // The weights of 64 keys, 2^(v * scale - m), packed to the input type; returns their sum (of the unrounded
-// values).  All exponentials go through the exp2 unit: a quarter of them by a polynomial on the FMA pipe
+// values).  Rounded once, also in a group's item, whose rows would have two parts as single tokens: with the rest as a second
+// part (twice the products of O) the error against 64 bits is the output's own, bf16 0.0017 of its norm instead of 0.0023, and
+// the calls take 13 to 18 % longer (64 requests on 8192: 42 -> 49 us, 128 on 30000: 93 -> 107).
+// All exponentials go through the exp2 unit: a quarter of them by a polynomial on the FMA pipe
 // instead measured the same to 7 % slower.
 template <typename T> __device__ __forceinline__ float weights(const float* v, float scale, float m, uint32_t* w) {
   const float2 sc = make_float2(scale, scale), neg_m = make_float2(-m, -m);
