@@ -404,6 +404,27 @@ def test_own_tokens_of_a_group_that_shares_more_than_it_says(zc):
     assert more.min() >= -2.0 ** -22 and more.max() <= hq // hkv * (1 + 2.0 ** -22)
 
 
+@pytest.mark.parametrize("per", range(1, 17))
+def test_every_number_of_logits_to_a_key(zc, per):
+    """Query heads of a KV head times rows, all that single tokens' kernels take."""
+    hkv, page = 2, 16
+    for G in (g for g in range(1, per + 1) if per % g == 0):
+        most, gen, dt = per // G, torch.Generator(device=DEV).manual_seed(per), torch.float16
+        new = [most, 1, max(1, most - 1)]
+        kv = [n + p for n, p in zip(new, (70, 0, 301))]
+        table, n_pages = ref.make_table(np.random.RandomState(per), kv, page)
+        k, v = ref.make_pages(gen, n_pages, page, hkv, dt, False, DEV)
+        row_start = [0] + np.cumsum(new).tolist()
+        q = torch.randn(row_start[-1], hkv * G, D, generator=gen, device=DEV).to(dt)
+        pool = zc.PagedKV(k, v, hkv * G, max_req=3, max_rows=row_start[-1], scored_rows=most)
+        start = torch.rand((n_pages, hkv, page), generator=gen, device=DEV)
+        got = start.clone()
+        pool.attention_scored(q, i32(table), i32(row_start), i32(kv), most, got, first=i32([3, 0, 0]))
+        settled(zc)
+        want, tol = er.add_weights(start, q, k, table, row_start, kv, [3, 0, 0], 0, 0)
+        assert ((got.double() - want).abs() <= tol).all()
+
+
 def test_compaction_of_no_requests_says_the_free_list_s_state(zc):
     k = torch.zeros((4, 16, 2, D), dtype=torch.float16, device=DEV)
     pool = zc.PagedKV(k, k, 2, max_req=0, max_rows=0)
