@@ -478,7 +478,7 @@ int zc_paged_attention_shared(zc_pages* p, const void* q, const int64_t q_stride
   float* kept = scores ? (float*)logits : nullptr;
   int e;
   // What sharing can save at most, by the table's width, against what its kernels take beside their keys: about 15 us, in
-  // which 90 MB are read (8 requests behind 1000 tokens, 8 KV heads: 22 us shared, 14 as any).
+  // which 90 MB are read (8 requests behind 1000 tokens, 8 KV heads: 24 us shared, 14 as any).
   const int spare = n_req - (n_groups < n_req ? n_groups : n_req);
   const double saved = (double)spare * ((long long)table_width << p->page_log2) * p->cfg.n_kv_heads * (4.0 * ZC_D);
   if (n_groups > 0 && saved > 90e6) {
