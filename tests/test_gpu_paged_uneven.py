@@ -260,7 +260,8 @@ def freed(table, n_pages, page, kv_len, lens, free, state):
 @pytest.mark.parametrize("page,lengths,lens,room", [
     (16, [300, 17, 0, 40, 500], [128, 17, 0, 16, 0], 30), (64, [5000, 700], [1, 640], 200), (16, [160] * 300, [16] * 300, 3000),
     (16, [160] * 300, [16 * (i % 11) for i in range(300)], 700), (256, [4000], [0], 5), (16, [30000], [9000], 2000),
-    (16, [20, 9000, 33], [4, 0, 0], 600)])
+    (16, [20, 9000, 33], [4, 0, 0], 600), (16, [40] * 5000, [16 * (i % 3) for i in range(5000)], 9000),
+    (16, [100000, 70], [16, 0], 7000)])
 @pytest.mark.parametrize("holes", [0.0, 0.3, 1.0])
 def test_only_pages_are_given_back(zc, page, lengths, lens, room, holes):
     rng, gen = np.random.RandomState(len(lengths)), torch.Generator(device=DEV).manual_seed(1)
