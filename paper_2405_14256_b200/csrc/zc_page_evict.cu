@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) k_page_select(const S
 // are the halves or quarters of the channels, which need not wait for one another either.  The places of 2048 rows are found
 // at once: found round by round, two dependent reads each, they held the rows up (16 requests of 5000-8192 tokens to 2048,
 // 8 KV heads: 76 us, whether the rows lay scattered or side by side).
-// Bound: HBM (a row that moves is read once and written once): 16 requests of 5000-8192 tokens to 2048, 8 KV heads, 54 us, 76 %.
+// Bound: HBM (a row that moves is read once and written once): 16 requests of 5000-8192 tokens to 2048, 8 KV heads, 52 us, 79 %.
 constexpr int kMoveThreads = 256, kMoveStages = 4, kMoveSteps = 4;
 constexpr int kMoveStage = kMoveSteps * kMoveThreads * 16;   // bytes of a round
 constexpr int kMoveSeg = 2048;                               // rows whose places are known
