@@ -369,8 +369,9 @@ int zc_paged_attention(zc_pages* p, const void* q, const int64_t q_strides[2], c
  * group_start[g] .. group_start[g + 1] - 1, the first shared_len[g] tokens of which are the same ones (a system prompt, a
  * document): their tables list the same pages for them, or copies of the same rows where a page is not filled by them.
  * Those keys and values are read once for all rows of the group, through the table of the first of its requests that has
- * rows in the call, instead of once per request (tables of requests without rows may hold anything).  group_start [device] n_groups + 1 ascending, shared_len [device] n_groups; requests in no group, and
- * groups too short to be worth it (down to groups of one), are attended like any.  At most 1024 groups (ZC_ECAPACITY).
+ * rows in the call, instead of once per request (tables of requests without rows may hold anything).
+ * group_start [device] n_groups + 1 ascending, shared_len [device] n_groups; requests in no group, and groups too short to
+ * be worth it (down to groups of one), are attended like any.  At most 1024 groups (ZC_ECAPACITY).
  * Of a group's shared tokens those count that lie before every new row of its requests.
  *   max_rows * G must be at most 16 (ZC_EINVAL): generated tokens, one or a few per request; a chunk reads each
  *   key once for 128 / G of its tokens as it is, and is zc_paged_attention's.
@@ -442,7 +443,8 @@ int zc_page_select(zc_pages* p, const int32_t* table, int table_width, const int
  * took them from: free_pages [device] n_free, free_state, free_out [device] 3 as there: free_out = {next - pages, end,
  * pages that found no room in front of next: 0 where all came from this list}.  Entries outside [0, n_pages) are no pages
  * (a step that ran out of them leaves such) and are not put back.  All three NULL: none.  n_req = 0 is a no-op: free_out is
- * not written.  The table is left as it is; its entries behind the kept tokens' pages mean nothing any more.  Outputs may not overlap inputs. */
+ * not written.  The table is left as it is; its entries behind the kept tokens' pages mean nothing any more.  Outputs may
+ * not overlap inputs. */
 int zc_page_compact(zc_pages* p, const int32_t* table, int table_width, const int32_t* kv_len, int n_req,
                     const int32_t* kept, int max_keep, const int32_t* kept_len, float* scores, int32_t* free_pages,
                     int n_free, const int32_t* free_state, int32_t* free_out, zc_stream_t stream);
